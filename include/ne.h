@@ -311,6 +311,125 @@ ne_status ne_score_pairs(const ne_tables* tables, const int32_t* pairs_dev, int6
                          int32_t second_from_context, float* scores_dev, void* hip_stream);
 
 /*
+ * Full-softmax training: the objective that negative sampling approximates, the operators that a step of it
+ * takes (lookup of rows, softmax cross entropy against a whole table, the gradients of both, AdamW), each usable
+ * by itself.  They take plain pointers and no tables handle.  Matrices are row-major with contiguous rows and a
+ * row stride in elements; a type argument is an ne_dtype.  Sums are held in fp32 and every output is rounded
+ * once.  All calls only enqueue kernels (no copies, no fills of other kinds), so they can be captured into a HIP
+ * graph.  Unless it says otherwise a workspace is scratch of the caller: 256-byte aligned, overwritten, it needs
+ * no initialisation and carries nothing between calls, and calls that overlap in time need one each.
+ */
+typedef enum { NE_F32 = 0, NE_BF16 = 1 } ne_dtype;
+enum { NE_OP_MAX_DIM = 16384, NE_EMBED_MAX_IDS = 1 << 26 };
+
+/*
+ * Rows of a table, scaled:  out[i] = scale * table[ids[i]].  An id outside [0, num_rows) names no row (walks are
+ * padded with -1): its output is a row of zeros.
+ *   table_dev : device, table_type [num_rows][dim], row stride table_stride >= dim; aligned to its elements.
+ *   ids_dev   : device, int32[n].
+ *   out_dev   : device, out_type [n][dim], row stride out_stride >= dim; must not overlap the table.
+ *   1 <= dim <= NE_OP_MAX_DIM, 0 < num_rows < 2^31, 0 <= n <= NE_EMBED_MAX_IDS; n == 0 is a no-op.  scale finite.
+ * Errors: NE_ERR_ARG, NE_ERR_HIP.
+ */
+ne_status ne_embed_lookup(const void* table_dev, int32_t table_type, int64_t table_stride, int64_t num_rows, int32_t dim,
+                          const int32_t* ids_dev, int64_t n, float scale, void* out_dev, int32_t out_type,
+                          int64_t out_stride, void* hip_stream);
+
+/*
+ * The lookup's gradient:  T[r] = (accumulate ? T[r] : 0) + scale * sum over i with ids[i] == r of grad[i].
+ * The ids are sorted (stably, so that a row's terms are added in an order that only the ids decide) and each row
+ * is written once: the result is the same bit for bit on every run.  Ids outside [0, num_rows) contribute nothing,
+ * whatever their gradient holds.  accumulate == 0 writes all num_rows rows; accumulate != 0 touches only rows that
+ * are named.
+ *   grad_dev       : device, grad_type [n][dim], row stride grad_stride >= dim, or 0 for one row that every
+ *                    position shares.
+ *   table_grad_dev : device, table_grad_type [num_rows][dim], row stride table_grad_stride >= dim; must not overlap grad.
+ *   workspace_dev  : at least ne_embed_workspace_bytes(num_rows, dim, n) bytes (0 there = invalid arguments or n == 0).
+ * n == 0 writes zeros, or nothing with accumulate.  Sizes and errors as for ne_embed_lookup.
+ */
+size_t ne_embed_workspace_bytes(int64_t num_rows, int32_t dim, int64_t n);
+ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev, int32_t grad_type, int64_t grad_stride,
+                        float scale, int64_t num_rows, int32_t dim, void* table_grad_dev, int32_t table_grad_type,
+                        int64_t table_grad_stride, int32_t accumulate, void* workspace_dev, size_t workspace_bytes,
+                        void* hip_stream);
+
+/*
+ * Softmax cross entropy of n rows h_i against all rows w_v of a table, the scores s_iv = <h_i, w_v> taken in pieces
+ * of the table and never kept:
+ *   lse[i] = log sum_v exp(s_iv),   loss[i] = lse[i] - s_i,target[i].
+ * A target outside [0, num_rows) marks a row without a target: its loss and lse are 0 and it has no gradient,
+ * whatever its h holds.
+ *   h_dev, w_dev : device, type [n][dim] and [num_rows][dim], row strides >= dim, aligned to their elements.
+ *   targets_dev  : device, int32[n].
+ *   loss_dev, lse_dev : device, float[n].
+ *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 0) bytes.
+ * ne_xent_grad gives, for G_iv = scale * loss_grad[i] * (exp(s_iv - lse[i]) - [v == target[i]]),
+ *   dh = G . W  and  dw = G^T . H,
+ * written whole (rows without a target: dh 0).  Both have the type of h and w; one of them may be NULL.
+ *   lse_dev       : device, float[n], as ne_xent_loss wrote it for the same h, w and targets.
+ *   loss_grad_dev : device, float[n]: the gradient of what is minimised in loss[i]; NULL = 1 for every row.
+ *   scale         : finite; 1 / n for the mean over the rows.
+ *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
+ *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 1) bytes.
+ * Precision: NE_BF16: products of bf16 values with fp32 sums; G is formed in fp32 and rounded to bf16 for its
+ * products.  NE_F32: every operand is the sum of two halves in fp16 (22 bits, at a common power of two that the
+ * largest finite magnitude sets), three products of halves with fp32 sums: errors as those of fp32 products, for
+ * elements of at least 2^-24 of the largest magnitude of their matrix; what is smaller counts to 2^-39 of it.
+ * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN; in a row of w, all losses.
+ *   1 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for the loss and writes zeros
+ *   to dw.  Errors: NE_ERR_ARG, NE_ERR_HIP.
+ */
+size_t ne_xent_workspace_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int32_t grad);
+ne_status ne_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type,
+                       const int32_t* targets_dev, int64_t n, int64_t num_rows, int32_t dim, float* loss_dev,
+                       float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type,
+                       const int32_t* targets_dev, const float* lse_dev, const float* loss_grad_dev, float scale,
+                       int64_t n, int64_t num_rows, int32_t dim, void* dh_dev, int64_t dh_stride, void* dw_dev,
+                       int64_t dw_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * AdamW over many tensors at once.  Element by element, with g = grad_scale * grad and step t >= 1:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * Parameters are fp32.  state_bits 32: m and v are float[n].  state_bits 8: every 256 elements of a tensor share
+ * two scales (float, ceil(n / 256) each); m is 8-bit floating point (e4m3, no infinities) times m_scale, and v holds
+ * sqrt(v) in the same form times v_scale; a scale is 1/448 of the block's largest magnitude (of 2^-100 at least).
+ * Values are rounded at random, up with the probability that keeps their expectation (a step moves v by a
+ * thousandth, which rounding to nearest at 3 bits would lose every time); sqrt(v) > 0 never becomes 0.  The random
+ * bits of element e of tensor t: word e % 4 of Philox(key = seed, counter = (e / 4, t, step, 3)), its low 16 bits
+ * for m and its high 16 bits for v.
+ *   ne_adamw_tensor: n > 0 elements, n < 2^33; param float[n]; grad of grad_type; param_bf16 NULL or bf16[n], which
+ *   receives a rounded copy of the new parameters; m_scale and v_scale are only used with state_bits 8.  All are
+ *   device memory of the caller, aligned to their elements, that stays valid while the handle is used.
+ *   weight_decay >= 0, finite.  States that start from zero bytes (scales too) are those of a new run.
+ *   workspace_dev : at least ne_adamw_workspace_bytes(tensors_host, n_tensors) bytes, caller-owned, written here
+ *                   (the call returns after the copy) and read by every step until the handle is destroyed.
+ *   1 <= n_tensors <= 65536.  tensors_host is read during the call only.
+ * ne_adamw_step moves every tensor of the handle by one step in one launch.  step >= 1; lr, eps >= 0,
+ * beta1 and beta2 in [0, 1), grad_scale finite.  Errors: NE_ERR_ARG, NE_ERR_NOMEM, NE_ERR_HIP.
+ */
+typedef struct ne_adamw ne_adamw;
+typedef struct ne_adamw_tensor {
+    float* param;
+    const void* grad;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* param_bf16;
+    int64_t n;
+    float weight_decay;
+    int32_t grad_type;
+} ne_adamw_tensor;
+size_t ne_adamw_workspace_bytes(const ne_adamw_tensor* tensors_host, int64_t n_tensors);
+ne_status ne_create_adamw(ne_adamw** out, const ne_adamw_tensor* tensors_host, int64_t n_tensors, int32_t state_bits,
+                          uint64_t seed, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+ne_status ne_adamw_step(ne_adamw* opt, int64_t step, float lr, float beta1, float beta2, float eps, float grad_scale,
+                        void* hip_stream);
+void ne_destroy_adamw(ne_adamw* opt);
+
+/*
  * Former tuning of the exact step: how a row that several references of a batch name collected their
  * deltas (list_cap: -1 or 0..8) and how finely hash positions were swept (sweep_per_thread: 0, 2, 4 or 8).
  * Neither choice exists any more: such a row has a list of coefficients and rows, and nothing is swept.  The

@@ -23,10 +23,17 @@ NE_ERR_NOMEM = -4
 NE_MAX_DIM = 1024
 NE_MAX_NEGATIVES = 62
 NE_MAX_BATCH = 1 << 22
+NE_F32 = 0
+NE_BF16 = 1
+NE_OP_MAX_DIM = 16384
+NE_EMBED_MAX_IDS = 1 << 26
+NE_ADAMW_BLOCK = 256    # elements that share a scale with 8-bit states
 
 EXPORTS = (
     "ne_create_tables", "ne_build_neg_alias", "ne_workspace_bytes", "ne_train_batch", "ne_train_block", "ne_train_runs", "ne_train_block_pinned", "ne_train_walks",
     "ne_shared_workspace_bytes", "ne_train_batch_shared", "ne_train_batch_shared_static", "ne_train_batch_async", "ne_train_block_async", "ne_set_vertex_window", "ne_eval_loss",
+    "ne_embed_lookup", "ne_embed_workspace_bytes", "ne_embed_grad", "ne_xent_workspace_bytes", "ne_xent_loss", "ne_xent_grad",
+    "ne_adamw_workspace_bytes", "ne_create_adamw", "ne_adamw_step", "ne_destroy_adamw",
     "ne_score_pairs", "ne_set_tuning", "ne_validate_pairs", "ne_hash_position", "ne_profile_enable", "ne_profile_read", "ne_destroy_tables", "ne_destroy_alias", "ne_last_error",
 )
 
@@ -37,6 +44,13 @@ class NeRun(ctypes.Structure):
     """struct ne_run of include/ne.h."""
     _fields_ = [("alias", ctypes.c_void_p), ("pairs_dev", ctypes.c_void_p), ("n_pairs", ctypes.c_int64),
                 ("sample_base", ctypes.c_uint64), ("neg_out_dev", ctypes.c_void_p)]
+
+
+class NeAdamwTensor(ctypes.Structure):
+    """struct ne_adamw_tensor of include/ne.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("param_bf16", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("grad_type", ctypes.c_int32)]
 
 
 class NeError(RuntimeError):
@@ -92,6 +106,28 @@ def lib() -> ctypes.CDLL:
     L.ne_train_walks.restype = c.c_int
     L.ne_score_pairs.argtypes = [vp, vp, c.c_int64, c.c_int32, vp, vp]
     L.ne_score_pairs.restype = c.c_int
+    L.ne_embed_lookup.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int32, vp, c.c_int64, c.c_float, vp, c.c_int32, c.c_int64, vp]
+    L.ne_embed_lookup.restype = c.c_int
+    L.ne_embed_workspace_bytes.argtypes = [c.c_int64, c.c_int32, c.c_int64]
+    L.ne_embed_workspace_bytes.restype = c.c_size_t
+    L.ne_embed_grad.argtypes = [vp, c.c_int64, vp, c.c_int32, c.c_int64, c.c_float, c.c_int64, c.c_int32, vp, c.c_int32, c.c_int64,
+                                c.c_int32, vp, c.c_size_t, vp]
+    L.ne_embed_grad.restype = c.c_int
+    L.ne_xent_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int32, c.c_int32, c.c_int32]
+    L.ne_xent_workspace_bytes.restype = c.c_size_t
+    L.ne_xent_loss.argtypes = [vp, c.c_int64, vp, c.c_int64, c.c_int32, vp, c.c_int64, c.c_int64, c.c_int32, vp, vp, vp, c.c_size_t, vp]
+    L.ne_xent_loss.restype = c.c_int
+    L.ne_xent_grad.argtypes = [vp, c.c_int64, vp, c.c_int64, c.c_int32, vp, vp, vp, c.c_float, c.c_int64, c.c_int64, c.c_int32,
+                               vp, c.c_int64, vp, c.c_int64, vp, c.c_size_t, vp]
+    L.ne_xent_grad.restype = c.c_int
+    L.ne_adamw_workspace_bytes.argtypes = [c.POINTER(NeAdamwTensor), c.c_int64]
+    L.ne_adamw_workspace_bytes.restype = c.c_size_t
+    L.ne_create_adamw.argtypes = [c.POINTER(vp), c.POINTER(NeAdamwTensor), c.c_int64, c.c_int32, c.c_uint64, vp, c.c_size_t, vp]
+    L.ne_create_adamw.restype = c.c_int
+    L.ne_adamw_step.argtypes = [vp, c.c_int64, c.c_float, c.c_float, c.c_float, c.c_float, c.c_float, vp]
+    L.ne_adamw_step.restype = c.c_int
+    L.ne_destroy_adamw.argtypes = [vp]
+    L.ne_destroy_adamw.restype = None
     L.ne_set_tuning.argtypes = [vp, c.c_int32, c.c_int32]
     L.ne_set_tuning.restype = c.c_int
     L.ne_validate_pairs.argtypes = [vp, vp, c.c_int64, vp, vp]
@@ -129,6 +165,25 @@ def _dev_ptr(t, dtype, name: str) -> int:
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: need a contiguous CUDA tensor of {dtype}")
     return t.data_ptr()
+
+
+_TYPES = {torch.float32: NE_F32, torch.bfloat16: NE_BF16}
+
+
+def _matrix(t, name: str, broadcast: bool = False):
+    """(pointer, ne_dtype, row stride) of a CUDA matrix of float32 or bfloat16 with contiguous rows; broadcast: one row
+    that all rows share (row stride 0) will do as well."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES):
+        raise TypeError(f"{name}: need a CUDA matrix of torch.float32 or torch.bfloat16")
+    rows, dim = t.shape
+    row, col = t.stride()
+    if dim > 1 and col != 1:
+        raise TypeError(f"{name}: need contiguous rows")
+    if rows <= 1:
+        row = dim
+    elif row < dim and not (broadcast and row == 0):
+        raise TypeError(f"{name}: rows overlap")
+    return t.data_ptr(), _TYPES[t.dtype], row
 
 
 class Tables:
@@ -389,6 +444,170 @@ def ne_score_pairs(tables: Tables, pairs: torch.Tensor, scores: torch.Tensor, se
         raise ValueError("scores is shorter than pairs")
     _check(lib().ne_score_pairs(tables.handle, pp, int(pairs.shape[0]), 1 if second_from_context else 0, sp,
                                 _stream_ptr(stream)))
+
+
+def ne_embed_lookup(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None) -> None:
+    """out[i] = scale * table[ids[i]] (ids CUDA int32 [n]; an id outside the table gives a row of zeros); table and out
+    CUDA float32 or bfloat16 matrices with contiguous rows."""
+    tp, tt, ts = _matrix(table, "table")
+    op, ot, os_ = _matrix(out, "out")
+    ip = _dev_ptr(ids, torch.int32, "ids")
+    n = ids.numel()
+    if out.shape[0] != n or out.shape[1] != table.shape[1]:
+        raise TypeError("out must be [len(ids)][dim]")
+    _check(lib().ne_embed_lookup(tp, tt, ts, table.shape[0], table.shape[1], ip, n, scale, op, ot, os_, _stream_ptr(stream)))
+
+
+def ne_embed_workspace_bytes(num_rows: int, dim: int, n: int) -> int:
+    return int(lib().ne_embed_workspace_bytes(num_rows, dim, n))
+
+
+def ne_embed_grad(ids: torch.Tensor, grad: torch.Tensor, table_grad: torch.Tensor, workspace: torch.Tensor | None,
+                  scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """table_grad[r] = (table_grad[r] if accumulate else 0) + scale * sum of grad[i] over ids[i] == r.  grad: [n][dim], or one
+    row expanded over the positions; workspace: CUDA uint8 of ne_embed_workspace_bytes(num_rows, dim, n) bytes."""
+    gp, gt, gs = _matrix(grad, "grad", broadcast=True)
+    tp, tt, ts = _matrix(table_grad, "table_grad")
+    ip = _dev_ptr(ids, torch.int32, "ids")
+    wp = _dev_ptr(workspace, torch.uint8, "workspace")
+    n = ids.numel()
+    if grad.shape[0] != n or grad.shape[1] != table_grad.shape[1]:
+        raise TypeError("grad must be [len(ids)][dim]")
+    _check(lib().ne_embed_grad(ip, n, gp, gt, gs, scale, table_grad.shape[0], table_grad.shape[1], tp, tt, ts,
+                               1 if accumulate else 0, wp, workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+
+
+def ne_xent_workspace_bytes(n: int, num_rows: int, dim: int, dtype: torch.dtype, grad: bool) -> int:
+    if dtype not in _TYPES:
+        raise TypeError("dtype must be torch.float32 or torch.bfloat16")
+    return int(lib().ne_xent_workspace_bytes(n, num_rows, dim, _TYPES[dtype], 1 if grad else 0))
+
+
+def _xent_operands(h, w, targets):
+    hp, ht, hs = _matrix(h, "h")
+    wp, wt, ws = _matrix(w, "w")
+    if ht != wt or h.shape[1] != w.shape[1]:
+        raise TypeError("h and w must have one type and one dim")
+    tp = _dev_ptr(targets, torch.int32, "targets")
+    if targets.numel() != h.shape[0]:
+        raise TypeError("targets must have one id per row of h")
+    return hp, hs, wp, ws, ht, tp
+
+
+def _row_floats(t, n: int, name: str) -> int:
+    p = _dev_ptr(t, torch.float32, name)
+    if t is not None and t.numel() != n:
+        raise TypeError(f"{name} must have one value per row of h")
+    return p
+
+
+def ne_xent_loss(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                 workspace: torch.Tensor, stream=None) -> None:
+    """Softmax cross entropy of each row of h [n][dim] against all rows of w [num_rows][dim] (both float32 or both bfloat16,
+    CUDA): loss and lse float32 [n].  targets int32 [n]; one outside [0, num_rows) leaves its row out (0, 0).
+    workspace: CUDA uint8 of ne_xent_workspace_bytes(n, num_rows, dim, dtype, grad=False) bytes."""
+    hp, hs, wp, ws, ty, tp = _xent_operands(h, w, targets)
+    n = h.shape[0]
+    lp, zp = _row_floats(loss, n, "loss"), _row_floats(lse, n, "lse")
+    kp = _dev_ptr(workspace, torch.uint8, "workspace")
+    _check(lib().ne_xent_loss(hp, hs, wp, ws, ty, tp, n, w.shape[0], h.shape[1], lp, zp, kp,
+                              workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+
+
+def ne_xent_grad(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dh: torch.Tensor | None,
+                 dw: torch.Tensor | None, workspace: torch.Tensor, loss_grad: torch.Tensor | None = None, scale: float = 1.0,
+                 stream=None) -> None:
+    """Gradients of scale * sum of loss_grad[i] * loss[i] (loss_grad None: 1 for every row) with respect to h and w, in their
+    type, into dh and dw (either may be None); lse as ne_xent_loss wrote it.  workspace: CUDA uint8 of
+    ne_xent_workspace_bytes(n, num_rows, dim, dtype, grad=True) bytes."""
+    hp, hs, wp, ws, ty, tp = _xent_operands(h, w, targets)
+    n = h.shape[0]
+    zp, cp = _row_floats(lse, n, "lse"), _row_floats(loss_grad, n, "loss_grad")
+    kp = _dev_ptr(workspace, torch.uint8, "workspace")
+    outs = []
+    for t, like, name in ((dh, h, "dh"), (dw, w, "dw")):
+        if t is None:
+            outs += [0, 0]
+            continue
+        p, t_type, stride = _matrix(t, name)
+        if t.shape != like.shape or t_type != ty:
+            raise TypeError(f"{name} must have the shape and type of {name[1:]}")
+        outs += [p, stride]
+    _check(lib().ne_xent_grad(hp, hs, wp, ws, ty, tp, zp, cp, scale, n, w.shape[0], h.shape[1], *outs, kp,
+                              workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+
+
+class AdamW:
+    """Handle from ne_create_adamw; keeps the tensors and the workspace alive."""
+
+    def __init__(self, handle: int, tensors, workspace: torch.Tensor):
+        self.handle = handle
+        self.tensors = tensors
+        self.workspace = workspace
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.ne_destroy_adamw(self.handle)
+            self.handle = None
+
+
+def ne_adamw_workspace_bytes(numels) -> int:
+    """Workspace of a handle on tensors of these numbers of elements."""
+    arr = (NeAdamwTensor * max(len(numels), 1))(*[NeAdamwTensor(n=int(n)) for n in numels])
+    return int(lib().ne_adamw_workspace_bytes(arr, len(numels)))
+
+
+def ne_create_adamw(params, grads, m, v, workspace: torch.Tensor, weight_decay=0.0, m_scale=None, v_scale=None, params_bf16=None,
+                    seed: int = 0, stream=None) -> AdamW:
+    """AdamW on lists of contiguous CUDA tensors: params float32, grads float32 or bfloat16, states m and v of the same
+    numbers of elements, all float32 (32 bits) or all float8_e4m3fn with float32 scales m_scale and v_scale, one per
+    started block of 256 elements (8 bits: v holds the root of the second moment); zeros everywhere for a new run.
+    weight_decay: one value or one per tensor.  params_bf16: None, or bfloat16 copies (entries may be None) that every step writes."""
+    count = len(params)
+    lists = {"grads": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "params_bf16": params_bf16}
+    for name, ts in lists.items():
+        if ts is not None and len(ts) != count:
+            raise TypeError(f"{name} must have one tensor per parameter")
+    states = {t.dtype for t in list(m) + list(v)}
+    if len(states) != 1 or not states <= {torch.float32, torch.float8_e4m3fn}:
+        raise TypeError("m and v must all be torch.float32 or all torch.float8_e4m3fn")
+    eight = torch.float8_e4m3fn in states
+    if eight and (m_scale is None or v_scale is None):
+        raise TypeError("8-bit states need m_scale and v_scale")
+    decays = [float(weight_decay)] * count if not hasattr(weight_decay, "__len__") else [float(x) for x in weight_decay]
+    if len(decays) != count:
+        raise TypeError("weight_decay must be one value or one per parameter")
+    arr = (NeAdamwTensor * max(count, 1))()
+    for i in range(count):
+        n = params[i].numel()
+        blocks = -(-n // NE_ADAMW_BLOCK)
+        grad_type = _TYPES.get(grads[i].dtype)
+        if grad_type is None:
+            raise TypeError("grads must be torch.float32 or torch.bfloat16")
+        wanted = [("grads", grads[i], grads[i].dtype, n), ("m", m[i], m[i].dtype, n), ("v", v[i], v[i].dtype, n)]
+        if eight:
+            wanted += [("m_scale", m_scale[i], torch.float32, blocks), ("v_scale", v_scale[i], torch.float32, blocks)]
+        copy = params_bf16[i] if params_bf16 is not None else None
+        if copy is not None:
+            wanted.append(("params_bf16", copy, torch.bfloat16, n))
+        ptr = {"params": _dev_ptr(params[i], torch.float32, "params")}
+        for name, t, dtype, numel in wanted:
+            ptr[name] = _dev_ptr(t, dtype, name)
+            if t.numel() != numel:
+                raise TypeError(f"{name}[{i}] needs {numel} elements")
+        arr[i] = NeAdamwTensor(ptr["params"], ptr["grads"], ptr["m"], ptr["v"], ptr.get("m_scale"), ptr.get("v_scale"),
+                               ptr.get("params_bf16"), n, decays[i], grad_type)
+    wp = _dev_ptr(workspace, torch.uint8, "workspace")
+    out = ctypes.c_void_p()
+    _check(lib().ne_create_adamw(ctypes.byref(out), arr, count, 8 if eight else 32, seed & (2**64 - 1), wp,
+                                 workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+    return AdamW(out.value, (params, grads, m, v, m_scale, v_scale, params_bf16), workspace)
+
+
+def ne_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                  grad_scale: float = 1.0, stream=None) -> None:
+    """Step number `step` (from 1 on) of every tensor of the handle, with the gradients that its grads hold."""
+    _check(lib().ne_adamw_step(opt.handle, step, lr, beta1, beta2, eps, grad_scale, _stream_ptr(stream)))
 
 
 def ne_set_tuning(tables: Tables, list_cap: int = -1, sweep_per_thread: int = 0) -> None:

@@ -7,7 +7,7 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRCS = [os.path.join(PKG, "csrc", "ne.hip"), os.path.join(PKG, "csrc", "ne_shared.hip")]
+SRCS = [os.path.join(PKG, "csrc", f) for f in ("ne.hip", "ne_shared.hip", "ne_embed.hip", "ne_xent.hip", "ne_adamw.hip")]
 OUT = os.path.join(PKG, "libne.so")
 
 HIPCC_FLAGS = [

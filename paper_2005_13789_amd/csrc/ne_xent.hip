@@ -1,0 +1,859 @@
+// Softmax cross entropy against a whole table, without keeping the scores: ne_xent_loss, ne_xent_grad.
+//
+//     S = H . W^T [n x V],   lse_i = log sum_v exp S_iv,   loss_i = lse_i - S_i,target
+//     G_iv = scale c_i (exp(S_iv - lse_i) - [v = target_i]),   dH = G . W,   dW = G^T . H
+//
+// Everything is a matrix product with something small around it, so one tile loop on the matrix cores serves all
+// three products; they differ in where their operands lie and in what becomes of the sums:
+//   scores   every lane of a tile's sums belongs to one row of H (table rows run along the registers), so the running
+//            maximum and sum of a row's softmax are two registers, joined between lanes once at the end.
+//   gradient the same product again for a piece of the table, whose G is written to the workspace (sized to stay in
+//            the 256 MB of last-level cache), then dH += G . W_piece and dW_piece = G^T . H in one launch.
+// The scores are computed twice (8 n V d operations in training, where 6 would do with all scores kept).
+//
+// Types: bf16 operands go to the matrix cores as they are.  fp32 operands are split into two fp16 halves at a common
+// power of two, x 2^k = hi + lo with 22 bits, and a product is hi hi + hi lo + lo hi: the error of an fp32 product at
+// three matrix instructions, where the fp32 matrix instructions take 16 times as long as one.
+//
+// Operands in LDS are 16-byte pieces placed so that reads are free of bank conflicts (an XOR of the piece's
+// index with the row's); they come from memory straight to LDS, 16 bytes a lane, and the XOR is applied to the
+// address that a lane reads.  Operands whose rows run along the contraction are read with the transposing LDS read.
+#include "ne_internal.h"
+#include "ne_ops.h"
+
+namespace {
+
+typedef _Float16 f16_t;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kThreads = 256;          // 4 wavefronts, 2 x 2 over a tile
+constexpr int kTile = 128;             // rows and columns of a tile of sums
+constexpr int kOperandBytes = 16384;   // one operand's share of a stage in LDS (all its parts)
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kPadDim = 64;            // packed rows are a multiple of this, filled with zeros
+constexpr int kSlots = 512;            // workgroups that run at once: 256 CUs, two each
+constexpr int kAmaxBlocks = 256;
+constexpr size_t kGBytes = size_t{128} << 20;      // G of one piece
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
+
+template <int P> constexpr int step_of() { return P == 1 ? 64 : 32; }   // contraction indices of a stage
+
+// An operand of a product.  ROWS: element (row, k) at row * stride + k.  Otherwise (row, k) at k * stride + row.
+struct Operand {
+    const uint16_t* part[2];
+    int64_t stride;
+    uint32_t last;      // ROWS: last row; otherwise: last k
+    uint32_t width;     // columns that there are: a multiple of 8
+};
+
+// ---------------------------------------------------------------------------------------------
+// a stage: 128 rows x step_of<P>() contraction indices of each operand's P parts
+// ---------------------------------------------------------------------------------------------
+template <int P, bool ROWS>
+__device__ __forceinline__ void fetch(const Operand& o, uint32_t row0, uint32_t k0, unsigned char* lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int i = q * 4 + wave;                         // 1 KB pieces of the operand's 16 KB
+        const int part = P == 1 ? 0 : i >> 3, j = P == 1 ? i : i & 7;
+        int64_t at;
+        if (ROWS && P == 1) {
+            const uint32_t row = min(row0 + j * 8 + (lane >> 3), o.last);
+            at = static_cast<int64_t>(row) * o.stride + k0 + (((lane & 7) ^ (lane >> 3)) << 3);
+        } else if (ROWS) {
+            const uint32_t row = min(row0 + j * 16 + (lane >> 2), o.last);
+            at = static_cast<int64_t>(row) * o.stride + k0 + (((lane & 3) ^ ((lane >> 3) & 3)) << 3);
+        } else {
+            const uint32_t k = min(k0 + j * 4 + (lane >> 4), o.last);
+            const uint32_t col = row0 + ((((lane & 15) ^ ((lane >> 4) << 2))) << 3);
+            at = static_cast<int64_t>(k) * o.stride + min(col, o.width - 8);
+        }
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(o.part[part] + at),
+                                         (__attribute__((address_space(3))) void*)(lds + i * 1024), 16, 0, 0);
+    }
+}
+
+// What lane l supplies for rows r0 .. r0 + 31 and contraction indices 16 kk .. + 15 of a stage: row l % 32, the eight
+// indices from (l / 32) * 8 on.
+template <int P, bool ROWS>
+__device__ __forceinline__ s16x8 fragment(const unsigned char* lds, int part, int r0, int kk)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned char* base = lds + (P == 1 ? 0 : part * (kOperandBytes / 2));
+    if (ROWS) {
+        const int row = r0 + (lane & 31), piece = kk * 2 + (lane >> 5);
+        const int at = P == 1 ? row * 128 + ((piece ^ (row & 7)) << 4) : row * 64 + ((piece ^ ((row >> 1) & 3)) << 4);
+        return *reinterpret_cast<const s16x8*>(base + at);
+    }
+    // 16 lanes get 16 columns of 4 rows: lane i points to the i % 4-th 8 bytes of row i / 4 and receives column i
+    const int i = lane & 15, g = lane >> 4;
+    const int k = kk * 16 + (g >> 1) * 8 + (i >> 2), unit = (r0 >> 4) + (g & 1);
+    const int at = k * 256 + ((unit ^ ((i >> 2) << 1)) << 5) + ((i & 3) << 3);
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + at));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + at + 1024));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <int P>
+__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
+{
+    if (P == 1) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// acc[im][in] += A B^T over one stage; a wavefront has rows 64 (wave / 2) .. and columns 64 (wave % 2) .. of the tile.
+template <int P, bool AROWS, bool BROWS>
+__device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&acc)[2][2])
+{
+    const int wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
+    const unsigned char* A = stage;
+    const unsigned char* B = stage + kOperandBytes;
+#pragma unroll
+    for (int kk = 0; kk < step_of<P>() / 16; ++kk) {
+        s16x8 a[P][2], b[P][2];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                a[p][i] = fragment<P, AROWS>(A, p, m0 + 32 * i, kk);
+                b[p][i] = fragment<P, BROWS>(B, p, n0 + 32 * i, kk);
+            }
+#pragma unroll
+        for (int im = 0; im < 2; ++im)
+#pragma unroll
+            for (int in = 0; in < 2; ++in) {
+                acc[im][in] = mfma<P>(a[0][im], b[0][in], acc[im][in]);
+                if (P == 2) {
+                    acc[im][in] = mfma<P>(a[0][im], b[P - 1][in], acc[im][in]);
+                    acc[im][in] = mfma<P>(a[P - 1][im], b[0][in], acc[im][in]);
+                }
+            }
+    }
+}
+
+__device__ __forceinline__ void clear(f32x16 (&acc)[2][2])
+{
+#pragma unroll
+    for (int im = 0; im < 2; ++im)
+#pragma unroll
+        for (int in = 0; in < 2; ++in)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[im][in][i] = 0.0f;
+}
+
+// Row (of 32) of a lane's i-th sum.
+__device__ __forceinline__ int sum_row(int i) { return (i & 3) + 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5); }
+
+// ---------------------------------------------------------------------------------------------
+// packing
+// ---------------------------------------------------------------------------------------------
+// Largest finite magnitudes, kAmaxBlocks of each: of W, of H's rows with a target, of the same rows times c_i.
+struct AmaxArgs {
+    const float* h;
+    const float* w;
+    const int32_t* targets;
+    const float* c;
+    int64_t h_stride, w_stride, n, num_rows;
+    int32_t dim;
+    float* amax;        // [3][kAmaxBlocks]
+};
+
+__device__ __forceinline__ float finite_abs(float x)
+{
+    x = fabsf(x);
+    return x < INFINITY ? x : 0.0f;     // (false for a NaN)
+}
+
+__device__ __forceinline__ float block_max(float v, float* lds)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
+
+__global__ void __launch_bounds__(kThreads) amax_kernel(AmaxArgs a)
+{
+    __shared__ float lds[4];
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = blockIdx.x * 4 + (threadIdx.x >> 6), waves = kAmaxBlocks * 4;
+    float w = 0.0f, h = 0.0f, ch = 0.0f;
+    for (int64_t v = wave; v < a.num_rows; v += waves)
+        for (int e = lane; e < a.dim; e += 64) w = fmaxf(w, finite_abs(a.w[v * a.w_stride + e]));
+    for (int64_t i = wave; i < a.n; i += waves) {
+        if (static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) continue;
+        const float c = a.c ? a.c[i] : 1.0f;
+        for (int e = lane; e < a.dim; e += 64) {
+            const float x = a.h[i * a.h_stride + e];
+            h = fmaxf(h, finite_abs(x));
+            ch = fmaxf(ch, finite_abs(c * x));
+        }
+    }
+    w = block_max(w, lds);
+    h = block_max(h, lds);
+    ch = block_max(ch, lds);
+    if (threadIdx.x == 0) {
+        a.amax[blockIdx.x] = w;
+        a.amax[kAmaxBlocks + blockIdx.x] = h;
+        a.amax[2 * kAmaxBlocks + blockIdx.x] = ch;
+    }
+}
+
+// The power of two that brings a matrix's largest magnitude into [2^13, 2^14).
+__device__ __forceinline__ int shift_of(float amax)
+{
+    if (amax == 0.0f) return 0;
+    const int e = static_cast<int>(__float_as_uint(amax) >> 23);
+    return 13 - (max(e, 1) - 127);
+}
+
+struct PackArgs {
+    const void* in;
+    int64_t in_stride, rows, padded_rows;
+    const int32_t* targets;        // rows without a target become zeros; NULL: all rows count
+    uint32_t num_targets;
+    const float* c;                // NULL, or factors of the rows
+    int32_t dim, padded;
+    uint16_t* out[2];
+    const float* amax;             // fp32 only
+    int32_t* shift;                // fp32 only: receives the power of two
+};
+
+// One row per wavefront at a time, 8 elements a lane.
+template <int P>
+__global__ void __launch_bounds__(kThreads) pack_kernel(PackArgs a)
+{
+    __shared__ float lds[4];
+    int k = 0;
+    if (P == 2) {
+        k = shift_of(block_max(a.amax[threadIdx.x], lds));
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.shift = k;
+    }
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), waves = static_cast<int64_t>(gridDim.x) * 4;
+    for (int64_t r = wave; r < a.padded_rows; r += waves) {
+        const bool counts = r < a.rows && (!a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets);
+        const float c = counts && a.c ? a.c[r] : 1.0f;
+        for (int e0 = lane * 8; e0 < a.padded; e0 += 512) {
+            s16x8 out[P];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool have = counts && e0 + e < a.dim;
+                if (P == 1) {
+                    out[0][e] = have ? static_cast<const short*>(a.in)[r * a.in_stride + e0 + e] : 0;
+                } else {
+                    const float x = have ? ldexpf(c * static_cast<const float*>(a.in)[r * a.in_stride + e0 + e], k) : 0.0f;
+                    const f16_t hi = static_cast<f16_t>(x), lo = static_cast<f16_t>(x - static_cast<float>(hi));
+                    out[0][e] = __builtin_bit_cast(short, hi);
+                    out[P - 1][e] = P == 2 ? __builtin_bit_cast(short, lo) : out[0][e];
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + r * a.padded + e0) = out[p];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// scores: the softmax's maximum and sum of every row of H, and its target's score
+// ---------------------------------------------------------------------------------------------
+struct ScoreArgs {
+    Operand w, h;                  // both by rows
+    const int32_t* targets;
+    const int32_t* shift;          // fp32 only: powers of two of W and H
+    int64_t n;
+    uint32_t num_rows, row_tiles, splits, tokens;   // tokens: padded n
+    int32_t steps;                 // stages of a tile
+    float2* stat;                  // [splits][tokens]  maximum and sum, in powers of two
+    float* target_score;           // [tokens]
+};
+
+template <int P>
+__device__ __forceinline__ float score_factor(const int32_t* shift)
+{
+    if (P == 1) return 1.0f;
+    return ldexpf(1.0f, max(min(-(shift[0] + shift[1]), 127), -126));
+}
+
+template <int P>
+__global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[2][kStageBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
+    const uint32_t token_tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits;
+    const uint32_t tile0 = split * per, tile1 = min(tile0 + per, a.row_tiles);
+    const float factor = score_factor<P>(a.shift), to_log2 = kLog2e * factor;
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
+    uint32_t target[2];
+    int64_t token[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        token[j] = static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31);
+        target[j] = token[j] < a.n ? static_cast<uint32_t>(a.targets[token[j]]) : 0xFFFFFFFFu;
+    }
+    f32x16 acc[2][2];
+    clear(acc);
+    const uint32_t stages = tile1 > tile0 ? (tile1 - tile0) * a.steps : 0;
+    auto get = [&](uint32_t tile, int step, int to) {
+        fetch<P, true>(a.w, tile * kTile, step * step_of<P>(), lds[to]);
+        fetch<P, true>(a.h, token_tile * kTile, step * step_of<P>(), lds[to] + kOperandBytes);
+    };
+    uint32_t tile = tile0, next_tile = tile0;
+    int step = 0, next_step = 0;
+    auto advance = [&](uint32_t& t, int& s) { if (++s == a.steps) { s = 0; ++t; } };
+    if (stages) get(tile0, 0, 0);
+    advance(next_tile, next_step);
+    __syncthreads();
+    for (uint32_t s = 0; s < stages; ++s) {
+        if (s + 1 < stages) get(next_tile, next_step, (s + 1) & 1);
+        multiply<P, true, true>(lds[s & 1], acc);
+        if (step == a.steps - 1) {
+            const uint32_t row0 = tile * kTile + m0;
+            if (row0 + 64 > a.num_rows) {
+#pragma unroll
+                for (int im = 0; im < 2; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (row0 + 32 * im + sum_row(i) >= a.num_rows) acc[im][0][i] = acc[im][1][i] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (__any(target[j] - row0 < 64)) {
+#pragma unroll
+                    for (int im = 0; im < 2; ++im)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (target[j] == row0 + 32 * im + sum_row(i) && target[j] < a.num_rows) a.target_score[token[j]] = acc[im][j][i] * factor;
+                }
+                float t = acc[0][j][0];
+#pragma unroll
+                for (int im = 0; im < 2; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) t = fmaxf(t, acc[im][j][i]);
+                const float now = fmaxf(top[j], t * to_log2);
+                const float by = now == -INFINITY ? 0.0f : now;         // (nothing seen yet but scores of minus infinity)
+                float part = 0.0f;
+#pragma unroll
+                for (int im = 0; im < 2; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by));
+                sum[j] = fmaf(sum[j], __builtin_amdgcn_exp2f(top[j] - by), part);
+                top[j] = now;
+            }
+            clear(acc);
+        }
+        __syncthreads();
+        advance(tile, step);
+        advance(next_tile, next_step);
+    }
+    // lanes l and l + 32 and the two wavefronts of a column have the same rows of H
+    float2* join = reinterpret_cast<float2*>(lds[0]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float other = __shfl_xor(top[j], 32, 64), other_sum = __shfl_xor(sum[j], 32, 64);
+        const float now = fmaxf(top[j], other), by = now == -INFINITY ? 0.0f : now;
+        sum[j] = sum[j] * __builtin_amdgcn_exp2f(top[j] - by) + other_sum * __builtin_amdgcn_exp2f(other - by);
+        top[j] = now;
+        if (lane < 32) join[(wave >> 1) * kTile + n0 + 32 * j + lane] = make_float2(top[j], sum[j]);
+    }
+    __syncthreads();
+    if (threadIdx.x < kTile) {
+        const float2 p = join[threadIdx.x], q = join[kTile + threadIdx.x];
+        const float now = fmaxf(p.x, q.x), by = now == -INFINITY ? 0.0f : now;
+        const float both = p.y * __builtin_amdgcn_exp2f(p.x - by) + q.y * __builtin_amdgcn_exp2f(q.x - by);
+        a.stat[static_cast<int64_t>(split) * a.tokens + static_cast<int64_t>(token_tile) * kTile + threadIdx.x] = make_float2(now, both);
+    }
+}
+
+// Joins the splits of the table: lse and loss of every row.
+__global__ void __launch_bounds__(kThreads) loss_join_kernel(const float2* stat, const float* target_score, const int32_t* targets, int64_t n,
+                                                             uint32_t num_rows, uint32_t splits, int64_t tokens, float* loss, float* lse)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= n) return;
+    if (static_cast<uint32_t>(targets[i]) >= num_rows) {
+        loss[i] = 0.0f;
+        lse[i] = 0.0f;
+        return;
+    }
+    float top = -INFINITY;
+    for (uint32_t s = 0; s < splits; ++s) top = fmaxf(top, stat[s * tokens + i].x);
+    const float by = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    for (uint32_t s = 0; s < splits; ++s) {
+        const float2 p = stat[s * tokens + i];
+        sum += p.y * exp2f(p.x - by);
+    }
+    const float z = (top + log2f(sum)) * kLn2;
+    lse[i] = z;
+    loss[i] = z - target_score[i];
+}
+
+// ---------------------------------------------------------------------------------------------
+// G of a piece of the table
+// ---------------------------------------------------------------------------------------------
+struct CoefArgs {
+    Operand w, h;                  // both by rows
+    const int32_t* targets;
+    const int32_t* shift;
+    const float* lse;
+    const float* c;                // bf16 only (fp32: applied to dH and to the rows of H)
+    float scale;                   // bf16 only
+    int64_t n, g_stride;
+    uint32_t num_rows, row_base, row_tiles;
+    int32_t steps;
+    uint16_t* g[2];                // [tokens][g_stride], table rows of the piece side by side
+};
+
+template <int P>
+__global__ void __launch_bounds__(kThreads, 2) coef_kernel(CoefArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[2][kStageBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
+    const uint32_t token_tile = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles;
+    const uint32_t row0 = a.row_base + tile * kTile;
+    f32x16 acc[2][2];
+    clear(acc);
+    auto get = [&](int step, int to) {
+        fetch<P, true>(a.w, row0, step * step_of<P>(), lds[to]);
+        fetch<P, true>(a.h, token_tile * kTile, step * step_of<P>(), lds[to] + kOperandBytes);
+    };
+    get(0, 0);
+    __syncthreads();
+    for (int s = 0; s < a.steps; ++s) {
+        if (s + 1 < a.steps) get(s + 1, (s + 1) & 1);
+        multiply<P, true, true>(lds[s & 1], acc);
+        __syncthreads();
+    }
+    const float to_log2 = kLog2e * score_factor<P>(a.shift);
+    unsigned char* out = lds[0];       // [parts][128 rows of H][128 table rows], 16-byte pieces at piece ^ row % 16
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int t = n0 + 32 * j + (lane & 31);
+        const int64_t token = static_cast<int64_t>(token_tile) * kTile + t;
+        const uint32_t target = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
+        const bool counts = target < a.num_rows;
+        const float by = counts ? a.lse[token] * kLog2e : 0.0f;
+        const float c = P == 1 ? (counts ? a.scale * (a.c ? a.c[token] : 1.0f) : 0.0f) : 0x1p14f;
+#pragma unroll
+        for (int im = 0; im < 2; ++im)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                s16x4 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t row = row0 + m0 + 32 * im + sum_row(4 * q + e);
+                    float x = __builtin_amdgcn_exp2f(fmaf(acc[im][j][4 * q + e], to_log2, -by));
+                    if (row == target) x -= 1.0f;
+                    x = counts && row < a.num_rows ? x * c : 0.0f;
+                    if (P == 1) {
+                        hi[e] = __builtin_bit_cast(short, static_cast<bf16_t>(x));
+                    } else {
+                        const f16_t xh = static_cast<f16_t>(x);
+                        hi[e] = __builtin_bit_cast(short, xh);
+                        lo[e] = __builtin_bit_cast(short, static_cast<f16_t>(x - static_cast<float>(xh)));
+                    }
+                }
+                const int v = m0 + 32 * im + 8 * q + 4 * (lane >> 5);
+                const int at = t * 256 + (((v >> 3) ^ (t & 15)) << 4) + ((v & 4) << 1);
+                *reinterpret_cast<s16x4*>(out + at) = hi;
+                if (P == 2) *reinterpret_cast<s16x4*>(out + kStageBytes + at) = lo;
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = i * 16 + (threadIdx.x >> 4), piece = threadIdx.x & 15;
+            const s16x8 x = *reinterpret_cast<const s16x8*>(out + p * kStageBytes + t * 256 + ((piece ^ (t & 15)) << 4));
+            *reinterpret_cast<s16x8*>(a.g[p] + (static_cast<int64_t>(token_tile) * kTile + t) * a.g_stride + tile * kTile + piece * 8) = x;
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// dH += G . W_piece and dW_piece = G^T . H
+// ---------------------------------------------------------------------------------------------
+struct ProductArgs {
+    Operand g_rows, w;             // dH: G by rows (contraction along them), W across
+    Operand g_cols, h;             // dW: G across, H across
+    float* dh;                     // [h_splits][tokens][cols]  sums over the pieces
+    float* dw;                     // [w_splits][piece rows][cols]
+    uint32_t tokens, piece_rows, cols;      // multiples of 128
+    uint32_t h_tiles, w_tiles, col_tiles;   // tiles over tokens, piece rows, columns
+    uint32_t h_splits, w_splits, h_share, w_share;      // splits of the contraction, stages of each
+    uint32_t h_stages, w_stages;
+    int32_t add;                   // dh: added to what earlier pieces left
+};
+
+template <int P, bool AROWS>
+__device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, uint32_t row0, uint32_t col0, uint32_t s0, uint32_t s1,
+                                             unsigned char (*lds)[kStageBytes], f32x16 (&acc)[2][2])
+{
+    auto get = [&](uint32_t s, int to) {
+        fetch<P, AROWS>(A, row0, s * step_of<P>(), lds[to]);
+        fetch<P, false>(B, col0, s * step_of<P>(), lds[to] + kOperandBytes);
+    };
+    clear(acc);
+    if (s0 < s1) get(s0, 0);
+    __syncthreads();
+    for (uint32_t s = s0; s < s1; ++s) {
+        if (s + 1 < s1) get(s + 1, (s - s0 + 1) & 1);
+        multiply<P, AROWS, false>(lds[(s - s0) & 1], acc);
+        __syncthreads();
+    }
+}
+
+template <int P>
+__global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[2][kStageBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t h_blocks = a.h_tiles * a.col_tiles * a.h_splits;
+    uint32_t b = blockIdx.x;
+    const bool dh = b < h_blocks;
+    if (!dh) b -= h_blocks;
+    const uint32_t splits = dh ? a.h_splits : a.w_splits, share = dh ? a.h_share : a.w_share, stages = dh ? a.h_stages : a.w_stages;
+    const uint32_t col = b % a.col_tiles, split = b / a.col_tiles % splits, tile = b / a.col_tiles / splits;
+    const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
+    f32x16 acc[2][2];
+    if (dh) product_tile<P, true>(a.g_rows, a.w, tile * kTile, col * kTile, s0, s1, lds, acc);
+    else product_tile<P, false>(a.g_cols, a.h, tile * kTile, col * kTile, s0, s1, lds, acc);
+    float* out = dh ? a.dh + static_cast<int64_t>(split) * a.tokens * a.cols : a.dw + static_cast<int64_t>(split) * a.piece_rows * a.cols;
+    const bool add = dh && a.add;
+#pragma unroll
+    for (int im = 0; im < 2; ++im)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int64_t row = static_cast<int64_t>(tile) * kTile + (wave >> 1) * 64 + 32 * im + sum_row(i);
+            float* to = out + row * a.cols + col * kTile + (wave & 1) * 64 + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) to[32 * j] = add ? to[32 * j] + acc[im][j][i] : acc[im][j][i];
+        }
+}
+
+// Sums the splits and rounds once.  dH: rows without a target become zeros, the others take their factor.
+struct ReduceArgs {
+    const float* in;               // [splits][rows_in][cols]
+    int64_t split_stride;
+    uint32_t splits, cols;
+    int64_t rows;
+    int32_t dim;
+    void* out;
+    int64_t out_stride;
+    const int32_t* targets;        // dH only
+    uint32_t num_targets;
+    const float* c;
+    float scale;
+    const int32_t* shift;          // fp32 only: power of two of the other operand
+};
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t waves = static_cast<int64_t>(gridDim.x) * 4;
+    const int k = a.shift ? -(*a.shift + kGShift) : 0;
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); r < a.rows; r += waves) {
+        const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
+        const float c = counts && a.c ? a.c[r] : 1.0f;
+        for (int e = lane; e < a.dim; e += 64) {
+            float sum = 0.0f;
+            for (uint32_t s = 0; s < a.splits; ++s) sum += a.in[s * a.split_stride + r * a.cols + e];
+            if (a.shift) sum = ldexpf(sum, k) * a.scale * c;
+            static_cast<T*>(a.out)[r * a.out_stride + e] = from_float<T>(counts ? sum : 0.0f);
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) zero_kernel(T* out, int64_t stride, int64_t rows, int32_t dim)
+{
+    const int64_t total = rows * dim;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * kThreads)
+        out[i / dim * stride + i % dim] = from_float<T>(0.0f);
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+struct XentWs {
+    int32_t parts, padded, cols;
+    int64_t tokens;
+    uint32_t row_tiles, splits;        // of the scores
+    int64_t piece;                     // table rows of a piece
+    uint32_t h_splits, w_splits, h_share, w_share, h_stages, w_stages;
+    float* amax;
+    int32_t* shift;                    // of W, H, c H
+    uint16_t *h[2], *hc[2], *w[2];
+    float2* stat;
+    float* target_score;
+    uint16_t* g[2];
+    float *dh, *dw;
+    size_t total;
+};
+
+bool xent_sizes_ok(int64_t n, int64_t num_rows, int32_t dim, int32_t type)
+{
+    return n >= 0 && n <= (1 << 24) && num_rows > 0 && num_rows < (1ll << 31) && dim >= 1 && dim <= NE_OP_MAX_DIM && type_ok(type);
+}
+
+// The workspace has room for packed copies whether or not this call's alignment needs them.
+XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad, char* base)
+{
+    XentWs w{};
+    w.parts = type == NE_F32 ? 2 : 1;
+    w.padded = static_cast<int32_t>(round_up(dim, kPadDim));
+    w.cols = static_cast<int32_t>(round_up(dim, kTile));
+    w.tokens = round_up(n, kTile);
+    w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, kTile));
+    const int64_t token_tiles = w.tokens / kTile;
+    Carver take{base};
+    w.amax = take.get<float>(3 * kAmaxBlocks);
+    w.shift = take.get<int32_t>(3);
+    for (int p = 0; p < w.parts; ++p) {
+        w.h[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded);
+        w.w[p] = take.get<uint16_t>(static_cast<size_t>(num_rows) * w.padded);
+    }
+    if (!grad) {
+        w.splits = static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>(w.row_tiles, kSlots / std::min<int64_t>(token_tiles, kSlots))));
+        w.stat = take.get<float2>(static_cast<size_t>(w.splits) * w.tokens);
+        w.target_score = take.get<float>(static_cast<size_t>(w.tokens));
+    } else {
+        const int64_t step = w.parts == 1 ? step_of<1>() : step_of<2>();
+        const int64_t most = std::max<int64_t>(kTile, static_cast<int64_t>(kGBytes / (2 * w.parts)) / w.tokens / kTile * kTile);
+        const int64_t pieces = ceil_div(num_rows, most);
+        w.piece = round_up(ceil_div(num_rows, pieces), kTile);
+        // contractions are split so that all workgroups of a launch have about as many stages, and the machine is full
+        const int64_t cols = w.cols / kTile, h_tiles = token_tiles * cols, w_tiles = w.piece / kTile * cols;
+        w.h_stages = static_cast<uint32_t>(w.piece / step);
+        w.w_stages = static_cast<uint32_t>(w.tokens / step);
+        const int64_t share = std::max<int64_t>(16, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, kSlots));
+        w.h_splits = static_cast<uint32_t>(ceil_div(w.h_stages, share));
+        w.w_splits = static_cast<uint32_t>(ceil_div(w.w_stages, share));
+        w.h_share = static_cast<uint32_t>(ceil_div(w.h_stages, w.h_splits));
+        w.w_share = static_cast<uint32_t>(ceil_div(w.w_stages, w.w_splits));
+        for (int p = 0; p < w.parts; ++p) {
+            w.hc[p] = w.parts == 2 ? take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded) : nullptr;
+            w.g[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.piece);
+        }
+        w.dh = take.get<float>(static_cast<size_t>(w.h_splits) * w.tokens * w.cols);
+        w.dw = take.get<float>(static_cast<size_t>(w.w_splits) * w.piece * w.cols);
+    }
+    w.total = take.total();
+    return w;
+}
+
+struct XentCall {
+    const void *h, *w;
+    int64_t h_stride, w_stride, n, num_rows;
+    int32_t dim, type;
+    const int32_t* targets;
+    const float* c;
+};
+
+// Packs H (and c H) and, where it cannot be used as it is, W.
+hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Operand* hc, Operand* wo, hipStream_t st)
+{
+    const bool direct = x.type == NE_BF16 && x.dim % kPadDim == 0 && x.w_stride % 8 == 0 && aligned(x.w, 16);
+    if (x.type == NE_F32) {
+        AmaxArgs a{static_cast<const float*>(x.h), static_cast<const float*>(x.w), x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, x.dim, w.amax};
+        hipLaunchKernelGGL(amax_kernel, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    auto run = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which) {
+        PackArgs a{};
+        a.in = in; a.in_stride = stride; a.rows = rows; a.padded_rows = padded_rows; a.targets = targets;
+        a.num_targets = static_cast<uint32_t>(x.num_rows); a.c = c; a.dim = x.dim; a.padded = w.padded;
+        a.out[0] = out[0]; a.out[1] = out[1]; a.amax = w.amax + which * kAmaxBlocks; a.shift = w.shift + which;
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(padded_rows, 4), 2048)));
+        if (w.parts == 1) hipLaunchKernelGGL(pack_kernel<1>, grid, dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL(pack_kernel<2>, grid, dim3(kThreads), 0, st, a);
+        return hipGetLastError();
+    };
+    auto operand = [&](uint16_t* const* part, int64_t rows) {
+        Operand o{};
+        o.part[0] = part[0]; o.part[1] = part[1]; o.stride = w.padded; o.last = static_cast<uint32_t>(rows - 1); o.width = static_cast<uint32_t>(w.padded);
+        return o;
+    };
+    hipError_t e = run(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1);
+    *h = operand(w.h, w.tokens);
+    *hc = *h;
+    if (e == hipSuccess && grad && x.type == NE_F32 && x.c) {
+        e = run(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, 2);
+        *hc = operand(w.hc, w.tokens);
+    }
+    if (direct) {
+        *wo = operand(w.w, x.num_rows);
+        wo->part[0] = static_cast<const uint16_t*>(x.w);
+        wo->stride = x.w_stride;
+    } else {
+        if (e == hipSuccess) e = run(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
+        *wo = operand(w.w, x.num_rows);
+    }
+    return e;
+}
+
+template <int P>
+hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse, hipStream_t st)
+{
+    ScoreArgs a{};
+    Operand unused;
+    hipError_t e = pack(x, w, false, &a.h, &unused, &a.w, st);
+    if (e != hipSuccess) return e;
+    a.targets = x.targets; a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles;
+    a.splits = w.splits; a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.target_score = w.target_score;
+    hipLaunchKernelGGL(scores_kernel<P>, dim3(static_cast<unsigned>(w.tokens / kTile * w.splits)), dim3(kThreads), 0, st, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(loss_join_kernel, dim3(static_cast<unsigned>(ceil_div(x.n, kThreads))), dim3(kThreads), 0, st, w.stat, w.target_score, x.targets,
+                       x.n, a.num_rows, w.splits, w.tokens, loss, lse);
+    return hipGetLastError();
+}
+
+template <int P, class T>
+hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw, int64_t dw_stride, hipStream_t st)
+{
+    CoefArgs ca{};
+    ProductArgs pa{};
+    hipError_t e = pack(x, w, true, &ca.h, &pa.h, &ca.w, st);
+    if (e != hipSuccess) return e;
+    const Operand all = ca.w;
+    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.c = x.c; ca.scale = scale; ca.n = x.n; ca.g_stride = w.piece;
+    ca.num_rows = static_cast<uint32_t>(x.num_rows); ca.steps = w.padded / step_of<P>();
+    const uint32_t token_tiles = static_cast<uint32_t>(w.tokens / kTile);
+    pa.dh = w.dh; pa.dw = w.dw; pa.tokens = static_cast<uint32_t>(w.tokens); pa.piece_rows = static_cast<uint32_t>(w.piece);
+    pa.cols = static_cast<uint32_t>(w.cols); pa.col_tiles = pa.cols / kTile;
+    pa.h_splits = w.h_splits; pa.w_splits = w.w_splits; pa.h_share = w.h_share; pa.w_share = w.w_share;
+    pa.w_stages = w.w_stages;
+    auto reduce = [&](ReduceArgs r) {
+        r.cols = pa.cols; r.dim = x.dim; r.scale = scale;
+        if (P == 1) r.shift = nullptr;
+        hipLaunchKernelGGL(reduce_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(ceil_div(r.rows, 4), 4096))), dim3(kThreads), 0, st, r);
+        return hipGetLastError();
+    };
+    for (int64_t base = 0; base < x.num_rows; base += w.piece) {
+        const int64_t rows = std::min<int64_t>(w.piece, x.num_rows - base);
+        ca.row_base = static_cast<uint32_t>(base);
+        ca.row_tiles = static_cast<uint32_t>(ceil_div(rows, kTile));
+        for (int p = 0; p < P; ++p) ca.g[p] = w.g[p];
+        hipLaunchKernelGGL(coef_kernel<P>, dim3(token_tiles * ca.row_tiles), dim3(kThreads), 0, st, ca);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        pa.g_rows = Operand{{w.g[0], w.g[1]}, w.piece, static_cast<uint32_t>(w.tokens - 1), static_cast<uint32_t>(w.piece)};
+        pa.g_cols = pa.g_rows;
+        pa.w = all;
+        for (int p = 0; p < P; ++p) pa.w.part[p] = all.part[p] + base * all.stride;
+        pa.w.last = static_cast<uint32_t>(rows - 1);
+        pa.h_tiles = dh ? token_tiles : 0;
+        pa.w_tiles = dw ? ca.row_tiles : 0;
+        pa.h_stages = ca.row_tiles * kTile / step_of<P>();
+        pa.add = base > 0;
+        const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
+        if (!blocks) continue;
+        hipLaunchKernelGGL(products_kernel<P>, dim3(blocks), dim3(kThreads), 0, st, pa);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (dw) {
+            ReduceArgs r{};
+            r.in = w.dw; r.split_stride = w.piece * pa.cols; r.splits = w.w_splits; r.rows = rows;
+            r.out = static_cast<T*>(dw) + base * dw_stride; r.out_stride = dw_stride;
+            r.shift = w.shift + (x.c ? 2 : 1);
+            e = reduce(r);
+            if (e != hipSuccess) return e;
+        }
+    }
+    if (dh) {
+        ReduceArgs r{};
+        r.in = w.dh; r.split_stride = w.tokens * pa.cols; r.splits = w.h_splits; r.rows = x.n; r.out = dh; r.out_stride = dh_stride;
+        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = x.c; r.shift = w.shift;
+        return reduce(r);
+    }
+    return hipSuccess;
+}
+
+ne_status check_xent(const XentCall& x, const char* who)
+{
+    const std::string name(who);
+    if (!xent_sizes_ok(x.n, x.num_rows, x.dim, x.type)) return fail(NE_ERR_ARG, name + ": n, num_rows, dim or type out of range");
+    if (x.h_stride < x.dim || x.w_stride < x.dim) return fail(NE_ERR_ARG, name + ": a row stride is smaller than dim");
+    if (!x.w || !aligned(x.w, type_bytes(x.type))) return fail(NE_ERR_ARG, name + ": w_dev is NULL or misaligned");
+    if (x.n == 0) return NE_OK;
+    if (!x.h || !aligned(x.h, type_bytes(x.type))) return fail(NE_ERR_ARG, name + ": h_dev is NULL or misaligned");
+    if (!x.targets || !aligned(x.targets, 4)) return fail(NE_ERR_ARG, name + ": targets_dev is NULL or not 4-byte aligned");
+    return NE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ne_xent_workspace_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int32_t grad)
+{
+    if (!xent_sizes_ok(n, num_rows, dim, type) || n == 0) return 0;
+    return xent_layout(n, num_rows, dim, type, grad != 0, nullptr).total;
+}
+
+ne_status ne_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type,
+                       const int32_t* targets_dev, int64_t n, int64_t num_rows, int32_t dim, float* loss_dev,
+                       float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream)
+{
+    const XentCall x{h_dev, w_dev, h_stride, w_stride, n, num_rows, dim, type, targets_dev, nullptr};
+    const ne_status rc = check_xent(x, "ne_xent_loss");
+    if (rc != NE_OK || n == 0) return rc;
+    if (!loss_dev || !lse_dev || !aligned(loss_dev, 4) || !aligned(lse_dev, 4)) return fail(NE_ERR_ARG, "ne_xent_loss: loss_dev or lse_dev is NULL or misaligned");
+    const XentWs w = xent_layout(n, num_rows, dim, type, false, static_cast<char*>(workspace_dev));
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
+        return fail(NE_ERR_ARG, "ne_xent_loss: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = type == NE_F32 ? run_loss<2>(x, w, loss_dev, lse_dev, st) : run_loss<1>(x, w, loss_dev, lse_dev, st);
+    if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("cross entropy launch: ") + hipGetErrorString(e));
+    return NE_OK;
+}
+
+ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type,
+                       const int32_t* targets_dev, const float* lse_dev, const float* loss_grad_dev, float scale,
+                       int64_t n, int64_t num_rows, int32_t dim, void* dh_dev, int64_t dh_stride, void* dw_dev,
+                       int64_t dw_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream)
+{
+    const XentCall x{h_dev, w_dev, h_stride, w_stride, n, num_rows, dim, type, targets_dev, loss_grad_dev};
+    const ne_status rc = check_xent(x, "ne_xent_grad");
+    if (rc != NE_OK) return rc;
+    if (!std::isfinite(scale)) return fail(NE_ERR_ARG, "ne_xent_grad: scale is not finite");
+    if ((dh_dev && dh_stride < dim) || (dw_dev && dw_stride < dim)) return fail(NE_ERR_ARG, "ne_xent_grad: a row stride is smaller than dim");
+    if (!aligned(dh_dev, type_bytes(type)) || !aligned(dw_dev, type_bytes(type))) return fail(NE_ERR_ARG, "ne_xent_grad: dh_dev or dw_dev is misaligned");
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (n == 0) {
+        if (!dw_dev) return NE_OK;
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(num_rows * dim, kThreads), 4096)));
+        if (type == NE_F32) hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(kThreads), 0, st, static_cast<float*>(dw_dev), dw_stride, num_rows, dim);
+        else hipLaunchKernelGGL(zero_kernel<bf16_t>, grid, dim3(kThreads), 0, st, static_cast<bf16_t*>(dw_dev), dw_stride, num_rows, dim);
+        NE_HIP_CHECK(hipGetLastError());
+        return NE_OK;
+    }
+    if (!lse_dev || !aligned(lse_dev, 4) || !aligned(loss_grad_dev, 4)) return fail(NE_ERR_ARG, "ne_xent_grad: lse_dev is NULL, or it or loss_grad_dev misaligned");
+    const XentWs w = xent_layout(n, num_rows, dim, type, true, static_cast<char*>(workspace_dev));
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
+        return fail(NE_ERR_ARG, "ne_xent_grad: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
+    if (!dh_dev && !dw_dev) return NE_OK;
+    const hipError_t e = type == NE_F32 ? run_grad<2, float>(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st)
+                                        : run_grad<1, bf16_t>(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st);
+    if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("cross entropy gradient launch: ") + hipGetErrorString(e));
+    return NE_OK;
+}
+
+}  // extern "C"

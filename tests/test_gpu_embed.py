@@ -1,0 +1,203 @@
+"""Embedding lookup with scaling and its gradient by sorted ids, against 64-bit sums."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2005_13789_amd as ne
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16]
+U = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def rows(n, d, dtype, gen, pad=0, shift=0):
+    """[n][d] on the GPU with row stride d + pad, starting `shift` elements into its buffer."""
+    buf = torch.randn(shift + n * (d + pad) + 8, generator=gen).to(dtype).to(DEV)
+    return buf[shift:shift + n * (d + pad)].view(n, d + pad)[:, :d]
+
+
+def make_ids(kind, n, V, gen):
+    if kind == "uniform":
+        ids = torch.randint(0, V, (n,), generator=gen)
+    elif kind == "skewed":
+        ids = (torch.rand(n, generator=gen, dtype=torch.float64) ** 4 * V).long().clamp(max=V - 1)
+    elif kind == "one":
+        ids = torch.full((n,), V // 2)
+    elif kind == "none":
+        ids = torch.full((n,), -1)
+    else:       # padding, ids far outside on both sides, the first and the last row
+        ids = torch.randint(0, V, (n,), generator=gen)
+        ids[::3] = -1
+        ids[1::7] = V
+        ids[2::11] = 2 ** 31 - 1
+        ids[3::13] = -2 ** 31
+        ids[4::17] = V - 1
+        ids[5::19] = 0
+    return ids.to(torch.int32)
+
+
+@pytest.mark.parametrize("ti", TYPES)
+@pytest.mark.parametrize("to", TYPES)
+@pytest.mark.parametrize("d,pad,shift", [(1, 0, 0), (3, 2, 1), (8, 0, 0), (100, 0, 0), (129, 1, 3), (512, 8, 0), (1030, 0, 5)])
+def test_lookup(ti, to, d, pad, shift):
+    gen = torch.Generator().manual_seed(d)
+    for V, n in ((1, 1), (7, 0), (1000, 517)):
+        say("lookup", ti, to, d, pad, shift, V, n)
+        table = rows(V, d, ti, gen, pad, shift)
+        ids = make_ids("edges", n, V, gen).to(DEV)
+        out = rows(n, d, to, gen, pad, shift)
+        around = out.clone() if n else None
+        scale = -1.7
+        ne.ne_embed_lookup(table, ids, out, scale=scale)
+        ok = ((ids >= 0) & (ids < V)).cpu()
+        x = table.cpu().float()[ids.cpu().long().clamp(0, V - 1)] * np.float32(scale)
+        want = torch.where(ok[:, None], x, torch.zeros(()))
+        assert torch.equal(out.cpu(), want.to(to))      # one product, one rounding
+        assert around is None or around.shape == out.shape
+
+
+def test_lookup_leaves_the_gaps_between_rows():
+    out = torch.full((50, 40), 7.0, device=DEV)
+    table = torch.randn(20, 33, device=DEV)
+    ids = torch.arange(50, dtype=torch.int32, device=DEV) % 20
+    ne.ne_embed_lookup(table, ids, out[:, 3:36])
+    assert torch.equal(out[:, :3], torch.full((50, 3), 7.0, device=DEV)) and torch.equal(out[:, 36:], torch.full((50, 4), 7.0, device=DEV))
+    assert torch.equal(out[:, 3:36], table[ids.long()])
+
+
+def check_grad(ids, grad, table_grad, V, scale, accumulate, before):
+    """Against sums in 64 bits.  A row of k terms: k + 2 roundings of at most 2^-24 of the terms' summed magnitudes (any order
+    of the sum), and the output's own rounding."""
+    n, d = grad.shape
+    ok = (ids >= 0) & (ids < V)
+    at = ids.long()[ok].cpu()
+    g = grad[ok.to(grad.device)].cpu().double() * float(np.float32(scale)) if n else torch.zeros(0, d, dtype=torch.float64)
+    want = before.double() if accumulate else torch.zeros(V, d, dtype=torch.float64)
+    size = want.abs().clone()
+    want.index_add_(0, at, g)
+    size.index_add_(0, at, g.abs())
+    k = torch.bincount(at, minlength=V).double()[:, None]
+    got = table_grad.cpu().double()
+    bound = (k + 2) * 2.0 ** -24 * size + U[table_grad.dtype] * (want.abs() + (k + 2) * 2.0 ** -24 * size)
+    bound = torch.where(k == 0, torch.zeros(()).double(), bound)      # rows that are not named: zeros, or as they were
+    bad = ((got - want).abs() > bound)
+    assert not bad.any(), (int(bad.sum()), float(((got - want).abs() - bound).max()))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "none", "edges"])
+@pytest.mark.parametrize("n,V,d", [(1, 1, 1), (5, 3, 7), (64, 1000, 16), (300, 40, 100), (1000, 70000, 33), (4096, 257, 64),
+                                   (4097, 1 << 20, 20), (9001, 5000, 130), (20000, 1023, 257)])
+def test_gradient(n, V, d, kind, accumulate):
+    gen = torch.Generator().manual_seed(n + V + d)
+    for tg, tt in ((torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+        say("gradient", n, V, d, kind, accumulate, tg, tt)
+        ids = make_ids(kind, n, V, gen)
+        grad = rows(n, d, tg, gen, pad=3, shift=1)
+        table = rows(V, d, tt, gen, pad=1)
+        before = table.cpu().clone()
+        work = torch.empty(ne.ne_embed_workspace_bytes(V, d, n), dtype=torch.uint8, device=DEV)
+        dev_ids = ids.to(DEV)
+        ne.ne_embed_grad(dev_ids, grad, table, work, scale=0.3, accumulate=accumulate)
+        check_grad(ids, grad, table, V, 0.3, accumulate, before)
+
+
+@pytest.mark.parametrize("n,V", [(262144, 200003), (262144, 3), (100000, 2 ** 31 - 1)])
+def test_gradient_of_many_positions(n, V):
+    """Three sorting passes, runs of a third of all positions, keys of 31 bits (only rows that are named are touched there)."""
+    gen = torch.Generator().manual_seed(5)
+    d = 4
+    say("many positions", n, V)
+    rows_there = min(V, 300000)
+    ids = make_ids("skewed", n, rows_there, gen)
+    grad = torch.randn(n, d, generator=gen).to(DEV)
+    table = torch.randn(rows_there, d, generator=gen).to(DEV)
+    before = table.cpu().clone()
+    work = torch.empty(ne.ne_embed_workspace_bytes(V, d, n), dtype=torch.uint8, device=DEV)
+    L = ne.lib()
+    dev_ids = ids.to(DEV)
+    rc = L.ne_embed_grad(dev_ids.data_ptr(), n, grad.data_ptr(), ne.NE_F32, d, 1.0, V, d, table.data_ptr(), ne.NE_F32, d, 1,
+                         work.data_ptr(), work.numel(), int(torch.cuda.current_stream().cuda_stream))
+    assert rc == ne.NE_OK
+    check_grad(ids, grad, table, rows_there, 1.0, True, before)
+
+
+def test_gradient_is_the_same_every_time_and_takes_nothing_from_unnamed_positions():
+    gen = torch.Generator().manual_seed(9)
+    n, V, d = 30000, 400, 96
+    ids = make_ids("edges", n, V, gen)
+    grad = torch.randn(n, d, generator=gen).to(DEV)
+    out = ((ids < 0) | (ids >= V)).to(DEV)
+    grad[out] = float("nan")
+    work = torch.empty(ne.ne_embed_workspace_bytes(V, d, n), dtype=torch.uint8, device=DEV)
+    first = None
+    for fill in (0, 255, 7):
+        work.fill_(fill)        # nothing of the workspace is read before it is written
+        table = torch.full((V, d), float("nan"), device=DEV)
+        ne.ne_embed_grad(ids.to(DEV), grad, table, work)
+        assert bool(torch.isfinite(table).all())
+        assert first is None or torch.equal(first, table)
+        first = table
+
+
+def test_gradient_of_one_row_shared_by_all_positions():
+    ids = torch.tensor([3, 1, 3, 3, -1], dtype=torch.int32, device=DEV)
+    one = torch.randn(1, 50, device=DEV)
+    table = torch.empty(5, 50, device=DEV)
+    work = torch.empty(ne.ne_embed_workspace_bytes(5, 50, 5), dtype=torch.uint8, device=DEV)
+    ne.ne_embed_grad(ids, one.expand(5, 50), table, work)
+    want = torch.zeros(5, 50, dtype=torch.float64)
+    want[1], want[3] = one[0].cpu().double(), 3 * one[0].cpu().double()
+    assert float((table.cpu().double() - want).abs().max()) <= 5 * 2.0 ** -24 * float(want.abs().max())
+
+
+def test_gradient_of_no_positions():
+    ids, grad = torch.empty(0, dtype=torch.int32, device=DEV), torch.empty(0, 12, device=DEV)
+    for dt in TYPES:
+        table = torch.ones(9, 12, dtype=dt, device=DEV)
+        ne.ne_embed_grad(ids, grad, table, None, accumulate=True)
+        assert bool((table == 1).all())
+        ne.ne_embed_grad(ids, grad, table, None)
+        assert bool((table == 0).all())
+
+
+def test_gradient_against_differences():
+    """The sum of weights times the lookup is linear in the table: its difference over a step of one element is the gradient."""
+    gen = torch.Generator().manual_seed(2)
+    V, d, n = 11, 6, 40
+    ids = make_ids("edges", n, V, gen).to(DEV)
+    weight = torch.randint(-4, 5, (n, d), generator=gen).float().to(DEV)      # whole numbers: every sum is exact
+    table = torch.randint(-8, 9, (V, d), generator=gen).float().to(DEV)
+    work = torch.empty(ne.ne_embed_workspace_bytes(V, d, n), dtype=torch.uint8, device=DEV)
+    grad = torch.empty(V, d, device=DEV)
+    ne.ne_embed_grad(ids, weight, grad, work, scale=2.0)
+
+    def value(t):
+        out = torch.empty(n, d, device=DEV)
+        ne.ne_embed_lookup(t, ids, out, scale=2.0)
+        return float((out.double() * weight.double()).sum())
+
+    base = value(table)
+    for r in range(V):
+        for c in range(d):
+            t = table.clone()
+            t[r, c] += 1.0
+            assert value(t) - base == float(grad[r, c])
+
+
+def test_on_a_stream_of_the_callers():
+    side = torch.cuda.Stream()
+    table = torch.randn(100, 64, device=DEV)
+    ids = torch.arange(100, dtype=torch.int32, device=DEV)
+    out = torch.empty(100, 64, device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    ne.ne_embed_lookup(table, ids, out, scale=math.pi, stream=side)
+    side.synchronize()
+    assert torch.equal(out, table * np.float32(math.pi))
