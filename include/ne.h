@@ -371,8 +371,8 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  *   scale         : finite; 1 / n for the mean over the rows.
  *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
  *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 1) bytes.
- * Precision: NE_BF16: products of bf16 values with fp32 sums; G is formed in fp32 and rounded to bf16 for its
- * products.  NE_F32: every operand is the sum of two halves in fp16 (22 bits, at a common power of two that the
+ * Precision: NE_BF16: products of bf16 values with fp32 sums; loss_grad[i] (exp(s - lse) - [v == target]) is formed in
+ * fp32 and rounded to bf16 for its products; scale is applied in fp32.  NE_F32: every operand is the sum of two halves in fp16 (22 bits, at a common power of two that the
  * largest finite magnitude sets), three products of halves with fp32 sums: errors as those of fp32 products, for
  * elements of at least 2^-24 of the largest magnitude of their matrix; what is smaller counts to 2^-39 of it.
  * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN; in a row of w, all losses.
@@ -394,7 +394,8 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
  * Parameters are fp32.  state_bits 32: m and v are float[n].  state_bits 8: every 256 elements of a tensor share
  * two scales (float, ceil(n / 256) each); m is 8-bit floating point (e4m3, no infinities) times m_scale, and v holds
- * sqrt(v) in the same form times v_scale; a scale is 1/448 of the block's largest magnitude (of 2^-100 at least).
+ * sqrt(v) in the same form times v_scale; a scale is the block's largest magnitude
+ * (2^-100 at least) times 1/448, and what is rounded are the values times (1/largest) * 448, each operation rounded to fp32.
  * Values are rounded at random, up with the probability that keeps their expectation (a step moves v by a
  * thousandth, which rounding to nearest at 3 bits would lose every time); sqrt(v) > 0 never becomes 0.  The random
  * bits of element e of tensor t: word e % 4 of Philox(key = seed, counter = (e / 4, t, step, 3)), its low 16 bits

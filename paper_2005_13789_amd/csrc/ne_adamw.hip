@@ -60,8 +60,8 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[4], const uint32_t
     for (int e = 0; e < 4; ++e) top_bits = max(top_bits, __float_as_uint(x[e]) & 0x7FFFFFFFu);
     top_bits = max(wave_max(top_bits), __float_as_uint(0x1p-100f));
     const float top = __uint_as_float(top_bits);
-    const float to = kTopE4m3 / top;
-    *scale = top / kTopE4m3;
+    const float to = (1.0f / top) * kTopE4m3;
+    *scale = top * (1.0f / kTopE4m3);
     float q[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -133,7 +133,6 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(StepArgs a)
     const ne_adamw_tensor t = a.tensors[unit.x];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float kept = 1.0f - t.weight_decay * a.lr;
-#pragma unroll 2
     for (int b = wave; b < kUnitBlocks; b += kThreads / 64) {
         const int64_t block = static_cast<int64_t>(unit.y) * kUnitBlocks + b;
         const int64_t at = block * kBlock + lane * 4;

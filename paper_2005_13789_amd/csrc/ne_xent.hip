@@ -1,7 +1,8 @@
 // Softmax cross entropy against a whole table, without keeping the scores: ne_xent_loss, ne_xent_grad.
 //
 //     S = H . W^T [n x V],   lse_i = log sum_v exp S_iv,   loss_i = lse_i - S_i,target
-//     G_iv = scale c_i (exp(S_iv - lse_i) - [v = target_i]),   dH = G . W,   dW = G^T . H
+//     G_iv = exp(S_iv - lse_i) - [v = target_i],   dH_i = scale c_i (G . W)_i,   dW = scale G^T . (c H)
+// (bf16: c_i is in G, which is rounded once; scale, the same for all, is applied in fp32 to the sums)
 //
 // Everything is a matrix product with something small around it, so one tile loop on the matrix cores serves all
 // three products; they differ in where their operands lie and in what becomes of the sums:
@@ -407,8 +408,7 @@ struct CoefArgs {
     const int32_t* targets;
     const int32_t* shift;
     const float* lse;
-    const float* c;                // bf16 only (fp32: applied to dH and to the rows of H)
-    float scale;                   // bf16 only
+    const float* c;                // bf16 only: NULL, or factors that G is rounded with (fp32: the rows of H have them)
     int64_t n, g_stride;
     uint32_t num_rows, row_base, row_tiles;
     int32_t steps;
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 2) coef_kernel(CoefArgs a)
         const uint32_t target = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
         const bool counts = target < a.num_rows;
         const float by = counts ? a.lse[token] * kLog2e : 0.0f;
-        const float c = P == 1 ? (counts ? a.scale * (a.c ? a.c[token] : 1.0f) : 0.0f) : 0x1p14f;
+        const float c = P == 2 ? 0x1p14f : counts && a.c ? a.c[token] : 1.0f;
 #pragma unroll
         for (int im = 0; im < 2; ++im)
 #pragma unroll
@@ -563,14 +563,14 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
 {
     const int lane = threadIdx.x & 63;
     const int64_t waves = static_cast<int64_t>(gridDim.x) * 4;
-    const int k = a.shift ? -(*a.shift + kGShift) : 0;
+    const int k = a.shift ? -(*a.shift + kGShift) : 0;      // (bf16: the sums are what they are)
     for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); r < a.rows; r += waves) {
         const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
         const float c = counts && a.c ? a.c[r] : 1.0f;
         for (int e = lane; e < a.dim; e += 64) {
             float sum = 0.0f;
             for (uint32_t s = 0; s < a.splits; ++s) sum += a.in[s * a.split_stride + r * a.cols + e];
-            if (a.shift) sum = ldexpf(sum, k) * a.scale * c;
+            sum = ldexpf(sum, k) * a.scale * c;
             static_cast<T*>(a.out)[r * a.out_stride + e] = from_float<T>(counts ? sum : 0.0f);
         }
     }
@@ -733,7 +733,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     hipError_t e = pack(x, w, true, &ca.h, &pa.h, &ca.w, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
-    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.c = x.c; ca.scale = scale; ca.n = x.n; ca.g_stride = w.piece;
+    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.c = x.c; ca.g_stride = w.piece;
     ca.num_rows = static_cast<uint32_t>(x.num_rows); ca.steps = w.padded / step_of<P>();
     const uint32_t token_tiles = static_cast<uint32_t>(w.tokens / kTile);
     pa.dh = w.dh; pa.dw = w.dw; pa.tokens = static_cast<uint32_t>(w.tokens); pa.piece_rows = static_cast<uint32_t>(w.piece);
@@ -780,7 +780,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     if (dh) {
         ReduceArgs r{};
         r.in = w.dh; r.split_stride = w.tokens * pa.cols; r.splits = w.h_splits; r.rows = x.n; r.out = dh; r.out_stride = dh_stride;
-        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = x.c; r.shift = w.shift;
+        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = P == 2 ? x.c : nullptr; r.shift = w.shift;
         return reduce(r);
     }
     return hipSuccess;

@@ -34,14 +34,14 @@ def at_random(x, r16, keep):
     full = np.zeros(blocks * BLOCK, F)
     full[:n] = x
     top = np.maximum(np.abs(full.reshape(blocks, BLOCK)).max(1), F(2.0 ** -100))
-    y = x * np.repeat(F(448.0) / top, BLOCK)[:n]
+    y = x * np.repeat((F(1.0) / top) * F(448.0), BLOCK)[:n]
     a = np.minimum(np.abs(y), F(448.0))
     big = ((a.view(np.uint32) + (r16.astype(np.uint32) << np.uint32(4))) & np.uint32(0xFFF00000)).view(F)
     small = np.floor(a * F(512.0) + r16.astype(F) * F(2.0 ** -16))
     if keep:
         small = np.where(a > 0, np.maximum(small, F(1.0)), small)
     q = np.where(a < F(2.0 ** -6), small * F(2.0 ** -9), big).astype(F)
-    return np.copysign(q, y), (top / F(448.0)).astype(F)
+    return np.copysign(q, y), (top * (F(1.0) / F(448.0))).astype(F)
 
 
 def one_step(p, g, m, v, wd, step, lr, b1, b2, eps, gs):
