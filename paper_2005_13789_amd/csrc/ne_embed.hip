@@ -18,15 +18,21 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunk = 16;          // sorted positions that are summed together where they name one row
 constexpr int kSuper = 256;         // the same, one size up
+constexpr int kSuperFrom = 131072;  // positions from which on that is a launch of its own (6 us); below, the longest runs have 8192 sums of 16
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortItems = 4;
 constexpr int kSortRound = kSortThreads * kSortItems;
 constexpr int kMostTiles = 128;     // workgroups of a sorting pass; each reads the counts of all
 constexpr int kMostDigits = 1024;
-constexpr int kSmallSort = 4096;    // ids that one workgroup sorts in LDS, in one launch
-constexpr int kSmallBits = 8;
 constexpr int kRowsPerGroup = 64;   // table rows of a workgroup of the rows launch
+constexpr int kFewIds = 16384;      // up to so many ids every workgroup looks through all of them
+constexpr int kFewThreads = 256;    // threads of a workgroup there
+constexpr int kScan = 16;           // ids of a thread and round there
+constexpr int kMostSlots = 256;     // rows of a workgroup there
+constexpr int kAddIds = 32;         // accumulate: positions of a workgroup there ...
+constexpr int kAddPlaces = 128;     // ... places of the hash table that finds their rows
+constexpr int kAddFilter = 1024;    // ... and words of the filter before it: a bit for each hash of 15 bits
 
 // ---------------------------------------------------------------------------------------------
 // lookup
@@ -87,9 +93,9 @@ struct SortArgs {
     const int32_t* ids;        // first pass
     const uint2* in;           // later passes
     uint2* out;
-    uint32_t* hist;            // [passes][tiles][digits]
+    uint32_t* hist;            // [tiles][digits]
     uint32_t n, num_rows, tile_len, tiles;
-    int32_t pass, passes, bits, shift;
+    int32_t pass, bits, shift;
 };
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t num_rows) { return min(static_cast<uint32_t>(id), num_rows); }
@@ -120,19 +126,19 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a)
 {
     __shared__ uint32_t count[kMostDigits];
     const uint32_t digits = 1u << a.bits, mask = digits - 1;
-    for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) {
-        count[d] = 0;
-        for (int p = 1; p < a.passes; ++p) a.hist[(static_cast<size_t>(p) * a.tiles + blockIdx.x) * digits + d] = 0;
-    }
+    for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
     __syncthreads();
     const uint32_t lo = blockIdx.x * a.tile_len, hi = min(lo + a.tile_len, a.n);
-    for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads) atomicAdd(&count[key_of(a.ids[i], a.num_rows) & mask], 1u);
+#pragma unroll 4
+    for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads)
+        atomicAdd(&count[((a.pass == 0 ? key_of(a.ids[i], a.num_rows) : a.in[i].x) >> a.shift) & mask], 1u);
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) a.hist[static_cast<size_t>(blockIdx.x) * digits + d] = count[d];
 }
 
-// Sum of all earlier threads' values (and of none of the later ones'); total over the workgroup in *total.
-__device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* wave_sums)
+// Sum of all earlier threads' values (and of none of the later ones'), THREADS of them.
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* wave_sums, uint32_t* total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t s = v;
@@ -142,14 +148,19 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* wave_sums
     }
     if (lane == 63) wave_sums[wave] = s;
     __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < wave; ++w) before += wave_sums[w];
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        const uint32_t u = wave_sums[w];
+        before += w < wave ? u : 0;
+        all += u;
+    }
+    *total = all;
     return before + s - v;
 }
 
 // One pass: where a tile's entries of a digit begin follows from the counts of all tiles, which each workgroup adds up
-// by itself (at most 128 x 1024 words, in L2); the next pass's counts are made with integer additions, whose order
-// changes nothing.
+// by itself (at most 128 x 1024 words, in L2: a launch less than with sums made in between).
 __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
 {
     __shared__ uint32_t base[kMostDigits];
@@ -157,29 +168,33 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
     __shared__ uint32_t wave_sums[kSortWaves];
     const uint32_t digits = 1u << a.bits, mask = digits - 1;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint32_t* hist = a.hist + static_cast<size_t>(a.pass) * a.tiles * digits;
     // thread t has digits 2t and 2t + 1
     uint32_t total[2] = {0, 0}, mine[2] = {0, 0};
-    for (int q = 0; q < 2; ++q) {
-        const uint32_t d = 2 * threadIdx.x + q;
-        if (d >= digits) break;
-        for (uint32_t t = 0; t < a.tiles; ++t) {
-            const uint32_t c = hist[static_cast<size_t>(t) * digits + d];
-            if (t < blockIdx.x) mine[q] += c;
-            total[q] += c;
+    if (2 * threadIdx.x < digits) {
+        const uint2* hist = reinterpret_cast<const uint2*>(a.hist) + threadIdx.x;
+        for (uint32_t t0 = 0; t0 < a.tiles; t0 += 16) {
+            uint2 c[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) c[q] = t0 + q < a.tiles ? hist[static_cast<size_t>(t0 + q) * (digits / 2)] : make_uint2(0, 0);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                total[0] += c[q].x;
+                total[1] += c[q].y;
+                if (t0 + q < blockIdx.x) {
+                    mine[0] += c[q].x;
+                    mine[1] += c[q].y;
+                }
+            }
         }
     }
-    const uint32_t before = block_prefix(total[0] + total[1], wave_sums);
+    uint32_t all;
+    const uint32_t before = block_prefix<kSortThreads>(total[0] + total[1], wave_sums, &all);
     if (2 * threadIdx.x < digits) {
         base[2 * threadIdx.x] = before + mine[0];
-        if (2 * threadIdx.x + 1 < digits) base[2 * threadIdx.x + 1] = before + total[0] + mine[1];
+        base[2 * threadIdx.x + 1] = before + total[0] + mine[1];
     }
-    uint32_t* next = a.hist + static_cast<size_t>(a.pass + 1) * a.tiles * digits;
     const uint32_t lo = blockIdx.x * a.tile_len, hi = min(lo + a.tile_len, a.n);
     for (uint32_t r0 = lo; r0 < hi; r0 += kSortRound) {
-        for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads)
-#pragma unroll
-            for (int w = 0; w < kSortWaves; ++w) count[w][d] = 0;
         uint2 e[kSortItems];
         uint32_t digit[kSortItems], rank[kSortItems];
         bool valid[kSortItems];
@@ -191,6 +206,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
             if (valid[j]) e[j] = a.pass == 0 ? make_uint2(key_of(a.ids[i], a.num_rows), i) : a.in[i];
             digit[j] = (e[j].x >> a.shift) & mask;
         }
+        for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads)
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) count[w][d] = 0;
         __syncthreads();
         wave_ranks<kSortItems>(digit, valid, a.bits, count[wave], rank);
         __syncthreads();
@@ -207,64 +225,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kSortItems; ++j)
-            if (valid[j]) {
-                const uint32_t to = count[wave][digit[j]] + rank[j];
-                a.out[to] = e[j];
-                if (a.pass + 1 < a.passes) atomicAdd(&next[static_cast<size_t>(to / a.tile_len) * digits + ((e[j].x >> (a.shift + a.bits)) & mask)], 1u);
-            }
-        __syncthreads();
-    }
-}
-
-// All passes of up to kSmallSort ids by one workgroup.
-__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a)
-{
-    __shared__ uint2 buf[2][kSmallSort];
-    __shared__ uint32_t count[kSortWaves][1 << kSmallBits];
-    __shared__ uint32_t wave_sums[kSortWaves];
-    constexpr int ITEMS = kSmallSort / kSortThreads;
-    const uint32_t digits = 1u << a.bits, mask = digits - 1;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint32_t per = (a.n + kSortThreads - 1) / kSortThreads;      // items of a lane; a wavefront's lie side by side
-    for (uint32_t i = threadIdx.x; i < a.n; i += kSortThreads) buf[0][i] = make_uint2(key_of(a.ids[i], a.num_rows), i);
-    for (int p = 0; p < a.passes; ++p) {
-        const int shift = p * a.bits;
-        for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads)
-#pragma unroll
-            for (int w = 0; w < kSortWaves; ++w) count[w][d] = 0;
-        __syncthreads();
-        uint2 e[ITEMS];
-        uint32_t digit[ITEMS], rank[ITEMS];
-        bool valid[ITEMS];
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            const uint32_t i = (static_cast<uint32_t>(wave) * per + j) * 64 + lane;
-            valid[j] = static_cast<uint32_t>(j) < per && i < a.n;
-            e[j] = valid[j] ? buf[p & 1][i] : make_uint2(0, 0);
-            digit[j] = (e[j].x >> shift) & mask;
-        }
-        wave_ranks<ITEMS>(digit, valid, a.bits, count[wave], rank);
-        __syncthreads();
-        uint32_t sum = 0;
-        if (threadIdx.x < digits)
-#pragma unroll
-            for (int w = 0; w < kSortWaves; ++w) sum += count[w][threadIdx.x];
-        uint32_t at = block_prefix(sum, wave_sums);
-        if (threadIdx.x < digits)
-#pragma unroll
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = count[w][threadIdx.x];
-                count[w][threadIdx.x] = at;
-                at += c;
-            }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j)
-            if (valid[j]) {
-                const uint32_t to = count[wave][digit[j]] + rank[j];
-                if (p + 1 < a.passes) buf[(p + 1) & 1][to] = e[j];
-                else a.out[to] = e[j];
-            }
+            if (valid[j]) a.out[count[wave][digit[j]] + rank[j]] = e[j];
         __syncthreads();
     }
 }
@@ -275,7 +236,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a)
 struct GradArgs {
     const uint2* sorted;
     const void* grad;
-    float* partial;            // [n / kChunk][dim]  sums of chunks that name one row; of 256 positions in the place of their first chunk
+    float* partial;            // [n / kChunk][dim]  sums of chunks that name one row
+    float* super;              // the same array's other half: sums of 256 positions, in the place of their first chunk
     void* table;
     int64_t grad_stride, table_stride;
     uint32_t n, num_rows;
@@ -290,21 +252,21 @@ struct Run {
     uint32_t terms;
 };
 
-__device__ __forceinline__ Run run_of(uint32_t s, uint32_t e)
+__device__ __forceinline__ Run run_of(uint32_t s, uint32_t e, bool supers)
 {
     Run r;
     r.s = s; r.e = e;
     r.c0 = min((s + kChunk - 1) / kChunk * kChunk, e);
     r.c1 = max(e / kChunk * kChunk, r.c0);
-    r.u0 = min((r.c0 + kSuper - 1) / kSuper * kSuper, r.c1);
+    r.u0 = supers ? min((r.c0 + kSuper - 1) / kSuper * kSuper, r.c1) : r.c1;
     r.u1 = max(r.c1 / kSuper * kSuper, r.u0);
     r.terms = (r.c0 - r.s) + (r.u0 - r.c0) / kChunk + (r.u1 - r.u0) / kSuper + (r.c1 - r.u1) / kChunk + (r.e - r.c1);
     return r;
 }
 
-// Adds term t of the run to acc.
-template <class TG, int V>
-__device__ __forceinline__ void load_term(const GradArgs& a, const Run& r, uint32_t t, int at, float (&x)[V])
+// Term t of the run.
+template <class TG, int V, class Position>
+__device__ __forceinline__ void load_term(const GradArgs& a, const Run& r, uint32_t t, int at, float (&x)[V], Position position)
 {
     uint32_t single = 0xFFFFFFFFu, chunk = 0;
     uint32_t k = r.c0 - r.s;
@@ -329,60 +291,69 @@ __device__ __forceinline__ void load_term(const GradArgs& a, const Run& r, uint3
         }
     }
     if (single != 0xFFFFFFFFu)
-        load_vec<TG, V>(static_cast<const TG*>(a.grad) + static_cast<int64_t>(a.sorted[single].y) * a.grad_stride + at, x);
+        load_vec<TG, V>(static_cast<const TG*>(a.grad) + static_cast<int64_t>(position(single)) * a.grad_stride + at, x);
     else
-        load_vec<float, V>(a.partial + static_cast<int64_t>(chunk) * a.dim + at, x);
+        load_vec<float, V>((r.u1 > r.u0 && chunk * kChunk >= r.u0 && chunk * kChunk < r.u1 ? a.super : a.partial) + static_cast<int64_t>(chunk) * a.dim + at, x);
 }
 
-// Every `step`-th term of a run from `t` on, four in flight.
-template <class TG, int V>
-__device__ __forceinline__ void sum_terms(const GradArgs& a, const Run& r, uint32_t t, uint32_t step, int at, float (&acc)[V])
+// Every `step`-th of `terms` terms from t on, added up, U in flight; term(t, x) gives one.
+template <int U, int V, class Term>
+__device__ __forceinline__ void sum_terms(uint32_t t, uint32_t terms, uint32_t step, float (&acc)[V], Term term)
 {
-    for (; t + 3 * step < r.terms; t += 4 * step) {
-        float x[4][V];
+    for (; t + (U - 1) * step < terms; t += U * step) {
+        float x[U][V];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load_term<TG, V>(a, r, t + q * step, at, x[q]);
+        for (int q = 0; q < U; ++q) term(t + q * step, x[q]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < U; ++q)
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] += x[q][e];
     }
-    for (; t < r.terms; t += step) {
-        float x[V];
-        load_term<TG, V>(a, r, t, at, x);
+    if (t < terms) {        // the last of them together, too
+        float x[U - 1][V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += x[e];
+        for (int q = 0; q < U - 1; ++q) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[q][e] = 0.0f;
+            if (t + q * step < terms) term(t + q * step, x[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < U - 1; ++q)
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] += x[q][e];
     }
 }
 
-// Writes scale * acc to chunk c of a row, added to what is there where it accumulates.  (The last chunk of a dim that V
-// does not divide overlaps the one before: an addition must not be made twice.)
+// What a row holds where a chunk of it will be added to.
+template <class TT, int V>
+__device__ __forceinline__ void load_old(const GradArgs& a, uint32_t row, int at, float (&x)[V])
+{
+    load_vec<TT, V>(static_cast<const TT*>(a.table) + static_cast<int64_t>(row) * a.table_stride + at, x);
+}
+
+// Writes scale * acc to chunk c of a row, ADD: added to what was there.  (The last chunk of a dim that V does not divide
+// overlaps the one before: an addition must not be made twice.)
 template <class TT, int V, bool ADD>
-__device__ __forceinline__ void write_chunk(const GradArgs& a, uint32_t row, int c, int at, const float (&acc)[V])
+__device__ __forceinline__ void write_chunk(const GradArgs& a, uint32_t row, int c, int at, const float (&acc)[V], const float (&old)[V])
 {
     TT* to = static_cast<TT*>(a.table) + static_cast<int64_t>(row) * a.table_stride + at;
     float x[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = ADD ? fmaf(a.scale, acc[e], old[e]) : a.scale * acc[e];
     if (ADD && at != c * V) {
 #pragma unroll
         for (int e = 0; e < V; ++e)
-            if (at + e >= c * V) {
-                load_vec<TT, 1>(to + e, *reinterpret_cast<float(*)[1]>(&x[e]));
-                x[e] = fmaf(a.scale, acc[e], x[e]);
-                store_vec<TT, 1>(to + e, *reinterpret_cast<const float(*)[1]>(&x[e]));
-            }
-        return;
+            if (at + e >= c * V) to[e] = from_float<TT>(x[e]);
+    } else {
+        store_vec<TT, V>(to, x);
     }
-    if (ADD) load_vec<TT, V>(to, x);
-#pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = ADD ? fmaf(a.scale, acc[e], x[e]) : a.scale * acc[e];
-    store_vec<TT, V>(to, x);
 }
 
 // Sum over the lane groups of a workgroup, in the groups' order, for group 0.
-template <int V>
+template <int THREADS, int V>
 __device__ __forceinline__ void join_groups(float (*lds)[V], int lanes_log2, float (&acc)[V])
 {
-    const int lanes = 1 << lanes_log2, groups = kThreads >> lanes_log2;
+    const int lanes = 1 << lanes_log2, groups = THREADS >> lanes_log2;
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) lds[threadIdx.x][e] = acc[e];
@@ -393,38 +364,113 @@ __device__ __forceinline__ void join_groups(float (*lds)[V], int lanes_log2, flo
             for (int e = 0; e < V; ++e) acc[e] += lds[threadIdx.x + g * lanes][e];
 }
 
-// Sums of 16 and of 256 sorted positions that name one row; a workgroup has 256 positions.
-template <class TG, int V>
-__global__ void __launch_bounds__(kThreads) chunk_sums_kernel(GradArgs a)
+// The rows [0, rows) of a workgroup, whose positions lie side by side: row r has those from start[r] to start[r + 1].  A lane
+// group has some neighbouring rows and goes through their positions eight at a time, whichever rows they are of (most rows have
+// none or one, and a fetch takes a microsecond: rows one after the other, four terms of each in flight, took 97 us where this
+// takes 66, 65 536 positions, 200 003 rows of 512 bf16).  Rows of kLongRun positions or more are summed by the
+// whole workgroup afterwards, from the terms of their run.
+//   none(r): leave row r alone;  single(k, at, x): position k's values;  term(r, t, at, x): term t of a long row, which has terms(r).
+constexpr uint32_t kLongRun = 32;
+
+template <int THREADS, class TT, int V, bool ADD, class None, class Single, class Terms, class Term, class Row>
+__device__ __forceinline__ void sum_rows(const GradArgs& a, uint32_t rows, const uint32_t* start, float (*lds)[V], None none, Single single, Terms terms,
+                                         Term term, Row row_of)
 {
-    __shared__ float lds[kThreads][V];
-    const uint32_t k0 = blockIdx.x * kSuper, end = min(k0 + kSuper, a.n);
-    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
-    const uint32_t key = a.sorted[k0].x;
-    if (key >= a.num_rows) return;
-    if (end == k0 + kSuper && a.sorted[end - 1].x == key) {
-        Run all;
-        all.s = k0; all.c0 = all.u0 = all.u1 = all.c1 = all.e = end; all.terms = kSuper;
+    constexpr int U = 8, OLD = ADD ? 4 : 1;
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = THREADS >> a.lanes_log2;
+    const uint32_t share = (rows + groups - 1) / groups, begin = min(group * share, rows), end = min(begin + share, rows);
+    auto skip = [&](uint32_t r) { return start[r + 1] - start[r] >= kLongRun || none(r); };
+    for (int c = lane; c < a.chunks; c += lanes) {
+        const int at = min(c * V, a.dim - V);
+        for (uint32_t r = begin; r < end;) {
+            if (skip(r)) { ++r; continue; }
+            uint32_t last = r + 1;
+            while (last < end && !skip(last) && (!ADD || last < r + OLD)) ++last;
+            const uint32_t stop = start[last];
+            uint32_t k = start[r], next = start[r + 1];
+            float acc[V] = {}, old[OLD][V] = {};        // (old: of the rows still to be written, the next one first)
+            if (ADD)
+#pragma unroll
+                for (int q = 0; q < OLD; ++q)
+                    if (r + q < last) load_old<TT, V>(a, row_of(r + q), at, old[q]);
+            auto finish_row = [&]() {
+                write_chunk<TT, V, ADD>(a, row_of(r), c, at, acc, old[0]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    acc[e] = 0.0f;
+#pragma unroll
+                    for (int q = 0; q + 1 < OLD; ++q) old[q][e] = old[q + 1][e];
+                }
+                ++r;
+                next = start[min(r + 1, rows)];
+            };
+            for (; k < stop; k += U) {
+                float x[U][V];
+#pragma unroll
+                for (int q = 0; q < U; ++q)
+                    if (k + q < stop) single(k + q, at, x[q]);
+#pragma unroll
+                for (int q = 0; q < U; ++q)
+                    if (k + q < stop) {
+                        while (k + q >= next) finish_row();
+#pragma unroll
+                        for (int e = 0; e < V; ++e) acc[e] += x[q][e];
+                    }
+            }
+            while (r < last) finish_row();
+        }
+    }
+    for (uint32_t r = 0; r < rows; ++r) {
+        if (start[r + 1] - start[r] < kLongRun || none(r)) continue;
         for (int c0 = 0; c0 < a.chunks; c0 += lanes) {
             const int c = c0 + lane, at = min(min(c, a.chunks - 1) * V, a.dim - V);
             float acc[V] = {};
-            sum_terms<TG, V>(a, all, group, groups, at, acc);
-            join_groups<V>(lds, a.lanes_log2, acc);
-            if (group == 0 && c < a.chunks) store_vec<float, V>(a.partial + static_cast<int64_t>(k0 / kChunk) * a.dim + at, acc);
+            sum_terms<U, V>(group, terms(r), groups, acc, [&](uint32_t t, float (&x)[V]) { term(r, t, at, x); });
+            join_groups<THREADS, V>(lds, a.lanes_log2, acc);
+            if (group == 0 && c < a.chunks) {
+                float old[V] = {};
+                if (ADD) load_old<TT, V>(a, row_of(r), at, old);
+                write_chunk<TT, V, ADD>(a, row_of(r), c, at, acc, old);
+            }
         }
-        return;
     }
-    for (uint32_t k = k0 + group * kChunk; k + kChunk <= end; k += groups * kChunk) {
-        const uint32_t row = a.sorted[k].x;
-        if (row >= a.num_rows || a.sorted[k + kChunk - 1].x != row) continue;
-        Run all;
-        all.s = k; all.c0 = all.u0 = all.u1 = all.c1 = all.e = k + kChunk; all.terms = kChunk;
-        for (int c = lane; c < a.chunks; c += lanes) {
-            const int at = min(c * V, a.dim - V);
-            float acc[V] = {};
-            sum_terms<TG, V>(a, all, 0, 1, at, acc);
-            store_vec<float, V>(a.partial + static_cast<int64_t>(k / kChunk) * a.dim + at, acc);
-        }
+}
+
+// Sums of 16 sorted positions that name one row; a lane group has 16 positions, all of whose rows are in flight at once.
+template <class TG, int V>
+__global__ void __launch_bounds__(kThreads) chunk_sums_kernel(GradArgs a)
+{
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+    const uint32_t chunk = blockIdx.x * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    if (chunk >= a.n / kChunk) return;
+    const uint32_t k = chunk * kChunk, row = a.sorted[k].x;
+    if (row >= a.num_rows || a.sorted[k + kChunk - 1].x != row) return;
+    for (int c = lane; c < a.chunks; c += lanes) {
+        const int at = min(c * V, a.dim - V);
+        float acc[V] = {};
+        sum_terms<kChunk, V>(0, kChunk, 1, acc, [&](uint32_t t, float (&x)[V]) {
+            load_vec<TG, V>(static_cast<const TG*>(a.grad) + static_cast<int64_t>(a.sorted[k + t].y) * a.grad_stride + at, x);
+        });
+        store_vec<float, V>(a.partial + static_cast<int64_t>(chunk) * a.dim + at, acc);
+    }
+}
+
+// The same for 16 such sums, of 256 positions that name one row.
+template <int V>
+__global__ void __launch_bounds__(kThreads) super_sums_kernel(GradArgs a)
+{
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+    const uint32_t group = blockIdx.x * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    if (group >= a.n / kSuper) return;
+    const uint32_t k = group * kSuper, row = a.sorted[k].x;
+    if (row >= a.num_rows || a.sorted[k + kSuper - 1].x != row) return;
+    for (int c = lane; c < a.chunks; c += lanes) {
+        const int at = min(c * V, a.dim - V);
+        float acc[V] = {};
+        sum_terms<kSuper / kChunk, V>(0, kSuper / kChunk, 1, acc, [&](uint32_t t, float (&x)[V]) {
+            load_vec<float, V>(a.partial + static_cast<int64_t>(k / kChunk + t) * a.dim + at, x);
+        });
+        store_vec<float, V>(a.super + static_cast<int64_t>(k / kChunk) * a.dim + at, acc);
     }
 }
 
@@ -440,7 +486,22 @@ __device__ __forceinline__ uint32_t lower_bound(const uint2* sorted, uint32_t n,
     return lo;
 }
 
-constexpr uint32_t kLongRun = 64;   // terms from which on a run is summed by the whole workgroup
+// The same by a whole wavefront: 64 probes at a time, three rounds of them for 2^18 positions (each waits for memory, as
+// the positions come from the launch before: 17 rounds of single probes are 17 times a microsecond).
+__device__ __forceinline__ uint32_t wave_lower_bound(const uint2* sorted, uint32_t n, uint32_t key)
+{
+    uint32_t lo = 0, len = n;
+    while (len) {
+        const uint32_t step = (len + 63) / 64, at = lo + (threadIdx.x & 63) * step + step - 1;
+        const uint32_t below = __popcll(__ballot(at < lo + len && sorted[at].x < key));
+        const uint32_t next = lo + below * step;
+        len = min(step - 1, lo + len - next);
+        lo = next;
+    }
+    return lo;
+}
+
+constexpr uint32_t kKeysInLds = 1024;   // positions of a workgroup whose keys fit there
 
 // The rows launch.  ADD: a workgroup has 64 sorted positions and writes the rows whose runs begin there; otherwise it has
 // 64 rows and writes them all.
@@ -448,14 +509,15 @@ template <class TG, class TT, int V, bool ADD>
 __global__ void __launch_bounds__(kThreads) rows_kernel(GradArgs a)
 {
     __shared__ float lds[kThreads][V];
-    __shared__ uint32_t start[kRowsPerGroup + 1], key[kRowsPerGroup];
-    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
+    __shared__ uint32_t start[kRowsPerGroup + 1], key[ADD ? kRowsPerGroup : kKeysInLds], place[ADD ? 1 : kKeysInLds], bounds[2];
+    const int wave = threadIdx.x >> 6;
+    uint32_t lo = 0, len = 0xFFFFFFFFu;
     const uint32_t first = blockIdx.x * kRowsPerGroup;
     uint32_t rows;
     if (ADD) {
         // the runs that begin in [first, first + 64), side by side; the last one's end is looked for
         const uint32_t k = first + threadIdx.x;
-        const int in = threadIdx.x < kRowsPerGroup && k < a.n;
+        const bool in = threadIdx.x < kRowsPerGroup && k < a.n;
         const uint32_t mine = in ? a.sorted[k].x : 0xFFFFFFFFu;
         const bool begins = in && mine < a.num_rows && (k == 0 || a.sorted[k - 1].x != mine);
         const uint64_t all = __ballot(begins);
@@ -468,35 +530,196 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(GradArgs a)
         rows = start[kRowsPerGroup];
         __syncthreads();
         if (rows == 0) return;
-        if (threadIdx.x == 0) start[rows] = lower_bound(a.sorted, a.n, key[rows - 1] + 1);
+        if (wave == 0) {
+            const uint32_t end = wave_lower_bound(a.sorted, a.n, key[rows - 1] + 1);
+            if (threadIdx.x == 0) start[rows] = end;
+        }
     } else {
         rows = min(static_cast<uint32_t>(kRowsPerGroup), a.num_rows - first);
-        if (threadIdx.x <= rows) start[threadIdx.x] = lower_bound(a.sorted, a.n, first + threadIdx.x);
+        if (wave < 2) {
+            const uint32_t at = wave_lower_bound(a.sorted, a.n, first + wave * rows);
+            if ((threadIdx.x & 63) == 0) bounds[wave] = at;
+        }
+        __syncthreads();
+        lo = bounds[0];
+        len = bounds[1] - lo;
+        if (len <= kKeysInLds) {
+            for (uint32_t i = threadIdx.x; i < len; i += kThreads) {
+                const uint2 e = a.sorted[lo + i];
+                key[i] = e.x;
+                place[i] = e.y;
+            }
+            __syncthreads();
+            if (threadIdx.x <= rows) {
+                uint32_t at = 0, left = len;
+                while (left) {
+                    const uint32_t half = left >> 1;
+                    if (key[at + half] < first + threadIdx.x) { at += half + 1; left -= half + 1; }
+                    else left = half;
+                }
+                start[threadIdx.x] = lo + at;
+            }
+        } else if (threadIdx.x <= rows) {
+            start[threadIdx.x] = lo + lower_bound(a.sorted + lo, len, first + threadIdx.x);
+        }
     }
     __syncthreads();
-    for (uint32_t r = group; r < rows; r += groups) {
-        const Run run = run_of(start[r], start[r + 1]);
-        if (run.terms >= kLongRun) continue;
-        const uint32_t row = ADD ? key[r] : first + r;
-        for (int c = lane; c < a.chunks; c += lanes) {
-            const int at = min(c * V, a.dim - V);
-            float acc[V] = {};
-            sum_terms<TG, V>(a, run, 0, 1, at, acc);
-            write_chunk<TT, V, ADD>(a, row, c, at, acc);
+    auto position = [&](uint32_t k) { return !ADD && len <= kKeysInLds ? place[k - lo] : a.sorted[k].y; };
+    const TG* grad = static_cast<const TG*>(a.grad);
+    sum_rows<kThreads, TT, V, ADD>(
+        a, rows, start, lds, [](uint32_t) { return false; },
+        [&](uint32_t k, int at, float (&x)[V]) { load_vec<TG, V>(grad + static_cast<int64_t>(position(k)) * a.grad_stride + at, x); },
+        [&](uint32_t r) { return run_of(start[r], start[r + 1], a.super != nullptr).terms; },
+        [&](uint32_t r, uint32_t t, int at, float (&x)[V]) { load_term<TG, V>(a, run_of(start[r], start[r + 1], a.super != nullptr), t, at, x, position); },
+        [&](uint32_t r) { return ADD ? key[r] : first + r; });
+}
+
+// ---------------------------------------------------------------------------------------------
+// few ids: one launch, no sorting of all of them
+// ---------------------------------------------------------------------------------------------
+// Every workgroup looks through all ids (they are in L2 after the first) for those that name one of its rows: its range of
+// rows, or with ADD the rows that 32 positions are the first to name.  What it finds lies in LDS in the order of the positions and is
+// sorted there by row (stably), so the order of a row's terms is that of the sorting path.
+struct FewArgs {
+    GradArgs g;
+    const int32_t* ids;
+    uint32_t slots;            // rows of a workgroup; a power of two
+    int32_t slot_bits;
+};
+
+template <class TG, class TT, int V, bool ADD>
+__global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
+{
+    extern __shared__ uint32_t found[];        // [n rounded up]  slot << 16 | position; behind them [n] positions by slot (16 bits)
+    __shared__ float lds[kFewThreads][V];
+    __shared__ uint32_t count[kFewThreads / 64][kMostSlots], wave_sums[kFewThreads / 64];
+    __shared__ uint32_t start[kMostSlots + 1];
+    // ADD: the ids of the places and the slots that they have, the slots' ids, and whether an earlier workgroup has them
+    __shared__ uint32_t place_id[ADD ? kAddPlaces : 1], owner[ADD ? kAddIds : 1], taken[ADD ? kAddIds : 1], slots_used;
+    __shared__ uint8_t place_slot[ADD ? kAddPlaces : 1];
+    __shared__ uint32_t filter[ADD ? kAddFilter : 1];
+    const GradArgs& a = f.g;
+    uint16_t* sorted = reinterpret_cast<uint16_t*>(found + ((a.n + 1) & ~1u));
+    const uint32_t first = ADD ? blockIdx.x * kAddIds : blockIdx.x * f.slots;
+    const int wave = threadIdx.x >> 6, lane64 = threadIdx.x & 63;
+    if (ADD) {
+        for (uint32_t i = threadIdx.x; i < kAddPlaces; i += kFewThreads) place_id[i] = 0xFFFFFFFFu;
+        for (uint32_t i = threadIdx.x; i < kAddFilter; i += kFewThreads) filter[i] = 0;
+        if (threadIdx.x < kAddIds) taken[threadIdx.x] = 0;
+        if (threadIdx.x == 0) slots_used = 0;
+        __syncthreads();
+        if (threadIdx.x < kAddIds && first + threadIdx.x < a.n) {
+            const uint32_t id = static_cast<uint32_t>(f.ids[first + threadIdx.x]);
+            if (id < a.num_rows)
+                for (uint32_t at = hash_position(id, kAddPlaces - 1);; at = (at + 1) & (kAddPlaces - 1)) {
+                    const uint32_t was = atomicCAS(&place_id[at], 0xFFFFFFFFu, id);
+                    if (was == 0xFFFFFFFFu) {       // (which slot an id gets changes nothing)
+                        const uint32_t slot = atomicAdd(&slots_used, 1u);
+                        place_slot[at] = static_cast<uint8_t>(slot);
+                        owner[slot] = id;
+                        const uint32_t bit = hash_position(id, 32 * kAddFilter - 1);
+                        atomicOr(&filter[bit >> 5], 1u << (bit & 31));
+                    }
+                    if (was == 0xFFFFFFFFu || was == id) break;
+                }
+        }
+        __syncthreads();
+    }
+    uint32_t have = 0;
+    uint32_t ahead[kScan];      // the next round's ids travel during a round
+    auto fetch_ids = [&](uint32_t at) {
+        if (at + kScan <= a.n) {
+#pragma unroll
+            for (int q = 0; q < kScan; q += 4) __builtin_memcpy(&ahead[q], f.ids + at + q, 16);
+        } else {
+#pragma unroll
+            for (int q = 0; q < kScan; ++q) ahead[q] = at + q < a.n ? static_cast<uint32_t>(f.ids[at + q]) : 0xFFFFFFFFu;
+        }
+    };
+    fetch_ids(threadIdx.x * kScan);
+    for (uint32_t r0 = 0; r0 < a.n; r0 += kFewThreads * kScan) {
+        uint32_t id[kScan];
+        const uint32_t at = r0 + threadIdx.x * kScan;
+#pragma unroll
+        for (int q = 0; q < kScan; ++q) id[q] = ahead[q];
+        if (r0 + kFewThreads * kScan < a.n) fetch_ids(at + kFewThreads * kScan);
+        uint32_t wanted = 0, word[kScan];
+        if (ADD)
+#pragma unroll
+            for (int q = 0; q < kScan; ++q) word[q] = filter[hash_position(id[q], 32 * kAddFilter - 1) >> 5];
+#pragma unroll
+        for (int q = 0; q < kScan; ++q) {
+            const bool in = id[q] < a.num_rows && (ADD ? word[q] >> (hash_position(id[q], 32 * kAddFilter - 1) & 31) & 1 : id[q] - first < f.slots);
+            wanted |= static_cast<uint32_t>(in) << q;
+        }
+        uint32_t total;
+        uint32_t to = have + block_prefix<kFewThreads>(__popc(wanted), wave_sums, &total);
+#pragma unroll
+        for (int q = 0; q < kScan; ++q)
+            if (wanted >> q & 1) found[to++] = (ADD ? 0 : (id[q] - first) << 16) | (at + q);
+        have += total;
+        __syncthreads();
+    }
+    if (ADD) {      // what passed the filter is looked up; slot kAddIds takes what has no row here, or stands before all of this workgroup's
+        for (uint32_t i = threadIdx.x; i < have; i += kFewThreads) {
+            const uint32_t k = found[i], id = static_cast<uint32_t>(f.ids[k]);
+            uint32_t slot = kAddIds;
+            for (uint32_t at = hash_position(id, kAddPlaces - 1);; at = (at + 1) & (kAddPlaces - 1)) {
+                const uint32_t o = place_id[at];
+                if (o == id) slot = place_slot[at];
+                if (o == id || o == 0xFFFFFFFFu) break;
+            }
+            if (k < first && slot != kAddIds) {
+                taken[slot] = 1;
+                slot = kAddIds;
+            }
+            found[i] = slot << 16 | k;
+        }
+        __syncthreads();
+    }
+    // stable sort by slot: counts of every wavefront's share, then places
+    const uint32_t share = (have + kFewThreads - 1) / kFewThreads * 64;      // entries of a wavefront, side by side
+    for (uint32_t i = threadIdx.x; i < kMostSlots; i += kFewThreads)
+#pragma unroll
+        for (int w = 0; w < kFewThreads / 64; ++w) count[w][i] = 0;
+    __syncthreads();
+    for (uint32_t i = wave * share + lane64; i < min((wave + 1) * share, have); i += 64) atomicAdd(&count[wave][found[i] >> 16], 1u);
+    __syncthreads();
+    {
+        const bool has_slot = threadIdx.x < kMostSlots;
+        uint32_t sum = 0, total;
+        if (has_slot)
+#pragma unroll
+            for (int w = 0; w < kFewThreads / 64; ++w) sum += count[w][threadIdx.x];
+        uint32_t at = block_prefix<kFewThreads>(sum, wave_sums, &total);
+        if (threadIdx.x == 0) start[kMostSlots] = total;
+        if (has_slot) {
+            start[threadIdx.x] = at;
+#pragma unroll
+            for (int w = 0; w < kFewThreads / 64; ++w) {
+                const uint32_t c = count[w][threadIdx.x];
+                count[w][threadIdx.x] = at;
+                at += c;
+            }
         }
     }
-    for (uint32_t r = 0; r < rows; ++r) {
-        const Run run = run_of(start[r], start[r + 1]);
-        if (run.terms < kLongRun) continue;
-        const uint32_t row = ADD ? key[r] : first + r;
-        for (int c0 = 0; c0 < a.chunks; c0 += lanes) {
-            const int c = c0 + lane, at = min(min(c, a.chunks - 1) * V, a.dim - V);
-            float acc[V] = {};
-            sum_terms<TG, V>(a, run, group, groups, at, acc);
-            join_groups<V>(lds, a.lanes_log2, acc);
-            if (group == 0 && c < a.chunks) write_chunk<TT, V, ADD>(a, row, c, at, acc);
-        }
+    __syncthreads();
+    for (uint32_t i0 = wave * share; i0 < min((wave + 1) * share, have); i0 += 64) {
+        const bool valid[1] = {i0 + lane64 < min((wave + 1) * share, have)};
+        const uint32_t e = valid[0] ? found[i0 + lane64] : 0;
+        const uint32_t digit[1] = {e >> 16};
+        uint32_t rank[1];
+        wave_ranks<1>(digit, valid, f.slot_bits, count[wave], rank);
+        if (valid[0]) sorted[rank[0]] = static_cast<uint16_t>(e);
     }
+    __syncthreads();
+    auto single = [&](uint32_t k, int at, float (&x)[V]) {
+        load_vec<TG, V>(static_cast<const TG*>(a.grad) + static_cast<int64_t>(sorted[k]) * a.grad_stride + at, x);
+    };
+    sum_rows<kFewThreads, TT, V, ADD>(
+        a, ADD ? slots_used : min(f.slots, a.num_rows - first), start, lds, [&](uint32_t r) { return ADD && taken[r]; }, single,
+        [&](uint32_t r) { return start[r + 1] - start[r]; },
+        [&](uint32_t r, uint32_t t, int at, float (&x)[V]) { single(start[r] + t, at, x); }, [&](uint32_t r) { return ADD ? owner[r] : first + r; });
 }
 
 // Writes zeros: the gradient of no positions.
@@ -514,11 +737,14 @@ __global__ void __launch_bounds__(kThreads) zero_rows_kernel(TT* table, int64_t 
 struct EmbedWs {
     uint2* entries[2];
     uint32_t* hist;
-    float* partial;
+    float *partial, *super;
     uint32_t tiles, tile_len;
     int32_t passes, bits;
     size_t total;
 };
+
+// Whether every workgroup looks through all ids: few of them, and no fewer rows than share them among enough workgroups.
+bool few_ids(int64_t num_rows, int64_t n) { return n <= kFewIds && n <= 16 * num_rows; }
 
 bool sizes_ok(int64_t num_rows, int32_t dim, int64_t n)
 {
@@ -530,19 +756,21 @@ EmbedWs embed_layout(int64_t num_rows, int32_t dim, int64_t n, char* base)
     EmbedWs w{};
     int key_bits = 1;
     while ((num_rows >> key_bits) != 0) key_bits += 1;      // keys are 0 .. num_rows
-    const int most = n <= kSmallSort ? kSmallBits : 10;
-    w.passes = (key_bits + most - 1) / most;
+    w.passes = (key_bits + 9) / 10;
     w.bits = (key_bits + w.passes - 1) / w.passes;
     int64_t len = (n + kMostTiles - 1) / kMostTiles;
     len = std::max<int64_t>((len + kSortRound - 1) / kSortRound * kSortRound, kSortRound);
     w.tile_len = static_cast<uint32_t>(len);
     w.tiles = static_cast<uint32_t>((n + len - 1) / len);
     Carver take{base};
-    w.entries[0] = take.get<uint2>(static_cast<size_t>(n));
-    w.entries[1] = take.get<uint2>(n > kSmallSort ? static_cast<size_t>(n) : 0);
-    w.hist = take.get<uint32_t>(n > kSmallSort ? (static_cast<size_t>(w.passes) * w.tiles) << w.bits : 0);
-    w.partial = take.get<float>(static_cast<size_t>((n + kChunk - 1) / kChunk) * dim);
-    w.total = take.total();
+    if (!few_ids(num_rows, n)) {
+        w.entries[0] = take.get<uint2>(static_cast<size_t>(n));
+        w.entries[1] = take.get<uint2>(static_cast<size_t>(n));
+        w.hist = take.get<uint32_t>(static_cast<size_t>(w.tiles) << w.bits);
+        w.partial = take.get<float>(static_cast<size_t>(n / kChunk) * dim);
+        if (n > kSuperFrom) w.super = take.get<float>(static_cast<size_t>(n / kChunk) * dim);
+    }
+    w.total = std::max<size_t>(take.total(), 256);
     return w;
 }
 
@@ -554,11 +782,34 @@ int lanes_log2_for(int chunks)
 }
 
 template <class TG, class TT, int V>
-hipError_t launch_grad(const GradArgs& a, bool add, hipStream_t st)
+hipError_t launch_few(const GradArgs& a, const int32_t* ids, bool add, hipStream_t st)
 {
-    if (a.n >= kChunk) {
-        hipLaunchKernelGGL((chunk_sums_kernel<TG, V>), dim3((a.n + kSuper - 1) / kSuper), dim3(kThreads), 0, st, a);
-        const hipError_t e = hipGetLastError();
+    FewArgs f{a, ids, 0, 0};
+    const size_t lds = static_cast<size_t>((a.n + 1) & ~1u) * 4 + static_cast<size_t>(a.n) * 2;
+    if (add) {
+        f.slots = kAddIds;
+    } else {        // as many rows as make about 512 workgroups: each looks through all ids
+        f.slots = 32;
+        while (f.slots < kMostSlots && a.num_rows / f.slots > 512) f.slots *= 2;
+    }
+    while ((1u << f.slot_bits) < f.slots + (add ? 1 : 0)) f.slot_bits += 1;
+    const uint32_t blocks = add ? (a.n + kAddIds - 1) / kAddIds : (a.num_rows + f.slots - 1) / f.slots;
+    if (add) hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, true>), dim3(blocks), dim3(kFewThreads), lds, st, f);
+    else hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, false>), dim3(blocks), dim3(kFewThreads), lds, st, f);
+    return hipGetLastError();
+}
+
+template <class TG, class TT, int V>
+hipError_t launch_grad(const GradArgs& a, const int32_t* ids, bool add, hipStream_t st)
+{
+    if (few_ids(a.num_rows, a.n)) return launch_few<TG, TT, V>(a, ids, add, st);
+    const uint32_t groups = kThreads >> a.lanes_log2;
+    hipLaunchKernelGGL((chunk_sums_kernel<TG, V>), dim3((a.n / kChunk + groups - 1) / groups), dim3(kThreads), 0, st, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.super) {
+        hipLaunchKernelGGL((super_sums_kernel<V>), dim3((a.n / kSuper + groups - 1) / groups), dim3(kThreads), 0, st, a);
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (add)
@@ -569,13 +820,13 @@ hipError_t launch_grad(const GradArgs& a, bool add, hipStream_t st)
 }
 
 template <class TG, class TT>
-hipError_t launch_grad_dim(GradArgs a, bool add, hipStream_t st)
+hipError_t launch_grad_dim(GradArgs a, const int32_t* ids, bool add, hipStream_t st)
 {
     constexpr int V = vec_of<TG, TT>();
     const bool wide = a.dim >= V;
     a.chunks = wide ? (a.dim + V - 1) / V : a.dim;
     a.lanes_log2 = lanes_log2_for(a.chunks);
-    return wide ? launch_grad<TG, TT, V>(a, add, st) : launch_grad<TG, TT, 1>(a, add, st);
+    return wide ? launch_grad<TG, TT, V>(a, ids, add, st) : launch_grad<TG, TT, 1>(a, ids, add, st);
 }
 
 template <class TI, class TO>
@@ -596,20 +847,16 @@ hipError_t launch_sort(const EmbedWs& w, const int32_t* ids, int64_t n, int64_t 
 {
     SortArgs s{};
     s.ids = ids; s.hist = w.hist; s.n = static_cast<uint32_t>(n); s.num_rows = static_cast<uint32_t>(num_rows);
-    s.tile_len = w.tile_len; s.tiles = w.tiles; s.passes = w.passes; s.bits = w.bits;
-    if (n <= kSmallSort) {
-        s.out = w.entries[0];
-        *sorted = w.entries[0];
-        hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSortThreads), 0, st, s);
-        return hipGetLastError();
-    }
-    hipLaunchKernelGGL(sort_count_kernel, dim3(w.tiles), dim3(kSortThreads), 0, st, s);
-    hipError_t e = hipGetLastError();
+    s.tile_len = w.tile_len; s.tiles = w.tiles; s.bits = w.bits;
+    hipError_t e = hipSuccess;
     for (int p = 0; p < w.passes && e == hipSuccess; ++p) {
         s.pass = p; s.shift = p * w.bits;
         s.in = w.entries[(p + 1) & 1];
         s.out = w.entries[p & 1];
         *sorted = s.out;
+        hipLaunchKernelGGL(sort_count_kernel, dim3(w.tiles), dim3(kSortThreads), 0, st, s);
+        e = hipGetLastError();
+        if (e != hipSuccess) break;
         hipLaunchKernelGGL(sort_pass_kernel, dim3(w.tiles), dim3(kSortThreads), 0, st, s);
         e = hipGetLastError();
     }
@@ -677,13 +924,13 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
         return fail(NE_ERR_ARG, "ne_embed_grad: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_embed_workspace_bytes()");
     GradArgs a{};
-    hipError_t e = launch_sort(w, ids_dev, n, num_rows, &a.sorted, st);
+    hipError_t e = few_ids(num_rows, n) ? hipSuccess : launch_sort(w, ids_dev, n, num_rows, &a.sorted, st);
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("sort launch: ") + hipGetErrorString(e));
-    a.grad = grad_dev; a.partial = w.partial; a.table = table_grad_dev; a.grad_stride = grad_stride; a.table_stride = table_grad_stride;
+    a.grad = grad_dev; a.partial = w.partial; a.super = w.super; a.table = table_grad_dev; a.grad_stride = grad_stride; a.table_stride = table_grad_stride;
     a.n = static_cast<uint32_t>(n); a.num_rows = static_cast<uint32_t>(num_rows); a.dim = dim; a.scale = scale;
     const bool add = accumulate != 0;
-    e = grad_type == NE_F32 ? (table_grad_type == NE_F32 ? launch_grad_dim<float, float>(a, add, st) : launch_grad_dim<float, bf16_t>(a, add, st))
-                            : (table_grad_type == NE_F32 ? launch_grad_dim<bf16_t, float>(a, add, st) : launch_grad_dim<bf16_t, bf16_t>(a, add, st));
+    e = grad_type == NE_F32 ? (table_grad_type == NE_F32 ? launch_grad_dim<float, float>(a, ids_dev, add, st) : launch_grad_dim<float, bf16_t>(a, ids_dev, add, st))
+                            : (table_grad_type == NE_F32 ? launch_grad_dim<bf16_t, float>(a, ids_dev, add, st) : launch_grad_dim<bf16_t, bf16_t>(a, ids_dev, add, st));
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("embedding gradient launch: ") + hipGetErrorString(e));
     return NE_OK;
 }
