@@ -38,6 +38,9 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kPadDim = 64;            // packed rows are a multiple of this, filled with zeros
 constexpr int kSlots = 512;            // workgroups that run at once: 256 CUs, two each
 constexpr int kAmaxBlocks = 256;
+constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
+constexpr int kFewBytes = 65536;
+constexpr int kFewGroups = 1024;
 constexpr size_t kGBytes = size_t{128} << 20;      // G of one piece
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
@@ -274,9 +277,17 @@ struct ScoreArgs {
     int64_t n;
     uint32_t num_rows, row_tiles, splits, tokens;   // tokens: padded n
     int32_t steps;                 // stages of a tile
-    float2* stat;                  // [splits][tokens]  maximum and sum, in powers of two
+    float2* stat;                  // [tokens][splits]  maximum and sum, in powers of two
     float* target_score;           // [tokens]
 };
+
+// A softmax's maximum and sum, in powers of two, joined with those of other scores.
+__device__ __forceinline__ void join_stat(float& top, float& sum, float2 other)
+{
+    const float now = fmaxf(top, other.x), by = now == -INFINITY ? 0.0f : now;      // (nothing seen yet but scores of minus infinity)
+    sum = sum * __builtin_amdgcn_exp2f(top - by) + other.y * __builtin_amdgcn_exp2f(other.x - by);
+    top = now;
+}
 
 template <int P>
 __device__ __forceinline__ float score_factor(const int32_t* shift)
@@ -361,43 +372,183 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
     float2* join = reinterpret_cast<float2*>(lds[0]);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const float other = __shfl_xor(top[j], 32, 64), other_sum = __shfl_xor(sum[j], 32, 64);
-        const float now = fmaxf(top[j], other), by = now == -INFINITY ? 0.0f : now;
-        sum[j] = sum[j] * __builtin_amdgcn_exp2f(top[j] - by) + other_sum * __builtin_amdgcn_exp2f(other - by);
-        top[j] = now;
+        join_stat(top[j], sum[j], make_float2(__shfl_xor(top[j], 32, 64), __shfl_xor(sum[j], 32, 64)));
         if (lane < 32) join[(wave >> 1) * kTile + n0 + 32 * j + lane] = make_float2(top[j], sum[j]);
     }
     __syncthreads();
     if (threadIdx.x < kTile) {
-        const float2 p = join[threadIdx.x], q = join[kTile + threadIdx.x];
-        const float now = fmaxf(p.x, q.x), by = now == -INFINITY ? 0.0f : now;
-        const float both = p.y * __builtin_amdgcn_exp2f(p.x - by) + q.y * __builtin_amdgcn_exp2f(q.x - by);
-        a.stat[static_cast<int64_t>(split) * a.tokens + static_cast<int64_t>(token_tile) * kTile + threadIdx.x] = make_float2(now, both);
+        float2 p = join[threadIdx.x];
+        join_stat(p.x, p.y, join[kTile + threadIdx.x]);
+        a.stat[(static_cast<int64_t>(token_tile) * kTile + threadIdx.x) * a.splits + split] = p;
     }
 }
 
-// Joins the splits of the table: lse and loss of every row.
+// Joins the splits of the table: lse and loss of every row, a wavefront each.
 __global__ void __launch_bounds__(kThreads) loss_join_kernel(const float2* stat, const float* target_score, const int32_t* targets, int64_t n,
-                                                             uint32_t num_rows, uint32_t splits, int64_t tokens, float* loss, float* lse)
+                                                             uint32_t num_rows, uint32_t splits, float* loss, float* lse)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    const int lane = threadIdx.x & 63;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
     if (i >= n) return;
     if (static_cast<uint32_t>(targets[i]) >= num_rows) {
-        loss[i] = 0.0f;
-        lse[i] = 0.0f;
+        if (lane == 0) loss[i] = lse[i] = 0.0f;
         return;
     }
-    float top = -INFINITY;
-    for (uint32_t s = 0; s < splits; ++s) top = fmaxf(top, stat[s * tokens + i].x);
-    const float by = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    for (uint32_t s = 0; s < splits; ++s) {
-        const float2 p = stat[s * tokens + i];
-        sum += p.y * exp2f(p.x - by);
+    float top = -INFINITY, sum = 0.0f;
+    for (uint32_t s = lane; s < splits; s += 64) join_stat(top, sum, stat[i * splits + s]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) join_stat(top, sum, make_float2(__shfl_xor(top, o, 64), __shfl_xor(sum, o, 64)));
+    if (lane == 0) {
+        const float z = (top + log2f(sum)) * kLn2;
+        lse[i] = z;
+        loss[i] = z - target_score[i];
     }
-    const float z = (top + log2f(sum)) * kLn2;
-    lse[i] = z;
-    loss[i] = z - target_score[i];
+}
+
+// ---------------------------------------------------------------------------------------------
+// few rows of H: the table streams through registers once, straight from memory
+// ---------------------------------------------------------------------------------------------
+// Bound by reading the table.  A wavefront has 16 table rows at a time, whose elements go from memory to the matrix cores' first
+// operand as they lie (lane l: row l % 16, eight elements from (l / 16) * 8 on of every 32); H lies in LDS as second operands, in blocks
+// of 16 rows.  fp32 operands are split into three bf16 parts (24 bits, no common scale to be found first: that would read the
+// table twice), of whose nine products the six largest are taken.
+struct FewArgs {
+    const void *h, *w;
+    int64_t h_stride, w_stride;
+    const int32_t* targets;
+    uint32_t n, num_rows;
+    int32_t dim, steps;            // steps of 32 elements
+    float2* stat;                  // [n][workgroups]
+    float* target_score;
+};
+
+// Eight elements from index e on as floats or bf16, zeros beyond dim.
+template <class T>
+__device__ __forceinline__ void load_eight(const T* row, int e, int dim, T (&x)[8])
+{
+    if (e + 8 <= dim) {
+        __builtin_memcpy(x, row + e, 8 * sizeof(T));
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = e + q < dim ? row[e + q] : from_float<T>(0.0f);
+    }
+}
+
+template <int PARTS>
+__device__ __forceinline__ void split_bf16(const bf16_t (&x)[8], bf16x8 (&out)[PARTS])
+{
+#pragma unroll
+    for (int q = 0; q < 8; ++q) out[0][q] = x[q];
+}
+
+template <int PARTS>
+__device__ __forceinline__ void split_bf16(const float (&x)[8], bf16x8 (&out)[PARTS])
+{
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        float rest = x[q];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            out[p][q] = static_cast<bf16_t>(rest);
+            rest -= static_cast<float>(out[p][q]);
+        }
+    }
+}
+
+template <class T, int BLOCKS>
+__global__ void __launch_bounds__(kThreads) few_rows_kernel(FewArgs a)
+{
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, AHEAD = sizeof(T) == 4 ? 4 : 8;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    extern __shared__ __align__(16) unsigned char few_lds[];       // [blocks][steps][parts][64 lanes] 16 bytes
+    bf16x8* hs = reinterpret_cast<bf16x8*>(few_lds);
+    __shared__ float2 join[kThreads / 64][BLOCKS * 16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+    for (int i = wave; i < BLOCKS * a.steps; i += kThreads / 64) {
+        const int block = i / a.steps, step = i % a.steps;
+        const uint32_t t = block * 16 + col;
+        T x[8];
+        if (t < a.n && static_cast<uint32_t>(a.targets[t]) < a.num_rows) {
+            load_eight(static_cast<const T*>(a.h) + t * a.h_stride, step * 32 + quarter * 8, a.dim, x);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = from_float<T>(0.0f);
+        }
+        bf16x8 parts[PARTS];
+        split_bf16<PARTS>(x, parts);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) hs[(i * PARTS + p) * 64 + lane] = parts[p];
+    }
+    float top[BLOCKS], sum[BLOCKS];
+    uint32_t target[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        top[b] = -INFINITY;
+        sum[b] = 0.0f;
+        target[b] = b * 16 + col < a.n ? static_cast<uint32_t>(a.targets[b * 16 + col]) : 0xFFFFFFFFu;
+    }
+    __syncthreads();
+    const uint32_t tiles = (a.num_rows + 15) / 16, stride = gridDim.x * (kThreads / 64);
+    for (uint32_t tile = blockIdx.x * (kThreads / 64) + wave; tile < tiles; tile += stride) {
+        const T* row = static_cast<const T*>(a.w) + static_cast<int64_t>(min(tile * 16 + col, a.num_rows - 1)) * a.w_stride;
+        f32x4 acc[BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s0 = 0; s0 < a.steps; s0 += AHEAD) {
+            T x[AHEAD][8];
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s)
+                if (s0 + s < a.steps) load_eight(row, (s0 + s) * 32 + quarter * 8, a.dim, x[s]);
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s) {
+                if (s0 + s >= a.steps) break;
+                bf16x8 w[PARTS];
+                split_bf16<PARTS>(x[s], w);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    bf16x8 h[PARTS];
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) h[p] = hs[((b * a.steps + s0 + s) * PARTS + p) * 64 + lane];
+                    // (the smallest products first)
+#pragma unroll
+                    for (int sum_of_parts = PARTS - 1; sum_of_parts >= 0; --sum_of_parts)
+#pragma unroll
+                        for (int p = 0; p <= sum_of_parts; ++p)
+                            acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[p], h[sum_of_parts - p], acc[b], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            float now = top[b];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = tile * 16 + quarter * 4 + i;
+                if (r == target[b] && r < a.num_rows) a.target_score[b * 16 + col] = acc[b][i];
+                if (r >= a.num_rows) acc[b][i] = -INFINITY;
+                now = fmaxf(now, acc[b][i] * kLog2e);
+            }
+            const float by = now == -INFINITY ? 0.0f : now;
+            float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part += __builtin_amdgcn_exp2f(fmaf(acc[b][i], kLog2e, -by));
+            sum[b] = fmaf(sum[b], __builtin_amdgcn_exp2f(top[b] - by), part);
+            top[b] = now;
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1) join_stat(top[b], sum[b], make_float2(__shfl_xor(top[b], o, 64), __shfl_xor(sum[b], o, 64)));
+        if (lane < 16) join[wave][b * 16 + lane] = make_float2(top[b], sum[b]);
+    }
+    __syncthreads();
+    if (threadIdx.x < a.n) {
+        float2 p = join[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) join_stat(p.x, p.y, join[w][threadIdx.x]);
+        a.stat[static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x] = p;
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -594,6 +745,7 @@ struct XentWs {
     int32_t parts, padded, cols;
     int64_t tokens;
     uint32_t row_tiles, splits;        // of the scores
+    int32_t few_blocks;                // > 0: few rows of H, so many blocks of 16
     int64_t piece;                     // table rows of a piece
     uint32_t h_splits, w_splits, h_share, w_share, h_stages, w_stages;
     float* amax;
@@ -622,6 +774,16 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, kTile));
     const int64_t token_tiles = w.tokens / kTile;
     Carver take{base};
+    // H as second operands of the few-rows kernel has to leave room in LDS for a second workgroup
+    const int64_t few_bytes = (n <= 16 ? 1 : n <= 32 ? 2 : 4) * ceil_div(dim, 32) * (type == NE_F32 ? 3 : 1) * 1024;
+    if (!grad && n <= kFewRows && few_bytes <= kFewBytes) {
+        w.few_blocks = static_cast<int32_t>(n <= 16 ? 1 : n <= 32 ? 2 : 4);
+        w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups));
+        w.stat = take.get<float2>(static_cast<size_t>(w.splits) * n);
+        w.target_score = take.get<float>(static_cast<size_t>(n));
+        w.total = take.total();
+        return w;
+    }
     w.amax = take.get<float>(3 * kAmaxBlocks);
     w.shift = take.get<int32_t>(3);
     for (int p = 0; p < w.parts; ++p) {
@@ -708,6 +870,29 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Opera
     return e;
 }
 
+hipError_t join_losses(const XentCall& x, const XentWs& w, float* loss, float* lse, hipStream_t st)
+{
+    hipLaunchKernelGGL(loss_join_kernel, dim3(static_cast<unsigned>(ceil_div(x.n, kThreads / 64))), dim3(kThreads), 0, st, w.stat, w.target_score,
+                       x.targets, x.n, static_cast<uint32_t>(x.num_rows), w.splits, loss, lse);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t run_few(const XentCall& x, const XentWs& w, float* loss, float* lse, hipStream_t st)
+{
+    FewArgs a{};
+    a.h = x.h; a.w = x.w; a.h_stride = x.h_stride; a.w_stride = x.w_stride; a.targets = x.targets; a.n = static_cast<uint32_t>(x.n);
+    a.num_rows = static_cast<uint32_t>(x.num_rows); a.dim = x.dim; a.steps = static_cast<int32_t>(ceil_div(x.dim, 32)); a.stat = w.stat;
+    a.target_score = w.target_score;
+    const size_t lds = static_cast<size_t>(w.few_blocks) * a.steps * (sizeof(T) == 4 ? 3 : 1) * 1024;
+    const dim3 grid(w.splits);
+    if (w.few_blocks == 1) hipLaunchKernelGGL((few_rows_kernel<T, 1>), grid, dim3(kThreads), lds, st, a);
+    else if (w.few_blocks == 2) hipLaunchKernelGGL((few_rows_kernel<T, 2>), grid, dim3(kThreads), lds, st, a);
+    else hipLaunchKernelGGL((few_rows_kernel<T, 4>), grid, dim3(kThreads), lds, st, a);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : join_losses(x, w, loss, lse, st);
+}
+
 template <int P>
 hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse, hipStream_t st)
 {
@@ -720,9 +905,7 @@ hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse,
     hipLaunchKernelGGL(scores_kernel<P>, dim3(static_cast<unsigned>(w.tokens / kTile * w.splits)), dim3(kThreads), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(loss_join_kernel, dim3(static_cast<unsigned>(ceil_div(x.n, kThreads))), dim3(kThreads), 0, st, w.stat, w.target_score, x.targets,
-                       x.n, a.num_rows, w.splits, w.tokens, loss, lse);
-    return hipGetLastError();
+    return join_losses(x, w, loss, lse, st);
 }
 
 template <int P, class T>
@@ -820,7 +1003,8 @@ ne_status ne_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, i
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
         return fail(NE_ERR_ARG, "ne_xent_loss: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = type == NE_F32 ? run_loss<2>(x, w, loss_dev, lse_dev, st) : run_loss<1>(x, w, loss_dev, lse_dev, st);
+    const hipError_t e = w.few_blocks ? (type == NE_F32 ? run_few<float>(x, w, loss_dev, lse_dev, st) : run_few<bf16_t>(x, w, loss_dev, lse_dev, st))
+                                      : (type == NE_F32 ? run_loss<2>(x, w, loss_dev, lse_dev, st) : run_loss<1>(x, w, loss_dev, lse_dev, st));
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("cross entropy launch: ") + hipGetErrorString(e));
     return NE_OK;
 }
