@@ -58,30 +58,78 @@ struct Operand {
 // ---------------------------------------------------------------------------------------------
 // a stage: 128 rows x step_of<P>() contraction indices of each operand's P parts
 // ---------------------------------------------------------------------------------------------
-template <int P, bool ROWS>
-__device__ __forceinline__ void fetch(const Operand& o, uint32_t row0, uint32_t k0, unsigned char* lds)
+// Loads go from memory to LDS directly, and are waited for once a stage (stage_done), before the barrier that hands the stage
+// over: a stage is in flight while the one before it is multiplied.  They are written in assembly because the compiler waits for
+// loads of this kind before every LDS read that follows.  The address is a uniform base and a lane's offset, which stays the same
+// from stage to stage.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int i = q * 4 + wave;                         // 1 KB pieces of the operand's 16 KB
-        const int part = P == 1 ? 0 : i >> 3, j = P == 1 ? i : i & 7;
-        int64_t at;
-        if (ROWS && P == 1) {
-            const uint32_t row = min(row0 + j * 8 + (lane >> 3), o.last);
-            at = static_cast<int64_t>(row) * o.stride + k0 + (((lane & 7) ^ (lane >> 3)) << 3);
-        } else if (ROWS) {
-            const uint32_t row = min(row0 + j * 16 + (lane >> 2), o.last);
-            at = static_cast<int64_t>(row) * o.stride + k0 + (((lane & 3) ^ ((lane >> 3) & 3)) << 3);
-        } else {
-            const uint32_t k = min(k0 + j * 4 + (lane >> 4), o.last);
-            const uint32_t col = row0 + ((((lane & 15) ^ ((lane >> 4) << 2))) << 3);
-            at = static_cast<int64_t>(k) * o.stride + min(col, o.width - 8);
-        }
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(o.part[part] + at),
-                                         (__attribute__((address_space(3))) void*)(lds + i * 1024), 16, 0, 0);
-    }
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
+
+__device__ __forceinline__ void stage_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t lds_address(const unsigned char* p)
+{
+    return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char*)p)));
+}
+
+// Rows row0 .. row0 + 127 of an operand, stage after stage.
+template <int P, bool ROWS>
+struct Loader {
+    const unsigned char* base[P];
+    int64_t advance;               // bytes from one stage to the next
+    uint32_t offset[4];
+    uint32_t stride, ks;           // bytes of a row; contraction indices that are left (!ROWS)
+
+    __device__ __forceinline__ static int piece(int q)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+        return (P == 1 ? q * 4 : (q & 1) * 4) + wave;
+    }
+
+    __device__ __forceinline__ void start(const Operand& o, uint32_t row0, uint32_t stage)
+    {
+        const int lane = threadIdx.x & 63;
+        stride = static_cast<uint32_t>(o.stride * 2);
+        const int64_t first = ROWS ? static_cast<int64_t>(row0) * o.stride + stage * step_of<P>() : static_cast<int64_t>(stage) * step_of<P>() * o.stride;
+        advance = ROWS ? step_of<P>() * 2 : static_cast<int64_t>(step_of<P>()) * o.stride * 2;
+        ks = ROWS ? 0 : o.last + 1 - stage * step_of<P>();
+#pragma unroll
+        for (int p = 0; p < P; ++p) base[p] = reinterpret_cast<const unsigned char*>(o.part[p] + first);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int j = piece(q);
+            if (ROWS) {
+                const uint32_t row = P == 1 ? j * 8 + (lane >> 3) : j * 16 + (lane >> 2);
+                const uint32_t at = P == 1 ? (lane & 7) ^ (lane >> 3) : (lane & 3) ^ ((lane >> 3) & 3);
+                offset[q] = min(row, o.last - row0) * stride + at * 16;
+            } else {
+                const uint32_t col = row0 + (((lane & 15) ^ ((lane >> 4) << 2)) << 3);
+                offset[q] = (j * 4 + (lane >> 4)) * stride + min(col, o.width - 8) * 2;
+            }
+        }
+    }
+
+    // (a contraction index beyond the last one is the last one: the other operand has zeros there)
+    __device__ __forceinline__ void fetch(uint32_t lds)
+    {
+        const int lane = threadIdx.x & 63;
+        if (ROWS || ks >= static_cast<uint32_t>(step_of<P>())) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q], lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t k = piece(q) * 4 + (lane >> 4);
+                load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q] - (k - min(k, ks - 1)) * stride, lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) base[p] += advance;
+        ks -= step_of<P>();
+    }
+};
 
 // What lane l supplies for rows r0 .. r0 + 31 and contraction indices 16 kk .. + 15 of a stage: row l % 32, the eight
 // indices from (l / 32) * 8 on.
@@ -316,18 +364,23 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
     f32x16 acc[2][2];
     clear(acc);
     const uint32_t stages = tile1 > tile0 ? (tile1 - tile0) * a.steps : 0;
-    auto get = [&](uint32_t tile, int step, int to) {
-        fetch<P, true>(a.w, tile * kTile, step * step_of<P>(), lds[to]);
-        fetch<P, true>(a.h, token_tile * kTile, step * step_of<P>(), lds[to] + kOperandBytes);
-    };
+    Loader<P, true> load_w, load_h;
     uint32_t tile = tile0, next_tile = tile0;
     int step = 0, next_step = 0;
-    auto advance = [&](uint32_t& t, int& s) { if (++s == a.steps) { s = 0; ++t; } };
-    if (stages) get(tile0, 0, 0);
-    advance(next_tile, next_step);
-    __syncthreads();
+    const uint32_t lds0 = lds_address(lds[0]);
+    auto get = [&](uint32_t s) {
+        if (next_step == 0) {
+            load_w.start(a.w, next_tile * kTile, 0);
+            load_h.start(a.h, token_tile * kTile, 0);
+        }
+        load_w.fetch(lds0 + (s & 1) * kStageBytes);
+        load_h.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
+        if (++next_step == a.steps) { next_step = 0; ++next_tile; }
+    };
+    if (stages) get(0);
+    stage_done();
     for (uint32_t s = 0; s < stages; ++s) {
-        if (s + 1 < stages) get(next_tile, next_step, (s + 1) & 1);
+        if (s + 1 < stages) get(s + 1);
         multiply<P, true, true>(lds[s & 1], acc);
         if (step == a.steps - 1) {
             const uint32_t row0 = tile * kTile + m0;
@@ -364,9 +417,8 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
             }
             clear(acc);
         }
-        __syncthreads();
-        advance(tile, step);
-        advance(next_tile, next_step);
+        stage_done();
+        if (++step == a.steps) { step = 0; ++tile; }
     }
     // lanes l and l + 32 and the two wavefronts of a column have the same rows of H
     float2* join = reinterpret_cast<float2*>(lds[0]);
@@ -395,6 +447,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(const float2* stat,
         return;
     }
     float top = -INFINITY, sum = 0.0f;
+#pragma unroll 4
     for (uint32_t s = lane; s < splits; s += 64) join_stat(top, sum, stat[i * splits + s]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) join_stat(top, sum, make_float2(__shfl_xor(top, o, 64), __shfl_xor(sum, o, 64)));
@@ -575,16 +628,20 @@ __global__ void __launch_bounds__(kThreads, 2) coef_kernel(CoefArgs a)
     const uint32_t row0 = a.row_base + tile * kTile;
     f32x16 acc[2][2];
     clear(acc);
-    auto get = [&](int step, int to) {
-        fetch<P, true>(a.w, row0, step * step_of<P>(), lds[to]);
-        fetch<P, true>(a.h, token_tile * kTile, step * step_of<P>(), lds[to] + kOperandBytes);
+    Loader<P, true> load_w, load_h;
+    load_w.start(a.w, row0, 0);
+    load_h.start(a.h, token_tile * kTile, 0);
+    const uint32_t lds0 = lds_address(lds[0]);
+    auto get = [&](int s) {
+        load_w.fetch(lds0 + (s & 1) * kStageBytes);
+        load_h.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
     };
-    get(0, 0);
-    __syncthreads();
+    get(0);
+    stage_done();
     for (int s = 0; s < a.steps; ++s) {
-        if (s + 1 < a.steps) get(s + 1, (s + 1) & 1);
+        if (s + 1 < a.steps) get(s + 1);
         multiply<P, true, true>(lds[s & 1], acc);
-        __syncthreads();
+        stage_done();
     }
     const float to_log2 = kLog2e * score_factor<P>(a.shift);
     unsigned char* out = lds[0];       // [parts][128 rows of H][128 table rows], 16-byte pieces at piece ^ row % 16
@@ -651,17 +708,23 @@ template <int P, bool AROWS>
 __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, uint32_t row0, uint32_t col0, uint32_t s0, uint32_t s1,
                                              unsigned char (*lds)[kStageBytes], f32x16 (&acc)[2][2])
 {
-    auto get = [&](uint32_t s, int to) {
-        fetch<P, AROWS>(A, row0, s * step_of<P>(), lds[to]);
-        fetch<P, false>(B, col0, s * step_of<P>(), lds[to] + kOperandBytes);
-    };
     clear(acc);
-    if (s0 < s1) get(s0, 0);
-    __syncthreads();
-    for (uint32_t s = s0; s < s1; ++s) {
-        if (s + 1 < s1) get(s + 1, (s - s0 + 1) & 1);
-        multiply<P, AROWS, false>(lds[(s - s0) & 1], acc);
-        __syncthreads();
+    if (s0 >= s1) return;
+    Loader<P, AROWS> load_a;
+    Loader<P, false> load_b;
+    load_a.start(A, row0, s0);
+    load_b.start(B, col0, s0);
+    const uint32_t lds0 = lds_address(lds[0]);
+    auto get = [&](uint32_t s) {
+        load_a.fetch(lds0 + (s & 1) * kStageBytes);
+        load_b.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
+    };
+    get(0);
+    stage_done();
+    for (uint32_t s = 0; s < s1 - s0; ++s) {
+        if (s + 1 < s1 - s0) get(s + 1);
+        multiply<P, AROWS, false>(lds[s & 1], acc);
+        stage_done();
     }
 }
 
@@ -944,7 +1007,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         pa.w.last = static_cast<uint32_t>(rows - 1);
         pa.h_tiles = dh ? token_tiles : 0;
         pa.w_tiles = dw ? ca.row_tiles : 0;
-        pa.h_stages = ca.row_tiles * kTile / step_of<P>();
+        pa.h_stages = static_cast<uint32_t>(ceil_div(rows, step_of<P>()));      // (no stage begins beyond the last row)
         pa.add = base > 0;
         const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
         if (!blocks) continue;
