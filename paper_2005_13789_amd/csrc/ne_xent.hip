@@ -200,6 +200,22 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[2][2])
             for (int i = 0; i < 16; ++i) acc[im][in][i] = 0.0f;
 }
 
+// Workgroups go to the eight XCDs in turn, and each XCD has an L2 of its own: this numbers them so that an XCD's have
+// consecutive numbers, and what neighbours share is fetched into one L2.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks)
+{
+    const uint32_t xcd = block & 7, per = blocks >> 3, more = blocks & 7;
+    return xcd * per + min(xcd, more) + (block >> 3);
+}
+
+// Number b of tiles_a x tiles_b pairs, eight of a against one of b after the other: the 64 workgroups of an XCD have 16 operands.
+__device__ __forceinline__ void pair_of(uint32_t b, uint32_t tiles_a, uint32_t tiles_b, uint32_t& ta, uint32_t& tb)
+{
+    const uint32_t group = b / (8 * tiles_b), rest = b - group * 8 * tiles_b, size = min(8u, tiles_a - group * 8);
+    tb = rest / size;
+    ta = group * 8 + rest - tb * size;
+}
+
 // Row (of 32) of a lane's i-th sum.
 __device__ __forceinline__ int sum_row(int i) { return (i & 3) + 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5); }
 
@@ -349,7 +365,8 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2][kStageBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
-    const uint32_t token_tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    uint32_t token_tile, split;
+    pair_of(by_xcd(blockIdx.x, gridDim.x), a.tokens / kTile, a.splits, token_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits;
     const uint32_t tile0 = split * per, tile1 = min(tile0 + per, a.row_tiles);
     const float factor = score_factor<P>(a.shift), to_log2 = kLog2e * factor;
@@ -624,7 +641,8 @@ __global__ void __launch_bounds__(kThreads, 2) coef_kernel(CoefArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2][kStageBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
-    const uint32_t token_tile = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles;
+    uint32_t token_tile, tile;
+    pair_of(by_xcd(blockIdx.x, gridDim.x), gridDim.x / a.row_tiles, a.row_tiles, token_tile, tile);
     const uint32_t row0 = a.row_base + tile * kTile;
     f32x16 acc[2][2];
     clear(acc);
@@ -734,9 +752,19 @@ __global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
     __shared__ __align__(16) unsigned char lds[2][kStageBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t h_blocks = a.h_tiles * a.col_tiles * a.h_splits;
+    // eight workgroups of dH, eight of dW, as long as there are both: every XCD has its share of either
+    const uint32_t w_blocks = gridDim.x - h_blocks, both = min(h_blocks, w_blocks) & ~7u;
     uint32_t b = blockIdx.x;
-    const bool dh = b < h_blocks;
-    if (!dh) b -= h_blocks;
+    bool dh;
+    if (b < 2 * both) {
+        dh = !(b & 8);
+        b = (b >> 4) * 8 + (b & 7);
+    } else {
+        b -= both;
+        dh = b < h_blocks;
+        if (!dh) b -= h_blocks - both;
+    }
+    b = by_xcd(b, dh ? h_blocks : w_blocks);
     const uint32_t splits = dh ? a.h_splits : a.w_splits, share = dh ? a.h_share : a.w_share, stages = dh ? a.h_stages : a.w_stages;
     const uint32_t col = b % a.col_tiles, split = b / a.col_tiles % splits, tile = b / a.col_tiles / splits;
     const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
