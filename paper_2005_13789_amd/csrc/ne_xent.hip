@@ -19,6 +19,8 @@
 // Operands in LDS are 16-byte pieces placed so that reads are free of bank conflicts (an XOR of the piece's
 // index with the row's); they come from memory straight to LDS, 16 bytes a lane, and the XOR is applied to the
 // address that a lane reads.  Operands whose rows run along the contraction are read with the transposing LDS read.
+#include <type_traits>
+
 #include "ne_internal.h"
 #include "ne_ops.h"
 
@@ -52,7 +54,7 @@ struct Operand {
     const uint16_t* part[2];
     int64_t stride;
     uint32_t last;      // ROWS: last row; otherwise: last k
-    uint32_t width;     // columns that there are: a multiple of 8
+    uint32_t width;     // elements of a row that there are: a multiple of 8
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -80,7 +82,7 @@ struct Loader {
     const unsigned char* base[P];
     int64_t advance;               // bytes from one stage to the next
     uint32_t offset[4];
-    uint32_t stride, ks;           // bytes of a row; contraction indices that are left (!ROWS)
+    uint32_t stride, ks;           // bytes of a row; contraction indices that are left
 
     __device__ __forceinline__ static int piece(int q)
     {
@@ -94,7 +96,7 @@ struct Loader {
         stride = static_cast<uint32_t>(o.stride * 2);
         const int64_t first = ROWS ? static_cast<int64_t>(row0) * o.stride + stage * step_of<P>() : static_cast<int64_t>(stage) * step_of<P>() * o.stride;
         advance = ROWS ? step_of<P>() * 2 : static_cast<int64_t>(step_of<P>()) * o.stride * 2;
-        ks = ROWS ? 0 : o.last + 1 - stage * step_of<P>();
+        ks = (ROWS ? o.width : o.last + 1) - stage * step_of<P>();
 #pragma unroll
         for (int p = 0; p < P; ++p) base[p] = reinterpret_cast<const unsigned char*>(o.part[p] + first);
 #pragma unroll
@@ -111,18 +113,25 @@ struct Loader {
         }
     }
 
-    // (a contraction index beyond the last one is the last one: the other operand has zeros there)
+    // (contraction indices beyond the last ones are those again: the other operand has zeros there)
     __device__ __forceinline__ void fetch(uint32_t lds)
     {
         const int lane = threadIdx.x & 63;
-        if (ROWS || ks >= static_cast<uint32_t>(step_of<P>())) {
+        if (ks >= static_cast<uint32_t>(step_of<P>())) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q], lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
         } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t k = piece(q) * 4 + (lane >> 4);
-                load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q] - (k - min(k, ks - 1)) * stride, lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
+                uint32_t back;
+                if (ROWS) {
+                    const uint32_t e = 8 * (P == 1 ? (lane & 7) ^ (lane >> 3) : (lane & 3) ^ ((lane >> 3) & 3));
+                    back = (e - min(e, ks - 8)) * 2;
+                } else {
+                    const uint32_t k = piece(q) * 4 + (lane >> 4);
+                    back = (k - min(k, ks - 1)) * stride;
+                }
+                load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q] - back, lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
             }
         }
 #pragma unroll
@@ -360,6 +369,42 @@ __device__ __forceinline__ float score_factor(const int32_t* shift)
     return ldexpf(1.0f, max(min(-(shift[0] + shift[1]), 127), -126));
 }
 
+// Scores of tiles tile0 .. tile1 - 1 of the table's rows against one tile of H's, epilogue(row0, acc) for each; the next tile's first
+// stage travels meanwhile.
+template <int P, class Epilogue>
+__device__ __forceinline__ void score_tiles(const Operand& w, const Operand& h, uint32_t token_tile, uint32_t first_row, uint32_t tile0, uint32_t tile1, int steps,
+                                            unsigned char (*lds)[kStageBytes], Epilogue epilogue)
+{
+    f32x16 acc[2][2];
+    clear(acc);
+    const uint32_t stages = tile1 > tile0 ? (tile1 - tile0) * steps : 0;
+    Loader<P, true> load_w, load_h;
+    uint32_t row0 = first_row + tile0 * kTile, next_row0 = row0;
+    int step = 0, next_step = 0;
+    const uint32_t lds0 = lds_address(lds[0]);
+    auto get = [&](uint32_t s) {
+        if (next_step == 0) {
+            load_w.start(w, next_row0, 0);
+            load_h.start(h, token_tile * kTile, 0);
+        }
+        load_w.fetch(lds0 + (s & 1) * kStageBytes);
+        load_h.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
+        if (++next_step == steps) { next_step = 0; next_row0 += kTile; }
+    };
+    if (stages) get(0);
+    stage_done();
+    for (uint32_t s = 0; s < stages; ++s) {
+        if (s + 1 < stages) get(s + 1);
+        multiply<P, true, true>(lds[s & 1], acc);
+        if (step == steps - 1) {
+            epilogue(row0, acc);
+            clear(acc);
+        }
+        stage_done();
+        if (++step == steps) { step = 0; row0 += kTile; }
+    }
+}
+
 template <int P>
 __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
 {
@@ -367,8 +412,7 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
     uint32_t token_tile, split;
     pair_of(by_xcd(blockIdx.x, gridDim.x), a.tokens / kTile, a.splits, token_tile, split);
-    const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits;
-    const uint32_t tile0 = split * per, tile1 = min(tile0 + per, a.row_tiles);
+    const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const float factor = score_factor<P>(a.shift), to_log2 = kLog2e * factor;
     float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
     uint32_t target[2];
@@ -378,65 +422,40 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
         token[j] = static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31);
         target[j] = token[j] < a.n ? static_cast<uint32_t>(a.targets[token[j]]) : 0xFFFFFFFFu;
     }
-    f32x16 acc[2][2];
-    clear(acc);
-    const uint32_t stages = tile1 > tile0 ? (tile1 - tile0) * a.steps : 0;
-    Loader<P, true> load_w, load_h;
-    uint32_t tile = tile0, next_tile = tile0;
-    int step = 0, next_step = 0;
-    const uint32_t lds0 = lds_address(lds[0]);
-    auto get = [&](uint32_t s) {
-        if (next_step == 0) {
-            load_w.start(a.w, next_tile * kTile, 0);
-            load_h.start(a.h, token_tile * kTile, 0);
+    score_tiles<P>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+        const uint32_t row0 = tile_row0 + m0;
+        if (row0 + 64 > a.num_rows) {
+#pragma unroll
+            for (int im = 0; im < 2; ++im)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (row0 + 32 * im + sum_row(i) >= a.num_rows) acc[im][0][i] = acc[im][1][i] = -INFINITY;
         }
-        load_w.fetch(lds0 + (s & 1) * kStageBytes);
-        load_h.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
-        if (++next_step == a.steps) { next_step = 0; ++next_tile; }
-    };
-    if (stages) get(0);
-    stage_done();
-    for (uint32_t s = 0; s < stages; ++s) {
-        if (s + 1 < stages) get(s + 1);
-        multiply<P, true, true>(lds[s & 1], acc);
-        if (step == a.steps - 1) {
-            const uint32_t row0 = tile * kTile + m0;
-            if (row0 + 64 > a.num_rows) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (__any(target[j] - row0 < 64)) {
 #pragma unroll
                 for (int im = 0; im < 2; ++im)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (row0 + 32 * im + sum_row(i) >= a.num_rows) acc[im][0][i] = acc[im][1][i] = -INFINITY;
+                        if (target[j] == row0 + 32 * im + sum_row(i) && target[j] < a.num_rows) a.target_score[token[j]] = acc[im][j][i] * factor;
             }
+            float t = acc[0][j][0];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (__any(target[j] - row0 < 64)) {
+            for (int im = 0; im < 2; ++im)
 #pragma unroll
-                    for (int im = 0; im < 2; ++im)
+                for (int i = 0; i < 16; ++i) t = fmaxf(t, acc[im][j][i]);
+            const float now = fmaxf(top[j], t * to_log2);
+            const float by = now == -INFINITY ? 0.0f : now;         // (nothing seen yet but scores of minus infinity)
+            float part = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (target[j] == row0 + 32 * im + sum_row(i) && target[j] < a.num_rows) a.target_score[token[j]] = acc[im][j][i] * factor;
-                }
-                float t = acc[0][j][0];
+            for (int im = 0; im < 2; ++im)
 #pragma unroll
-                for (int im = 0; im < 2; ++im)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) t = fmaxf(t, acc[im][j][i]);
-                const float now = fmaxf(top[j], t * to_log2);
-                const float by = now == -INFINITY ? 0.0f : now;         // (nothing seen yet but scores of minus infinity)
-                float part = 0.0f;
-#pragma unroll
-                for (int im = 0; im < 2; ++im)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by));
-                sum[j] = fmaf(sum[j], __builtin_amdgcn_exp2f(top[j] - by), part);
-                top[j] = now;
-            }
-            clear(acc);
+                for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by));
+            sum[j] = fmaf(sum[j], __builtin_amdgcn_exp2f(top[j] - by), part);
+            top[j] = now;
         }
-        stage_done();
-        if (++step == a.steps) { step = 0; ++tile; }
-    }
+    });
     // lanes l and l + 32 and the two wavefronts of a column have the same rows of H
     float2* join = reinterpret_cast<float2*>(lds[0]);
 #pragma unroll
@@ -631,80 +650,77 @@ struct CoefArgs {
     const float* lse;
     const float* c;                // bf16 only: NULL, or factors that G is rounded with (fp32: the rows of H have them)
     int64_t n, g_stride;
-    uint32_t num_rows, row_base, row_tiles;
+    uint32_t num_rows, row_base, row_tiles, splits, tokens;
     int32_t steps;
     uint16_t* g[2];                // [tokens][g_stride], table rows of the piece side by side
 };
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+// A lane has 4 values of 16 bits of rows 8 q + 4 (lane / 32) .. + 3 (a: of q, b: of q + 1): lanes l and l + 32 swap halves, so that
+// l has the 8 of q and l + 32 the 8 of q + 1, side by side.
+__device__ __forceinline__ u32x4 eight_of(u32x2 a, u32x2 b)
+{
+    const auto x = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false), y = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+    return u32x4{x[0], y[0], x[1], y[1]};
+}
 
 template <int P>
 __global__ void __launch_bounds__(kThreads, 2) coef_kernel(CoefArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2][kStageBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
-    uint32_t token_tile, tile;
-    pair_of(by_xcd(blockIdx.x, gridDim.x), gridDim.x / a.row_tiles, a.row_tiles, token_tile, tile);
-    const uint32_t row0 = a.row_base + tile * kTile;
-    f32x16 acc[2][2];
-    clear(acc);
-    Loader<P, true> load_w, load_h;
-    load_w.start(a.w, row0, 0);
-    load_h.start(a.h, token_tile * kTile, 0);
-    const uint32_t lds0 = lds_address(lds[0]);
-    auto get = [&](int s) {
-        load_w.fetch(lds0 + (s & 1) * kStageBytes);
-        load_h.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
-    };
-    get(0);
-    stage_done();
-    for (int s = 0; s < a.steps; ++s) {
-        if (s + 1 < a.steps) get(s + 1);
-        multiply<P, true, true>(lds[s & 1], acc);
-        stage_done();
-    }
+    uint32_t token_tile, split;
+    pair_of(by_xcd(blockIdx.x, gridDim.x), a.tokens / kTile, a.splits, token_tile, split);
+    const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const float to_log2 = kLog2e * score_factor<P>(a.shift);
-    unsigned char* out = lds[0];       // [parts][128 rows of H][128 table rows], 16-byte pieces at piece ^ row % 16
+    uint32_t target[2];
+    float by[2], c[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int t = n0 + 32 * j + (lane & 31);
-        const int64_t token = static_cast<int64_t>(token_tile) * kTile + t;
-        const uint32_t target = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
-        const bool counts = target < a.num_rows;
-        const float by = counts ? a.lse[token] * kLog2e : 0.0f;
-        const float c = P == 2 ? 0x1p14f : counts && a.c ? a.c[token] : 1.0f;
-#pragma unroll
-        for (int im = 0; im < 2; ++im)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                s16x4 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t row = row0 + m0 + 32 * im + sum_row(4 * q + e);
-                    float x = __builtin_amdgcn_exp2f(fmaf(acc[im][j][4 * q + e], to_log2, -by));
-                    if (row == target) x -= 1.0f;
-                    x = counts && row < a.num_rows ? x * c : 0.0f;
-                    if (P == 1) {
-                        hi[e] = __builtin_bit_cast(short, static_cast<bf16_t>(x));
-                    } else {
-                        const f16_t xh = static_cast<f16_t>(x);
-                        hi[e] = __builtin_bit_cast(short, xh);
-                        lo[e] = __builtin_bit_cast(short, static_cast<f16_t>(x - static_cast<float>(xh)));
-                    }
-                }
-                const int v = m0 + 32 * im + 8 * q + 4 * (lane >> 5);
-                const int at = t * 256 + (((v >> 3) ^ (t & 15)) << 4) + ((v & 4) << 1);
-                *reinterpret_cast<s16x4*>(out + at) = hi;
-                if (P == 2) *reinterpret_cast<s16x4*>(out + kStageBytes + at) = lo;
-            }
+        const int64_t token = static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31);
+        target[j] = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
+        if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
+        const bool counts = target[j] != 0xFFFFFFFFu;
+        by[j] = counts ? a.lse[token] * kLog2e : 0.0f;
+        c[j] = P == 2 ? 0x1p14f : counts && a.c ? a.c[token] : 1.0f;
     }
-    __syncthreads();
+    score_tiles<P>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+        const uint32_t row0 = tile_row0 + m0;
+        const bool ends = row0 + 64 > a.num_rows;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+        for (int j = 0; j < 2; ++j) {
+            const bool here = __any(target[j] - row0 < 64);
+            const bool counts = target[j] != 0xFFFFFFFFu;
+            uint16_t* const* g = a.g;
+            const int64_t to = (static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31)) * a.g_stride + (row0 - a.row_base) + 8 * (lane >> 5);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = i * 16 + (threadIdx.x >> 4), piece = threadIdx.x & 15;
-            const s16x8 x = *reinterpret_cast<const s16x8*>(out + p * kStageBytes + t * 256 + ((piece ^ (t & 15)) << 4));
-            *reinterpret_cast<s16x8*>(a.g[p] + (static_cast<int64_t>(token_tile) * kTile + t) * a.g_stride + tile * kTile + piece * 8) = x;
+            for (int im = 0; im < 2; ++im)
+#pragma unroll
+                for (int q = 0; q < 4; q += 2) {
+                    s16x4 hi[2], lo[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int i = 4 * (q + r) + e;
+                            float x = __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by[j]));
+                            if (here && row0 + 32 * im + sum_row(i) == target[j]) x -= 1.0f;
+                            x = counts && !(ends && row0 + 32 * im + sum_row(i) >= a.num_rows) ? x * c[j] : 0.0f;
+                            if (P == 1) {
+                                hi[r][e] = __builtin_bit_cast(short, static_cast<bf16_t>(x));
+                            } else {
+                                const f16_t xh = static_cast<f16_t>(x);
+                                hi[r][e] = __builtin_bit_cast(short, xh);
+                                lo[r][e] = __builtin_bit_cast(short, static_cast<f16_t>(x - static_cast<float>(xh)));
+                            }
+                        }
+                    *reinterpret_cast<u32x4*>(g[0] + to + 32 * im + 8 * q) = eight_of(__builtin_bit_cast(u32x2, hi[0]), __builtin_bit_cast(u32x2, hi[1]));
+                    if (P == 2) *reinterpret_cast<u32x4*>(g[P - 1] + to + 32 * im + 8 * q) = eight_of(__builtin_bit_cast(u32x2, lo[0]), __builtin_bit_cast(u32x2, lo[1]));
+                }
         }
+    });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -714,35 +730,55 @@ struct ProductArgs {
     Operand g_rows, w;             // dH: G by rows (contraction along them), W across
     Operand g_cols, h;             // dW: G across, H across
     float* dh;                     // [h_splits][tokens][cols]  sums over the pieces
-    float* dw;                     // [w_splits][piece rows][cols]
+    float* dw;                     // [w_splits][piece rows][cols], or NULL: one split, whose sums are dW
+    void* out;                     // dW of the piece
+    int64_t out_stride;
     uint32_t tokens, piece_rows, cols;      // multiples of 128
     uint32_t h_tiles, w_tiles, col_tiles;   // tiles over tokens, piece rows, columns
     uint32_t h_splits, w_splits, h_share, w_share;      // splits of the contraction, stages of each
     uint32_t h_stages, w_stages;
     int32_t add;                   // dh: added to what earlier pieces left
+    uint32_t rows;                 // table rows of the piece that there are
+    int32_t dim;
+    float scale;
+    const int32_t* shift;          // fp32 only: power of two of the rows of H
 };
 
-template <int P, bool AROWS>
-__device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, uint32_t row0, uint32_t col0, uint32_t s0, uint32_t s1,
+// (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
+template <int P, bool GROWS>
+__device__ __forceinline__ void product_tile(const Operand& cols, const Operand& g, uint32_t col0, uint32_t row0, uint32_t s0, uint32_t s1,
                                              unsigned char (*lds)[kStageBytes], f32x16 (&acc)[2][2])
 {
     clear(acc);
     if (s0 >= s1) return;
-    Loader<P, AROWS> load_a;
-    Loader<P, false> load_b;
-    load_a.start(A, row0, s0);
-    load_b.start(B, col0, s0);
+    Loader<P, false> load_c;
+    Loader<P, GROWS> load_g;
+    load_c.start(cols, col0, s0);
+    load_g.start(g, row0, s0);
     const uint32_t lds0 = lds_address(lds[0]);
     auto get = [&](uint32_t s) {
-        load_a.fetch(lds0 + (s & 1) * kStageBytes);
-        load_b.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
+        load_c.fetch(lds0 + (s & 1) * kStageBytes);
+        load_g.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
     };
     get(0);
     stage_done();
     for (uint32_t s = 0; s < s1 - s0; ++s) {
         if (s + 1 < s1 - s0) get(s + 1);
-        multiply<P, AROWS, false>(lds[s & 1], acc);
+        multiply<P, false, GROWS>(lds[s & 1], acc);
         stage_done();
+    }
+}
+
+// Writes up to V values, the first `have` of them.
+template <class T, int V>
+__device__ __forceinline__ void store_some(T* to, int have, const float (&x)[V])
+{
+    if (have >= V) {
+        store_vec<T, V>(to, x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (e < have) to[e] = from_float<T>(x[e]);
     }
 }
 
@@ -752,36 +788,54 @@ __global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
     __shared__ __align__(16) unsigned char lds[2][kStageBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t h_blocks = a.h_tiles * a.col_tiles * a.h_splits;
-    // eight workgroups of dH, eight of dW, as long as there are both: every XCD has its share of either
-    const uint32_t w_blocks = gridDim.x - h_blocks, both = min(h_blocks, w_blocks) & ~7u;
+    // (dH's workgroups first, then dW's: a CU that has two has one of either, which differ in how long they take)
     uint32_t b = blockIdx.x;
-    bool dh;
-    if (b < 2 * both) {
-        dh = !(b & 8);
-        b = (b >> 4) * 8 + (b & 7);
-    } else {
-        b -= both;
-        dh = b < h_blocks;
-        if (!dh) b -= h_blocks - both;
-    }
-    b = by_xcd(b, dh ? h_blocks : w_blocks);
+    const bool dh = b < h_blocks;
+    if (!dh) b -= h_blocks;
     const uint32_t splits = dh ? a.h_splits : a.w_splits, share = dh ? a.h_share : a.w_share, stages = dh ? a.h_stages : a.w_stages;
     const uint32_t col = b % a.col_tiles, split = b / a.col_tiles % splits, tile = b / a.col_tiles / splits;
     const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
     f32x16 acc[2][2];
-    if (dh) product_tile<P, true>(a.g_rows, a.w, tile * kTile, col * kTile, s0, s1, lds, acc);
-    else product_tile<P, false>(a.g_cols, a.h, tile * kTile, col * kTile, s0, s1, lds, acc);
+    if (dh) product_tile<P, true>(a.w, a.g_rows, col * kTile, tile * kTile, s0, s1, lds, acc);
+    else product_tile<P, false>(a.h, a.g_cols, col * kTile, tile * kTile, s0, s1, lds, acc);
+    const uint32_t row0 = tile * kTile + (wave & 1) * 64 + (lane & 31), col0 = col * kTile + (wave >> 1) * 64 + 4 * (lane >> 5);
+    if (!dh && !a.dw) {
+        const int k = P == 2 ? -(*a.shift + kGShift) : 0;
+        typedef typename std::conditional<P == 2, float, bf16_t>::type T;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (row0 + 32 * j >= a.rows) continue;
+            T* to = static_cast<T*>(a.out) + static_cast<int64_t>(row0 + 32 * j) * a.out_stride + col0;
+#pragma unroll
+            for (int im = 0; im < 2; ++im)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float x[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = (P == 2 ? ldexpf(acc[im][j][4 * q + e], k) : acc[im][j][4 * q + e]) * a.scale;
+                    store_some<T, 4>(to + 32 * im + 8 * q, a.dim - static_cast<int>(col0 + 32 * im + 8 * q), x);
+                }
+        }
+        return;
+    }
     float* out = dh ? a.dh + static_cast<int64_t>(split) * a.tokens * a.cols : a.dw + static_cast<int64_t>(split) * a.piece_rows * a.cols;
     const bool add = dh && a.add;
 #pragma unroll
-    for (int im = 0; im < 2; ++im)
+    for (int j = 0; j < 2; ++j) {
+        float* to = out + static_cast<int64_t>(row0 + 32 * j) * a.cols + col0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int64_t row = static_cast<int64_t>(tile) * kTile + (wave >> 1) * 64 + 32 * im + sum_row(i);
-            float* to = out + row * a.cols + col * kTile + (wave & 1) * 64 + (lane & 31);
+        for (int im = 0; im < 2; ++im)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) to[32 * j] = add ? to[32 * j] + acc[im][j][i] : acc[im][j][i];
-        }
+            for (int q = 0; q < 4; ++q) {
+                float4 x = make_float4(acc[im][j][4 * q], acc[im][j][4 * q + 1], acc[im][j][4 * q + 2], acc[im][j][4 * q + 3]);
+                float4* at = reinterpret_cast<float4*>(to + 32 * im + 8 * q);
+                if (add) {
+                    const float4 old = *at;
+                    x = make_float4(old.x + x.x, old.y + x.y, old.z + x.z, old.w + x.w);
+                }
+                *at = x;
+            }
+    }
 }
 
 // Sums the splits and rounds once.  dH: rows without a target become zeros, the others take their factor.
@@ -835,7 +889,7 @@ int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 struct XentWs {
     int32_t parts, padded, cols;
     int64_t tokens;
-    uint32_t row_tiles, splits;        // of the scores
+    uint32_t row_tiles, splits;        // of the scores, or of a piece's coefficients
     int32_t few_blocks;                // > 0: few rows of H, so many blocks of 16
     int64_t piece;                     // table rows of a piece
     uint32_t h_splits, w_splits, h_share, w_share, h_stages, w_stages;
@@ -852,6 +906,13 @@ struct XentWs {
 bool xent_sizes_ok(int64_t n, int64_t num_rows, int32_t dim, int32_t type)
 {
     return n >= 0 && n <= (1 << 24) && num_rows > 0 && num_rows < (1ll << 31) && dim >= 1 && dim <= NE_OP_MAX_DIM && type_ok(type);
+}
+
+// Workgroups over table tiles for one tile of H: as many as fill the machine, all with about as many tiles.
+uint32_t splits_of(int64_t row_tiles, int64_t token_tiles)
+{
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(row_tiles, kSlots / std::min<int64_t>(token_tiles, kSlots)));
+    return static_cast<uint32_t>(ceil_div(row_tiles, ceil_div(row_tiles, most)));
 }
 
 // The workspace has room for packed copies whether or not this call's alignment needs them.
@@ -882,7 +943,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
         w.w[p] = take.get<uint16_t>(static_cast<size_t>(num_rows) * w.padded);
     }
     if (!grad) {
-        w.splits = static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>(w.row_tiles, kSlots / std::min<int64_t>(token_tiles, kSlots))));
+        w.splits = splits_of(w.row_tiles, token_tiles);
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * w.tokens);
         w.target_score = take.get<float>(static_cast<size_t>(w.tokens));
     } else {
@@ -904,7 +965,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
             w.g[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.piece);
         }
         w.dh = take.get<float>(static_cast<size_t>(w.h_splits) * w.tokens * w.cols);
-        w.dw = take.get<float>(static_cast<size_t>(w.w_splits) * w.piece * w.cols);
+        w.dw = w.w_splits > 1 ? take.get<float>(static_cast<size_t>(w.w_splits) * w.piece * w.cols) : nullptr;
     }
     w.total = take.total();
     return w;
@@ -921,7 +982,7 @@ struct XentCall {
 // Packs H (and c H) and, where it cannot be used as it is, W.
 hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Operand* hc, Operand* wo, hipStream_t st)
 {
-    const bool direct = x.type == NE_BF16 && x.dim % kPadDim == 0 && x.w_stride % 8 == 0 && aligned(x.w, 16);
+    const bool direct = x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && aligned(x.w, 16);
     if (x.type == NE_F32) {
         AmaxArgs a{static_cast<const float*>(x.h), static_cast<const float*>(x.w), x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, x.dim, w.amax};
         hipLaunchKernelGGL(amax_kernel, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
@@ -954,6 +1015,7 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Opera
         *wo = operand(w.w, x.num_rows);
         wo->part[0] = static_cast<const uint16_t*>(x.w);
         wo->stride = x.w_stride;
+        wo->width = static_cast<uint32_t>(x.dim);
     } else {
         if (e == hipSuccess) e = run(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
         *wo = operand(w.w, x.num_rows);
@@ -1014,6 +1076,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     pa.cols = static_cast<uint32_t>(w.cols); pa.col_tiles = pa.cols / kTile;
     pa.h_splits = w.h_splits; pa.w_splits = w.w_splits; pa.h_share = w.h_share; pa.w_share = w.w_share;
     pa.w_stages = w.w_stages;
+    pa.out_stride = dw_stride; pa.dim = x.dim; pa.scale = scale; pa.shift = w.shift + (x.c ? 2 : 1);
     auto reduce = [&](ReduceArgs r) {
         r.cols = pa.cols; r.dim = x.dim; r.scale = scale;
         if (P == 1) r.shift = nullptr;
@@ -1024,8 +1087,10 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         const int64_t rows = std::min<int64_t>(w.piece, x.num_rows - base);
         ca.row_base = static_cast<uint32_t>(base);
         ca.row_tiles = static_cast<uint32_t>(ceil_div(rows, kTile));
+        ca.splits = splits_of(ca.row_tiles, token_tiles);
+        ca.tokens = static_cast<uint32_t>(w.tokens);
         for (int p = 0; p < P; ++p) ca.g[p] = w.g[p];
-        hipLaunchKernelGGL(coef_kernel<P>, dim3(token_tiles * ca.row_tiles), dim3(kThreads), 0, st, ca);
+        hipLaunchKernelGGL(coef_kernel<P>, dim3(token_tiles * ca.splits), dim3(kThreads), 0, st, ca);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         pa.g_rows = Operand{{w.g[0], w.g[1]}, w.piece, static_cast<uint32_t>(w.tokens - 1), static_cast<uint32_t>(w.piece)};
@@ -1037,12 +1102,14 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         pa.w_tiles = dw ? ca.row_tiles : 0;
         pa.h_stages = static_cast<uint32_t>(ceil_div(rows, step_of<P>()));      // (no stage begins beyond the last row)
         pa.add = base > 0;
+        pa.rows = static_cast<uint32_t>(rows);
+        pa.out = dw ? static_cast<T*>(dw) + base * dw_stride : nullptr;
         const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
         if (!blocks) continue;
         hipLaunchKernelGGL(products_kernel<P>, dim3(blocks), dim3(kThreads), 0, st, pa);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
-        if (dw) {
+        if (dw && w.dw) {
             ReduceArgs r{};
             r.in = w.dw; r.split_stride = w.piece * pa.cols; r.splits = w.w_splits; r.rows = rows;
             r.out = static_cast<T*>(dw) + base * dw_stride; r.out_stride = dw_stride;
