@@ -90,6 +90,14 @@ struct Loader {
         return (P == 1 ? q * 4 : (q & 1) * 4) + wave;
     }
 
+    // ROWS: which 16 bytes of its row a lane fetches: those that are read from the lane's place in LDS.  (Pieces of rows 0, 2, 4 .. lie at
+    // the index XOR 0, 1, 2 ..; half-length rows 0, 4, 8 ..: so the 16 rows that LDS serves at a time are in different banks.)
+    __device__ __forceinline__ static uint32_t place_in_row()
+    {
+        const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        return P == 1 ? (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4)) : (lane & 3) ^ (lane >> 4);
+    }
+
     __device__ __forceinline__ void start(const Operand& o, uint32_t row0, uint32_t stage)
     {
         const int lane = threadIdx.x & 63;
@@ -104,8 +112,7 @@ struct Loader {
             const int j = piece(q);
             if (ROWS) {
                 const uint32_t row = P == 1 ? j * 8 + (lane >> 3) : j * 16 + (lane >> 2);
-                const uint32_t at = P == 1 ? (lane & 7) ^ (lane >> 3) : (lane & 3) ^ ((lane >> 3) & 3);
-                offset[q] = min(row, o.last - row0) * stride + at * 16;
+                offset[q] = min(row, o.last - row0) * stride + place_in_row() * 16;
             } else {
                 const uint32_t col = row0 + (((lane & 15) ^ ((lane >> 4) << 2)) << 3);
                 offset[q] = (j * 4 + (lane >> 4)) * stride + min(col, o.width - 8) * 2;
@@ -125,7 +132,7 @@ struct Loader {
             for (int q = 0; q < 4; ++q) {
                 uint32_t back;
                 if (ROWS) {
-                    const uint32_t e = 8 * (P == 1 ? (lane & 7) ^ (lane >> 3) : (lane & 3) ^ ((lane >> 3) & 3));
+                    const uint32_t e = 8 * place_in_row();
                     back = (e - min(e, ks - 8)) * 2;
                 } else {
                     const uint32_t k = piece(q) * 4 + (lane >> 4);
@@ -149,7 +156,7 @@ __device__ __forceinline__ s16x8 fragment(const unsigned char* lds, int part, in
     const unsigned char* base = lds + (P == 1 ? 0 : part * (kOperandBytes / 2));
     if (ROWS) {
         const int row = r0 + (lane & 31), piece = kk * 2 + (lane >> 5);
-        const int at = P == 1 ? row * 128 + ((piece ^ (row & 7)) << 4) : row * 64 + ((piece ^ ((row >> 1) & 3)) << 4);
+        const int at = P == 1 ? row * 128 + ((piece ^ ((row >> 1) & 7)) << 4) : row * 64 + ((piece ^ ((row >> 2) & 3)) << 4);
         return *reinterpret_cast<const s16x8*>(base + at);
     }
     // 16 lanes get 16 columns of 4 rows: lane i points to the i % 4-th 8 bytes of row i / 4 and receives column i
