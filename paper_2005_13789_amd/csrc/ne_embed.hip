@@ -27,7 +27,6 @@ constexpr int kMostTiles = 128;     // workgroups of a sorting pass; each reads 
 constexpr int kMostDigits = 1024;
 constexpr int kRowsPerGroup = 64;   // table rows of a workgroup of the rows launch
 constexpr int kFewIds = 16384;      // up to so many ids every workgroup looks through all of them
-constexpr int kFewThreads = 256;    // threads of a workgroup there
 constexpr int kScan = 16;           // ids of a thread and round there
 constexpr int kMostSlots = 256;     // rows of a workgroup there
 constexpr int kAddIds = 32;         // accumulate: positions of a workgroup there ...
@@ -350,10 +349,10 @@ __device__ __forceinline__ void write_chunk(const GradArgs& a, uint32_t row, int
 }
 
 // Sum over the lane groups of a workgroup, in the groups' order, for group 0.
-template <int THREADS, int V>
+template <int V>
 __device__ __forceinline__ void join_groups(float (*lds)[V], int lanes_log2, float (&acc)[V])
 {
-    const int lanes = 1 << lanes_log2, groups = THREADS >> lanes_log2;
+    const int lanes = 1 << lanes_log2, groups = kThreads >> lanes_log2;
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) lds[threadIdx.x][e] = acc[e];
@@ -372,27 +371,49 @@ __device__ __forceinline__ void join_groups(float (*lds)[V], int lanes_log2, flo
 //   none(r): leave row r alone;  single(k, at, x): position k's values;  term(r, t, at, x): term t of a long row, which has terms(r).
 constexpr uint32_t kLongRun = 32;
 
-template <int THREADS, class TT, int V, bool ADD, class None, class Single, class Terms, class Term, class Row>
-__device__ __forceinline__ void sum_rows(const GradArgs& a, uint32_t rows, const uint32_t* start, float (*lds)[V], None none, Single single, Terms terms,
-                                         Term term, Row row_of)
+struct RowLists {
+    uint16_t live[kMostSlots], hot[kMostSlots];     // rows of fewer than kLongRun positions (but some), and of more
+    uint32_t wave_sums[kThreads / 64];
+};
+
+template <class TT, int V, bool ADD, class None, class Single, class Terms, class Term, class Row>
+__device__ __forceinline__ void sum_rows(const GradArgs& a, uint32_t rows, const uint32_t* start, float (*lds)[V], RowLists& lists, None none, Single single,
+                                         Terms terms, Term term, Row row_of)
 {
     constexpr int U = 8, OLD = ADD ? 4 : 1;
-    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = THREADS >> a.lanes_log2;
-    const uint32_t share = (rows + groups - 1) / groups, begin = min(group * share, rows), end = min(begin + share, rows);
-    auto skip = [&](uint32_t r) { return start[r + 1] - start[r] >= kLongRun || none(r); };
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
+    const uint32_t mine = threadIdx.x < rows && !none(threadIdx.x) ? start[threadIdx.x + 1] - start[threadIdx.x] : 0;
+    const uint32_t is_live = mine > 0 && mine < kLongRun, is_hot = mine >= kLongRun;
+    uint32_t total;
+    const uint32_t at_list = block_prefix<kThreads>(is_live | is_hot << 16, lists.wave_sums, &total);
+    if (is_live) lists.live[at_list & 0xFFFF] = static_cast<uint16_t>(threadIdx.x);
+    if (is_hot) lists.hot[at_list >> 16] = static_cast<uint16_t>(threadIdx.x);
+    const uint32_t lives = total & 0xFFFF, hots = total >> 16;
+    if (!ADD) {
+        float zero[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) zero[e] = 0.0f;
+#pragma unroll 4
+        for (uint32_t r = group; r < rows; r += groups)
+            if (start[r] == start[r + 1])
+                for (int c = lane; c < a.chunks; c += lanes)
+                    store_vec<TT, V>(static_cast<TT*>(a.table) + static_cast<int64_t>(row_of(r)) * a.table_stride + min(c * V, a.dim - V), zero);
+    }
+    __syncthreads();
+    const uint32_t share = (lives + groups - 1) / groups, begin = min(group * share, lives), end = min(begin + share, lives);
     for (int c = lane; c < a.chunks; c += lanes) {
         const int at = min(c * V, a.dim - V);
-        for (uint32_t r = begin; r < end;) {
-            if (skip(r)) { ++r; continue; }
-            uint32_t last = r + 1;
-            while (last < end && !skip(last) && (!ADD || last < r + OLD)) ++last;
-            const uint32_t stop = start[last];
-            uint32_t k = start[r], next = start[r + 1];
+        uint32_t i = begin;
+        while (i < end) {
+            // rows whose positions follow one another (no long row's are between them)
+            uint32_t last = i + 1, stop = start[lists.live[i] + 1];
+            while (last < end && (!ADD || last < i + OLD) && start[lists.live[last]] == stop) stop = start[lists.live[last++] + 1];
+            uint32_t r = lists.live[i], k = start[r], next = start[r + 1];
             float acc[V] = {}, old[OLD][V] = {};        // (old: of the rows still to be written, the next one first)
             if (ADD)
 #pragma unroll
                 for (int q = 0; q < OLD; ++q)
-                    if (r + q < last) load_old<TT, V>(a, row_of(r + q), at, old[q]);
+                    if (i + q < last) load_old<TT, V>(a, row_of(lists.live[i + q]), at, old[q]);
             auto finish_row = [&]() {
                 write_chunk<TT, V, ADD>(a, row_of(r), c, at, acc, old[0]);
 #pragma unroll
@@ -401,8 +422,10 @@ __device__ __forceinline__ void sum_rows(const GradArgs& a, uint32_t rows, const
 #pragma unroll
                     for (int q = 0; q + 1 < OLD; ++q) old[q][e] = old[q + 1][e];
                 }
-                ++r;
-                next = start[min(r + 1, rows)];
+                if (++i < last) {
+                    r = lists.live[i];
+                    next = start[r + 1];
+                }
             };
             for (; k < stop; k += U) {
                 float x[U][V];
@@ -412,21 +435,21 @@ __device__ __forceinline__ void sum_rows(const GradArgs& a, uint32_t rows, const
 #pragma unroll
                 for (int q = 0; q < U; ++q)
                     if (k + q < stop) {
-                        while (k + q >= next) finish_row();
+                        if (k + q == next) finish_row();
 #pragma unroll
                         for (int e = 0; e < V; ++e) acc[e] += x[q][e];
                     }
             }
-            while (r < last) finish_row();
+            finish_row();
         }
     }
-    for (uint32_t r = 0; r < rows; ++r) {
-        if (start[r + 1] - start[r] < kLongRun || none(r)) continue;
+    for (uint32_t h = 0; h < hots; ++h) {
+        const uint32_t r = lists.hot[h];
         for (int c0 = 0; c0 < a.chunks; c0 += lanes) {
             const int c = c0 + lane, at = min(min(c, a.chunks - 1) * V, a.dim - V);
             float acc[V] = {};
             sum_terms<U, V>(group, terms(r), groups, acc, [&](uint32_t t, float (&x)[V]) { term(r, t, at, x); });
-            join_groups<THREADS, V>(lds, a.lanes_log2, acc);
+            join_groups<V>(lds, a.lanes_log2, acc);
             if (group == 0 && c < a.chunks) {
                 float old[V] = {};
                 if (ADD) load_old<TT, V>(a, row_of(r), at, old);
@@ -509,6 +532,7 @@ template <class TG, class TT, int V, bool ADD>
 __global__ void __launch_bounds__(kThreads) rows_kernel(GradArgs a)
 {
     __shared__ float lds[kThreads][V];
+    __shared__ RowLists lists;
     __shared__ uint32_t start[kRowsPerGroup + 1], key[ADD ? kRowsPerGroup : kKeysInLds], place[ADD ? 1 : kKeysInLds], bounds[2];
     const int wave = threadIdx.x >> 6;
     uint32_t lo = 0, len = 0xFFFFFFFFu;
@@ -566,8 +590,8 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(GradArgs a)
     __syncthreads();
     auto position = [&](uint32_t k) { return !ADD && len <= kKeysInLds ? place[k - lo] : a.sorted[k].y; };
     const TG* grad = static_cast<const TG*>(a.grad);
-    sum_rows<kThreads, TT, V, ADD>(
-        a, rows, start, lds, [](uint32_t) { return false; },
+    sum_rows<TT, V, ADD>(
+        a, rows, start, lds, lists, [](uint32_t) { return false; },
         [&](uint32_t k, int at, float (&x)[V]) { load_vec<TG, V>(grad + static_cast<int64_t>(position(k)) * a.grad_stride + at, x); },
         [&](uint32_t r) { return run_of(start[r], start[r + 1], a.super != nullptr).terms; },
         [&](uint32_t r, uint32_t t, int at, float (&x)[V]) { load_term<TG, V>(a, run_of(start[r], start[r + 1], a.super != nullptr), t, at, x, position); },
@@ -588,11 +612,12 @@ struct FewArgs {
 };
 
 template <class TG, class TT, int V, bool ADD>
-__global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
+__global__ void __launch_bounds__(kThreads) few_ids_kernel(FewArgs f)
 {
     extern __shared__ uint32_t found[];        // [n rounded up]  slot << 16 | position; behind them [n] positions by slot (16 bits)
-    __shared__ float lds[kFewThreads][V];
-    __shared__ uint32_t count[kFewThreads / 64][kMostSlots], wave_sums[kFewThreads / 64];
+    __shared__ float lds[kThreads][V];
+    __shared__ RowLists lists;
+    __shared__ uint32_t count[kThreads / 64][kMostSlots], wave_sums[kThreads / 64];
     __shared__ uint32_t start[kMostSlots + 1];
     // ADD: the ids of the places and the slots that they have, the slots' ids, and whether an earlier workgroup has them
     __shared__ uint32_t place_id[ADD ? kAddPlaces : 1], owner[ADD ? kAddIds : 1], taken[ADD ? kAddIds : 1], slots_used;
@@ -603,8 +628,8 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
     const uint32_t first = ADD ? blockIdx.x * kAddIds : blockIdx.x * f.slots;
     const int wave = threadIdx.x >> 6, lane64 = threadIdx.x & 63;
     if (ADD) {
-        for (uint32_t i = threadIdx.x; i < kAddPlaces; i += kFewThreads) place_id[i] = 0xFFFFFFFFu;
-        for (uint32_t i = threadIdx.x; i < kAddFilter; i += kFewThreads) filter[i] = 0;
+        for (uint32_t i = threadIdx.x; i < kAddPlaces; i += kThreads) place_id[i] = 0xFFFFFFFFu;
+        for (uint32_t i = threadIdx.x; i < kAddFilter; i += kThreads) filter[i] = 0;
         if (threadIdx.x < kAddIds) taken[threadIdx.x] = 0;
         if (threadIdx.x == 0) slots_used = 0;
         __syncthreads();
@@ -637,12 +662,12 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
         }
     };
     fetch_ids(threadIdx.x * kScan);
-    for (uint32_t r0 = 0; r0 < a.n; r0 += kFewThreads * kScan) {
+    for (uint32_t r0 = 0; r0 < a.n; r0 += kThreads * kScan) {
         uint32_t id[kScan];
         const uint32_t at = r0 + threadIdx.x * kScan;
 #pragma unroll
         for (int q = 0; q < kScan; ++q) id[q] = ahead[q];
-        if (r0 + kFewThreads * kScan < a.n) fetch_ids(at + kFewThreads * kScan);
+        if (r0 + kThreads * kScan < a.n) fetch_ids(at + kThreads * kScan);
         uint32_t wanted = 0, word[kScan];
         if (ADD)
 #pragma unroll
@@ -653,7 +678,7 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
             wanted |= static_cast<uint32_t>(in) << q;
         }
         uint32_t total;
-        uint32_t to = have + block_prefix<kFewThreads>(__popc(wanted), wave_sums, &total);
+        uint32_t to = have + block_prefix<kThreads>(__popc(wanted), wave_sums, &total);
 #pragma unroll
         for (int q = 0; q < kScan; ++q)
             if (wanted >> q & 1) found[to++] = (ADD ? 0 : (id[q] - first) << 16) | (at + q);
@@ -661,7 +686,7 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
         __syncthreads();
     }
     if (ADD) {      // what passed the filter is looked up; slot kAddIds takes what has no row here, or stands before all of this workgroup's
-        for (uint32_t i = threadIdx.x; i < have; i += kFewThreads) {
+        for (uint32_t i = threadIdx.x; i < have; i += kThreads) {
             const uint32_t k = found[i], id = static_cast<uint32_t>(f.ids[k]);
             uint32_t slot = kAddIds;
             for (uint32_t at = hash_position(id, kAddPlaces - 1);; at = (at + 1) & (kAddPlaces - 1)) {
@@ -678,10 +703,10 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
         __syncthreads();
     }
     // stable sort by slot: counts of every wavefront's share, then places
-    const uint32_t share = (have + kFewThreads - 1) / kFewThreads * 64;      // entries of a wavefront, side by side
-    for (uint32_t i = threadIdx.x; i < kMostSlots; i += kFewThreads)
+    const uint32_t share = (have + kThreads - 1) / kThreads * 64;      // entries of a wavefront, side by side
+    for (uint32_t i = threadIdx.x; i < kMostSlots; i += kThreads)
 #pragma unroll
-        for (int w = 0; w < kFewThreads / 64; ++w) count[w][i] = 0;
+        for (int w = 0; w < kThreads / 64; ++w) count[w][i] = 0;
     __syncthreads();
     for (uint32_t i = wave * share + lane64; i < min((wave + 1) * share, have); i += 64) atomicAdd(&count[wave][found[i] >> 16], 1u);
     __syncthreads();
@@ -690,13 +715,13 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
         uint32_t sum = 0, total;
         if (has_slot)
 #pragma unroll
-            for (int w = 0; w < kFewThreads / 64; ++w) sum += count[w][threadIdx.x];
-        uint32_t at = block_prefix<kFewThreads>(sum, wave_sums, &total);
+            for (int w = 0; w < kThreads / 64; ++w) sum += count[w][threadIdx.x];
+        uint32_t at = block_prefix<kThreads>(sum, wave_sums, &total);
         if (threadIdx.x == 0) start[kMostSlots] = total;
         if (has_slot) {
             start[threadIdx.x] = at;
 #pragma unroll
-            for (int w = 0; w < kFewThreads / 64; ++w) {
+            for (int w = 0; w < kThreads / 64; ++w) {
                 const uint32_t c = count[w][threadIdx.x];
                 count[w][threadIdx.x] = at;
                 at += c;
@@ -716,8 +741,8 @@ __global__ void __launch_bounds__(kFewThreads) few_ids_kernel(FewArgs f)
     auto single = [&](uint32_t k, int at, float (&x)[V]) {
         load_vec<TG, V>(static_cast<const TG*>(a.grad) + static_cast<int64_t>(sorted[k]) * a.grad_stride + at, x);
     };
-    sum_rows<kFewThreads, TT, V, ADD>(
-        a, ADD ? slots_used : min(f.slots, a.num_rows - first), start, lds, [&](uint32_t r) { return ADD && taken[r]; }, single,
+    sum_rows<TT, V, ADD>(
+        a, ADD ? slots_used : min(f.slots, a.num_rows - first), start, lds, lists, [&](uint32_t r) { return ADD && taken[r]; }, single,
         [&](uint32_t r) { return start[r + 1] - start[r]; },
         [&](uint32_t r, uint32_t t, int at, float (&x)[V]) { single(start[r] + t, at, x); }, [&](uint32_t r) { return ADD ? owner[r] : first + r; });
 }
@@ -794,8 +819,8 @@ hipError_t launch_few(const GradArgs& a, const int32_t* ids, bool add, hipStream
     }
     while ((1u << f.slot_bits) < f.slots + (add ? 1 : 0)) f.slot_bits += 1;
     const uint32_t blocks = add ? (a.n + kAddIds - 1) / kAddIds : (a.num_rows + f.slots - 1) / f.slots;
-    if (add) hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, true>), dim3(blocks), dim3(kFewThreads), lds, st, f);
-    else hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, false>), dim3(blocks), dim3(kFewThreads), lds, st, f);
+    if (add) hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, true>), dim3(blocks), dim3(kThreads), lds, st, f);
+    else hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, false>), dim3(blocks), dim3(kThreads), lds, st, f);
     return hipGetLastError();
 }
 

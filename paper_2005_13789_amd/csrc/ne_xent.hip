@@ -39,7 +39,7 @@ constexpr int kOperandBytes = 16384;   // one operand's share of a stage in LDS 
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kPadDim = 64;            // packed rows are a multiple of this, filled with zeros
 constexpr int kSlots = 512;            // workgroups that run at once: 256 CUs, two each
-constexpr int kAmaxBlocks = 256;
+constexpr int kAmaxBlocks = 1024;
 constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
 constexpr int kFewBytes = 65536;
 constexpr int kFewGroups = 1024;
@@ -265,23 +265,56 @@ __device__ __forceinline__ float block_max(float v, float* lds)
     return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
 }
 
+// Eight elements from index e on, zeros beyond dim.
+template <class T>
+__device__ __forceinline__ void load_eight(const T* row, int e, int dim, T (&x)[8])
+{
+    if (e + 8 <= dim) {
+        __builtin_memcpy(x, row + e, 8 * sizeof(T));
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = e + q < dim ? row[e + q] : from_float<T>(0.0f);
+    }
+}
+
+// Rows of `dim` elements, eight a lane: use(row, e, x) for a lane group's rows, two of them in flight.
+template <class T, class Use>
+__device__ __forceinline__ void for_eights(const T* in, int64_t stride, int64_t rows, int dim, int width, Use use)
+{
+    int lanes_log2 = 0;
+    while (lanes_log2 < 6 && (8 << lanes_log2) < width) ++lanes_log2;
+    const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
+    const int64_t groups = static_cast<int64_t>(gridDim.x) * (kThreads >> lanes_log2);
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
+    for (int e = lane * 8; e < width; e += 8 * lanes)
+        for (int64_t r = first; r < rows; r += 4 * groups) {
+            T x[4][8];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (r + q * groups < rows) load_eight(in + (r + q * groups) * stride, e, dim, x[q]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (r + q * groups < rows) use(r + q * groups, e, x[q]);
+        }
+}
+
 __global__ void __launch_bounds__(kThreads) amax_kernel(AmaxArgs a)
 {
     __shared__ float lds[4];
-    const int lane = threadIdx.x & 63;
-    const int64_t wave = blockIdx.x * 4 + (threadIdx.x >> 6), waves = kAmaxBlocks * 4;
     float w = 0.0f, h = 0.0f, ch = 0.0f;
-    for (int64_t v = wave; v < a.num_rows; v += waves)
-        for (int e = lane; e < a.dim; e += 64) w = fmaxf(w, finite_abs(a.w[v * a.w_stride + e]));
-    for (int64_t i = wave; i < a.n; i += waves) {
-        if (static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) continue;
+    for_eights(a.w, a.w_stride, a.num_rows, a.dim, a.dim, [&](int64_t, int, const float (&x)[8]) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w = fmaxf(w, finite_abs(x[q]));
+    });
+    for_eights(a.h, a.h_stride, a.n, a.dim, a.dim, [&](int64_t i, int, const float (&x)[8]) {
+        if (static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) return;
         const float c = a.c ? a.c[i] : 1.0f;
-        for (int e = lane; e < a.dim; e += 64) {
-            const float x = a.h[i * a.h_stride + e];
-            h = fmaxf(h, finite_abs(x));
-            ch = fmaxf(ch, finite_abs(c * x));
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            h = fmaxf(h, finite_abs(x[q]));
+            ch = fmaxf(ch, finite_abs(c * x[q]));
         }
-    }
+    });
     w = block_max(w, lds);
     h = block_max(h, lds);
     ch = block_max(ch, lds);
@@ -312,39 +345,43 @@ struct PackArgs {
     int32_t* shift;                // fp32 only: receives the power of two
 };
 
-// One row per wavefront at a time, 8 elements a lane.
 template <int P>
 __global__ void __launch_bounds__(kThreads) pack_kernel(PackArgs a)
 {
+    typedef typename std::conditional<P == 2, float, bf16_t>::type T;
     __shared__ float lds[4];
     int k = 0;
     if (P == 2) {
-        k = shift_of(block_max(a.amax[threadIdx.x], lds));
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kAmaxBlocks / kThreads; ++i) top = fmaxf(top, a.amax[i * kThreads + threadIdx.x]);
+        k = shift_of(block_max(top, lds));
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.shift = k;
     }
-    const int lane = threadIdx.x & 63;
-    const int64_t wave = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), waves = static_cast<int64_t>(gridDim.x) * 4;
-    for (int64_t r = wave; r < a.padded_rows; r += waves) {
-        const bool counts = r < a.rows && (!a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets);
-        const float c = counts && a.c ? a.c[r] : 1.0f;
-        for (int e0 = lane * 8; e0 < a.padded; e0 += 512) {
-            s16x8 out[P];
+    auto write = [&](int64_t r, int e0, const T (&x)[8]) {
+        s16x8 out[P];
+        const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
+        const float c = a.c ? a.c[r] : 1.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool have = counts && e0 + e < a.dim;
-                if (P == 1) {
-                    out[0][e] = have ? static_cast<const short*>(a.in)[r * a.in_stride + e0 + e] : 0;
-                } else {
-                    const float x = have ? ldexpf(c * static_cast<const float*>(a.in)[r * a.in_stride + e0 + e], k) : 0.0f;
-                    const f16_t hi = static_cast<f16_t>(x), lo = static_cast<f16_t>(x - static_cast<float>(hi));
-                    out[0][e] = __builtin_bit_cast(short, hi);
-                    out[P - 1][e] = P == 2 ? __builtin_bit_cast(short, lo) : out[0][e];
-                }
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (P == 1) {
+                out[0][e] = counts ? __builtin_bit_cast(short, x[e]) : 0;
+            } else {
+                const float y = counts ? ldexpf(c * x[e], k) : 0.0f;
+                const f16_t hi = static_cast<f16_t>(y);
+                out[0][e] = __builtin_bit_cast(short, hi);
+                out[1][e] = __builtin_bit_cast(short, static_cast<f16_t>(y - static_cast<float>(hi)));
             }
-#pragma unroll
-            for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + r * a.padded + e0) = out[p];
         }
-    }
+#pragma unroll
+        for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + r * a.padded + e0) = out[p];
+    };
+    for_eights(static_cast<const T*>(a.in), a.in_stride, a.rows, a.dim, a.padded, write);
+    // rows beyond the last one: zeros
+    const int64_t zeros = (a.padded_rows - a.rows) * a.padded / 8;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < zeros; i += static_cast<int64_t>(gridDim.x) * kThreads)
+#pragma unroll
+        for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + a.rows * a.padded + i * 8) = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -517,18 +554,6 @@ struct FewArgs {
     float2* stat;                  // [n][workgroups]
     float* target_score;
 };
-
-// Eight elements from index e on as floats or bf16, zeros beyond dim.
-template <class T>
-__device__ __forceinline__ void load_eight(const T* row, int e, int dim, T (&x)[8])
-{
-    if (e + 8 <= dim) {
-        __builtin_memcpy(x, row + e, 8 * sizeof(T));
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) x[q] = e + q < dim ? row[e + q] : from_float<T>(0.0f);
-    }
-}
 
 template <int PARTS>
 __device__ __forceinline__ void split_bf16(const bf16_t (&x)[8], bf16x8 (&out)[PARTS])
@@ -861,22 +886,51 @@ struct ReduceArgs {
     const int32_t* shift;          // fp32 only: power of two of the other operand
 };
 
+// A workgroup has 256 columns of a row; where there are many splits its wavefronts share them, and their sums are added in order.
 template <class T>
 __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t waves = static_cast<int64_t>(gridDim.x) * 4;
-    const int k = a.shift ? -(*a.shift + kGShift) : 0;      // (bf16: the sums are what they are)
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); r < a.rows; r += waves) {
-        const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
-        const float c = counts && a.c ? a.c[r] : 1.0f;
-        for (int e = lane; e < a.dim; e += 64) {
-            float sum = 0.0f;
-            for (uint32_t s = 0; s < a.splits; ++s) sum += a.in[s * a.split_stride + r * a.cols + e];
-            sum = ldexpf(sum, k) * a.scale * c;
-            static_cast<T*>(a.out)[r * a.out_stride + e] = from_float<T>(counts ? sum : 0.0f);
+    __shared__ float4 lds[kThreads];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t parts = a.splits >= 16 ? 4 : 1;           // wavefronts of a row
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * (4 / parts) + (parts == 4 ? 0 : wave);
+    const int e = blockIdx.y * 256 + lane * 4;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const bool in = r < a.rows && e < static_cast<int>(a.cols);
+    if (in) {
+        const float* from = a.in + r * a.cols + e;
+        const uint32_t step = parts;
+        uint32_t s = parts == 4 ? wave : 0;
+        for (; s + 7 * step < a.splits; s += 8 * step) {
+            float4 x[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = *reinterpret_cast<const float4*>(from + (s + q * step) * a.split_stride);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum = make_float4(sum.x + x[q].x, sum.y + x[q].y, sum.z + x[q].z, sum.w + x[q].w);
+        }
+        for (; s < a.splits; s += step) {
+            const float4 x = *reinterpret_cast<const float4*>(from + s * a.split_stride);
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
         }
     }
+    if (parts == 4) {
+        lds[threadIdx.x] = sum;
+        __syncthreads();
+        if (wave != 0) return;
+        for (int w = 1; w < 4; ++w) {
+            const float4 x = lds[w * 64 + lane];
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+        }
+    }
+    if (!in) return;
+    const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
+    const int k = a.shift ? -(*a.shift + kGShift) : 0;      // (bf16: the sums are what they are)
+    const float c = counts && a.c ? a.c[r] : 1.0f;
+    const float all[4] = {sum.x, sum.y, sum.z, sum.w};
+    float x[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = counts ? ldexpf(all[q], k) * a.scale * c : 0.0f;
+    store_some<T, 4>(static_cast<T*>(a.out) + r * a.out_stride + e, a.dim - e, x);
 }
 
 template <class T>
@@ -1087,7 +1141,8 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     auto reduce = [&](ReduceArgs r) {
         r.cols = pa.cols; r.dim = x.dim; r.scale = scale;
         if (P == 1) r.shift = nullptr;
-        hipLaunchKernelGGL(reduce_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(ceil_div(r.rows, 4), 4096))), dim3(kThreads), 0, st, r);
+        const dim3 grid(static_cast<unsigned>(ceil_div(r.rows, r.splits >= 16 ? 1 : 4)), static_cast<unsigned>(ceil_div(x.dim, 256)));
+        hipLaunchKernelGGL(reduce_kernel<T>, grid, dim3(kThreads), 0, st, r);
         return hipGetLastError();
     };
     for (int64_t base = 0; base < x.num_rows; base += w.piece) {
