@@ -183,26 +183,36 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
     const int wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
     const unsigned char* A = stage;
     const unsigned char* B = stage + kOperandBytes;
-#pragma unroll
-    for (int kk = 0; kk < step_of<P>() / 16; ++kk) {
-        s16x8 a[P][2], b[P][2];
+    // Operands of the next 16 indices are read while these are multiplied: a read takes as long as four products.  (The compiler would
+    // reuse the registers at once and wait for every read.)
+    constexpr int KK = step_of<P>() / 16;
+    s16x8 a[2][P][2], b[2][P][2];
+    auto read = [&](int kk) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                a[p][i] = fragment<P, AROWS>(A, p, m0 + 32 * i, kk);
-                b[p][i] = fragment<P, BROWS>(B, p, n0 + 32 * i, kk);
+                a[kk & 1][p][i] = fragment<P, AROWS>(A, p, m0 + 32 * i, kk);
+                b[kk & 1][p][i] = fragment<P, BROWS>(B, p, n0 + 32 * i, kk);
             }
+    };
+    read(0);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) read(kk + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const int at = kk & 1;
 #pragma unroll
         for (int im = 0; im < 2; ++im)
 #pragma unroll
             for (int in = 0; in < 2; ++in) {
-                acc[im][in] = mfma<P>(a[0][im], b[0][in], acc[im][in]);
+                acc[im][in] = mfma<P>(a[at][0][im], b[at][0][in], acc[im][in]);
                 if (P == 2) {
-                    acc[im][in] = mfma<P>(a[0][im], b[P - 1][in], acc[im][in]);
-                    acc[im][in] = mfma<P>(a[P - 1][im], b[0][in], acc[im][in]);
+                    acc[im][in] = mfma<P>(a[at][0][im], b[at][P - 1][in], acc[im][in]);
+                    acc[im][in] = mfma<P>(a[at][P - 1][im], b[at][0][in], acc[im][in]);
                 }
             }
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
