@@ -37,7 +37,6 @@ constexpr int kThreads = 256;          // 4 wavefronts, 2 x 2 over a tile
 constexpr int kTile = 128;             // rows and columns of a tile of sums
 constexpr int kOperandBytes = 16384;   // one operand's share of a stage in LDS (all its parts)
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kPadDim = 64;            // packed rows are a multiple of this, filled with zeros
 constexpr int kSlots = 512;            // workgroups that run at once: 256 CUs, two each
 constexpr int kAmaxBlocks = 1024;
 constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
@@ -355,9 +354,14 @@ struct PackArgs {
     int32_t* shift;                // fp32 only: receives the power of two
 };
 
+struct PackJobs {
+    PackArgs job[3];
+};
+
 template <int P>
-__global__ void __launch_bounds__(kThreads) pack_kernel(PackArgs a)
+__global__ void __launch_bounds__(kThreads) pack_kernel(PackJobs jobs)
 {
+    const PackArgs& a = jobs.job[blockIdx.y];
     typedef typename std::conditional<P == 2, float, bf16_t>::type T;
     __shared__ float lds[4];
     int k = 0;
@@ -991,7 +995,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
 {
     XentWs w{};
     w.parts = type == NE_F32 ? 2 : 1;
-    w.padded = static_cast<int32_t>(round_up(dim, kPadDim));
+    w.padded = static_cast<int32_t>(round_up(dim, w.parts == 1 ? step_of<1>() : step_of<2>()));
     w.cols = static_cast<int32_t>(round_up(dim, kTile));
     w.tokens = round_up(n, kTile);
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, kTile));
@@ -1060,38 +1064,40 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Opera
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    auto run = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which) {
-        PackArgs a{};
+    PackJobs jobs{};
+    int count = 0;
+    int64_t most = 0;
+    auto add = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which) {
+        PackArgs& a = jobs.job[count++];
         a.in = in; a.in_stride = stride; a.rows = rows; a.padded_rows = padded_rows; a.targets = targets;
         a.num_targets = static_cast<uint32_t>(x.num_rows); a.c = c; a.dim = x.dim; a.padded = w.padded;
         a.out[0] = out[0]; a.out[1] = out[1]; a.amax = w.amax + which * kAmaxBlocks; a.shift = w.shift + which;
-        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(padded_rows, 4), 2048)));
-        if (w.parts == 1) hipLaunchKernelGGL(pack_kernel<1>, grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(pack_kernel<2>, grid, dim3(kThreads), 0, st, a);
-        return hipGetLastError();
+        most = std::max(most, padded_rows);
     };
     auto operand = [&](uint16_t* const* part, int64_t rows) {
         Operand o{};
         o.part[0] = part[0]; o.part[1] = part[1]; o.stride = w.padded; o.last = static_cast<uint32_t>(rows - 1); o.width = static_cast<uint32_t>(w.padded);
         return o;
     };
-    hipError_t e = run(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1);
+    add(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1);
     *h = operand(w.h, w.tokens);
     *hc = *h;
-    if (e == hipSuccess && grad && x.type == NE_F32 && x.c) {
-        e = run(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, 2);
+    if (grad && x.type == NE_F32 && x.c) {
+        add(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, 2);
         *hc = operand(w.hc, w.tokens);
     }
+    *wo = operand(w.w, x.num_rows);
     if (direct) {
-        *wo = operand(w.w, x.num_rows);
         wo->part[0] = static_cast<const uint16_t*>(x.w);
         wo->stride = x.w_stride;
         wo->width = static_cast<uint32_t>(x.dim);
     } else {
-        if (e == hipSuccess) e = run(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
-        *wo = operand(w.w, x.num_rows);
+        add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
     }
-    return e;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(most, 4), 2048)), static_cast<unsigned>(count));
+    if (w.parts == 1) hipLaunchKernelGGL(pack_kernel<1>, grid, dim3(kThreads), 0, st, jobs);
+    else hipLaunchKernelGGL(pack_kernel<2>, grid, dim3(kThreads), 0, st, jobs);
+    return hipGetLastError();
 }
 
 hipError_t join_losses(const XentCall& x, const XentWs& w, float* loss, float* lse, hipStream_t st)
