@@ -33,11 +33,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kThreads = 256;          // 4 wavefronts, 2 x 2 over a tile
-constexpr int kTile = 128;             // rows and columns of a tile of sums
-constexpr int kOperandBytes = 16384;   // one operand's share of a stage in LDS (all its parts)
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kSlots = 512;            // workgroups that run at once: 256 CUs, two each
+constexpr int kThreads = 256;
+constexpr int kTile = 128;             // rows of H and columns of the gradients are padded to multiples of this
 constexpr int kAmaxBlocks = 1024;
 constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
 constexpr int kFewBytes = 65536;
@@ -48,6 +45,14 @@ constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
 
 template <int P> constexpr int step_of() { return P == 1 ? 64 : 32; }   // contraction indices of a stage
 
+// A tile of sums is 128 x 128, of four wavefronts (W = 4) with 64 x 64 each, or 256 x 256, of eight (W = 8) with 128 x 64 each.  Two stages
+// of a large tile fill LDS (128 KB), so one workgroup runs on a CU; of small tiles two run, and one multiplies while the other
+// takes exponentials or waits.  Per operation a large tile fetches half as much from L2, which is what bounds the small ones.
+template <int W> constexpr int rows_of() { return W == 8 ? 256 : 128; }
+template <int W> constexpr int operand_bytes() { return rows_of<W>() * 128; }   // one operand's share of a stage in LDS (all its parts)
+template <int W> constexpr int stage_bytes() { return 2 * operand_bytes<W>(); }
+constexpr int slots_of(bool large) { return large ? 256 : 512; }        // workgroups that run at once
+
 // An operand of a product.  ROWS: element (row, k) at row * stride + k.  Otherwise (row, k) at k * stride + row.
 struct Operand {
     const uint16_t* part[2];
@@ -57,7 +62,7 @@ struct Operand {
 };
 
 // ---------------------------------------------------------------------------------------------
-// a stage: 128 rows x step_of<P>() contraction indices of each operand's P parts
+// a stage: rows_of<W>() rows x step_of<P>() contraction indices of each operand's P parts
 // ---------------------------------------------------------------------------------------------
 // Loads go from memory to LDS directly, and are waited for once a stage (stage_done), before the barrier that hands the stage
 // over: a stage is in flight while the one before it is multiplied.  They are written in assembly because the compiler waits for
@@ -75,19 +80,16 @@ __device__ __forceinline__ uint32_t lds_address(const unsigned char* p)
     return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char*)p)));
 }
 
-// Rows row0 .. row0 + 127 of an operand, stage after stage.
-template <int P, bool ROWS>
+// Rows row0 .. row0 + rows_of<W>() - 1 of an operand, stage after stage, in pieces of 1 KB.
+template <int P, int W, bool ROWS>
 struct Loader {
+    static constexpr int R = rows_of<W>(), kPieces = 4 / P;     // pieces of a wavefront, per part
     const unsigned char* base[P];
     int64_t advance;               // bytes from one stage to the next
-    uint32_t offset[4];
+    uint32_t offset[kPieces];
     uint32_t stride, ks;           // bytes of a row; contraction indices that are left
 
-    __device__ __forceinline__ static int piece(int q)
-    {
-        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-        return (P == 1 ? q * 4 : (q & 1) * 4) + wave;
-    }
+    __device__ __forceinline__ static int piece(int q) { return q * W + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)); }
 
     // ROWS: which 16 bytes of its row a lane fetches: those that are read from the lane's place in LDS.  (Pieces of rows 0, 2, 4 .. lie at
     // the index XOR 0, 1, 2 ..; half-length rows 0, 4, 8 ..: so the 16 rows that LDS serves at a time are in different banks.)
@@ -95,6 +97,13 @@ struct Loader {
     {
         const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         return P == 1 ? (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4)) : (lane & 3) ^ (lane >> 4);
+    }
+
+    // Otherwise: which contraction index of the stage.
+    __device__ __forceinline__ static uint32_t k_of(int q)
+    {
+        const int lane = threadIdx.x & 63;
+        return R == 128 ? piece(q) * 4 + (lane >> 4) : piece(q) * 2 + (lane >> 5);
     }
 
     __device__ __forceinline__ void start(const Operand& o, uint32_t row0, uint32_t stage)
@@ -107,14 +116,13 @@ struct Loader {
 #pragma unroll
         for (int p = 0; p < P; ++p) base[p] = reinterpret_cast<const unsigned char*>(o.part[p] + first);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int j = piece(q);
+        for (int q = 0; q < kPieces; ++q) {
             if (ROWS) {
-                const uint32_t row = P == 1 ? j * 8 + (lane >> 3) : j * 16 + (lane >> 2);
+                const uint32_t row = P == 1 ? piece(q) * 8 + (lane >> 3) : piece(q) * 16 + (lane >> 2);
                 offset[q] = min(row, o.last - row0) * stride + place_in_row() * 16;
-            } else {
-                const uint32_t col = row0 + (((lane & 15) ^ ((lane >> 4) << 2)) << 3);
-                offset[q] = (j * 4 + (lane >> 4)) * stride + min(col, o.width - 8) * 2;
+            } else {        // (the 32 bytes u of row k lie at u XOR 2 (k % 4))
+                const uint32_t k = k_of(q), col = row0 + (((lane & (R / 8 - 1)) ^ ((k & 3) << 2)) << 3);
+                offset[q] = k * stride + min(col, o.width - 8) * 2;
             }
         }
     }
@@ -122,37 +130,31 @@ struct Loader {
     // (contraction indices beyond the last ones are those again: the other operand has zeros there)
     __device__ __forceinline__ void fetch(uint32_t lds)
     {
-        const int lane = threadIdx.x & 63;
-        if (ks >= static_cast<uint32_t>(step_of<P>())) {
+        uint32_t back[kPieces] = {};
+        if (ks < static_cast<uint32_t>(step_of<P>()))
 #pragma unroll
-            for (int q = 0; q < 4; ++q) load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q], lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t back;
-                if (ROWS) {
-                    const uint32_t e = 8 * place_in_row();
-                    back = (e - min(e, ks - 8)) * 2;
-                } else {
-                    const uint32_t k = piece(q) * 4 + (lane >> 4);
-                    back = (k - min(k, ks - 1)) * stride;
-                }
-                load_to_lds(base[P == 1 ? 0 : q >> 1], offset[q] - back, lds + ((P == 1 ? 0 : q >> 1) * 8 + piece(q)) * 1024);
+            for (int q = 0; q < kPieces; ++q) {
+                const uint32_t k = ROWS ? 8 * place_in_row() : k_of(q);
+                back[q] = ROWS ? (k - min(k, ks - 8)) * 2 : (k - min(k, ks - 1)) * stride;
             }
-        }
 #pragma unroll
-        for (int p = 0; p < P; ++p) base[p] += advance;
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) load_to_lds(base[p], offset[q] - back[q], lds + p * (operand_bytes<W>() / P) + piece(q) * 1024);
+            base[p] += advance;
+        }
         ks -= step_of<P>();
     }
 };
 
 // What lane l supplies for rows r0 .. r0 + 31 and contraction indices 16 kk .. + 15 of a stage: row l % 32, the eight
 // indices from (l / 32) * 8 on.
-template <int P, bool ROWS>
+template <int P, int W, bool ROWS>
 __device__ __forceinline__ s16x8 fragment(const unsigned char* lds, int part, int r0, int kk)
 {
+    constexpr int R = rows_of<W>();
     const int lane = threadIdx.x & 63;
-    const unsigned char* base = lds + (P == 1 ? 0 : part * (kOperandBytes / 2));
+    const unsigned char* base = lds + part * (operand_bytes<W>() / P);
     if (ROWS) {
         const int row = r0 + (lane & 31), piece = kk * 2 + (lane >> 5);
         const int at = P == 1 ? row * 128 + ((piece ^ ((row >> 1) & 7)) << 4) : row * 64 + ((piece ^ ((row >> 2) & 3)) << 4);
@@ -161,10 +163,10 @@ __device__ __forceinline__ s16x8 fragment(const unsigned char* lds, int part, in
     // 16 lanes get 16 columns of 4 rows: lane i points to the i % 4-th 8 bytes of row i / 4 and receives column i
     const int i = lane & 15, g = lane >> 4;
     const int k = kk * 16 + (g >> 1) * 8 + (i >> 2), unit = (r0 >> 4) + (g & 1);
-    const int at = k * 256 + ((unit ^ ((i >> 2) << 1)) << 5) + ((i & 3) << 3);
+    const int at = k * (2 * R) + ((unit ^ ((i >> 2) << 1)) << 5) + ((i & 3) << 3);
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + at));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + at + 1024));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + at + 8 * R));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -175,25 +177,29 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// acc[im][in] += A B^T over one stage; a wavefront has rows 64 (wave / 2) .. and columns 64 (wave % 2) .. of the tile.
-template <int P, bool AROWS, bool BROWS>
-__device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&acc)[2][2])
+// Where a wavefront's share of a tile begins.
+template <int W> __device__ __forceinline__ int first_row() { return static_cast<int>(threadIdx.x >> 6) / (W / 2) * (rows_of<W>() / 2); }
+template <int W> __device__ __forceinline__ int first_col() { return static_cast<int>(threadIdx.x >> 6) % (W / 2) * 64; }
+
+// acc[im][in] += A B^T over one stage.
+template <int P, int W, bool AROWS, bool BROWS>
+__device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&acc)[W / 2][2])
 {
-    const int wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
+    constexpr int MT = W / 2, KK = step_of<P>() / 16;
+    const int m0 = first_row<W>(), n0 = first_col<W>();
     const unsigned char* A = stage;
-    const unsigned char* B = stage + kOperandBytes;
+    const unsigned char* B = stage + operand_bytes<W>();
     // Operands of the next 16 indices are read while these are multiplied: a read takes as long as four products.  (The compiler would
     // reuse the registers at once and wait for every read.)
-    constexpr int KK = step_of<P>() / 16;
-    s16x8 a[2][P][2], b[2][P][2];
+    s16x8 a[2][P][MT], b[2][P][2];
     auto read = [&](int kk) {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                a[kk & 1][p][i] = fragment<P, AROWS>(A, p, m0 + 32 * i, kk);
-                b[kk & 1][p][i] = fragment<P, BROWS>(B, p, n0 + 32 * i, kk);
-            }
+            for (int i = 0; i < MT; ++i) a[kk & 1][p][i] = fragment<P, W, AROWS>(A, p, m0 + 32 * i, kk);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) b[kk & 1][p][i] = fragment<P, W, BROWS>(B, p, n0 + 32 * i, kk);
+        }
     };
     read(0);
 #pragma unroll
@@ -202,7 +208,7 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
         __builtin_amdgcn_sched_barrier(0);
         const int at = kk & 1;
 #pragma unroll
-        for (int im = 0; im < 2; ++im)
+        for (int im = 0; im < MT; ++im)
 #pragma unroll
             for (int in = 0; in < 2; ++in) {
                 acc[im][in] = mfma<P>(a[at][0][im], b[at][0][in], acc[im][in]);
@@ -215,14 +221,29 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
     }
 }
 
-__device__ __forceinline__ void clear(f32x16 (&acc)[2][2])
+template <int MT>
+__device__ __forceinline__ void clear(f32x16 (&acc)[MT][2])
 {
 #pragma unroll
-    for (int im = 0; im < 2; ++im)
+    for (int im = 0; im < MT; ++im)
 #pragma unroll
         for (int in = 0; in < 2; ++in)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[im][in][i] = 0.0f;
+}
+
+// All stages of a workgroup, one travelling while the one before it is used: get(lds) fetches the next, use(stage) multiplies one.
+template <int W, class Get, class Use>
+__device__ __forceinline__ void run_stages(uint32_t stages, unsigned char* lds, Get get, Use use)
+{
+    const uint32_t lds0 = lds_address(lds);
+    if (stages) get(lds0);
+    stage_done();
+    for (uint32_t s = 0; s < stages; ++s) {
+        if (s + 1 < stages) get(lds0 + ((s + 1) & 1) * stage_bytes<W>());
+        use(lds + (s & 1) * stage_bytes<W>());
+        stage_done();
+    }
 }
 
 // Workgroups go to the eight XCDs in turn, and each XCD has an L2 of its own: this numbers them so that an XCD's have
@@ -429,47 +450,46 @@ __device__ __forceinline__ float score_factor(const int32_t* shift)
 
 // Scores of tiles tile0 .. tile1 - 1 of the table's rows against one tile of H's, epilogue(row0, acc) for each; the next tile's first
 // stage travels meanwhile.
-template <int P, class Epilogue>
-__device__ __forceinline__ void score_tiles(const Operand& w, const Operand& h, uint32_t token_tile, uint32_t first_row, uint32_t tile0, uint32_t tile1, int steps,
-                                            unsigned char (*lds)[kStageBytes], Epilogue epilogue)
+template <int P, int W, class Epilogue>
+__device__ __forceinline__ void score_tiles(const Operand& w, const Operand& h, uint32_t token_tile, uint32_t first, uint32_t tile0, uint32_t tile1, int steps,
+                                            unsigned char* lds, Epilogue epilogue)
 {
-    f32x16 acc[2][2];
+    constexpr int R = rows_of<W>();
+    f32x16 acc[W / 2][2];
     clear(acc);
-    const uint32_t stages = tile1 > tile0 ? (tile1 - tile0) * steps : 0;
-    Loader<P, true> load_w, load_h;
-    uint32_t row0 = first_row + tile0 * kTile, next_row0 = row0;
+    Loader<P, W, true> load_w, load_h;
+    uint32_t row0 = first + tile0 * R, next_row0 = row0;
     int step = 0, next_step = 0;
-    const uint32_t lds0 = lds_address(lds[0]);
-    auto get = [&](uint32_t s) {
-        if (next_step == 0) {
-            load_w.start(w, next_row0, 0);
-            load_h.start(h, token_tile * kTile, 0);
-        }
-        load_w.fetch(lds0 + (s & 1) * kStageBytes);
-        load_h.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
-        if (++next_step == steps) { next_step = 0; next_row0 += kTile; }
-    };
-    if (stages) get(0);
-    stage_done();
-    for (uint32_t s = 0; s < stages; ++s) {
-        if (s + 1 < stages) get(s + 1);
-        multiply<P, true, true>(lds[s & 1], acc);
-        if (step == steps - 1) {
-            epilogue(row0, acc);
-            clear(acc);
-        }
-        stage_done();
-        if (++step == steps) { step = 0; row0 += kTile; }
-    }
+    run_stages<W>(
+        tile1 > tile0 ? (tile1 - tile0) * steps : 0, lds,
+        [&](uint32_t to) {
+            if (next_step == 0) {
+                load_w.start(w, next_row0, 0);
+                load_h.start(h, token_tile * R, 0);
+            }
+            load_w.fetch(to);
+            load_h.fetch(to + operand_bytes<W>());
+            if (++next_step == steps) { next_step = 0; next_row0 += R; }
+        },
+        [&](const unsigned char* stage) {
+            multiply<P, W, true, true>(stage, acc);
+            if (++step == steps) {
+                epilogue(row0, acc);
+                clear(acc);
+                step = 0;
+                row0 += R;
+            }
+        });
 }
 
-template <int P>
-__global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
+template <int P, int W>
+__global__ void __launch_bounds__(64 * W, 2) scores_kernel(ScoreArgs a)
 {
-    __shared__ __align__(16) unsigned char lds[2][kStageBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
+    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
+    constexpr int R = rows_of<W>(), MT = W / 2;
+    const int lane = threadIdx.x & 63, m0 = first_row<W>(), n0 = first_col<W>();
     uint32_t token_tile, split;
-    pair_of(by_xcd(blockIdx.x, gridDim.x), a.tokens / kTile, a.splits, token_tile, split);
+    pair_of(by_xcd(blockIdx.x, gridDim.x), (a.tokens + R - 1) / R, a.splits, token_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const float factor = score_factor<P>(a.shift), to_log2 = kLog2e * factor;
     float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
@@ -477,37 +497,37 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
     int64_t token[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        token[j] = static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31);
+        token[j] = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
         target[j] = token[j] < a.n ? static_cast<uint32_t>(a.targets[token[j]]) : 0xFFFFFFFFu;
     }
-    score_tiles<P>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+    score_tiles<P, W>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0;
-        if (row0 + 64 > a.num_rows) {
+        if (row0 + 32 * MT > a.num_rows) {
 #pragma unroll
-            for (int im = 0; im < 2; ++im)
+            for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (row0 + 32 * im + sum_row(i) >= a.num_rows) acc[im][0][i] = acc[im][1][i] = -INFINITY;
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if (__any(target[j] - row0 < 64)) {
+            if (__any(target[j] - row0 < 32 * MT)) {
 #pragma unroll
-                for (int im = 0; im < 2; ++im)
+                for (int im = 0; im < MT; ++im)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (target[j] == row0 + 32 * im + sum_row(i) && target[j] < a.num_rows) a.target_score[token[j]] = acc[im][j][i] * factor;
             }
             float t = acc[0][j][0];
 #pragma unroll
-            for (int im = 0; im < 2; ++im)
+            for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) t = fmaxf(t, acc[im][j][i]);
             const float now = fmaxf(top[j], t * to_log2);
             const float by = now == -INFINITY ? 0.0f : now;         // (nothing seen yet but scores of minus infinity)
             float part = 0.0f;
 #pragma unroll
-            for (int im = 0; im < 2; ++im)
+            for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by));
             sum[j] = fmaf(sum[j], __builtin_amdgcn_exp2f(top[j] - by), part);
@@ -515,17 +535,18 @@ __global__ void __launch_bounds__(kThreads, 2) scores_kernel(ScoreArgs a)
         }
     });
     // lanes l and l + 32 and the two wavefronts of a column have the same rows of H
-    float2* join = reinterpret_cast<float2*>(lds[0]);
+    float2* join = reinterpret_cast<float2*>(lds);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         join_stat(top[j], sum[j], make_float2(__shfl_xor(top[j], 32, 64), __shfl_xor(sum[j], 32, 64)));
-        if (lane < 32) join[(wave >> 1) * kTile + n0 + 32 * j + lane] = make_float2(top[j], sum[j]);
+        if (lane < 32) join[(m0 ? R : 0) + n0 + 32 * j + lane] = make_float2(top[j], sum[j]);
     }
     __syncthreads();
-    if (threadIdx.x < kTile) {
+    const uint32_t row = token_tile * R + threadIdx.x;
+    if (threadIdx.x < R && row < a.tokens) {
         float2 p = join[threadIdx.x];
-        join_stat(p.x, p.y, join[kTile + threadIdx.x]);
-        a.stat[(static_cast<int64_t>(token_tile) * kTile + threadIdx.x) * a.splits + split] = p;
+        join_stat(p.x, p.y, join[R + threadIdx.x]);
+        a.stat[static_cast<int64_t>(row) * a.splits + split] = p;
     }
 }
 
@@ -712,37 +733,39 @@ __device__ __forceinline__ u32x4 eight_of(u32x2 a, u32x2 b)
     return u32x4{x[0], y[0], x[1], y[1]};
 }
 
-template <int P>
-__global__ void __launch_bounds__(kThreads, 2) coef_kernel(CoefArgs a)
+template <int P, int W>
+__global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 {
-    __shared__ __align__(16) unsigned char lds[2][kStageBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m0 = (wave >> 1) * 64, n0 = (wave & 1) * 64;
+    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
+    constexpr int R = rows_of<W>(), MT = W / 2;
+    const int lane = threadIdx.x & 63, m0 = first_row<W>(), n0 = first_col<W>();
     uint32_t token_tile, split;
-    pair_of(by_xcd(blockIdx.x, gridDim.x), a.tokens / kTile, a.splits, token_tile, split);
+    pair_of(by_xcd(blockIdx.x, gridDim.x), (a.tokens + R - 1) / R, a.splits, token_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const float to_log2 = kLog2e * score_factor<P>(a.shift);
     uint32_t target[2];
     float by[2], c[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int64_t token = static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31);
+        const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
         target[j] = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
         if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
         const bool counts = target[j] != 0xFFFFFFFFu;
         by[j] = counts ? a.lse[token] * kLog2e : 0.0f;
         c[j] = P == 2 ? 0x1p14f : counts && a.c ? a.c[token] : 1.0f;
     }
-    score_tiles<P>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+    score_tiles<P, W>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0;
-        const bool ends = row0 + 64 > a.num_rows;
+        const bool ends = row0 + 32 * MT > a.num_rows;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const bool here = __any(target[j] - row0 < 64);
+            const bool here = __any(target[j] - row0 < 32 * MT);
             const bool counts = target[j] != 0xFFFFFFFFu;
             uint16_t* const* g = a.g;
-            const int64_t to = (static_cast<int64_t>(token_tile) * kTile + n0 + 32 * j + (lane & 31)) * a.g_stride + (row0 - a.row_base) + 8 * (lane >> 5);
+            if (token_tile * R + n0 + 32 * j >= a.tokens) continue;     // (tokens: a multiple of 32)
+            const int64_t to = (static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31)) * a.g_stride + (row0 - a.row_base) + 8 * (lane >> 5);
 #pragma unroll
-            for (int im = 0; im < 2; ++im)
+            for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int q = 0; q < 4; q += 2) {
                     s16x4 hi[2], lo[2];
@@ -791,28 +814,23 @@ struct ProductArgs {
 };
 
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
-template <int P, bool GROWS>
+template <int P, int W, bool GROWS>
 __device__ __forceinline__ void product_tile(const Operand& cols, const Operand& g, uint32_t col0, uint32_t row0, uint32_t s0, uint32_t s1,
-                                             unsigned char (*lds)[kStageBytes], f32x16 (&acc)[2][2])
+                                             unsigned char* lds, f32x16 (&acc)[W / 2][2])
 {
     clear(acc);
     if (s0 >= s1) return;
-    Loader<P, false> load_c;
-    Loader<P, GROWS> load_g;
+    Loader<P, W, false> load_c;
+    Loader<P, W, GROWS> load_g;
     load_c.start(cols, col0, s0);
     load_g.start(g, row0, s0);
-    const uint32_t lds0 = lds_address(lds[0]);
-    auto get = [&](uint32_t s) {
-        load_c.fetch(lds0 + (s & 1) * kStageBytes);
-        load_g.fetch(lds0 + (s & 1) * kStageBytes + kOperandBytes);
-    };
-    get(0);
-    stage_done();
-    for (uint32_t s = 0; s < s1 - s0; ++s) {
-        if (s + 1 < s1 - s0) get(s + 1);
-        multiply<P, false, GROWS>(lds[s & 1], acc);
-        stage_done();
-    }
+    run_stages<W>(
+        s1 - s0, lds,
+        [&](uint32_t to) {
+            load_c.fetch(to);
+            load_g.fetch(to + operand_bytes<W>());
+        },
+        [&](const unsigned char* stage) { multiply<P, W, false, GROWS>(stage, acc); });
 }
 
 // Writes up to V values, the first `have` of them.
@@ -828,11 +846,11 @@ __device__ __forceinline__ void store_some(T* to, int have, const float (&x)[V])
     }
 }
 
-template <int P>
-__global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
+template <int P, int W>
+__global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
 {
-    __shared__ __align__(16) unsigned char lds[2][kStageBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
+    const int lane = threadIdx.x & 63;
     const uint32_t h_blocks = a.h_tiles * a.col_tiles * a.h_splits;
     // (dH's workgroups first, then dW's: a CU that has two has one of either, which differ in how long they take)
     uint32_t b = blockIdx.x;
@@ -841,10 +859,11 @@ __global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
     const uint32_t splits = dh ? a.h_splits : a.w_splits, share = dh ? a.h_share : a.w_share, stages = dh ? a.h_stages : a.w_stages;
     const uint32_t col = b % a.col_tiles, split = b / a.col_tiles % splits, tile = b / a.col_tiles / splits;
     const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
-    f32x16 acc[2][2];
-    if (dh) product_tile<P, true>(a.w, a.g_rows, col * kTile, tile * kTile, s0, s1, lds, acc);
-    else product_tile<P, false>(a.h, a.g_cols, col * kTile, tile * kTile, s0, s1, lds, acc);
-    const uint32_t row0 = tile * kTile + (wave & 1) * 64 + (lane & 31), col0 = col * kTile + (wave >> 1) * 64 + 4 * (lane >> 5);
+    constexpr int R = rows_of<W>(), MT = W / 2;
+    f32x16 acc[MT][2];
+    if (dh) product_tile<P, W, true>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
+    else product_tile<P, W, false>(a.h, a.g_cols, col * R, tile * R, s0, s1, lds, acc);
+    const uint32_t row0 = tile * R + first_col<W>() + (lane & 31), col0 = col * R + first_row<W>() + 4 * (lane >> 5);
     if (!dh && !a.dw) {
         const int k = P == 2 ? -(*a.shift + kGShift) : 0;
         typedef typename std::conditional<P == 2, float, bf16_t>::type T;
@@ -853,7 +872,7 @@ __global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
             if (row0 + 32 * j >= a.rows) continue;
             T* to = static_cast<T*>(a.out) + static_cast<int64_t>(row0 + 32 * j) * a.out_stride + col0;
 #pragma unroll
-            for (int im = 0; im < 2; ++im)
+            for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float x[4];
@@ -868,11 +887,13 @@ __global__ void __launch_bounds__(kThreads, 2) products_kernel(ProductArgs a)
     const bool add = dh && a.add;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+        if (row0 + 32 * j >= (dh ? a.tokens : a.piece_rows)) continue;
         float* to = out + static_cast<int64_t>(row0 + 32 * j) * a.cols + col0;
 #pragma unroll
-        for (int im = 0; im < 2; ++im)
+        for (int im = 0; im < MT; ++im)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
+                if (col0 + 32 * im + 8 * q >= a.cols) continue;
                 float4 x = make_float4(acc[im][j][4 * q], acc[im][j][4 * q + 1], acc[im][j][4 * q + 2], acc[im][j][4 * q + 3]);
                 float4* at = reinterpret_cast<float4*>(to + 32 * im + 8 * q);
                 if (add) {
@@ -967,6 +988,7 @@ struct XentWs {
     uint32_t row_tiles, splits;        // of the scores, or of a piece's coefficients
     int32_t few_blocks;                // > 0: few rows of H, so many blocks of 16
     int64_t piece;                     // table rows of a piece
+    bool large_scores, large_products; // tiles of 256 x 256
     uint32_t h_splits, w_splits, h_share, w_share, h_stages, w_stages;
     float* amax;
     int32_t* shift;                    // of W, H, c H
@@ -984,11 +1006,15 @@ bool xent_sizes_ok(int64_t n, int64_t num_rows, int32_t dim, int32_t type)
 }
 
 // Workgroups over table tiles for one tile of H: as many as fill the machine, all with about as many tiles.
-uint32_t splits_of(int64_t row_tiles, int64_t token_tiles)
+uint32_t splits_of(int64_t row_tiles, int64_t token_tiles, bool large)
 {
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(row_tiles, kSlots / std::min<int64_t>(token_tiles, kSlots)));
+    const int64_t slots = slots_of(large), most = std::max<int64_t>(1, std::min<int64_t>(row_tiles, slots / std::min<int64_t>(token_tiles, slots)));
     return static_cast<uint32_t>(ceil_div(row_tiles, ceil_div(row_tiles, most)));
 }
+
+// Large tiles where there are enough of them to fill the machine several times over.
+bool large_scores(int64_t n, int64_t num_rows, int parts) { return parts == 1 && ceil_div(n, 256) * ceil_div(num_rows, 256) >= 1024; }
+bool large_products(int64_t tokens, int64_t piece, int32_t dim, int parts) { return parts == 1 && dim >= 256 && tokens >= 2048 && piece >= 2048; }
 
 // The workspace has room for packed copies whether or not this call's alignment needs them.
 XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad, char* base)
@@ -998,8 +1024,9 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     w.padded = static_cast<int32_t>(round_up(dim, w.parts == 1 ? step_of<1>() : step_of<2>()));
     w.cols = static_cast<int32_t>(round_up(dim, kTile));
     w.tokens = round_up(n, kTile);
-    w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, kTile));
-    const int64_t token_tiles = w.tokens / kTile;
+    w.large_scores = large_scores(n, num_rows, w.parts);
+    const int64_t side = w.large_scores ? 256 : 128, token_tiles = ceil_div(w.tokens, side);
+    w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     Carver take{base};
     // H as second operands of the few-rows kernel has to leave room in LDS for a second workgroup
     const int64_t few_bytes = (n <= 16 ? 1 : n <= 32 ? 2 : 4) * ceil_div(dim, 32) * (type == NE_F32 ? 3 : 1) * 1024;
@@ -1018,19 +1045,21 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
         w.w[p] = take.get<uint16_t>(static_cast<size_t>(num_rows) * w.padded);
     }
     if (!grad) {
-        w.splits = splits_of(w.row_tiles, token_tiles);
+        w.splits = splits_of(w.row_tiles, token_tiles, w.large_scores);
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * w.tokens);
         w.target_score = take.get<float>(static_cast<size_t>(w.tokens));
     } else {
         const int64_t step = w.parts == 1 ? step_of<1>() : step_of<2>();
-        const int64_t most = std::max<int64_t>(kTile, static_cast<int64_t>(kGBytes / (2 * w.parts)) / w.tokens / kTile * kTile);
+        const int64_t most = std::max<int64_t>(256, static_cast<int64_t>(kGBytes / (2 * w.parts)) / w.tokens / 256 * 256);
         const int64_t pieces = ceil_div(num_rows, most);
-        w.piece = round_up(ceil_div(num_rows, pieces), kTile);
+        w.piece = round_up(ceil_div(num_rows, pieces), 256);
         // contractions are split so that all workgroups of a launch have about as many stages, and the machine is full
-        const int64_t cols = w.cols / kTile, h_tiles = token_tiles * cols, w_tiles = w.piece / kTile * cols;
+        w.large_products = large_products(w.tokens, w.piece, dim, w.parts);
+        const int64_t edge = w.large_products ? 256 : 128;
+        const int64_t cols = ceil_div(dim, edge), h_tiles = ceil_div(w.tokens, edge) * cols, w_tiles = ceil_div(w.piece, edge) * cols;
         w.h_stages = static_cast<uint32_t>(w.piece / step);
         w.w_stages = static_cast<uint32_t>(w.tokens / step);
-        const int64_t share = std::max<int64_t>(16, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, kSlots));
+        const int64_t share = std::max<int64_t>(16, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, slots_of(w.large_products)));
         w.h_splits = static_cast<uint32_t>(ceil_div(w.h_stages, share));
         w.w_splits = static_cast<uint32_t>(ceil_div(w.w_stages, share));
         w.h_share = static_cast<uint32_t>(ceil_div(w.h_stages, w.h_splits));
@@ -1132,7 +1161,8 @@ hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse,
     if (e != hipSuccess) return e;
     a.targets = x.targets; a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles;
     a.splits = w.splits; a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.target_score = w.target_score;
-    hipLaunchKernelGGL(scores_kernel<P>, dim3(static_cast<unsigned>(w.tokens / kTile * w.splits)), dim3(kThreads), 0, st, a);
+    if (w.large_scores) hipLaunchKernelGGL((scores_kernel<P, 8>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 256) * w.splits)), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((scores_kernel<P, 4>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 128) * w.splits)), dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     return join_losses(x, w, loss, lse, st);
@@ -1148,9 +1178,10 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     const Operand all = ca.w;
     ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.c = x.c; ca.g_stride = w.piece;
     ca.num_rows = static_cast<uint32_t>(x.num_rows); ca.steps = w.padded / step_of<P>();
-    const uint32_t token_tiles = static_cast<uint32_t>(w.tokens / kTile);
+    const int64_t side = w.large_scores ? 256 : 128, edge = w.large_products ? 256 : 128;
+    const uint32_t token_tiles = static_cast<uint32_t>(ceil_div(w.tokens, side));
     pa.dh = w.dh; pa.dw = w.dw; pa.tokens = static_cast<uint32_t>(w.tokens); pa.piece_rows = static_cast<uint32_t>(w.piece);
-    pa.cols = static_cast<uint32_t>(w.cols); pa.col_tiles = pa.cols / kTile;
+    pa.cols = static_cast<uint32_t>(w.cols); pa.col_tiles = static_cast<uint32_t>(ceil_div(x.dim, edge));
     pa.h_splits = w.h_splits; pa.w_splits = w.w_splits; pa.h_share = w.h_share; pa.w_share = w.w_share;
     pa.w_stages = w.w_stages;
     pa.out_stride = dw_stride; pa.dim = x.dim; pa.scale = scale; pa.shift = w.shift + (x.c ? 2 : 1);
@@ -1164,11 +1195,12 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     for (int64_t base = 0; base < x.num_rows; base += w.piece) {
         const int64_t rows = std::min<int64_t>(w.piece, x.num_rows - base);
         ca.row_base = static_cast<uint32_t>(base);
-        ca.row_tiles = static_cast<uint32_t>(ceil_div(rows, kTile));
-        ca.splits = splits_of(ca.row_tiles, token_tiles);
+        ca.row_tiles = static_cast<uint32_t>(ceil_div(rows, side));
+        ca.splits = splits_of(ca.row_tiles, token_tiles, w.large_scores);
         ca.tokens = static_cast<uint32_t>(w.tokens);
         for (int p = 0; p < P; ++p) ca.g[p] = w.g[p];
-        hipLaunchKernelGGL(coef_kernel<P>, dim3(token_tiles * ca.splits), dim3(kThreads), 0, st, ca);
+        if (w.large_scores) hipLaunchKernelGGL((coef_kernel<P, 8>), dim3(token_tiles * ca.splits), dim3(512), 0, st, ca);
+        else hipLaunchKernelGGL((coef_kernel<P, 4>), dim3(token_tiles * ca.splits), dim3(256), 0, st, ca);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         pa.g_rows = Operand{{w.g[0], w.g[1]}, w.piece, static_cast<uint32_t>(w.tokens - 1), static_cast<uint32_t>(w.piece)};
@@ -1176,15 +1208,16 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         pa.w = all;
         for (int p = 0; p < P; ++p) pa.w.part[p] = all.part[p] + base * all.stride;
         pa.w.last = static_cast<uint32_t>(rows - 1);
-        pa.h_tiles = dh ? token_tiles : 0;
-        pa.w_tiles = dw ? ca.row_tiles : 0;
+        pa.h_tiles = dh ? static_cast<uint32_t>(ceil_div(w.tokens, edge)) : 0;
+        pa.w_tiles = dw ? static_cast<uint32_t>(ceil_div(rows, edge)) : 0;
         pa.h_stages = static_cast<uint32_t>(ceil_div(rows, step_of<P>()));      // (no stage begins beyond the last row)
         pa.add = base > 0;
         pa.rows = static_cast<uint32_t>(rows);
         pa.out = dw ? static_cast<T*>(dw) + base * dw_stride : nullptr;
         const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
         if (!blocks) continue;
-        hipLaunchKernelGGL(products_kernel<P>, dim3(blocks), dim3(kThreads), 0, st, pa);
+        if (w.large_products) hipLaunchKernelGGL((products_kernel<P, 8>), dim3(blocks), dim3(512), 0, st, pa);
+        else hipLaunchKernelGGL((products_kernel<P, 4>), dim3(blocks), dim3(256), 0, st, pa);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (dw && w.dw) {
