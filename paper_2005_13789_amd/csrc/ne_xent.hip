@@ -32,14 +32,16 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kTile = 128;             // rows of H and columns of the gradients are padded to multiples of this
 constexpr int kAmaxBlocks = 1024;
 constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
 constexpr int kFewBytes = 65536;
 constexpr int kFewGroups = 1024;
-constexpr size_t kGBytes = size_t{128} << 20;      // G of one piece
+constexpr size_t kGBytes = size_t{128} << 20, kGBytesAtOnce = size_t{192} << 20;      // G of one piece; of all, where there is only one
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
 
@@ -262,8 +264,9 @@ __device__ __forceinline__ void pair_of(uint32_t b, uint32_t tiles_a, uint32_t t
     ta = group * 8 + rest - tb * size;
 }
 
-// Row (of 32) of a lane's i-th sum.
-__device__ __forceinline__ int sum_row(int i) { return (i & 3) + 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5); }
+// Row (of 32) of a lane's i-th sum, without the lane's own share of it.
+constexpr int sum_row(int i) { return (i & 3) + 8 * (i >> 2); }
+__device__ __forceinline__ uint32_t lane_row() { return 4 * ((threadIdx.x & 63) >> 5); }
 
 // ---------------------------------------------------------------------------------------------
 // packing
@@ -499,15 +502,17 @@ __global__ void __launch_bounds__(64 * W, 2) scores_kernel(ScoreArgs a)
     for (int j = 0; j < 2; ++j) {
         token[j] = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
         target[j] = token[j] < a.n ? static_cast<uint32_t>(a.targets[token[j]]) : 0xFFFFFFFFu;
+        if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
     }
     score_tiles<P, W>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
-        const uint32_t row0 = tile_row0 + m0;
+        const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
         if (row0 + 32 * MT > a.num_rows) {
+            const int left = static_cast<int>(a.num_rows) - static_cast<int>(lane_row0);
 #pragma unroll
             for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (row0 + 32 * im + sum_row(i) >= a.num_rows) acc[im][0][i] = acc[im][1][i] = -INFINITY;
+                    if (32 * im + sum_row(i) >= left) acc[im][0][i] = acc[im][1][i] = -INFINITY;
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -516,7 +521,7 @@ __global__ void __launch_bounds__(64 * W, 2) scores_kernel(ScoreArgs a)
                 for (int im = 0; im < MT; ++im)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (target[j] == row0 + 32 * im + sum_row(i) && target[j] < a.num_rows) a.target_score[token[j]] = acc[im][j][i] * factor;
+                        if (target[j] - lane_row0 == 32 * im + sum_row(i)) a.target_score[token[j]] = acc[im][j][i] * factor;
             }
             float t = acc[0][j][0];
 #pragma unroll
@@ -615,7 +620,6 @@ template <class T, int BLOCKS>
 __global__ void __launch_bounds__(kThreads) few_rows_kernel(FewArgs a)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, AHEAD = sizeof(T) == 4 ? 4 : 8;
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
     extern __shared__ __align__(16) unsigned char few_lds[];       // [blocks][steps][parts][64 lanes] 16 bytes
     bf16x8* hs = reinterpret_cast<bf16x8*>(few_lds);
     __shared__ float2 join[kThreads / 64][BLOCKS * 16];
@@ -750,43 +754,60 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
         const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
         target[j] = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
         if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
+        // (a row without a target: 2 to the minus infinity; halves: G 2^14)
         const bool counts = target[j] != 0xFFFFFFFFu;
-        by[j] = counts ? a.lse[token] * kLog2e : 0.0f;
-        c[j] = P == 2 ? 0x1p14f : counts && a.c ? a.c[token] : 1.0f;
+        by[j] = counts ? fmaf(a.lse[token], kLog2e, P == 2 ? -static_cast<float>(kGShift) : 0.0f) : INFINITY;
+        c[j] = P == 1 && a.c && counts ? a.c[token] : 1.0f;
     }
     score_tiles<P, W>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
-        const uint32_t row0 = tile_row0 + m0;
-        const bool ends = row0 + 32 * MT > a.num_rows;
+        const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const bool here = __any(target[j] - row0 < 32 * MT);
-            const bool counts = target[j] != 0xFFFFFFFFu;
-            uint16_t* const* g = a.g;
             if (token_tile * R + n0 + 32 * j >= a.tokens) continue;     // (tokens: a multiple of 32)
+#pragma unroll
+            for (int im = 0; im < MT; ++im)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[im][j][i] = __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by[j]));
+            if (__any(target[j] - row0 < 32 * MT)) {
+#pragma unroll
+                for (int im = 0; im < MT; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (target[j] - lane_row0 == 32 * im + sum_row(i)) acc[im][j][i] -= P == 2 ? 0x1p14f : 1.0f;
+            }
+            if (row0 + 32 * MT > a.num_rows) {
+                const int left = static_cast<int>(a.num_rows) - static_cast<int>(lane_row0);
+#pragma unroll
+                for (int im = 0; im < MT; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * im + sum_row(i) >= left) acc[im][j][i] = 0.0f;
+            }
+            if (P == 1 && a.c) {
+#pragma unroll
+                for (int im = 0; im < MT; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[im][j][i] *= c[j];
+            }
             const int64_t to = (static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31)) * a.g_stride + (row0 - a.row_base) + 8 * (lane >> 5);
 #pragma unroll
             for (int im = 0; im < MT; ++im)
 #pragma unroll
                 for (int q = 0; q < 4; q += 2) {
-                    s16x4 hi[2], lo[2];
+                    u32x2 hi[2], lo[2];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int i = 4 * (q + r) + e;
-                            float x = __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by[j]));
-                            if (here && row0 + 32 * im + sum_row(i) == target[j]) x -= 1.0f;
-                            x = counts && !(ends && row0 + 32 * im + sum_row(i) >= a.num_rows) ? x * c[j] : 0.0f;
-                            if (P == 1) {
-                                hi[r][e] = __builtin_bit_cast(short, static_cast<bf16_t>(x));
-                            } else {
-                                const f16_t xh = static_cast<f16_t>(x);
-                                hi[r][e] = __builtin_bit_cast(short, xh);
-                                lo[r][e] = __builtin_bit_cast(short, static_cast<f16_t>(x - static_cast<float>(xh)));
-                            }
+                    for (int r = 0; r < 2; ++r) {
+                        const f32x4 x = {acc[im][j][4 * (q + r)], acc[im][j][4 * (q + r) + 1], acc[im][j][4 * (q + r) + 2], acc[im][j][4 * (q + r) + 3]};
+                        if constexpr (P == 1) {
+                            hi[r] = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
+                        } else {
+                            const f16x4 xh = __builtin_convertvector(x, f16x4);
+                            hi[r] = __builtin_bit_cast(u32x2, xh);
+                            lo[r] = __builtin_bit_cast(u32x2, __builtin_convertvector(x - __builtin_convertvector(xh, f32x4), f16x4));
                         }
-                    *reinterpret_cast<u32x4*>(g[0] + to + 32 * im + 8 * q) = eight_of(__builtin_bit_cast(u32x2, hi[0]), __builtin_bit_cast(u32x2, hi[1]));
-                    if (P == 2) *reinterpret_cast<u32x4*>(g[P - 1] + to + 32 * im + 8 * q) = eight_of(__builtin_bit_cast(u32x2, lo[0]), __builtin_bit_cast(u32x2, lo[1]));
+                    }
+                    *reinterpret_cast<u32x4*>(a.g[0] + to + 32 * im + 8 * q) = eight_of(hi[0], hi[1]);
+                    if constexpr (P == 2) *reinterpret_cast<u32x4*>(a.g[1] + to + 32 * im + 8 * q) = eight_of(lo[0], lo[1]);
                 }
         }
     });
@@ -802,7 +823,7 @@ struct ProductArgs {
     float* dw;                     // [w_splits][piece rows][cols], or NULL: one split, whose sums are dW
     void* out;                     // dW of the piece
     int64_t out_stride;
-    uint32_t tokens, piece_rows, cols;      // multiples of 128
+    uint32_t tokens, piece_rows, cols;      // multiples of 32 or 64, of 256, of 32
     uint32_t h_tiles, w_tiles, col_tiles;   // tiles over tokens, piece rows, columns
     uint32_t h_splits, w_splits, h_share, w_share;      // splits of the contraction, stages of each
     uint32_t h_stages, w_stages;
@@ -1012,9 +1033,13 @@ uint32_t splits_of(int64_t row_tiles, int64_t token_tiles, bool large)
     return static_cast<uint32_t>(ceil_div(row_tiles, ceil_div(row_tiles, most)));
 }
 
-// Large tiles where there are enough of them to fill the machine several times over.
-bool large_scores(int64_t n, int64_t num_rows, int parts) { return parts == 1 && ceil_div(n, 256) * ceil_div(num_rows, 256) >= 1024; }
-bool large_products(int64_t tokens, int64_t piece, int32_t dim, int parts) { return parts == 1 && dim >= 256 && tokens >= 2048 && piece >= 2048; }
+// Large tiles of scores: where a tile's products take longer than its exponentials, which nothing else runs beside there, and where there are
+// enough of them to fill the machine several times over (bf16, 2048 rows against 100 000 of 512: 218 us, 231 with small tiles; of 256: 122 and
+// 117).  Halves take three products per fetch, which small tiles keep up with (4096 x 50 000 x 512: 657 us, large tiles 674).
+bool large_scores(int64_t n, int64_t num_rows, int32_t dim, int parts)
+{
+    return parts == 1 && dim >= 384 && ceil_div(n, 256) * ceil_div(num_rows, 256) >= 1024;
+}
 
 // The workspace has room for packed copies whether or not this call's alignment needs them.
 XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad, char* base)
@@ -1022,9 +1047,10 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     XentWs w{};
     w.parts = type == NE_F32 ? 2 : 1;
     w.padded = static_cast<int32_t>(round_up(dim, w.parts == 1 ? step_of<1>() : step_of<2>()));
-    w.cols = static_cast<int32_t>(round_up(dim, kTile));
-    w.tokens = round_up(n, kTile);
-    w.large_scores = large_scores(n, num_rows, w.parts);
+    w.cols = static_cast<int32_t>(round_up(dim, 32));
+    const int64_t step = w.parts == 1 ? step_of<1>() : step_of<2>();
+    w.tokens = round_up(n, step);
+    w.large_scores = large_scores(n, num_rows, dim, w.parts);
     const int64_t side = w.large_scores ? 256 : 128, token_tiles = ceil_div(w.tokens, side);
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     Carver take{base};
@@ -1049,21 +1075,27 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * w.tokens);
         w.target_score = take.get<float>(static_cast<size_t>(w.tokens));
     } else {
-        const int64_t step = w.parts == 1 ? step_of<1>() : step_of<2>();
-        const int64_t most = std::max<int64_t>(256, static_cast<int64_t>(kGBytes / (2 * w.parts)) / w.tokens / 256 * 256);
-        const int64_t pieces = ceil_div(num_rows, most);
+        const int64_t row_bytes = 2 * w.parts * w.tokens;       // G of one row of the table
+        const int64_t most = std::max<int64_t>(256, static_cast<int64_t>(kGBytes) / row_bytes / 256 * 256);
+        const int64_t pieces = round_up(num_rows, 256) * row_bytes <= static_cast<int64_t>(kGBytesAtOnce) ? 1 : ceil_div(num_rows, most);
         w.piece = round_up(ceil_div(num_rows, pieces), 256);
         // contractions are split so that all workgroups of a launch have about as many stages, and the machine is full
-        w.large_products = large_products(w.tokens, w.piece, dim, w.parts);
-        const int64_t edge = w.large_products ? 256 : 128;
-        const int64_t cols = ceil_div(dim, edge), h_tiles = ceil_div(w.tokens, edge) * cols, w_tiles = ceil_div(w.piece, edge) * cols;
-        w.h_stages = static_cast<uint32_t>(w.piece / step);
-        w.w_stages = static_cast<uint32_t>(w.tokens / step);
-        const int64_t share = std::max<int64_t>(16, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, slots_of(w.large_products)));
-        w.h_splits = static_cast<uint32_t>(ceil_div(w.h_stages, share));
-        w.w_splits = static_cast<uint32_t>(ceil_div(w.w_stages, share));
-        w.h_share = static_cast<uint32_t>(ceil_div(w.h_stages, w.h_splits));
-        w.w_share = static_cast<uint32_t>(ceil_div(w.w_stages, w.w_splits));
+        auto split = [&](bool large) {
+            const int64_t edge = large ? 256 : 128;
+            const int64_t cols = ceil_div(dim, edge), h_tiles = ceil_div(w.tokens, edge) * cols, w_tiles = ceil_div(w.piece, edge) * cols;
+            w.large_products = large;
+            w.h_stages = static_cast<uint32_t>(w.piece / step);
+            w.w_stages = static_cast<uint32_t>(w.tokens / step);
+            const int64_t share = std::max<int64_t>(16, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, slots_of(large)));
+            w.h_splits = static_cast<uint32_t>(ceil_div(w.h_stages, share));
+            w.w_splits = static_cast<uint32_t>(ceil_div(w.w_stages, share));
+            w.h_share = static_cast<uint32_t>(ceil_div(w.h_stages, w.h_splits));
+            w.w_share = static_cast<uint32_t>(ceil_div(w.w_stages, w.w_splits));
+        };
+        // Large tiles of products (bf16, of more than 128 columns): where dW needs no partial sums with them, or has columns enough that these are
+        // worth it (2048 x 100 000 x 512: 778 us, 906 with small tiles; 4096 x 100 000 x 256, two partial sums: 1056 and 971).
+        split(w.parts == 1 && dim > 128);
+        if (w.large_products && w.w_splits > 1 && dim < 384) split(false);
         for (int p = 0; p < w.parts; ++p) {
             w.hc[p] = w.parts == 2 ? take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded) : nullptr;
             w.g[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.piece);
@@ -1161,7 +1193,7 @@ hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse,
     if (e != hipSuccess) return e;
     a.targets = x.targets; a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles;
     a.splits = w.splits; a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.target_score = w.target_score;
-    if (w.large_scores) hipLaunchKernelGGL((scores_kernel<P, 8>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 256) * w.splits)), dim3(512), 0, st, a);
+    if (P == 1 && w.large_scores) hipLaunchKernelGGL((scores_kernel<1, 8>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 256) * w.splits)), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((scores_kernel<P, 4>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 128) * w.splits)), dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -1199,7 +1231,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         ca.splits = splits_of(ca.row_tiles, token_tiles, w.large_scores);
         ca.tokens = static_cast<uint32_t>(w.tokens);
         for (int p = 0; p < P; ++p) ca.g[p] = w.g[p];
-        if (w.large_scores) hipLaunchKernelGGL((coef_kernel<P, 8>), dim3(token_tiles * ca.splits), dim3(512), 0, st, ca);
+        if (P == 1 && w.large_scores) hipLaunchKernelGGL((coef_kernel<1, 8>), dim3(token_tiles * ca.splits), dim3(512), 0, st, ca);
         else hipLaunchKernelGGL((coef_kernel<P, 4>), dim3(token_tiles * ca.splits), dim3(256), 0, st, ca);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -1216,7 +1248,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         pa.out = dw ? static_cast<T*>(dw) + base * dw_stride : nullptr;
         const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
         if (!blocks) continue;
-        if (w.large_products) hipLaunchKernelGGL((products_kernel<P, 8>), dim3(blocks), dim3(512), 0, st, pa);
+        if (P == 1 && w.large_products) hipLaunchKernelGGL((products_kernel<1, 8>), dim3(blocks), dim3(512), 0, st, pa);
         else hipLaunchKernelGGL((products_kernel<P, 4>), dim3(blocks), dim3(256), 0, st, pa);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
