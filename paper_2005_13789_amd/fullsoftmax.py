@@ -1,0 +1,64 @@
+"""Skip-gram with the full softmax: the objective that negative sampling approximates.
+
+A pair (src, ctx) is scored against every row of the context table instead of a few sampled ones:
+loss = -log softmax(context . vertex[src])[ctx].  A step looks up the batch's vertex rows, takes the softmax cross
+entropy against the whole context table without keeping the scores, brings the gradients back to both tables (the
+vertex table's by sorted ids) and moves both with AdamW.  Every part is a call of the library; torch allocates.
+"""
+from __future__ import annotations
+
+import torch
+
+import paper_2005_13789_amd as ne
+
+
+class SoftmaxTrainer:
+    """Trains vertex and context (float32 [num_nodes][dim], CUDA, updated in place) on batches of at most `batch` pairs.
+
+    compute: torch.float32, or torch.bfloat16 for products and gradients in bf16 on rounded copies of the tables that
+    every step of AdamW writes.  state_bits: 32, or 8 for AdamW states of a byte each."""
+
+    def __init__(self, vertex: torch.Tensor, context: torch.Tensor, batch: int, state_bits: int = 32, weight_decay: float = 0.0,
+                 compute: torch.dtype = torch.float32, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        if vertex.shape != context.shape or vertex.dim() != 2:
+            raise ValueError("vertex and context must both be [num_nodes][dim]")
+        V, d = vertex.shape
+        dev = vertex.device
+        self.batch, self.steps = batch, 0
+        self.tables = [vertex, context]
+        copies = None
+        if compute == torch.bfloat16:
+            copies = [t.bfloat16() for t in self.tables]
+        self.rows = copies if copies is not None else self.tables       # what products read
+        self.grads = [torch.empty((V, d), dtype=compute, device=dev) for _ in range(2)]
+        self.h, self.dh = (torch.empty((batch, d), dtype=compute, device=dev) for _ in range(2))
+        self.loss, self.lse = (torch.empty(batch, dtype=torch.float32, device=dev) for _ in range(2))
+        size = max(ne.ne_embed_workspace_bytes(V, d, batch), ne.ne_xent_workspace_bytes(batch, V, d, compute, False),
+                   ne.ne_xent_workspace_bytes(batch, V, d, compute, True))
+        self.work = torch.empty(size, dtype=torch.uint8, device=dev)     # one after the other on one stream: shared by the calls
+        kw = {}
+        if state_bits == 8:
+            states = [[torch.zeros((V, d), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) for _ in range(2)] for _ in range(2)]
+            blocks = -(-V * d // ne.NE_ADAMW_BLOCK)
+            kw["m_scale"], kw["v_scale"] = ([torch.zeros(blocks, device=dev) for _ in range(2)] for _ in range(2))
+        else:
+            states = [[torch.zeros((V, d), device=dev) for _ in range(2)] for _ in range(2)]
+        opt_work = torch.empty(ne.ne_adamw_workspace_bytes([V * d] * 2), dtype=torch.uint8, device=dev)
+        self.opt = ne.ne_create_adamw(self.tables, self.grads, *states, opt_work, weight_decay=weight_decay, params_bf16=copies, seed=seed, **kw)
+
+    def step(self, pairs: torch.Tensor, lr: float) -> torch.Tensor:
+        """One step of the mean loss of pairs int32 [n][2] (CUDA, n <= batch; a pair whose ctx is outside the tables does not count).  Returns the pairs' losses before the step (a view that the next step overwrites)."""
+        n = int(pairs.shape[0])
+        if n < 1 or n > self.batch:
+            raise ValueError(f"a step takes 1 to {self.batch} pairs")
+        src, ctx = pairs[:, 0].contiguous(), pairs[:, 1].contiguous()
+        h, dh, loss, lse = self.h[:n], self.dh[:n], self.loss[:n], self.lse[:n]
+        ne.ne_embed_lookup(self.rows[0], src, h)
+        ne.ne_xent_loss(h, self.rows[1], ctx, loss, lse, self.work)
+        ne.ne_xent_grad(h, self.rows[1], ctx, lse, dh, self.grads[1], self.work, scale=1.0 / n)
+        ne.ne_embed_grad(src, dh, self.grads[0], self.work)
+        self.steps += 1
+        ne.ne_adamw_step(self.opt, self.steps, lr)
+        return loss

@@ -21,6 +21,7 @@ import torch
 
 import paper_2005_13789_amd as ne
 import workloads as wl
+from paper_2005_13789_amd.fullsoftmax import SoftmaxTrainer
 
 
 def read_edge_list(path: str):
@@ -101,7 +102,8 @@ def train(train_edges: np.ndarray, num_nodes: int, dim: int = 64, epochs: int = 
     """Embeddings from walks over the training edges: per epoch one walk per node, window pairs shuffled,
     batches of `batch` pairs through ne_train_block (mode "sync", the exact step) or ne_train_block_async
     (mode "async", the per-sample mode), or the walks themselves through ne_train_walks (mode "walks": the exact step on batches of
-    whole walks, unshuffled), learning rate decaying linearly over the run.  Returns (Tables, Alias); the handles keep
+    whole walks, unshuffled), or SoftmaxTrainer (mode "softmax": the full softmax over all nodes in the place of sampled
+    negatives, AdamW with 32-bit states; lr0 is Adam's), learning rate decaying linearly over the run.  Returns (Tables, Alias); the handles keep
     their device tensors alive (tables.vertex, tables.context)."""
     dev = torch.device(device)
     graph = wl.build_graph(num_nodes, torch.from_numpy(np.asarray(train_edges, dtype=np.int64)))
@@ -116,6 +118,11 @@ def train(train_edges: np.ndarray, num_nodes: int, dim: int = 64, epochs: int = 
     tables = ne.ne_create_tables(vertex, context, seed, init=True, max_batch=max_batch, max_negatives=negatives, workspace=ws)
     table = torch.empty((num_nodes, 2), dtype=torch.int32, device=dev)
     alias = ne.ne_build_neg_alias(graph.degree.clamp(max=2**32 - 1).numpy().astype(np.uint32), 0, table)
+    trainer = None
+    if mode == "softmax":
+        # as the sampled objective starts, but with context rows that differ: a table of zeros has no gradient towards vertex rows
+        context.copy_(vertex[torch.randperm(num_nodes, generator=torch.Generator().manual_seed(seed)).to(dev)])
+        trainer = SoftmaxTrainer(vertex, context, batch, seed=seed)
     if mode == "walks":
         # on-device augmentation: the walks themselves are the input; a batch is as many whole walks as hold
         # about `batch` samples
@@ -145,8 +152,11 @@ def train(train_edges: np.ndarray, num_nodes: int, dim: int = 64, epochs: int = 
             ne.ne_train_block(tables, alias, p, batch, negatives, lrs, done)
         elif mode == "async":
             ne.ne_train_block_async(tables, alias, p, batch, negatives, lrs, done)
+        elif mode == "softmax":
+            for s, lr in zip(starts, lrs):
+                trainer.step(p[s:s + batch], float(lr))
         else:
-            raise ValueError("mode must be 'sync', 'async' or 'walks'")
+            raise ValueError("mode must be 'sync', 'async', 'walks' or 'softmax'")
         done += n
     torch.cuda.synchronize(dev)
     return tables, alias
@@ -166,7 +176,7 @@ def main(argv=None) -> int:
     ap.add_argument("--lr", type=float, default=0.025)
     ap.add_argument("--walk-length", type=int, default=40)
     ap.add_argument("--window", type=int, default=5)
-    ap.add_argument("--mode", default="sync", choices=["sync", "walks", "async"])
+    ap.add_argument("--mode", default="sync", choices=["sync", "walks", "async", "softmax"])
     ap.add_argument("--seed", type=int, default=0)
     args = ap.parse_args(argv)
     edges, n = read_edge_list(args.edges)
