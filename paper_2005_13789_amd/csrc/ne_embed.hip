@@ -242,6 +242,7 @@ struct GradArgs {
     uint32_t n, num_rows;
     int32_t dim, chunks, lanes_log2;
     float scale;
+    int32_t clear_all;         // rows are cleared before the named ones are written
 };
 
 // Terms of a run [s, e) of sorted positions: single positions up to a multiple of 16, sums of 16 up to a multiple of
@@ -393,8 +394,15 @@ __device__ __forceinline__ void sum_rows(const GradArgs& a, uint32_t rows, const
         float zero[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) zero[e] = 0.0f;
+        if (a.clear_all) {      // rows side by side, few of them named: all are cleared as one range (named ones are written after the barrier)
+            TT* to = static_cast<TT*>(a.table) + static_cast<int64_t>(row_of(0)) * a.dim;
+            const uint32_t count = rows * static_cast<uint32_t>(a.dim);
 #pragma unroll 4
-        for (uint32_t r = group; r < rows; r += groups)
+            for (uint32_t i = threadIdx.x * V; i + V <= count; i += kThreads * V) store_vec<TT, V>(to + i, zero);
+            for (uint32_t i = count / V * V + threadIdx.x; i < count; i += kThreads) to[i] = from_float<TT>(0.0f);
+        }
+#pragma unroll 4
+        for (uint32_t r = a.clear_all ? rows : group; r < rows; r += groups)
             if (start[r] == start[r + 1])
                 for (int c = lane; c < a.chunks; c += lanes)
                     store_vec<TT, V>(static_cast<TT*>(a.table) + static_cast<int64_t>(row_of(r)) * a.table_stride + min(c * V, a.dim - V), zero);
@@ -813,9 +821,10 @@ hipError_t launch_few(const GradArgs& a, const int32_t* ids, bool add, hipStream
     const size_t lds = static_cast<size_t>((a.n + 1) & ~1u) * 4 + static_cast<size_t>(a.n) * 2;
     if (add) {
         f.slots = kAddIds;
-    } else {        // as many rows as make about 512 workgroups: each looks through all ids
+    } else {        // 512 workgroups, and up to 4096 where looking through all ids costs each of them little
+        const uint32_t most = std::min(std::max(4u << 20, 512 * a.n) / a.n, 4096u);
         f.slots = 32;
-        while (f.slots < kMostSlots && a.num_rows / f.slots > 512) f.slots *= 2;
+        while (f.slots < kMostSlots && a.num_rows / f.slots > most) f.slots *= 2;
     }
     while ((1u << f.slot_bits) < f.slots + (add ? 1 : 0)) f.slot_bits += 1;
     const uint32_t blocks = add ? (a.n + kAddIds - 1) / kAddIds : (a.num_rows + f.slots - 1) / f.slots;
@@ -953,6 +962,7 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("sort launch: ") + hipGetErrorString(e));
     a.grad = grad_dev; a.partial = w.partial; a.super = w.super; a.table = table_grad_dev; a.grad_stride = grad_stride; a.table_stride = table_grad_stride;
     a.n = static_cast<uint32_t>(n); a.num_rows = static_cast<uint32_t>(num_rows); a.dim = dim; a.scale = scale;
+    a.clear_all = table_grad_stride == dim && n * 4 <= num_rows;      // (a row written twice costs less than rows cleared one by one)
     const bool add = accumulate != 0;
     e = grad_type == NE_F32 ? (table_grad_type == NE_F32 ? launch_grad_dim<float, float>(a, ids_dev, add, st) : launch_grad_dim<float, bf16_t>(a, ids_dev, add, st))
                             : (table_grad_type == NE_F32 ? launch_grad_dim<bf16_t, float>(a, ids_dev, add, st) : launch_grad_dim<bf16_t, bf16_t>(a, ids_dev, add, st));
