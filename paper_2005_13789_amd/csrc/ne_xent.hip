@@ -75,7 +75,9 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
-__device__ __forceinline__ void stage_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Waits for all but the last LATER loads of this wavefront, and for the other wavefronts.
+template <int LATER = 0>
+__device__ __forceinline__ void stage_done() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory"); }
 
 __device__ __forceinline__ uint32_t lds_address(const unsigned char* p)
 {
@@ -485,7 +487,105 @@ __device__ __forceinline__ void score_tiles(const Operand& w, const Operand& h, 
         });
 }
 
-template <int P, int W>
+// The same with small tiles where H's rows have at most KS stages: a wavefront holds its 64 rows of H in registers, as the operands that they
+// are, and only the table travels, in a ring of four stages, three of them ahead.  (Loads from L2 are what bounds these shapes.)
+template <int P, int KS, class Epilogue>
+__device__ __forceinline__ void score_tiles_held(const Operand& w, const Operand& h, uint32_t token_tile, uint32_t first, uint32_t tile0, uint32_t tile1, int steps,
+                                                 unsigned char* lds, Epilogue epilogue)
+{
+    constexpr int BYTES = operand_bytes<4>(), KK = step_of<P>() / 16, LOADS = 4;
+    const int m0 = first_row<4>(), n0 = first_col<4>();
+    const uint32_t lds0 = lds_address(lds);
+    s16x8 held[KS][KK][P][2];
+    {
+        Loader<P, 4, true> load_h;
+        load_h.start(h, token_tile * rows_of<4>(), 0);
+        for (int s = 0; s < steps; ++s) load_h.fetch(lds0 + s * BYTES);
+        stage_done();
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        held[s][kk][p][i] = s < steps ? fragment<P, 4, true>(lds + s * BYTES, p, n0 + 32 * i, kk) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        stage_done();
+    }
+    f32x16 acc[2][2];
+    clear(acc);
+    const uint32_t total = tile1 > tile0 ? (tile1 - tile0) * steps : 0;
+    Loader<P, 4, true> load_w;
+    uint32_t row0 = first + tile0 * rows_of<4>(), next_row0 = row0, issued = 0, used = 0;
+    int next_step = 0;
+    auto issue = [&]() {
+        if (issued == total) return;
+        if (next_step == 0) load_w.start(w, next_row0, 0);
+        load_w.fetch(lds0 + (issued & 3) * BYTES);
+        ++issued;
+        if (++next_step == steps) { next_step = 0; next_row0 += rows_of<4>(); }
+    };
+    // (writes may overtake loads: after some, all loads are waited for)
+    auto wait = [&](bool wrote) {
+        if (issued - used == 3 && !wrote) stage_done<2 * LOADS>();
+        else stage_done();
+    };
+    issue();
+    issue();
+    issue();
+    wait(false);
+    while (used < total) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if (s >= steps) break;
+            issue();
+            const unsigned char* stage = lds + (used & 3) * BYTES;
+            s16x8 a[2][P][2];
+            auto read = [&](int kk) {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) a[kk & 1][p][i] = fragment<P, 4, true>(stage, p, m0 + 32 * i, kk);
+            };
+            read(0);
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if (kk + 1 < KK) read(kk + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int im = 0; im < 2; ++im)
+#pragma unroll
+                    for (int in = 0; in < 2; ++in) {
+                        acc[im][in] = mfma<P>(a[kk & 1][0][im], held[s][kk][0][in], acc[im][in]);
+                        if (P == 2) {
+                            acc[im][in] = mfma<P>(a[kk & 1][0][im], held[s][kk][P - 1][in], acc[im][in]);
+                            acc[im][in] = mfma<P>(a[kk & 1][P - 1][im], held[s][kk][0][in], acc[im][in]);
+                        }
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (s == steps - 1) {
+                epilogue(row0, acc);
+                clear(acc);
+                row0 += rows_of<4>();
+            }
+            ++used;
+            wait(s == steps - 1);
+        }
+    }
+}
+
+// Either: KS stages of H at most in registers, or none.
+template <int P, int W, int KS, class Epilogue>
+__device__ __forceinline__ void all_scores(const Operand& w, const Operand& h, uint32_t token_tile, uint32_t first, uint32_t tile0, uint32_t tile1, int steps,
+                                           unsigned char* lds, Epilogue epilogue)
+{
+    if constexpr (KS > 0) score_tiles_held<P, KS>(w, h, token_tile, first, tile0, tile1, steps, lds, epilogue);
+    else score_tiles<P, W>(w, h, token_tile, first, tile0, tile1, steps, lds, epilogue);
+}
+
+template <int P, int W, int KS>
 __global__ void __launch_bounds__(64 * W, 2) scores_kernel(ScoreArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
@@ -504,7 +604,7 @@ __global__ void __launch_bounds__(64 * W, 2) scores_kernel(ScoreArgs a)
         target[j] = token[j] < a.n ? static_cast<uint32_t>(a.targets[token[j]]) : 0xFFFFFFFFu;
         if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
     }
-    score_tiles<P, W>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
+    all_scores<P, W, KS>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
         if (row0 + 32 * MT > a.num_rows) {
             const int left = static_cast<int>(a.num_rows) - static_cast<int>(lane_row0);
@@ -737,7 +837,7 @@ __device__ __forceinline__ u32x4 eight_of(u32x2 a, u32x2 b)
     return u32x4{x[0], y[0], x[1], y[1]};
 }
 
-template <int P, int W>
+template <int P, int W, int KS>
 __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
@@ -759,7 +859,7 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
         by[j] = counts ? fmaf(a.lse[token], kLog2e, P == 2 ? -static_cast<float>(kGShift) : 0.0f) : INFINITY;
         c[j] = P == 1 && a.c && counts ? a.c[token] : 1.0f;
     }
-    score_tiles<P, W>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
+    all_scores<P, W, KS>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -1107,6 +1207,14 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     return w;
 }
 
+// Stages of H that the scores' wavefronts hold in registers: 2, 4, or 0 for H through LDS like the table: where there are more, with large
+// tiles, and where a workgroup has so few tiles that fetching H ahead of them does not pay.
+int held_stages(const XentWs& w, uint32_t row_tiles, uint32_t splits, int steps)
+{
+    if (w.large_scores || steps > 4 || ceil_div(row_tiles, splits) < 3) return 0;
+    return steps > 2 ? 4 : 2;
+}
+
 struct XentCall {
     const void *h, *w;
     int64_t h_stride, w_stride, n, num_rows;
@@ -1193,8 +1301,12 @@ hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse,
     if (e != hipSuccess) return e;
     a.targets = x.targets; a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles;
     a.splits = w.splits; a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.target_score = w.target_score;
-    if (P == 1 && w.large_scores) hipLaunchKernelGGL((scores_kernel<1, 8>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 256) * w.splits)), dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((scores_kernel<P, 4>), dim3(static_cast<unsigned>(ceil_div(w.tokens, 128) * w.splits)), dim3(256), 0, st, a);
+    const dim3 grid(static_cast<unsigned>(ceil_div(w.tokens, w.large_scores ? 256 : 128) * w.splits));
+    const int held = held_stages(w, w.row_tiles, w.splits, a.steps);
+    if (P == 1 && w.large_scores) hipLaunchKernelGGL((scores_kernel<1, 8, 0>), grid, dim3(512), 0, st, a);
+    else if (held == 0) hipLaunchKernelGGL((scores_kernel<P, 4, 0>), grid, dim3(256), 0, st, a);
+    else if (held == 2) hipLaunchKernelGGL((scores_kernel<P, 4, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((scores_kernel<P, 4, 4>), grid, dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     return join_losses(x, w, loss, lse, st);
@@ -1231,8 +1343,12 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         ca.splits = splits_of(ca.row_tiles, token_tiles, w.large_scores);
         ca.tokens = static_cast<uint32_t>(w.tokens);
         for (int p = 0; p < P; ++p) ca.g[p] = w.g[p];
-        if (P == 1 && w.large_scores) hipLaunchKernelGGL((coef_kernel<1, 8>), dim3(token_tiles * ca.splits), dim3(512), 0, st, ca);
-        else hipLaunchKernelGGL((coef_kernel<P, 4>), dim3(token_tiles * ca.splits), dim3(256), 0, st, ca);
+        const dim3 grid(token_tiles * ca.splits);
+        const int held = held_stages(w, ca.row_tiles, ca.splits, ca.steps);
+        if (P == 1 && w.large_scores) hipLaunchKernelGGL((coef_kernel<1, 8, 0>), grid, dim3(512), 0, st, ca);
+        else if (held == 0) hipLaunchKernelGGL((coef_kernel<P, 4, 0>), grid, dim3(256), 0, st, ca);
+        else if (held == 2) hipLaunchKernelGGL((coef_kernel<P, 4, 2>), grid, dim3(256), 0, st, ca);
+        else hipLaunchKernelGGL((coef_kernel<P, 4, 4>), grid, dim3(256), 0, st, ca);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         pa.g_rows = Operand{{w.g[0], w.g[1]}, w.piece, static_cast<uint32_t>(w.tokens - 1), static_cast<uint32_t>(w.piece)};
