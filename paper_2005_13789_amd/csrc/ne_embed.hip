@@ -95,7 +95,29 @@ struct SortArgs {
     uint32_t* hist;            // [tiles][digits]
     uint32_t n, num_rows, tile_len, tiles;
     int32_t pass, bits, shift;
+    // the table's rows [clear_from, clear_to) are cleared by the launch's further workgroups, so many bytes of every clear_stride
+    unsigned char* table;
+    int64_t clear_stride, clear_bytes;
+    uint32_t clear_from, clear_to;
 };
+
+// Share `part` of `parts` of the rows that a sorting launch clears.  (A sorting pass occupies an eighth of the machine for 5 to 8 us, most of
+// which it waits.)
+__device__ __forceinline__ void clear_rows(const SortArgs& a, uint32_t part, uint32_t parts)
+{
+    const uint32_t rows = a.clear_to - a.clear_from;
+    const uint32_t r0 = a.clear_from + static_cast<uint32_t>(static_cast<uint64_t>(rows) * part / parts);
+    const uint32_t r1 = a.clear_from + static_cast<uint32_t>(static_cast<uint64_t>(rows) * (part + 1) / parts);
+    const bool flat = a.clear_stride == a.clear_bytes;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (uint32_t r = r0; r < r1; r = flat ? r1 : r + 1) {
+        unsigned char* to = a.table + r * a.clear_stride;
+        const int64_t bytes = flat ? (r1 - r0) * a.clear_bytes : a.clear_bytes;
+#pragma unroll 4
+        for (int64_t i = threadIdx.x * 16; i + 16 <= bytes; i += kSortThreads * 16) __builtin_memcpy(to + i, &zero, 16);
+        for (int64_t i = bytes / 16 * 16 + threadIdx.x * 2; i < bytes; i += kSortThreads * 2) __builtin_memcpy(to + i, &zero, 2);
+    }
+}
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t num_rows) { return min(static_cast<uint32_t>(id), num_rows); }
 
@@ -124,6 +146,10 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[ITEMS], const
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a)
 {
     __shared__ uint32_t count[kMostDigits];
+    if (blockIdx.x >= a.tiles) {
+        clear_rows(a, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+        return;
+    }
     const uint32_t digits = 1u << a.bits, mask = digits - 1;
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
     __syncthreads();
@@ -165,6 +191,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
     __shared__ uint32_t base[kMostDigits];
     __shared__ uint32_t count[kSortWaves][kMostDigits];
     __shared__ uint32_t wave_sums[kSortWaves];
+    if (blockIdx.x >= a.tiles) {
+        clear_rows(a, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+        return;
+    }
     const uint32_t digits = 1u << a.bits, mask = digits - 1;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     // thread t has digits 2t and 2t + 1
@@ -505,20 +535,8 @@ __global__ void __launch_bounds__(kThreads) super_sums_kernel(GradArgs a)
     }
 }
 
-// First sorted position whose key is at least `key`.
-__device__ __forceinline__ uint32_t lower_bound(const uint2* sorted, uint32_t n, uint32_t key)
-{
-    uint32_t lo = 0, len = n;
-    while (len) {
-        const uint32_t half = len >> 1;
-        if (sorted[lo + half].x < key) { lo += half + 1; len -= half + 1; }
-        else len = half;
-    }
-    return lo;
-}
-
-// The same by a whole wavefront: 64 probes at a time, three rounds of them for 2^18 positions (each waits for memory, as
-// the positions come from the launch before: 17 rounds of single probes are 17 times a microsecond).
+// First sorted position whose key is at least `key`, by a whole wavefront: 64 probes at a time, three rounds of them for 2^18
+// positions (each waits for memory, as the positions come from the launch before).
 __device__ __forceinline__ uint32_t wave_lower_bound(const uint2* sorted, uint32_t n, uint32_t key)
 {
     uint32_t lo = 0, len = n;
@@ -532,78 +550,44 @@ __device__ __forceinline__ uint32_t wave_lower_bound(const uint2* sorted, uint32
     return lo;
 }
 
-constexpr uint32_t kKeysInLds = 1024;   // positions of a workgroup whose keys fit there
-
-// The rows launch.  ADD: a workgroup has 64 sorted positions and writes the rows whose runs begin there; otherwise it has
-// 64 rows and writes them all.
+// The rows launch: a workgroup has 64 sorted positions and writes the rows whose runs begin there (the others were cleared while the
+// positions were sorted; ADD: they keep what they hold).
 template <class TG, class TT, int V, bool ADD>
 __global__ void __launch_bounds__(kThreads) rows_kernel(GradArgs a)
 {
     __shared__ float lds[kThreads][V];
     __shared__ RowLists lists;
-    __shared__ uint32_t start[kRowsPerGroup + 1], key[ADD ? kRowsPerGroup : kKeysInLds], place[ADD ? 1 : kKeysInLds], bounds[2];
-    const int wave = threadIdx.x >> 6;
-    uint32_t lo = 0, len = 0xFFFFFFFFu;
+    __shared__ uint32_t start[kRowsPerGroup + 1], key[kRowsPerGroup], place[2 * kRowsPerGroup], found;
     const uint32_t first = blockIdx.x * kRowsPerGroup;
-    uint32_t rows;
-    if (ADD) {
-        // the runs that begin in [first, first + 64), side by side; the last one's end is looked for
+    // the runs that begin here, side by side; the last one's end is looked for
+    if (threadIdx.x < 2 * kRowsPerGroup) {
         const uint32_t k = first + threadIdx.x;
-        const bool in = threadIdx.x < kRowsPerGroup && k < a.n;
-        const uint32_t mine = in ? a.sorted[k].x : 0xFFFFFFFFu;
-        const bool begins = in && mine < a.num_rows && (k == 0 || a.sorted[k - 1].x != mine);
-        const uint64_t all = __ballot(begins);
-        if (threadIdx.x < 64) {
+        const uint2 e = k < a.n ? a.sorted[k] : make_uint2(0xFFFFFFFFu, 0);
+        place[threadIdx.x] = e.y;
+        if (threadIdx.x < kRowsPerGroup) {
+            const bool begins = e.x < a.num_rows && (k == 0 || a.sorted[k - 1].x != e.x);
+            const uint64_t all = __ballot(begins);
             const int at = __popcll(all & ((1ull << threadIdx.x) - 1));
-            if (begins) { start[at] = k; key[at] = mine; }
-            if (threadIdx.x == 0) start[kRowsPerGroup] = __popcll(all);
-        }
-        __syncthreads();
-        rows = start[kRowsPerGroup];
-        __syncthreads();
-        if (rows == 0) return;
-        if (wave == 0) {
-            const uint32_t end = wave_lower_bound(a.sorted, a.n, key[rows - 1] + 1);
-            if (threadIdx.x == 0) start[rows] = end;
-        }
-    } else {
-        rows = min(static_cast<uint32_t>(kRowsPerGroup), a.num_rows - first);
-        if (wave < 2) {
-            const uint32_t at = wave_lower_bound(a.sorted, a.n, first + wave * rows);
-            if ((threadIdx.x & 63) == 0) bounds[wave] = at;
-        }
-        __syncthreads();
-        lo = bounds[0];
-        len = bounds[1] - lo;
-        if (len <= kKeysInLds) {
-            for (uint32_t i = threadIdx.x; i < len; i += kThreads) {
-                const uint2 e = a.sorted[lo + i];
-                key[i] = e.x;
-                place[i] = e.y;
-            }
-            __syncthreads();
-            if (threadIdx.x <= rows) {
-                uint32_t at = 0, left = len;
-                while (left) {
-                    const uint32_t half = left >> 1;
-                    if (key[at + half] < first + threadIdx.x) { at += half + 1; left -= half + 1; }
-                    else left = half;
-                }
-                start[threadIdx.x] = lo + at;
-            }
-        } else if (threadIdx.x <= rows) {
-            start[threadIdx.x] = lo + lower_bound(a.sorted + lo, len, first + threadIdx.x);
+            if (begins) { start[at] = k; key[at] = e.x; }
+            if (threadIdx.x == 0) found = __popcll(all);
         }
     }
     __syncthreads();
-    auto position = [&](uint32_t k) { return !ADD && len <= kKeysInLds ? place[k - lo] : a.sorted[k].y; };
+    const uint32_t rows = found;
+    if (rows == 0) return;
+    if (threadIdx.x < 64) {
+        const uint32_t end = wave_lower_bound(a.sorted, a.n, key[rows - 1] + 1);
+        if (threadIdx.x == 0) start[rows] = end;
+    }
+    __syncthreads();
     const TG* grad = static_cast<const TG*>(a.grad);
+    auto position = [&](uint32_t k) { return k - first < 2 * kRowsPerGroup ? place[k - first] : a.sorted[k].y; };
     sum_rows<TT, V, ADD>(
         a, rows, start, lds, lists, [](uint32_t) { return false; },
         [&](uint32_t k, int at, float (&x)[V]) { load_vec<TG, V>(grad + static_cast<int64_t>(position(k)) * a.grad_stride + at, x); },
         [&](uint32_t r) { return run_of(start[r], start[r + 1], a.super != nullptr).terms; },
         [&](uint32_t r, uint32_t t, int at, float (&x)[V]) { load_term<TG, V>(a, run_of(start[r], start[r + 1], a.super != nullptr), t, at, x, position); },
-        [&](uint32_t r) { return ADD ? key[r] : first + r; });
+        [&](uint32_t r) { return key[r]; });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -846,10 +830,9 @@ hipError_t launch_grad(const GradArgs& a, const int32_t* ids, bool add, hipStrea
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (add)
-        hipLaunchKernelGGL((rows_kernel<TG, TT, V, true>), dim3((a.n + kRowsPerGroup - 1) / kRowsPerGroup), dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL((rows_kernel<TG, TT, V, false>), dim3((a.num_rows + kRowsPerGroup - 1) / kRowsPerGroup), dim3(kThreads), 0, st, a);
+    const dim3 grid((a.n + kRowsPerGroup - 1) / kRowsPerGroup);
+    if (add) hipLaunchKernelGGL((rows_kernel<TG, TT, V, true>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((rows_kernel<TG, TT, V, false>), grid, dim3(kThreads), 0, st, a);
     return hipGetLastError();
 }
 
@@ -877,21 +860,35 @@ hipError_t launch_lookup(LookupArgs a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_sort(const EmbedWs& w, const int32_t* ids, int64_t n, int64_t num_rows, const uint2** sorted, hipStream_t st)
+// table: NULL, or the rows that the sorting launches clear meanwhile, an equal share each.
+hipError_t launch_sort(const EmbedWs& w, const int32_t* ids, int64_t n, int64_t num_rows, void* table, int64_t row_bytes, int64_t row_stride,
+                       const uint2** sorted, hipStream_t st)
 {
     SortArgs s{};
     s.ids = ids; s.hist = w.hist; s.n = static_cast<uint32_t>(n); s.num_rows = static_cast<uint32_t>(num_rows);
     s.tile_len = w.tile_len; s.tiles = w.tiles; s.bits = w.bits;
+    s.table = static_cast<unsigned char*>(table); s.clear_bytes = row_bytes; s.clear_stride = row_stride;
+    const int launches = 2 * w.passes;
+    int done = 0;
+    auto share = [&]() -> uint32_t {        // the next share, and the workgroups for it: 64 KB or more each
+        if (!table) return 0;
+        s.clear_from = static_cast<uint32_t>(num_rows * done / launches);
+        s.clear_to = static_cast<uint32_t>(num_rows * (done + 1) / launches);
+        done += 1;
+        return static_cast<uint32_t>(std::min<int64_t>(((s.clear_to - s.clear_from) * row_bytes + 65535) / 65536, 1024));
+    };
     hipError_t e = hipSuccess;
     for (int p = 0; p < w.passes && e == hipSuccess; ++p) {
         s.pass = p; s.shift = p * w.bits;
         s.in = w.entries[(p + 1) & 1];
         s.out = w.entries[p & 1];
         *sorted = s.out;
-        hipLaunchKernelGGL(sort_count_kernel, dim3(w.tiles), dim3(kSortThreads), 0, st, s);
+        uint32_t more = share();
+        hipLaunchKernelGGL(sort_count_kernel, dim3(w.tiles + more), dim3(kSortThreads), 0, st, s);
         e = hipGetLastError();
         if (e != hipSuccess) break;
-        hipLaunchKernelGGL(sort_pass_kernel, dim3(w.tiles), dim3(kSortThreads), 0, st, s);
+        more = share();
+        hipLaunchKernelGGL(sort_pass_kernel, dim3(w.tiles + more), dim3(kSortThreads), 0, st, s);
         e = hipGetLastError();
     }
     return e;
@@ -958,11 +955,14 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
         return fail(NE_ERR_ARG, "ne_embed_grad: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_embed_workspace_bytes()");
     GradArgs a{};
-    hipError_t e = few_ids(num_rows, n) ? hipSuccess : launch_sort(w, ids_dev, n, num_rows, &a.sorted, st);
+    const bool few = few_ids(num_rows, n);
+    const int64_t element = static_cast<int64_t>(type_bytes(table_grad_type));
+    hipError_t e = few ? hipSuccess
+                       : launch_sort(w, ids_dev, n, num_rows, accumulate ? nullptr : table_grad_dev, dim * element, table_grad_stride * element, &a.sorted, st);
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("sort launch: ") + hipGetErrorString(e));
     a.grad = grad_dev; a.partial = w.partial; a.super = w.super; a.table = table_grad_dev; a.grad_stride = grad_stride; a.table_stride = table_grad_stride;
     a.n = static_cast<uint32_t>(n); a.num_rows = static_cast<uint32_t>(num_rows); a.dim = dim; a.scale = scale;
-    a.clear_all = table_grad_stride == dim && n * 4 <= num_rows;      // (a row written twice costs less than rows cleared one by one)
+    a.clear_all = few && table_grad_stride == dim && n * 4 <= num_rows;      // (a row written twice costs less than rows cleared one by one)
     const bool add = accumulate != 0;
     e = grad_type == NE_F32 ? (table_grad_type == NE_F32 ? launch_grad_dim<float, float>(a, ids_dev, add, st) : launch_grad_dim<float, bf16_t>(a, ids_dev, add, st))
                             : (table_grad_type == NE_F32 ? launch_grad_dim<bf16_t, float>(a, ids_dev, add, st) : launch_grad_dim<bf16_t, bf16_t>(a, ids_dev, add, st));
