@@ -38,6 +38,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kAmaxBlocks = 1024;
+constexpr int64_t kMostStride = 1 << 22;   // elements: a tile's 256 rows are within 32 bits of its first
 constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
 constexpr int kFewBytes = 65536;
 constexpr int kFewGroups = 1024;
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(64 * W, 2) scores_kernel(ScoreArgs a)
     all_scores<P, W, KS>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
         if (row0 + 32 * MT > a.num_rows) {
-            const int left = static_cast<int>(a.num_rows) - static_cast<int>(lane_row0);
+            const int left = static_cast<int>(a.num_rows - lane_row0);     // (the difference is small where both are not)
 #pragma unroll
             for (int im = 0; im < MT; ++im)
 #pragma unroll
@@ -876,7 +877,7 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
                         if (target[j] - lane_row0 == 32 * im + sum_row(i)) acc[im][j][i] -= P == 2 ? 0x1p14f : 1.0f;
             }
             if (row0 + 32 * MT > a.num_rows) {
-                const int left = static_cast<int>(a.num_rows) - static_cast<int>(lane_row0);
+                const int left = static_cast<int>(a.num_rows - lane_row0);     // (the difference is small where both are not)
 #pragma unroll
                 for (int im = 0; im < MT; ++im)
 #pragma unroll
@@ -1186,15 +1187,15 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
             w.large_products = large;
             w.h_stages = static_cast<uint32_t>(w.piece / step);
             w.w_stages = static_cast<uint32_t>(w.tokens / step);
-            const int64_t share = std::max<int64_t>(16, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, slots_of(large)));
+            const int64_t share = std::max<int64_t>(8, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, slots_of(large)));
             w.h_splits = static_cast<uint32_t>(ceil_div(w.h_stages, share));
             w.w_splits = static_cast<uint32_t>(ceil_div(w.w_stages, share));
             w.h_share = static_cast<uint32_t>(ceil_div(w.h_stages, w.h_splits));
             w.w_share = static_cast<uint32_t>(ceil_div(w.w_stages, w.w_splits));
         };
-        // Large tiles of products (bf16, of more than 128 columns): where dW needs no partial sums with them, or has columns enough that these are
+        // Large tiles of products (bf16, of more than 128 columns, with stages enough for a workgroup that is alone on its CU): where dW needs no partial sums with them, or has columns enough that these are
         // worth it (2048 x 100 000 x 512: 778 us, 906 with small tiles; 4096 x 100 000 x 256, two partial sums: 1056 and 971).
-        split(w.parts == 1 && dim > 128);
+        split(w.parts == 1 && dim > 128 && n >= 256);
         if (w.large_products && w.w_splits > 1 && dim < 384) split(false);
         for (int p = 0; p < w.parts; ++p) {
             w.hc[p] = w.parts == 2 ? take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded) : nullptr;
@@ -1226,7 +1227,7 @@ struct XentCall {
 // Packs H (and c H) and, where it cannot be used as it is, W.
 hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Operand* hc, Operand* wo, hipStream_t st)
 {
-    const bool direct = x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && aligned(x.w, 16);
+    const bool direct = x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && x.w_stride < kMostStride && aligned(x.w, 16);
     if (x.type == NE_F32) {
         AmaxArgs a{static_cast<const float*>(x.h), static_cast<const float*>(x.w), x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, x.dim, w.amax};
         hipLaunchKernelGGL(amax_kernel, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
@@ -1263,7 +1264,9 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Opera
     } else {
         add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
     }
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(most, 4), 2048)), static_cast<unsigned>(count));
+    int lanes = 1;      // of a row, as in the kernel; four rows of a lane group in flight
+    while (lanes < 64 && 8 * lanes < w.padded) lanes *= 2;
+    const dim3 grid(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(ceil_div(most, 4 * (kThreads / lanes)), 2048))), static_cast<unsigned>(count));
     if (w.parts == 1) hipLaunchKernelGGL(pack_kernel<1>, grid, dim3(kThreads), 0, st, jobs);
     else hipLaunchKernelGGL(pack_kernel<2>, grid, dim3(kThreads), 0, st, jobs);
     return hipGetLastError();

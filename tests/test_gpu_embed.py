@@ -129,6 +129,20 @@ def test_gradient_of_many_positions(n, V):
     check_grad(ids, grad, table, rows_there, 1.0, True, before)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [1, 3, 64, 130, 520])
+def test_tables_of_which_few_rows_are_named(d, dtype):
+    """Rows side by side, cleared as one range before the named ones are written, by few ids and by many."""
+    gen = torch.Generator().manual_seed(d)
+    for n, V in ((1, 100), (100, 5003), (1200, 20011), (17000, 70001)):
+        ids = make_ids("skewed", n, V, gen)
+        grad = torch.randn(n, d, generator=gen).to(dtype).to(DEV)
+        table = torch.full((V, d), float("nan"), dtype=dtype, device=DEV)
+        work = torch.empty(ne.ne_embed_workspace_bytes(V, d, n), dtype=torch.uint8, device=DEV)
+        ne.ne_embed_grad(ids.to(DEV), grad, table, work, scale=1.5)
+        check_grad(ids, grad, table, V, 1.5, False, table.cpu())
+
+
 def test_gradient_is_the_same_every_time_and_takes_nothing_from_unnamed_positions():
     gen = torch.Generator().manual_seed(9)
     n, V, d = 30000, 400, 96

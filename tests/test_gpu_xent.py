@@ -116,6 +116,18 @@ def test_strides_and_alignment(pad, shift, dtype):
         assert bool((gap == 3.0).all())
 
 
+def test_rows_far_apart():
+    """Rows of a table that lie 8 MB or more apart: a tile's rows span more than 32 bits of bytes."""
+    n, V, d, stride = 100, 700, 64, (1 << 22) + 8
+    gen = torch.Generator().manual_seed(20)
+    big = torch.empty(V * stride, dtype=torch.bfloat16, device=DEV)
+    for step in (1 << 12, stride):
+        w = big[:V * step].view(V, step)[:, :d]
+        w.copy_((torch.randn(V, d, generator=gen) * 0.3).bfloat16())
+        h, _, t = make(n, V, d, torch.bfloat16, 21)
+        check(h, w, t, *call(h, w, t))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_loss_gradients_of_rows(dtype):
     """A factor for every row, some of them zero, negative, or very small."""
@@ -214,6 +226,31 @@ def test_gradient_against_differences():
         slope = float((up - down) / (2 * step))
         want = float((dh.double() * a.double()).sum() + (dw.double() * b.double()).sum())
         assert abs(slope - want) <= 2e-3, (slope, want)
+
+
+@pytest.mark.parametrize("dtype,n,V,d", [(torch.bfloat16, 1100, 60000, 400), (torch.bfloat16, 8300, 8200, 384), (torch.bfloat16, 600, 9000, 200),
+                                         (torch.bfloat16, 3000, 20000, 100), (torch.float32, 1500, 20000, 60), (torch.float32, 2000, 9000, 120),
+                                         (torch.float32, 1000, 30000, 300), (torch.bfloat16, 300, 150001, 256), (torch.float32, 16, 200003, 32)])
+def test_larger_shapes(dtype, n, V, d):
+    """Large and small tiles, rows of H in registers, partial sums and none, one piece and several: against 64 bits on the GPU.  Norms of
+    the differences: scores are off by about 2^-22 sqrt(d), bf16 coefficients and outputs by 2^-9 each (rounding errors of independent
+    elements: 2^-9 / sqrt(3) of their root mean square); twice that."""
+    say("larger", dtype, n, V, d)
+    h, w, t = make(n, V, d, dtype, n + d, ignored=0.1)
+    loss, lse, dh, dw = call(h, w, t, scale=1.0 / n)
+    H, W, T = h.double(), w.double(), t.long()
+    ok = (T >= 0) & (T < V)
+    S = torch.mm(H, W.t().contiguous())
+    z = torch.logsumexp(S, 1)
+    at = T.clamp(0, V - 1)
+    want = z - S.gather(1, at[:, None])[:, 0]
+    assert float((lse.double() - z)[ok].abs().max()) <= 2e-5 and float((loss.double() - want)[ok].abs().max()) <= 2e-5
+    G = torch.exp(S - z[:, None])
+    G[torch.arange(n, device=DEV), at] -= 1.0
+    G = G * (ok / n)[:, None]
+    bar = 2 * 2.0 ** -9 * (2 / 3) ** 0.5 if dtype == torch.bfloat16 else 1e-5
+    for got, ref in ((dh, torch.mm(G, W)), (dw, torch.mm(G.t().contiguous(), H))):
+        assert float((got.double() - ref).norm() / ref.norm()) <= bar, float((got.double() - ref).norm() / ref.norm())
 
 
 def test_no_rows():
