@@ -94,7 +94,7 @@ def check_grad(ids, grad, table_grad, V, scale, accumulate, before):
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "none", "edges"])
 @pytest.mark.parametrize("n,V,d", [(1, 1, 1), (5, 3, 7), (64, 1000, 16), (300, 40, 100), (1000, 70000, 33), (4096, 257, 64),
-                                   (4097, 1 << 20, 20), (9001, 5000, 130), (20000, 1023, 257)])
+                                   (4097, 1 << 20, 20), (9001, 5000, 130), (16384, 1024, 40), (16384, 100003, 24), (20000, 1023, 257)])
 def test_gradient(n, V, d, kind, accumulate):
     gen = torch.Generator().manual_seed(n + V + d)
     for tg, tt in ((torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
@@ -134,7 +134,7 @@ def test_gradient_of_many_positions(n, V):
 def test_tables_of_which_few_rows_are_named(d, dtype):
     """Rows side by side, cleared as one range before the named ones are written, by few ids and by many."""
     gen = torch.Generator().manual_seed(d)
-    for n, V in ((1, 100), (100, 5003), (1200, 20011), (17000, 70001)):
+    for n, V in ((1, 100), (100, 5003), (1200, 20011), (16384, 66000), (16385, 70001)):
         ids = make_ids("skewed", n, V, gen)
         grad = torch.randn(n, d, generator=gen).to(dtype).to(DEV)
         table = torch.full((V, d), float("nan"), dtype=dtype, device=DEV)
