@@ -43,6 +43,7 @@ constexpr int kFewRows = 64;           // rows of H up to which the table stream
 constexpr int kFewBytes = 65536;
 constexpr int kFewGroups = 1024;
 constexpr size_t kGBytes = size_t{128} << 20, kGBytesAtOnce = size_t{192} << 20;      // G of one piece; of all, where there is only one
+constexpr int kLeastShare = 8, kTileCost = 1;    // stages: the fewest of a product's workgroup; what beginning and writing a tile take
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
 
@@ -1111,7 +1112,7 @@ struct XentWs {
     int32_t few_blocks;                // > 0: few rows of H, so many blocks of 16
     int64_t piece;                     // table rows of a piece
     bool large_scores, large_products; // tiles of 256 x 256
-    uint32_t h_splits, w_splits, h_share, w_share, h_stages, w_stages;
+    uint32_t h_splits, w_splits, w_share, w_stages;
     float* amax;
     int32_t* shift;                    // of W, H, c H
     uint16_t *h[2], *hc[2], *w[2];
@@ -1132,6 +1133,19 @@ uint32_t splits_of(int64_t row_tiles, int64_t token_tiles, bool large)
 {
     const int64_t slots = slots_of(large), most = std::max<int64_t>(1, std::min<int64_t>(row_tiles, slots / std::min<int64_t>(token_tiles, slots)));
     return static_cast<uint32_t>(ceil_div(row_tiles, ceil_div(row_tiles, most)));
+}
+
+// When a launch ends, in stages: `first` workgroups of `first_time` stages begin in order, then `second` ones, and `slots` run at once.
+int64_t launch_time(int64_t first, int64_t first_time, int64_t second, int64_t second_time, int64_t slots)
+{
+    // the second kind finds `late` slots that are free one round of the first after the others
+    const int64_t begin = first / slots * first_time, late = first % slots;
+    int64_t early_rounds = std::max<int64_t>(0, second / slots - first_time / second_time - 2), late_rounds = early_rounds;
+    while ((slots - late) * early_rounds + late * late_rounds < second) {
+        if (begin + early_rounds * second_time <= begin + first_time + late_rounds * second_time) ++early_rounds;
+        else ++late_rounds;
+    }
+    return std::max(begin + early_rounds * second_time, late ? begin + first_time + late_rounds * second_time : 0);
 }
 
 // Large tiles of scores: where a tile's products take longer than its exponentials, which nothing else runs beside there, and where there are
@@ -1180,23 +1194,29 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
         const int64_t most = std::max<int64_t>(256, static_cast<int64_t>(kGBytes) / row_bytes / 256 * 256);
         const int64_t pieces = round_up(num_rows, 256) * row_bytes <= static_cast<int64_t>(kGBytesAtOnce) ? 1 : ceil_div(num_rows, most);
         w.piece = round_up(ceil_div(num_rows, pieces), 256);
-        // contractions are split so that all workgroups of a launch have about as many stages, and the machine is full
         auto split = [&](bool large) {
             const int64_t edge = large ? 256 : 128;
             const int64_t cols = ceil_div(dim, edge), h_tiles = ceil_div(w.tokens, edge) * cols, w_tiles = ceil_div(w.piece, edge) * cols;
+            const int64_t h_stages = w.piece / step, w_stages = w.tokens / step;
             w.large_products = large;
-            w.h_stages = static_cast<uint32_t>(w.piece / step);
-            w.w_stages = static_cast<uint32_t>(w.tokens / step);
-            const int64_t share = std::max<int64_t>(8, ceil_div(h_tiles * w.h_stages + w_tiles * w.w_stages, slots_of(large)));
-            w.h_splits = static_cast<uint32_t>(ceil_div(w.h_stages, share));
-            w.w_splits = static_cast<uint32_t>(ceil_div(w.w_stages, share));
-            w.h_share = static_cast<uint32_t>(ceil_div(w.h_stages, w.h_splits));
-            w.w_share = static_cast<uint32_t>(ceil_div(w.w_stages, w.w_splits));
+            w.w_stages = static_cast<uint32_t>(w_stages);
+            const int64_t even = std::max<int64_t>(kLeastShare, ceil_div(h_tiles * h_stages + w_tiles * w_stages, slots_of(large)));
+            int64_t best = INT64_MAX;
+            for (int64_t share = even; share <= 2 * even; share += ceil_div(even, 32)) {
+                const int64_t hs = ceil_div(h_stages, share), ws = ceil_div(w_stages, share);
+                const int64_t time = launch_time(h_tiles * hs, ceil_div(h_stages, hs) + kTileCost, w_tiles * ws, ceil_div(w_stages, ws) + kTileCost, slots_of(large));
+                if (time >= best) continue;
+                best = time;
+                w.h_splits = static_cast<uint32_t>(hs);
+                w.w_splits = static_cast<uint32_t>(ws);
+                w.w_share = static_cast<uint32_t>(ceil_div(w_stages, ws));
+            }
         };
-        // Large tiles of products (bf16, of more than 128 columns, with stages enough for a workgroup that is alone on its CU): where dW needs no partial sums with them, or has columns enough that these are
-        // worth it (2048 x 100 000 x 512: 778 us, 906 with small tiles; 4096 x 100 000 x 256, two partial sums: 1056 and 971).
+        // Large tiles of products (bf16, of more than 128 columns): where dW needs no partial sums with them, or where they have few more columns
+        // than small tiles (4096 x 50 000, gradients: of 640 columns 1070 us, small tiles 1118; of 300, which become 512: 768 and 641; 6000 x 30 000
+        // x 200: 386 and 440; 1024 x 50 000 x 384, no partial sums: 182 and 205).
         split(w.parts == 1 && dim > 128 && n >= 256);
-        if (w.large_products && w.w_splits > 1 && dim < 384) split(false);
+        if (w.large_products && w.w_splits > 1 && round_up(dim, 256) * 5 > round_up(dim, 128) * 6) split(false);
         for (int p = 0; p < w.parts; ++p) {
             w.hc[p] = w.parts == 2 ? take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded) : nullptr;
             w.g[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.piece);
@@ -1329,7 +1349,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     const uint32_t token_tiles = static_cast<uint32_t>(ceil_div(w.tokens, side));
     pa.dh = w.dh; pa.dw = w.dw; pa.tokens = static_cast<uint32_t>(w.tokens); pa.piece_rows = static_cast<uint32_t>(w.piece);
     pa.cols = static_cast<uint32_t>(w.cols); pa.col_tiles = static_cast<uint32_t>(ceil_div(x.dim, edge));
-    pa.h_splits = w.h_splits; pa.w_splits = w.w_splits; pa.h_share = w.h_share; pa.w_share = w.w_share;
+    pa.h_splits = w.h_splits; pa.w_splits = w.w_splits; pa.w_share = w.w_share;
     pa.w_stages = w.w_stages;
     pa.out_stride = dw_stride; pa.dim = x.dim; pa.scale = scale; pa.shift = w.shift + (x.c ? 2 : 1);
     auto reduce = [&](ReduceArgs r) {
@@ -1362,6 +1382,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         pa.h_tiles = dh ? static_cast<uint32_t>(ceil_div(w.tokens, edge)) : 0;
         pa.w_tiles = dw ? static_cast<uint32_t>(ceil_div(rows, edge)) : 0;
         pa.h_stages = static_cast<uint32_t>(ceil_div(rows, step_of<P>()));      // (no stage begins beyond the last row)
+        pa.h_share = static_cast<uint32_t>(ceil_div(pa.h_stages, w.h_splits));
         pa.add = base > 0;
         pa.rows = static_cast<uint32_t>(rows);
         pa.out = dw ? static_cast<T*>(dw) + base * dw_stride : nullptr;
