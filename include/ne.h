@@ -337,8 +337,8 @@ ne_status ne_embed_lookup(const void* table_dev, int32_t table_type, int64_t tab
 
 /*
  * The lookup's gradient:  T[r] = (accumulate ? T[r] : 0) + scale * sum over i with ids[i] == r of grad[i].
- * The ids are sorted (stably, so that a row's terms are added in an order that only the ids decide) and each row
- * is written once: the result is the same bit for bit on every run.  Ids outside [0, num_rows) contribute nothing,
+ * The ids are sorted (stably, so that a row's terms are added in an order that only the ids decide) and each row's
+ * sum is rounded once: the result is the same bit for bit on every run.  Ids outside [0, num_rows) contribute nothing,
  * whatever their gradient holds.  accumulate == 0 writes all num_rows rows; accumulate != 0 touches only rows that
  * are named.
  *   grad_dev       : device, grad_type [n][dim], row stride grad_stride >= dim, or 0 for one row that every
@@ -371,10 +371,11 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  *   scale         : finite; 1 / n for the mean over the rows.
  *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
  *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 1) bytes.
- * Precision: NE_BF16: products of bf16 values with fp32 sums; loss_grad[i] (exp(s - lse) - [v == target]) is formed in
- * fp32 and rounded to bf16 for its products; scale is applied in fp32.  NE_F32: every operand is the sum of two halves in fp16 (22 bits, at a common power of two that the
- * largest finite magnitude sets), three products of halves with fp32 sums: errors as those of fp32 products, for
- * elements of at least 2^-24 of the largest magnitude of their matrix; what is smaller counts to 2^-39 of it.
+ * Precision.  NE_BF16: products of bf16 values with fp32 sums; loss_grad[i] (exp(s - lse) - [v == target]) is formed
+ * in fp32 and rounded to bf16 for its products; scale is applied in fp32.  NE_F32: every operand is the sum of two
+ * halves in fp16 (22 bits, at a common power of two that the largest finite magnitude sets), three products of halves
+ * with fp32 sums: errors as those of fp32 products, for elements of at least 2^-24 of the largest magnitude of their
+ * matrix; what is smaller counts to 2^-39 of it.
  * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN; in a row of w, all losses.
  *   1 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for the loss and writes zeros
  *   to dw.  Errors: NE_ERR_ARG, NE_ERR_HIP.
@@ -394,12 +395,11 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
  * Parameters are fp32.  state_bits 32: m and v are float[n].  state_bits 8: every 256 elements of a tensor share
  * two scales (float, ceil(n / 256) each); m is 8-bit floating point (e4m3, no infinities) times m_scale, and v holds
- * sqrt(v) in the same form times v_scale; a scale is the block's largest magnitude
- * (2^-100 at least) times 1/448, and what is rounded are the values times (1/largest) * 448, each operation rounded to fp32.
- * Values are rounded at random, up with the probability that keeps their expectation (a step moves v by a
- * thousandth, which rounding to nearest at 3 bits would lose every time); sqrt(v) > 0 never becomes 0.  The random
- * bits of element e of tensor t: word e % 4 of Philox(key = seed, counter = (e / 4, t, step, 3)), its low 16 bits
- * for m and its high 16 bits for v.
+ * sqrt(v) in the same form times v_scale; a scale is the block's largest magnitude (2^-100 at least) times 1/448, and
+ * what is rounded are the values times (1/largest) * 448, each operation rounded to fp32.  Values are rounded at
+ * random, up with the probability that keeps their expectation (a step moves v by a thousandth, which rounding to
+ * nearest at 3 bits would lose every time); sqrt(v) > 0 never becomes 0.  The random bits of element e of tensor t:
+ * word e % 4 of Philox(key = seed, counter = (e / 4, t, step, 3)), its low 16 bits for m and its high 16 bits for v.
  *   ne_adamw_tensor: n > 0 elements, n < 2^33; param float[n]; grad of grad_type; param_bf16 NULL or bf16[n], which
  *   receives a rounded copy of the new parameters; m_scale and v_scale are only used with state_bits 8.  All are
  *   device memory of the caller, aligned to their elements, that stays valid while the handle is used.

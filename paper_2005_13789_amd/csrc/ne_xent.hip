@@ -4,17 +4,25 @@
 //     G_iv = exp(S_iv - lse_i) - [v = target_i],   dH_i = scale c_i (G . W)_i,   dW = scale G^T . (c H)
 // (bf16: c_i is in G, which is rounded once; scale, the same for all, is applied in fp32 to the sums)
 //
-// Everything is a matrix product with something small around it, so one tile loop on the matrix cores serves all
-// three products; they differ in where their operands lie and in what becomes of the sums:
+// Everything is a matrix product with something small around it, so the same loads to LDS, operand reads and matrix
+// instructions serve all three products; they differ in where their operands lie and in what becomes of the sums:
 //   scores   every lane of a tile's sums belongs to one row of H (table rows run along the registers), so the running
 //            maximum and sum of a row's softmax are two registers, joined between lanes once at the end.
 //   gradient the same product again for a piece of the table, whose G is written to the workspace (sized to stay in
 //            the 256 MB of last-level cache), then dH += G . W_piece and dW_piece = G^T . H in one launch.
-// The scores are computed twice (8 n V d operations in training, where 6 would do with all scores kept).
+// The scores are computed twice (8 n V d operations in training, where 6 would do with all scores kept: n V of them,
+// 6.6 GB in fp32 at the sizes below, written once and read twice).
+// For few rows of H the loss is bound by reading the table, which then streams through registers (few_rows_kernel).
 //
 // Types: bf16 operands go to the matrix cores as they are.  fp32 operands are split into two fp16 halves at a common
 // power of two, x 2^k = hi + lo with 22 bits, and a product is hi hi + hi lo + lo hi: the error of an fp32 product at
-// three matrix instructions, where the fp32 matrix instructions take 16 times as long as one.
+// three matrix instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
+//
+// Bound by the matrix cores and by the loads from L2 that feed them.  Measured, 8192 rows, 200 003 of 512, bf16: loss
+// 1.7 to 1.8 ms (950 TF; a copy of the kernel without loads took 0.87 of the time, without exponentials 0.90, without
+// products 0.87: none of them hides the others completely), gradients of a piece of 8192 table rows 87 us for G and
+// 130 to 136 for both products (1.03 PF), 7.0 to 7.4 ms in all.
+// 4096 rows, 10 000 of 128, fp32: scores 40 us, G 55, products 72, and 35 us for the small launches around them.
 //
 // Operands in LDS are 16-byte pieces placed so that reads are free of bank conflicts (an XOR of the piece's
 // index with the row's); they come from memory straight to LDS, 16 bytes a lane, and the XOR is applied to the
@@ -42,8 +50,10 @@ constexpr int64_t kMostStride = 1 << 22;   // elements: a tile's 256 rows are wi
 constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
 constexpr int kFewBytes = 65536;
 constexpr int kFewGroups = 1024;
-constexpr size_t kGBytes = size_t{128} << 20, kGBytesAtOnce = size_t{192} << 20;      // G of one piece; of all, where there is only one
-constexpr int kLeastShare = 8, kTileCost = 1;    // stages: the fewest of a product's workgroup; what beginning and writing a tile take
+// Bytes of G of one piece: at most, those from which on smaller pieces are not looked at, those that stay in the last-level cache beside the
+// table and the sums, and what is written or read of these in a stage's time.
+constexpr int64_t kGBytes = 512 << 20, kGLeast = 64 << 20, kGCached = 256 << 20, kStageBytes = 8 << 20;
+constexpr int kLeastShare = 8, kTileCost = 1, kLaunchCost = 10;   // stages: the fewest of a product's workgroup; what beginning and writing a tile, and a launch, take
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
 
@@ -260,7 +270,8 @@ __device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks)
     return xcd * per + min(xcd, more) + (block >> 3);
 }
 
-// Number b of tiles_a x tiles_b pairs, eight of a against one of b after the other: the 64 workgroups of an XCD have 16 operands.
+// Number b of tiles_a x tiles_b pairs, eight of a against one of b after the other: neighbours share their operands with one another, and with
+// by_xcd in one L2 (all scores of 8192 x 200 003 x 512: 1.97 ms in plain order, 1.79 so).
 __device__ __forceinline__ void pair_of(uint32_t b, uint32_t tiles_a, uint32_t tiles_b, uint32_t& ta, uint32_t& tb)
 {
     const uint32_t group = b / (8 * tiles_b), rest = b - group * 8 * tiles_b, size = min(8u, tiles_a - group * 8);
@@ -335,6 +346,7 @@ __device__ __forceinline__ void for_eights(const T* in, int64_t stride, int64_t 
         }
 }
 
+// (Bound by memory: 84 284 rows of 452, 152 MB: 29 us, 5.2 TB/s.  A small table's 5 us are a launch.)
 __global__ void __launch_bounds__(kThreads) amax_kernel(AmaxArgs a)
 {
     __shared__ float lds[4];
@@ -370,6 +382,7 @@ __device__ __forceinline__ int shift_of(float amax)
     return 13 - (max(e, 1) - 127);
 }
 
+// (Bound by memory: 84 284 rows of 452 fp32, 312 MB read and written: 57 us, 5.5 TB/s.)
 struct PackArgs {
     const void* in;
     int64_t in_stride, rows, padded_rows;
@@ -490,7 +503,8 @@ __device__ __forceinline__ void score_tiles(const Operand& w, const Operand& h, 
 }
 
 // The same with small tiles where H's rows have at most KS stages: a wavefront holds its 64 rows of H in registers, as the operands that they
-// are, and only the table travels, in a ring of four stages, three of them ahead.  (Loads from L2 are what bounds these shapes.)
+// are, and only the table travels, in a ring of four stages, three of them ahead.  (Loads from L2 are what bounds these shapes: 10 007 rows
+// against 10 000 of 100, fp32: 94 us, 5 more with H through LDS; a copy without the exponentials took 73, without loads 87.)
 template <int P, int KS, class Epilogue>
 __device__ __forceinline__ void score_tiles_held(const Operand& w, const Operand& h, uint32_t token_tile, uint32_t first, uint32_t tile0, uint32_t tile1, int steps,
                                                  unsigned char* lds, Epilogue epilogue)
@@ -683,7 +697,8 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(const float2* stat,
 // ---------------------------------------------------------------------------------------------
 // few rows of H: the table streams through registers once, straight from memory
 // ---------------------------------------------------------------------------------------------
-// Bound by reading the table.  A wavefront has 16 table rows at a time, whose elements go from memory to the matrix cores' first
+// Bound by reading the table (one row against 200 003 of 256 bf16: 19.5 us, 5.2 TB/s; 23.6 with the launch that joins the workgroups'
+// shares).  A wavefront has 16 table rows at a time, whose elements go from memory to the matrix cores' first
 // operand as they lie (lane l: row l % 16, eight elements from (l / 16) * 8 on of every 32); H lies in LDS as second operands, in blocks
 // of 16 rows.  fp32 operands are split into three bf16 parts (24 bits, no common scale to be found first: that would read the
 // table twice), of whose nine products the six largest are taken.
@@ -816,6 +831,9 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(FewArgs a)
 // ---------------------------------------------------------------------------------------------
 // G of a piece of the table
 // ---------------------------------------------------------------------------------------------
+// The scores again, with the exponentials written as operands of the next products instead of added up: bf16, of values at most 1 whose errors
+// of 2^-9 average out over the products' sums, or two fp16 halves of G 2^14, which keep 22 bits of 2^-14 and more.  8192 x 8192 x 512 bf16: 87 us (0.79 PF,
+// 134 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
 struct CoefArgs {
     Operand w, h;                  // both by rows
     const int32_t* targets;
@@ -936,6 +954,8 @@ struct ProductArgs {
     const int32_t* shift;          // fp32 only: power of two of the rows of H
 };
 
+// Both products of a piece are one launch: either alone leaves places empty.  (8192 x 8192 x 512 bf16, large tiles: 130 us, 1.05 PF; 4096 x 10 000 x
+// 128 fp32, small tiles: 72 us, 0.87 PF of half products.)
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
 template <int P, int W, bool GROWS>
 __device__ __forceinline__ void product_tile(const Operand& cols, const Operand& g, uint32_t col0, uint32_t row0, uint32_t s0, uint32_t s1,
@@ -1028,7 +1048,7 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     }
 }
 
-// Sums the splits and rounds once.  dH: rows without a target become zeros, the others take their factor.
+// Sums the splits and rounds once: 2 x 8192 x 512, 42 MB: 7.7 us.  dH: rows without a target become zeros, the others take their factor.
 struct ReduceArgs {
     const float* in;               // [splits][rows_in][cols]
     int64_t split_stride;
@@ -1156,6 +1176,60 @@ bool large_scores(int64_t n, int64_t num_rows, int32_t dim, int parts)
     return parts == 1 && dim >= 384 && ceil_div(n, 256) * ceil_div(num_rows, 256) >= 1024;
 }
 
+// Splits the contractions of a piece's two products, which are one launch of two kinds of workgroups, into shares of about the same length, as many
+// as fill the machine; of these shares the one with which the launch is over first, as a workgroup too many takes a whole round more (1500 x
+// 100 003 x 200 bf16: 257 workgroups 97 us a piece, 251 longer ones 66).  Returns its time in stages of small tiles.
+int64_t split_products(XentWs& w, int32_t dim, bool large)
+{
+    const int64_t edge = large ? 256 : 128, step = w.parts == 1 ? step_of<1>() : step_of<2>();
+    const int64_t cols = ceil_div(dim, edge), h_tiles = ceil_div(w.tokens, edge) * cols, w_tiles = ceil_div(w.piece, edge) * cols;
+    const int64_t h_stages = w.piece / step, w_stages = w.tokens / step;
+    w.large_products = large;
+    w.w_stages = static_cast<uint32_t>(w_stages);
+    const int64_t even = std::max<int64_t>(kLeastShare, ceil_div(h_tiles * h_stages + w_tiles * w_stages, slots_of(large)));
+    int64_t best = INT64_MAX;
+    for (int64_t share = even; share <= 2 * even; share += ceil_div(even, 32)) {
+        const int64_t hs = ceil_div(h_stages, share), ws = ceil_div(w_stages, share);
+        const int64_t time = launch_time(h_tiles * hs, ceil_div(h_stages, hs) + kTileCost, w_tiles * ws, ceil_div(w_stages, ws) + kTileCost, slots_of(large));
+        if (time >= best) continue;
+        best = time;
+        w.h_splits = static_cast<uint32_t>(hs);
+        w.w_splits = static_cast<uint32_t>(ws);
+        w.w_share = static_cast<uint32_t>(ceil_div(w_stages, ws));
+    }
+    return large ? 2 * best : best;
+}
+
+// The pieces of the table: large ones mean few launches, some sizes fill the machine and others just miss it, and G of a small one stays in the
+// last-level cache, which narrow tables need, whose products are over faster than G is read.  Of up to seventeen numbers of pieces the
+// one whose launches take the least time, by their stages and by G's bytes.  (Gradients, us, and with pieces of always 128 MB: 8192 x 200 003 x
+// 512 bf16 5220 and 5580, 4096 x 100 000 x 256 795 and 910, 8192 x 100 000 x 128 fp32 2595 and 3100, 1000 x 500 000 x 128 bf16 833 and 818,
+// x 64 680 and 625: the estimate is not always right.)
+void choose_pieces(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
+{
+    const int64_t row_tiles = ceil_div(num_rows, 256), bytes = row_tiles * 256 * 2 * w.parts * w.tokens;
+    const int64_t side = w.large_scores ? 256 : 128, steps = w.padded / (w.parts == 1 ? step_of<1>() : step_of<2>());
+    const int64_t fewest = std::min<int64_t>(ceil_div(bytes, kGBytes), row_tiles);
+    int64_t best = INT64_MAX;
+    XentWs chosen = w;
+    for (int64_t pieces = fewest; pieces <= 5 * fewest && pieces <= row_tiles && pieces * kGLeast <= bytes + kGLeast; pieces += ceil_div(fewest, 4)) {
+        w.piece = ceil_div(row_tiles, pieces) * 256;
+        // Large tiles of products (bf16, of more than 128 columns): where dW needs no partial sums with them, or where they have few more columns
+        // than small tiles (4096 x 50 000, gradients: of 640 columns 1070 us, small tiles 1118; of 300, which become 512: 768 and 641; 6000 x 30 000
+        // x 200: 386 and 440; 1024 x 50 000 x 384, no partial sums: 182 and 205).
+        int64_t time = split_products(w, dim, w.parts == 1 && dim > 128 && n >= 256);
+        if (w.large_products && w.w_splits > 1 && round_up(dim, 256) * 5 > round_up(dim, 128) * 6) time = split_products(w, dim, false);
+        const int64_t g_tiles = ceil_div(w.piece, side), g_splits = splits_of(g_tiles, ceil_div(w.tokens, side), w.large_scores);
+        const int64_t g_bytes = w.piece * 2 * w.parts * w.tokens, g_time = g_bytes / (g_bytes <= kGCached ? kStageBytes : kStageBytes / 2);
+        time = std::max(time, 2 * g_time) + std::max(ceil_div(g_tiles, g_splits) * steps * (w.large_scores ? 2 : 1), g_time) + 2 * kLaunchCost;
+        time *= ceil_div(num_rows, w.piece);
+        if (time >= best) continue;
+        best = time;
+        chosen = w;
+    }
+    w = chosen;
+}
+
 // The workspace has room for packed copies whether or not this call's alignment needs them.
 XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad, char* base)
 {
@@ -1190,33 +1264,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * w.tokens);
         w.target_score = take.get<float>(static_cast<size_t>(w.tokens));
     } else {
-        const int64_t row_bytes = 2 * w.parts * w.tokens;       // G of one row of the table
-        const int64_t most = std::max<int64_t>(256, static_cast<int64_t>(kGBytes) / row_bytes / 256 * 256);
-        const int64_t pieces = round_up(num_rows, 256) * row_bytes <= static_cast<int64_t>(kGBytesAtOnce) ? 1 : ceil_div(num_rows, most);
-        w.piece = round_up(ceil_div(num_rows, pieces), 256);
-        auto split = [&](bool large) {
-            const int64_t edge = large ? 256 : 128;
-            const int64_t cols = ceil_div(dim, edge), h_tiles = ceil_div(w.tokens, edge) * cols, w_tiles = ceil_div(w.piece, edge) * cols;
-            const int64_t h_stages = w.piece / step, w_stages = w.tokens / step;
-            w.large_products = large;
-            w.w_stages = static_cast<uint32_t>(w_stages);
-            const int64_t even = std::max<int64_t>(kLeastShare, ceil_div(h_tiles * h_stages + w_tiles * w_stages, slots_of(large)));
-            int64_t best = INT64_MAX;
-            for (int64_t share = even; share <= 2 * even; share += ceil_div(even, 32)) {
-                const int64_t hs = ceil_div(h_stages, share), ws = ceil_div(w_stages, share);
-                const int64_t time = launch_time(h_tiles * hs, ceil_div(h_stages, hs) + kTileCost, w_tiles * ws, ceil_div(w_stages, ws) + kTileCost, slots_of(large));
-                if (time >= best) continue;
-                best = time;
-                w.h_splits = static_cast<uint32_t>(hs);
-                w.w_splits = static_cast<uint32_t>(ws);
-                w.w_share = static_cast<uint32_t>(ceil_div(w_stages, ws));
-            }
-        };
-        // Large tiles of products (bf16, of more than 128 columns): where dW needs no partial sums with them, or where they have few more columns
-        // than small tiles (4096 x 50 000, gradients: of 640 columns 1070 us, small tiles 1118; of 300, which become 512: 768 and 641; 6000 x 30 000
-        // x 200: 386 and 440; 1024 x 50 000 x 384, no partial sums: 182 and 205).
-        split(w.parts == 1 && dim > 128 && n >= 256);
-        if (w.large_products && w.w_splits > 1 && round_up(dim, 256) * 5 > round_up(dim, 128) * 6) split(false);
+        choose_pieces(w, n, num_rows, dim);
         for (int p = 0; p < w.parts; ++p) {
             w.hc[p] = w.parts == 2 ? take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded) : nullptr;
             w.g[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.piece);

@@ -49,7 +49,8 @@ class SoftmaxTrainer:
         self.opt = ne.ne_create_adamw(self.tables, self.grads, *states, opt_work, weight_decay=weight_decay, params_bf16=copies, seed=seed, **kw)
 
     def step(self, pairs: torch.Tensor, lr: float) -> torch.Tensor:
-        """One step of the mean loss of pairs int32 [n][2] (CUDA, n <= batch; a pair whose ctx is outside the tables does not count).  Returns the pairs' losses before the step (a view that the next step overwrites)."""
+        """One step of the mean loss of pairs int32 [n][2] (CUDA, n <= batch; a pair whose ctx is outside the tables does
+        not count).  Returns the pairs' losses before the step (a view that the next step overwrites)."""
         n = int(pairs.shape[0])
         if n < 1 or n > self.batch:
             raise ValueError(f"a step takes 1 to {self.batch} pairs")
