@@ -253,6 +253,13 @@ def test_larger_shapes(dtype, n, V, d):
         assert float((got.double() - ref).norm() / ref.norm()) <= bar, float((got.double() - ref).norm() / ref.norm())
 
 
+@pytest.mark.parametrize("dtype,n,V,d", [(torch.bfloat16, 3000, 130000, 64), (torch.float32, 5000, 40000, 40), (torch.bfloat16, 4136, 100000, 300),
+                                         (torch.bfloat16, 40, 4300000, 8), (torch.float32, 20, 4300000, 8), (torch.bfloat16, 100, 3000000, 16)])
+def test_pieces_and_long_rows(dtype, n, V, d):
+    """Coefficients that take several pieces of the table, and pieces of which one row of H has millions: bounds as above."""
+    test_larger_shapes(dtype, n, V, d)
+
+
 def test_no_rows():
     w = torch.randn(50, 16, device=DEV)
     empty = torch.empty(0, 16, device=DEV)
