@@ -1148,11 +1148,21 @@ bool xent_sizes_ok(int64_t n, int64_t num_rows, int32_t dim, int32_t type)
     return n >= 0 && n <= (1 << 24) && num_rows > 0 && num_rows < (1ll << 31) && dim >= 1 && dim <= NE_OP_MAX_DIM && type_ok(type);
 }
 
-// Workgroups over table tiles for one tile of H: as many as fill the machine, all with about as many tiles.
+// Workgroups over table tiles for one tile of H, all with about as many tiles: as many as fill the machine once, or up to four times over where
+// that ends sooner, and a workgroup's beginning counts as half a tile (bf16 losses of 38 400 rows against 20 000 of 128, 300 tiles of H for 512
+// places: 460 us with one workgroup each, 298 with five).
 uint32_t splits_of(int64_t row_tiles, int64_t token_tiles, bool large)
 {
-    const int64_t slots = slots_of(large), most = std::max<int64_t>(1, std::min<int64_t>(row_tiles, slots / std::min<int64_t>(token_tiles, slots)));
-    return static_cast<uint32_t>(ceil_div(row_tiles, ceil_div(row_tiles, most)));
+    const int64_t slots = slots_of(large);
+    int64_t best = INT64_MAX, splits = 1;
+    for (int64_t rounds = 1; rounds <= 4; ++rounds) {
+        const int64_t most = std::max<int64_t>(1, std::min(row_tiles, rounds * slots / token_tiles)), per = ceil_div(row_tiles, most), s = ceil_div(row_tiles, per);
+        const int64_t time = ceil_div(s * token_tiles, slots) * (2 * per + 1);
+        if (time >= best) continue;
+        best = time;
+        splits = s;
+    }
+    return static_cast<uint32_t>(splits);
 }
 
 // When a launch ends, in stages: `first` workgroups of `first_time` stages begin in order, then `second` ones, and `slots` run at once.

@@ -260,6 +260,12 @@ def test_pieces_and_long_rows(dtype, n, V, d):
     test_larger_shapes(dtype, n, V, d)
 
 
+@pytest.mark.parametrize("dtype,n,V,d", [(torch.bfloat16, 38400, 3000, 64), (torch.float32, 40000, 2000, 40), (torch.bfloat16, 20000, 5000, 400)])
+def test_many_rows(dtype, n, V, d):
+    """More tiles of rows than places for workgroups, or about as many: bounds as above."""
+    test_larger_shapes(dtype, n, V, d)
+
+
 def test_no_rows():
     w = torch.randn(50, 16, device=DEV)
     empty = torch.empty(0, 16, device=DEV)
