@@ -36,7 +36,9 @@ constexpr int kRowsPerGroup = 64;   // table rows of a workgroup of the rows lau
 constexpr int kFewIds = 16384;      // up to so many ids every workgroup looks through all of them
 constexpr int kScan = 16;           // ids of a thread and round there
 constexpr int kMostSlots = 256;     // rows of a workgroup there
-constexpr int kAddIds = 32;         // accumulate: positions of a workgroup there ...
+constexpr int kFewWide = 6800;      // up to so many their slots are kept in LDS, too (4096: 7.2 us, 8.3 if ids are read again)
+constexpr int kFewLds = 43000;      // bytes for what is found with which three workgroups have place on a CU, twice as many ids two
+constexpr int kAddIds = 32;         // accumulate: positions of a workgroup there, at most ...
 constexpr int kAddPlaces = 128;     // ... places of the hash table that finds their rows
 constexpr int kAddFilter = 1024;    // ... and words of the filter before it: a bit for each hash of 15 bits
 
@@ -604,30 +606,39 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(GradArgs a)
 // rows, or with ADD the rows that 32 positions are the first to name.  What it finds lies in LDS in the order of the positions and is
 // sorted there by row (stably), so the order of a row's terms is that of the sorting path.
 // Bound by the chain of a launch, the ids, the found rows' gradients and the store, each of which waits for memory once (4096 ids, 10 000
-// rows of 128 fp32: 8.5 us), and with more ids by the looking (10 007 ids, ADD: 16 us; one bit for each hash is looked up first, since most
-// ids of most workgroups are then done with).
+// rows of 128 fp32: 8.5 us), and with more ids by the looking (10 007 ids, ADD: 14 us; one bit for each hash is looked up first, since most
+// ids of most workgroups are then done with).  LDS for as many found positions as there are ids bounds the workgroups of a CU, so it is
+// kept small (16 384 ids, ADD: 17 us, 29 with 6 bytes for each; without ADD into 10 000 rows 13 and 20).
 struct FewArgs {
     GradArgs g;
     const int32_t* ids;
-    uint32_t slots;            // rows of a workgroup; a power of two
+    uint32_t slots;            // rows of a workgroup, ADD: positions; a power of two
     int32_t slot_bits;
+    int32_t wide;              // what is found is kept with its slot; otherwise (less LDS) its id is read and looked up again
 };
+
+// Words of what is found, at most all n positions.
+__host__ __device__ __forceinline__ uint32_t few_found(uint32_t n, bool wide) { return wide ? n : (n + 1) / 2; }
 
 template <class TG, class TT, int V, bool ADD>
 __global__ void __launch_bounds__(kThreads) few_ids_kernel(FewArgs f)
 {
-    extern __shared__ uint32_t found[];        // [n rounded up]  slot << 16 | position; behind them [n] positions by slot (16 bits)
-    __shared__ float lds[kThreads][V];
+    extern __shared__ uint32_t found[];        // [n]  slot << 16 | position, or positions of 16 bits; behind them [n] positions by slot (16 bits)
+    __shared__ union {
+        uint32_t count[kThreads / 64][kMostSlots];      // while sorting
+        float sums[kThreads][V];                        // afterwards
+    } lds;
     __shared__ RowLists lists;
-    __shared__ uint32_t count[kThreads / 64][kMostSlots], wave_sums[kThreads / 64];
+    __shared__ uint32_t wave_sums[kThreads / 64];
     __shared__ uint32_t start[kMostSlots + 1];
     // ADD: the ids of the places and the slots that they have, the slots' ids, and whether an earlier workgroup has them
     __shared__ uint32_t place_id[ADD ? kAddPlaces : 1], owner[ADD ? kAddIds : 1], taken[ADD ? kAddIds : 1], slots_used;
     __shared__ uint8_t place_slot[ADD ? kAddPlaces : 1];
     __shared__ uint32_t filter[ADD ? kAddFilter : 1];
     const GradArgs& a = f.g;
-    uint16_t* sorted = reinterpret_cast<uint16_t*>(found + ((a.n + 1) & ~1u));
-    const uint32_t first = ADD ? blockIdx.x * kAddIds : blockIdx.x * f.slots;
+    uint16_t* found16 = reinterpret_cast<uint16_t*>(found);
+    uint16_t* sorted = found16 + few_found(a.n, f.wide) * 2;
+    const uint32_t first = blockIdx.x * f.slots;
     const int wave = threadIdx.x >> 6, lane64 = threadIdx.x & 63;
     if (ADD) {
         for (uint32_t i = threadIdx.x; i < kAddPlaces; i += kThreads) place_id[i] = 0xFFFFFFFFu;
@@ -635,7 +646,7 @@ __global__ void __launch_bounds__(kThreads) few_ids_kernel(FewArgs f)
         if (threadIdx.x < kAddIds) taken[threadIdx.x] = 0;
         if (threadIdx.x == 0) slots_used = 0;
         __syncthreads();
-        if (threadIdx.x < kAddIds && first + threadIdx.x < a.n) {
+        if (threadIdx.x < f.slots && first + threadIdx.x < a.n) {
             const uint32_t id = static_cast<uint32_t>(f.ids[first + threadIdx.x]);
             if (id < a.num_rows)
                 for (uint32_t at = hash_position(id, kAddPlaces - 1);; at = (at + 1) & (kAddPlaces - 1)) {
@@ -683,49 +694,60 @@ __global__ void __launch_bounds__(kThreads) few_ids_kernel(FewArgs f)
         uint32_t to = have + block_prefix<kThreads>(__popc(wanted), wave_sums, &total);
 #pragma unroll
         for (int q = 0; q < kScan; ++q)
-            if (wanted >> q & 1) found[to++] = (ADD ? 0 : (id[q] - first) << 16) | (at + q);
+            if (wanted >> q & 1) {
+                if (f.wide) found[to++] = (ADD ? 0 : (id[q] - first) << 16) | (at + q);
+                else found16[to++] = static_cast<uint16_t>(at + q);
+            }
         have += total;
         __syncthreads();
     }
-    if (ADD) {      // what passed the filter is looked up; slot kAddIds takes what has no row here, or stands before all of this workgroup's
-        for (uint32_t i = threadIdx.x; i < have; i += kThreads) {
-            const uint32_t k = found[i], id = static_cast<uint32_t>(f.ids[k]);
-            uint32_t slot = kAddIds;
-            for (uint32_t at = hash_position(id, kAddPlaces - 1);; at = (at + 1) & (kAddPlaces - 1)) {
-                const uint32_t o = place_id[at];
-                if (o == id) slot = place_slot[at];
-                if (o == id || o == 0xFFFFFFFFu) break;
-            }
-            if (k < first && slot != kAddIds) {
-                taken[slot] = 1;
-                slot = kAddIds;
-            }
-            found[i] = slot << 16 | k;
+    // ADD: what passed the filter is looked up; slot kAddIds takes what has no row here, or stands before all of this workgroup's
+    auto look_up = [&](uint32_t k) -> uint32_t {
+        const uint32_t id = static_cast<uint32_t>(f.ids[k]);
+        if (!ADD) return id - first;
+        for (uint32_t at = hash_position(id, kAddPlaces - 1);; at = (at + 1) & (kAddPlaces - 1)) {
+            const uint32_t o = place_id[at];
+            if (o == 0xFFFFFFFFu) return kAddIds;
+            if (o != id) continue;
+            const uint32_t slot = place_slot[at];
+            if (k >= first) return slot;
+            taken[slot] = 1;
+            return kAddIds;
         }
+    };
+    if (ADD && f.wide) {
+        for (uint32_t i = threadIdx.x; i < have; i += kThreads) found[i] |= look_up(found[i]) << 16;
         __syncthreads();
     }
+    auto entry = [&](uint32_t i) -> uint32_t { return f.wide ? found[i] : look_up(found16[i]) << 16 | found16[i]; };
     // stable sort by slot: counts of every wavefront's share, then places
     const uint32_t share = (have + kThreads - 1) / kThreads * 64;      // entries of a wavefront, side by side
     for (uint32_t i = threadIdx.x; i < kMostSlots; i += kThreads)
 #pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w) count[w][i] = 0;
+        for (int w = 0; w < kThreads / 64; ++w) lds.count[w][i] = 0;
     __syncthreads();
-    for (uint32_t i = wave * share + lane64; i < min((wave + 1) * share, have); i += 64) atomicAdd(&count[wave][found[i] >> 16], 1u);
+    uint32_t first_entry = 0;
+    for (uint32_t i0 = wave * share; i0 < min((wave + 1) * share, have); i0 += 64) {
+        if (i0 + lane64 >= min((wave + 1) * share, have)) continue;
+        const uint32_t e = entry(i0 + lane64);
+        if (i0 == wave * share) first_entry = e;
+        atomicAdd(&lds.count[wave][e >> 16], 1u);
+    }
     __syncthreads();
     {
         const bool has_slot = threadIdx.x < kMostSlots;
         uint32_t sum = 0, total;
         if (has_slot)
 #pragma unroll
-            for (int w = 0; w < kThreads / 64; ++w) sum += count[w][threadIdx.x];
+            for (int w = 0; w < kThreads / 64; ++w) sum += lds.count[w][threadIdx.x];
         uint32_t at = block_prefix<kThreads>(sum, wave_sums, &total);
         if (threadIdx.x == 0) start[kMostSlots] = total;
         if (has_slot) {
             start[threadIdx.x] = at;
 #pragma unroll
             for (int w = 0; w < kThreads / 64; ++w) {
-                const uint32_t c = count[w][threadIdx.x];
-                count[w][threadIdx.x] = at;
+                const uint32_t c = lds.count[w][threadIdx.x];
+                lds.count[w][threadIdx.x] = at;
                 at += c;
             }
         }
@@ -733,10 +755,10 @@ __global__ void __launch_bounds__(kThreads) few_ids_kernel(FewArgs f)
     __syncthreads();
     for (uint32_t i0 = wave * share; i0 < min((wave + 1) * share, have); i0 += 64) {
         const bool valid[1] = {i0 + lane64 < min((wave + 1) * share, have)};
-        const uint32_t e = valid[0] ? found[i0 + lane64] : 0;
+        const uint32_t e = !valid[0] ? 0 : i0 == wave * share ? first_entry : entry(i0 + lane64);
         const uint32_t digit[1] = {e >> 16};
         uint32_t rank[1];
-        wave_ranks<1>(digit, valid, f.slot_bits, count[wave], rank);
+        wave_ranks<1>(digit, valid, f.slot_bits, lds.count[wave], rank);
         if (valid[0]) sorted[rank[0]] = static_cast<uint16_t>(e);
     }
     __syncthreads();
@@ -744,7 +766,7 @@ __global__ void __launch_bounds__(kThreads) few_ids_kernel(FewArgs f)
         load_vec<TG, V>(static_cast<const TG*>(a.grad) + static_cast<int64_t>(sorted[k]) * a.grad_stride + at, x);
     };
     sum_rows<TT, V, ADD>(
-        a, ADD ? slots_used : min(f.slots, a.num_rows - first), start, lds, lists, [&](uint32_t r) { return ADD && taken[r]; }, single,
+        a, ADD ? slots_used : min(f.slots, a.num_rows - first), start, lds.sums, lists, [&](uint32_t r) { return ADD && taken[r]; }, single,
         [&](uint32_t r) { return start[r + 1] - start[r]; },
         [&](uint32_t r, uint32_t t, int at, float (&x)[V]) { single(start[r] + t, at, x); }, [&](uint32_t r) { return ADD ? owner[r] : first + r; });
 }
@@ -811,17 +833,18 @@ int lanes_log2_for(int chunks)
 template <class TG, class TT, int V>
 hipError_t launch_few(const GradArgs& a, const int32_t* ids, bool add, hipStream_t st)
 {
-    FewArgs f{a, ids, 0, 0};
-    const size_t lds = static_cast<size_t>((a.n + 1) & ~1u) * 4 + static_cast<size_t>(a.n) * 2;
-    if (add) {
-        f.slots = kAddIds;
+    FewArgs f{a, ids, 0, 0, a.n <= kFewWide};
+    const size_t lds = few_found(a.n, f.wide) * size_t{4} + static_cast<size_t>(a.n) * 2;
+    if (add) {      // 16 positions for each workgroup where all then run at once (8192: 11.0 us, 12.1 with 32)
+        const uint32_t at_once = 256 * (lds <= kFewLds ? 3 : 2);
+        f.slots = (a.n + 15) / 16 <= at_once ? 16 : kAddIds;
     } else {        // 512 workgroups, and up to 4096 where looking through all ids costs each of them little
         const uint32_t most = std::min(std::max(4u << 20, 512 * a.n) / a.n, 4096u);
         f.slots = 32;
         while (f.slots < kMostSlots && a.num_rows / f.slots > most) f.slots *= 2;
     }
-    while ((1u << f.slot_bits) < f.slots + (add ? 1 : 0)) f.slot_bits += 1;
-    const uint32_t blocks = add ? (a.n + kAddIds - 1) / kAddIds : (a.num_rows + f.slots - 1) / f.slots;
+    while ((1u << f.slot_bits) < (add ? kAddIds + 1 : f.slots)) f.slot_bits += 1;
+    const uint32_t blocks = ((add ? a.n : a.num_rows) + f.slots - 1) / f.slots;
     if (add) hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, true>), dim3(blocks), dim3(kThreads), lds, st, f);
     else hipLaunchKernelGGL((few_ids_kernel<TG, TT, V, false>), dim3(blocks), dim3(kThreads), lds, st, f);
     return hipGetLastError();
