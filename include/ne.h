@@ -372,10 +372,11 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
  *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 1) bytes.
  * Precision.  NE_BF16: products of bf16 values with fp32 sums; loss_grad[i] (exp(s - lse) - [v == target]) is formed
- * in fp32 and rounded to bf16 for its products; scale is applied in fp32.  NE_F32: every operand is the sum of two
- * halves in fp16 (22 bits, at a common power of two that the largest finite magnitude sets), three products of halves
- * with fp32 sums: errors as those of fp32 products, for elements of at least 2^-24 of the largest magnitude of their
- * matrix; what is smaller counts to 2^-39 of it.
+ * in fp32 and, but where n is small, rounded to bf16 for its products; scale is applied in fp32.  NE_F32: where n is
+ * small, products in fp32 or of operands split into three bf16 parts (24 bits); otherwise every operand is the sum of
+ * two halves in fp16 (22 bits, at a common power of two that the largest finite magnitude sets), three products of
+ * halves with fp32 sums: errors as those of fp32 products, for elements of at least 2^-24 of the largest magnitude of
+ * their matrix; what is smaller counts to 2^-39 of it.
  * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN; in a row of w, all losses.
  *   1 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for the loss and writes zeros
  *   to dw.  Errors: NE_ERR_ARG, NE_ERR_HIP.

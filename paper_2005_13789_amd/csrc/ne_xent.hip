@@ -12,7 +12,8 @@
 //            the 256 MB of last-level cache), then dH += G . W_piece and dW_piece = G^T . H in one launch.
 // The scores are computed twice (8 n V d operations in training, where 6 would do with all scores kept: n V of them,
 // 6.6 GB in fp32 at the sizes below, written once and read twice).
-// For few rows of H the loss is bound by reading the table, which then streams through registers (few_rows_kernel).
+// With few rows of H all of it is bound by reading the table and writing its gradient, and other kernels let the table stream through
+// registers once (few_rows_kernel, few_grad_kernel).
 //
 // Types: bf16 operands go to the matrix cores as they are.  fp32 operands are split into two fp16 halves at a common
 // power of two, x 2^k = hi + lo with 22 bits, and a product is hi hi + hi lo + lo hi: the error of an fp32 product at
@@ -47,9 +48,9 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kAmaxBlocks = 1024;
 constexpr int64_t kMostStride = 1 << 22;   // elements: a tile's 256 rows are within 32 bits of its first
-constexpr int kFewRows = 64;           // rows of H up to which the table streams through registers
-constexpr int kFewBytes = 65536;
+constexpr int kFewBytes = 65536, kFewBytesAlone = 147456;     // LDS of H for the loss: of a workgroup of 4 wavefronts, and of one of 8 that is alone on its CU
 constexpr int kFewGroups = 1024;
+constexpr int kFewGradGroups = 1024;       // workgroups of the gradients; half as many where one takes more registers and LDS
 // Bytes of G of one piece: at most, those from which on smaller pieces are not looked at, those that stay in the last-level cache beside the
 // table and the sums, and what is written or read of these in a stage's time.
 constexpr int64_t kGBytes = 512 << 20, kGLeast = 64 << 20, kGCached = 256 << 20, kStageBytes = 8 << 20;
@@ -733,15 +734,15 @@ __device__ __forceinline__ void split_bf16(const float (&x)[8], bf16x8 (&out)[PA
     }
 }
 
-template <class T, int BLOCKS>
-__global__ void __launch_bounds__(kThreads) few_rows_kernel(FewArgs a)
+template <class T, int BLOCKS, int THREADS>
+__global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, AHEAD = sizeof(T) == 4 ? 4 : 8;
     extern __shared__ __align__(16) unsigned char few_lds[];       // [blocks][steps][parts][64 lanes] 16 bytes
     bf16x8* hs = reinterpret_cast<bf16x8*>(few_lds);
-    __shared__ float2 join[kThreads / 64][BLOCKS * 16];
+    __shared__ float2 join[THREADS / 64][BLOCKS * 16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-    for (int i = wave; i < BLOCKS * a.steps; i += kThreads / 64) {
+    for (int i = wave; i < BLOCKS * a.steps; i += THREADS / 64) {
         const int block = i / a.steps, step = i % a.steps;
         const uint32_t t = block * 16 + col;
         T x[8];
@@ -765,8 +766,8 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(FewArgs a)
         target[b] = b * 16 + col < a.n ? static_cast<uint32_t>(a.targets[b * 16 + col]) : 0xFFFFFFFFu;
     }
     __syncthreads();
-    const uint32_t tiles = (a.num_rows + 15) / 16, stride = gridDim.x * (kThreads / 64);
-    for (uint32_t tile = blockIdx.x * (kThreads / 64) + wave; tile < tiles; tile += stride) {
+    const uint32_t tiles = (a.num_rows + 15) / 16, stride = gridDim.x * (THREADS / 64);
+    for (uint32_t tile = blockIdx.x * (THREADS / 64) + wave; tile < tiles; tile += stride) {
         const T* row = static_cast<const T*>(a.w) + static_cast<int64_t>(min(tile * 16 + col, a.num_rows - 1)) * a.w_stride;
         f32x4 acc[BLOCKS];
 #pragma unroll
@@ -823,7 +824,7 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(FewArgs a)
     if (threadIdx.x < a.n) {
         float2 p = join[0][threadIdx.x];
 #pragma unroll
-        for (int w = 1; w < kThreads / 64; ++w) join_stat(p.x, p.y, join[w][threadIdx.x]);
+        for (int w = 1; w < THREADS / 64; ++w) join_stat(p.x, p.y, join[w][threadIdx.x]);
         a.stat[static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x] = p;
     }
 }
@@ -1111,6 +1112,207 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
     store_some<T, 4>(static_cast<T*>(a.out) + r * a.out_stride + e, a.dim - e, x);
 }
 
+// ---------------------------------------------------------------------------------------------
+// few rows of H: both gradients in one pass over the table
+// ---------------------------------------------------------------------------------------------
+// Bound by reading the table and writing its gradient.  A workgroup has 16 table rows at a time, of which a wavefront has CT groups of 16
+// columns: its share of the scores goes to the others through LDS, then every wavefront has all coefficients and makes dW of its columns, which
+// leaves at once, and adds to dH of its columns, which stays in registers to the end.  All products are fp32 matrix
+// instructions: with few rows of H they take less time than the table does, and no operand has to be split or scaled, so nothing reads the table
+// twice (200 003 x 256 fp32, 410 MB read and written: one row 92 us, 4.4 TB/s; 16 rows 102; in bf16 81, by then bound by the tile's chain of
+// LDS exchanges and products).
+// Contraction indices are taken in the order in which a lane has them side by side: 16 indices in four instructions, instruction i with index
+// 4 q + i in quarter q of the wavefront.
+struct FewGradArgs {
+    const void *h, *w;
+    int64_t h_stride, w_stride;
+    const int32_t* targets;
+    const float *lse, *c;          // c: NULL, or factors of the rows
+    uint32_t n, num_rows, cols;
+    int32_t dim;
+    float scale;
+    float* dh;                     // NULL, or [workgroups][n][cols]
+    void* dw;                      // NULL, or the table's gradient
+    int64_t dw_stride;
+};
+
+template <int CT, int WAVES> constexpr int few_stride() { return WAVES * CT * 16 + 4; }        // of a row of H in LDS: quarters in different banks
+template <int BLOCKS, int CT, int WAVES> constexpr size_t few_grad_lds() { return size_t{16} * BLOCKS * few_stride<CT, WAVES>() * 4; }
+
+template <class T, int BLOCKS, int CT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) few_grad_kernel(FewGradArgs a)
+{
+    constexpr int STRIDE = few_stride<CT, WAVES>();
+    extern __shared__ __align__(16) float few_h[];      // [16 BLOCKS][STRIDE]
+    __shared__ __align__(16) float part[2][WAVES][BLOCKS][256], turn[WAVES][BLOCKS][256];      // [row of H][row of the table]
+    __shared__ __align__(16) float crossing[WAVES][2][16][20];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+    for (int i = threadIdx.x; i < 16 * BLOCKS * STRIDE; i += 64 * WAVES) {
+        const uint32_t t = i / STRIDE;
+        const int e = i % STRIDE;
+        const bool in = t < a.n && e < a.dim && static_cast<uint32_t>(a.targets[t]) < a.num_rows;
+        few_h[i] = in ? static_cast<float>(static_cast<const T*>(a.h)[t * a.h_stride + e]) : 0.0f;
+    }
+    uint32_t target[BLOCKS];
+    float by[BLOCKS], c[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        const uint32_t t = b * 16 + col;
+        target[b] = t < a.n ? static_cast<uint32_t>(a.targets[t]) : 0xFFFFFFFFu;
+        const bool counts = target[b] < a.num_rows;     // (otherwise 2 to the minus infinity)
+        by[b] = counts ? a.lse[t] * kLog2e : INFINITY;
+        c[b] = counts && a.c ? a.c[t] : 1.0f;
+    }
+    f32x4 dh[BLOCKS][CT];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int g = 0; g < CT; ++g) dh[b][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t tiles = (a.num_rows + 15) / 16, last = a.num_rows - 1;
+    const int first_col = wave * CT * 16;
+    const T* w = static_cast<const T*>(a.w);
+    // row `col` of a tile, columns 4 quarter .. + 3 of each group: zeros beyond the last column
+    auto load = [&](uint32_t tile, float (&x)[CT][4]) {
+        const T* row = w + min(tile * 16 + col, last) * a.w_stride;
+#pragma unroll
+        for (int g = 0; g < CT; ++g) {
+            const int e = first_col + g * 16 + quarter * 4;
+            if (e + 4 <= a.dim) {
+                load_vec<T, 4>(row + e, x[g]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[g][q] = e + q < a.dim ? static_cast<float>(row[e + q]) : 0.0f;
+            }
+        }
+    };
+    float x[CT][4];
+    load(blockIdx.x, x);
+    __syncthreads();
+    uint32_t turns = 0;
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turns ^= 1) {
+        float next[CT][4];
+        if (tile + gridDim.x < tiles) load(tile + gridDim.x, next);
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int g = 0; g < CT; ++g) {
+                const f32x4 h = *reinterpret_cast<const f32x4*>(few_h + (b * 16 + col) * STRIDE + first_col + g * 16 + quarter * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[g][i], h[i], s, 0, 0, 0);
+            }
+            *reinterpret_cast<f32x4*>(&part[turns][wave][b][col * 16 + quarter * 4]) = s;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (loads travel on; the other half of `part` is for the next tile)
+        // coefficients of row `col` of H and rows 4 quarter .. + 3 of the table
+        f32x4 coef[BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            f32x4 s = *reinterpret_cast<const f32x4*>(&part[turns][0][b][col * 16 + quarter * 4]);
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4*>(&part[turns][v][b][col * 16 + quarter * 4]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t row = tile * 16 + quarter * 4 + i;
+                float p = __builtin_amdgcn_exp2f(fmaf(s[i], kLog2e, -by[b]));
+                if (row == target[b]) p -= 1.0f;
+                coef[b][i] = row <= last ? p * c[b] : 0.0f;
+            }
+            if (a.dw) *reinterpret_cast<f32x4*>(&turn[wave][b][col * 16 + quarter * 4]) = coef[b];
+        }
+        if (a.dh) {     // the tile with its rows along the registers, by way of LDS
+            float across[CT][4];
+#pragma unroll
+            for (int g = 0; g < CT; ++g) {
+                float (&at)[16][20] = crossing[wave][g & 1];
+                *reinterpret_cast<f32x4*>(&at[col][quarter * 4]) = f32x4{x[g][0], x[g][1], x[g][2], x[g][3]};
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                for (int i = 0; i < 4; ++i) across[g][i] = at[quarter * 4 + i][col];
+            }
+#pragma unroll
+            for (int g = 0; g < CT; ++g)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dh[b][g] = __builtin_amdgcn_mfma_f32_16x16x4f32(coef[b][i], across[g][i], dh[b][g], 0, 0, 0);
+        }
+        if (a.dw) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            float turned[BLOCKS][4];        // of rows 4 quarter .. + 3 of H and row `col` of the table
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) turned[b][i] = turn[wave][b][(quarter * 4 + i) * 16 + col];
+            T* to = static_cast<T*>(a.dw) + static_cast<int64_t>(tile * 16 + col) * a.dw_stride;
+#pragma unroll
+            for (int g = 0; g < CT; ++g) {
+                f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sum = __builtin_amdgcn_mfma_f32_16x16x4f32(few_h[(b * 16 + quarter * 4 + i) * STRIDE + first_col + g * 16 + col], turned[b][i], sum, 0, 0, 0);
+                const int e = first_col + g * 16 + quarter * 4;
+                const float out[4] = {sum[0] * a.scale, sum[1] * a.scale, sum[2] * a.scale, sum[3] * a.scale};
+                if (tile * 16 + col <= last) store_some<T, 4>(to + e, a.dim - e, out);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < CT; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[g][i] = next[g][i];
+    }
+    if (!a.dh) return;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t t = b * 16 + quarter * 4 + i;
+            if (t >= a.n) continue;
+            float* to = a.dh + (static_cast<int64_t>(blockIdx.x) * a.n + t) * a.cols;
+#pragma unroll
+            for (int g = 0; g < CT; ++g)
+                if (first_col + g * 16 + col < a.dim) to[first_col + g * 16 + col] = dh[b][g][i];
+        }
+}
+
+// dH from the workgroups' shares, added in their order: 64 columns of a row, 64 shares at a time.
+struct FewJoinArgs {
+    const float* in;               // [shares][n][cols]
+    uint32_t shares, n, num_targets, cols;
+    const int32_t* targets;
+    int32_t dim;
+    float scale;
+    void* out;
+    int64_t out_stride;
+};
+
+template <class T>
+__global__ void __launch_bounds__(1024) few_join_kernel(FewJoinArgs a)
+{
+    __shared__ __align__(16) float lds[64][64];
+    const uint32_t group = threadIdx.x >> 4, t = blockIdx.x;
+    const int e = blockIdx.y * 64 + (threadIdx.x & 15) * 4;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (e < static_cast<int>(a.cols)) {
+        const float* from = a.in + static_cast<int64_t>(t) * a.cols + e;
+        const int64_t step = static_cast<int64_t>(a.n) * a.cols;
+#pragma unroll 8
+        for (uint32_t v = group; v < a.shares; v += 64) sum += *reinterpret_cast<const f32x4*>(from + v * step);
+    }
+    *reinterpret_cast<f32x4*>(&lds[group][(threadIdx.x & 15) * 4]) = sum;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    float all = 0.0f;
+#pragma unroll 16
+    for (int v = 0; v < 64; ++v) all += lds[v][threadIdx.x];
+    const int at = blockIdx.y * 64 + threadIdx.x;
+    if (at >= a.dim) return;
+    const bool counts = static_cast<uint32_t>(a.targets[t]) < a.num_targets;
+    static_cast<T*>(a.out)[t * a.out_stride + at] = from_float<T>(counts ? all * a.scale : 0.0f);
+}
+
 template <class T>
 __global__ void __launch_bounds__(kThreads) zero_kernel(T* out, int64_t stride, int64_t rows, int32_t dim)
 {
@@ -1130,6 +1332,7 @@ struct XentWs {
     int64_t tokens;
     uint32_t row_tiles, splits;        // of the scores, or of a piece's coefficients
     int32_t few_blocks;                // > 0: few rows of H, so many blocks of 16
+    int32_t few_waves, few_groups;     // of their gradients: wavefronts of a workgroup, groups of 16 columns of each
     int64_t piece;                     // table rows of a piece
     bool large_scores, large_products; // tiles of 256 x 256
     uint32_t h_splits, w_splits, w_share, w_stages;
@@ -1240,6 +1443,36 @@ void choose_pieces(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
     w = chosen;
 }
 
+// LDS of the rows of H that a launch of the few-rows kernel has, as second operands.
+int64_t few_bytes_of(const XentWs& w, int32_t dim) { return w.few_blocks * ceil_div(dim, 32) * (w.parts == 2 ? 3 : 1) * 1024; }
+
+// Whether the table streams through registers for the loss: up to 64 rows, or in fp32, where the other way makes halves of the table first, two
+// launches of as many rows as LDS has place for (200 003 x 256 fp32: 64 rows 55 us, 128 rows 107, the other way 178 and 182).
+bool few_loss(XentWs& w, int64_t n, int32_t dim)
+{
+    w.few_blocks = n <= 16 ? 1 : n <= 32 ? 2 : 4;
+    while (w.few_blocks > 1 && few_bytes_of(w, dim) > kFewBytesAlone) w.few_blocks /= 2;
+    if (few_bytes_of(w, dim) <= kFewBytesAlone && ceil_div(n, 16 * w.few_blocks) <= w.parts) return true;
+    w.few_blocks = 0;
+    return false;
+}
+
+// Whether both gradients take one pass over the table, and how.  Up to 32 rows in fp32, where the other way makes halves of the table first (us at
+// 200 003 x 256: 16 rows 102 and 280, 32 rows 149 and 281), and up to 16 in bf16 where columns are few (100 000 x 100: 32 and 45; 200 003 x 256:
+// 81 and 88; 100 000 x 512: 102 and 85; 17 rows of 256: 132 and 88).
+bool few_grad(XentWs& w, int64_t n, int32_t dim)
+{
+    if (n > 32 || (w.parts == 1 && (n > 16 || dim > 256))) return false;
+    const int64_t groups = ceil_div(dim, 16);
+    w.few_blocks = n <= 16 ? 1 : 2;
+    w.few_waves = groups <= 32 ? 4 : 8;
+    w.few_groups = 1;
+    while (w.few_groups * w.few_waves < groups) w.few_groups *= 2;
+    if (w.few_groups <= 8 && (w.few_blocks == 1 || w.few_waves == 4)) return true;
+    w.few_blocks = 0;
+    return false;
+}
+
 // The workspace has room for packed copies whether or not this call's alignment needs them.
 XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad, char* base)
 {
@@ -1253,13 +1486,16 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     const int64_t side = w.large_scores ? 256 : 128, token_tiles = ceil_div(w.tokens, side);
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     Carver take{base};
-    // H as second operands of the few-rows kernel has to leave room in LDS for a second workgroup
-    const int64_t few_bytes = (n <= 16 ? 1 : n <= 32 ? 2 : 4) * ceil_div(dim, 32) * (type == NE_F32 ? 3 : 1) * 1024;
-    if (!grad && n <= kFewRows && few_bytes <= kFewBytes) {
-        w.few_blocks = static_cast<int32_t>(n <= 16 ? 1 : n <= 32 ? 2 : 4);
-        w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups));
+    if (!grad && few_loss(w, n, dim)) {
+        w.splits = static_cast<uint32_t>(few_bytes_of(w, dim) > kFewBytes ? std::min<int64_t>(ceil_div(num_rows, 128), 256) : std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups));
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * n);
         w.target_score = take.get<float>(static_cast<size_t>(n));
+        w.total = take.total();
+        return w;
+    }
+    if (grad && few_grad(w, n, dim)) {
+        w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, 16), w.few_blocks == 1 && w.few_groups <= 4 ? kFewGradGroups : kFewGradGroups / 2));
+        w.dh = take.get<float>(static_cast<size_t>(w.splits) * n * w.cols);
         w.total = take.total();
         return w;
     }
@@ -1361,16 +1597,27 @@ template <class T>
 hipError_t run_few(const XentCall& x, const XentWs& w, float* loss, float* lse, hipStream_t st)
 {
     FewArgs a{};
-    a.h = x.h; a.w = x.w; a.h_stride = x.h_stride; a.w_stride = x.w_stride; a.targets = x.targets; a.n = static_cast<uint32_t>(x.n);
-    a.num_rows = static_cast<uint32_t>(x.num_rows); a.dim = x.dim; a.steps = static_cast<int32_t>(ceil_div(x.dim, 32)); a.stat = w.stat;
-    a.target_score = w.target_score;
-    const size_t lds = static_cast<size_t>(w.few_blocks) * a.steps * (sizeof(T) == 4 ? 3 : 1) * 1024;
-    const dim3 grid(w.splits);
-    if (w.few_blocks == 1) hipLaunchKernelGGL((few_rows_kernel<T, 1>), grid, dim3(kThreads), lds, st, a);
-    else if (w.few_blocks == 2) hipLaunchKernelGGL((few_rows_kernel<T, 2>), grid, dim3(kThreads), lds, st, a);
-    else hipLaunchKernelGGL((few_rows_kernel<T, 4>), grid, dim3(kThreads), lds, st, a);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : join_losses(x, w, loss, lse, st);
+    a.w = x.w; a.h_stride = x.h_stride; a.w_stride = x.w_stride; a.num_rows = static_cast<uint32_t>(x.num_rows); a.dim = x.dim;
+    a.steps = static_cast<int32_t>(ceil_div(x.dim, 32));
+    const size_t lds = static_cast<size_t>(few_bytes_of(w, x.dim));
+    auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(w.splits), dim3(threads), lds, st, a); };
+    for (int64_t base = 0; base < x.n; base += 16 * w.few_blocks) {
+        a.h = static_cast<const T*>(x.h) + base * x.h_stride; a.targets = x.targets + base;
+        a.n = static_cast<uint32_t>(std::min<int64_t>(x.n - base, 16 * w.few_blocks));
+        a.stat = w.stat + base * w.splits; a.target_score = w.target_score + base;
+        if (lds > kFewBytes) {
+            if (w.few_blocks == 1) launch(few_rows_kernel<T, 1, 512>, 512);
+            else if (w.few_blocks == 2) launch(few_rows_kernel<T, 2, 512>, 512);
+            else launch(few_rows_kernel<T, 4, 512>, 512);
+        } else {
+            if (w.few_blocks == 1) launch(few_rows_kernel<T, 1, 256>, 256);
+            else if (w.few_blocks == 2) launch(few_rows_kernel<T, 2, 256>, 256);
+            else launch(few_rows_kernel<T, 4, 256>, 256);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return join_losses(x, w, loss, lse, st);
 }
 
 template <int P>
@@ -1391,6 +1638,28 @@ hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse,
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     return join_losses(x, w, loss, lse, st);
+}
+
+template <class T, int BLOCKS>
+hipError_t run_few_grad(const XentCall& x, const XentWs& w, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw, int64_t dw_stride, hipStream_t st)
+{
+    FewGradArgs a{};
+    a.h = x.h; a.w = x.w; a.h_stride = x.h_stride; a.w_stride = x.w_stride; a.targets = x.targets; a.lse = lse; a.c = x.c;
+    a.n = static_cast<uint32_t>(x.n); a.num_rows = static_cast<uint32_t>(x.num_rows); a.cols = static_cast<uint32_t>(w.cols); a.dim = x.dim;
+    a.scale = scale; a.dh = dh ? w.dh : nullptr; a.dw = dw; a.dw_stride = dw_stride;
+    const dim3 grid(w.splits);
+    if (w.few_groups == 1) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 1, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 1, 4>()), st, a);
+    else if (w.few_groups == 2) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 2, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 2, 4>()), st, a);
+    else if (w.few_groups == 4) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 4, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 4, 4>()), st, a);
+    if constexpr (sizeof(T) == 4) {
+        if (BLOCKS == 1 && w.few_waves == 8) hipLaunchKernelGGL((few_grad_kernel<T, 1, 8, 8>), grid, dim3(512), (few_grad_lds<1, 8, 8>()), st, a);
+        else if (w.few_groups == 8) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 8, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 8, 4>()), st, a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !dh) return e;
+    FewJoinArgs j{w.dh, w.splits, a.n, a.num_rows, a.cols, x.targets, x.dim, scale, dh, dh_stride};
+    hipLaunchKernelGGL(few_join_kernel<T>, dim3(a.n, static_cast<unsigned>(ceil_div(x.dim, 64))), dim3(1024), 0, st, j);
+    return hipGetLastError();
 }
 
 template <int P, class T>
@@ -1533,8 +1802,10 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
         return fail(NE_ERR_ARG, "ne_xent_grad: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
     if (!dh_dev && !dw_dev) return NE_OK;
-    const hipError_t e = type == NE_F32 ? run_grad<2, float>(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st)
-                                        : run_grad<1, bf16_t>(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st);
+    auto run = [&](auto grad) { return grad(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st); };
+    const hipError_t e = w.few_blocks == 1 ? (type == NE_F32 ? run(run_few_grad<float, 1>) : run(run_few_grad<bf16_t, 1>))
+                         : w.few_blocks == 2 ? run(run_few_grad<float, 2>)
+                         : type == NE_F32 ? run(run_grad<2, float>) : run(run_grad<1, bf16_t>);
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("cross entropy gradient launch: ") + hipGetErrorString(e));
     return NE_OK;
 }

@@ -266,6 +266,55 @@ def test_many_rows(dtype, n, V, d):
     test_larger_shapes(dtype, n, V, d)
 
 
+FEW = [(1, 3000, 1024), (16, 1000, 600), (20, 999, 500), (32, 777, 257), (5, 500, 16), (9, 17, 40), (16, 16, 128), (12, 5000, 250), (128, 300, 300),
+       (33, 400, 600), (30, 300, 1000), (64, 333, 384), (64, 150, 1100), (4, 100, 1500), (31, 4000, 30)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,d", FEW)
+def test_few_rows(n, V, d, dtype):
+    """Few rows against tables of all widths, in one launch or two, with factors, in strided rows, one gradient at a time."""
+    say("few", n, V, d, dtype)
+    h, w, t = make(n, V, d, dtype, n + V + d, pad=3, shift=1)
+    t[0] = V - 1
+    c = torch.randn(n, generator=torch.Generator().manual_seed(d)).to(DEV)
+    loss, lse, dh, dw = call(h, w, t, loss_grad=c, scale=0.5, fill=255)
+    check(h, w, t, loss, lse, dh, dw, loss_grad=c, scale=0.5)
+    assert torch.equal(call(h, w, t, loss_grad=c, scale=0.5, dw=False)[2], dh) and torch.equal(call(h, w, t, loss_grad=c, scale=0.5, dh=False)[3], dw)
+    big_h, big_w = torch.full((n, d + 5), 3.0, dtype=dtype, device=DEV), torch.full((V, d + 3), 3.0, dtype=dtype, device=DEV)
+    work = torch.empty(ne.ne_xent_workspace_bytes(n, V, d, dtype, True), dtype=torch.uint8, device=DEV)
+    ne.ne_xent_grad(h, w, t, lse, big_h[:, 2:2 + d], big_w[:, 1:1 + d], work, loss_grad=c, scale=0.5)
+    assert torch.equal(big_h[:, 2:2 + d], dh) and torch.equal(big_w[:, 1:1 + d], dw)
+    for gap in (big_h[:, :2], big_h[:, 2 + d:], big_w[:, :1], big_w[:, 1 + d:]):
+        assert bool((gap == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_rows_that_hold_anything(dtype):
+    n, V, d = 14, 700, 90
+    h, w, t = make(n, V, d, dtype, 30, ignored=0.0)
+    t[3], t[8] = -1, V
+    first = call(h, w, t)
+    dirty = h.clone()
+    dirty[3], dirty[8] = float("nan"), float("inf")
+    assert all(torch.equal(a, b) for a, b in zip(first, call(dirty, w, t)))
+    dirty = h.clone()
+    dirty[5, 7] = float("nan")
+    loss, lse, dh, dw = call(dirty, w, t)
+    keep = torch.arange(n, device=DEV) != 5
+    assert torch.equal(loss[keep], first[0][keep]) and torch.equal(dh[keep], first[2][keep])
+    assert bool(torch.isnan(loss[5])) and bool(torch.isnan(dh[5]).all()) and bool(torch.isnan(dw).all())
+    none = call(h, w, torch.full_like(t, -1))
+    assert all(bool((x == 0).all()) for x in none)
+
+
+@pytest.mark.parametrize("dtype,n,V,d", [(torch.float32, 1, 200003, 256), (torch.float32, 32, 100003, 130), (torch.float32, 9, 50001, 1000),
+                                         (torch.bfloat16, 16, 150001, 200), (torch.float32, 128, 60001, 250)])
+def test_few_rows_of_large_tables(dtype, n, V, d):
+    """Bounds as those of larger shapes."""
+    test_larger_shapes(dtype, n, V, d)
+
+
 def test_no_rows():
     w = torch.randn(50, 16, device=DEV)
     empty = torch.empty(0, 16, device=DEV)
