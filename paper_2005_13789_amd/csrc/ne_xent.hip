@@ -48,7 +48,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kAmaxBlocks = 1024;
 constexpr int64_t kMostStride = 1 << 22;   // elements: a tile's 256 rows are within 32 bits of its first
-constexpr int kFewBytes = 65536, kFewBytesAlone = 147456;     // LDS of H for the loss: of a workgroup of 4 wavefronts, and of one of 8 that is alone on its CU
+constexpr int kFewBytes = 65536, kFewBytesAlone = 153600;     // LDS of H for the loss: of a workgroup of 4 wavefronts, and of one of 8 that is alone on its CU
 constexpr int kFewGroups = 1024;
 constexpr int kFewGradGroups = 1024;       // workgroups of the gradients; half as many where one takes more registers and LDS
 // Bytes of G of one piece: at most, those from which on smaller pieces are not looked at, those that stay in the last-level cache beside the
@@ -1447,12 +1447,14 @@ void choose_pieces(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
 int64_t few_bytes_of(const XentWs& w, int32_t dim) { return w.few_blocks * ceil_div(dim, 32) * (w.parts == 2 ? 3 : 1) * 1024; }
 
 // Whether the table streams through registers for the loss: up to 64 rows, or in fp32, where the other way makes halves of the table first, two
-// launches of as many rows as LDS has place for (200 003 x 256 fp32: 64 rows 55 us, 128 rows 107, the other way 178 and 182).
-bool few_loss(XentWs& w, int64_t n, int32_t dim)
+// launches of as many rows as LDS has place for, three where the table is no small part of the last-level cache (us at 200 003 x 256 fp32:
+// 64 rows 55, 128 rows 107, 192 rows 169, the other way 178, 182 and 212; 192 rows against 100 000 x 100: 76 and 63).
+bool few_loss(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
 {
+    const int64_t launches = w.parts == 1 ? 1 : num_rows * dim < (1 << 25) ? 2 : 3;
     w.few_blocks = n <= 16 ? 1 : n <= 32 ? 2 : 4;
     while (w.few_blocks > 1 && few_bytes_of(w, dim) > kFewBytesAlone) w.few_blocks /= 2;
-    if (few_bytes_of(w, dim) <= kFewBytesAlone && ceil_div(n, 16 * w.few_blocks) <= w.parts) return true;
+    if (few_bytes_of(w, dim) <= kFewBytesAlone && ceil_div(n, 16 * w.few_blocks) <= launches) return true;
     w.few_blocks = 0;
     return false;
 }
@@ -1486,7 +1488,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     const int64_t side = w.large_scores ? 256 : 128, token_tiles = ceil_div(w.tokens, side);
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     Carver take{base};
-    if (!grad && few_loss(w, n, dim)) {
+    if (!grad && few_loss(w, n, num_rows, dim)) {
         w.splits = static_cast<uint32_t>(few_bytes_of(w, dim) > kFewBytes ? std::min<int64_t>(ceil_div(num_rows, 128), 256) : std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups));
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * n);
         w.target_score = take.get<float>(static_cast<size_t>(n));

@@ -309,7 +309,8 @@ def test_few_rows_that_hold_anything(dtype):
 
 
 @pytest.mark.parametrize("dtype,n,V,d", [(torch.float32, 1, 200003, 256), (torch.float32, 32, 100003, 130), (torch.float32, 9, 50001, 1000),
-                                         (torch.bfloat16, 16, 150001, 200), (torch.float32, 128, 60001, 250)])
+                                         (torch.bfloat16, 16, 150001, 200), (torch.float32, 128, 60001, 250),
+                                         (torch.float32, 170, 140001, 250), (torch.float32, 90, 45000, 790)])
 def test_few_rows_of_large_tables(dtype, n, V, d):
     """Bounds as those of larger shapes."""
     test_larger_shapes(dtype, n, V, d)
