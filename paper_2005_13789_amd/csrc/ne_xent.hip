@@ -8,8 +8,8 @@
 // instructions serve all three products; they differ in where their operands lie and in what becomes of the sums:
 //   scores   every lane of a tile's sums belongs to one row of H (table rows run along the registers), so the running
 //            maximum and sum of a row's softmax are two registers, joined between lanes once at the end.
-//   gradient the same product again for a piece of the table, whose G is written to the workspace (sized to stay in
-//            the 256 MB of last-level cache), then dH += G . W_piece and dW_piece = G^T . H in one launch.
+//   gradient the same product again for a piece of the table, whose G is written to the workspace (of sizes that
+//            fill the machine, and in the 256 MB of last-level cache where that matters), then dH += G . W_piece and dW_piece = G^T . H in one launch.
 // The scores are computed twice (8 n V d operations in training, where 6 would do with all scores kept: n V of them,
 // 6.6 GB in fp32 at the sizes below, written once and read twice).
 // With few rows of H all of it is bound by reading the table and writing its gradient, and other kernels let the table stream through
@@ -21,8 +21,8 @@
 //
 // Bound by the matrix cores and by the loads from L2 that feed them.  Measured, 8192 rows, 200 003 of 512, bf16: loss
 // 1.7 to 1.8 ms (950 TF; a copy of the kernel without loads took 0.87 of the time, without exponentials 0.90, without
-// products 0.87: none of them hides the others completely), gradients of a piece of 8192 table rows 87 us for G and
-// 130 to 136 for both products (1.03 PF), 7.0 to 7.4 ms in all.
+// products 0.87: none of them hides the others completely), gradients of a piece of 15 616 table rows 169 us for G and
+// 237 for both products (1.1 PF), 6.8 to 7.1 ms in all.
 // 4096 rows, 10 000 of 128, fp32: scores 40 us, G 55, products 72, and 35 us for the small launches around them.
 //
 // Operands in LDS are 16-byte pieces placed so that reads are free of bank conflicts (an XOR of the piece's
@@ -833,8 +833,8 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // G of a piece of the table
 // ---------------------------------------------------------------------------------------------
 // The scores again, with the exponentials written as operands of the next products instead of added up: bf16, of values at most 1 whose errors
-// of 2^-9 average out over the products' sums, or two fp16 halves of G 2^14, which keep 22 bits of 2^-14 and more.  8192 x 8192 x 512 bf16: 87 us (0.79 PF,
-// 134 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
+// of 2^-9 average out over the products' sums, or two fp16 halves of G 2^14, which keep 22 bits of 2^-14 and more.  8192 x 15 616 x 512 bf16: 169 us (0.78 PF,
+// 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
 struct CoefArgs {
     Operand w, h;                  // both by rows
     const int32_t* targets;
@@ -955,7 +955,7 @@ struct ProductArgs {
     const int32_t* shift;          // fp32 only: power of two of the rows of H
 };
 
-// Both products of a piece are one launch: either alone leaves places empty.  (8192 x 8192 x 512 bf16, large tiles: 130 us, 1.05 PF; 4096 x 10 000 x
+// Both products of a piece are one launch: either alone leaves places empty.  (8192 x 15 616 x 512 bf16, large tiles: 237 us, 1.1 PF; 4096 x 10 000 x
 // 128 fp32, small tiles: 72 us, 0.87 PF of half products.)
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
 template <int P, int W, bool GROWS>
@@ -1049,7 +1049,7 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     }
 }
 
-// Sums the splits and rounds once: 2 x 8192 x 512, 42 MB: 7.7 us.  dH: rows without a target become zeros, the others take their factor.
+// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us).  dH: rows without a target become zeros, the others take their factor.
 struct ReduceArgs {
     const float* in;               // [splits][rows_in][cols]
     int64_t split_stride;
