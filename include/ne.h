@@ -344,7 +344,8 @@ ne_status ne_embed_lookup(const void* table_dev, int32_t table_type, int64_t tab
  *   grad_dev       : device, grad_type [n][dim], row stride grad_stride >= dim, or 0 for one row that every
  *                    position shares.
  *   table_grad_dev : device, table_grad_type [num_rows][dim], row stride table_grad_stride >= dim; must not overlap grad.
- *   workspace_dev  : at least ne_embed_workspace_bytes(num_rows, dim, n) bytes (0 there = invalid arguments or n == 0).
+ *   workspace_dev  : at least ne_embed_workspace_bytes(num_rows, dim, n) bytes (0 there = invalid arguments or n == 0),
+ *                    which grow with n.
  * n == 0 writes zeros, or nothing with accumulate.  Sizes and errors as for ne_embed_lookup.
  */
 size_t ne_embed_workspace_bytes(int64_t num_rows, int32_t dim, int64_t n);
@@ -362,7 +363,8 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  *   h_dev, w_dev : device, type [n][dim] and [num_rows][dim], row strides >= dim, aligned to their elements.
  *   targets_dev  : device, int32[n].
  *   loss_dev, lse_dev : device, float[n].
- *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 0) bytes.
+ *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 0) bytes, which grow with n: a workspace
+ *                   for n rows serves fewer rows, too.
  * ne_xent_grad gives, for G_iv = scale * loss_grad[i] * (exp(s_iv - lse[i]) - [v == target[i]]),
  *   dh = G . W  and  dw = G^T . H,
  * written whole (rows without a target: dh 0).  Both have the type of h and w; one of them may be NULL.

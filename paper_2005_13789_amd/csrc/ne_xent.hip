@@ -1524,6 +1524,35 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     return w;
 }
 
+// Bytes of a workspace for up to n rows: bounds of what xent_layout takes, each growing with n, as what it takes itself need not (few rows take no
+// copies, a larger n may have smaller pieces or fewer splits).
+size_t xent_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad)
+{
+    XentWs w{};
+    w.parts = type == NE_F32 ? 2 : 1;
+    const int64_t step = w.parts == 1 ? step_of<1>() : step_of<2>();
+    const int64_t tokens = round_up(n, step), padded = round_up(dim, step), cols = round_up(dim, 32), rows = round_up(num_rows, 256);
+    int64_t bytes = 16 << 10;                                   // alignment, largest magnitudes
+    if (!grad) {
+        // shares of few rows; of tiles: as many workgroups as run in four rounds, or one for every tile
+        bytes += (std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups) * std::min<int64_t>(n, 192) + tokens +
+                  std::min<int64_t>(ceil_div(num_rows, 128) * tokens, 4 * 512 * 128)) * 8 + tokens * 4;
+        if (few_loss(w, n, num_rows, dim)) return static_cast<size_t>(bytes);
+    } else {
+        const int64_t few = ceil_div(num_rows, 16);
+        bytes += std::max(std::min<int64_t>(few, kFewGradGroups) * std::min<int64_t>(n, 16), std::min<int64_t>(few, kFewGradGroups / 2) * std::min<int64_t>(n, 32)) * cols * 4;
+        if (few_grad(w, n, dim)) return static_cast<size_t>(bytes);
+        // G of a piece; partial sums: a share has kLeastShare stages, and all workgroups but one for each tile have a place at once
+        const int64_t row_bytes = 2 * w.parts * tokens, places = int64_t{256} * 256 * 256;
+        const int64_t all_h = round_up(n, 256) * round_up(dim, 256), all_w = rows * round_up(dim, 256);
+        bytes += std::min(rows * row_bytes, kGBytes + 256 * row_bytes);
+        bytes += std::min(ceil_div(rows / step, kLeastShare) * tokens * cols, places + all_h) * 4;
+        if (tokens / step > kLeastShare) bytes += std::min({ceil_div(tokens / step, kLeastShare) * rows * cols, places + std::min(all_w, places)}) * 4;
+        bytes += w.parts == 2 ? 2 * tokens * padded * 2 : 0;
+    }
+    return static_cast<size_t>(bytes + w.parts * 2 * padded * (tokens + num_rows));
+}
+
 // Stages of H that the scores' wavefronts hold in registers: 2, 4, or 0 for H through LDS like the table: where there are more, with large
 // tiles, and where a workgroup has so few tiles that fetching H ahead of them does not pay.
 int held_stages(const XentWs& w, uint32_t row_tiles, uint32_t splits, int steps)
@@ -1758,7 +1787,7 @@ extern "C" {
 size_t ne_xent_workspace_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int32_t grad)
 {
     if (!xent_sizes_ok(n, num_rows, dim, type) || n == 0) return 0;
-    return xent_layout(n, num_rows, dim, type, grad != 0, nullptr).total;
+    return std::max(xent_bytes(n, num_rows, dim, type, grad != 0), xent_layout(n, num_rows, dim, type, grad != 0, nullptr).total);
 }
 
 ne_status ne_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type,
@@ -1770,7 +1799,7 @@ ne_status ne_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, i
     if (rc != NE_OK || n == 0) return rc;
     if (!loss_dev || !lse_dev || !aligned(loss_dev, 4) || !aligned(lse_dev, 4)) return fail(NE_ERR_ARG, "ne_xent_loss: loss_dev or lse_dev is NULL or misaligned");
     const XentWs w = xent_layout(n, num_rows, dim, type, false, static_cast<char*>(workspace_dev));
-    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < std::max(xent_bytes(n, num_rows, dim, type, false), w.total))
         return fail(NE_ERR_ARG, "ne_xent_loss: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const hipError_t e = w.few_blocks ? (type == NE_F32 ? run_few<float>(x, w, loss_dev, lse_dev, st) : run_few<bf16_t>(x, w, loss_dev, lse_dev, st))
@@ -1801,7 +1830,7 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
     }
     if (!lse_dev || !aligned(lse_dev, 4) || !aligned(loss_grad_dev, 4)) return fail(NE_ERR_ARG, "ne_xent_grad: lse_dev is NULL, or it or loss_grad_dev misaligned");
     const XentWs w = xent_layout(n, num_rows, dim, type, true, static_cast<char*>(workspace_dev));
-    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < std::max(xent_bytes(n, num_rows, dim, type, true), w.total))
         return fail(NE_ERR_ARG, "ne_xent_grad: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
     if (!dh_dev && !dw_dev) return NE_OK;
     auto run = [&](auto grad) { return grad(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st); };

@@ -142,3 +142,19 @@ def test_captured_calls_replay_as_eager_ones(n, dtype):
         for a, b in zip(out, want):
             assert torch.equal(a, b)
         torch.mm(p, p.t())      # eager work between the replays
+
+
+@pytest.mark.parametrize("compute", [torch.float32, torch.bfloat16])
+def test_steps_of_fewer_pairs(compute):
+    """One trainer takes steps of all sizes up to its batch: as a trainer of that batch does."""
+    V, d, batch = 9000, 120, 6605
+    gen = torch.Generator().manual_seed(7)
+    pairs = torch.randint(0, V, (batch, 2), generator=gen).to(torch.int32).to(DEV)
+    for n in (1, 20, 150, 2725, 4400, batch):
+        say("steps of", n, compute)
+        got = []
+        for size in (batch, n):
+            vertex, context = tables(V, d, 8)
+            trainer = SoftmaxTrainer(vertex, context, batch=size, compute=compute)
+            got.append([trainer.step(pairs[:n], 1e-2).clone(), vertex, context])
+        assert all(torch.equal(a, b) for a, b in zip(*got))

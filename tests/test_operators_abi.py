@@ -102,3 +102,15 @@ def test_binding_refuses_what_the_kernels_cannot_take():
         ne.ne_xent_loss(host, host, ids, host[0], host[0], None)
     with pytest.raises(TypeError):
         ne.ne_create_adamw([host], [host], [host.half()], [host], None)
+
+
+@pytest.mark.parametrize("V,d", [(1, 1), (100, 8), (3000, 64), (10000, 128), (100003, 200), (50000, 300), (200003, 512), (777, 1500), (1000000, 40)])
+def test_workspaces_serve_smaller_calls(V, d):
+    """What a call of n rows needs is no more than what a call of more rows needs."""
+    sizes = sorted(set(list(range(1, 140)) + [int(140 * 1.03 ** k) for k in range(180)]))
+    for dtype in (torch.float32, torch.bfloat16):
+        for grad in (False, True):
+            need = [ne.ne_xent_workspace_bytes(n, V, d, dtype, grad) for n in sizes]
+            assert need == sorted(need)
+    need = [ne.ne_embed_workspace_bytes(V, d, n) for n in sizes + [2 ** 18, 270000, 2 ** 20]]
+    assert need == sorted(need)
