@@ -815,7 +815,8 @@ EmbedWs embed_layout(int64_t num_rows, int32_t dim, int64_t n, char* base)
     if (!few_ids(num_rows, n)) {
         w.entries[0] = take.get<uint2>(static_cast<size_t>(n));
         w.entries[1] = take.get<uint2>(static_cast<size_t>(n));
-        w.hist = take.get<uint32_t>(static_cast<size_t>(std::min<int64_t>(kMostTiles, (n + kSortRound - 1) / kSortRound)) << w.bits);    // (no less for larger n)
+        // (for as many tiles as shorter ones would be: no less for larger n)
+        w.hist = take.get<uint32_t>(static_cast<size_t>(std::min<int64_t>(kMostTiles, (n + kSortRound - 1) / kSortRound)) << w.bits);
         w.partial = take.get<float>(static_cast<size_t>(n / kChunk) * dim);
         if (n > kSuperFrom) w.super = take.get<float>(static_cast<size_t>(n / kChunk) * dim);
     }

@@ -54,7 +54,8 @@ constexpr int kFewGradGroups = 1024;       // workgroups of the gradients; half 
 // Bytes of G of one piece: at most, those from which on smaller pieces are not looked at, those that stay in the last-level cache beside the
 // table and the sums, and what is written or read of these in a stage's time.
 constexpr int64_t kGBytes = 512 << 20, kGLeast = 64 << 20, kGCached = 256 << 20, kStageBytes = 8 << 20;
-constexpr int kLeastShare = 8, kTileCost = 1, kLaunchCost = 10;   // stages: the fewest of a product's workgroup; what beginning and writing a tile, and a launch, take
+// In stages: the fewest of a product's workgroup; what a tile takes besides (1, 4 and 8 choose alike); what a launch takes.
+constexpr int kLeastShare = 8, kTileCost = 1, kLaunchCost = 10;
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
 
@@ -1489,14 +1490,16 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     Carver take{base};
     if (!grad && few_loss(w, n, num_rows, dim)) {
-        w.splits = static_cast<uint32_t>(few_bytes_of(w, dim) > kFewBytes ? std::min<int64_t>(ceil_div(num_rows, 128), 256) : std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups));
+        const bool alone = few_bytes_of(w, dim) > kFewBytes;        // (a tile of 16 rows for each wavefront, at most)
+        w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, alone ? 128 : 64), alone ? 256 : kFewGroups));
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * n);
         w.target_score = take.get<float>(static_cast<size_t>(n));
         w.total = take.total();
         return w;
     }
     if (grad && few_grad(w, n, dim)) {
-        w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, 16), w.few_blocks == 1 && w.few_groups <= 4 ? kFewGradGroups : kFewGradGroups / 2));
+        const int64_t most = w.few_blocks == 1 && w.few_groups <= 4 ? kFewGradGroups : kFewGradGroups / 2;
+        w.splits = static_cast<uint32_t>(std::min(ceil_div(num_rows, 16), most));
         w.dh = take.get<float>(static_cast<size_t>(w.splits) * n * w.cols);
         w.total = take.total();
         return w;
@@ -1540,14 +1543,16 @@ size_t xent_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool g
         if (few_loss(w, n, num_rows, dim)) return static_cast<size_t>(bytes);
     } else {
         const int64_t few = ceil_div(num_rows, 16);
-        bytes += std::max(std::min<int64_t>(few, kFewGradGroups) * std::min<int64_t>(n, 16), std::min<int64_t>(few, kFewGradGroups / 2) * std::min<int64_t>(n, 32)) * cols * 4;
+        const int64_t narrow = std::min<int64_t>(few, kFewGradGroups) * std::min<int64_t>(n, 16);
+        const int64_t wide = std::min<int64_t>(few, kFewGradGroups / 2) * std::min<int64_t>(n, 32);
+        bytes += std::max(narrow, wide) * cols * 4;
         if (few_grad(w, n, dim)) return static_cast<size_t>(bytes);
         // G of a piece; partial sums: a share has kLeastShare stages, and all workgroups but one for each tile have a place at once
         const int64_t row_bytes = 2 * w.parts * tokens, places = int64_t{256} * 256 * 256;
         const int64_t all_h = round_up(n, 256) * round_up(dim, 256), all_w = rows * round_up(dim, 256);
         bytes += std::min(rows * row_bytes, kGBytes + 256 * row_bytes);
         bytes += std::min(ceil_div(rows / step, kLeastShare) * tokens * cols, places + all_h) * 4;
-        if (tokens / step > kLeastShare) bytes += std::min({ceil_div(tokens / step, kLeastShare) * rows * cols, places + std::min(all_w, places)}) * 4;
+        if (tokens / step > kLeastShare) bytes += std::min(ceil_div(tokens / step, kLeastShare) * rows * cols, places + std::min(all_w, places)) * 4;
         bytes += w.parts == 2 ? 2 * tokens * padded * 2 : 0;
     }
     return static_cast<size_t>(bytes + w.parts * 2 * padded * (tokens + num_rows));
