@@ -28,8 +28,7 @@ constexpr int kSuper = 256;         // the same, one size up
 constexpr int kSuperFrom = 131072;  // positions from which on that is done (a launch of 6 us); below, the longest runs have 8192 sums of 16
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortItems = 4;
-constexpr int kSortRound = kSortThreads * kSortItems;
+constexpr int kSortFew = 65536;     // positions up to which a thread has two at a time, otherwise four (16 385 ids 25.6 us, 27.8 with four; 114 438: 48.9 and 46.8)
 constexpr int kMostTiles = 128;     // workgroups of a sorting pass; each reads the counts of all
 constexpr int kMostDigits = 1024;
 constexpr int kRowsPerGroup = 64;   // table rows of a workgroup of the rows launch
@@ -195,6 +194,7 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* wave_sums
 
 // One pass: where a tile's entries of a digit begin follows from the counts of all tiles, which each workgroup adds up
 // by itself (at most 128 x 1024 words, in L2: a launch less than with sums made in between).
+template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
 {
     __shared__ uint32_t base[kMostDigits];
@@ -232,13 +232,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
         base[2 * threadIdx.x + 1] = before + total[0] + mine[1];
     }
     const uint32_t lo = blockIdx.x * a.tile_len, hi = min(lo + a.tile_len, a.n);
-    for (uint32_t r0 = lo; r0 < hi; r0 += kSortRound) {
-        uint2 e[kSortItems];
-        uint32_t digit[kSortItems], rank[kSortItems];
-        bool valid[kSortItems];
+    for (uint32_t r0 = lo; r0 < hi; r0 += kSortThreads * ITEMS) {
+        uint2 e[ITEMS];
+        uint32_t digit[ITEMS], rank[ITEMS];
+        bool valid[ITEMS];
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
-            const uint32_t i = r0 + wave * (64 * kSortItems) + j * 64 + lane;
+        for (int j = 0; j < ITEMS; ++j) {
+            const uint32_t i = r0 + wave * (64 * ITEMS) + j * 64 + lane;
             valid[j] = i < hi;
             e[j] = make_uint2(0, 0);
             if (valid[j]) e[j] = a.pass == 0 ? make_uint2(key_of(a.ids[i], a.num_rows), i) : a.in[i];
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) count[w][d] = 0;
         __syncthreads();
-        wave_ranks<kSortItems>(digit, valid, a.bits, count[wave], rank);
+        wave_ranks<ITEMS>(digit, valid, a.bits, count[wave], rank);
         __syncthreads();
         for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) {
             uint32_t at = base[d];
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_pass_kernel(SortArgs a)
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j)
+        for (int j = 0; j < ITEMS; ++j)
             if (valid[j]) a.out[count[wave][digit[j]] + rank[j]] = e[j];
         __syncthreads();
     }
@@ -808,7 +808,8 @@ EmbedWs embed_layout(int64_t num_rows, int32_t dim, int64_t n, char* base)
     w.passes = (key_bits + 9) / 10;
     w.bits = (key_bits + w.passes - 1) / w.passes;
     int64_t len = (n + kMostTiles - 1) / kMostTiles;
-    len = std::max<int64_t>((len + kSortRound - 1) / kSortRound * kSortRound, kSortRound);
+    const int64_t round = kSortThreads * (n <= kSortFew ? 2 : 4);
+    len = std::max<int64_t>((len + round - 1) / round * round, round);
     w.tile_len = static_cast<uint32_t>(len);
     w.tiles = static_cast<uint32_t>((n + len - 1) / len);
     Carver take{base};
@@ -816,7 +817,7 @@ EmbedWs embed_layout(int64_t num_rows, int32_t dim, int64_t n, char* base)
         w.entries[0] = take.get<uint2>(static_cast<size_t>(n));
         w.entries[1] = take.get<uint2>(static_cast<size_t>(n));
         // (for as many tiles as shorter ones would be: no less for larger n)
-        w.hist = take.get<uint32_t>(static_cast<size_t>(std::min<int64_t>(kMostTiles, (n + kSortRound - 1) / kSortRound)) << w.bits);
+        w.hist = take.get<uint32_t>(static_cast<size_t>(std::min<int64_t>(kMostTiles, (n + 2 * kSortThreads - 1) / (2 * kSortThreads))) << w.bits);
         w.partial = take.get<float>(static_cast<size_t>(n / kChunk) * dim);
         if (n > kSuperFrom) w.super = take.get<float>(static_cast<size_t>(n / kChunk) * dim);
     }
@@ -922,7 +923,8 @@ hipError_t launch_sort(const EmbedWs& w, const int32_t* ids, int64_t n, int64_t 
         e = hipGetLastError();
         if (e != hipSuccess) break;
         more = share();
-        hipLaunchKernelGGL(sort_pass_kernel, dim3(w.tiles + more), dim3(kSortThreads), 0, st, s);
+        if (n <= kSortFew) hipLaunchKernelGGL(sort_pass_kernel<2>, dim3(w.tiles + more), dim3(kSortThreads), 0, st, s);
+        else hipLaunchKernelGGL(sort_pass_kernel<4>, dim3(w.tiles + more), dim3(kSortThreads), 0, st, s);
         e = hipGetLastError();
     }
     return e;
