@@ -173,7 +173,7 @@ def main(argv=None) -> int:
     ap.add_argument("--epochs", type=int, default=10)
     ap.add_argument("--negatives", type=int, default=5)
     ap.add_argument("--batch", type=int, default=65536)
-    ap.add_argument("--lr", type=float, default=0.025)
+    ap.add_argument("--lr", type=float, default=0.025, help="first learning rate (mode softmax, which is trained by AdamW: about 0.001 to 0.01)")
     ap.add_argument("--walk-length", type=int, default=40)
     ap.add_argument("--window", type=int, default=5)
     ap.add_argument("--mode", default="sync", choices=["sync", "walks", "async", "softmax"])
