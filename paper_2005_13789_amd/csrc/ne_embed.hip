@@ -28,7 +28,8 @@ constexpr int kSuper = 256;         // the same, one size up
 constexpr int kSuperFrom = 131072;  // positions from which on that is done (a launch of 6 us); below, the longest runs have 8192 sums of 16
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortFew = 65536;     // positions up to which a thread has two at a time, otherwise four (16 385 ids 25.6 us, 27.8 with four; 114 438: 48.9 and 46.8)
+constexpr int kSortFew = 65536;     // positions up to which a thread has two at a time, otherwise four (16 385 ids 25.9 us, 27.8
+                                    // with four; 65 536 the same; 114 438: 48.9 and 46.8)
 constexpr int kMostTiles = 128;     // workgroups of a sorting pass; each reads the counts of all
 constexpr int kMostDigits = 1024;
 constexpr int kRowsPerGroup = 64;   // table rows of a workgroup of the rows launch
