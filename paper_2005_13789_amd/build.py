@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -22,10 +23,20 @@ HIPCC_FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    cmd = ["hipcc", *HIPCC_FLAGS, *SRCS, "-o", OUT]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    """Compiles the sources side by side, then links them."""
+    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SRCS]
+        commands = [["hipcc", *compile_flags, "-c", src, "-o", obj] for src, obj in zip(SRCS, objects)]
+        link = ["hipcc", "-shared", "-fPIC", "--offload-arch=gfx950", *objects, "-o", OUT]
+        if verbose:
+            for cmd in (*commands, link):
+                print(" ".join(cmd), flush=True)
+        running = [subprocess.Popen(cmd) for cmd in commands]
+        failed = [cmd for cmd, process in zip(commands, running) if process.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.run(link, check=True)
     return OUT
 
 
