@@ -86,7 +86,7 @@ struct Operand {
 // from stage to stage.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // Waits for all but the last LATER loads of this wavefront, and for the other wavefronts.
