@@ -3,7 +3,7 @@
 A pair (src, ctx) is scored against every row of the context table instead of a few sampled ones:
 loss = -log softmax(context . vertex[src])[ctx].  A step looks up the batch's vertex rows, takes the softmax cross
 entropy against the whole context table without keeping the scores, brings the gradients back to both tables (the
-vertex table's by sorted ids) and moves both with AdamW.  Every part is a call of the library; torch allocates.
+vertex table's by sorted ids) and moves both with AdamW.  Every part is a call of the library; torch allocates and marks the pairs that are left out.
 """
 from __future__ import annotations
 
@@ -49,12 +49,15 @@ class SoftmaxTrainer:
         self.opt = ne.ne_create_adamw(self.tables, self.grads, *states, opt_work, weight_decay=weight_decay, params_bf16=copies, seed=seed, **kw)
 
     def step(self, pairs: torch.Tensor, lr: float) -> torch.Tensor:
-        """One step of the mean loss of pairs int32 [n][2] (CUDA, n <= batch; a pair whose ctx is outside the tables does
-        not count).  Returns the pairs' losses before the step (a view that the next step overwrites)."""
+        """One step of the pairs' summed loss / n, pairs int32 [n][2] (CUDA, n <= batch).  A pair of which either id is outside the
+        tables (walks are padded with -1) is left out: its loss is 0 and it adds nothing to the gradients; n is the number of all pairs, so that
+        one of them weighs the same whatever else is in the step.  Returns the pairs' losses before the step (a view that the next
+        step overwrites)."""
         n = int(pairs.shape[0])
         if n < 1 or n > self.batch:
             raise ValueError(f"a step takes 1 to {self.batch} pairs")
-        src, ctx = pairs[:, 0].contiguous(), pairs[:, 1].contiguous()
+        src = pairs[:, 0].contiguous()
+        ctx = torch.where((src >= 0) & (src < self.tables[0].shape[0]), pairs[:, 1], -1)
         h, dh, loss, lse = self.h[:n], self.dh[:n], self.loss[:n], self.lse[:n]
         ne.ne_embed_lookup(self.rows[0], src, h)
         ne.ne_xent_loss(h, self.rows[1], ctx, loss, lse, self.work)

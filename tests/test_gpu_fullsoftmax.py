@@ -158,3 +158,32 @@ def test_steps_of_fewer_pairs(compute):
             trainer = SoftmaxTrainer(vertex, context, batch=size, compute=compute)
             got.append([trainer.step(pairs[:n], 1e-2).clone(), vertex, context])
         assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("compute", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [40, 600])
+def test_pairs_without_a_source_do_not_count(n, compute):
+    """A source outside of the tables (walks are padded with -1) leaves its pair out, as such a context does: its loss is 0, the others'
+    losses and both tables are those of a step in which its context is padding; a step of such pairs alone moves nothing."""
+    V, d = 700, 40
+    say("padded sources", n, compute)
+    gen = torch.Generator().manual_seed(9)
+    pairs = torch.randint(0, V, (n, 2), generator=gen).to(torch.int32)
+    out = torch.zeros(n, dtype=torch.bool)
+    for first, step, src in ((1, 5, -1), (2, 11, V), (3, 13, 2 ** 31 - 1), (4, 17, -2 ** 31)):
+        pairs[first::step, 0] = src
+        out[first::step] = True
+    both = pairs.clone()
+    both[out, 1] = -1
+    got = []
+    for p in (pairs, both):
+        vertex, context = tables(V, d, 10)
+        trainer = SoftmaxTrainer(vertex, context, batch=n, compute=compute)
+        got.append([trainer.step(p.to(DEV), 1e-2).clone(), vertex, context])
+    assert bool((got[0][0][out.to(DEV)] == 0).all()) and bool((got[0][0][~out.to(DEV)] > 0).all())
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    vertex, context = tables(V, d, 11)
+    before = vertex.clone(), context.clone()
+    trainer = SoftmaxTrainer(vertex, context, batch=n, compute=compute)
+    loss = trainer.step(pairs[out].to(DEV), 1e-2)
+    assert bool((loss == 0).all()) and torch.equal(vertex, before[0]) and torch.equal(context, before[1])
