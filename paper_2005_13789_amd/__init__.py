@@ -542,7 +542,7 @@ class AdamW:
 
     def __init__(self, handle: int, tensors, workspace: torch.Tensor):
         self.handle = handle
-        self.tensors = tensors
+        self.tensors = [ts if ts is None else list(ts) for ts in tensors]      # (lists of its own: the caller's may change)
         self.workspace = workspace
 
     def __del__(self):

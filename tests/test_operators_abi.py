@@ -1,5 +1,7 @@
 """Refusals of the full-softmax operators: every call below fails on the host before anything is enqueued."""
 import ctypes
+import gc
+import weakref
 
 import pytest
 import torch
@@ -114,3 +116,17 @@ def test_workspaces_serve_smaller_calls(V, d):
             assert need == sorted(need)
     need = [ne.ne_embed_workspace_bytes(V, d, n) for n in sizes + [2 ** 18, 270000, 2 ** 20]]
     assert need == sorted(need)
+
+
+def test_an_adamw_handle_keeps_its_tensors():
+    """The kernels hold the tensors' addresses: what the caller does to the lists afterwards must not free them."""
+    lists = [[torch.zeros(4), torch.zeros(5)] for _ in range(4)]
+    refs = [weakref.ref(t) for ts in lists for t in ts]
+    opt = ne.AdamW(None, (*lists, None, None, [None, torch.zeros(5)]), torch.zeros(8))
+    for ts in lists:
+        ts.clear()
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    del opt
+    gc.collect()
+    assert all(r() is None for r in refs)
