@@ -273,8 +273,8 @@ ne_status ne_adamw_step(ne_adamw* opt, int64_t step, float lr, float beta1, floa
 {
     if (!opt) return fail(NE_ERR_ARG, "ne_adamw_step: handle is NULL");
     if (step < 1 || step >= (1ll << 32)) return fail(NE_ERR_ARG, "ne_adamw_step: step outside [1, 2^32)");
-    if (!std::isfinite(lr) || !std::isfinite(grad_scale) || !std::isfinite(eps) || eps < 0.0f)
-        return fail(NE_ERR_ARG, "ne_adamw_step: lr, eps or grad_scale is not finite, or eps negative");
+    if (!std::isfinite(lr) || lr < 0.0f || !std::isfinite(grad_scale) || !std::isfinite(eps) || eps < 0.0f)
+        return fail(NE_ERR_ARG, "ne_adamw_step: lr, eps or grad_scale is not finite, or lr or eps negative");
     if (!(beta1 >= 0.0f && beta1 < 1.0f && beta2 >= 0.0f && beta2 < 1.0f)) return fail(NE_ERR_ARG, "ne_adamw_step: a beta is outside [0, 1)");
     StepArgs a{};
     a.tensors = opt->ws.tensors; a.units = opt->ws.units; a.step = static_cast<uint64_t>(step);

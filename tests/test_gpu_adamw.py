@@ -183,3 +183,19 @@ def test_a_nan_gradient_stays_in_its_block():
     bad = torch.isnan(p)
     assert int(bad.sum()) == 1 and bool(bad[300])
     assert torch.isnan(ms).tolist() == [False, True, False, False] and torch.isnan(vs).tolist() == [False, True, False, False]
+
+
+def test_step_refusals():
+    """What the header rules out is refused, and nothing moves."""
+    p, g = torch.ones(100, device=DEV), torch.ones(100, device=DEV)
+    m, v = torch.zeros(100, device=DEV), torch.zeros(100, device=DEV)
+    opt = ne.ne_create_adamw([p], [g], [m], [v], torch.empty(ne.ne_adamw_workspace_bytes([100]), dtype=torch.uint8, device=DEV))
+    nan, inf = float("nan"), float("inf")
+    for bad in (dict(step=0), dict(step=-1), dict(step=2 ** 32), dict(lr=-1e-3), dict(lr=nan), dict(lr=inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=nan),
+                dict(beta2=1.0), dict(beta2=-0.1), dict(eps=-1e-8), dict(eps=nan), dict(grad_scale=inf), dict(grad_scale=nan)):
+        with pytest.raises(ne.NeError):
+            ne.ne_adamw_step(opt, **(dict(step=1, lr=1e-3) | bad))
+    torch.cuda.synchronize()
+    assert bool((p == 1).all()) and bool((m == 0).all()) and bool((v == 0).all())
+    ne.ne_adamw_step(opt, 1, 0.0)       # (a rate of 0 is a step: the states move)
+    assert bool((p == 1).all()) and bool((m != 0).all()) and bool((v != 0).all())
