@@ -370,15 +370,17 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  * written whole (rows without a target: dh 0).  Both have the type of h and w; one of them may be NULL.
  *   lse_dev       : device, float[n], as ne_xent_loss wrote it for the same h, w and targets.
  *   loss_grad_dev : device, float[n]: the gradient of what is minimised in loss[i]; NULL = 1 for every row.
- *   scale         : finite; 1 / n for the mean over the rows.
+ *   scale         : finite; 1 / n for the mean over all rows, those without a target included.
  *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
  *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 1) bytes.
  * Precision.  NE_BF16: products of bf16 values with fp32 sums; loss_grad[i] (exp(s - lse) - [v == target]) is formed
  * in fp32 and, but where n is small, rounded to bf16 for its products; scale is applied in fp32.  NE_F32: where n is
  * small, products in fp32 or of operands split into three bf16 parts (24 bits); otherwise every operand is the sum of
- * two halves in fp16 (22 bits, at a common power of two that the largest finite magnitude sets), three products of
- * halves with fp32 sums: errors as those of fp32 products, for elements of at least 2^-24 of the largest magnitude of
- * their matrix; what is smaller counts to 2^-39 of it.
+ * two halves in fp16 at a common power of two that the largest finite magnitude of its matrix sets, three products of
+ * halves with fp32 sums: an element is off by up to 2^-22 of itself where it is at least 2^-16 of that magnitude, as an
+ * fp32 product about is, and by up to 2^-38 of that magnitude where it is smaller, so that one outlier takes bits from the
+ * rest of its matrix (for dw that of the rows loss_grad[i] h_i).  So is exp(s - lse) - [v == target]: 2^-22 of itself from
+ * 2^-16 on, 2^-39 below.
  * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN; in a row of w, all losses.
  *   1 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for the loss and writes zeros
  *   to dw.  Errors: NE_ERR_ARG, NE_ERR_HIP.

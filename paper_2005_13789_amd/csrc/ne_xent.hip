@@ -16,8 +16,9 @@
 // registers once (few_rows_kernel, few_grad_kernel).
 //
 // Types: bf16 operands go to the matrix cores as they are.  fp32 operands are split into two fp16 halves at a common
-// power of two, x 2^k = hi + lo with 22 bits, and a product is hi hi + hi lo + lo hi: the error of an fp32 product at
-// three matrix instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
+// power of two, x 2^k = hi + lo with 22 bits (of elements down to 2^-16 of the largest; smaller ones are off by up to 2^-38 of
+// it, fp16 ending there), and a product is hi hi + hi lo + lo hi: about the error of an fp32 product at three matrix
+// instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
 //
 // Bound by the matrix cores and by the loads from L2 that feed them.  Measured, 8192 rows, 200 003 of 512, bf16: loss
 // 1.7 to 1.8 ms (950 TF; a copy of the kernel without loads took 0.87 of the time, without exponentials 0.90, without
@@ -834,7 +835,7 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // G of a piece of the table
 // ---------------------------------------------------------------------------------------------
 // The scores again, with the exponentials written as operands of the next products instead of added up: bf16, of values at most 1 whose errors
-// of 2^-9 average out over the products' sums, or two fp16 halves of G 2^14, which keep 22 bits of 2^-14 and more.  8192 x 15 616 x 512 bf16: 169 us (0.78 PF,
+// of 2^-9 average out over the products' sums, or two fp16 halves of G 2^14, which keep 22 bits of 2^-16 and more (and 2^-39 of less).  8192 x 15 616 x 512 bf16: 169 us (0.78 PF,
 // 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
 struct CoefArgs {
     Operand w, h;                  // both by rows

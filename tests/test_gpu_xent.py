@@ -332,3 +332,66 @@ def test_the_same_every_time():
         first = call(h, w, t, fill=0)
         again = call(h, w, t, fill=255)
         assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def halves(x, floor):
+    """Largest error of x as the header states it: 2^-23 of the element, or `floor` of the matrix's largest magnitude."""
+    return torch.maximum(2.0 ** -23 * x.abs(), torch.full_like(x, floor * float(x.abs().max())))
+
+
+MIXED = ["plain", "outlier of w", "outlier of h", "small columns", "small rows", "small factors", "peaked"]
+
+
+@pytest.mark.parametrize("kind", MIXED)
+@pytest.mark.parametrize("n,V,d", [(16, 700, 96), (150, 900, 96), (200, 40000, 64)])
+def test_float32_magnitudes_mixed_in_a_matrix(n, V, d, kind):
+    """Bounds from the stated precision.  Halves: an element's error is 2^-23 of it, or 2^-38 of its matrix's largest magnitude, G's 2^-39 at
+    least; of the four products of halves the smallest, up to 2^-22 of the whole, is left out; a sum of k terms takes 3 k roundings.  Few
+    rows: no floors.  Every element is compared by itself, rows of the table that nobody's target names among them."""
+    say("mixed", n, V, d, kind)
+    few = n <= 32
+    u, floor_m, floor_g = 2.0 ** -24, 0.0 if few else 2.0 ** -38, 0.0 if few else 2.0 ** -39
+    h, w, t = make(n, V, d, torch.float32, n + V, ignored=0.1)
+    h, w, c = h.contiguous(), w.contiguous(), torch.ones(n, device=DEV)
+    if kind == "outlier of w":          # (a column that no row of H sees: the scores stay as they are)
+        h[:, 5] = 0.0
+        w[7, 5] = 2.0 ** 18
+    elif kind == "outlier of h":
+        w[:, 5] = 0.0
+        h[3, 5] = 2.0 ** 18
+        t[3] = 2
+    elif kind == "small columns":
+        h[:, 4:9] *= 2.0 ** -20
+        w[:, 11:13] *= 2.0 ** -22
+    elif kind == "small rows":
+        h[::3] *= 2.0 ** -20
+        w[1::3] *= 2.0 ** -22
+    elif kind == "small factors":
+        c[::2] = 2.0 ** -20
+    elif kind == "peaked":              # coefficients from 1 down to 2^-60 and less
+        h *= 6.0
+    loss, lse, dh, dw = call(h, w, t, loss_grad=c, scale=0.5)
+    H, W, T, C = h.double(), w.double(), t.long(), c.double()[:, None]
+    ok = ((T >= 0) & (T < V))[:, None]
+    H = torch.where(ok, H, 0.0)
+    eh, ew = halves(H, floor_m), halves(W, floor_m)
+    mm = lambda a, b: torch.mm(a.contiguous(), b.contiguous())  # noqa: E731
+    S, A = mm(H, W.t()), mm(H.abs(), W.abs().t())
+    z = torch.logsumexp(S, 1)[:, None]
+    at = T.clamp(0, V - 1)[:, None]
+    es = mm(eh, W.abs().t() + ew.t()) + mm(H.abs(), ew.t()) + (2.0 ** -22 + (3 * d + 32) * u) * A + 4 * u * (S.abs() + z.abs() + 1)
+    tol = 2 * es.max(1).values[:, None] + u * (V / 64 + 64)
+    for got, want, name in ((loss, z - S.gather(1, at), "loss"), (lse, z, "lse")):
+        e = (got.double()[:, None] - torch.where(ok, want, 0.0)).abs()
+        assert bool((e <= tol).all()), (name, float((e / tol).max()))
+    p = torch.exp(S - z)
+    G = torch.where(ok, p - torch.zeros_like(S).scatter_(1, at, 1.0), 0.0)
+    E = torch.where(ok, p * (1.01 * (es + tol) + 8 * u) + torch.clamp(2.0 ** -23 * G.abs(), min=floor_g), 0.0)
+    CH = C * H
+    ech = halves(CH, floor_m) + u * CH.abs()
+    for got, want, size, err, k, name in ((dh, mm(G, W) * C, mm(G.abs(), W.abs()) * C, (mm(E, W.abs() + ew) + mm(G.abs(), ew)) * C, V, "dh"),
+                                          (dw, mm(G.t(), CH), mm(G.abs().t(), CH.abs()), mm(E.t(), CH.abs() + ech) + mm(G.abs().t(), ech), n, "dw")):
+        bound = 0.5 * (err + (2.0 ** -22 + (3 * k + 64) * u) * size) * 1.01 + 1e-37
+        e = (got.double() - 0.5 * want).abs()
+        assert bool((e <= bound).all()), (name, float((e / bound).max()))
+        say("  ", name, "worst share of the bound", float((e / bound).max()))
