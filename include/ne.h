@@ -381,7 +381,10 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  * fp32 product about is, and by up to 2^-38 of that magnitude where it is smaller, so that one outlier takes bits from the
  * rest of its matrix (for dw that of the rows loss_grad[i] h_i).  So is exp(s - lse) - [v == target]: 2^-22 of itself from
  * 2^-16 on, 2^-39 below.
- * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN; in a row of w, all losses.
+ * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN.  A NaN in a row of w makes all losses NaN, and
+ * with NE_F32 an infinity does.  With NE_BF16 an infinity there makes a loss NaN, but where its row's score is minus infinity
+ * the loss may also be that of a row of probability 0 (which of the two depends on dim and alignment).  The gradients of a
+ * w that is not finite are not specified.
  *   1 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for the loss and writes zeros
  *   to dw.  Errors: NE_ERR_ARG, NE_ERR_HIP.
  */

@@ -395,3 +395,40 @@ def test_float32_magnitudes_mixed_in_a_matrix(n, V, d, kind):
         e = (got.double() - 0.5 * want).abs()
         assert bool((e <= bound).all()), (name, float((e / bound).max()))
         say("  ", name, "worst share of the bound", float((e / bound).max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,d", [(1, 50, 64), (14, 700, 90), (60, 300, 128), (140, 300, 64), (140, 300, 100), (300, 3000, 200), (1100, 60000, 400)])
+def test_infinities_and_nans_in_the_table(n, V, d, dtype):
+    """A NaN in w, and in float32 an infinity, makes every loss of a row with a target NaN.  In bfloat16 an infinity gives a row a score
+    of plus infinity (or NaN, against a zero): NaN; or of minus infinity: that table row counts as one of probability 0, or the loss
+    is NaN.  Rows without a target stay 0; nothing of it is left for the next call."""
+    say("infinities in w", n, V, d, dtype)
+    h, w, t = make(n, V, d, dtype, n + d, ignored=0.2 if n > 1 else 0.0)
+    at, col = V // 3, d - 3
+    if n > 1:
+        t[0] = at                   # its own score is the one that is not finite
+        h[1, col] = 0.0
+        t[1] = 2
+    ok = (t >= 0) & (t < V)
+    clean = call(h, w, t)
+    side = h[:, col].double()
+    rest = w.double().clone()
+    rest[at] = 0.0
+    S = torch.mm(h.double(), rest.t().contiguous())
+    S[:, at] = -float("inf")
+    z = torch.logsumexp(S, 1)
+    want = z - S.gather(1, t.long().clamp(0, V - 1)[:, None])[:, 0]        # (infinite where the target is that row)
+    for value in (float("inf"), -float("inf"), float("nan")):
+        bad = w.clone()
+        bad[at, col] = value
+        loss, lse, _, _ = call(h, bad, t)
+        assert bool((loss[~ok] == 0).all()) and bool((lse[~ok] == 0).all())
+        may = ok & (side * value < 0) if dtype == torch.bfloat16 else torch.zeros_like(ok)
+        assert bool(torch.isnan(loss[ok & ~may]).all()) and bool(torch.isnan(lse[ok & ~may]).all())
+        left = may & ~torch.isnan(loss)
+        say("  ", value, "rows that may go on without it", int(may.sum()), "that do", int(left.sum()))
+        assert bool(((lse.double() - z)[left].abs() <= 2e-5).all())
+        near = (loss.double() - want).abs() <= 2e-5
+        assert bool((near | (loss.double() == want))[left].all())
+    assert all(torch.equal(a, b) for a, b in zip(clean, call(h, w, t)))
