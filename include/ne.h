@@ -315,8 +315,9 @@ ne_status ne_score_pairs(const ne_tables* tables, const int32_t* pairs_dev, int6
  * takes (lookup of rows, softmax cross entropy against a whole table, the gradients of both, AdamW), each usable
  * by itself.  They take plain pointers and no tables handle.  Matrices are row-major with contiguous rows and a
  * row stride in elements; a type argument is an ne_dtype.  Sums are held in fp32 and every output is rounded
- * once.  All calls only enqueue kernels (no copies, no fills of other kinds), so they can be captured into a HIP
- * graph.  Unless it says otherwise a workspace is scratch of the caller: 256-byte aligned, overwritten, it needs
+ * once.  All calls but ne_create_adamw, which copies to the device and waits, only enqueue kernels (no copies, no fills
+ * of other kinds), so they can be captured into a HIP graph, which replays them with the arguments that they were
+ * captured with.  Unless it says otherwise a workspace is scratch of the caller: 256-byte aligned, overwritten, it needs
  * no initialisation and carries nothing between calls, and calls that overlap in time need one each.
  */
 typedef enum { NE_F32 = 0, NE_BF16 = 1 } ne_dtype;
@@ -415,7 +416,8 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
  *   workspace_dev : at least ne_adamw_workspace_bytes(tensors_host, n_tensors) bytes, caller-owned, written here
  *                   (the call returns after the copy) and read by every step until the handle is destroyed.
  *   1 <= n_tensors <= 65536.  tensors_host is read during the call only.
- * ne_adamw_step moves every tensor of the handle by one step in one launch.  step >= 1; lr, eps >= 0,
+ * ne_adamw_step moves every tensor of the handle by one step in one launch.  A captured step replays its own number: the
+ * learning rate, both corrections by beta^t and the random bits stay those of that step.  step >= 1; lr, eps >= 0,
  * beta1 and beta2 in [0, 1), grad_scale finite.  Errors: NE_ERR_ARG, NE_ERR_NOMEM, NE_ERR_HIP.
  */
 typedef struct ne_adamw ne_adamw;

@@ -199,3 +199,30 @@ def test_step_refusals():
     assert bool((p == 1).all()) and bool((m == 0).all()) and bool((v == 0).all())
     ne.ne_adamw_step(opt, 1, 0.0)       # (a rate of 0 is a step: the states move)
     assert bool((p == 1).all()) and bool((m != 0).all()) and bool((v != 0).all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_captured_step_replays_its_number(bits):
+    """Replays of a captured step 5 are eager steps of number 5 one after the other, whatever ran between them."""
+    numels = [5000, 700]
+    got = []
+    for captured in (False, True):
+        gen = torch.Generator().manual_seed(21)
+        p, g, m, v, ms, vs = tensors(numels, torch.float32, bits, 0, gen)
+        opt = ne.ne_create_adamw(p, g, m, v, torch.empty(ne.ne_adamw_workspace_bytes(numels), dtype=torch.uint8, device=DEV), m_scale=ms, v_scale=vs, seed=77)
+
+        def step():
+            ne.ne_adamw_step(opt, 5, 1e-2)
+
+        if captured:
+            stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph, stream=stream):
+                step()
+            step = graph.replay
+        for _ in range(4):
+            step()
+            torch.cuda.synchronize()
+            torch.mm(p[0].view(50, 100), p[0].view(100, 50))
+        got.append([t.float().cpu() for ts in (p, m, v, ms or [], vs or []) for t in ts])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
