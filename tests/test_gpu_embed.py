@@ -215,3 +215,83 @@ def test_on_a_stream_of_the_callers():
     ne.ne_embed_lookup(table, ids, out, scale=math.pi, stream=side)
     side.synchronize()
     assert torch.equal(out, table * np.float32(math.pi))
+
+
+def framed(n, d, dtype, pad, shift, value):
+    """A buffer filled with `value`, and its rows [n][d] of stride d + pad from element `shift` on."""
+    buf = torch.full((shift + n * (d + pad) + 8,), value, dtype=dtype, device=DEV)
+    return buf, buf[shift:shift + n * (d + pad)].view(n, d + pad)[:, :d]
+
+
+def assert_frame(buf, view, value):
+    """Everything in the buffer but the view's elements still holds `value`."""
+    kept = torch.ones(buf.numel(), dtype=torch.bool, device=DEV)
+    kept.as_strided(view.shape, view.stride(), view.storage_offset()).fill_(False)
+    assert bool((buf[kept] == value).all()), int((buf[kept] != value).sum())
+
+
+@pytest.mark.parametrize("to", TYPES)
+@pytest.mark.parametrize("d,pad,shift", [(1, 0, 1), (3, 2, 1), (7, 1, 0), (100, 0, 3), (129, 1, 3), (512, 8, 0), (1030, 3, 5)])
+def test_lookup_writes_its_rows_only(to, d, pad, shift):
+    gen = torch.Generator().manual_seed(d)
+    for ti in TYPES:
+        for n in (1, 517):
+            say("lookup in a frame", ti, to, d, pad, shift, n)
+            buf, out = framed(n, d, to, pad, shift, 7.0)
+            table, ids = rows(90, d, ti, gen), make_ids("edges", n, 90, gen).to(DEV)
+            ne.ne_embed_lookup(table, ids, out)
+            ok = ((ids >= 0) & (ids < 90))[:, None]
+            assert torch.equal(out, torch.where(ok, table[ids.long().clamp(0, 89)].to(to), 0.0))
+            assert_frame(buf, out, 7.0)
+
+
+def check_grad_here(ids, grad, got, scale, before):
+    """The bound of check_grad, on the GPU (before: what the table held, None for zeros), with fewer roundings where sums of 16, or of 256,
+    stand for terms of long runs: 16 for each such sum, 60 terms that are none, the rest of the run in their number, 256 lane groups' shares.
+    A row's sum is the difference of two running sums over the positions in the order of their ids, in 64 bits: off by 64 roundings of a
+    column's summed magnitudes at most."""
+    V, d = got.shape
+    n = ids.numel()
+    key = torch.where((ids >= 0) & (ids < V), ids, V).long()
+    order = torch.argsort(key, stable=True)
+    k = torch.bincount(key, minlength=V + 1)[:V]
+    end = torch.cumsum(k, 0)
+    g = grad[order[:int(end[-1])]].double() * float(np.float32(scale))
+
+    def sums(x):
+        run = torch.cat([torch.zeros(1, d, dtype=torch.float64, device=DEV), torch.cumsum(x, 0)])
+        return run[end] - run[end - k]
+
+    want, size = sums(g), sums(g.abs())
+    if before is not None:
+        want, size = want + before.double(), size + before.double().abs()
+    k = k.double()[:, None]
+    roundings = k + 2 if n <= 16384 else torch.minimum(k + 2, 350 + k / (16 if n <= 131072 else 256))
+    off = roundings * 2.0 ** -24 * size + 64 * 2.0 ** -53 * g.abs().sum(0)
+    bound = torch.where(k == 0, 0.0, off + U[got.dtype] * (want.abs() + off))
+    e = (got.double() - want).abs()
+    assert bool((e <= bound).all()), (int((~(e <= bound)).sum()), float((e - bound).max()))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1)])
+@pytest.mark.parametrize("n,V,d", [(5000, 900, 40), (16385, 70001, 33), (70001, 5003, 130), (140003, 3001, 257), (262144, 20011, 48), (131073, 200003, 5)])
+def test_gradient_of_large_batches(n, V, d, pad, shift, accumulate):
+    """Every sorting form with the table's clearing beside it, sums of 16 and of 256 positions, rows of one chunk and of several; rows side by
+    side and apart, the table holding NaN before it is overwritten.  What lies around the rows stays."""
+    gen = torch.Generator().manual_seed(n + d)
+    torch.manual_seed(n + V)
+    for kind in ("skewed", "edges", "one", "uniform"):
+        for tg, tt in ((torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+            say("large batch", n, V, d, pad, shift, accumulate, kind, tg, tt)
+            ids = make_ids(kind, n, V, gen).to(DEV)
+            grad = framed(n, d, tg, pad, shift, 0.0)[1]
+            grad.copy_(torch.randn(n, d, device=DEV) if kind == "uniform" else 0.5 + torch.rand(n, d, device=DEV))      # (a lost term of a long run shows)
+            buf, table = framed(V, d, tt, pad, shift, 7.0)
+            table.copy_(torch.randn(V, d, device=DEV) if accumulate else torch.full((V, d), float("nan"), device=DEV))
+            before = table.clone() if accumulate else None
+            work = torch.empty(ne.ne_embed_workspace_bytes(V, d, n), dtype=torch.uint8, device=DEV)
+            work.fill_(255)
+            ne.ne_embed_grad(ids, grad, table, work, scale=0.7, accumulate=accumulate)
+            check_grad_here(ids, grad, table, 0.7, before)
+            assert_frame(buf, table, 7.0)
