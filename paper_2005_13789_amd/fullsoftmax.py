@@ -57,7 +57,7 @@ class SoftmaxTrainer:
         if n < 1 or n > self.batch:
             raise ValueError(f"a step takes 1 to {self.batch} pairs")
         src = pairs[:, 0].contiguous()
-        ctx = torch.where((src >= 0) & (src < self.tables[0].shape[0]), pairs[:, 1], -1)
+        ctx = torch.where(src.clamp(0, self.tables[0].shape[0] - 1) == src, pairs[:, 1], -1)
         h, dh, loss, lse = self.h[:n], self.dh[:n], self.loss[:n], self.lse[:n]
         ne.ne_embed_lookup(self.rows[0], src, h)
         ne.ne_xent_loss(h, self.rows[1], ctx, loss, lse, self.work)
