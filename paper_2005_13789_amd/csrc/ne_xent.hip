@@ -2,7 +2,7 @@
 //
 //     S = H . W^T [n x V],   lse_i = log sum_v exp S_iv,   loss_i = lse_i - S_i,target
 //     G_iv = exp(S_iv - lse_i) - [v = target_i],   dH_i = scale c_i (G . W)_i,   dW = scale G^T . (c H)
-// (bf16: c_i is in G, which is rounded once; scale, the same for all, is applied in fp32 to the sums)
+// (bf16: c_i is in G, which is rounded once, but for dH the target's coefficient is whole; scale, the same for all, is applied in fp32 to the sums)
 //
 // Everything is a matrix product with something small around it, so the same loads to LDS, operand reads and matrix
 // instructions serve all three products; they differ in where their operands lie and in what becomes of the sums:
@@ -834,9 +834,12 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // ---------------------------------------------------------------------------------------------
 // G of a piece of the table
 // ---------------------------------------------------------------------------------------------
-// The scores again, with the exponentials written as operands of the next products instead of added up: bf16, of values at most 1 whose errors
-// of 2^-9 average out over the products' sums, or two fp16 halves of G 2^14, which keep 22 bits of 2^-16 and more (and 2^-39 of less).  8192 x 15 616 x 512 bf16: 169 us (0.78 PF,
-// 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
+// The scores again, with the exponentials written as operands of the next products instead of added up: bf16, each off by up to 2^-8 of
+// itself, or two fp16 halves of G 2^14, which keep 22 bits of 2^-16 and more (and 2^-39 of less).  By far the largest coefficient of most
+// rows is the target's.  What rounding takes from it in bf16 is kept and given back to dH, with the target's row of the table, when its
+// sums are rounded: dH's error is that of its own rounding then (0.0017 of it; 0.0021 without, and 0.013 where the table's rows share a part ten times
+// as large as what tells them apart, as a row's coefficients add up to nothing but their roundings do not).
+// 8192 x 15 616 x 512 bf16: 169 us (0.78 PF, 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
 struct CoefArgs {
     Operand w, h;                  // both by rows
     const int32_t* targets;
@@ -847,6 +850,7 @@ struct CoefArgs {
     uint32_t num_rows, row_base, row_tiles, splits, tokens;
     int32_t steps;
     uint16_t* g[2];                // [tokens][g_stride], table rows of the piece side by side
+    float* rest;                   // bf16 only: [tokens]  what rounding takes from the target's coefficient
 };
 
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -896,7 +900,13 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
                 for (int im = 0; im < MT; ++im)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (target[j] - lane_row0 == 32 * im + sum_row(i)) acc[im][j][i] -= P == 2 ? 0x1p14f : 1.0f;
+                        if (target[j] - lane_row0 == 32 * im + sum_row(i)) {
+                            acc[im][j][i] -= P == 2 ? 0x1p14f : 1.0f;
+                            if (P == 1) {
+                                const float g = acc[im][j][i] * c[j];
+                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - static_cast<float>(static_cast<bf16_t>(g));
+                            }
+                        }
             }
             if (row0 + 32 * MT > a.num_rows) {
                 const int left = static_cast<int>(a.num_rows - lane_row0);     // (the difference is small where both are not)
@@ -1051,7 +1061,8 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     }
 }
 
-// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us).  dH: rows without a target become zeros, the others take their factor.
+// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us).  dH: rows without a target become zeros, the others take their factor, or in bf16
+// what the target's coefficient lost.
 struct ReduceArgs {
     const float* in;               // [splits][rows_in][cols]
     int64_t split_stride;
@@ -1065,6 +1076,9 @@ struct ReduceArgs {
     const float* c;
     float scale;
     const int32_t* shift;          // fp32 only: power of two of the other operand
+    const float* rest;             // dH in bf16 only: what the targets' coefficients lost, ...
+    const bf16_t* w;               // ... and the table, whose rows of the targets take it
+    int64_t w_stride;
 };
 
 // A workgroup has 256 columns of a row; where there are many splits its wavefronts share them, and their sums are added in order.
@@ -1107,8 +1121,19 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
     const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
     const int k = a.shift ? -(*a.shift + kGShift) : 0;      // (bf16: the sums are what they are)
     const float c = counts && a.c ? a.c[r] : 1.0f;
-    const float all[4] = {sum.x, sum.y, sum.z, sum.w};
-    float x[4];
+    float all[4] = {sum.x, sum.y, sum.z, sum.w}, x[4];
+    if (a.rest && counts) {
+        const float rest = a.rest[r];
+        const bf16_t* w = a.w + a.targets[r] * a.w_stride + e;
+        if (e + 4 <= a.dim) {
+            load_vec<bf16_t, 4>(w, x);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = e + q < a.dim ? static_cast<float>(w[q]) : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) all[q] = fmaf(rest, x[q], all[q]);
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) x[q] = counts ? ldexpf(all[q], k) * a.scale * c : 0.0f;
     store_some<T, 4>(static_cast<T*>(a.out) + r * a.out_stride + e, a.dim - e, x);
@@ -1344,7 +1369,7 @@ struct XentWs {
     float2* stat;
     float* target_score;
     uint16_t* g[2];
-    float *dh, *dw;
+    float *dh, *dw, *rest;
     size_t total;
 };
 
@@ -1523,6 +1548,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
         }
         w.dh = take.get<float>(static_cast<size_t>(w.h_splits) * w.tokens * w.cols);
         w.dw = w.w_splits > 1 ? take.get<float>(static_cast<size_t>(w.w_splits) * w.piece * w.cols) : nullptr;
+        w.rest = w.parts == 1 ? take.get<float>(static_cast<size_t>(w.tokens)) : nullptr;
     }
     w.total = take.total();
     return w;
@@ -1554,7 +1580,7 @@ size_t xent_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool g
         bytes += std::min(rows * row_bytes, kGBytes + 256 * row_bytes);
         bytes += std::min(ceil_div(rows / step, kLeastShare) * tokens * cols, places + all_h) * 4;
         if (tokens / step > kLeastShare) bytes += std::min(ceil_div(tokens / step, kLeastShare) * rows * cols, places + std::min(all_w, places)) * 4;
-        bytes += w.parts == 2 ? 2 * tokens * padded * 2 : 0;
+        bytes += w.parts == 2 ? 2 * tokens * padded * 2 : tokens * 4;
     }
     return static_cast<size_t>(bytes + w.parts * 2 * padded * (tokens + num_rows));
 }
@@ -1707,7 +1733,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     hipError_t e = pack(x, w, true, &ca.h, &pa.h, &ca.w, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
-    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.c = x.c; ca.g_stride = w.piece;
+    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.c = x.c; ca.g_stride = w.piece; ca.rest = w.rest;
     ca.num_rows = static_cast<uint32_t>(x.num_rows); ca.steps = w.padded / step_of<P>();
     const int64_t side = w.large_scores ? 256 : 128, edge = w.large_products ? 256 : 128;
     const uint32_t token_tiles = static_cast<uint32_t>(ceil_div(w.tokens, side));
@@ -1769,6 +1795,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         ReduceArgs r{};
         r.in = w.dh; r.split_stride = w.tokens * pa.cols; r.splits = w.h_splits; r.rows = x.n; r.out = dh; r.out_stride = dh_stride;
         r.targets = x.targets; r.num_targets = ca.num_rows; r.c = P == 2 ? x.c : nullptr; r.shift = w.shift;
+        r.rest = w.rest; r.w = static_cast<const bf16_t*>(x.w); r.w_stride = x.w_stride;
         return reduce(r);
     }
     return hipSuccess;

@@ -432,3 +432,30 @@ def test_infinities_and_nans_in_the_table(n, V, d, dtype):
         near = (loss.double() - want).abs() <= 2e-5
         assert bool((near | (loss.double() == want))[left].all())
     assert all(torch.equal(a, b) for a, b in zip(clean, call(h, w, t)))
+
+
+@pytest.mark.parametrize("n,V,d,pad", [(100, 3000, 64, 0), (257, 1111, 257, 0), (300, 2000, 130, 3), (1100, 60000, 400, 0), (3000, 130000, 64, 0)])
+def test_rows_of_a_table_with_much_in_common(n, V, d, pad):
+    """bfloat16: a part that all rows of w share, ten times as large as what tells them apart, has no share in dh, as a row's coefficients
+    add up to nothing; their roundings must not bring it in.  Independent rounding errors of 2^-8 / sqrt(3) at most, relative: of every
+    coefficient but the target's, and of the output; twice their root mean square."""
+    gen = torch.Generator().manual_seed(n + d)
+    sd = d ** -0.25
+    w, common, t = torch.randn(V, d + pad, generator=gen) * sd, torch.randn(d + pad, generator=gen) * 10 * sd, torch.randint(0, V, (n,), generator=gen)
+    h = torch.randn(n, d + pad, generator=gen) * sd + 0.5 * w[t]
+    h -= (h @ common)[:, None] / (common @ common) * common         # (no row sees the common part: scores stay moderate)
+    h, w = h.bfloat16().to(DEV)[:, :d], (w + common).bfloat16().to(DEV)[:, :d]
+    t[::9] = -1
+    c = torch.rand(n, generator=gen).to(DEV) + 0.5
+    t = t.to(torch.int32).to(DEV)
+    dh = call(h, w, t, loss_grad=c, scale=1.0 / n)[2]
+    H, W, T = h.double(), w.double(), t.long()
+    ok, at = (T >= 0)[:, None], T.clamp(min=0)[:, None]
+    S = torch.mm(H, W.t().contiguous())
+    G = torch.where(ok, torch.exp(S - torch.logsumexp(S, 1)[:, None]) * c.double()[:, None] / n, 0.0)
+    others = G.scatter(1, at, 0.0)
+    G.scatter_add_(1, at, torch.where(ok, -c.double()[:, None] / n, 0.0))
+    want = torch.mm(G, W)
+    bar = 2 * 2.0 ** -8 / 3 ** 0.5 * (want.square().sum() + (others.square().sum(0) @ W.square()).sum()).sqrt()
+    say("common part", n, V, d, "share of the bar", float((dh.double() - want).norm() / bar), "relative error", float((dh.double() - want).norm() / want.norm()))
+    assert float((dh.double() - want).norm()) <= float(bar)
