@@ -85,10 +85,13 @@ struct Operand {
 // over: a stage is in flight while the one before it is multiplied.  They are written in assembly because the compiler waits for
 // loads of this kind before every LDS read that follows.  The address is a uniform base and a lane's offset, which stays the same
 // from stage to stage.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"     // (m0 is reserved: nothing is allocated to it, which is no reason not to name it)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Waits for all but the last LATER loads of this wavefront, and for the other wavefronts.
 template <int LATER = 0>
