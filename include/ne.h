@@ -374,9 +374,10 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  *   scale         : finite; 1 / n for the mean over all rows, those without a target included.
  *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
  *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 1) bytes.
- * Precision.  NE_BF16: products of bf16 values with fp32 sums; loss_grad[i] (exp(s - lse) - [v == target]) is formed
- * in fp32 and, but where n is small and for the target's share of dh, rounded to bf16 for its products (dw: an error of
- * about the size of the output's own rounding); scale is applied in fp32.  NE_F32: where n is
+ * Precision.  NE_BF16: products of bf16 values with fp32 sums; exp(s - lse) - [v == target] is formed in fp32 and, but
+ * where n is small, rounded for its products: for dw to 11 bits (2^-12 of itself from 2^-28 on, 2^-39 below), as are the
+ * rows loss_grad[i] h_i (below 2^-28 of the largest of them: 2^-38 of it), for dh to bf16, the target's excepted, which is
+ * whole; scale, and for dh loss_grad, are applied in fp32.  NE_F32: where n is
  * small, products in fp32 or of operands split into three bf16 parts (24 bits); otherwise every operand is the sum of
  * two halves in fp16 at a common power of two that the largest finite magnitude of its matrix sets, three products of
  * halves with fp32 sums: an element is off by up to 2^-22 of itself where it is at least 2^-16 of that magnitude, as an

@@ -2,7 +2,7 @@
 //
 //     S = H . W^T [n x V],   lse_i = log sum_v exp S_iv,   loss_i = lse_i - S_i,target
 //     G_iv = exp(S_iv - lse_i) - [v = target_i],   dH_i = scale c_i (G . W)_i,   dW = scale G^T . (c H)
-// (bf16: c_i is in G, which is rounded once, but for dH the target's coefficient is whole; scale, the same for all, is applied in fp32 to the sums)
+// (c_i is in the rows of H for dW and applied in fp32 to the sums of dH, scale to the sums of both)
 //
 // Everything is a matrix product with something small around it, so the same loads to LDS, operand reads and matrix
 // instructions serve all three products; they differ in where their operands lie and in what becomes of the sums:
@@ -15,7 +15,11 @@
 // With few rows of H all of it is bound by reading the table and writing its gradient, and other kernels let the table stream through
 // registers once (few_rows_kernel, few_grad_kernel).
 //
-// Types: bf16 operands go to the matrix cores as they are.  fp32 operands are split into two fp16 halves at a common
+// Types: bf16 operands go to the matrix cores as they are.  Their G is held in fp16, 11 bits in the place of bf16's 8: dW multiplies it with H in
+// fp16, which holds what bf16 does, and dH, whose table no pass turns into fp16, with W after it is rounded to bf16 in registers, but for the
+// target's coefficient, which dH takes whole.  So both gradients' errors are those of their own rounding (0.0017; with G in bf16 0.0021, and dH 0.013 where
+// the table's rows share a part ten times as large as what tells them apart: a row's coefficients add up to nothing, their roundings do not).
+// fp32 operands are split into two fp16 halves at a common
 // power of two, x 2^k = hi + lo with 22 bits (of elements down to 2^-16 of the largest; smaller ones are off by up to 2^-38 of
 // it, fp16 ending there), and a product is hi hi + hi lo + lo hi: about the error of an fp32 product at three matrix
 // instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
@@ -192,10 +196,19 @@ __device__ __forceinline__ s16x8 fragment(const unsigned char* lds, int part, in
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-template <int P>
+// What operands hold: as their parts say (one: bf16, two: fp16 halves), fp16, or the second one fp16 that becomes bf16 for its products.
+enum Kind { kPlain, kHalf, kToBf16 };
+
+__device__ __forceinline__ s16x8 to_bf16(s16x8 x)
+{
+    typedef float f32x8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(s16x8, __builtin_convertvector(__builtin_convertvector(__builtin_bit_cast(f16x8, x), f32x8), bf16x8));
+}
+
+template <int P, Kind K = kPlain>
 __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
 {
-    if (P == 1) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    if (P == 1 && K != kHalf) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
@@ -204,7 +217,7 @@ template <int W> __device__ __forceinline__ int first_row() { return static_cast
 template <int W> __device__ __forceinline__ int first_col() { return static_cast<int>(threadIdx.x >> 6) % (W / 2) * 64; }
 
 // acc[im][in] += A B^T over one stage.
-template <int P, int W, bool AROWS, bool BROWS>
+template <int P, int W, bool AROWS, bool BROWS, Kind K = kPlain>
 __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&acc)[W / 2][2])
 {
     constexpr int MT = W / 2, KK = step_of<P>() / 16;
@@ -223,22 +236,31 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
             for (int i = 0; i < 2; ++i) b[kk & 1][p][i] = fragment<P, W, BROWS>(B, p, n0 + 32 * i, kk);
         }
     };
+    // (in the middle of the products before: they have been read by then, and the other half hides it)
+    auto convert = [&](int kk) {
+        if (K == kToBf16)
+#pragma unroll
+            for (int in = 0; in < 2; ++in) b[kk & 1][0][in] = to_bf16(b[kk & 1][0][in]);
+    };
     read(0);
+    convert(0);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
         if (kk + 1 < KK) read(kk + 1);
         __builtin_amdgcn_sched_barrier(0);
         const int at = kk & 1;
 #pragma unroll
-        for (int im = 0; im < MT; ++im)
+        for (int im = 0; im < MT; ++im) {
+            if (im == MT / 2 && kk + 1 < KK) convert(kk + 1);
 #pragma unroll
             for (int in = 0; in < 2; ++in) {
-                acc[im][in] = mfma<P>(a[at][0][im], b[at][0][in], acc[im][in]);
+                acc[im][in] = mfma<P, K>(a[at][0][im], b[at][0][in], acc[im][in]);
                 if (P == 2) {
                     acc[im][in] = mfma<P>(a[at][0][im], b[at][P - 1][in], acc[im][in]);
                     acc[im][in] = mfma<P>(a[at][P - 1][im], b[at][0][in], acc[im][in]);
                 }
             }
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -294,11 +316,11 @@ __device__ __forceinline__ uint32_t lane_row() { return 4 * ((threadIdx.x & 63) 
 // ---------------------------------------------------------------------------------------------
 // Largest finite magnitudes, kAmaxBlocks of each: of W, of H's rows with a target, of the same rows times c_i.
 struct AmaxArgs {
-    const float* h;
-    const float* w;
+    const void* h;
+    const void* w;
     const int32_t* targets;
     const float* c;
-    int64_t h_stride, w_stride, n, num_rows;
+    int64_t h_stride, w_stride, n, num_rows, w_rows;        // w_rows: of W, 0 to leave it out
     int32_t dim;
     float* amax;        // [3][kAmaxBlocks]
 };
@@ -353,21 +375,22 @@ __device__ __forceinline__ void for_eights(const T* in, int64_t stride, int64_t 
 }
 
 // (Bound by memory: 84 284 rows of 452, 152 MB: 29 us, 5.2 TB/s.  A small table's 5 us are a launch.)
+template <class T>
 __global__ void __launch_bounds__(kThreads) amax_kernel(AmaxArgs a)
 {
     __shared__ float lds[4];
     float w = 0.0f, h = 0.0f, ch = 0.0f;
-    for_eights(a.w, a.w_stride, a.num_rows, a.dim, a.dim, [&](int64_t, int, const float (&x)[8]) {
+    for_eights(static_cast<const T*>(a.w), a.w_stride, a.w_rows, a.dim, a.dim, [&](int64_t, int, const T (&x)[8]) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) w = fmaxf(w, finite_abs(x[q]));
+        for (int q = 0; q < 8; ++q) w = fmaxf(w, finite_abs(static_cast<float>(x[q])));
     });
-    for_eights(a.h, a.h_stride, a.n, a.dim, a.dim, [&](int64_t i, int, const float (&x)[8]) {
+    for_eights(static_cast<const T*>(a.h), a.h_stride, a.n, a.dim, a.dim, [&](int64_t i, int, const T (&x)[8]) {
         if (static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) return;
         const float c = a.c ? a.c[i] : 1.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            h = fmaxf(h, finite_abs(x[q]));
-            ch = fmaxf(ch, finite_abs(c * x[q]));
+            h = fmaxf(h, finite_abs(static_cast<float>(x[q])));
+            ch = fmaxf(ch, finite_abs(c * static_cast<float>(x[q])));
         }
     });
     w = block_max(w, lds);
@@ -397,8 +420,8 @@ struct PackArgs {
     const float* c;                // NULL, or factors of the rows
     int32_t dim, padded;
     uint16_t* out[2];
-    const float* amax;             // fp32 only
-    int32_t* shift;                // fp32 only: receives the power of two
+    const float* amax;             // NULL: bf16 as it is; otherwise the largest magnitudes, for fp16 parts
+    int32_t* shift;                // receives their power of two
 };
 
 struct PackJobs {
@@ -412,7 +435,7 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(PackJobs jobs)
     typedef typename std::conditional<P == 2, float, bf16_t>::type T;
     __shared__ float lds[4];
     int k = 0;
-    if (P == 2) {
+    if (a.amax) {
         float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < kAmaxBlocks / kThreads; ++i) top = fmaxf(top, a.amax[i * kThreads + threadIdx.x]);
@@ -425,11 +448,11 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(PackJobs jobs)
         const float c = a.c ? a.c[r] : 1.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+            const float y = counts ? ldexpf(c * static_cast<float>(x[e]), k) : 0.0f;
+            const f16_t hi = static_cast<f16_t>(y);
             if constexpr (P == 1) {
-                out[0][e] = counts ? __builtin_bit_cast(short, x[e]) : 0;
+                out[0][e] = a.amax ? __builtin_bit_cast(short, hi) : counts ? __builtin_bit_cast(short, x[e]) : 0;
             } else {
-                const float y = counts ? ldexpf(c * x[e], k) : 0.0f;
-                const f16_t hi = static_cast<f16_t>(y);
                 out[0][e] = __builtin_bit_cast(short, hi);
                 out[1][e] = __builtin_bit_cast(short, static_cast<f16_t>(y - static_cast<float>(hi)));
             }
@@ -837,23 +860,21 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // ---------------------------------------------------------------------------------------------
 // G of a piece of the table
 // ---------------------------------------------------------------------------------------------
-// The scores again, with the exponentials written as operands of the next products instead of added up: bf16, each off by up to 2^-8 of
-// itself, or two fp16 halves of G 2^14, which keep 22 bits of 2^-16 and more (and 2^-39 of less).  By far the largest coefficient of most
-// rows is the target's.  What rounding takes from it in bf16 is kept and given back to dH, with the target's row of the table, when its
-// sums are rounded: dH's error is that of its own rounding then (0.0017 of it; 0.0021 without, and 0.013 where the table's rows share a part ten times
-// as large as what tells them apart, as a row's coefficients add up to nothing but their roundings do not).
+// The scores again, with the exponentials written as operands of the next products instead of added up: of bf16 tables G 2^14 in fp16, off by 2^-12 of
+// itself from 2^-28 on and by 2^-39 below; of fp32 ones two fp16 halves of it, which keep 22 bits of 2^-16 and more (and 2^-39 of less).  By far
+// the largest coefficient of most rows is the target's: what dH's product does not see of it in bf16 is kept, and given to dH with the target's row of the
+// table when its sums are rounded.
 // 8192 x 15 616 x 512 bf16: 169 us (0.78 PF, 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
 struct CoefArgs {
     Operand w, h;                  // both by rows
     const int32_t* targets;
     const int32_t* shift;
     const float* lse;
-    const float* c;                // bf16 only: NULL, or factors that G is rounded with (fp32: the rows of H have them)
     int64_t n, g_stride;
     uint32_t num_rows, row_base, row_tiles, splits, tokens;
     int32_t steps;
     uint16_t* g[2];                // [tokens][g_stride], table rows of the piece side by side
-    float* rest;                   // bf16 only: [tokens]  what rounding takes from the target's coefficient
+    float* rest;                   // bf16 only: [tokens]  what rounding to bf16 takes from the target's coefficient
 };
 
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -878,16 +899,14 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const float to_log2 = kLog2e * score_factor<P>(a.shift);
     uint32_t target[2];
-    float by[2], c[2];
+    float by[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
         target[j] = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
         if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
-        // (a row without a target: 2 to the minus infinity; halves: G 2^14)
-        const bool counts = target[j] != 0xFFFFFFFFu;
-        by[j] = counts ? fmaf(a.lse[token], kLog2e, P == 2 ? -static_cast<float>(kGShift) : 0.0f) : INFINITY;
-        c[j] = P == 1 && a.c && counts ? a.c[token] : 1.0f;
+        // (G 2^14; a row without a target: 2 to the minus infinity)
+        by[j] = target[j] != 0xFFFFFFFFu ? fmaf(a.lse[token], kLog2e, -static_cast<float>(kGShift)) : INFINITY;
     }
     all_scores<P, W, KS>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
@@ -904,10 +923,10 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (target[j] - lane_row0 == 32 * im + sum_row(i)) {
-                            acc[im][j][i] -= P == 2 ? 0x1p14f : 1.0f;
+                            acc[im][j][i] -= 0x1p14f;
                             if (P == 1) {
-                                const float g = acc[im][j][i] * c[j];
-                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - static_cast<float>(static_cast<bf16_t>(g));
+                                const float g = acc[im][j][i];
+                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - static_cast<float>(static_cast<bf16_t>(static_cast<float>(static_cast<f16_t>(g))));
                             }
                         }
             }
@@ -919,12 +938,6 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
                     for (int i = 0; i < 16; ++i)
                         if (32 * im + sum_row(i) >= left) acc[im][j][i] = 0.0f;
             }
-            if (P == 1 && a.c) {
-#pragma unroll
-                for (int im = 0; im < MT; ++im)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[im][j][i] *= c[j];
-            }
             const int64_t to = (static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31)) * a.g_stride + (row0 - a.row_base) + 8 * (lane >> 5);
 #pragma unroll
             for (int im = 0; im < MT; ++im)
@@ -934,13 +947,9 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const f32x4 x = {acc[im][j][4 * (q + r)], acc[im][j][4 * (q + r) + 1], acc[im][j][4 * (q + r) + 2], acc[im][j][4 * (q + r) + 3]};
-                        if constexpr (P == 1) {
-                            hi[r] = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
-                        } else {
-                            const f16x4 xh = __builtin_convertvector(x, f16x4);
-                            hi[r] = __builtin_bit_cast(u32x2, xh);
-                            lo[r] = __builtin_bit_cast(u32x2, __builtin_convertvector(x - __builtin_convertvector(xh, f32x4), f16x4));
-                        }
+                        const f16x4 xh = __builtin_convertvector(x, f16x4);
+                        hi[r] = __builtin_bit_cast(u32x2, xh);
+                        if constexpr (P == 2) lo[r] = __builtin_bit_cast(u32x2, __builtin_convertvector(x - __builtin_convertvector(xh, f32x4), f16x4));
                     }
                     *reinterpret_cast<u32x4*>(a.g[0] + to + 32 * im + 8 * q) = eight_of(hi[0], hi[1]);
                     if constexpr (P == 2) *reinterpret_cast<u32x4*>(a.g[1] + to + 32 * im + 8 * q) = eight_of(lo[0], lo[1]);
@@ -967,13 +976,15 @@ struct ProductArgs {
     uint32_t rows;                 // table rows of the piece that there are
     int32_t dim;
     float scale;
-    const int32_t* shift;          // fp32 only: power of two of the rows of H
+    const int32_t* shift;          // power of two of the rows of H
 };
 
 // Both products of a piece are one launch: either alone leaves places empty.  (8192 x 15 616 x 512 bf16, large tiles: 237 us, 1.1 PF; 4096 x 10 000 x
 // 128 fp32, small tiles: 72 us, 0.87 PF of half products.)
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
-template <int P, int W, bool GROWS>
+// (bf16: turning G from fp16 to bf16 in registers takes 3 to 4 % of the gradients' time, 8192 x 200 003 x 512 5210 -> 5400 us; W in fp16 would take a
+// pass over the table.)
+template <int P, int W, bool GROWS, Kind K>
 __device__ __forceinline__ void product_tile(const Operand& cols, const Operand& g, uint32_t col0, uint32_t row0, uint32_t s0, uint32_t s1,
                                              unsigned char* lds, f32x16 (&acc)[W / 2][2])
 {
@@ -989,7 +1000,7 @@ __device__ __forceinline__ void product_tile(const Operand& cols, const Operand&
             load_c.fetch(to);
             load_g.fetch(to + operand_bytes<W>());
         },
-        [&](const unsigned char* stage) { multiply<P, W, false, GROWS>(stage, acc); });
+        [&](const unsigned char* stage) { multiply<P, W, false, GROWS, K>(stage, acc); });
 }
 
 // Writes up to V values, the first `have` of them.
@@ -1020,11 +1031,11 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
     constexpr int R = rows_of<W>(), MT = W / 2;
     f32x16 acc[MT][2];
-    if (dh) product_tile<P, W, true>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
-    else product_tile<P, W, false>(a.h, a.g_cols, col * R, tile * R, s0, s1, lds, acc);
+    if (dh) product_tile<P, W, true, P == 1 ? kToBf16 : kPlain>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
+    else product_tile<P, W, false, P == 1 ? kHalf : kPlain>(a.h, a.g_cols, col * R, tile * R, s0, s1, lds, acc);
     const uint32_t row0 = tile * R + first_col<W>() + (lane & 31), col0 = col * R + first_row<W>() + 4 * (lane >> 5);
     if (!dh && !a.dw) {
-        const int k = P == 2 ? -(*a.shift + kGShift) : 0;
+        const int k = -(*a.shift + kGShift);
         typedef typename std::conditional<P == 2, float, bf16_t>::type T;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -1036,7 +1047,7 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
                 for (int q = 0; q < 4; ++q) {
                     float x[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = (P == 2 ? ldexpf(acc[im][j][4 * q + e], k) : acc[im][j][4 * q + e]) * a.scale;
+                    for (int e = 0; e < 4; ++e) x[e] = ldexpf(acc[im][j][4 * q + e], k) * a.scale;
                     store_some<T, 4>(to + 32 * im + 8 * q, a.dim - static_cast<int>(col0 + 32 * im + 8 * q), x);
                 }
         }
@@ -1078,7 +1089,7 @@ struct ReduceArgs {
     uint32_t num_targets;
     const float* c;
     float scale;
-    const int32_t* shift;          // fp32 only: power of two of the other operand
+    const int32_t* shift;          // NULL, or power of two of the other operand
     const float* rest;             // dH in bf16 only: what the targets' coefficients lost, ...
     const bf16_t* w;               // ... and the table, whose rows of the targets take it
     int64_t w_stride;
@@ -1122,7 +1133,7 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
     }
     if (!in) return;
     const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
-    const int k = a.shift ? -(*a.shift + kGShift) : 0;      // (bf16: the sums are what they are)
+    const int k = -((a.shift ? *a.shift : 0) + kGShift);
     const float c = counts && a.c ? a.c[r] : 1.0f;
     float all[4] = {sum.x, sum.y, sum.z, sum.w}, x[4];
     if (a.rest && counts) {
@@ -1546,7 +1557,7 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     } else {
         choose_pieces(w, n, num_rows, dim);
         for (int p = 0; p < w.parts; ++p) {
-            w.hc[p] = w.parts == 2 ? take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded) : nullptr;
+            w.hc[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.padded);
             w.g[p] = take.get<uint16_t>(static_cast<size_t>(w.tokens) * w.piece);
         }
         w.dh = take.get<float>(static_cast<size_t>(w.h_splits) * w.tokens * w.cols);
@@ -1583,7 +1594,7 @@ size_t xent_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool g
         bytes += std::min(rows * row_bytes, kGBytes + 256 * row_bytes);
         bytes += std::min(ceil_div(rows / step, kLeastShare) * tokens * cols, places + all_h) * 4;
         if (tokens / step > kLeastShare) bytes += std::min(ceil_div(tokens / step, kLeastShare) * rows * cols, places + std::min(all_w, places)) * 4;
-        bytes += w.parts == 2 ? 2 * tokens * padded * 2 : tokens * 4;
+        bytes += w.parts * tokens * padded * 2 + (w.parts == 1 ? tokens * 4 : 0);
     }
     return static_cast<size_t>(bytes + w.parts * 2 * padded * (tokens + num_rows));
 }
@@ -1605,23 +1616,26 @@ struct XentCall {
 };
 
 // Packs H (and c H) and, where it cannot be used as it is, W.
-hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Operand* hc, Operand* wo, hipStream_t st)
+// With dw, c H or H for its product: in fp32 halves, and in bf16 one fp16 part each, too.
+hipError_t pack(const XentCall& x, const XentWs& w, bool dw, Operand* h, Operand* hc, Operand* wo, hipStream_t st)
 {
     const bool direct = x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && x.w_stride < kMostStride && aligned(x.w, 16);
-    if (x.type == NE_F32) {
-        AmaxArgs a{static_cast<const float*>(x.h), static_cast<const float*>(x.w), x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, x.dim, w.amax};
-        hipLaunchKernelGGL(amax_kernel, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
+    const bool f32 = x.type == NE_F32;
+    if (f32 || dw) {
+        AmaxArgs a{x.h, x.w, x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, f32 ? x.num_rows : 0, x.dim, w.amax};
+        if (f32) hipLaunchKernelGGL(amax_kernel<float>, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL(amax_kernel<bf16_t>, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     PackJobs jobs{};
     int count = 0;
     int64_t most = 0;
-    auto add = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which) {
+    auto add = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which, bool halves) {
         PackArgs& a = jobs.job[count++];
         a.in = in; a.in_stride = stride; a.rows = rows; a.padded_rows = padded_rows; a.targets = targets;
         a.num_targets = static_cast<uint32_t>(x.num_rows); a.c = c; a.dim = x.dim; a.padded = w.padded;
-        a.out[0] = out[0]; a.out[1] = out[1]; a.amax = w.amax + which * kAmaxBlocks; a.shift = w.shift + which;
+        a.out[0] = out[0]; a.out[1] = out[1]; a.amax = halves ? w.amax + which * kAmaxBlocks : nullptr; a.shift = w.shift + which;
         most = std::max(most, padded_rows);
     };
     auto operand = [&](uint16_t* const* part, int64_t rows) {
@@ -1629,11 +1643,11 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Opera
         o.part[0] = part[0]; o.part[1] = part[1]; o.stride = w.padded; o.last = static_cast<uint32_t>(rows - 1); o.width = static_cast<uint32_t>(w.padded);
         return o;
     };
-    add(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1);
+    add(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1, f32);
     *h = operand(w.h, w.tokens);
     *hc = *h;
-    if (grad && x.type == NE_F32 && x.c) {
-        add(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, 2);
+    if (dw && (!f32 || x.c)) {
+        add(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, x.c ? 2 : 1, true);
         *hc = operand(w.hc, w.tokens);
     }
     *wo = operand(w.w, x.num_rows);
@@ -1642,7 +1656,7 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool grad, Operand* h, Opera
         wo->stride = x.w_stride;
         wo->width = static_cast<uint32_t>(x.dim);
     } else {
-        add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
+        add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0, f32);
     }
     int lanes = 1;      // of a row, as in the kernel; four rows of a lane group in flight
     while (lanes < 64 && 8 * lanes < w.padded) lanes *= 2;
@@ -1733,10 +1747,10 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
 {
     CoefArgs ca{};
     ProductArgs pa{};
-    hipError_t e = pack(x, w, true, &ca.h, &pa.h, &ca.w, st);
+    hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
-    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.c = x.c; ca.g_stride = w.piece; ca.rest = w.rest;
+    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.g_stride = w.piece; ca.rest = w.rest;
     ca.num_rows = static_cast<uint32_t>(x.num_rows); ca.steps = w.padded / step_of<P>();
     const int64_t side = w.large_scores ? 256 : 128, edge = w.large_products ? 256 : 128;
     const uint32_t token_tiles = static_cast<uint32_t>(ceil_div(w.tokens, side));
@@ -1747,7 +1761,6 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     pa.out_stride = dw_stride; pa.dim = x.dim; pa.scale = scale; pa.shift = w.shift + (x.c ? 2 : 1);
     auto reduce = [&](ReduceArgs r) {
         r.cols = pa.cols; r.dim = x.dim; r.scale = scale;
-        if (P == 1) r.shift = nullptr;
         const dim3 grid(static_cast<unsigned>(ceil_div(r.rows, r.splits >= 16 ? 1 : 4)), static_cast<unsigned>(ceil_div(x.dim, 256)));
         hipLaunchKernelGGL(reduce_kernel<T>, grid, dim3(kThreads), 0, st, r);
         return hipGetLastError();
@@ -1797,7 +1810,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
     if (dh) {
         ReduceArgs r{};
         r.in = w.dh; r.split_stride = w.tokens * pa.cols; r.splits = w.h_splits; r.rows = x.n; r.out = dh; r.out_stride = dh_stride;
-        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = P == 2 ? x.c : nullptr; r.shift = w.shift;
+        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = x.c; r.shift = P == 2 ? w.shift : nullptr;
         r.rest = w.rest; r.w = static_cast<const bf16_t*>(x.w); r.w_stride = x.w_stride;
         return reduce(r);
     }

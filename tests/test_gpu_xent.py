@@ -459,3 +459,33 @@ def test_rows_of_a_table_with_much_in_common(n, V, d, pad):
     bar = 2 * 2.0 ** -8 / 3 ** 0.5 * (want.square().sum() + (others.square().sum(0) @ W.square()).sum()).sqrt()
     say("common part", n, V, d, "share of the bar", float((dh.double() - want).norm() / bar), "relative error", float((dh.double() - want).norm() / want.norm()))
     assert float((dh.double() - want).norm()) <= float(bar)
+
+
+@pytest.mark.parametrize("factors", [False, True])
+@pytest.mark.parametrize("n,V,d,pad", [(100, 3000, 64, 0), (257, 1111, 257, 0), (300, 2000, 130, 3), (1100, 60000, 400, 0), (3000, 130000, 64, 0), (2000, 700, 512, 0)])
+def test_dw_in_bfloat16_is_nearly_the_rounded_one(n, V, d, pad, factors):
+    """dw against the 64-bit one rounded to bfloat16: they differ where an error reaches across the edge of two values, which an error e does
+    with probability |e| / spacing and which then makes a whole spacing, so that the squared difference is e times the spacing, 2^-7 of the
+    value at most.  e is the root mean square of rounding errors of 2^-12 / sqrt(3), relative, of coefficients and, with factors, of rows times
+    these; one and a half times the whole."""
+    gen = torch.Generator().manual_seed(n + d)
+    sd = d ** -0.25
+    w, t = torch.randn(V, d + pad, generator=gen) * sd, torch.randint(0, V, (n,), generator=gen)
+    h = (torch.randn(n, d + pad, generator=gen) * sd + 0.5 * w[t]).bfloat16().to(DEV)[:, :d]
+    w = w.bfloat16().to(DEV)[:, :d]
+    t[::9] = -1
+    t = t.to(torch.int32).to(DEV)
+    c = torch.rand(n, generator=gen).to(DEV) + 0.5 if factors else None
+    dw = call(h, w, t, loss_grad=c, scale=1.0 / n)[3].double()
+    H, T = h.double(), t.long()
+    ok, at = (T >= 0)[:, None], T.clamp(min=0)[:, None]
+    S = torch.mm(H, w.double().t().contiguous())
+    G = torch.exp(S - torch.logsumexp(S, 1)[:, None]).scatter_add_(1, at, torch.full((n, 1), -1.0, dtype=torch.float64, device=DEV))
+    G = torch.where(ok, G, 0.0).t().contiguous()
+    CH = H / n if c is None else H * c.double()[:, None] / n
+    want = torch.mm(G, CH)
+    e = 2.0 ** -12 / 3 ** 0.5 * ((2 if factors else 1) * torch.mm(G.square(), CH.square())).sqrt()
+    bar = 1.5 * (2.0 ** -7 * want.abs() * e).sum().sqrt()
+    off = (dw - want.bfloat16().double()).norm()
+    say("dw", n, V, d, "share of the bar", float(off / bar), "of dw", float(off / want.norm()), "error", float((dw - want).norm() / want.norm()))
+    assert float(off) <= float(bar)
