@@ -51,7 +51,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kAmaxBlocks = 1024;
+constexpr int kAmaxBlocks = 1024, kMostPack = 2048;      // (bf16: each of the packing workgroups leaves a maximum, in the room of three times 1024)
+static_assert(kMostPack <= 3 * kAmaxBlocks);
 constexpr int64_t kMostStride = 1 << 22;   // elements: a tile's 256 rows are within 32 bits of its first
 constexpr int kFewBytes = 65536, kFewBytesAlone = 153600;     // LDS of H for the loss: of a workgroup of 4 wavefronts, and of one of 8 that is alone on its CU
 constexpr int kFewGroups = 1024;
@@ -316,11 +317,11 @@ __device__ __forceinline__ uint32_t lane_row() { return 4 * ((threadIdx.x & 63) 
 // ---------------------------------------------------------------------------------------------
 // Largest finite magnitudes, kAmaxBlocks of each: of W, of H's rows with a target, of the same rows times c_i.
 struct AmaxArgs {
-    const void* h;
-    const void* w;
+    const float* h;
+    const float* w;
     const int32_t* targets;
     const float* c;
-    int64_t h_stride, w_stride, n, num_rows, w_rows;        // w_rows: of W, 0 to leave it out
+    int64_t h_stride, w_stride, n, num_rows;
     int32_t dim;
     float* amax;        // [3][kAmaxBlocks]
 };
@@ -331,6 +332,7 @@ __device__ __forceinline__ float finite_abs(float x)
     return x < INFINITY ? x : 0.0f;     // (false for a NaN)
 }
 
+template <int THREADS = kThreads>
 __device__ __forceinline__ float block_max(float v, float* lds)
 {
 #pragma unroll
@@ -338,7 +340,9 @@ __device__ __forceinline__ float block_max(float v, float* lds)
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) v = fmaxf(v, lds[w]);
+    return v;
 }
 
 // Eight elements from index e on, zeros beyond dim.
@@ -354,14 +358,14 @@ __device__ __forceinline__ void load_eight(const T* row, int e, int dim, T (&x)[
 }
 
 // Rows of `dim` elements, eight a lane: use(row, e, x) for a lane group's rows, two of them in flight.
-template <class T, class Use>
-__device__ __forceinline__ void for_eights(const T* in, int64_t stride, int64_t rows, int dim, int width, Use use)
+template <int THREADS = kThreads, class T, class Use>
+__device__ __forceinline__ void for_eights(const T* in, int64_t stride, int64_t rows, int dim, int width, uint32_t block, uint32_t blocks, Use use)
 {
     int lanes_log2 = 0;
     while (lanes_log2 < 6 && (8 << lanes_log2) < width) ++lanes_log2;
     const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int64_t groups = static_cast<int64_t>(gridDim.x) * (kThreads >> lanes_log2);
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
+    const int64_t groups = static_cast<int64_t>(blocks) * (THREADS >> lanes_log2);
+    const int64_t first = static_cast<int64_t>(block) * (THREADS >> lanes_log2) + (threadIdx.x >> lanes_log2);
     for (int e = lane * 8; e < width; e += 8 * lanes)
         for (int64_t r = first; r < rows; r += 4 * groups) {
             T x[4][8];
@@ -375,22 +379,21 @@ __device__ __forceinline__ void for_eights(const T* in, int64_t stride, int64_t 
 }
 
 // (Bound by memory: 84 284 rows of 452, 152 MB: 29 us, 5.2 TB/s.  A small table's 5 us are a launch.)
-template <class T>
 __global__ void __launch_bounds__(kThreads) amax_kernel(AmaxArgs a)
 {
     __shared__ float lds[4];
     float w = 0.0f, h = 0.0f, ch = 0.0f;
-    for_eights(static_cast<const T*>(a.w), a.w_stride, a.w_rows, a.dim, a.dim, [&](int64_t, int, const T (&x)[8]) {
+    for_eights(a.w, a.w_stride, a.num_rows, a.dim, a.dim, blockIdx.x, gridDim.x, [&](int64_t, int, const float (&x)[8]) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) w = fmaxf(w, finite_abs(static_cast<float>(x[q])));
+        for (int q = 0; q < 8; ++q) w = fmaxf(w, finite_abs(x[q]));
     });
-    for_eights(static_cast<const T*>(a.h), a.h_stride, a.n, a.dim, a.dim, [&](int64_t i, int, const T (&x)[8]) {
+    for_eights(a.h, a.h_stride, a.n, a.dim, a.dim, blockIdx.x, gridDim.x, [&](int64_t i, int, const float (&x)[8]) {
         if (static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) return;
         const float c = a.c ? a.c[i] : 1.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            h = fmaxf(h, finite_abs(static_cast<float>(x[q])));
-            ch = fmaxf(ch, finite_abs(c * static_cast<float>(x[q])));
+            h = fmaxf(h, finite_abs(x[q]));
+            ch = fmaxf(ch, finite_abs(c * x[q]));
         }
     });
     w = block_max(w, lds);
@@ -420,52 +423,67 @@ struct PackArgs {
     const float* c;                // NULL, or factors of the rows
     int32_t dim, padded;
     uint16_t* out[2];
-    const float* amax;             // NULL: bf16 as it is; otherwise the largest magnitudes, for fp16 parts
+    const float* amax;             // NULL: bf16 as it is (factors aside); otherwise `maxima` largest magnitudes, for fp16 parts
     int32_t* shift;                // receives their power of two
+    int32_t maxima;
+    float* amax_out;               // NULL, or where every workgroup leaves the largest magnitude of its rows times their factors
 };
 
 struct PackJobs {
     PackArgs job[3];
 };
 
-template <int P>
-__global__ void __launch_bounds__(kThreads) pack_kernel(PackJobs jobs)
+template <int P, int THREADS>
+__device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uint32_t blocks, float* lds)
 {
-    const PackArgs& a = jobs.job[blockIdx.y];
     typedef typename std::conditional<P == 2, float, bf16_t>::type T;
-    __shared__ float lds[4];
     int k = 0;
     if (a.amax) {
         float top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kAmaxBlocks / kThreads; ++i) top = fmaxf(top, a.amax[i * kThreads + threadIdx.x]);
-        k = shift_of(block_max(top, lds));
-        if (blockIdx.x == 0 && threadIdx.x == 0) *a.shift = k;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < a.maxima; i += THREADS) top = fmaxf(top, a.amax[i]);
+        k = shift_of(block_max<THREADS>(top, lds));
+        if (block == 0 && threadIdx.x == 0) *a.shift = k;
     }
+    float largest = 0.0f;
     auto write = [&](int64_t r, int e0, const T (&x)[8]) {
-        s16x8 out[P];
+        s16x8 out[P] = {};
         const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
         const float c = a.c ? a.c[r] : 1.0f;
+        if (P == 2 || a.amax) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = counts ? ldexpf(c * static_cast<float>(x[e]), k) : 0.0f;
-            const f16_t hi = static_cast<f16_t>(y);
-            if constexpr (P == 1) {
-                out[0][e] = a.amax ? __builtin_bit_cast(short, hi) : counts ? __builtin_bit_cast(short, x[e]) : 0;
-            } else {
+            for (int e = 0; e < 8; ++e) {
+                const float y = counts ? ldexpf(c * static_cast<float>(x[e]), k) : 0.0f;
+                const f16_t hi = static_cast<f16_t>(y);
                 out[0][e] = __builtin_bit_cast(short, hi);
-                out[1][e] = __builtin_bit_cast(short, static_cast<f16_t>(y - static_cast<float>(hi)));
+                if constexpr (P == 2) out[1][e] = __builtin_bit_cast(short, static_cast<f16_t>(y - static_cast<float>(hi)));
             }
+        } else if (counts) {
+            __builtin_memcpy(&out[0], x, 16);
+            if (a.amax_out)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) largest = fmaxf(largest, finite_abs(c * static_cast<float>(x[e])));
         }
 #pragma unroll
         for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + r * a.padded + e0) = out[p];
     };
-    for_eights(static_cast<const T*>(a.in), a.in_stride, a.rows, a.dim, a.padded, write);
+    for_eights<THREADS>(static_cast<const T*>(a.in), a.in_stride, a.rows, a.dim, a.padded, block, blocks, write);
     // rows beyond the last one: zeros
     const int64_t zeros = (a.padded_rows - a.rows) * a.padded / 8;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < zeros; i += static_cast<int64_t>(gridDim.x) * kThreads)
+    for (int64_t i = static_cast<int64_t>(block) * THREADS + threadIdx.x; i < zeros; i += static_cast<int64_t>(blocks) * THREADS)
 #pragma unroll
         for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + a.rows * a.padded + i * 8) = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    if (P == 1 && a.amax_out) {
+        largest = block_max<THREADS>(largest, lds);
+        if (threadIdx.x == 0) a.amax_out[block] = largest;
+    }
+}
+
+template <int P>
+__global__ void __launch_bounds__(kThreads) pack_kernel(PackJobs jobs)
+{
+    __shared__ float lds[kThreads / 64];
+    pack_rows<P, kThreads>(jobs.job[blockIdx.y], blockIdx.x, gridDim.x, lds);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -874,6 +892,9 @@ struct CoefArgs {
     uint32_t num_rows, row_base, row_tiles, splits, tokens;
     int32_t steps;
     uint16_t* g[2];                // [tokens][g_stride], table rows of the piece side by side
+    uint32_t blocks;               // workgroups that make G; bf16: further ones of the first piece bring c H into fp16 (1000 x 3000 x 64: 37 us with a
+                                   // launch of its own, 32 so)
+    PackArgs hc;
     float* rest;                   // bf16 only: [tokens]  what rounding to bf16 takes from the target's coefficient
 };
 
@@ -893,9 +914,13 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
     constexpr int R = rows_of<W>(), MT = W / 2;
+    if (P == 1 && blockIdx.x >= a.blocks) {
+        pack_rows<1, 64 * W>(a.hc, blockIdx.x - a.blocks, gridDim.x - a.blocks, reinterpret_cast<float*>(lds));
+        return;
+    }
     const int lane = threadIdx.x & 63, m0 = first_row<W>(), n0 = first_col<W>();
     uint32_t token_tile, split;
-    pair_of(by_xcd(blockIdx.x, gridDim.x), (a.tokens + R - 1) / R, a.splits, token_tile, split);
+    pair_of(by_xcd(blockIdx.x, a.blocks), (a.tokens + R - 1) / R, a.splits, token_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const float to_log2 = kLog2e * score_factor<P>(a.shift);
     uint32_t target[2];
@@ -982,8 +1007,8 @@ struct ProductArgs {
 // Both products of a piece are one launch: either alone leaves places empty.  (8192 x 15 616 x 512 bf16, large tiles: 237 us, 1.1 PF; 4096 x 10 000 x
 // 128 fp32, small tiles: 72 us, 0.87 PF of half products.)
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
-// (bf16: turning G from fp16 to bf16 in registers takes 3 to 4 % of the gradients' time, 8192 x 200 003 x 512 5210 -> 5400 us; W in fp16 would take a
-// pass over the table.)
+// (bf16: turning G from fp16 to bf16 in registers takes up to 4 % of the gradients' time, 8192 x 200 003 x 512 5180 -> 5370 us; W in fp16 would
+// take a pass over the table.)
 template <int P, int W, bool GROWS, Kind K>
 __device__ __forceinline__ void product_tile(const Operand& cols, const Operand& g, uint32_t col0, uint32_t row0, uint32_t s0, uint32_t s1,
                                              unsigned char* lds, f32x16 (&acc)[W / 2][2])
@@ -1106,6 +1131,23 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
     const int e = blockIdx.y * 256 + lane * 4;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const bool in = r < a.rows && e < static_cast<int>(a.cols);
+    bool counts = in;
+    float c = 1.0f, rest = 0.0f, x[4] = {};
+    if (in && a.targets) {      // (fetched ahead of the sums)
+        const uint32_t target = static_cast<uint32_t>(a.targets[r]);
+        counts = target < a.num_targets;
+        if (counts && a.c) c = a.c[r];
+        if (counts && a.rest) {
+            rest = a.rest[r];
+            const bf16_t* w = a.w + target * a.w_stride + e;
+            if (e + 4 <= a.dim) {
+                load_vec<bf16_t, 4>(w, x);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = e + q < a.dim ? static_cast<float>(w[q]) : 0.0f;
+            }
+        }
+    }
     if (in) {
         const float* from = a.in + r * a.cols + e;
         const uint32_t step = parts;
@@ -1132,24 +1174,10 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
         }
     }
     if (!in) return;
-    const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
     const int k = -((a.shift ? *a.shift : 0) + kGShift);
-    const float c = counts && a.c ? a.c[r] : 1.0f;
-    float all[4] = {sum.x, sum.y, sum.z, sum.w}, x[4];
-    if (a.rest && counts) {
-        const float rest = a.rest[r];
-        const bf16_t* w = a.w + a.targets[r] * a.w_stride + e;
-        if (e + 4 <= a.dim) {
-            load_vec<bf16_t, 4>(w, x);
-        } else {
+    const float all[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = e + q < a.dim ? static_cast<float>(w[q]) : 0.0f;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) all[q] = fmaf(rest, x[q], all[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = counts ? ldexpf(all[q], k) * a.scale * c : 0.0f;
+    for (int q = 0; q < 4; ++q) x[q] = counts ? ldexpf(a.rest ? fmaf(rest, x[q], all[q]) : all[q], k) * a.scale * c : 0.0f;
     store_some<T, 4>(static_cast<T*>(a.out) + r * a.out_stride + e, a.dim - e, x);
 }
 
@@ -1615,27 +1643,35 @@ struct XentCall {
     const float* c;
 };
 
-// Packs H (and c H) and, where it cannot be used as it is, W.
-// With dw, c H or H for its product: in fp32 halves, and in bf16 one fp16 part each, too.
-hipError_t pack(const XentCall& x, const XentWs& w, bool dw, Operand* h, Operand* hc, Operand* wo, hipStream_t st)
+// Workgroups of `threads` that pack `rows` rows: of a row's lanes, as in the kernel, four rows of a lane group in flight.
+uint32_t pack_blocks(const XentWs& w, int64_t rows, int threads, int64_t most)
+{
+    int lanes = 1;
+    while (lanes < 64 && 8 * lanes < w.padded) lanes *= 2;
+    return static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * (threads / lanes)), most)));
+}
+
+// Packs H and, where it cannot be used as it is, W.  With dw, c H for its product, too: in fp32 its halves, if there are factors; in bf16 it is to be
+// fp16, which `later` says how, as its largest magnitude is found here.
+hipError_t pack(const XentCall& x, const XentWs& w, bool dw, Operand* h, Operand* hc, Operand* wo, PackArgs* later, hipStream_t st)
 {
     const bool direct = x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && x.w_stride < kMostStride && aligned(x.w, 16);
     const bool f32 = x.type == NE_F32;
-    if (f32 || dw) {
-        AmaxArgs a{x.h, x.w, x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, f32 ? x.num_rows : 0, x.dim, w.amax};
-        if (f32) hipLaunchKernelGGL(amax_kernel<float>, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(amax_kernel<bf16_t>, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
+    if (f32) {
+        AmaxArgs a{static_cast<const float*>(x.h), static_cast<const float*>(x.w), x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, x.dim, w.amax};
+        hipLaunchKernelGGL(amax_kernel, dim3(kAmaxBlocks), dim3(kThreads), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     PackJobs jobs{};
     int count = 0;
     int64_t most = 0;
-    auto add = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which, bool halves) {
+    auto add = [&](const void* in, int64_t stride, int64_t rows, int64_t padded_rows, const int32_t* targets, const float* c, uint16_t* const* out, int which) {
         PackArgs& a = jobs.job[count++];
         a.in = in; a.in_stride = stride; a.rows = rows; a.padded_rows = padded_rows; a.targets = targets;
         a.num_targets = static_cast<uint32_t>(x.num_rows); a.c = c; a.dim = x.dim; a.padded = w.padded;
-        a.out[0] = out[0]; a.out[1] = out[1]; a.amax = halves ? w.amax + which * kAmaxBlocks : nullptr; a.shift = w.shift + which;
+        a.out[0] = out[0]; a.out[1] = out[1]; a.shift = w.shift + which;
+        if (f32) { a.amax = w.amax + which * kAmaxBlocks; a.maxima = kAmaxBlocks; }
         most = std::max(most, padded_rows);
     };
     auto operand = [&](uint16_t* const* part, int64_t rows) {
@@ -1643,24 +1679,27 @@ hipError_t pack(const XentCall& x, const XentWs& w, bool dw, Operand* h, Operand
         o.part[0] = part[0]; o.part[1] = part[1]; o.stride = w.padded; o.last = static_cast<uint32_t>(rows - 1); o.width = static_cast<uint32_t>(w.padded);
         return o;
     };
-    add(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1, f32);
+    add(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1);
     *h = operand(w.h, w.tokens);
     *hc = *h;
-    if (dw && (!f32 || x.c)) {
-        add(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, x.c ? 2 : 1, true);
-        *hc = operand(w.hc, w.tokens);
-    }
+    if (dw && f32 && x.c) add(x.h, x.h_stride, x.n, w.tokens, x.targets, x.c, w.hc, 2);
+    if (dw && (!f32 || x.c)) *hc = operand(w.hc, w.tokens);
     *wo = operand(w.w, x.num_rows);
     if (direct) {
         wo->part[0] = static_cast<const uint16_t*>(x.w);
         wo->stride = x.w_stride;
         wo->width = static_cast<uint32_t>(x.dim);
     } else {
-        add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0, f32);
+        add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
     }
-    int lanes = 1;      // of a row, as in the kernel; four rows of a lane group in flight
-    while (lanes < 64 && 8 * lanes < w.padded) lanes *= 2;
-    const dim3 grid(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(ceil_div(most, 4 * (kThreads / lanes)), 2048))), static_cast<unsigned>(count));
+    const dim3 grid(pack_blocks(w, most, kThreads, kMostPack), static_cast<unsigned>(count));
+    if (dw && !f32) {
+        *later = jobs.job[0];
+        later->c = jobs.job[0].c = x.c;
+        jobs.job[0].amax_out = w.amax;
+        later->amax = w.amax; later->maxima = static_cast<int32_t>(grid.x);
+        later->out[0] = w.hc[0]; later->shift = w.shift + (x.c ? 2 : 1);
+    }
     if (w.parts == 1) hipLaunchKernelGGL(pack_kernel<1>, grid, dim3(kThreads), 0, st, jobs);
     else hipLaunchKernelGGL(pack_kernel<2>, grid, dim3(kThreads), 0, st, jobs);
     return hipGetLastError();
@@ -1705,7 +1744,7 @@ hipError_t run_loss(const XentCall& x, const XentWs& w, float* loss, float* lse,
 {
     ScoreArgs a{};
     Operand unused;
-    hipError_t e = pack(x, w, false, &a.h, &unused, &a.w, st);
+    hipError_t e = pack(x, w, false, &a.h, &unused, &a.w, nullptr, st);
     if (e != hipSuccess) return e;
     a.targets = x.targets; a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles;
     a.splits = w.splits; a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.target_score = w.target_score;
@@ -1747,7 +1786,7 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
 {
     CoefArgs ca{};
     ProductArgs pa{};
-    hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, st);
+    hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, &ca.hc, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
     ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.g_stride = w.piece; ca.rest = w.rest;
@@ -1772,7 +1811,8 @@ hipError_t run_grad(const XentCall& x, const XentWs& w, const float* lse, float 
         ca.splits = splits_of(ca.row_tiles, token_tiles, w.large_scores);
         ca.tokens = static_cast<uint32_t>(w.tokens);
         for (int p = 0; p < P; ++p) ca.g[p] = w.g[p];
-        const dim3 grid(token_tiles * ca.splits);
+        ca.blocks = token_tiles * ca.splits;
+        const dim3 grid(ca.blocks + (P == 1 && dw && base == 0 ? pack_blocks(w, w.tokens, w.large_scores ? 512 : 256, 256) : 0));
         const int held = held_stages(w, ca.row_tiles, ca.splits, ca.steps);
         if (P == 1 && w.large_scores) hipLaunchKernelGGL((coef_kernel<1, 8, 0>), grid, dim3(512), 0, st, ca);
         else if (held == 0) hipLaunchKernelGGL((coef_kernel<P, 4, 0>), grid, dim3(256), 0, st, ca);
