@@ -365,7 +365,9 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  *   targets_dev  : device, int32[n].
  *   loss_dev, lse_dev : device, float[n].
  *   workspace_dev : at least ne_xent_workspace_bytes(n, num_rows, dim, type, 0) bytes, which grow with n: a workspace
- *                   for n rows serves fewer rows, too.
+ *                   for n rows serves fewer rows, too.  But for small n they have room for a copy of w (of two halves,
+ *                   with NE_F32).  A bf16 table whose rows begin at multiples of 16 bytes, less than 8 MB apart, with dim a
+ *                   multiple of 8, is read as it lies: there that room is not touched.
  * ne_xent_grad gives, for G_iv = scale * loss_grad[i] * (exp(s_iv - lse[i]) - [v == target[i]]),
  *   dh = G . W  and  dw = G^T . H,
  * written whole (rows without a target: dh 0).  Both have the type of h and w; one of them may be NULL.

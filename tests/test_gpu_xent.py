@@ -489,3 +489,26 @@ def test_dw_in_bfloat16_is_nearly_the_rounded_one(n, V, d, pad, factors):
     off = (dw - want.bfloat16().double()).norm()
     say("dw", n, V, d, "share of the bar", float(off / bar), "of dw", float(off / want.norm()), "error", float((dw - want).norm() / want.norm()))
     assert float(off) <= float(bar)
+
+
+@pytest.mark.parametrize("dtype,n,d", [(torch.float32, 16, 1000), (torch.float32, 16, 1600), (torch.float32, 1, 1011), (torch.float32, 30, 780), (torch.bfloat16, 16, 4700),
+                                       (torch.bfloat16, 30, 2300)])
+def test_sums_of_few_wide_rows(dtype, n, d):
+    """Root mean square of the errors of lse, which is nearly the score S of a target that a row leans to.  An addition in fp32 is off by 2^-24 / sqrt(3)
+    of its result, root mean square.  S is made of C sums (4 up to 16 rows, 2 up to 32) of m of the d / 32 steps each, which grow evenly to S / C, so that
+    together they are off by 2^-24 S sqrt(m / (9 C)); joining them and taking exponentials and the logarithm are six more roundings of S at most.  One
+    and a half times that."""
+    V, chains = 3000, 4 if n <= 16 else 2
+    square = bar = 0.0
+    runs = max(4, 96 // n)
+    for seed in range(runs):
+        gen = torch.Generator().manual_seed(seed)
+        w, t = torch.randn(V, d, generator=gen) * d ** -0.25, torch.randint(0, V, (n,), generator=gen)
+        h = (torch.randn(n, d, generator=gen) * d ** -0.25 + 0.5 * w[t]).to(dtype).to(DEV)
+        w, t = w.to(dtype).to(DEV), t.to(torch.int32).to(DEV)
+        lse = call(h, w, t, dh=False, dw=False)[1].double()
+        z = torch.logsumexp(torch.mm(h.double(), w.double().t().contiguous()), 1)
+        square += float((lse - z).square().mean()) / runs
+        bar += float((z.square() * (-(-d // 32) / chains / (9 * chains) + 6 / 3)).mean()) * 2.0 ** -48 / runs
+    say("few wide rows", dtype, n, d, "error", square ** 0.5, "share of the bar", (square / bar) ** 0.5 / 1.5)
+    assert square ** 0.5 <= 1.5 * bar ** 0.5
