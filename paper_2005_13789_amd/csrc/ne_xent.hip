@@ -26,8 +26,8 @@
 //
 // Bound by the matrix cores and by the loads from L2 that feed them.  Measured, 8192 rows, 200 003 of 512, bf16: loss
 // 1.7 to 1.8 ms (950 TF; a copy of the kernel without loads took 0.87 of the time, without exponentials 0.90, without
-// products 0.87: none of them hides the others completely), gradients of a piece of 15 616 table rows 169 us for G and
-// 237 for both products (1.1 PF), 6.8 to 7.1 ms in all.
+// products 0.87: none of them hides the others completely), gradients of a piece of 15 616 table rows 167 us for G and
+// 255 for both products (1.03 PF), 6.9 to 7.2 ms in all.
 // 4096 rows, 10 000 of 128, fp32: scores 40 us, G 55, products 72, and 35 us for the small launches around them.
 //
 // Operands in LDS are 16-byte pieces placed so that reads are free of bank conflicts (an XOR of the piece's
@@ -895,7 +895,7 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // itself from 2^-28 on and by 2^-39 below; of fp32 ones two fp16 halves of it, which keep 22 bits of 2^-16 and more (and 2^-39 of less).  By far
 // the largest coefficient of most rows is the target's: what dH's product does not see of it in bf16 is kept, and given to dH with the target's row of the
 // table when its sums are rounded.
-// 8192 x 15 616 x 512 bf16: 169 us (0.78 PF, 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
+// 8192 x 15 616 x 512 bf16: 167 us (0.78 PF, 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
 struct CoefArgs {
     Operand w, h;                  // both by rows
     const int32_t* targets;
@@ -1017,7 +1017,7 @@ struct ProductArgs {
     const int32_t* shift;          // power of two of the rows of H
 };
 
-// Both products of a piece are one launch: either alone leaves places empty.  (8192 x 15 616 x 512 bf16, large tiles: 237 us, 1.1 PF; 4096 x 10 000 x
+// Both products of a piece are one launch: either alone leaves places empty.  (8192 x 15 616 x 512 bf16, large tiles: 255 us, 1.03 PF; 4096 x 10 000 x
 // 128 fp32, small tiles: 72 us, 0.87 PF of half products.)
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
 // (bf16: turning G from fp16 to bf16 in registers takes up to 4 % of the gradients' time, 8192 x 200 003 x 512 5180 -> 5370 us; W in fp16 would
@@ -1113,7 +1113,7 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     }
 }
 
-// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us).  dH: rows without a target become zeros, the others take their factor, or in bf16
+// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us, 11 with the targets' rows).  dH: rows without a target become zeros, the others take their factor, or in bf16
 // what the target's coefficient lost.
 struct ReduceArgs {
     const float* in;               // [splits][rows_in][cols]
@@ -1499,7 +1499,8 @@ int64_t split_products(XentWs& w, int32_t dim, bool large)
 // last-level cache, which narrow tables need, whose products are over faster than G is read.  Of up to seventeen numbers of pieces the
 // one whose launches take the least time, by their stages and by G's bytes.  (Gradients, us, and with pieces of always 128 MB: 8192 x 200 003 x
 // 512 bf16 5220 and 5580, 4096 x 100 000 x 256 795 and 910, 8192 x 100 000 x 128 fp32 2595 and 3100, 1000 x 500 000 x 128 bf16 833 and 818,
-// x 64 680 and 625: the estimate is not always right.)
+// x 64 680 and 625: the estimate is not always right.  The bf16 figures, here and below, are those before G was held in fp16, which costs both sides
+// up to 4 %.)
 void choose_pieces(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
 {
     const int64_t row_tiles = ceil_div(num_rows, 256), bytes = row_tiles * 256 * 2 * w.parts * w.tokens;
@@ -1542,8 +1543,8 @@ bool few_loss(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
 }
 
 // Whether both gradients take one pass over the table, and how.  Up to 32 rows in fp32, where the other way makes halves of the table first (us at
-// 200 003 x 256: 16 rows 102 and 280, 32 rows 149 and 281), and up to 16 in bf16 where columns are few (100 000 x 100: 32 and 45; 200 003 x 256:
-// 81 and 88; 100 000 x 512: 102 and 85; 17 rows of 256: 132 and 88).
+// 200 003 x 256: 16 rows 102 and 280, 32 rows 149 and 281), and up to 16 in bf16 where columns are few (100 000 x 100: 33 and 48; 200 003 x 256:
+// 80 and 90; 100 000 x 512: 102 and 86; 17 rows of 256: 132 and 90).
 bool few_grad(XentWs& w, int64_t n, int32_t dim)
 {
     if (n > 32 || (w.parts == 1 && (n > 16 || dim > 256))) return false;
