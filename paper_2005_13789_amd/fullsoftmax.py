@@ -53,6 +53,8 @@ class SoftmaxTrainer:
         tables (walks are padded with -1) is left out: its loss is 0 and it adds nothing to the gradients; n is the number of all pairs, so that
         one of them weighs the same whatever else is in the step.  Returns the pairs' losses before the step (a view that the next
         step overwrites)."""
+        if pairs.dim() != 2 or pairs.shape[1] != 2:
+            raise ValueError("pairs must be [n][2]")
         n = int(pairs.shape[0])
         if n < 1 or n > self.batch:
             raise ValueError(f"a step takes 1 to {self.batch} pairs")

@@ -187,3 +187,20 @@ def test_pairs_without_a_source_do_not_count(n, compute):
     trainer = SoftmaxTrainer(vertex, context, batch=n, compute=compute)
     loss = trainer.step(pairs[out].to(DEV), 1e-2)
     assert bool((loss == 0).all()) and torch.equal(vertex, before[0]) and torch.equal(context, before[1])
+
+
+def test_trainer_refusals():
+    vertex, context = tables(50, 8, 12)
+    with pytest.raises(ValueError):
+        SoftmaxTrainer(vertex, context, batch=4, state_bits=16)
+    with pytest.raises(ValueError):
+        SoftmaxTrainer(vertex, context[:, :4].contiguous(), batch=4)
+    trainer = SoftmaxTrainer(vertex, context, batch=4)
+    before = vertex.clone(), context.clone()
+    for bad in (torch.zeros(0, 2), torch.zeros(5, 2), torch.zeros(4), torch.zeros(2, 3), torch.zeros(2, 1)):
+        with pytest.raises(ValueError):
+            trainer.step(bad.to(torch.int32).to(DEV), 1e-3)
+    for bad in (torch.zeros(3, 2, dtype=torch.int64, device=DEV), torch.zeros(3, 2, dtype=torch.int32)):
+        with pytest.raises((TypeError, RuntimeError)):
+            trainer.step(bad, 1e-3)
+    assert trainer.steps == 0 and torch.equal(vertex, before[0]) and torch.equal(context, before[1])
