@@ -379,13 +379,13 @@ ne_status ne_embed_grad(const int32_t* ids_dev, int64_t n, const void* grad_dev,
  * Precision.  NE_BF16: products of bf16 values with fp32 sums; exp(s - lse) - [v == target] is formed in fp32 and, but
  * where n is small, rounded for its products: for dw to 11 bits (2^-12 of itself from 2^-28 on, 2^-39 below), as are the
  * rows loss_grad[i] h_i (below 2^-28 of the largest of them: 2^-38 of it), for dh to bf16, the target's excepted, which is
- * whole; scale, and for dh loss_grad, are applied in fp32.  NE_F32: where n is
- * small, products in fp32 or of operands split into three bf16 parts (24 bits); otherwise every operand is the sum of
- * two halves in fp16 at a common power of two that the largest finite magnitude of its matrix sets, three products of
- * halves with fp32 sums: an element is off by up to 2^-22 of itself where it is at least 2^-16 of that magnitude, as an
- * fp32 product about is, and by up to 2^-38 of that magnitude where it is smaller, so that one outlier takes bits from the
- * rest of its matrix (for dw that of the rows loss_grad[i] h_i).  So is exp(s - lse) - [v == target]: 2^-22 of itself from
- * 2^-16 on, 2^-39 below.
+ * whole; scale, and for dh loss_grad, are applied in fp32.
+ * NE_F32: where n is small, products in fp32 or of operands split into three bf16 parts (24 bits); otherwise every operand
+ * is the sum of two halves in fp16 at a common power of two that the largest finite magnitude of its matrix sets, three
+ * products of halves with fp32 sums: an element is off by up to 2^-22 of itself where it is at least 2^-16 of that
+ * magnitude, as an fp32 product about is, and by up to 2^-38 of that magnitude where it is smaller, so that one outlier takes
+ * bits from the rest of its matrix (for dw that of the rows loss_grad[i] h_i).  So is exp(s - lse) - [v == target]: 2^-22 of
+ * itself from 2^-16 on, 2^-39 below.
  * An infinity or NaN in a row of h makes that row's loss and dh, and dw, NaN.  A NaN in a row of w makes all losses NaN, and
  * with NE_F32 an infinity does.  With NE_BF16 an infinity there makes a loss NaN, but where its row's score is minus infinity
  * the loss may also be that of a row of probability 0 (which of the two depends on dim and alignment).  The gradients of a

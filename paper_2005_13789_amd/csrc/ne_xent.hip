@@ -15,14 +15,13 @@
 // With few rows of H all of it is bound by reading the table and writing its gradient, and other kernels let the table stream through
 // registers once (few_rows_kernel, few_grad_kernel).
 //
-// Types: bf16 operands go to the matrix cores as they are.  Their G is held in fp16, 11 bits in the place of bf16's 8: dW multiplies it with H in
-// fp16, which holds what bf16 does, and dH, whose table no pass turns into fp16, with W after it is rounded to bf16 in registers, but for the
-// target's coefficient, which dH takes whole.  So both gradients' errors are those of their own rounding (0.0017; with G in bf16 0.0021, and dH 0.013 where
-// the table's rows share a part ten times as large as what tells them apart: a row's coefficients add up to nothing, their roundings do not).
-// fp32 operands are split into two fp16 halves at a common
-// power of two, x 2^k = hi + lo with 22 bits (of elements down to 2^-16 of the largest; smaller ones are off by up to 2^-38 of
-// it, fp16 ending there), and a product is hi hi + hi lo + lo hi: about the error of an fp32 product at three matrix
-// instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
+// Types: bf16 operands go to the matrix cores as they are.  G of bf16 tables is held in fp16, which keeps 11 bits where bf16 keeps 8.  dW
+// multiplies it with H in fp16.  dH, for which the table would have to be turned into fp16, rounds it to bf16 in registers, but takes the
+// target's coefficient whole.  So both gradients' errors are those of their own rounding: 0.0017.  (With G in bf16 0.0021, and dH 0.013 where the
+// table's rows share a part ten times as large as what tells them apart: a row's coefficients add up to nothing, their roundings do not.)
+// fp32 operands are split into two fp16 halves at a common power of two, x 2^k = hi + lo with 22 bits (of elements down to 2^-16 of the
+// largest; smaller ones are off by up to 2^-38 of it, fp16 ending there), and a product is hi hi + hi lo + lo hi: about the error of an fp32
+// product at three matrix instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
 //
 // Bound by the matrix cores and by the loads from L2 that feed them.  Measured, 8192 rows, 200 003 of 512, bf16: loss
 // 1.7 to 1.8 ms (950 TF; a copy of the kernel without loads took 0.87 of the time, without exponentials 0.90, without
@@ -964,7 +963,8 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
                             acc[im][j][i] -= 0x1p14f;
                             if (P == 1) {
                                 const float g = acc[im][j][i];
-                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - static_cast<float>(static_cast<bf16_t>(static_cast<float>(static_cast<f16_t>(g))));
+                                const float stored = static_cast<float>(static_cast<f16_t>(g));
+                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - static_cast<float>(static_cast<bf16_t>(stored));
                             }
                         }
             }
@@ -1113,8 +1113,8 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     }
 }
 
-// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us, 11 with the targets' rows).  dH: rows without a target become zeros, the others take their factor, or in bf16
-// what the target's coefficient lost.
+// Sums the splits and rounds once (2 x 8192 x 512, 42 MB: 8 us, 11 with the targets' rows).  dH: rows without a target become zeros, the others
+// take their factor, and in bf16 what the target's coefficient lost.
 struct ReduceArgs {
     const float* in;               // [splits][rows_in][cols]
     int64_t split_stride;
