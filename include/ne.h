@@ -403,6 +403,47 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
                        int64_t dw_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Answers from a whole table.  For the scores s_iv = <h_i, w_v> of n rows of h against all rows of w, never kept:
+ *   lse[i] = log sum_v exp(s_iv),   logp[i] = s_i,id - lse[i],   entropy[i] = - sum_v p_iv log p_iv with p_iv = exp(s_iv - lse[i]),
+ *   top_ids[i][0 .. k-1]: the ids of the k largest scores in falling order, of equal scores the lower id first, and top_logp[i][j],
+ *   their log probabilities.  A table of fewer than k rows leaves -1 and minus infinity behind its last.
+ * An id outside [0, num_rows) marks a row that has no answers: lse, logp and entropy 0, top_ids -1, top_logp minus infinity, whatever
+ * its h holds.  Without ids (NULL) every row is answered.
+ *   h_dev, w_dev : device, type [n][dim] and [num_rows][dim], row strides >= dim, aligned to their elements.
+ *   ids_dev      : NULL, or device, int32[n].
+ *   logp_dev     : NULL, or device, float[n] (needs ids).       entropy_dev : NULL, or device, float[n].
+ *   lse_dev      : device, float[n].
+ *   k            : 0 <= k <= NE_TOP_MAX; k > 0: top_ids_dev int32[n][k] and top_logp_dev float[n][k].
+ *   workspace_dev : at least ne_logprob_workspace_bytes(n, num_rows, dim, type, k, 0) bytes, which grow with n and with k from 0 to 1: 8 bytes for
+ *                   every 64 rows of w and row of h (for every 16 where n is small) with k > 0, and as for ne_xent_loss.
+ * Precision.  lse and entropy as ne_xent_loss has its lse.  Log probabilities are a score with products and sums in 64 bits less lse, and ids
+ * are ordered by such scores: which ids are answered, and in which order, depends on the values of h and w alone.
+ * A value in a row of h that is not finite makes that row's lse, logp, entropy and top_logp NaN and its top_ids -1; one in w all rows', as do norms of rows
+ * (a bound of them) whose product is 1e29 or more.
+ * ne_logprob_grad gives the gradients of  sum_i logp_scale * logp_grad[i] * logp[i] + entropy_scale * entropy_grad[i] * entropy[i],
+ *   dh = G . W and dw = G^T . H,  G_iv = l_i ([v == id[i]] - p_iv) - e_i p_iv (s_iv - lse[i] + entropy[i]),
+ * written whole (rows that have no answers: dh 0).  Both have the type of h and w; one of them may be NULL.
+ *   lse_dev, entropy_dev : device, float[n], as ne_logprob wrote them for the same h, w and ids; entropy_dev may be NULL where entropy_scale is 0.
+ *   logp_grad_dev, entropy_grad_dev : device, float[n]; NULL = 1 for every row.
+ *   logp_scale, entropy_scale : finite; without ids logp_scale has to be 0.
+ *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
+ *   workspace_dev : at least ne_logprob_workspace_bytes(n, num_rows, dim, type, 0, 1) bytes.
+ * Its precision is that of ne_xent_grad, coefficients being those of G over |l_i| + 8 |e_i|; values that are not finite: the gradients are not specified.
+ *   0 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for ne_logprob and writes zeros to dw.
+ * Errors: NE_ERR_ARG, NE_ERR_HIP.
+ */
+enum { NE_TOP_MAX = 64 };
+size_t ne_logprob_workspace_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int32_t k, int32_t grad);
+ne_status ne_logprob(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type, const int32_t* ids_dev,
+                     int64_t n, int64_t num_rows, int32_t dim, int32_t k, float* logp_dev, float* lse_dev, float* entropy_dev,
+                     int32_t* top_ids_dev, float* top_logp_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+ne_status ne_logprob_grad(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type, const int32_t* ids_dev,
+                          const float* lse_dev, const float* entropy_dev, const float* logp_grad_dev, const float* entropy_grad_dev,
+                          float logp_scale, float entropy_scale, int64_t n, int64_t num_rows, int32_t dim, void* dh_dev,
+                          int64_t dh_stride, void* dw_dev, int64_t dw_stride, void* workspace_dev, size_t workspace_bytes,
+                          void* hip_stream);
+
+/*
  * AdamW over many tensors at once.  Element by element, with g = grad_scale * grad and step t >= 1:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).

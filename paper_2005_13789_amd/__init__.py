@@ -27,12 +27,14 @@ NE_F32 = 0
 NE_BF16 = 1
 NE_OP_MAX_DIM = 16384
 NE_EMBED_MAX_IDS = 1 << 26
+NE_TOP_MAX = 64
 NE_ADAMW_BLOCK = 256    # elements that share a scale with 8-bit states
 
 EXPORTS = (
     "ne_create_tables", "ne_build_neg_alias", "ne_workspace_bytes", "ne_train_batch", "ne_train_block", "ne_train_runs", "ne_train_block_pinned", "ne_train_walks",
     "ne_shared_workspace_bytes", "ne_train_batch_shared", "ne_train_batch_shared_static", "ne_train_batch_async", "ne_train_block_async", "ne_set_vertex_window", "ne_eval_loss",
     "ne_embed_lookup", "ne_embed_workspace_bytes", "ne_embed_grad", "ne_xent_workspace_bytes", "ne_xent_loss", "ne_xent_grad",
+    "ne_logprob_workspace_bytes", "ne_logprob", "ne_logprob_grad",
     "ne_adamw_workspace_bytes", "ne_create_adamw", "ne_adamw_step", "ne_destroy_adamw",
     "ne_score_pairs", "ne_set_tuning", "ne_validate_pairs", "ne_hash_position", "ne_profile_enable", "ne_profile_read", "ne_destroy_tables", "ne_destroy_alias", "ne_last_error",
 )
@@ -120,6 +122,14 @@ def lib() -> ctypes.CDLL:
     L.ne_xent_grad.argtypes = [vp, c.c_int64, vp, c.c_int64, c.c_int32, vp, vp, vp, c.c_float, c.c_int64, c.c_int64, c.c_int32,
                                vp, c.c_int64, vp, c.c_int64, vp, c.c_size_t, vp]
     L.ne_xent_grad.restype = c.c_int
+    L.ne_logprob_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int32, c.c_int32, c.c_int32, c.c_int32]
+    L.ne_logprob_workspace_bytes.restype = c.c_size_t
+    L.ne_logprob.argtypes = [vp, c.c_int64, vp, c.c_int64, c.c_int32, vp, c.c_int64, c.c_int64, c.c_int32, c.c_int32, vp, vp, vp, vp, vp,
+                             vp, c.c_size_t, vp]
+    L.ne_logprob.restype = c.c_int
+    L.ne_logprob_grad.argtypes = [vp, c.c_int64, vp, c.c_int64, c.c_int32, vp, vp, vp, vp, vp, c.c_float, c.c_float, c.c_int64, c.c_int64,
+                                  c.c_int32, vp, c.c_int64, vp, c.c_int64, vp, c.c_size_t, vp]
+    L.ne_logprob_grad.restype = c.c_int
     L.ne_adamw_workspace_bytes.argtypes = [c.POINTER(NeAdamwTensor), c.c_int64]
     L.ne_adamw_workspace_bytes.restype = c.c_size_t
     L.ne_create_adamw.argtypes = [c.POINTER(vp), c.POINTER(NeAdamwTensor), c.c_int64, c.c_int32, c.c_uint64, vp, c.c_size_t, vp]
@@ -184,6 +194,13 @@ def _matrix(t, name: str, broadcast: bool = False):
     elif row < dim and not (broadcast and row == 0):
         raise TypeError(f"{name}: rows overlap")
     return t.data_ptr(), _TYPES[t.dtype], row
+
+
+def _on_current_device(*tensors) -> None:
+    """Launches go to the current device: tensors of another one are refused."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, and the current device is cuda:{torch.cuda.current_device()}")
 
 
 class Tables:
@@ -535,6 +552,72 @@ def ne_xent_grad(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: t
         outs += [p, stride]
     _check(lib().ne_xent_grad(hp, hs, wp, ws, ty, tp, zp, cp, scale, n, w.shape[0], h.shape[1], *outs, kp,
                               workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+
+
+def ne_logprob_workspace_bytes(n: int, num_rows: int, dim: int, dtype: torch.dtype, k: int = 0, grad: bool = False) -> int:
+    if dtype not in _TYPES:
+        raise TypeError("dtype must be torch.float32 or torch.bfloat16")
+    return int(lib().ne_logprob_workspace_bytes(n, num_rows, dim, _TYPES[dtype], k, 1 if grad else 0))
+
+
+def _logprob_operands(h, w, ids):
+    hp, ht, hs = _matrix(h, "h")
+    wp, wt, ws = _matrix(w, "w")
+    if ht != wt or h.shape[1] != w.shape[1]:
+        raise TypeError("h and w must have one type and one dim")
+    ip = _dev_ptr(ids, torch.int32, "ids")
+    if ids is not None and ids.numel() != h.shape[0]:
+        raise TypeError("ids must have one id per row of h")
+    return hp, hs, wp, ws, ht, ip
+
+
+def ne_logprob(h: torch.Tensor, w: torch.Tensor, ids: torch.Tensor | None, lse: torch.Tensor, workspace: torch.Tensor,
+               logp: torch.Tensor | None = None, entropy: torch.Tensor | None = None, top_ids: torch.Tensor | None = None,
+               top_logp: torch.Tensor | None = None, stream=None) -> None:
+    """Each row of h [n][dim] against all rows of w [num_rows][dim] (both float32 or both bfloat16, CUDA): lse float32 [n]; logp float32
+    [n], the log probabilities of ids (int32 [n]; one outside [0, num_rows) marks a row without answers); entropy float32 [n]; top_ids int32
+    [n][k] and top_logp float32 [n][k], the k most probable ids and their log probabilities.  ids None: every row is answered.
+    workspace: CUDA uint8 of ne_logprob_workspace_bytes(n, num_rows, dim, dtype, k) bytes."""
+    hp, hs, wp, ws, ty, ip = _logprob_operands(h, w, ids)
+    _on_current_device(h, w, ids, lse, workspace, logp, entropy, top_ids, top_logp)
+    n = h.shape[0]
+    lp, zp, ep = _row_floats(logp, n, "logp"), _row_floats(lse, n, "lse"), _row_floats(entropy, n, "entropy")
+    k = 0
+    if (top_ids is None) != (top_logp is None):
+        raise TypeError("top_ids and top_logp come together")
+    if top_ids is not None:
+        if top_ids.dim() != 2 or top_ids.shape[0] != n or top_logp.shape != top_ids.shape:
+            raise TypeError("top_ids and top_logp must be [n][k]")
+        k = top_ids.shape[1]
+    tp, vp = _dev_ptr(top_ids, torch.int32, "top_ids"), _dev_ptr(top_logp, torch.float32, "top_logp")
+    kp = _dev_ptr(workspace, torch.uint8, "workspace")
+    _check(lib().ne_logprob(hp, hs, wp, ws, ty, ip, n, w.shape[0], h.shape[1], k, lp, zp, ep, tp, vp, kp,
+                            workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+
+
+def ne_logprob_grad(h: torch.Tensor, w: torch.Tensor, ids: torch.Tensor | None, lse: torch.Tensor, entropy: torch.Tensor | None,
+                    dh: torch.Tensor | None, dw: torch.Tensor | None, workspace: torch.Tensor, logp_grad: torch.Tensor | None = None,
+                    entropy_grad: torch.Tensor | None = None, logp_scale: float = 1.0, entropy_scale: float = 0.0, stream=None) -> None:
+    """Gradients of sum_i logp_scale * logp_grad[i] * logp[i] + entropy_scale * entropy_grad[i] * entropy[i] (None: 1 for every row)
+    with respect to h and w, in their type, into dh and dw (either may be None); lse and entropy as ne_logprob wrote them.  Without ids
+    logp_scale has to be 0.  workspace: CUDA uint8 of ne_logprob_workspace_bytes(n, num_rows, dim, dtype, grad=True) bytes."""
+    hp, hs, wp, ws, ty, ip = _logprob_operands(h, w, ids)
+    _on_current_device(h, w, ids, lse, entropy, dh, dw, workspace, logp_grad, entropy_grad)
+    n = h.shape[0]
+    zp, ep = _row_floats(lse, n, "lse"), _row_floats(entropy, n, "entropy")
+    ap, bp = _row_floats(logp_grad, n, "logp_grad"), _row_floats(entropy_grad, n, "entropy_grad")
+    kp = _dev_ptr(workspace, torch.uint8, "workspace")
+    outs = []
+    for t, like, name in ((dh, h, "dh"), (dw, w, "dw")):
+        if t is None:
+            outs += [0, 0]
+            continue
+        p, t_type, stride = _matrix(t, name)
+        if t.shape != like.shape or t_type != ty:
+            raise TypeError(f"{name} must have the shape and type of {name[1:]}")
+        outs += [p, stride]
+    _check(lib().ne_logprob_grad(hp, hs, wp, ws, ty, ip, zp, ep, ap, bp, logp_scale, entropy_scale, n, w.shape[0], h.shape[1], *outs, kp,
+                                 workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
 
 
 class AdamW:

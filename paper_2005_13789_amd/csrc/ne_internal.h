@@ -21,6 +21,9 @@
 // Records the message for ne_last_error() on this thread and returns st (defined in ne.hip).
 ne_status fail(ne_status st, const std::string& msg);
 
+// Bytes of workspace that the gradient of log probabilities and entropies needs (defined in ne_xent.hip).
+size_t logprob_grad_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type);
+
 #define NE_HIP_CHECK(expr)                                                                       \
     do {                                                                                         \
         hipError_t e_ = (expr);                                                                  \

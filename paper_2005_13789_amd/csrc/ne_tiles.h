@@ -26,6 +26,8 @@ constexpr int kThreads = 256;
 constexpr int kAmaxBlocks = 1024, kMostPack = 2048;      // (bf16: each of the packing workgroups leaves a maximum, in the room of three times 1024)
 static_assert(kMostPack <= 3 * kAmaxBlocks);
 constexpr int64_t kMostStride = 1 << 22;   // elements: a tile's 256 rows are within 32 bits of its first
+constexpr int kFewBytes = 65536, kFewBytesAlone = 153600;     // LDS of H for the loss: of a workgroup of 4 wavefronts, and of one of 8 that is alone on its CU
+constexpr int kFewGroups = 1024;
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
 template <int P> constexpr int step_of() { return P == 1 ? 64 : 32; }   // contraction indices of a stage
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(kThreads) amax_kernel(AmaxArgs a)
         for (int q = 0; q < 8; ++q) w = fmaxf(w, finite_abs(x[q]));
     });
     for_eights(a.h, a.h_stride, a.n, a.dim, a.dim, blockIdx.x, gridDim.x, [&](int64_t i, int, const float (&x)[8]) {
-        if (static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) return;
+        if (a.targets && static_cast<uint32_t>(a.targets[i]) >= static_cast<uint32_t>(a.num_rows)) return;
         const float c = a.c ? a.c[i] : 1.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
@@ -695,6 +697,20 @@ bool large_scores(int64_t n, int64_t num_rows, int32_t dim, int parts)
     return parts == 1 && dim >= 384 && ceil_div(n, 256) * ceil_div(num_rows, 256) >= 1024;
 }
 
+// LDS of the rows of H that a launch of the few-rows kernels has, as second operands.
+int64_t few_bytes_of(int blocks, int32_t dim, int parts) { return blocks * ceil_div(dim, 32) * (parts == 2 ? 3 : 1) * 1024; }
+
+// Whether the table streams through registers for scores (blocks of 16 rows of H of a launch, or 0): up to 64 rows, or in fp32, where the other way
+// makes halves of the table first, two launches of as many rows as LDS has place for, three where the table is no small part of the last-level cache
+// (us of the loss at 200 003 x 256 fp32: 64 rows 55, 128 rows 107, 192 rows 169, the other way 178, 182 and 212; 192 rows against 100 000 x 100: 76 and 63).
+int few_blocks_of(int64_t n, int64_t num_rows, int32_t dim, int parts)
+{
+    const int64_t launches = parts == 1 ? 1 : num_rows * dim < (1 << 25) ? 2 : 3;
+    int blocks = n <= 16 ? 1 : n <= 32 ? 2 : 4;
+    while (blocks > 1 && few_bytes_of(blocks, dim, parts) > kFewBytesAlone) blocks /= 2;
+    return few_bytes_of(blocks, dim, parts) <= kFewBytesAlone && ceil_div(n, 16 * blocks) <= launches ? blocks : 0;
+}
+
 // Packed operands in a workspace.
 struct Packs {
     int32_t parts, padded, cols;
@@ -721,6 +737,17 @@ struct SoftmaxCall {
     const float* c;
 };
 
+// Whether a bf16 table is read as it lies, or has to be packed first.
+bool usable_as_it_lies(const SoftmaxCall& x)
+{
+    return x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && x.w_stride < kMostStride && aligned(x.w, 16);
+}
+
+Operand packed_operand(uint16_t* const* part, int64_t rows, int32_t padded)
+{
+    return Operand{{part[0], part[1]}, padded, static_cast<uint32_t>(rows - 1), static_cast<uint32_t>(padded)};
+}
+
 // Workgroups of `threads` that pack `rows` rows: of a row's lanes, as in the kernel, four rows of a lane group in flight.
 uint32_t pack_blocks(const Packs& w, int64_t rows, int threads, int64_t most)
 {
@@ -733,7 +760,7 @@ uint32_t pack_blocks(const Packs& w, int64_t rows, int threads, int64_t most)
 // fp16, which `later` says how, as its largest magnitude is found here.
 hipError_t pack(const SoftmaxCall& x, const Packs& w, bool dw, Operand* h, Operand* hc, Operand* wo, PackArgs* later, hipStream_t st)
 {
-    const bool direct = x.type == NE_BF16 && x.dim % 8 == 0 && x.w_stride % 8 == 0 && x.w_stride < kMostStride && aligned(x.w, 16);
+    const bool direct = usable_as_it_lies(x);
     const bool f32 = x.type == NE_F32;
     if (f32) {
         AmaxArgs a{static_cast<const float*>(x.h), static_cast<const float*>(x.w), x.targets, x.c, x.h_stride, x.w_stride, x.n, x.num_rows, x.dim, w.amax};
@@ -752,11 +779,7 @@ hipError_t pack(const SoftmaxCall& x, const Packs& w, bool dw, Operand* h, Opera
         if (f32) { a.amax = w.amax + which * kAmaxBlocks; a.maxima = kAmaxBlocks; }
         most = std::max(most, padded_rows);
     };
-    auto operand = [&](uint16_t* const* part, int64_t rows) {
-        Operand o{};
-        o.part[0] = part[0]; o.part[1] = part[1]; o.stride = w.padded; o.last = static_cast<uint32_t>(rows - 1); o.width = static_cast<uint32_t>(w.padded);
-        return o;
-    };
+    auto operand = [&](uint16_t* const* part, int64_t rows) { return packed_operand(part, rows, w.padded); };
     add(x.h, x.h_stride, x.n, w.tokens, x.targets, nullptr, w.h, 1);
     *h = operand(w.h, w.tokens);
     *hc = *h;

@@ -32,8 +32,6 @@
 
 namespace {
 
-constexpr int kFewBytes = 65536, kFewBytesAlone = 153600;     // LDS of H for the loss: of a workgroup of 4 wavefronts, and of one of 8 that is alone on its CU
-constexpr int kFewGroups = 1024;
 constexpr int kFewGradGroups = 1024;       // workgroups of the gradients; half as many where one takes more registers and LDS
 // Bytes of G of one piece: at most, those from which on smaller pieces are not looked at, those that stay in the last-level cache beside the
 // table and the sums, and what is written or read of these in a stage's time.
@@ -283,6 +281,11 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // the largest coefficient of most rows is the target's: what dH's product does not see of it in bf16 is kept, and given to dH with the target's row of the
 // table when its sums are rounded.
 // 8192 x 15 616 x 512 bf16: 167 us (0.78 PF, 256 MB written); 4096 x 10 000 x 128 fp32: 55 us (164 MB written).
+// A row's coefficients where its entropy counts: p (a + b x) 2^14 - target at the target, for p 2^14 = 2^x.
+struct Mix {
+    float a, b, target, unused;
+};
+
 struct CoefArgs {
     Operand w, h;                  // both by rows
     const int32_t* targets;
@@ -296,9 +299,10 @@ struct CoefArgs {
                                    // launch of its own, 32 so)
     PackArgs hc;
     float* rest;                   // bf16 only: [tokens]  what rounding to bf16 takes from the target's coefficient
+    const Mix* mix;                // with entropies only: [n]
 };
 
-template <int P, int W, int KS>
+template <int P, int W, int KS, bool ENTROPY>
 __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
@@ -314,13 +318,17 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
     const float to_log2 = kLog2e * score_factor<P>(a.shift);
     uint32_t target[2];
     float by[2];
+    Mix mix[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
-        target[j] = token < a.n ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
+        const bool all = ENTROPY && !a.targets;      // (rows that have no ids all count)
+        target[j] = token < a.n && !all ? static_cast<uint32_t>(a.targets[token]) : 0xFFFFFFFFu;
         if (target[j] >= a.num_rows) target[j] = 0xFFFFFFFFu;
+        const bool counts = all ? token < a.n : target[j] != 0xFFFFFFFFu;
         // (G 2^14; a row without a target: 2 to the minus infinity)
-        by[j] = target[j] != 0xFFFFFFFFu ? fmaf(a.lse[token], kLog2e, -static_cast<float>(kGShift)) : INFINITY;
+        by[j] = counts ? fmaf(a.lse[token], kLog2e, -static_cast<float>(kGShift)) : INFINITY;
+        mix[j] = ENTROPY && counts ? a.mix[token] : Mix{0.0f, 0.0f, 0x1p14f, 0.0f};
     }
     all_scores<P, W, KS>(a.w, a.h, token_tile, a.row_base, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0, lane_row0 = row0 + lane_row();
@@ -330,14 +338,19 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 #pragma unroll
             for (int im = 0; im < MT; ++im)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[im][j][i] = __builtin_amdgcn_exp2f(fmaf(acc[im][j][i], to_log2, -by[j]));
+                for (int i = 0; i < 16; ++i) {
+                    float x = fmaf(acc[im][j][i], to_log2, -by[j]);
+                    if (ENTROPY) x = x < -1000.0f ? -1000.0f : x;       // (0 times infinity is no coefficient)
+                    acc[im][j][i] = __builtin_amdgcn_exp2f(x);
+                    if (ENTROPY) acc[im][j][i] *= fmaf(mix[j].b, x, mix[j].a);
+                }
             if (__any(target[j] - row0 < 32 * MT)) {
 #pragma unroll
                 for (int im = 0; im < MT; ++im)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (target[j] - lane_row0 == 32 * im + sum_row(i)) {
-                            acc[im][j][i] -= 0x1p14f;
+                            acc[im][j][i] -= ENTROPY ? mix[j].target : 0x1p14f;
                             if (P == 1) {
                                 const float g = acc[im][j][i];
                                 const float stored = static_cast<float>(static_cast<f16_t>(g));
@@ -491,9 +504,9 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
     const bool in = r < a.rows && e < static_cast<int>(a.cols);
     bool counts = in;
     float c = 1.0f, rest = 0.0f, x[4] = {};
-    if (in && a.targets) {      // (fetched ahead of the sums)
-        const uint32_t target = static_cast<uint32_t>(a.targets[r]);
-        counts = target < a.num_targets;
+    if (in && (a.targets || a.c)) {      // (fetched ahead of the sums)
+        const uint32_t target = a.targets ? static_cast<uint32_t>(a.targets[r]) : 0;
+        counts = !a.targets || target < a.num_targets;
         if (counts && a.c) c = a.c[r];
         if (counts && a.rest) {
             rest = a.rest[r];
@@ -561,12 +574,13 @@ struct FewGradArgs {
     float* dh;                     // NULL, or [workgroups][n][cols]
     void* dw;                      // NULL, or the table's gradient
     int64_t dw_stride;
+    const Mix* mix;                // with entropies only: [n]
 };
 
 template <int CT, int WAVES> constexpr int few_stride() { return WAVES * CT * 16 + 4; }        // of a row of H in LDS: quarters in different banks
 template <int BLOCKS, int CT, int WAVES> constexpr size_t few_grad_lds() { return size_t{16} * BLOCKS * few_stride<CT, WAVES>() * 4; }
 
-template <class T, int BLOCKS, int CT, int WAVES>
+template <class T, int BLOCKS, int CT, int WAVES, bool ENTROPY>
 __global__ void __launch_bounds__(64 * WAVES) few_grad_kernel(FewGradArgs a)
 {
     constexpr int STRIDE = few_stride<CT, WAVES>();
@@ -577,18 +591,26 @@ __global__ void __launch_bounds__(64 * WAVES) few_grad_kernel(FewGradArgs a)
     for (int i = threadIdx.x; i < 16 * BLOCKS * STRIDE; i += 64 * WAVES) {
         const uint32_t t = i / STRIDE;
         const int e = i % STRIDE;
-        const bool in = t < a.n && e < a.dim && static_cast<uint32_t>(a.targets[t]) < a.num_rows;
+        const bool in = t < a.n && e < a.dim && ((ENTROPY && !a.targets) || static_cast<uint32_t>(a.targets[t]) < a.num_rows);
         few_h[i] = in ? static_cast<float>(static_cast<const T*>(a.h)[t * a.h_stride + e]) : 0.0f;
     }
     uint32_t target[BLOCKS];
     float by[BLOCKS], c[BLOCKS];
+    Mix mix[BLOCKS];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
         const uint32_t t = b * 16 + col;
-        target[b] = t < a.n ? static_cast<uint32_t>(a.targets[t]) : 0xFFFFFFFFu;
-        const bool counts = target[b] < a.num_rows;     // (otherwise 2 to the minus infinity)
+        const bool all = ENTROPY && !a.targets;
+        target[b] = t < a.n && !all ? static_cast<uint32_t>(a.targets[t]) : 0xFFFFFFFFu;
+        const bool counts = all ? t < a.n : target[b] < a.num_rows;     // (otherwise 2 to the minus infinity)
         by[b] = counts ? a.lse[t] * kLog2e : INFINITY;
         c[b] = counts && a.c ? a.c[t] : 1.0f;
+        mix[b] = Mix{};
+        if (ENTROPY && counts) {
+            mix[b] = a.mix[t];
+            mix[b].a = fmaf(mix[b].b, static_cast<float>(kGShift), mix[b].a);      // (p = 2^x here)
+            mix[b].target *= 0x1p-14f;
+        }
     }
     f32x4 dh[BLOCKS][CT];
 #pragma unroll
@@ -641,8 +663,11 @@ __global__ void __launch_bounds__(64 * WAVES) few_grad_kernel(FewGradArgs a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t row = tile * 16 + quarter * 4 + i;
-                float p = __builtin_amdgcn_exp2f(fmaf(s[i], kLog2e, -by[b]));
-                if (row == target[b]) p -= 1.0f;
+                float x = fmaf(s[i], kLog2e, -by[b]);
+                if (ENTROPY) x = x < -1000.0f ? -1000.0f : x;
+                float p = __builtin_amdgcn_exp2f(x);
+                if (ENTROPY) p *= fmaf(mix[b].b, x, mix[b].a);
+                if (row == target[b]) p -= ENTROPY ? mix[b].target : 1.0f;
                 coef[b][i] = row <= last ? p * c[b] : 0.0f;
             }
             if (a.dw) *reinterpret_cast<f32x4*>(&turn[wave][b][col * 16 + quarter * 4]) = coef[b];
@@ -736,8 +761,33 @@ __global__ void __launch_bounds__(1024) few_join_kernel(FewJoinArgs a)
     for (int v = 0; v < 64; ++v) all += lds[v][threadIdx.x];
     const int at = blockIdx.y * 64 + threadIdx.x;
     if (at >= a.dim) return;
-    const bool counts = static_cast<uint32_t>(a.targets[t]) < a.num_targets;
+    const bool counts = !a.targets || static_cast<uint32_t>(a.targets[t]) < a.num_targets;
     static_cast<T*>(a.out)[t * a.out_stride + at] = from_float<T>(counts ? all * a.scale : 0.0f);
+}
+
+// Gradients of sum_i l_i logp_i + e_i entropy_i: with f = |l| + 8 |e|, a = l / f and b = e / f the coefficient of table row v is
+//     - f [ p (a + b (s - lse + entropy)) - a [v = id] ],
+// the bracket at most 1 in magnitude (p |log p| < 0.37, p entropy < 6 for tables of less than 2^31 rows), as that of the loss alone is.
+struct MixArgs {
+    const int32_t* ids;            // NULL: no log probabilities, and all rows count
+    const float *logp_grad, *entropy_grad, *entropy;      // the gradients: NULL for 1
+    float logp_scale, entropy_scale;
+    int64_t n;
+    uint32_t num_rows;
+    Mix* mix;                      // [n]
+    float* c;                      // [n]  - f
+};
+
+__global__ void __launch_bounds__(kThreads) mix_kernel(MixArgs a)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= a.n) return;
+    const bool counts = !a.ids || static_cast<uint32_t>(a.ids[i]) < a.num_rows;
+    const float l = counts && a.ids ? a.logp_scale * (a.logp_grad ? a.logp_grad[i] : 1.0f) : 0.0f;
+    const float e = counts ? a.entropy_scale * (a.entropy_grad ? a.entropy_grad[i] : 1.0f) : 0.0f;
+    const float f = fabsf(l) + 8.0f * fabsf(e), u = f == 0.0f ? 0.0f : l / f, v = f == 0.0f ? 0.0f : e / f;
+    a.mix[i] = counts ? Mix{fmaf(v, a.entropy[i] - kGShift * kLn2, u), v * kLn2, u * 0x1p14f, 0.0f} : Mix{};
+    a.c[i] = -f;
 }
 
 template <class T>
@@ -838,22 +888,6 @@ void choose_pieces(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
     w = chosen;
 }
 
-// LDS of the rows of H that a launch of the few-rows kernel has, as second operands.
-int64_t few_bytes_of(const XentWs& w, int32_t dim) { return w.few_blocks * ceil_div(dim, 32) * (w.parts == 2 ? 3 : 1) * 1024; }
-
-// Whether the table streams through registers for the loss: up to 64 rows, or in fp32, where the other way makes halves of the table first, two
-// launches of as many rows as LDS has place for, three where the table is no small part of the last-level cache (us at 200 003 x 256 fp32:
-// 64 rows 55, 128 rows 107, 192 rows 169, the other way 178, 182 and 212; 192 rows against 100 000 x 100: 76 and 63).
-bool few_loss(XentWs& w, int64_t n, int64_t num_rows, int32_t dim)
-{
-    const int64_t launches = w.parts == 1 ? 1 : num_rows * dim < (1 << 25) ? 2 : 3;
-    w.few_blocks = n <= 16 ? 1 : n <= 32 ? 2 : 4;
-    while (w.few_blocks > 1 && few_bytes_of(w, dim) > kFewBytesAlone) w.few_blocks /= 2;
-    if (few_bytes_of(w, dim) <= kFewBytesAlone && ceil_div(n, 16 * w.few_blocks) <= launches) return true;
-    w.few_blocks = 0;
-    return false;
-}
-
 // Whether both gradients take one pass over the table, and how.  Up to 32 rows in fp32, where the other way makes halves of the table first (us at
 // 200 003 x 256: 16 rows 102 and 280, 32 rows 149 and 281), and up to 16 in bf16 where columns are few (100 000 x 100: 33 and 48; 200 003 x 256:
 // 80 and 90; 100 000 x 512: 102 and 86; 17 rows of 256: 132 and 90).
@@ -883,8 +917,8 @@ XentWs xent_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool 
     const int64_t side = w.large_scores ? 256 : 128, token_tiles = ceil_div(w.tokens, side);
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     Carver take{base};
-    if (!grad && few_loss(w, n, num_rows, dim)) {
-        const bool alone = few_bytes_of(w, dim) > kFewBytes;        // (a tile of 16 rows for each wavefront, at most)
+    if (!grad && (w.few_blocks = few_blocks_of(n, num_rows, dim, w.parts)) > 0) {
+        const bool alone = few_bytes_of(w.few_blocks, dim, w.parts) > kFewBytes;        // (a tile of 16 rows for each wavefront, at most)
         w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, alone ? 128 : 64), alone ? 256 : kFewGroups));
         w.stat = take.get<float2>(static_cast<size_t>(w.splits) * n);
         w.target_score = take.get<float>(static_cast<size_t>(n));
@@ -935,7 +969,7 @@ size_t xent_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool g
         // shares of few rows; of tiles: as many workgroups as run in four rounds, or one for every tile
         bytes += (std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups) * std::min<int64_t>(n, 192) + tokens +
                   std::min<int64_t>(ceil_div(num_rows, 128) * tokens, 4 * 512 * 128)) * 8 + tokens * 4;
-        if (few_loss(w, n, num_rows, dim)) return static_cast<size_t>(bytes);
+        if (few_blocks_of(n, num_rows, dim, w.parts)) return static_cast<size_t>(bytes);
     } else {
         const int64_t few = ceil_div(num_rows, 16);
         const int64_t narrow = std::min<int64_t>(few, kFewGradGroups) * std::min<int64_t>(n, 16);
@@ -966,7 +1000,7 @@ hipError_t run_few(const SoftmaxCall& x, const XentWs& w, float* loss, float* ls
     FewArgs a{};
     a.w = x.w; a.h_stride = x.h_stride; a.w_stride = x.w_stride; a.num_rows = static_cast<uint32_t>(x.num_rows); a.dim = x.dim;
     a.steps = static_cast<int32_t>(ceil_div(x.dim, 32));
-    const size_t lds = static_cast<size_t>(few_bytes_of(w, x.dim));
+    const size_t lds = static_cast<size_t>(few_bytes_of(w.few_blocks, x.dim, w.parts));
     auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(w.splits), dim3(threads), lds, st, a); };
     for (int64_t base = 0; base < x.n; base += 16 * w.few_blocks) {
         a.h = static_cast<const T*>(x.h) + base * x.h_stride; a.targets = x.targets + base;
@@ -1007,20 +1041,20 @@ hipError_t run_loss(const SoftmaxCall& x, const XentWs& w, float* loss, float* l
     return join_losses(x, w, loss, lse, st);
 }
 
-template <class T, int BLOCKS>
-hipError_t run_few_grad(const SoftmaxCall& x, const XentWs& w, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw, int64_t dw_stride, hipStream_t st)
+template <class T, int BLOCKS, bool ENTROPY = false>
+hipError_t run_few_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw, int64_t dw_stride, hipStream_t st)
 {
     FewGradArgs a{};
     a.h = x.h; a.w = x.w; a.h_stride = x.h_stride; a.w_stride = x.w_stride; a.targets = x.targets; a.lse = lse; a.c = x.c;
     a.n = static_cast<uint32_t>(x.n); a.num_rows = static_cast<uint32_t>(x.num_rows); a.cols = static_cast<uint32_t>(w.cols); a.dim = x.dim;
-    a.scale = scale; a.dh = dh ? w.dh : nullptr; a.dw = dw; a.dw_stride = dw_stride;
+    a.scale = scale; a.dh = dh ? w.dh : nullptr; a.dw = dw; a.dw_stride = dw_stride; a.mix = mix;
     const dim3 grid(w.splits);
-    if (w.few_groups == 1) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 1, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 1, 4>()), st, a);
-    else if (w.few_groups == 2) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 2, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 2, 4>()), st, a);
-    else if (w.few_groups == 4) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 4, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 4, 4>()), st, a);
+    if (w.few_groups == 1) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 1, 4, ENTROPY>), grid, dim3(256), (few_grad_lds<BLOCKS, 1, 4>()), st, a);
+    else if (w.few_groups == 2) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 2, 4, ENTROPY>), grid, dim3(256), (few_grad_lds<BLOCKS, 2, 4>()), st, a);
+    else if (w.few_groups == 4) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 4, 4, ENTROPY>), grid, dim3(256), (few_grad_lds<BLOCKS, 4, 4>()), st, a);
     if constexpr (sizeof(T) == 4) {
-        if (BLOCKS == 1 && w.few_waves == 8) hipLaunchKernelGGL((few_grad_kernel<T, 1, 8, 8>), grid, dim3(512), (few_grad_lds<1, 8, 8>()), st, a);
-        else if (w.few_groups == 8) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 8, 4>), grid, dim3(256), (few_grad_lds<BLOCKS, 8, 4>()), st, a);
+        if (BLOCKS == 1 && w.few_waves == 8) hipLaunchKernelGGL((few_grad_kernel<T, 1, 8, 8, ENTROPY>), grid, dim3(512), (few_grad_lds<1, 8, 8>()), st, a);
+        else if (w.few_groups == 8) hipLaunchKernelGGL((few_grad_kernel<T, BLOCKS, 8, 4, ENTROPY>), grid, dim3(256), (few_grad_lds<BLOCKS, 8, 4>()), st, a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !dh) return e;
@@ -1029,15 +1063,15 @@ hipError_t run_few_grad(const SoftmaxCall& x, const XentWs& w, const float* lse,
     return hipGetLastError();
 }
 
-template <int P, class T>
-hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw, int64_t dw_stride, hipStream_t st)
+template <int P, class T, bool ENTROPY = false>
+hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw, int64_t dw_stride, hipStream_t st)
 {
     CoefArgs ca{};
     ProductArgs pa{};
     hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, &ca.hc, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
-    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.g_stride = w.piece; ca.rest = w.rest;
+    ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.g_stride = w.piece; ca.rest = w.rest; ca.mix = mix;
     ca.num_rows = static_cast<uint32_t>(x.num_rows); ca.steps = w.padded / step_of<P>();
     const int64_t side = w.large_scores ? 256 : 128, edge = w.large_products ? 256 : 128;
     const uint32_t token_tiles = static_cast<uint32_t>(ceil_div(w.tokens, side));
@@ -1062,10 +1096,10 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const float* lse, flo
         ca.blocks = token_tiles * ca.splits;
         const dim3 grid(ca.blocks + (P == 1 && dw && base == 0 ? pack_blocks(w, w.tokens, w.large_scores ? 512 : 256, 256) : 0));
         const int held = held_stages(w, ca.row_tiles, ca.splits, ca.steps);
-        if (P == 1 && w.large_scores) hipLaunchKernelGGL((coef_kernel<1, 8, 0>), grid, dim3(512), 0, st, ca);
-        else if (held == 0) hipLaunchKernelGGL((coef_kernel<P, 4, 0>), grid, dim3(256), 0, st, ca);
-        else if (held == 2) hipLaunchKernelGGL((coef_kernel<P, 4, 2>), grid, dim3(256), 0, st, ca);
-        else hipLaunchKernelGGL((coef_kernel<P, 4, 4>), grid, dim3(256), 0, st, ca);
+        if (P == 1 && w.large_scores) hipLaunchKernelGGL((coef_kernel<1, 8, 0, ENTROPY>), grid, dim3(512), 0, st, ca);
+        else if (held == 0) hipLaunchKernelGGL((coef_kernel<P, 4, 0, ENTROPY>), grid, dim3(256), 0, st, ca);
+        else if (held == 2) hipLaunchKernelGGL((coef_kernel<P, 4, 2, ENTROPY>), grid, dim3(256), 0, st, ca);
+        else hipLaunchKernelGGL((coef_kernel<P, 4, 4, ENTROPY>), grid, dim3(256), 0, st, ca);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         pa.g_rows = Operand{{w.g[0], w.g[1]}, w.piece, static_cast<uint32_t>(w.tokens - 1), static_cast<uint32_t>(w.piece)};
@@ -1099,7 +1133,7 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const float* lse, flo
         ReduceArgs r{};
         r.in = w.dh; r.split_stride = w.tokens * pa.cols; r.splits = w.h_splits; r.rows = x.n; r.out = dh; r.out_stride = dh_stride;
         r.targets = x.targets; r.num_targets = ca.num_rows; r.c = x.c; r.shift = P == 2 ? w.shift : nullptr;
-        r.rest = w.rest; r.w = static_cast<const bf16_t*>(x.w); r.w_stride = x.w_stride;
+        r.rest = x.targets ? w.rest : nullptr; r.w = static_cast<const bf16_t*>(x.w); r.w_stride = x.w_stride;
         return reduce(r);
     }
     return hipSuccess;
@@ -1117,14 +1151,48 @@ ne_status check_xent(const SoftmaxCall& x, const char* who)
     return NE_OK;
 }
 
+// Gradients through whichever way the sizes take; with a mix, those of log probabilities and entropies.
+hipError_t gradients(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const float* lse, float scale, void* dh, int64_t dh_stride, void* dw,
+                     int64_t dw_stride, hipStream_t st)
+{
+    auto run = [&](auto grad) { return grad(x, w, mix, lse, scale, dh, dh_stride, dw, dw_stride, st); };
+    const bool f32 = x.type == NE_F32;
+    if (mix) {
+        return w.few_blocks == 1 ? (f32 ? run(run_few_grad<float, 1, true>) : run(run_few_grad<bf16_t, 1, true>))
+               : w.few_blocks == 2 ? run(run_few_grad<float, 2, true>)
+               : f32 ? run(run_grad<2, float, true>) : run(run_grad<1, bf16_t, true>);
+    }
+    return w.few_blocks == 1 ? (f32 ? run(run_few_grad<float, 1>) : run(run_few_grad<bf16_t, 1>))
+           : w.few_blocks == 2 ? run(run_few_grad<float, 2>)
+           : f32 ? run(run_grad<2, float>) : run(run_grad<1, bf16_t>);
+}
+
+hipError_t clear_gradient(void* dw, int64_t stride, int64_t rows, int32_t dim, int32_t type, hipStream_t st)
+{
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(rows * dim, kThreads), 4096)));
+    if (type == NE_F32) hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(kThreads), 0, st, static_cast<float*>(dw), stride, rows, dim);
+    else hipLaunchKernelGGL(zero_kernel<bf16_t>, grid, dim3(kThreads), 0, st, static_cast<bf16_t*>(dw), stride, rows, dim);
+    return hipGetLastError();
+}
+
+size_t xent_need(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool grad)
+{
+    return std::max(xent_bytes(n, num_rows, dim, type, grad), xent_layout(n, num_rows, dim, type, grad, nullptr).total);
+}
+
+// A row's factors lie in front of the gradients' workspace.
+size_t mix_bytes(int64_t n) { return static_cast<size_t>(round_up(n * static_cast<int64_t>(sizeof(Mix)), 256) + round_up(n * 4, 256)); }
+
 }  // namespace
+
+size_t logprob_grad_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type) { return mix_bytes(n) + xent_need(n, num_rows, dim, type, true); }
 
 extern "C" {
 
 size_t ne_xent_workspace_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int32_t grad)
 {
     if (!xent_sizes_ok(n, num_rows, dim, type) || n == 0) return 0;
-    return std::max(xent_bytes(n, num_rows, dim, type, grad != 0), xent_layout(n, num_rows, dim, type, grad != 0, nullptr).total);
+    return xent_need(n, num_rows, dim, type, grad != 0);
 }
 
 ne_status ne_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type,
@@ -1159,10 +1227,7 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (n == 0) {
         if (!dw_dev) return NE_OK;
-        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(num_rows * dim, kThreads), 4096)));
-        if (type == NE_F32) hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(kThreads), 0, st, static_cast<float*>(dw_dev), dw_stride, num_rows, dim);
-        else hipLaunchKernelGGL(zero_kernel<bf16_t>, grid, dim3(kThreads), 0, st, static_cast<bf16_t*>(dw_dev), dw_stride, num_rows, dim);
-        NE_HIP_CHECK(hipGetLastError());
+        NE_HIP_CHECK(clear_gradient(dw_dev, dw_stride, num_rows, dim, type, st));
         return NE_OK;
     }
     if (!lse_dev || !aligned(lse_dev, 4) || !aligned(loss_grad_dev, 4)) return fail(NE_ERR_ARG, "ne_xent_grad: lse_dev is NULL, or it or loss_grad_dev misaligned");
@@ -1170,11 +1235,54 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < std::max(xent_bytes(n, num_rows, dim, type, true), w.total))
         return fail(NE_ERR_ARG, "ne_xent_grad: workspace_dev is NULL, not 256-byte aligned, or smaller than ne_xent_workspace_bytes()");
     if (!dh_dev && !dw_dev) return NE_OK;
-    auto run = [&](auto grad) { return grad(x, w, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st); };
-    const hipError_t e = w.few_blocks == 1 ? (type == NE_F32 ? run(run_few_grad<float, 1>) : run(run_few_grad<bf16_t, 1>))
-                         : w.few_blocks == 2 ? run(run_few_grad<float, 2>)
-                         : type == NE_F32 ? run(run_grad<2, float>) : run(run_grad<1, bf16_t>);
+    const hipError_t e = gradients(x, w, nullptr, lse_dev, scale, dh_dev, dh_stride, dw_dev, dw_stride, st);
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("cross entropy gradient launch: ") + hipGetErrorString(e));
+    return NE_OK;
+}
+
+ne_status ne_logprob_grad(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int32_t type, const int32_t* ids_dev,
+                          const float* lse_dev, const float* entropy_dev, const float* logp_grad_dev, const float* entropy_grad_dev, float logp_scale,
+                          float entropy_scale, int64_t n, int64_t num_rows, int32_t dim, void* dh_dev, int64_t dh_stride, void* dw_dev,
+                          int64_t dw_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream)
+{
+    const std::string who = "ne_logprob_grad: ";
+    if (!xent_sizes_ok(n, num_rows, dim, type)) return fail(NE_ERR_ARG, who + "n, num_rows, dim or type out of range");
+    if (h_stride < dim || w_stride < dim || (dh_dev && dh_stride < dim) || (dw_dev && dw_stride < dim))
+        return fail(NE_ERR_ARG, who + "a row stride is smaller than dim");
+    const size_t size = type_bytes(type);
+    if (!w_dev || !aligned(w_dev, size)) return fail(NE_ERR_ARG, who + "w_dev is NULL or misaligned");
+    if (!aligned(dh_dev, size) || !aligned(dw_dev, size)) return fail(NE_ERR_ARG, who + "dh_dev or dw_dev is misaligned");
+    if (!std::isfinite(logp_scale) || !std::isfinite(entropy_scale)) return fail(NE_ERR_ARG, who + "logp_scale or entropy_scale is not finite");
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (n == 0) {
+        if (dw_dev) NE_HIP_CHECK(clear_gradient(dw_dev, dw_stride, num_rows, dim, type, st));
+        return NE_OK;
+    }
+    if (!h_dev || !aligned(h_dev, size)) return fail(NE_ERR_ARG, who + "h_dev is NULL or misaligned");
+    if (!aligned(ids_dev, 4)) return fail(NE_ERR_ARG, who + "ids_dev is not 4-byte aligned");
+    if (!ids_dev && logp_scale != 0.0f) return fail(NE_ERR_ARG, who + "log probabilities need ids");
+    if (!lse_dev || !aligned(lse_dev, 4)) return fail(NE_ERR_ARG, who + "lse_dev is NULL or misaligned");
+    if (!aligned(entropy_dev, 4) || (!entropy_dev && entropy_scale != 0.0f)) return fail(NE_ERR_ARG, who + "entropy_dev is NULL or misaligned");
+    if (!aligned(logp_grad_dev, 4) || !aligned(entropy_grad_dev, 4)) return fail(NE_ERR_ARG, who + "logp_grad_dev or entropy_grad_dev is misaligned");
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < logprob_grad_bytes(n, num_rows, dim, type))
+        return fail(NE_ERR_ARG, who + "workspace_dev is NULL, not 256-byte aligned, or smaller than ne_logprob_workspace_bytes()");
+    if (!dh_dev && !dw_dev) return NE_OK;
+    const XentWs w = xent_layout(n, num_rows, dim, type, true, static_cast<char*>(workspace_dev) + mix_bytes(n));
+    SoftmaxCall x{h_dev, w_dev, h_stride, w_stride, n, num_rows, dim, type, ids_dev, logp_grad_dev};
+    hipError_t e;
+    if (entropy_scale == 0.0f && ids_dev) {         // the loss's gradient with its sign turned
+        e = gradients(x, w, nullptr, lse_dev, -logp_scale, dh_dev, dh_stride, dw_dev, dw_stride, st);
+    } else {
+        Carver take{static_cast<char*>(workspace_dev)};
+        Mix* mix = take.get<Mix>(static_cast<size_t>(n));
+        float* c = take.get<float>(static_cast<size_t>(n));
+        const MixArgs a{ids_dev, logp_grad_dev, entropy_grad_dev, entropy_dev, logp_scale, entropy_scale, n, static_cast<uint32_t>(num_rows), mix, c};
+        hipLaunchKernelGGL(mix_kernel, dim3(static_cast<unsigned>(ceil_div(n, kThreads))), dim3(kThreads), 0, st, a);
+        e = hipGetLastError();
+        x.c = c;
+        if (e == hipSuccess) e = gradients(x, w, mix, lse_dev, 1.0f, dh_dev, dh_stride, dw_dev, dw_stride, st);
+    }
+    if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("log probability gradient launch: ") + hipGetErrorString(e));
     return NE_OK;
 }
 
