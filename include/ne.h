@@ -486,6 +486,38 @@ ne_status ne_adamw_step(ne_adamw* opt, int64_t step, float lr, float beta1, floa
 void ne_destroy_adamw(ne_adamw* opt);
 
 /*
+ * An update whose singular values are brought near 1 by Newton-Schulz products, as the Muon optimizer takes them.  With X = x / |x| (the Frobenius
+ * norm; a matrix of zeros stays one), steps times, for rows >= cols (otherwise the same of the transposed matrix):
+ *   X = X (a + b G + c G^2),  G = X^T X,  a = 3.4445, b = -4.7750, c = 2.0315.
+ * After five steps singular values that were 1/400 of the norm or more are about 0.7 to 1.2.
+ *   x_dev, out_dev : device, x_type and out_type [rows][cols], row strides >= cols, aligned to their elements; out may be x itself (same
+ *                    type and stride), and must not overlap it otherwise.
+ *   steps          : 1 .. NE_ORTHOGONAL_MAX_STEPS.
+ *   workspace_dev  : at least ne_orthogonalize_workspace_bytes(rows, cols) bytes (0 there = invalid arguments or an empty matrix): 8 bytes an element
+ *                    and up to 33 MB for sums.
+ * Precision: products of operands with 22 bits, fp32 sums, the norm and the sums of G's parts in 64 bits: as far from the values in 64 bits as the same
+ * products one after the other in fp32.  Elements below 2^-16 of the largest keep 2^-38 of it.  A value that is not finite makes the result NaN.
+ *   0 <= rows, cols; max(rows, cols) < 2^31 - 128, min(rows, cols) <= NE_ORTHOGONAL_MAX_SIDE.  An empty matrix is a no-op.
+ * ne_muon_step is the optimizer's step of one matrix:
+ *   m = momentum m + grad_scale g,   u = nesterov ? grad_scale g + momentum m : m,
+ *   p = p (1 - lr weight_decay) - lr scale orthogonalized(u).
+ *   param_dev, momentum_dev : device, float [rows][cols]; grad_dev: grad_type [rows][cols]; param_bf16_dev: NULL, or bf16 [rows][cols], which
+ *                    receives a rounded copy of the new parameters.  Row strides >= cols; none may overlap another.  A momentum of zeros is that of
+ *                    a new run.
+ *   scale          : of the update, whose elements are about 1 / sqrt(max(rows, cols)): 0.2 sqrt(max(rows, cols)) makes steps as large as AdamW's.
+ *   lr, weight_decay >= 0, 0 <= momentum < 1, all finite.  Workspace and sizes as for ne_orthogonalize.
+ * Errors: NE_ERR_ARG, NE_ERR_HIP.
+ */
+enum { NE_ORTHOGONAL_MAX_SIDE = 4096, NE_ORTHOGONAL_MAX_STEPS = 10 };
+size_t ne_orthogonalize_workspace_bytes(int64_t rows, int64_t cols);
+ne_status ne_orthogonalize(const void* x_dev, int32_t x_type, int64_t x_stride, int64_t rows, int64_t cols, int32_t steps, void* out_dev,
+                           int32_t out_type, int64_t out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+ne_status ne_muon_step(float* param_dev, int64_t param_stride, const void* grad_dev, int32_t grad_type, int64_t grad_stride,
+                       float* momentum_dev, int64_t momentum_stride, void* param_bf16_dev, int64_t param_bf16_stride, int64_t rows,
+                       int64_t cols, int32_t steps, float lr, float momentum, int32_t nesterov, float weight_decay, float scale,
+                       float grad_scale, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Former tuning of the exact step: how a row that several references of a batch name collected their
  * deltas (list_cap: -1 or 0..8) and how finely hash positions were swept (sweep_per_thread: 0, 2, 4 or 8).
  * Neither choice exists any more: such a row has a list of coefficients and rows, and nothing is swept.  The

@@ -28,6 +28,8 @@ NE_BF16 = 1
 NE_OP_MAX_DIM = 16384
 NE_EMBED_MAX_IDS = 1 << 26
 NE_TOP_MAX = 64
+NE_ORTHOGONAL_MAX_SIDE = 4096
+NE_ORTHOGONAL_MAX_STEPS = 10
 NE_ADAMW_BLOCK = 256    # elements that share a scale with 8-bit states
 
 EXPORTS = (
@@ -36,6 +38,7 @@ EXPORTS = (
     "ne_embed_lookup", "ne_embed_workspace_bytes", "ne_embed_grad", "ne_xent_workspace_bytes", "ne_xent_loss", "ne_xent_grad",
     "ne_logprob_workspace_bytes", "ne_logprob", "ne_logprob_grad",
     "ne_adamw_workspace_bytes", "ne_create_adamw", "ne_adamw_step", "ne_destroy_adamw",
+    "ne_orthogonalize_workspace_bytes", "ne_orthogonalize", "ne_muon_step",
     "ne_score_pairs", "ne_set_tuning", "ne_validate_pairs", "ne_hash_position", "ne_profile_enable", "ne_profile_read", "ne_destroy_tables", "ne_destroy_alias", "ne_last_error",
 )
 
@@ -138,6 +141,13 @@ def lib() -> ctypes.CDLL:
     L.ne_adamw_step.restype = c.c_int
     L.ne_destroy_adamw.argtypes = [vp]
     L.ne_destroy_adamw.restype = None
+    L.ne_orthogonalize_workspace_bytes.argtypes = [c.c_int64, c.c_int64]
+    L.ne_orthogonalize_workspace_bytes.restype = c.c_size_t
+    L.ne_orthogonalize.argtypes = [vp, c.c_int32, c.c_int64, c.c_int64, c.c_int64, c.c_int32, vp, c.c_int32, c.c_int64, vp, c.c_size_t, vp]
+    L.ne_orthogonalize.restype = c.c_int
+    L.ne_muon_step.argtypes = [vp, c.c_int64, vp, c.c_int32, c.c_int64, vp, c.c_int64, vp, c.c_int64, c.c_int64, c.c_int64, c.c_int32,
+                               c.c_float, c.c_float, c.c_int32, c.c_float, c.c_float, c.c_float, vp, c.c_size_t, vp]
+    L.ne_muon_step.restype = c.c_int
     L.ne_set_tuning.argtypes = [vp, c.c_int32, c.c_int32]
     L.ne_set_tuning.restype = c.c_int
     L.ne_validate_pairs.argtypes = [vp, vp, c.c_int64, vp, vp]
@@ -691,6 +701,48 @@ def ne_adamw_step(opt: AdamW, step: int, lr: float, beta1: float = 0.9, beta2: f
                   grad_scale: float = 1.0, stream=None) -> None:
     """Step number `step` (from 1 on) of every tensor of the handle, with the gradients that its grads hold."""
     _check(lib().ne_adamw_step(opt.handle, step, lr, beta1, beta2, eps, grad_scale, _stream_ptr(stream)))
+
+
+def ne_orthogonalize_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().ne_orthogonalize_workspace_bytes(rows, cols))
+
+
+def ne_orthogonalize(x: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, steps: int = 5, stream=None) -> None:
+    """out = x with its singular values brought near 1 by Newton-Schulz products (out may be x itself); both CUDA float32 or bfloat16
+    matrices with contiguous rows.  workspace: CUDA uint8 of ne_orthogonalize_workspace_bytes(rows, cols) bytes."""
+    xp, xt, xs = _matrix(x, "x")
+    op, ot, os_ = _matrix(out, "out")
+    if out.shape != x.shape:
+        raise TypeError("out must have the shape of x")
+    _on_current_device(x, out, workspace)
+    wp = _dev_ptr(workspace, torch.uint8, "workspace")
+    _check(lib().ne_orthogonalize(xp, xt, xs, x.shape[0], x.shape[1], steps, op, ot, os_, wp,
+                                  workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
+
+
+def ne_muon_step(param: torch.Tensor, grad: torch.Tensor, momentum_buffer: torch.Tensor, workspace: torch.Tensor, lr: float, momentum: float = 0.95,
+                 nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0, steps: int = 5, grad_scale: float = 1.0,
+                 param_bf16: torch.Tensor | None = None, stream=None) -> None:
+    """Muon on one matrix: momentum_buffer = momentum * momentum_buffer + grad_scale * grad, then param -= lr * scale * orthogonalized update, after
+    its decay.  param and momentum_buffer CUDA float32, grad float32 or bfloat16, param_bf16 None or a bfloat16 copy that every step writes; all
+    [rows][cols] with contiguous rows.  workspace: CUDA uint8 of ne_orthogonalize_workspace_bytes(rows, cols) bytes."""
+    pp, pt, ps = _matrix(param, "param")
+    gp, gt, gs = _matrix(grad, "grad")
+    mp, mt, ms = _matrix(momentum_buffer, "momentum_buffer")
+    if pt != NE_F32 or mt != NE_F32:
+        raise TypeError("param and momentum_buffer must be torch.float32")
+    cp, cs = 0, 0
+    if param_bf16 is not None:
+        cp, ct, cs = _matrix(param_bf16, "param_bf16")
+        if ct != NE_BF16:
+            raise TypeError("param_bf16 must be torch.bfloat16")
+    for t, name in ((grad, "grad"), (momentum_buffer, "momentum_buffer"), (param_bf16, "param_bf16")):
+        if t is not None and t.shape != param.shape:
+            raise TypeError(f"{name} must have the shape of param")
+    _on_current_device(param, grad, momentum_buffer, workspace, param_bf16)
+    wp = _dev_ptr(workspace, torch.uint8, "workspace")
+    _check(lib().ne_muon_step(pp, ps, gp, gt, gs, mp, ms, cp, cs, param.shape[0], param.shape[1], steps, lr, momentum, 1 if nesterov else 0, weight_decay,
+                              scale, grad_scale, wp, workspace.numel() if workspace is not None else 0, _stream_ptr(stream)))
 
 
 def ne_set_tuning(tables: Tables, list_cap: int = -1, sweep_per_thread: int = 0) -> None:

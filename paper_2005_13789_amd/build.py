@@ -8,7 +8,7 @@ import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRCS = [os.path.join(PKG, "csrc", f) for f in ("ne.hip", "ne_shared.hip", "ne_embed.hip", "ne_xent.hip", "ne_logprob.hip", "ne_adamw.hip")]
+SRCS = [os.path.join(PKG, "csrc", f) for f in ("ne.hip", "ne_shared.hip", "ne_embed.hip", "ne_xent.hip", "ne_logprob.hip", "ne_adamw.hip", "ne_muon.hip")]
 OUT = os.path.join(PKG, "libne.so")
 
 HIPCC_FLAGS = [

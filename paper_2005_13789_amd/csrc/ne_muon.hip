@@ -1,0 +1,704 @@
+// Updates whose singular values are brought near 1 by Newton-Schulz products: ne_orthogonalize, ne_muon_step.
+//
+//     X <- M / |M|_F,   then steps times   X <- X (a + b G + c G^2),  G = X^T X     (of the smaller side; a wide M is taken transposed)
+//
+// A step multiplies X from the right by a polynomial of its own G, and all these polynomials commute.  So instead of two products with X
+// for every step, X is read twice for several steps: once for G, then G's successors G <- G Q^2 and P = Q Q' .. are made of the small side alone
+// (Q = a + b G + c G^2), then X <- X P.  How many steps a G can serve is a matter of digits: a direction of X of singular value
+// s is s^2 in G, beside errors of 2^-24 of the largest, so weak directions are lost first.  A step brings them up by 3.4445; three steps, then a new G
+// and two more leave an error like that of the products taken one after the other in fp32 (all five at once: up to a hundred times that).
+//
+// All products are of fp16 halves at a power of two (x 2^k = hi + lo, 22 bits), three matrix instructions each, with fp32 sums: about the error
+// of an fp32 product.  X's power follows from its largest magnitude, those of the others from what they are: singular values of G's successors
+// and of X stay below 1.3, of Q below 3.45, of P of three steps below 41.  G is the sum of a long contraction: sums of 256 rows
+// are added to a second set of registers, and the workgroups' shares in 64 bits.
+#include "ne_tiles.h"
+
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr int kSmallShift = 13, kPShift = 10;          // powers of two of G, Q and later X; of products of Qs
+constexpr int kStatBlocks = 1024;
+constexpr int kMostSplits = 512;
+constexpr int kFlush = 8;                              // stages whose sums are added up apart
+constexpr int kSide = 128;                             // of a tile of G
+
+// A matrix of halves, rows of `stride` elements.
+struct Halves {
+    uint16_t* part[2];
+    int64_t stride;
+};
+
+struct Scalars {
+    double inverse;         // 1 / |M|_F, 0 for a matrix of zeros
+    int32_t shift;          // power of two of X's first halves
+};
+
+// ---------------------------------------------------------------------------------------------
+// momentum, norm, largest magnitude
+// ---------------------------------------------------------------------------------------------
+// (u is what is brought to singular values near 1: x itself, or with momentum m <- beta m + g the sum that g's look ahead makes of it)
+struct UpdateArgs {
+    const void* g;
+    int64_t g_stride;
+    float* m;               // NULL: u = g
+    int64_t m_stride;
+    int64_t rows;
+    int32_t cols;
+    float grad_scale, beta;
+    int32_t nesterov;
+    double* squares;        // [kStatBlocks]
+    float* amax;            // [kStatBlocks]
+};
+
+__device__ __forceinline__ float update_of(const UpdateArgs& a, float g, float m) { return a.nesterov ? fmaf(a.beta, m, a.grad_scale * g) : m; }
+
+template <class T, bool MOMENTUM>
+__global__ void __launch_bounds__(kThreads) stats_kernel(UpdateArgs a)
+{
+    __shared__ float lds[kThreads / 64];
+    __shared__ double sums[kThreads / 64];
+    double total = 0.0;
+    float top = 0.0f;
+    const int64_t pieces = (a.cols + 7) / 8, all = a.rows * pieces, stride = static_cast<int64_t>(gridDim.x) * kThreads;
+    constexpr int FLIGHT = 4;
+    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i0 < all; i0 += FLIGHT * stride) {
+        T g[FLIGHT][8];
+        float m[FLIGHT][8];
+        int64_t row[FLIGHT];
+        int e[FLIGHT];
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            const int64_t i = i0 + f * stride;
+            row[f] = i / pieces;
+            e[f] = static_cast<int>(i - row[f] * pieces) * 8;
+            if (i >= all) continue;
+            load_eight(static_cast<const T*>(a.g) + row[f] * a.g_stride, e[f], a.cols, g[f]);
+            if (MOMENTUM) load_eight(a.m + row[f] * a.m_stride, e[f], a.cols, m[f]);
+        }
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            if (i0 + f * stride >= all) continue;
+            float most = 0.0f, u[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                u[q] = static_cast<float>(g[f][q]);
+                if (MOMENTUM) {
+                    m[f][q] = fmaf(a.beta, m[f][q], a.grad_scale * u[q]);
+                    u[q] = update_of(a, u[q], m[f][q]);
+                }
+                most = fmaxf(most, finite_abs(u[q]));
+                total = fma(static_cast<double>(u[q]), static_cast<double>(u[q]), total);
+            }
+            top = fmaxf(top, most);
+            if (MOMENTUM) {
+                float* to = a.m + row[f] * a.m_stride + e[f];
+                store_some<float, 8>(to, a.cols - e[f], m[f]);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = total;
+    top = block_max(top, lds);
+    if (threadIdx.x == 0) {
+        a.squares[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+        a.amax[blockIdx.x] = top;
+    }
+}
+
+// X's halves: rows and columns up to multiples of 32, zeros beyond the matrix; a wide matrix transposed.
+struct PackUpdateArgs {
+    UpdateArgs u;
+    Halves x;
+    int64_t tall, padded_tall;      // rows of X
+    int32_t small, padded_small;    // columns
+    Scalars* scalars;
+};
+
+__device__ __forceinline__ int first_shift(const UpdateArgs& a, float* lds)
+{
+    float top = 0.0f;
+    for (int i = threadIdx.x; i < kStatBlocks; i += kThreads) top = fmaxf(top, a.amax[i]);
+    return shift_of(block_max(top, lds));
+}
+
+__device__ __forceinline__ void split_half(float x, int shift, short& hi, short& lo)
+{
+    const float y = ldexpf(x, shift);
+    const f16_t h = static_cast<f16_t>(y);
+    hi = __builtin_bit_cast(short, h);
+    lo = __builtin_bit_cast(short, static_cast<f16_t>(y - static_cast<float>(h)));
+}
+
+template <class T, bool MOMENTUM, bool WIDE>
+__global__ void __launch_bounds__(kThreads) pack_update_kernel(PackUpdateArgs a)
+{
+    __shared__ float lds[kThreads / 64];
+    __shared__ double sums[kThreads];
+    __shared__ uint32_t turn[WIDE ? 64 * 65 : 1];
+    const int shift = first_shift(a.u, lds);
+    if (blockIdx.x == 0) {
+        double total = 0.0;
+        for (int i = threadIdx.x; i < kStatBlocks; i += kThreads) total += a.u.squares[i];
+        sums[threadIdx.x] = total;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            total = 0.0;
+            for (int i = 0; i < kThreads; ++i) total += sums[i];
+            a.scalars->inverse = total == 0.0 ? 0.0 : 1.0 / sqrt(total);
+            a.scalars->shift = shift;
+        }
+    }
+    auto value = [&](int64_t row, int e, float (&u)[8]) {
+        T g[8];
+        load_eight(static_cast<const T*>(a.u.g) + row * a.u.g_stride, e, a.u.cols, g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) u[q] = static_cast<float>(g[q]);
+        if (MOMENTUM) {
+            float m[8];
+            load_eight(a.u.m + row * a.u.m_stride, e, a.u.cols, m);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) u[q] = update_of(a.u, u[q], m[q]);
+        }
+    };
+    if constexpr (!WIDE) {
+        const int64_t pieces = a.padded_small / 8, all = a.padded_tall * pieces;
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+            const int64_t row = i / pieces;
+            const int e = static_cast<int>(i - row * pieces) * 8;
+            s16x8 hi = {}, lo = {};
+            if (row < a.tall && e < a.small) {
+                float u[8];
+                value(row, e, u);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    short h, l;
+                    split_half(u[q], shift, h, l);
+                    hi[q] = h;
+                    lo[q] = l;
+                }
+            }
+            *reinterpret_cast<s16x8*>(a.x.part[0] + row * a.x.stride + e) = hi;
+            *reinterpret_cast<s16x8*>(a.x.part[1] + row * a.x.stride + e) = lo;
+        }
+    } else {
+        // 64 x 64 at a time, by way of LDS: matrix rows are X's columns
+        const int64_t across = (a.padded_tall + 63) / 64, down = (a.padded_small + 63) / 64;
+        for (int64_t t = blockIdx.x; t < across * down; t += gridDim.x) {
+            const int64_t x0 = t / down * 64;
+            const int c0 = static_cast<int>(t % down) * 64;
+            __syncthreads();
+            for (int i = threadIdx.x; i < 64 * 8; i += kThreads) {
+                const int r = i >> 3, e = (i & 7) * 8;
+                float u[8] = {};
+                if (c0 + r < a.small && x0 + e < a.tall) value(c0 + r, static_cast<int>(x0 + e), u);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    short h, l;
+                    split_half(u[q], shift, h, l);
+                    turn[(e + q) * 65 + r] = static_cast<uint16_t>(h) | static_cast<uint32_t>(static_cast<uint16_t>(l)) << 16;
+                }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < 64 * 8; i += kThreads) {
+                const int r = i >> 3, e = (i & 7) * 8;
+                if (x0 + r >= a.padded_tall || c0 + e >= a.padded_small) continue;
+                s16x8 hi, lo;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t both = turn[r * 65 + e + q];
+                    hi[q] = static_cast<short>(both & 0xFFFF);
+                    lo[q] = static_cast<short>(both >> 16);
+                }
+                *reinterpret_cast<s16x8*>(a.x.part[0] + (x0 + r) * a.x.stride + c0 + e) = hi;
+                *reinterpret_cast<s16x8*>(a.x.part[1] + (x0 + r) * a.x.stride + c0 + e) = lo;
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// G = X^T X
+// ---------------------------------------------------------------------------------------------
+struct GramArgs {
+    Operand x;              // across: element (column, row of X)
+    uint32_t tiles, splits, share, stages;      // tiles of a side; stages of a split, of all
+    float* part;            // [splits][pairs][kSide][kSide]
+};
+
+// Tile pairs (i, j), i <= j, one after the other.
+__device__ __forceinline__ void pair_at(uint32_t p, uint32_t tiles, uint32_t& i, uint32_t& j)
+{
+    i = 0;
+    while (p >= tiles - i) {
+        p -= tiles - i;
+        ++i;
+    }
+    j = i + p;
+}
+
+__global__ void __launch_bounds__(256, 2) gram_kernel(GramArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<4>()];
+    const uint32_t pairs = a.tiles * (a.tiles + 1) / 2, b = by_xcd(blockIdx.x, gridDim.x), split = b / pairs, pair = b - split * pairs;
+    uint32_t ti, tj;
+    pair_at(pair, a.tiles, ti, tj);
+    const uint32_t s0 = min(split * a.share, a.stages), s1 = min(s0 + a.share, a.stages);
+    f32x16 acc[2][2], all[2][2];
+    clear(acc);
+    clear(all);
+    if (s0 < s1) {
+        Loader<2, 4, false> load_a, load_b;
+        load_a.start(a.x, ti * kSide, s0);
+        load_b.start(a.x, tj * kSide, s0);
+        uint32_t done = 0;
+        run_stages<4>(
+            s1 - s0, lds,
+            [&](uint32_t to) {
+                load_a.fetch(to);
+                if (ti != tj) load_b.fetch(to + operand_bytes<4>());
+            },
+            [&](const unsigned char* stage) {
+                multiply<2, 4, false, false>(stage, acc, ti == tj ? 0 : operand_bytes<4>());
+                if ((++done & (kFlush - 1)) == 0) {
+#pragma unroll
+                    for (int im = 0; im < 2; ++im)
+#pragma unroll
+                        for (int in = 0; in < 2; ++in) all[im][in] += acc[im][in];
+                    clear(acc);
+                }
+            });
+    }
+    const int lane = threadIdx.x & 63;
+    float* out = a.part + (static_cast<int64_t>(split) * pairs + pair) * (kSide * kSide);
+#pragma unroll
+    for (int im = 0; im < 2; ++im)
+#pragma unroll
+        for (int in = 0; in < 2; ++in)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                out[(first_row<4>() + 32 * im + sum_row(i) + lane_row()) * kSide + first_col<4>() + 32 * in + (lane & 31)] = all[im][in][i] + acc[im][in][i];
+}
+
+// The splits' sums, joined in 64 bits and scaled; both triangles.
+struct GramJoinArgs {
+    const float* part;
+    uint32_t tiles, splits;
+    int32_t padded_small;
+    const Scalars* scalars; // NULL: X's halves are of X 2^kSmallShift
+    Halves g;
+};
+
+__device__ __forceinline__ void put(const Halves& to, int64_t row, int64_t col, float x, int shift)
+{
+    short hi, lo;
+    split_half(x, shift, hi, lo);
+    to.part[0][row * to.stride + col] = static_cast<uint16_t>(hi);
+    to.part[1][row * to.stride + col] = static_cast<uint16_t>(lo);
+}
+
+__global__ void __launch_bounds__(kThreads) gram_join_kernel(GramJoinArgs a)
+{
+    // 64 elements of a row of a tile pair, whose splits four wavefronts share
+    __shared__ double lds[kThreads];
+    const uint32_t pairs = a.tiles * (a.tiles + 1) / 2, per = kSide * kSide / 64, pair = blockIdx.x / per, at = (blockIdx.x % per) * 64 + (threadIdx.x & 63);
+    uint32_t ti, tj;
+    pair_at(pair, a.tiles, ti, tj);
+    const int64_t row = ti * kSide + at / kSide, col = tj * kSide + at % kSide;
+    if (row >= a.padded_small) return;      // (the same for all of the workgroup)
+    double sum = 0.0;
+    const float* from = a.part + static_cast<int64_t>(pair) * (kSide * kSide) + at;
+#pragma unroll 8
+    for (uint32_t s = threadIdx.x >> 6; s < a.splits; s += 4) sum += static_cast<double>(from[static_cast<int64_t>(s) * pairs * (kSide * kSide)]);
+    lds[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 64 || col >= a.padded_small || row > col) return;
+    sum = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
+    if (a.scalars) sum = ldexp(sum * a.scalars->inverse * a.scalars->inverse, -2 * a.scalars->shift);
+    else sum = ldexp(sum, -2 * kSmallShift);
+    put(a.g, row, col, static_cast<float>(sum), kSmallShift);
+    if (row != col) put(a.g, col, row, static_cast<float>(sum), kSmallShift);
+}
+
+// ---------------------------------------------------------------------------------------------
+// products of the small side
+// ---------------------------------------------------------------------------------------------
+// All of them are polynomials of one symmetric matrix, so they are symmetric, commute, and rows serve as columns.  A workgroup has a tile of
+// 32 x 32 on or above the diagonal, its four wavefronts a quarter of the contraction each, straight from L2 into the matrix cores' operands.
+struct SmallJob {
+    Halves a, b, out;
+    float factor;           // 2 to the minus sum of both powers
+    int32_t shift;          // power of two of what is written
+    int32_t polynomial;     // out = kA + kB a + kC (a b), for a = b = G
+};
+
+struct SmallArgs {
+    SmallJob job[2];
+    int32_t side;           // multiple of 32
+};
+
+__device__ __forceinline__ s16x8 row_piece(const uint16_t* p) { return *reinterpret_cast<const s16x8*>(p); }
+
+__global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
+{
+    __shared__ __align__(16) float lds[4][32 * 33];
+    const SmallJob& job = args.job[blockIdx.y];
+    const uint32_t tiles = args.side / 32;
+    uint32_t ti, tj;
+    pair_at(blockIdx.x, tiles, ti, tj);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, steps = args.side / 16;
+    const int64_t a_at = static_cast<int64_t>(ti * 32 + (lane & 31)) * job.a.stride + (lane >> 5) * 8;
+    const int64_t b_at = static_cast<int64_t>(tj * 32 + (lane & 31)) * job.b.stride + (lane >> 5) * 8;
+    const uint16_t *ah = job.a.part[0] + a_at, *al = job.a.part[1] + a_at, *bh = job.b.part[0] + b_at, *bl = job.b.part[1] + b_at;
+    f32x16 sum, small;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] = small[i] = 0.0f;
+    constexpr int FLIGHT = 4;
+    for (int s0 = wave; s0 < steps; s0 += 4 * FLIGHT) {
+        s16x8 a0[FLIGHT] = {}, a1[FLIGHT] = {}, b0[FLIGHT] = {}, b1[FLIGHT] = {};
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            const int at = (s0 + 4 * f) * 16;
+            if (s0 + 4 * f >= steps) break;
+            a0[f] = row_piece(ah + at);
+            a1[f] = row_piece(al + at);
+            b0[f] = row_piece(bh + at);
+            b1[f] = row_piece(bl + at);
+        }
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            small = mfma<2>(a0[f], b1[f], small);
+            small = mfma<2>(a1[f], b0[f], small);
+            sum = mfma<2>(a0[f], b0[f], sum);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lds[wave][(sum_row(i) + lane_row()) * 33 + (lane & 31)] = sum[i] + small[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * 32; i += 256) {
+        const int r = i >> 5, c = i & 31;
+        const int64_t row = ti * 32 + r, col = tj * 32 + c;
+        if (row > col) continue;
+        const int at = r * 33 + c;
+        float x = ((lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at])) * job.factor;
+        if (job.polynomial) {
+            const int64_t g_at = row * job.a.stride + col;
+            const float g = (static_cast<float>(__builtin_bit_cast(f16_t, job.a.part[0][g_at])) + static_cast<float>(__builtin_bit_cast(f16_t, job.a.part[1][g_at]))) *
+                            (1.0f / (1 << kSmallShift));
+            x = fmaf(kC, x, kB * g) + (row == col ? kA : 0.0f);
+        }
+        put(job.out, row, col, x, job.shift);
+        if (row != col) put(job.out, col, row, x, job.shift);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// X <- X P, and what becomes of the last one
+// ---------------------------------------------------------------------------------------------
+struct ApplyArgs {
+    Operand x, p;           // both by rows (P is symmetric)
+    uint32_t row_tiles, splits, col_tiles;
+    int32_t steps;
+    int64_t tall, padded_tall;
+    int32_t small, padded_small;
+    const Scalars* scalars; // NULL: X's halves are of X 2^kSmallShift
+    // one of: the next X's halves; a matrix out; parameters
+    Halves next;
+    void* out;
+    int64_t out_stride;
+    float* param;
+    int64_t param_stride;
+    bf16_t* copy;
+    int64_t copy_stride;
+    float keep, step;       // p keep - step o
+};
+
+enum Last { kNext, kFloat, kBfloat, kParam };
+
+template <Last L, bool WIDE>
+__device__ __forceinline__ void finish(const ApplyArgs& a, int64_t row, int col, float x)
+{
+    if (row >= a.tall || col >= a.small) return;
+    const int64_t r = WIDE ? col : row, c = WIDE ? row : col;
+    if (L == kFloat) static_cast<float*>(a.out)[r * a.out_stride + c] = x;
+    if (L == kBfloat) static_cast<bf16_t*>(a.out)[r * a.out_stride + c] = static_cast<bf16_t>(x);
+    if (L == kParam) {
+        float* p = a.param + r * a.param_stride + c;
+        const float now = fmaf(-a.step, x, *p * a.keep);
+        *p = now;
+        if (a.copy) a.copy[r * a.copy_stride + c] = static_cast<bf16_t>(now);
+    }
+}
+
+template <int KS, Last L, bool WIDE>
+__global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
+{
+    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<4>()];
+    const int lane = threadIdx.x & 63, m0 = first_row<4>(), n0 = first_col<4>();
+    uint32_t col_tile, split;
+    pair_of(by_xcd(blockIdx.x, gridDim.x), a.col_tiles, a.splits, col_tile, split);
+    const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
+    const float factor = a.scalars ? static_cast<float>(ldexp(a.scalars->inverse, -(a.scalars->shift + kPShift))) : ldexpf(1.0f, -(kSmallShift + kPShift));
+    all_scores<2, 4, KS>(a.x, a.p, col_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+#pragma unroll
+        for (int im = 0; im < 2; ++im)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int64_t row = static_cast<int64_t>(tile_row0) + m0 + 32 * im + sum_row(i) + lane_row();
+                    const int col = col_tile * kSide + n0 + 32 * j + (lane & 31);
+                    const float x = acc[im][j][i] * factor;
+                    if (L == kNext) {
+                        if (row < a.padded_tall && col < a.padded_small) put(a.next, row, col, x, kSmallShift);
+                    } else {
+                        finish<L, WIDE>(a, row, col, x);
+                    }
+                }
+    });
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+struct MuonWs {
+    int64_t tall, padded_tall;
+    int32_t small, padded_small;
+    bool wide;
+    uint32_t tiles, pairs, splits, share, stages;
+    double* squares;
+    float* amax;
+    Scalars* scalars;
+    Halves x[2];
+    float* part;
+    Halves g[7];
+    size_t total;
+};
+
+MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
+{
+    MuonWs w{};
+    w.wide = cols > rows;
+    w.tall = w.wide ? cols : rows;
+    w.small = static_cast<int32_t>(w.wide ? rows : cols);
+    w.padded_tall = round_up(w.tall, 32);
+    w.padded_small = static_cast<int32_t>(round_up(w.small, 32));
+    w.tiles = static_cast<uint32_t>(ceil_div(w.padded_small, kSide));
+    w.pairs = w.tiles * (w.tiles + 1) / 2;
+    // splits of the long contraction: two workgroups a CU, of eight stages at least
+    w.stages = static_cast<uint32_t>(w.padded_tall / step_of<2>());
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(ceil_div(kMostSplits, w.pairs), w.stages / kFlush));
+    w.share = static_cast<uint32_t>(ceil_div(w.stages, most));
+    w.splits = static_cast<uint32_t>(ceil_div(w.stages, w.share));
+    Carver take{base};
+    w.squares = take.get<double>(kStatBlocks);
+    w.amax = take.get<float>(kStatBlocks);
+    w.scalars = take.get<Scalars>(1);
+    for (auto& x : w.x) {
+        for (auto& p : x.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_tall) * w.padded_small);
+        x.stride = w.padded_small;
+    }
+    w.part = take.get<float>(static_cast<size_t>(w.splits) * w.pairs * kSide * kSide);
+    for (auto& g : w.g) {
+        for (auto& p : g.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_small) * w.padded_small);
+        g.stride = w.padded_small;
+    }
+    w.total = take.total();
+    return w;
+}
+
+// The polynomial of `steps` steps from G (w.g[0]) on; returns where it is.
+hipError_t polynomial(const MuonWs& w, int steps, Halves* result, hipStream_t st)
+{
+    Halves g = w.g[0], q = w.g[1], t = w.g[2], next = w.g[3], q2 = w.g[4], p = q, p2 = w.g[5], p3 = w.g[6];
+    const uint32_t tiles = static_cast<uint32_t>(w.padded_small / 32);
+    SmallArgs args{};
+    args.side = w.padded_small;
+    int jobs = 0;
+    int p_shift = kSmallShift;
+    auto add = [&](const Halves& a, int sa, const Halves& b, int sb, const Halves& out, int so, bool poly) {
+        args.job[jobs++] = SmallJob{a, b, out, ldexpf(1.0f, -(sa + sb)), so, poly ? 1 : 0};
+    };
+    auto run = [&]() {
+        hipLaunchKernelGGL(small_kernel, dim3(tiles * (tiles + 1) / 2, jobs), dim3(256), 0, st, args);
+        jobs = 0;
+        return hipGetLastError();
+    };
+    hipError_t e;
+    // (a single step's polynomial is P at once)
+    add(g, kSmallShift, g, kSmallShift, q, steps == 1 ? kPShift : kSmallShift, true);
+    if ((e = run()) != hipSuccess) return e;
+    for (int s = 1; s < steps; ++s) {
+        // G Q, then G Q^2 and its polynomial, then P times that beside the next G Q
+        if (s == 1) {
+            add(g, kSmallShift, q, kSmallShift, t, kSmallShift, false);
+            if ((e = run()) != hipSuccess) return e;
+        }
+        add(t, kSmallShift, q, kSmallShift, next, kSmallShift, false);
+        if ((e = run()) != hipSuccess) return e;
+        std::swap(g, next);
+        add(g, kSmallShift, g, kSmallShift, q2, kSmallShift, true);
+        if ((e = run()) != hipSuccess) return e;
+        add(p, p_shift, q2, kSmallShift, p2, kPShift, false);
+        if (s + 1 < steps) add(g, kSmallShift, q2, kSmallShift, t, kSmallShift, false);
+        if ((e = run()) != hipSuccess) return e;
+        p_shift = kPShift;
+        if (s == 1) {
+            p = p2;
+            p2 = p3;
+        } else {
+            std::swap(p, p2);
+        }
+        std::swap(q, q2);
+    }
+    *result = p;
+    return hipSuccess;
+}
+
+// What is done with the last product.
+struct Result {
+    Last kind;
+    void* out;
+    int64_t out_stride;
+    float* param;
+    int64_t param_stride;
+    void* copy;
+    int64_t copy_stride;
+    float keep, step;
+};
+
+template <int KS>
+void launch_apply(const ApplyArgs& a, Last kind, bool wide, dim3 grid, hipStream_t st)
+{
+    if (kind == kNext) hipLaunchKernelGGL((apply_kernel<KS, kNext, false>), grid, dim3(256), 0, st, a);
+    else if (kind == kFloat && !wide) hipLaunchKernelGGL((apply_kernel<KS, kFloat, false>), grid, dim3(256), 0, st, a);
+    else if (kind == kFloat) hipLaunchKernelGGL((apply_kernel<KS, kFloat, true>), grid, dim3(256), 0, st, a);
+    else if (kind == kBfloat && !wide) hipLaunchKernelGGL((apply_kernel<KS, kBfloat, false>), grid, dim3(256), 0, st, a);
+    else if (kind == kBfloat) hipLaunchKernelGGL((apply_kernel<KS, kBfloat, true>), grid, dim3(256), 0, st, a);
+    else if (!wide) hipLaunchKernelGGL((apply_kernel<KS, kParam, false>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((apply_kernel<KS, kParam, true>), grid, dim3(256), 0, st, a);
+}
+
+hipError_t apply(const MuonWs& w, const Halves& x, const Scalars* scalars, const Halves& p, const Halves* next, const Result& r, hipStream_t st)
+{
+    ApplyArgs a{};
+    a.x = packed_operand(x.part, w.padded_tall, w.padded_small);     // (X's rows of zeros stay such)
+    a.p = packed_operand(p.part, w.padded_small, w.padded_small);
+    a.row_tiles = static_cast<uint32_t>(ceil_div(w.tall, kSide));
+    a.col_tiles = w.tiles;
+    a.splits = splits_of(a.row_tiles, a.col_tiles, false);
+    a.steps = w.padded_small / step_of<2>();
+    a.tall = w.tall; a.padded_tall = w.padded_tall; a.small = w.small; a.padded_small = w.padded_small; a.scalars = scalars;
+    if (next) a.next = *next;
+    a.out = r.out; a.out_stride = r.out_stride; a.param = r.param; a.param_stride = r.param_stride;
+    a.copy = static_cast<bf16_t*>(r.copy); a.copy_stride = r.copy_stride; a.keep = r.keep; a.step = r.step;
+    const Last kind = next ? kNext : r.kind;
+    const dim3 grid(a.col_tiles * a.splits);
+    const int held = a.steps > 4 || ceil_div(a.row_tiles, a.splits) < 3 ? 0 : a.steps > 2 ? 4 : 2;
+    if (held == 0) launch_apply<0>(a, kind, w.wide, grid, st);
+    else if (held == 2) launch_apply<2>(a, kind, w.wide, grid, st);
+    else launch_apply<4>(a, kind, w.wide, grid, st);
+    return hipGetLastError();
+}
+
+template <class T, bool MOMENTUM>
+hipError_t run_update(const UpdateArgs& u, const MuonWs& w, int steps, const Result& r, hipStream_t st)
+{
+    hipLaunchKernelGGL((stats_kernel<T, MOMENTUM>), dim3(kStatBlocks), dim3(kThreads), 0, st, u);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const PackUpdateArgs pack{u, w.x[0], w.tall, w.padded_tall, w.small, w.padded_small, w.scalars};
+    const int64_t items = w.wide ? ceil_div(w.padded_tall, 64) * ceil_div(w.padded_small, 64) : ceil_div(w.padded_tall * (w.padded_small / 8), kThreads);
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 8192)));
+    if (w.wide) hipLaunchKernelGGL((pack_update_kernel<T, MOMENTUM, true>), grid, dim3(kThreads), 0, st, pack);
+    else hipLaunchKernelGGL((pack_update_kernel<T, MOMENTUM, false>), grid, dim3(kThreads), 0, st, pack);
+    e = hipGetLastError();
+    int which = 0, take = 3;            // the first G serves three steps, later ones two
+    for (int left = steps; left > 0 && e == hipSuccess; which ^= 1, take = 2) {
+        const int now = std::min(left, take);
+        const Scalars* scalars = left == steps ? w.scalars : nullptr;
+        GramArgs g{};
+        g.x = Operand{{w.x[which].part[0], w.x[which].part[1]}, w.padded_small, static_cast<uint32_t>(w.padded_tall - 1), static_cast<uint32_t>(w.padded_small)};
+        g.tiles = w.tiles; g.splits = w.splits; g.share = w.share; g.stages = w.stages; g.part = w.part;
+        hipLaunchKernelGGL(gram_kernel, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_small, scalars, w.g[0]};
+        hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(kThreads), 0, st, j);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        Halves p;
+        if ((e = polynomial(w, now, &p, st)) != hipSuccess) return e;
+        left -= now;
+        e = apply(w, w.x[which], scalars, p, left > 0 ? &w.x[which ^ 1] : nullptr, r, st);
+    }
+    return e;
+}
+
+bool muon_sizes_ok(int64_t rows, int64_t cols)
+{
+    return rows >= 0 && cols >= 0 && std::max(rows, cols) < (1ll << 31) - 128 && std::min(rows, cols) <= NE_ORTHOGONAL_MAX_SIDE;
+}
+
+// Whether some of `rows` rows of `cols` elements, `stride` apart, share places.
+bool rows_overlap(int64_t rows, int64_t cols, int64_t stride) { return rows > 1 && stride < cols; }
+
+}  // namespace
+
+extern "C" {
+
+size_t ne_orthogonalize_workspace_bytes(int64_t rows, int64_t cols)
+{
+    return muon_sizes_ok(rows, cols) && rows > 0 && cols > 0 ? muon_layout(rows, cols, nullptr).total : 0;
+}
+
+ne_status ne_orthogonalize(const void* x_dev, int32_t x_type, int64_t x_stride, int64_t rows, int64_t cols, int32_t steps, void* out_dev,
+                           int32_t out_type, int64_t out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream)
+{
+    const std::string who = "ne_orthogonalize: ";
+    if (!muon_sizes_ok(rows, cols) || !type_ok(x_type) || !type_ok(out_type) || steps < 1 || steps > NE_ORTHOGONAL_MAX_STEPS)
+        return fail(NE_ERR_ARG, who + "rows, cols, steps or a type out of range");
+    if (rows_overlap(rows, cols, x_stride) || rows_overlap(rows, cols, out_stride)) return fail(NE_ERR_ARG, who + "a row stride is smaller than cols");
+    if (rows == 0 || cols == 0) return NE_OK;
+    if (!x_dev || !aligned(x_dev, type_bytes(x_type)) || !out_dev || !aligned(out_dev, type_bytes(out_type)))
+        return fail(NE_ERR_ARG, who + "x_dev or out_dev is NULL or misaligned");
+    const MuonWs w = muon_layout(rows, cols, static_cast<char*>(workspace_dev));
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
+        return fail(NE_ERR_ARG, who + "workspace_dev is NULL, not 256-byte aligned, or smaller than ne_orthogonalize_workspace_bytes()");
+    const UpdateArgs u{x_dev, x_stride, nullptr, 0, rows, static_cast<int32_t>(cols), 1.0f, 0.0f, 0, w.squares, w.amax};
+    const Result r{out_type == NE_F32 ? kFloat : kBfloat, out_dev, out_stride, nullptr, 0, nullptr, 0, 0.0f, 0.0f};
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = x_type == NE_F32 ? run_update<float, false>(u, w, steps, r, st) : run_update<bf16_t, false>(u, w, steps, r, st);
+    if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("orthogonalize launch: ") + hipGetErrorString(e));
+    return NE_OK;
+}
+
+ne_status ne_muon_step(float* param_dev, int64_t param_stride, const void* grad_dev, int32_t grad_type, int64_t grad_stride, float* momentum_dev,
+                       int64_t momentum_stride, void* param_bf16_dev, int64_t param_bf16_stride, int64_t rows, int64_t cols, int32_t steps, float lr,
+                       float momentum, int32_t nesterov, float weight_decay, float scale, float grad_scale, void* workspace_dev, size_t workspace_bytes,
+                       void* hip_stream)
+{
+    const std::string who = "ne_muon_step: ";
+    if (!muon_sizes_ok(rows, cols) || !type_ok(grad_type) || steps < 1 || steps > NE_ORTHOGONAL_MAX_STEPS)
+        return fail(NE_ERR_ARG, who + "rows, cols, steps or grad_type out of range");
+    if (!(std::isfinite(lr) && lr >= 0.0f && momentum >= 0.0f && momentum < 1.0f && std::isfinite(weight_decay) && weight_decay >= 0.0f &&
+          std::isfinite(scale) && std::isfinite(grad_scale) && std::isfinite(lr * scale) && std::isfinite(lr * weight_decay)))
+        return fail(NE_ERR_ARG, who + "lr, momentum, weight_decay, scale or grad_scale out of range");
+    if (rows_overlap(rows, cols, param_stride) || rows_overlap(rows, cols, grad_stride) || rows_overlap(rows, cols, momentum_stride) ||
+        (param_bf16_dev && rows_overlap(rows, cols, param_bf16_stride)))
+        return fail(NE_ERR_ARG, who + "a row stride is smaller than cols");
+    if (rows == 0 || cols == 0) return NE_OK;
+    if (!param_dev || !aligned(param_dev, 4) || !grad_dev || !aligned(grad_dev, type_bytes(grad_type)) || !momentum_dev || !aligned(momentum_dev, 4) ||
+        !aligned(param_bf16_dev, 2))
+        return fail(NE_ERR_ARG, who + "a matrix is NULL or misaligned");
+    const MuonWs w = muon_layout(rows, cols, static_cast<char*>(workspace_dev));
+    if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
+        return fail(NE_ERR_ARG, who + "workspace_dev is NULL, not 256-byte aligned, or smaller than ne_orthogonalize_workspace_bytes()");
+    const UpdateArgs u{grad_dev, grad_stride, momentum_dev, momentum_stride, rows, static_cast<int32_t>(cols), grad_scale, momentum, nesterov != 0, w.squares, w.amax};
+    const Result r{kParam, nullptr, 0, param_dev, param_stride, param_bf16_dev, param_bf16_stride, 1.0f - lr * weight_decay, lr * scale};
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = grad_type == NE_F32 ? run_update<float, true>(u, w, steps, r, st) : run_update<bf16_t, true>(u, w, steps, r, st);
+    if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("Muon step launch: ") + hipGetErrorString(e));
+    return NE_OK;
+}
+
+}  // extern "C"

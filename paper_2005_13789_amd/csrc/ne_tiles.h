@@ -182,14 +182,14 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
 template <int W> __device__ __forceinline__ int first_row() { return static_cast<int>(threadIdx.x >> 6) / (W / 2) * (rows_of<W>() / 2); }
 template <int W> __device__ __forceinline__ int first_col() { return static_cast<int>(threadIdx.x >> 6) % (W / 2) * 64; }
 
-// acc[im][in] += A B^T over one stage.
+// acc[im][in] += A B^T over one stage (b_at: where B lies behind A, 0 where A is B).
 template <int P, int W, bool AROWS, bool BROWS, Kind K = kPlain>
-__device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&acc)[W / 2][2])
+__device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&acc)[W / 2][2], int b_at = operand_bytes<W>())
 {
     constexpr int MT = W / 2, KK = step_of<P>() / 16;
     const int m0 = first_row<W>(), n0 = first_col<W>();
     const unsigned char* A = stage;
-    const unsigned char* B = stage + operand_bytes<W>();
+    const unsigned char* B = stage + b_at;
     // Operands of the next 16 indices are read while these are multiplied: a read takes as long as four products.  (The compiler would
     // reuse the registers at once and wait for every read.)
     s16x8 a[2][P][MT], b[2][P][2];
