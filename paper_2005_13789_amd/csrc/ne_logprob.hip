@@ -5,17 +5,19 @@
 //     top: the k ids of largest S_iv in falling order, of equal scores the lowest id first
 //
 // Scores are never kept.  One pass over them leaves, beside the maximum and the two sums of every row's softmax, one record of 8 bytes for every
-// chunk of table rows (64 with tiles, 16 where the table streams) and row of H: the chunk's best score with its place in the low bits, and
+// chunk of table rows (64, or 16) and row of H: the chunk's best score with its place in the low bits, and
 // its second best.  A score is off by at most `off_by` from what 64 bits would give.  So, with t the k-th largest of the chunks' best, the answers are among
 // the chunks' best of at least t - 2 off_by and, where a chunk's second best reaches that, too (4 chunks in 100 rows at k = 16 of 200 003), its
-// other rows.  A workgroup for every row of H finds these in the records, takes their scores again with sums in 64 bits, and orders them: what
-// it answers does not depend on how the table was cut into tiles, and equal rows tie exactly.
+// other rows.  A wavefront or more for every row of H finds these in the records, takes their scores again with sums in 64 bits, and orders them:
+// what it answers does not depend on how the table was cut into tiles, and equal rows tie exactly.
 #include "ne_tiles.h"
 
 namespace {
 
-constexpr int kTileChunk = 6, kFewChunk = 4;           // log2 of a chunk's rows
-constexpr int kMostFound = 2048;                       // candidates that a workgroup looks at together
+// Chunks of table rows.  kWide: 64.  kNarrow: 16, what a lane has of 32 rows of a tile.  kStreamed: 16, a tile of few rows' kernel.
+enum Chunks { kNone, kWide, kNarrow, kStreamed };
+constexpr int chunk_log2(int chunks) { return chunks == kWide ? 6 : 4; }
+constexpr int64_t kTeamsOfMany = 512;                  // rows of H up to which sixteen wavefronts look for the answers of each
 constexpr float kNoScore = -1e30f;                     // below all scores: they are bounded by kMostScore
 constexpr float kMostScore = 1e29f;
 
@@ -159,9 +161,12 @@ struct TileArgs {
     Softmax* stat;                 // [n][splits]
     float2* best;                  // [n][chunks]
     int64_t chunks;
+    const uint32_t* norms;         // [norm_count]
+    uint32_t norm_count;
+    uint32_t* norm;
 };
 
-template <int P, int W, int KS, bool TOP>
+template <int P, int W, int KS, int CHUNKS>
 __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
@@ -170,6 +175,13 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
     uint32_t token_tile, split;
     pair_of(by_xcd(blockIdx.x, gridDim.x), (a.tokens + R - 1) / R, a.splits, token_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
+    if (blockIdx.x == 0) {          // the table's norm, from shares
+        uint32_t all = 0;
+        for (uint32_t i = threadIdx.x; i < a.norm_count; i += 64 * W) all = max(all, a.norms[i]);
+        all = block_max_bits(all, reinterpret_cast<uint32_t*>(lds));
+        if (threadIdx.x == 0) *a.norm = all;
+        __syncthreads();
+    }
     const float factor = score_factor<P>(a.shift), to_log2 = kLog2e * factor;
     Softmax s[2] = {{kNoScore, 0.0f, 0.0f, 0.0f}, {kNoScore, 0.0f, 0.0f, 0.0f}};
     const float low = fmaxf(-3e38f, kNoScore / factor);          // (in units of the sums; below all of them)
@@ -186,8 +198,9 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             float t = low;
-            if constexpr (TOP) {
-                const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
+            const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
+            float2* best = a.best + token * a.chunks;
+            if constexpr (CHUNKS == kWide) {
 #pragma unroll
                 for (int c = 0; c < MT / 2; ++c) {
                     Best b{low, low};
@@ -198,8 +211,18 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
                     t = fmaxf(t, b.first);
                     b.first = __uint_as_float(__float_as_uint(b.first) | lane_row());
                     b.join_lanes(32);
-                    const uint32_t chunk = (row0 >> kTileChunk) + c;
-                    if (lane < 32 && token < a.n && chunk < a.chunks) a.best[token * a.chunks + chunk] = make_float2(b.first * factor, b.second * factor);
+                    const uint32_t chunk = (row0 >> 6) + c;
+                    if (lane < 32 && token < a.n && chunk < a.chunks) best[chunk] = make_float2(b.first * factor, b.second * factor);
+                }
+            } else if constexpr (CHUNKS == kNarrow) {
+#pragma unroll
+                for (int im = 0; im < MT; ++im) {
+                    Best b{low, low};
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) b.see(acc[im][j][i], i, ~15u);
+                    t = fmaxf(t, b.first);
+                    const uint32_t chunk = 2 * ((row0 >> 5) + im) + (lane >> 5);
+                    if (token < a.n && chunk < a.chunks) best[chunk] = make_float2(b.first * factor, b.second * factor);
                 }
             } else {
 #pragma unroll
@@ -393,8 +416,9 @@ struct FinishArgs {
     const void *h, *w;
     int64_t h_stride, w_stride;
     const int32_t* ids;
+    int64_t n;
     uint32_t num_rows, splits, norm_count, k;
-    int32_t dim;
+    int32_t dim, kind;             // kind of chunks
     const Softmax* stat;           // [n][splits]
     const uint32_t* norms;
     const int32_t* shift;          // NULL, or powers of two of W and H
@@ -405,37 +429,65 @@ struct FinishArgs {
     float* top_logp;
 };
 
-// What a workgroup holds of a row: candidates and, in front of them, the best so far.
-struct Found {
-    uint32_t ids[64 + kMostFound];
-    double scores[64 + kMostFound];
-    uint32_t count;
+// A row of H is a team's: a wavefront where there are many rows (four teams a workgroup, which never wait for one another), or sixteen.
+template <int WAVES> constexpr int threads_of() { return WAVES == 1 ? kThreads : 64 * WAVES; }
+template <int WAVES> constexpr int most_found() { return WAVES == 1 ? 128 : WAVES == 4 ? 512 : 2048; }       // candidates that a team looks at together
+
+template <int WAVES>
+__device__ __forceinline__ void team_sync()
+{
+    if (WAVES == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    else __syncthreads();
+}
+
+template <int WAVES>
+struct Team {
+    uint32_t ids[64 + most_found<WAVES>() + 1];        // the best so far, candidates, the given id
+    double scores[64 + most_found<WAVES>() + 1];
+    uint32_t next_ids[64];
+    double next_scores[64];
+    Softmax stats[WAVES];
+    float norms[WAVES];
+    float maxima[WAVES == 1 ? 1 : 64 * WAVES];
+    uint32_t count, bits[WAVES];
+    float threshold;
 };
 
-// Scores of found.ids[first ..], 16 lanes each, with products and sums in 64 bits, in an order that depends on dim alone.
+// Eight elements of a row, from `at` on; of fewer than eight columns elements one by one, zeros behind them.
 template <class T>
-__device__ __forceinline__ void exact_scores(const FinishArgs& a, const float* h, const uint32_t* ids, double* scores, uint32_t first, uint32_t count)
+__device__ __forceinline__ void load_piece(const T* row, int at, int dim, T (&x)[8])
 {
-    const int lane = threadIdx.x & 15;
-    constexpr int FLIGHT = 2;
-    for (uint32_t c = first + (threadIdx.x >> 4) * FLIGHT; c < count; c += kThreads / 16 * FLIGHT) {
+    if (dim >= 8) __builtin_memcpy(x, row + at, 8 * sizeof(T));
+    else load_eight(row, 0, dim, x);
+}
+
+// Scores of table rows, 16 lanes each, with products and sums in 64 bits, in an order that depends on dim alone.  A row's last piece ends with the row:
+// what it has in common with the piece before it is multiplied with zeros.
+template <class T, int WAVES>
+__device__ __forceinline__ void exact_scores(const FinishArgs& a, const T* h, const uint32_t* ids, double* scores, uint32_t count, uint32_t thread)
+{
+    constexpr uint32_t FLIGHT = WAVES == 1 ? 4 : 2, GROUPS = WAVES * 4;
+    const int lane = thread & 15;
+    for (uint32_t c = (thread >> 4) * FLIGHT; c < count; c += GROUPS * FLIGHT) {
         double sum[FLIGHT] = {};
         const T* row[FLIGHT];
 #pragma unroll
-        for (int f = 0; f < FLIGHT; ++f) row[f] = static_cast<const T*>(a.w) + static_cast<int64_t>(ids[min(c + f, count - 1)]) * a.w_stride;
+        for (uint32_t f = 0; f < FLIGHT; ++f) row[f] = static_cast<const T*>(a.w) + static_cast<int64_t>(ids[min(c + f, count - 1)]) * a.w_stride;
         for (int e = lane * 8; e < a.dim; e += 128) {
-            T x[FLIGHT][8];
+            const int at = max(min(e, a.dim - 8), 0);
+            T x[FLIGHT][8], y[8];
+            load_piece(h, at, a.dim, y);
 #pragma unroll
-            for (int f = 0; f < FLIGHT; ++f) load_eight(row[f], e, a.dim, x[f]);
+            for (uint32_t f = 0; f < FLIGHT; ++f) load_piece(row[f], at, a.dim, x[f]);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const double y = e + q < a.dim ? static_cast<double>(h[e + q]) : 0.0;
+                const double z = at + q >= e ? static_cast<double>(static_cast<float>(y[q])) : 0.0;
 #pragma unroll
-                for (int f = 0; f < FLIGHT; ++f) sum[f] = fma(static_cast<double>(static_cast<float>(x[f][q])), y, sum[f]);
+                for (uint32_t f = 0; f < FLIGHT; ++f) sum[f] = fma(static_cast<double>(static_cast<float>(x[f][q])), z, sum[f]);
             }
         }
 #pragma unroll
-        for (int f = 0; f < FLIGHT; ++f) {
+        for (uint32_t f = 0; f < FLIGHT; ++f) {
 #pragma unroll
             for (int o = 1; o < 16; o <<= 1) sum[f] += __shfl_xor(sum[f], o, 16);
             if (lane == 0 && c + f < count) scores[c + f] = sum[f];
@@ -443,185 +495,312 @@ __device__ __forceinline__ void exact_scores(const FinishArgs& a, const float* h
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) answers_kernel(FinishArgs a, int chunk_log2)
+// Floats as numbers of the same order.
+__device__ __forceinline__ uint32_t ordered(float x)
 {
-    extern __shared__ __align__(16) float row_lds[];      // [dim]  the row of H
-    __shared__ Found found;
-    __shared__ Softmax stats[kThreads / 64];
-    __shared__ double norms[kThreads / 64];
-    __shared__ uint32_t bits[kThreads / 64];
-    __shared__ __align__(16) float maxima[kThreads];
-    __shared__ uint32_t next_ids[64], total;
-    __shared__ double next_scores[64];
-    __shared__ float threshold;
-    const int64_t i = blockIdx.x;
+    const uint32_t u = __float_as_uint(x);
+    return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+
+// A bound that k of a wavefront's values reach, within 2^-9 below the k-th largest: bit after bit, counted by ballots.
+template <int VALUES>
+__device__ __forceinline__ float reached_by(const float (&x)[VALUES], uint32_t k)
+{
+    uint32_t key[VALUES], t = 0;
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) key[v] = ordered(x[v]);
+    for (uint32_t bit = 0x80000000u; bit >= 1u << 14; bit >>= 1) {
+        uint32_t count = 0;
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) count += __popcll(__ballot(key[v] >= (t | bit)));
+        if (count >= k) t |= bit;
+    }
+    return from_ordered(t);
+}
+
+// A thread's records c0 + thread, + threads .. below c1, all loads in flight.  A team of sixteen wavefronts keeps them in registers where these are all
+// (fewer wavefronts would lose more to the registers than a second read from L2 costs).
+template <int WAVES> constexpr int at_once() { return WAVES == 16 ? 16 : 8; }
+
+template <int THREADS, int COUNT>
+__device__ __forceinline__ void load_records(const float2* best, int64_t c0, int64_t c1, uint32_t thread, float2 (&b)[COUNT])
+{
+#pragma unroll
+    for (int f = 0; f < COUNT; ++f) {
+        const int64_t c = c0 + thread + f * THREADS;
+        b[f] = make_float2(-INFINITY, -INFINITY);
+        if (c < c1) b[f] = best[c];
+    }
+}
+
+// A softmax's logarithm of its sum, in powers of two (of a mantissa, whose logarithm is below 1 and as much more exact).
+__device__ __forceinline__ double log2_of(float top, float sum)
+{
+    int e;
+    const float m = frexpf(sum, &e);
+    return static_cast<double>(top) + e + static_cast<double>(log2f(m));
+}
+
+template <class T, int WAVES>
+__global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs a)
+{
+    __shared__ Team<WAVES> teams[threads_of<WAVES>() / 64 / WAVES];
+    constexpr uint32_t MOST = most_found<WAVES>(), THREADS = 64 * WAVES;
+    const uint32_t thread = threadIdx.x % THREADS, lane = thread & 63, wave = thread >> 6;
+    Team<WAVES>& team = teams[threadIdx.x / THREADS];
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * (threads_of<WAVES>() / THREADS) + threadIdx.x / THREADS;
+    if (i >= a.n) return;
+    // (what is loaded first does not wait for the id)
+    const T* h = static_cast<const T*>(a.h) + i * a.h_stride;
     const uint32_t id = a.ids ? static_cast<uint32_t>(a.ids[i]) : 0xFFFFFFFFu, k = a.k;
+    Softmax s{kNoScore, 0.0f, 0.0f, 0.0f};
+    uint32_t largest = 0;
+    if (thread < a.splits) s = a.stat[i * a.splits + thread];
+    if (thread < a.norm_count) largest = a.norms[thread];
+    constexpr int HELD = at_once<WAVES>();
+    float2 record[HELD];
+    const float2* best = a.best + i * a.chunks;
+    const bool held = WAVES == 16 && a.chunks <= HELD * THREADS;
+    if (k && held) load_records<THREADS>(best, 0, a.chunks, thread, record);
     int32_t* top_ids = a.top_ids + i * k;
     float* top_logp = a.top_logp + i * k;
     if (a.ids && id >= a.num_rows) {
-        if (threadIdx.x == 0) {
+        if (thread == 0) {
             a.lse[i] = 0.0f;
             if (a.logp) a.logp[i] = 0.0f;
             if (a.entropy) a.entropy[i] = 0.0f;
         }
-        if (threadIdx.x < k) {
-            top_ids[threadIdx.x] = -1;
-            top_logp[threadIdx.x] = -INFINITY;
+        if (thread < k) {
+            top_ids[thread] = -1;
+            top_logp[thread] = -INFINITY;
         }
         return;
     }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // the row, its softmax and norm, and the table's largest norm
-    double norm = 0.0;
-    const T* h = static_cast<const T*>(a.h) + i * a.h_stride;
-    for (int e = threadIdx.x; e < a.dim; e += kThreads) {
-        const float x = static_cast<float>(h[e]);
-        row_lds[e] = x;
-        norm = fma(static_cast<double>(x), static_cast<double>(x), norm);
+    // the row's norm and softmax, and the table's largest norm
+    float squares = 0.0f;
+    for (int e = thread * 8; e < a.dim; e += 8 * THREADS) {
+        const int at = max(min(e, a.dim - 8), 0);
+        T x[8];
+        load_piece(h, at, a.dim, x);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float y = at + q >= e ? static_cast<float>(x[q]) : 0.0f;
+            squares = fmaf(y, y, squares);
+        }
+        if (magnitude_bits(x) && squares < 0x1p-126f) squares = 0x1p-126f;      // (squares of small values may be 0)
     }
-    Softmax s{kNoScore, 0.0f, 0.0f, 0.0f};
-    for (uint32_t p = threadIdx.x; p < a.splits; p += kThreads) {
+    for (uint32_t p = thread + THREADS; p < a.splits; p += THREADS) {
         const Softmax q = a.stat[i * a.splits + p];
         join(s, q.top, q.sum, q.moment);
     }
-    uint32_t largest = 0;
-    for (uint32_t p = threadIdx.x; p < a.norm_count; p += kThreads) largest = max(largest, a.norms[p]);
+    for (uint32_t p = thread + THREADS; p < a.norm_count; p += THREADS) largest = max(largest, a.norms[p]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         join_lanes(s, o);
-        norm += __shfl_xor(norm, o, 64);
+        squares += __shfl_xor(squares, o, 64);
+        largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), o, 64)));
     }
-    if (lane == 0) {
-        stats[wave] = s;
-        norms[wave] = norm;
-    }
-    double w_norm = sqrt(static_cast<double>(__uint_as_float(block_max_bits(largest, bits))));
-    if (w_norm > 0.0) w_norm += 0x1p-62 * sqrt(static_cast<double>(a.dim));        // (what squares of small values left out)
-    s = stats[0];
-    norm = norms[0];
+    if constexpr (WAVES > 1) {
+        if (lane == 0) {
+            team.stats[wave] = s;
+            team.norms[wave] = squares;
+            team.bits[wave] = largest;
+        }
+        __syncthreads();
+        s = team.stats[lane % WAVES];
+        squares = team.norms[lane % WAVES];
+        largest = team.bits[lane % WAVES];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) {
-        join(s, stats[w].top, stats[w].sum, stats[w].moment);
-        norm += norms[w];
+        for (int o = 1; o < WAVES; o <<= 1) {
+            join_lanes(s, o);
+            squares += __shfl_xor(squares, o, 64);
+            largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), o, 64)));
+        }
     }
-    const double product = sqrt(norm) * w_norm, lse = (static_cast<double>(s.top) + log2(static_cast<double>(s.sum))) * 0.693147180559945309;
-    const bool bad = !(product < kMostScore);       // a value that is not finite, or scores that fp32 may not hold
-    if (threadIdx.x == 0) {
+    // Bounds of both norms: squares and roots are rounded, and those of small values left something out.
+    const float left_out = 0x1p-62f * sqrtf(static_cast<float>(a.dim));
+    const float h_norm = squares == 0.0f ? 0.0f : 1.001f * sqrtf(squares) + left_out;
+    const float w_norm = largest == 0 ? 0.0f : 1.001f * sqrtf(__uint_as_float(largest)) + left_out;
+    const float product = h_norm * w_norm;
+    const double lse = log2_of(s.top, s.sum) * 0.693147180559945309;
+    const bool bad = !(product < kMostScore), zero = h_norm == 0.0f || w_norm == 0.0f;       // bad: a value that is not finite, or scores that fp32 may not hold
+    if (thread == 0) {
         a.lse[i] = bad ? NAN : static_cast<float>(lse);
         if (a.entropy) a.entropy[i] = bad ? NAN : (log2f(s.sum) - s.moment / s.sum) * kLn2;
         if (bad && a.logp) a.logp[i] = NAN;
     }
-    if (bad) {
-        if (threadIdx.x < k) {
-            top_ids[threadIdx.x] = -1;
-            top_logp[threadIdx.x] = NAN;
+    if (bad || k == 0 || zero) {
+        // (all scores are 0 where a norm is: the lowest ids)
+        if (thread < k) {
+            const bool is = !bad && thread < a.num_rows;
+            top_ids[thread] = is ? static_cast<int32_t>(thread) : -1;
+            top_logp[thread] = bad ? NAN : is ? static_cast<float>(-lse) : -INFINITY;
         }
-        return;
-    }
-    if (a.logp) {
-        if (threadIdx.x == 0) next_ids[0] = id;
-        __syncthreads();
-        exact_scores<T>(a, row_lds, next_ids, next_scores, 0, 1);
-        if (threadIdx.x == 0) a.logp[i] = static_cast<float>(next_scores[0] - lse);
-    }
-    if (k == 0) return;
-    if (product == 0.0) {           // all scores are 0: the lowest ids
-        if (threadIdx.x < k) {
-            const bool is = threadIdx.x < a.num_rows;
-            top_ids[threadIdx.x] = is ? static_cast<int32_t>(threadIdx.x) : -1;
-            top_logp[threadIdx.x] = is ? static_cast<float>(-lse) : -INFINITY;
-        }
+        if (bad || !a.logp) return;
+        if (thread == 0) team.ids[0] = id;
+        team_sync<WAVES>();
+        exact_scores<T, WAVES>(a, h, team.ids, team.scores, 1, thread);
+        if (thread == 0) a.logp[i] = static_cast<float>(team.scores[0] - lse);
         return;
     }
     // How far a score of the pass may be off: rounded products and sums (a chain of dim / 16 of them), and what halves of the rows leave out.
-    float off_by = static_cast<float>((a.dim / 16 + 8) * 0x1p-23 * product);
-    if (sizeof(T) == 4) off_by += static_cast<float>(0x1p-20 * product);
-    if (a.shift) off_by += static_cast<float>(0x1p-36 * sqrt(static_cast<double>(a.dim)) * w_norm * (sqrt(norm) + ldexp(1.0, 14 - a.shift[1])));
+    float off_by = static_cast<float>(a.dim / 16 + 8) * 0x1p-23f * product;
+    if (sizeof(T) == 4) off_by += 0x1p-20f * product;
+    if (a.shift) off_by += 0x1p-36f * sqrtf(static_cast<float>(a.dim)) * w_norm * (h_norm + ldexpf(1.0f, 14 - a.shift[1]));
     off_by = 2.0f * off_by + 1e-36f * a.dim;
-    // t: the k-th largest of the threads' best, below the k-th largest of all
-    const float2* best = a.best + i * a.chunks;
-    float mine = kNoScore;
-    for (int64_t c = threadIdx.x; c < a.chunks; c += kThreads) mine = fmaxf(mine, best[c].x);
-    maxima[threadIdx.x] = mine;
-    if (threadIdx.x == 0) {
-        threshold = kNoScore;
-        total = 0;
-        found.count = 64;
+    // t: what k of the chunks' best reach: of each lane's best two, or of each thread's best
+    float mine[2] = {-INFINITY, -INFINITY};
+    auto see = [&](const float2 (&b)[HELD]) {
+#pragma unroll
+        for (int f = 0; f < HELD; ++f) {
+            if (WAVES == 1) mine[1] = __builtin_amdgcn_fmed3f(mine[0], mine[1], b[f].x);
+            mine[0] = fmaxf(mine[0], b[f].x);
+        }
+    };
+    if (held) {
+        see(record);
+    } else {
+        for (int64_t c = 0; c < a.chunks; c += HELD * THREADS) {
+            load_records<THREADS>(best, c, a.chunks, thread, record);
+            see(record);
+        }
     }
-    __syncthreads();
+    float t = -INFINITY;
     if (a.chunks >= k) {
-        uint32_t rank = 0;
-#pragma unroll 8
-        for (uint32_t o = 0; o < kThreads; o += 4) {
-            const float4 m = *reinterpret_cast<const float4*>(maxima + o);
-            rank += (m.x > mine || (m.x == mine && o < threadIdx.x)) + (m.y > mine || (m.y == mine && o + 1 < threadIdx.x)) +
-                    (m.z > mine || (m.z == mine && o + 2 < threadIdx.x)) + (m.w > mine || (m.w == mine && o + 3 < threadIdx.x));
+        if constexpr (WAVES == 1) {
+            t = reached_by(mine, k);
+        } else {
+            team.maxima[thread] = mine[0];
+            __syncthreads();
+            if (wave == 0) {
+                float all[WAVES];
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) all[w] = team.maxima[w * 64 + lane];
+                t = reached_by(all, k);
+                if (lane == 0) team.threshold = t;
+            }
+            __syncthreads();
+            t = team.threshold;
         }
-        if (rank == k - 1) threshold = mine;
+        t -= 2.0f * off_by + fabsf(t) * 0x1p-15f;
     }
-    __syncthreads();
-    float t = threshold;
-    if (t > kNoScore) t -= 2.0f * off_by + fabsf(t) * 0x1p-15f;
-    // how many rows reach it
-    uint32_t rows = 0;
-    for (int64_t c = threadIdx.x; c < a.chunks; c += kThreads) {
-        const float2 b = best[c];
-        if (b.x >= t) rows += b.y >= t ? 1u << chunk_log2 : 1u;
-    }
-    atomicAdd(&total, rows);
-    __syncthreads();
-    // All of them together where there is room, otherwise so many chunks at a time that there is.
-    const int64_t at_a_time = total <= kMostFound ? a.chunks : kMostFound >> chunk_log2;
-    uint32_t have = 0;              // the best so far lie in front of the candidates: found.ids[64 - have ..]
-    for (int64_t c0 = 0; c0 < a.chunks; c0 += at_a_time) {
-        const int64_t c1 = min(c0 + at_a_time, a.chunks);
-        for (int64_t c = c0 + threadIdx.x; c < c1; c += kThreads) {
-            const float2 b = best[c];
-            if (!(b.x >= t)) continue;
-            const uint32_t row = static_cast<uint32_t>(c) << chunk_log2;
-            if (b.y >= t) {
-                const uint32_t some = min(1u << chunk_log2, a.num_rows - row), to = atomicAdd(&found.count, some);
-                for (uint32_t r = 0; r < some; ++r) found.ids[to + r] = row + r;
+    // Candidates of chunks c0 .. c1 - 1 go to team.ids[64 ..]: a chunk's best, or all of its rows.  Returns their number, of which those beyond MOST
+    // are not written.
+    const int log2_rows = chunk_log2(a.kind);
+    auto collect = [&](int64_t c0, int64_t c1) {
+        uint32_t count = 0;
+        if (WAVES > 1) {
+            if (thread == 0) team.count = 0;
+            __syncthreads();
+        }
+        auto place_for = [&](uint32_t some) {
+            uint32_t to = count;
+            if constexpr (WAVES == 1) {
+                count += some;
             } else {
-                found.ids[atomicAdd(&found.count, 1u)] = row + (__float_as_uint(b.x) & ((1u << chunk_log2) - 1));
+                if (lane == 0) to = atomicAdd(&team.count, some);
+                to = __builtin_amdgcn_readfirstlane(to);
+            }
+            return to;
+        };
+        auto write = [&](bool is, uint32_t row) {
+            const uint64_t mask = __ballot(is);
+            if (!mask) return;
+            const uint32_t to = place_for(__popcll(mask)) + __popcll(mask & ((1ull << lane) - 1));
+            if (is && to < MOST) team.ids[64 + to] = row;
+        };
+        auto row_of = [&](uint32_t chunk, uint32_t place) {
+            return a.kind == kNarrow ? (chunk >> 1) * 32 + 8 * (place >> 2) + 4 * (chunk & 1) + (place & 3) : (chunk << log2_rows) + place;
+        };
+        for (int64_t c = held ? 0 : c0; c < c1; c += HELD * THREADS) {
+            if (!held) load_records<THREADS>(best, c, c1, thread, record);
+#pragma unroll
+            for (int f = 0; f < HELD; ++f) {
+                const int64_t mine = c + thread + f * THREADS;
+                const bool reaches = record[f].x >= t && mine >= c0 && mine < c1;
+                if (!__any(reaches)) continue;
+                const bool whole = reaches && record[f].y >= t;
+                const uint32_t one = row_of(static_cast<uint32_t>(mine), __float_as_uint(record[f].x) & ((1u << log2_rows) - 1));
+                write(reaches && !whole && one < a.num_rows, one);       // (narrow chunks behind the last row hold nothing)
+                for (uint64_t wholes = __ballot(whole); wholes; wholes &= wholes - 1) {
+                    const uint32_t chunk = __builtin_amdgcn_readlane(static_cast<uint32_t>(mine), __builtin_ctzll(wholes)), row = row_of(chunk, lane);
+                    write(lane < 1u << log2_rows && row < a.num_rows, row);
+                }
             }
         }
-        __syncthreads();
-        const uint32_t count = found.count;
-        exact_scores<T>(a, row_lds, found.ids, found.scores, 64, count);
-        __syncthreads();
-        const uint32_t all = have + count - 64, base = 64 - have;
-        for (uint32_t c = threadIdx.x; c < all; c += kThreads) {
-            const uint32_t my_id = found.ids[base + c];
-            const double my_score = found.scores[base + c];
-            uint32_t rank = 0;
-            for (uint32_t o = 0; o < all; ++o) {
-                const double other = found.scores[base + o];
-                rank += other > my_score || (other == my_score && found.ids[base + o] < my_id);
+        if (WAVES > 1) {
+            __syncthreads();
+            count = team.count;
+        }
+        return count;
+    };
+    const int64_t part = MOST >> log2_rows;         // chunks whose rows all fit
+    int64_t at = 0, to = 0, span = a.chunks;        // so many chunks at a time that there is room for their candidates
+    auto next_candidates = [&]() {
+        at = to;
+        while (true) {
+            to = min(at + span, a.chunks);
+            const uint32_t count = collect(at, to);
+            if (count <= MOST) return count;
+            span = max(span / 2, part);
+        }
+    };
+    uint32_t count = next_candidates(), have = 0;
+    bool given = a.logp != nullptr;
+    while (true) {
+        if (given && thread == 0) team.ids[64 + count] = id;
+        team_sync<WAVES>();
+        exact_scores<T, WAVES>(a, h, team.ids + 64, team.scores + 64, count + given, thread);
+        team_sync<WAVES>();
+        if (given && thread == 0) a.logp[i] = static_cast<float>(team.scores[64 + count] - lse);
+        given = false;
+        // the best so far lie in front of the candidates
+        const uint32_t all = have + count, base = 64 - have;
+        const bool last = to >= a.chunks;
+        for (uint32_t c = thread; c < all; c += THREADS) {
+            const uint32_t my_id = team.ids[base + c];
+            const double my_score = team.scores[base + c];
+            uint32_t rank = 0, o = 0;
+            auto beats = [&](double other, uint32_t other_id) { return other > my_score || (other == my_score && other_id < my_id); };
+            for (; o + 8 <= all; o += 8) {
+                double other[8];
+                uint32_t other_id[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    other[q] = team.scores[base + o + q];
+                    other_id[q] = team.ids[base + o + q];
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) rank += beats(other[q], other_id[q]);
             }
-            if (rank < k) {
-                next_ids[rank] = my_id;
-                next_scores[rank] = my_score;
+            for (; o < all; ++o) rank += beats(team.scores[base + o], team.ids[base + o]);
+            if (rank >= k) continue;
+            if (last) {
+                top_ids[rank] = static_cast<int32_t>(my_id);
+                top_logp[rank] = static_cast<float>(my_score - lse);
+            } else {
+                team.next_ids[rank] = my_id;
+                team.next_scores[rank] = my_score;
             }
         }
-        __syncthreads();
         have = min(all, k);
-        if (threadIdx.x < have) {
-            found.ids[64 - have + threadIdx.x] = next_ids[threadIdx.x];
-            found.scores[64 - have + threadIdx.x] = next_scores[threadIdx.x];
+        if (last) break;
+        team_sync<WAVES>();
+        if (thread < have) {
+            team.ids[64 - have + thread] = team.next_ids[thread];
+            team.scores[64 - have + thread] = team.next_scores[thread];
         }
-        if (threadIdx.x == 0) found.count = 64;
-        __syncthreads();
+        team_sync<WAVES>();
         if (have == k) {
-            const float last = static_cast<float>(found.scores[63]);
-            t = fmaxf(t, last - off_by - fabsf(last) * 0x1p-15f);
+            const float least = static_cast<float>(team.scores[63]);
+            t = fmaxf(t, least - off_by - fabsf(least) * 0x1p-15f);
         }
+        count = next_candidates();
     }
-    if (threadIdx.x < k) {
-        const bool is = threadIdx.x < have;
-        top_ids[threadIdx.x] = is ? static_cast<int32_t>(found.ids[64 - have + threadIdx.x]) : -1;
-        top_logp[threadIdx.x] = is ? static_cast<float>(found.scores[64 - have + threadIdx.x] - lse) : -INFINITY;
+    if (thread >= have && thread < k) {
+        top_ids[thread] = -1;
+        top_logp[thread] = -INFINITY;
     }
 }
 
@@ -630,13 +809,18 @@ __global__ void __launch_bounds__(kThreads) answers_kernel(FinishArgs a, int chu
 // ---------------------------------------------------------------------------------------------
 struct AnswerWs : Packs {
     uint32_t row_tiles, splits;
-    int32_t few_blocks;
+    int32_t few_blocks, kind;
     int64_t chunks;
-    uint32_t* norms;
+    uint32_t *norms, *norm;
     Softmax* stat;
     float2* best;
     size_t total;
 };
+
+// Wide chunks where hardly any has two of the best k: the rows of those that have are looked at again, k^2 64^2 / (2 num_rows) of them about.
+int chunks_of(int64_t num_rows, int32_t k) { return k == 0 ? kNone : static_cast<int64_t>(k) * k * 320 > num_rows ? kNarrow : kWide; }
+
+int64_t chunk_count(int64_t num_rows, int kind) { return kind == kNone ? 0 : kind == kNarrow ? 2 * ceil_div(num_rows, 32) : ceil_div(num_rows, int64_t{1} << chunk_log2(kind)); }
 
 AnswerWs answer_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int32_t k, char* base)
 {
@@ -649,9 +833,11 @@ AnswerWs answer_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, i
     const int64_t side = w.large_scores ? 256 : 128, token_tiles = ceil_div(w.tokens, side);
     w.row_tiles = static_cast<uint32_t>(ceil_div(num_rows, side));
     w.few_blocks = few_blocks_of(n, num_rows, dim, w.parts);
-    w.chunks = ceil_div(num_rows, 1 << (w.few_blocks ? kFewChunk : kTileChunk));
+    w.kind = w.few_blocks && k ? kStreamed : chunks_of(num_rows, k);
+    w.chunks = chunk_count(num_rows, w.kind);
     Carver take{base};
     w.norms = take.get<uint32_t>(kMostPack);
+    w.norm = take.get<uint32_t>(1);
     if (w.few_blocks) {
         const bool alone = few_bytes_of(w.few_blocks, dim, w.parts) > kFewBytes;
         w.splits = static_cast<uint32_t>(std::min<int64_t>(ceil_div(num_rows, alone ? 128 : 64), alone ? 256 : kFewGroups));
@@ -678,7 +864,7 @@ size_t answer_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int3
     int64_t bytes = 32 << 10;
     // shares of few rows; of tiles: as many workgroups as run in four rounds, or one for every tile
     bytes += (std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups) * few + tokens + std::min<int64_t>(ceil_div(num_rows, 128) * tokens, 4 * 512 * 128)) * 16;
-    if (k) bytes += std::max(ceil_div(num_rows, 1 << kFewChunk) * few, ceil_div(num_rows, 1 << kTileChunk) * n) * 8;
+    bytes += std::max(chunk_count(num_rows, k ? kStreamed : kNone) * few, chunk_count(num_rows, chunks_of(num_rows, k)) * n) * 8;
     if (!few_blocks_of(n, num_rows, dim, parts)) bytes += parts * 2 * padded * (tokens + num_rows);
     return static_cast<size_t>(bytes);
 }
@@ -716,8 +902,8 @@ hipError_t few_answers(const SoftmaxCall& x, const AnswerWs& w, hipStream_t st)
     return hipSuccess;
 }
 
-template <int P, bool TOP>
-hipError_t tile_answers(const SoftmaxCall& x, const AnswerWs& w, uint32_t* norm_count, hipStream_t st)
+template <int P, int CHUNKS>
+hipError_t tile_answers(const SoftmaxCall& x, const AnswerWs& w, hipStream_t st)
 {
     PackJobs jobs{};
     const bool direct = P == 1 && usable_as_it_lies(x);
@@ -732,13 +918,11 @@ hipError_t tile_answers(const SoftmaxCall& x, const AnswerWs& w, uint32_t* norm_
     const NormArgs norms{x.w, x.h, x.w_stride, x.h_stride, x.n, x.num_rows, x.targets, x.dim, w.norms, P == 2 ? w.amax : nullptr};
     const uint32_t blocks = pack_blocks(w, std::max(w.tokens, x.num_rows), kThreads, kMostPack);
     if (P == 2) {
-        *norm_count = kAmaxBlocks;
         hipLaunchKernelGGL(norms_kernel, dim3(kAmaxBlocks), dim3(kThreads), 0, st, norms);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(pack_kernel<2>, dim3(blocks, 2), dim3(kThreads), 0, st, jobs);
     } else {
-        *norm_count = blocks;
         hipLaunchKernelGGL(prepare_kernel, dim3(blocks, direct ? 2 : 3), dim3(kThreads), 0, st, jobs, norms);
     }
     hipError_t e = hipGetLastError();
@@ -749,12 +933,13 @@ hipError_t tile_answers(const SoftmaxCall& x, const AnswerWs& w, uint32_t* norm_
     a.h = packed_operand(w.h, w.tokens, w.padded);
     a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles; a.splits = w.splits;
     a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.best = w.best; a.chunks = w.chunks;
+    a.norms = w.norms; a.norm_count = P == 2 ? kAmaxBlocks : blocks; a.norm = w.norm;
     const dim3 grid(static_cast<unsigned>(ceil_div(w.tokens, w.large_scores ? 256 : 128) * w.splits));
     const int held = held_stages(w, w.row_tiles, w.splits, a.steps);
-    if (P == 1 && w.large_scores) hipLaunchKernelGGL((answer_tiles_kernel<1, 8, 0, TOP>), grid, dim3(512), 0, st, a);
-    else if (held == 0) hipLaunchKernelGGL((answer_tiles_kernel<P, 4, 0, TOP>), grid, dim3(256), 0, st, a);
-    else if (held == 2) hipLaunchKernelGGL((answer_tiles_kernel<P, 4, 2, TOP>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((answer_tiles_kernel<P, 4, 4, TOP>), grid, dim3(256), 0, st, a);
+    if (P == 1 && w.large_scores) hipLaunchKernelGGL((answer_tiles_kernel<1, 8, 0, CHUNKS>), grid, dim3(512), 0, st, a);
+    else if (held == 0) hipLaunchKernelGGL((answer_tiles_kernel<P, 4, 0, CHUNKS>), grid, dim3(256), 0, st, a);
+    else if (held == 2) hipLaunchKernelGGL((answer_tiles_kernel<P, 4, 2, CHUNKS>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((answer_tiles_kernel<P, 4, 4, CHUNKS>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
@@ -793,19 +978,20 @@ ne_status ne_logprob(const void* h_dev, int64_t h_stride, const void* w_dev, int
     const AnswerWs w = answer_layout(n, num_rows, dim, type, k, static_cast<char*>(workspace_dev));
     const SoftmaxCall x{h_dev, w_dev, h_stride, w_stride, n, num_rows, dim, type, ids_dev, nullptr};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    uint32_t norm_count = w.splits;
+    const bool f32 = type == NE_F32;
     hipError_t e;
-    if (w.few_blocks) e = type == NE_F32 ? few_answers<float>(x, w, st) : few_answers<bf16_t>(x, w, st);
-    else if (k) e = type == NE_F32 ? tile_answers<2, true>(x, w, &norm_count, st) : tile_answers<1, true>(x, w, &norm_count, st);
-    else e = type == NE_F32 ? tile_answers<2, false>(x, w, &norm_count, st) : tile_answers<1, false>(x, w, &norm_count, st);
+    if (w.few_blocks) e = f32 ? few_answers<float>(x, w, st) : few_answers<bf16_t>(x, w, st);
+    else if (w.kind == kWide) e = f32 ? tile_answers<2, kWide>(x, w, st) : tile_answers<1, kWide>(x, w, st);
+    else if (w.kind == kNarrow) e = f32 ? tile_answers<2, kNarrow>(x, w, st) : tile_answers<1, kNarrow>(x, w, st);
+    else e = f32 ? tile_answers<2, kNone>(x, w, st) : tile_answers<1, kNone>(x, w, st);
     if (e == hipSuccess) {
-        const FinishArgs f{h_dev, w_dev, h_stride, w_stride, ids_dev, static_cast<uint32_t>(num_rows), w.splits, norm_count, static_cast<uint32_t>(k), dim,
-                           w.stat, w.norms, type == NE_F32 && !w.few_blocks ? w.shift : nullptr, w.best, w.chunks, logp_dev, lse_dev, entropy_dev,
-                           top_ids_dev, top_logp_dev};
-        const size_t lds = static_cast<size_t>(dim) * 4;
-        const int chunk_log2 = w.few_blocks ? kFewChunk : kTileChunk;
-        if (type == NE_F32) hipLaunchKernelGGL(answers_kernel<float>, dim3(static_cast<unsigned>(n)), dim3(kThreads), lds, st, f, chunk_log2);
-        else hipLaunchKernelGGL(answers_kernel<bf16_t>, dim3(static_cast<unsigned>(n)), dim3(kThreads), lds, st, f, chunk_log2);
+        const FinishArgs f{h_dev, w_dev, h_stride, w_stride, ids_dev, n, static_cast<uint32_t>(num_rows), w.splits, w.few_blocks ? w.splits : 1,
+                           static_cast<uint32_t>(k), dim, w.kind, w.stat, w.few_blocks ? w.norms : w.norm, f32 && !w.few_blocks ? w.shift : nullptr, w.best,
+                           w.chunks, logp_dev, lse_dev, entropy_dev, top_ids_dev, top_logp_dev};
+        auto launch = [&](auto kernel, int64_t groups, int threads) { hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(threads), 0, st, f); };
+        if (n <= kTeamsOfMany) f32 ? launch(answers_kernel<float, 16>, n, 1024) : launch(answers_kernel<bf16_t, 16>, n, 1024);
+        else if (w.chunks > 1024) f32 ? launch(answers_kernel<float, 4>, n, kThreads) : launch(answers_kernel<bf16_t, 4>, n, kThreads);
+        else f32 ? launch(answers_kernel<float, 1>, ceil_div(n, 4), kThreads) : launch(answers_kernel<bf16_t, 1>, ceil_div(n, 4), kThreads);
         e = hipGetLastError();
     }
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("log probability launch: ") + hipGetErrorString(e));

@@ -8,16 +8,17 @@
 // s is s^2 in G, beside errors of 2^-24 of the largest, so weak directions are lost first.  A step brings them up by 3.4445; three steps, then a new G
 // and two more leave an error like that of the products taken one after the other in fp32 (all five at once: up to a hundred times that).
 //
-// All products are of fp16 halves at a power of two (x 2^k = hi + lo, 22 bits), three matrix instructions each, with fp32 sums: about the error
-// of an fp32 product.  X's power follows from its largest magnitude, those of the others from what they are: singular values of G's successors
-// and of X stay below 1.3, of Q below 3.45, of P of three steps below 41.  G is the sum of a long contraction: sums of 256 rows
-// are added to a second set of registers, and the workgroups' shares in 64 bits.
+// Products with X are of fp16 halves at a power of two (x 2^k = hi + lo, 22 bits), three matrix instructions each, with fp32 sums: about the error
+// of an fp32 product.  The first X's power follows from its largest magnitude, those of later ones and of P from what they are: singular values of X stay
+// below 1.3, of P of three steps below 41.  G is the sum of a long contraction: sums of 256 rows are added to a second set of registers, and the
+// workgroups' shares in 64 bits.  Matrices of the small side are fp32, each taken apart into three bf16 parts (24 bits) for its products, of
+// which the six largest are taken.
 #include "ne_tiles.h"
 
 namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr int kSmallShift = 13, kPShift = 10;          // powers of two of G, Q and later X; of products of Qs
+constexpr int kHalfShift = 13, kPShift = 10;           // powers of two of later Xs, of P
 constexpr int kStatBlocks = 1024;
 constexpr int kMostSplits = 512;
 constexpr int kFlush = 8;                              // stages whose sums are added up apart
@@ -286,8 +287,8 @@ struct GramJoinArgs {
     const float* part;
     uint32_t tiles, splits;
     int32_t padded_small;
-    const Scalars* scalars; // NULL: X's halves are of X 2^kSmallShift
-    Halves g;
+    const Scalars* scalars; // NULL: X's halves are of X 2^kHalfShift
+    float* g;               // [padded_small][padded_small]
 };
 
 __device__ __forceinline__ void put(const Halves& to, int64_t row, int64_t col, float x, int shift)
@@ -316,9 +317,8 @@ __global__ void __launch_bounds__(kThreads) gram_join_kernel(GramJoinArgs a)
     if (threadIdx.x >= 64 || col >= a.padded_small || row > col) return;
     sum = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
     if (a.scalars) sum = ldexp(sum * a.scalars->inverse * a.scalars->inverse, -2 * a.scalars->shift);
-    else sum = ldexp(sum, -2 * kSmallShift);
-    put(a.g, row, col, static_cast<float>(sum), kSmallShift);
-    if (row != col) put(a.g, col, row, static_cast<float>(sum), kSmallShift);
+    else sum = ldexp(sum, -2 * kHalfShift);
+    a.g[row * a.padded_small + col] = a.g[col * a.padded_small + row] = static_cast<float>(sum);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -327,18 +327,16 @@ __global__ void __launch_bounds__(kThreads) gram_join_kernel(GramJoinArgs a)
 // All of them are polynomials of one symmetric matrix, so they are symmetric, commute, and rows serve as columns.  A workgroup has a tile of
 // 32 x 32 on or above the diagonal, its four wavefronts a quarter of the contraction each, straight from L2 into the matrix cores' operands.
 struct SmallJob {
-    Halves a, b, out;
-    float factor;           // 2 to the minus sum of both powers
-    int32_t shift;          // power of two of what is written
+    const float *a, *b;
+    float* out;             // NULL: the halves of P, for the product with X
     int32_t polynomial;     // out = kA + kB a + kC (a b), for a = b = G
 };
 
 struct SmallArgs {
     SmallJob job[2];
+    Halves p;
     int32_t side;           // multiple of 32
 };
-
-__device__ __forceinline__ s16x8 row_piece(const uint16_t* p) { return *reinterpret_cast<const s16x8*>(p); }
 
 __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
 {
@@ -348,48 +346,48 @@ __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
     uint32_t ti, tj;
     pair_at(blockIdx.x, tiles, ti, tj);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, steps = args.side / 16;
-    const int64_t a_at = static_cast<int64_t>(ti * 32 + (lane & 31)) * job.a.stride + (lane >> 5) * 8;
-    const int64_t b_at = static_cast<int64_t>(tj * 32 + (lane & 31)) * job.b.stride + (lane >> 5) * 8;
-    const uint16_t *ah = job.a.part[0] + a_at, *al = job.a.part[1] + a_at, *bh = job.b.part[0] + b_at, *bl = job.b.part[1] + b_at;
+    const float* a = job.a + static_cast<int64_t>(ti * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
+    const float* b = job.b + static_cast<int64_t>(tj * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
     f32x16 sum, small;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i] = small[i] = 0.0f;
     constexpr int FLIGHT = 4;
     for (int s0 = wave; s0 < steps; s0 += 4 * FLIGHT) {
-        s16x8 a0[FLIGHT] = {}, a1[FLIGHT] = {}, b0[FLIGHT] = {}, b1[FLIGHT] = {};
+        float x[FLIGHT][8] = {}, y[FLIGHT][8] = {};
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
-            const int at = (s0 + 4 * f) * 16;
             if (s0 + 4 * f >= steps) break;
-            a0[f] = row_piece(ah + at);
-            a1[f] = row_piece(al + at);
-            b0[f] = row_piece(bh + at);
-            b1[f] = row_piece(bl + at);
+            __builtin_memcpy(x[f], a + (s0 + 4 * f) * 16, 32);
+            __builtin_memcpy(y[f], b + (s0 + 4 * f) * 16, 32);
         }
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
-            small = mfma<2>(a0[f], b1[f], small);
-            small = mfma<2>(a1[f], b0[f], small);
-            sum = mfma<2>(a0[f], b0[f], sum);
+            bf16x8 u[3], v[3];
+            split_bf16<3>(x[f], u);
+            split_bf16<3>(y[f], v);
+#pragma unroll
+            for (int of_parts = 2; of_parts >= 0; --of_parts) {
+                f32x16& to = of_parts > 0 ? small : sum;
+#pragma unroll
+                for (int q = 0; q <= of_parts; ++q) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[q], v[of_parts - q], to, 0, 0, 0);
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) lds[wave][(sum_row(i) + lane_row()) * 33 + (lane & 31)] = sum[i] + small[i];
     __syncthreads();
     for (int i = threadIdx.x; i < 32 * 32; i += 256) {
-        const int r = i >> 5, c = i & 31;
+        const int r = i >> 5, c = i & 31, at = r * 33 + c;
         const int64_t row = ti * 32 + r, col = tj * 32 + c;
         if (row > col) continue;
-        const int at = r * 33 + c;
-        float x = ((lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at])) * job.factor;
-        if (job.polynomial) {
-            const int64_t g_at = row * job.a.stride + col;
-            const float g = (static_cast<float>(__builtin_bit_cast(f16_t, job.a.part[0][g_at])) + static_cast<float>(__builtin_bit_cast(f16_t, job.a.part[1][g_at]))) *
-                            (1.0f / (1 << kSmallShift));
-            x = fmaf(kC, x, kB * g) + (row == col ? kA : 0.0f);
+        float x = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
+        if (job.polynomial) x = fmaf(kC, x, kB * job.a[row * args.side + col]) + (row == col ? kA : 0.0f);
+        if (job.out) {
+            job.out[row * args.side + col] = job.out[col * args.side + row] = x;
+        } else {
+            put(args.p, row, col, x, kPShift);
+            if (row != col) put(args.p, col, row, x, kPShift);
         }
-        put(job.out, row, col, x, job.shift);
-        if (row != col) put(job.out, col, row, x, job.shift);
     }
 }
 
@@ -402,7 +400,7 @@ struct ApplyArgs {
     int32_t steps;
     int64_t tall, padded_tall;
     int32_t small, padded_small;
-    const Scalars* scalars; // NULL: X's halves are of X 2^kSmallShift
+    const Scalars* scalars; // NULL: X's halves are of X 2^kHalfShift
     // one of: the next X's halves; a matrix out; parameters
     Halves next;
     void* out;
@@ -439,7 +437,7 @@ __global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
     uint32_t col_tile, split;
     pair_of(by_xcd(blockIdx.x, gridDim.x), a.col_tiles, a.splits, col_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
-    const float factor = a.scalars ? static_cast<float>(ldexp(a.scalars->inverse, -(a.scalars->shift + kPShift))) : ldexpf(1.0f, -(kSmallShift + kPShift));
+    const float factor = a.scalars ? static_cast<float>(ldexp(a.scalars->inverse, -(a.scalars->shift + kPShift))) : ldexpf(1.0f, -(kHalfShift + kPShift));
     all_scores<2, 4, KS>(a.x, a.p, col_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
 #pragma unroll
         for (int im = 0; im < 2; ++im)
@@ -451,7 +449,7 @@ __global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
                     const int col = col_tile * kSide + n0 + 32 * j + (lane & 31);
                     const float x = acc[im][j][i] * factor;
                     if (L == kNext) {
-                        if (row < a.padded_tall && col < a.padded_small) put(a.next, row, col, x, kSmallShift);
+                        if (row < a.padded_tall && col < a.padded_small) put(a.next, row, col, x, kHalfShift);
                     } else {
                         finish<L, WIDE>(a, row, col, x);
                     }
@@ -464,7 +462,7 @@ __global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
 // ---------------------------------------------------------------------------------------------
 struct MuonWs {
     int64_t tall, padded_tall;
-    int32_t small, padded_small;
+    int32_t side, padded_side;      // the smaller one
     bool wide;
     uint32_t tiles, pairs, splits, share, stages;
     double* squares;
@@ -472,7 +470,8 @@ struct MuonWs {
     Scalars* scalars;
     Halves x[2];
     float* part;
-    Halves g[7];
+    float* small[6];                // matrices of the small side
+    Halves p;
     size_t total;
 };
 
@@ -481,10 +480,10 @@ MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
     MuonWs w{};
     w.wide = cols > rows;
     w.tall = w.wide ? cols : rows;
-    w.small = static_cast<int32_t>(w.wide ? rows : cols);
+    w.side = static_cast<int32_t>(w.wide ? rows : cols);
     w.padded_tall = round_up(w.tall, 32);
-    w.padded_small = static_cast<int32_t>(round_up(w.small, 32));
-    w.tiles = static_cast<uint32_t>(ceil_div(w.padded_small, kSide));
+    w.padded_side = static_cast<int32_t>(round_up(w.side, 32));
+    w.tiles = static_cast<uint32_t>(ceil_div(w.padded_side, kSide));
     w.pairs = w.tiles * (w.tiles + 1) / 2;
     // splits of the long contraction: two workgroups a CU, of eight stages at least
     w.stages = static_cast<uint32_t>(w.padded_tall / step_of<2>());
@@ -496,63 +495,50 @@ MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
     w.amax = take.get<float>(kStatBlocks);
     w.scalars = take.get<Scalars>(1);
     for (auto& x : w.x) {
-        for (auto& p : x.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_tall) * w.padded_small);
-        x.stride = w.padded_small;
+        for (auto& p : x.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_tall) * w.padded_side);
+        x.stride = w.padded_side;
     }
     w.part = take.get<float>(static_cast<size_t>(w.splits) * w.pairs * kSide * kSide);
-    for (auto& g : w.g) {
-        for (auto& p : g.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_small) * w.padded_small);
-        g.stride = w.padded_small;
-    }
+    for (auto*& m : w.small) m = take.get<float>(static_cast<size_t>(w.padded_side) * w.padded_side);
+    for (auto& p : w.p.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_side) * w.padded_side);
+    w.p.stride = w.padded_side;
     w.total = take.total();
     return w;
 }
 
-// The polynomial of `steps` steps from G (w.g[0]) on; returns where it is.
-hipError_t polynomial(const MuonWs& w, int steps, Halves* result, hipStream_t st)
+// The polynomial P of `steps` steps from G (w.small[0]) on, as halves in w.p.
+hipError_t polynomial(const MuonWs& w, int steps, hipStream_t st)
 {
-    Halves g = w.g[0], q = w.g[1], t = w.g[2], next = w.g[3], q2 = w.g[4], p = q, p2 = w.g[5], p3 = w.g[6];
-    const uint32_t tiles = static_cast<uint32_t>(w.padded_small / 32);
+    float *g = w.small[0], *q = w.small[1], *t = w.small[2], *next = w.small[3], *p = q, *q2 = w.small[4], *p2 = w.small[5];
+    const uint32_t tiles = static_cast<uint32_t>(w.padded_side / 32);
     SmallArgs args{};
-    args.side = w.padded_small;
+    args.side = w.padded_side;
+    args.p = w.p;
     int jobs = 0;
-    int p_shift = kSmallShift;
-    auto add = [&](const Halves& a, int sa, const Halves& b, int sb, const Halves& out, int so, bool poly) {
-        args.job[jobs++] = SmallJob{a, b, out, ldexpf(1.0f, -(sa + sb)), so, poly ? 1 : 0};
-    };
+    auto add = [&](const float* a, const float* b, float* out, bool poly) { args.job[jobs++] = SmallJob{a, b, out, poly ? 1 : 0}; };
     auto run = [&]() {
         hipLaunchKernelGGL(small_kernel, dim3(tiles * (tiles + 1) / 2, jobs), dim3(256), 0, st, args);
         jobs = 0;
         return hipGetLastError();
     };
     hipError_t e;
-    // (a single step's polynomial is P at once)
-    add(g, kSmallShift, g, kSmallShift, q, steps == 1 ? kPShift : kSmallShift, true);
+    add(g, g, steps == 1 ? nullptr : q, true);
+    if ((e = run()) != hipSuccess || steps == 1) return e;
+    add(g, q, t, false);                            // G Q
     if ((e = run()) != hipSuccess) return e;
     for (int s = 1; s < steps; ++s) {
-        // G Q, then G Q^2 and its polynomial, then P times that beside the next G Q
-        if (s == 1) {
-            add(g, kSmallShift, q, kSmallShift, t, kSmallShift, false);
-            if ((e = run()) != hipSuccess) return e;
-        }
-        add(t, kSmallShift, q, kSmallShift, next, kSmallShift, false);
+        add(t, q, next, false);                     // G Q^2 is the next G,
         if ((e = run()) != hipSuccess) return e;
         std::swap(g, next);
-        add(g, kSmallShift, g, kSmallShift, q2, kSmallShift, true);
+        add(g, g, q2, true);                        // whose polynomial P is multiplied with, beside the G Q after it
         if ((e = run()) != hipSuccess) return e;
-        add(p, p_shift, q2, kSmallShift, p2, kPShift, false);
-        if (s + 1 < steps) add(g, kSmallShift, q2, kSmallShift, t, kSmallShift, false);
+        const bool last = s + 1 == steps;
+        add(p, q2, last ? nullptr : p2, false);
+        if (!last) add(g, q2, t, false);
         if ((e = run()) != hipSuccess) return e;
-        p_shift = kPShift;
-        if (s == 1) {
-            p = p2;
-            p2 = p3;
-        } else {
-            std::swap(p, p2);
-        }
+        p = p2;                                     // (three steps at most: P's place is written once)
         std::swap(q, q2);
     }
-    *result = p;
     return hipSuccess;
 }
 
@@ -580,16 +566,16 @@ void launch_apply(const ApplyArgs& a, Last kind, bool wide, dim3 grid, hipStream
     else hipLaunchKernelGGL((apply_kernel<KS, kParam, true>), grid, dim3(256), 0, st, a);
 }
 
-hipError_t apply(const MuonWs& w, const Halves& x, const Scalars* scalars, const Halves& p, const Halves* next, const Result& r, hipStream_t st)
+hipError_t apply(const MuonWs& w, const Halves& x, const Scalars* scalars, const Halves* next, const Result& r, hipStream_t st)
 {
     ApplyArgs a{};
-    a.x = packed_operand(x.part, w.padded_tall, w.padded_small);     // (X's rows of zeros stay such)
-    a.p = packed_operand(p.part, w.padded_small, w.padded_small);
+    a.x = packed_operand(x.part, w.padded_tall, w.padded_side);     // (X's rows of zeros stay such)
+    a.p = packed_operand(w.p.part, w.padded_side, w.padded_side);
     a.row_tiles = static_cast<uint32_t>(ceil_div(w.tall, kSide));
     a.col_tiles = w.tiles;
     a.splits = splits_of(a.row_tiles, a.col_tiles, false);
-    a.steps = w.padded_small / step_of<2>();
-    a.tall = w.tall; a.padded_tall = w.padded_tall; a.small = w.small; a.padded_small = w.padded_small; a.scalars = scalars;
+    a.steps = w.padded_side / step_of<2>();
+    a.tall = w.tall; a.padded_tall = w.padded_tall; a.small = w.side; a.padded_small = w.padded_side; a.scalars = scalars;
     if (next) a.next = *next;
     a.out = r.out; a.out_stride = r.out_stride; a.param = r.param; a.param_stride = r.param_stride;
     a.copy = static_cast<bf16_t*>(r.copy); a.copy_stride = r.copy_stride; a.keep = r.keep; a.step = r.step;
@@ -608,8 +594,8 @@ hipError_t run_update(const UpdateArgs& u, const MuonWs& w, int steps, const Res
     hipLaunchKernelGGL((stats_kernel<T, MOMENTUM>), dim3(kStatBlocks), dim3(kThreads), 0, st, u);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const PackUpdateArgs pack{u, w.x[0], w.tall, w.padded_tall, w.small, w.padded_small, w.scalars};
-    const int64_t items = w.wide ? ceil_div(w.padded_tall, 64) * ceil_div(w.padded_small, 64) : ceil_div(w.padded_tall * (w.padded_small / 8), kThreads);
+    const PackUpdateArgs pack{u, w.x[0], w.tall, w.padded_tall, w.side, w.padded_side, w.scalars};
+    const int64_t items = w.wide ? ceil_div(w.padded_tall, 64) * ceil_div(w.padded_side, 64) : ceil_div(w.padded_tall * (w.padded_side / 8), kThreads);
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 8192)));
     if (w.wide) hipLaunchKernelGGL((pack_update_kernel<T, MOMENTUM, true>), grid, dim3(kThreads), 0, st, pack);
     else hipLaunchKernelGGL((pack_update_kernel<T, MOMENTUM, false>), grid, dim3(kThreads), 0, st, pack);
@@ -619,17 +605,16 @@ hipError_t run_update(const UpdateArgs& u, const MuonWs& w, int steps, const Res
         const int now = std::min(left, take);
         const Scalars* scalars = left == steps ? w.scalars : nullptr;
         GramArgs g{};
-        g.x = Operand{{w.x[which].part[0], w.x[which].part[1]}, w.padded_small, static_cast<uint32_t>(w.padded_tall - 1), static_cast<uint32_t>(w.padded_small)};
+        g.x = Operand{{w.x[which].part[0], w.x[which].part[1]}, w.padded_side, static_cast<uint32_t>(w.padded_tall - 1), static_cast<uint32_t>(w.padded_side)};
         g.tiles = w.tiles; g.splits = w.splits; g.share = w.share; g.stages = w.stages; g.part = w.part;
         hipLaunchKernelGGL(gram_kernel, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_small, scalars, w.g[0]};
+        const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_side, scalars, w.small[0]};
         hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(kThreads), 0, st, j);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        Halves p;
-        if ((e = polynomial(w, now, &p, st)) != hipSuccess) return e;
+        if ((e = polynomial(w, now, st)) != hipSuccess) return e;
         left -= now;
-        e = apply(w, w.x[which], scalars, p, left > 0 ? &w.x[which ^ 1] : nullptr, r, st);
+        e = apply(w, w.x[which], scalars, left > 0 ? &w.x[which ^ 1] : nullptr, r, st);
     }
     return e;
 }
