@@ -9,7 +9,7 @@
 // and two more leave an error like that of the products taken one after the other in fp32 (all five at once: up to a hundred times that).
 //
 // Products with X are of fp16 halves at a power of two (x 2^k = hi + lo, 22 bits), three matrix instructions each, with fp32 sums: about the error
-// of an fp32 product.  The first X's power follows from its largest magnitude, those of later ones and of P from what they are: singular values of X stay
+// of an fp32 product.  The first X's powers follow from its rows' largest magnitudes, those of later ones and of P from what they are: singular values of X stay
 // below 1.3, of P of three steps below 41.  G is the sum of a long contraction: sums of 256 rows are added to a second set of registers, and the
 // workgroups' shares in 64 bits.  Matrices of the small side are fp32, each taken apart into three bf16 parts (24 bits) for its products, of
 // which the six largest are taken.
@@ -19,7 +19,7 @@ namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr int kHalfShift = 13, kPShift = 10;           // powers of two of later Xs, of P
-constexpr int kStatBlocks = 1024;
+constexpr int kPrepBlocks = 2048;
 constexpr int kMostSplits = 512;
 constexpr int kFlush = 8;                              // stages whose sums are added up apart
 constexpr int kSide = 128;                             // of a tile of G
@@ -30,16 +30,16 @@ struct Halves {
     int64_t stride;
 };
 
-struct Scalars {
-    double inverse;         // 1 / |M|_F, 0 for a matrix of zeros
-    int32_t shift;          // power of two of X's first halves
-};
 
+// momentum, norm, X's first halves
 // ---------------------------------------------------------------------------------------------
-// momentum, norm, largest magnitude
-// ---------------------------------------------------------------------------------------------
-// (u is what is brought to singular values near 1: x itself, or with momentum m <- beta m + g the sum that g's look ahead makes of it)
-struct UpdateArgs {
+// Every 32 rows of X (a stage of G's contraction) have a power of two of their own, which their largest magnitude sets, so that one pass is enough: the
+// norm comes in later, with the powers.
+constexpr int kBlock = 32;              // rows of X that share a power of two
+constexpr int kZeroShift = 200;         // of rows of zeros: beyond all others
+constexpr int kPieces = 8;              // of eight elements, that a thread keeps between finding the largest magnitude and writing
+
+struct PrepArgs {
     const void* g;
     int64_t g_stride;
     float* m;               // NULL: u = g
@@ -48,81 +48,12 @@ struct UpdateArgs {
     int32_t cols;
     float grad_scale, beta;
     int32_t nesterov;
-    double* squares;        // [kStatBlocks]
-    float* amax;            // [kStatBlocks]
+    Halves x;               // rows and columns up to multiples of 32, zeros beyond the matrix; a wide matrix transposed
+    int64_t tall, blocks;
+    int32_t small, padded_small;
+    double* squares;        // [kPrepBlocks]
+    int32_t* shifts;        // [blocks]
 };
-
-__device__ __forceinline__ float update_of(const UpdateArgs& a, float g, float m) { return a.nesterov ? fmaf(a.beta, m, a.grad_scale * g) : m; }
-
-template <class T, bool MOMENTUM>
-__global__ void __launch_bounds__(kThreads) stats_kernel(UpdateArgs a)
-{
-    __shared__ float lds[kThreads / 64];
-    __shared__ double sums[kThreads / 64];
-    double total = 0.0;
-    float top = 0.0f;
-    const int64_t pieces = (a.cols + 7) / 8, all = a.rows * pieces, stride = static_cast<int64_t>(gridDim.x) * kThreads;
-    constexpr int FLIGHT = 4;
-    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i0 < all; i0 += FLIGHT * stride) {
-        T g[FLIGHT][8];
-        float m[FLIGHT][8];
-        int64_t row[FLIGHT];
-        int e[FLIGHT];
-#pragma unroll
-        for (int f = 0; f < FLIGHT; ++f) {
-            const int64_t i = i0 + f * stride;
-            row[f] = i / pieces;
-            e[f] = static_cast<int>(i - row[f] * pieces) * 8;
-            if (i >= all) continue;
-            load_eight(static_cast<const T*>(a.g) + row[f] * a.g_stride, e[f], a.cols, g[f]);
-            if (MOMENTUM) load_eight(a.m + row[f] * a.m_stride, e[f], a.cols, m[f]);
-        }
-#pragma unroll
-        for (int f = 0; f < FLIGHT; ++f) {
-            if (i0 + f * stride >= all) continue;
-            float most = 0.0f, u[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                u[q] = static_cast<float>(g[f][q]);
-                if (MOMENTUM) {
-                    m[f][q] = fmaf(a.beta, m[f][q], a.grad_scale * u[q]);
-                    u[q] = update_of(a, u[q], m[f][q]);
-                }
-                most = fmaxf(most, finite_abs(u[q]));
-                total = fma(static_cast<double>(u[q]), static_cast<double>(u[q]), total);
-            }
-            top = fmaxf(top, most);
-            if (MOMENTUM) {
-                float* to = a.m + row[f] * a.m_stride + e[f];
-                store_some<float, 8>(to, a.cols - e[f], m[f]);
-            }
-        }
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = total;
-    top = block_max(top, lds);
-    if (threadIdx.x == 0) {
-        a.squares[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
-        a.amax[blockIdx.x] = top;
-    }
-}
-
-// X's halves: rows and columns up to multiples of 32, zeros beyond the matrix; a wide matrix transposed.
-struct PackUpdateArgs {
-    UpdateArgs u;
-    Halves x;
-    int64_t tall, padded_tall;      // rows of X
-    int32_t small, padded_small;    // columns
-    Scalars* scalars;
-};
-
-__device__ __forceinline__ int first_shift(const UpdateArgs& a, float* lds)
-{
-    float top = 0.0f;
-    for (int i = threadIdx.x; i < kStatBlocks; i += kThreads) top = fmaxf(top, a.amax[i]);
-    return shift_of(block_max(top, lds));
-}
 
 __device__ __forceinline__ void split_half(float x, int shift, short& hi, short& lo)
 {
@@ -132,91 +63,163 @@ __device__ __forceinline__ void split_half(float x, int shift, short& hi, short&
     lo = __builtin_bit_cast(short, static_cast<f16_t>(y - static_cast<float>(h)));
 }
 
-template <class T, bool MOMENTUM, bool WIDE>
-__global__ void __launch_bounds__(kThreads) pack_update_kernel(PackUpdateArgs a)
+// u: x itself, or with momentum m <- beta m + g what g's look ahead makes of it.  Eight elements from (row, e) on, zeros beyond the columns.
+template <class T, bool MOMENTUM, bool FIRST>
+__device__ __forceinline__ void update_of(const PrepArgs& a, int64_t row, int e, float (&u)[8])
+{
+    T g[8];
+    load_eight(static_cast<const T*>(a.g) + row * a.g_stride, e, a.cols, g);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) u[q] = static_cast<float>(g[q]);
+    if (!MOMENTUM) return;
+    float m[8];
+    float* at = a.m + row * a.m_stride;
+    load_eight(at, e, a.cols, m);
+    if (FIRST) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) m[q] = fmaf(a.beta, m[q], a.grad_scale * u[q]);
+        store_some<float, 8>(at + e, a.cols - e, m);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) u[q] = a.nesterov ? fmaf(a.beta, m[q], a.grad_scale * u[q]) : m[q];
+}
+
+// A block's largest magnitude, found, leaves its power of two behind.
+__device__ __forceinline__ int block_shift(float top, int32_t* shifts, int64_t block, float* lds)
+{
+    top = block_max(top, lds);
+    const int shift = top == 0.0f ? kZeroShift : shift_of(top);
+    if (threadIdx.x == 0) shifts[block] = shift;
+    return shift;
+}
+
+// (HELD: a thread's pieces stay in registers; otherwise they are read again.)
+template <class T, bool MOMENTUM, bool HELD>
+__global__ void __launch_bounds__(kThreads) prep_kernel(PrepArgs a)
 {
     __shared__ float lds[kThreads / 64];
-    __shared__ double sums[kThreads];
-    __shared__ uint32_t turn[WIDE ? 64 * 65 : 1];
-    const int shift = first_shift(a.u, lds);
-    if (blockIdx.x == 0) {
-        double total = 0.0;
-        for (int i = threadIdx.x; i < kStatBlocks; i += kThreads) total += a.u.squares[i];
-        sums[threadIdx.x] = total;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            total = 0.0;
-            for (int i = 0; i < kThreads; ++i) total += sums[i];
-            a.scalars->inverse = total == 0.0 ? 0.0 : 1.0 / sqrt(total);
-            a.scalars->shift = shift;
-        }
-    }
-    auto value = [&](int64_t row, int e, float (&u)[8]) {
-        T g[8];
-        load_eight(static_cast<const T*>(a.u.g) + row * a.u.g_stride, e, a.u.cols, g);
+    __shared__ double sums[kThreads / 64];
+    double total = 0.0;
+    const int across = a.padded_small / 8, pieces = kBlock * across;
+    for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
+        float u[kPieces][8], top = 0.0f;
+        auto first = [&](int p, float (&x)[8]) {
+            const int64_t row = block * kBlock + p / across;
+            const int e = p % across * 8;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) u[q] = static_cast<float>(g[q]);
-        if (MOMENTUM) {
-            float m[8];
-            load_eight(a.u.m + row * a.u.m_stride, e, a.u.cols, m);
+            for (int q = 0; q < 8; ++q) x[q] = 0.0f;
+            if (p < pieces && row < a.tall && e < a.small) update_of<T, MOMENTUM, true>(a, row, e, x);
+        };
+        auto look = [&](const float (&x)[8]) {
+            double more = 0.0;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) u[q] = update_of(a.u, u[q], m[q]);
-        }
-    };
-    if constexpr (!WIDE) {
-        const int64_t pieces = a.padded_small / 8, all = a.padded_tall * pieces;
-        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-            const int64_t row = i / pieces;
-            const int e = static_cast<int>(i - row * pieces) * 8;
-            s16x8 hi = {}, lo = {};
-            if (row < a.tall && e < a.small) {
-                float u[8];
-                value(row, e, u);
+            for (int q = 0; q < 8; ++q) {
+                top = fmaxf(top, finite_abs(x[q]));
+                more = fma(static_cast<double>(x[q]), static_cast<double>(x[q]), more);
+            }
+            total += more;
+        };
+        auto write = [&](int p, const float (&x)[8], int shift) {
+            const int64_t row = block * kBlock + p / across;
+            const int e = p % across * 8;
+            s16x8 hi, lo;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    short h, l;
-                    split_half(u[q], shift, h, l);
-                    hi[q] = h;
-                    lo[q] = l;
-                }
+            for (int q = 0; q < 8; ++q) {
+                short h, l;
+                split_half(x[q], shift, h, l);
+                hi[q] = h;
+                lo[q] = l;
             }
             *reinterpret_cast<s16x8*>(a.x.part[0] + row * a.x.stride + e) = hi;
             *reinterpret_cast<s16x8*>(a.x.part[1] + row * a.x.stride + e) = lo;
-        }
-    } else {
-        // 64 x 64 at a time, by way of LDS: matrix rows are X's columns
-        const int64_t across = (a.padded_tall + 63) / 64, down = (a.padded_small + 63) / 64;
-        for (int64_t t = blockIdx.x; t < across * down; t += gridDim.x) {
-            const int64_t x0 = t / down * 64;
-            const int c0 = static_cast<int>(t % down) * 64;
-            __syncthreads();
-            for (int i = threadIdx.x; i < 64 * 8; i += kThreads) {
-                const int r = i >> 3, e = (i & 7) * 8;
-                float u[8] = {};
-                if (c0 + r < a.small && x0 + e < a.tall) value(c0 + r, static_cast<int>(x0 + e), u);
+        };
+        if constexpr (HELD) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    short h, l;
-                    split_half(u[q], shift, h, l);
-                    turn[(e + q) * 65 + r] = static_cast<uint16_t>(h) | static_cast<uint32_t>(static_cast<uint16_t>(l)) << 16;
-                }
+            for (int i = 0; i < kPieces; ++i)
+                if (i * kThreads < pieces) first(i * kThreads + threadIdx.x, u[i]);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                if (i * kThreads < pieces) look(u[i]);
+            const int shift = block_shift(top, a.shifts, block, lds);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                if (i * kThreads + static_cast<int>(threadIdx.x) < pieces) write(i * kThreads + threadIdx.x, u[i], shift);
+        } else {
+            for (int p = threadIdx.x; p < pieces; p += kThreads) {
+                first(p, u[0]);
+                look(u[0]);
             }
-            __syncthreads();
-            for (int i = threadIdx.x; i < 64 * 8; i += kThreads) {
-                const int r = i >> 3, e = (i & 7) * 8;
-                if (x0 + r >= a.padded_tall || c0 + e >= a.padded_small) continue;
-                s16x8 hi, lo;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const uint32_t both = turn[r * 65 + e + q];
-                    hi[q] = static_cast<short>(both & 0xFFFF);
-                    lo[q] = static_cast<short>(both >> 16);
-                }
-                *reinterpret_cast<s16x8*>(a.x.part[0] + (x0 + r) * a.x.stride + c0 + e) = hi;
-                *reinterpret_cast<s16x8*>(a.x.part[1] + (x0 + r) * a.x.stride + c0 + e) = lo;
+            const int shift = block_shift(top, a.shifts, block, lds);
+            for (int p = threadIdx.x; p < pieces; p += kThreads) {
+                const int64_t row = block * kBlock + p / across;
+                const int e = p % across * 8;
+                float x[8] = {};
+                if (row < a.tall && e < a.small) update_of<T, MOMENTUM, false>(a, row, e, x);
+                write(p, x, shift);
             }
         }
     }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) a.squares[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+// A wide matrix: 32 of its columns are a block, turned by way of LDS, 64 rows at a time.
+template <class T, bool MOMENTUM>
+__global__ void __launch_bounds__(kThreads) prep_wide_kernel(PrepArgs a)
+{
+    __shared__ float lds[kThreads / 64];
+    __shared__ double sums[kThreads / 64];
+    __shared__ uint32_t turn[kBlock * 65];
+    double total = 0.0;
+    for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
+        const int64_t x0 = block * kBlock;
+        float top = 0.0f;
+        for (int p = threadIdx.x; p < a.small * 4; p += kThreads) {
+            const int e = static_cast<int>(x0) + (p & 3) * 8;
+            float u[8];
+            if (e >= a.cols) continue;
+            update_of<T, MOMENTUM, true>(a, p >> 2, e, u);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                top = fmaxf(top, finite_abs(u[q]));
+                total = fma(static_cast<double>(u[q]), static_cast<double>(u[q]), total);
+            }
+        }
+        const int shift = block_shift(top, a.shifts, block, lds);
+        for (int c0 = 0; c0 < a.padded_small; c0 += 64) {
+            __syncthreads();
+            const int r = threadIdx.x >> 2, e = (threadIdx.x & 3) * 8;
+            float u[8] = {};
+            if (c0 + r < a.small && x0 + e < a.cols) update_of<T, MOMENTUM, false>(a, c0 + r, static_cast<int>(x0) + e, u);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                short h, l;
+                split_half(u[q], shift, h, l);
+                turn[(e + q) * 65 + r] = static_cast<uint16_t>(h) | static_cast<uint32_t>(static_cast<uint16_t>(l)) << 16;
+            }
+            __syncthreads();
+            const int x = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+            if (c0 + c < a.padded_small) {
+                s16x8 hi, lo;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t both = turn[x * 65 + c + q];
+                    hi[q] = static_cast<short>(both & 0xFFFF);
+                    lo[q] = static_cast<short>(both >> 16);
+                }
+                *reinterpret_cast<s16x8*>(a.x.part[0] + (x0 + x) * a.x.stride + c0 + c) = hi;
+                *reinterpret_cast<s16x8*>(a.x.part[1] + (x0 + x) * a.x.stride + c0 + c) = lo;
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) a.squares[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -226,6 +229,11 @@ struct GramArgs {
     Operand x;              // across: element (column, row of X)
     uint32_t tiles, splits, share, stages;      // tiles of a side; stages of a split, of all
     float* part;            // [splits][pairs][kSide][kSide]
+    const int32_t* shifts;  // FIRST: powers of two of X's blocks
+    int32_t* split_shift;   // [splits]  of a split's sums
+    const double* squares;  // [square_count], for 1 / |M|_F
+    uint32_t square_count;
+    double* inverse;
 };
 
 // Tile pairs (i, j), i <= j, one after the other.
@@ -239,9 +247,24 @@ __device__ __forceinline__ void pair_at(uint32_t p, uint32_t tiles, uint32_t& i,
     j = i + p;
 }
 
+// FIRST: of X as it came, whose blocks of rows have powers of two of their own: a stage's sums are added by themselves.
+template <bool FIRST>
 __global__ void __launch_bounds__(256, 2) gram_kernel(GramArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<4>()];
+    if (FIRST && blockIdx.x == 0) {         // the norm, from shares
+        double* sums = reinterpret_cast<double*>(lds);
+        double total = 0.0;
+        for (uint32_t i = threadIdx.x; i < a.square_count; i += 256) total += a.squares[i];
+        sums[threadIdx.x] = total;
+        __syncthreads();
+        for (int o = 128; o > 0; o >>= 1) {
+            if (static_cast<int>(threadIdx.x) < o) sums[threadIdx.x] += sums[threadIdx.x + o];
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) *a.inverse = sums[0] == 0.0 ? 0.0 : 1.0 / sqrt(sums[0]);
+        __syncthreads();
+    }
     const uint32_t pairs = a.tiles * (a.tiles + 1) / 2, b = by_xcd(blockIdx.x, gridDim.x), split = b / pairs, pair = b - split * pairs;
     uint32_t ti, tj;
     pair_at(pair, a.tiles, ti, tj);
@@ -249,6 +272,14 @@ __global__ void __launch_bounds__(256, 2) gram_kernel(GramArgs a)
     f32x16 acc[2][2], all[2][2];
     clear(acc);
     clear(all);
+    int least = kZeroShift;                 // of the split's powers of two: that of its sums
+    if (FIRST) {
+        for (uint32_t s = s0 + (threadIdx.x & 63); s < s1; s += 64) least = min(least, a.shifts[s]);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) least = min(least, __shfl_xor(least, o, 64));
+        least = __builtin_amdgcn_readfirstlane(least);
+        if (pair == 0 && threadIdx.x == 0) a.split_shift[split] = least;
+    }
     if (s0 < s1) {
         Loader<2, 4, false> load_a, load_b;
         load_a.start(a.x, ti * kSide, s0);
@@ -262,7 +293,17 @@ __global__ void __launch_bounds__(256, 2) gram_kernel(GramArgs a)
             },
             [&](const unsigned char* stage) {
                 multiply<2, 4, false, false>(stage, acc, ti == tj ? 0 : operand_bytes<4>());
-                if ((++done & (kFlush - 1)) == 0) {
+                if constexpr (FIRST) {
+                    const float factor = ldexpf(1.0f, max(2 * (least - a.shifts[s0 + done]), -200));
+                    ++done;
+#pragma unroll
+                    for (int im = 0; im < 2; ++im)
+#pragma unroll
+                        for (int in = 0; in < 2; ++in)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) all[im][in][i] = fmaf(acc[im][in][i], factor, all[im][in][i]);
+                    clear(acc);
+                } else if ((++done & (kFlush - 1)) == 0) {
 #pragma unroll
                     for (int im = 0; im < 2; ++im)
 #pragma unroll
@@ -287,7 +328,8 @@ struct GramJoinArgs {
     const float* part;
     uint32_t tiles, splits;
     int32_t padded_small;
-    const Scalars* scalars; // NULL: X's halves are of X 2^kHalfShift
+    const int32_t* split_shift;     // NULL: X's halves are of X 2^kHalfShift
+    const double* inverse;
     float* g;               // [padded_small][padded_small]
 };
 
@@ -311,12 +353,15 @@ __global__ void __launch_bounds__(kThreads) gram_join_kernel(GramJoinArgs a)
     double sum = 0.0;
     const float* from = a.part + static_cast<int64_t>(pair) * (kSide * kSide) + at;
 #pragma unroll 8
-    for (uint32_t s = threadIdx.x >> 6; s < a.splits; s += 4) sum += static_cast<double>(from[static_cast<int64_t>(s) * pairs * (kSide * kSide)]);
+    for (uint32_t s = threadIdx.x >> 6; s < a.splits; s += 4) {
+        const double x = static_cast<double>(from[static_cast<int64_t>(s) * pairs * (kSide * kSide)]);
+        sum += a.split_shift ? ldexp(x, -2 * a.split_shift[s]) : x;
+    }
     lds[threadIdx.x] = sum;
     __syncthreads();
     if (threadIdx.x >= 64 || col >= a.padded_small || row > col) return;
     sum = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
-    if (a.scalars) sum = ldexp(sum * a.scalars->inverse * a.scalars->inverse, -2 * a.scalars->shift);
+    if (a.split_shift) sum = sum * *a.inverse * *a.inverse;
     else sum = ldexp(sum, -2 * kHalfShift);
     a.g[row * a.padded_small + col] = a.g[col * a.padded_small + row] = static_cast<float>(sum);
 }
@@ -400,7 +445,8 @@ struct ApplyArgs {
     int32_t steps;
     int64_t tall, padded_tall;
     int32_t small, padded_small;
-    const Scalars* scalars; // NULL: X's halves are of X 2^kHalfShift
+    const int32_t* shifts;  // NULL: X's halves are of X 2^kHalfShift
+    const double* inverse;
     // one of: the next X's halves; a matrix out; parameters
     Halves next;
     void* out;
@@ -414,19 +460,42 @@ struct ApplyArgs {
 
 enum Last { kNext, kFloat, kBfloat, kParam };
 
+// Sixteen results of a lane: rows row + sum_row(i) of X, a column.
 template <Last L, bool WIDE>
-__device__ __forceinline__ void finish(const ApplyArgs& a, int64_t row, int col, float x)
+__device__ __forceinline__ void finish(const ApplyArgs& a, int64_t row, int col, const float (&x)[16])
 {
-    if (row >= a.tall || col >= a.small) return;
-    const int64_t r = WIDE ? col : row, c = WIDE ? row : col;
-    if (L == kFloat) static_cast<float*>(a.out)[r * a.out_stride + c] = x;
-    if (L == kBfloat) static_cast<bf16_t*>(a.out)[r * a.out_stride + c] = static_cast<bf16_t>(x);
-    if (L == kParam) {
-        float* p = a.param + r * a.param_stride + c;
-        const float now = fmaf(-a.step, x, *p * a.keep);
-        *p = now;
-        if (a.copy) a.copy[r * a.copy_stride + c] = static_cast<bf16_t>(now);
+    if (L == kNext) {
+        if (col >= a.padded_small) return;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (row + sum_row(i) < a.padded_tall) put(a.next, row + sum_row(i), col, x[i], kHalfShift);
+        return;
     }
+    if (col >= a.small) return;
+    // (a wide matrix has X's rows as columns: four of them are side by side)
+    const int64_t step = WIDE ? 1 : L == kParam ? a.param_stride : a.out_stride, first = WIDE ? col * (L == kParam ? a.param_stride : a.out_stride) + row : row * step + col;
+    if (L == kFloat || L == kBfloat) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (row + sum_row(i) >= a.tall) continue;
+            if (L == kFloat) static_cast<float*>(a.out)[first + sum_row(i) * step] = x[i];
+            else static_cast<bf16_t*>(a.out)[first + sum_row(i) * step] = static_cast<bf16_t>(x[i]);
+        }
+        return;
+    }
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = row + sum_row(i) < a.tall ? a.param[first + sum_row(i) * step] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = fmaf(-a.step, x[i], p[i] * a.keep);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (row + sum_row(i) < a.tall) a.param[first + sum_row(i) * step] = p[i];
+    if (!a.copy) return;
+    const int64_t copy_step = WIDE ? 1 : a.copy_stride, copy_first = WIDE ? col * a.copy_stride + row : row * a.copy_stride + col;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (row + sum_row(i) < a.tall) a.copy[copy_first + sum_row(i) * copy_step] = static_cast<bf16_t>(p[i]);
 }
 
 template <int KS, Last L, bool WIDE>
@@ -437,23 +506,22 @@ __global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
     uint32_t col_tile, split;
     pair_of(by_xcd(blockIdx.x, gridDim.x), a.col_tiles, a.splits, col_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
-    const float factor = a.scalars ? static_cast<float>(ldexp(a.scalars->inverse, -(a.scalars->shift + kPShift))) : ldexpf(1.0f, -(kHalfShift + kPShift));
+    const double inverse = a.shifts ? *a.inverse : 1.0;
     all_scores<2, 4, KS>(a.x, a.p, col_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
 #pragma unroll
-        for (int im = 0; im < 2; ++im)
+        for (int im = 0; im < 2; ++im) {
+            const int64_t row0 = static_cast<int64_t>(tile_row0) + m0 + 32 * im;
+            if (row0 >= a.padded_tall) continue;
+            const int shift = a.shifts ? a.shifts[row0 / kBlock] : kHalfShift;
+            const float factor = static_cast<float>(ldexp(inverse, -(shift + kPShift)));
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 2; ++j) {
+                float x[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int64_t row = static_cast<int64_t>(tile_row0) + m0 + 32 * im + sum_row(i) + lane_row();
-                    const int col = col_tile * kSide + n0 + 32 * j + (lane & 31);
-                    const float x = acc[im][j][i] * factor;
-                    if (L == kNext) {
-                        if (row < a.padded_tall && col < a.padded_small) put(a.next, row, col, x, kHalfShift);
-                    } else {
-                        finish<L, WIDE>(a, row, col, x);
-                    }
-                }
+                for (int i = 0; i < 16; ++i) x[i] = acc[im][j][i] * factor;
+                finish<L, WIDE>(a, row0 + lane_row(), col_tile * kSide + n0 + 32 * j + (lane & 31), x);
+            }
+        }
     });
 }
 
@@ -465,9 +533,8 @@ struct MuonWs {
     int32_t side, padded_side;      // the smaller one
     bool wide;
     uint32_t tiles, pairs, splits, share, stages;
-    double* squares;
-    float* amax;
-    Scalars* scalars;
+    double *squares, *inverse;
+    int32_t *shifts, *split_shift;
     Halves x[2];
     float* part;
     float* small[6];                // matrices of the small side
@@ -491,9 +558,10 @@ MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
     w.share = static_cast<uint32_t>(ceil_div(w.stages, most));
     w.splits = static_cast<uint32_t>(ceil_div(w.stages, w.share));
     Carver take{base};
-    w.squares = take.get<double>(kStatBlocks);
-    w.amax = take.get<float>(kStatBlocks);
-    w.scalars = take.get<Scalars>(1);
+    w.squares = take.get<double>(kPrepBlocks);
+    w.inverse = take.get<double>(1);
+    w.shifts = take.get<int32_t>(static_cast<size_t>(w.padded_tall / kBlock));
+    w.split_shift = take.get<int32_t>(w.splits);
     for (auto& x : w.x) {
         for (auto& p : x.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_tall) * w.padded_side);
         x.stride = w.padded_side;
@@ -566,7 +634,7 @@ void launch_apply(const ApplyArgs& a, Last kind, bool wide, dim3 grid, hipStream
     else hipLaunchKernelGGL((apply_kernel<KS, kParam, true>), grid, dim3(256), 0, st, a);
 }
 
-hipError_t apply(const MuonWs& w, const Halves& x, const Scalars* scalars, const Halves* next, const Result& r, hipStream_t st)
+hipError_t apply(const MuonWs& w, const Halves& x, bool first, const Halves* next, const Result& r, hipStream_t st)
 {
     ApplyArgs a{};
     a.x = packed_operand(x.part, w.padded_tall, w.padded_side);     // (X's rows of zeros stay such)
@@ -575,7 +643,7 @@ hipError_t apply(const MuonWs& w, const Halves& x, const Scalars* scalars, const
     a.col_tiles = w.tiles;
     a.splits = splits_of(a.row_tiles, a.col_tiles, false);
     a.steps = w.padded_side / step_of<2>();
-    a.tall = w.tall; a.padded_tall = w.padded_tall; a.small = w.side; a.padded_small = w.padded_side; a.scalars = scalars;
+    a.tall = w.tall; a.padded_tall = w.padded_tall; a.small = w.side; a.padded_small = w.padded_side; a.shifts = first ? w.shifts : nullptr; a.inverse = w.inverse;
     if (next) a.next = *next;
     a.out = r.out; a.out_stride = r.out_stride; a.param = r.param; a.param_stride = r.param_stride;
     a.copy = static_cast<bf16_t*>(r.copy); a.copy_stride = r.copy_stride; a.keep = r.keep; a.step = r.step;
@@ -589,32 +657,31 @@ hipError_t apply(const MuonWs& w, const Halves& x, const Scalars* scalars, const
 }
 
 template <class T, bool MOMENTUM>
-hipError_t run_update(const UpdateArgs& u, const MuonWs& w, int steps, const Result& r, hipStream_t st)
+hipError_t run_update(PrepArgs u, const MuonWs& w, int steps, const Result& r, hipStream_t st)
 {
-    hipLaunchKernelGGL((stats_kernel<T, MOMENTUM>), dim3(kStatBlocks), dim3(kThreads), 0, st, u);
+    u.x = w.x[0]; u.tall = w.tall; u.blocks = w.padded_tall / kBlock; u.small = w.side; u.padded_small = w.padded_side; u.squares = w.squares; u.shifts = w.shifts;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(u.blocks, kPrepBlocks)));
+    if (w.wide) hipLaunchKernelGGL((prep_wide_kernel<T, MOMENTUM>), grid, dim3(kThreads), 0, st, u);
+    else if (kBlock * w.padded_side / 8 <= kPieces * kThreads) hipLaunchKernelGGL((prep_kernel<T, MOMENTUM, true>), grid, dim3(kThreads), 0, st, u);
+    else hipLaunchKernelGGL((prep_kernel<T, MOMENTUM, false>), grid, dim3(kThreads), 0, st, u);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const PackUpdateArgs pack{u, w.x[0], w.tall, w.padded_tall, w.side, w.padded_side, w.scalars};
-    const int64_t items = w.wide ? ceil_div(w.padded_tall, 64) * ceil_div(w.padded_side, 64) : ceil_div(w.padded_tall * (w.padded_side / 8), kThreads);
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 8192)));
-    if (w.wide) hipLaunchKernelGGL((pack_update_kernel<T, MOMENTUM, true>), grid, dim3(kThreads), 0, st, pack);
-    else hipLaunchKernelGGL((pack_update_kernel<T, MOMENTUM, false>), grid, dim3(kThreads), 0, st, pack);
-    e = hipGetLastError();
     int which = 0, take = 3;            // the first G serves three steps, later ones two
     for (int left = steps; left > 0 && e == hipSuccess; which ^= 1, take = 2) {
         const int now = std::min(left, take);
-        const Scalars* scalars = left == steps ? w.scalars : nullptr;
+        const bool first = left == steps;
         GramArgs g{};
         g.x = Operand{{w.x[which].part[0], w.x[which].part[1]}, w.padded_side, static_cast<uint32_t>(w.padded_tall - 1), static_cast<uint32_t>(w.padded_side)};
         g.tiles = w.tiles; g.splits = w.splits; g.share = w.share; g.stages = w.stages; g.part = w.part;
-        hipLaunchKernelGGL(gram_kernel, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
+        g.shifts = w.shifts; g.split_shift = w.split_shift; g.squares = w.squares; g.square_count = grid.x; g.inverse = w.inverse;
+        if (first) hipLaunchKernelGGL(gram_kernel<true>, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
+        else hipLaunchKernelGGL(gram_kernel<false>, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_side, scalars, w.small[0]};
+        const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_side, first ? w.split_shift : nullptr, w.inverse, w.small[0]};
         hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(kThreads), 0, st, j);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if ((e = polynomial(w, now, st)) != hipSuccess) return e;
         left -= now;
-        e = apply(w, w.x[which], scalars, left > 0 ? &w.x[which ^ 1] : nullptr, r, st);
+        e = apply(w, w.x[which], first, left > 0 ? &w.x[which ^ 1] : nullptr, r, st);
     }
     return e;
 }
@@ -649,7 +716,7 @@ ne_status ne_orthogonalize(const void* x_dev, int32_t x_type, int64_t x_stride, 
     const MuonWs w = muon_layout(rows, cols, static_cast<char*>(workspace_dev));
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
         return fail(NE_ERR_ARG, who + "workspace_dev is NULL, not 256-byte aligned, or smaller than ne_orthogonalize_workspace_bytes()");
-    const UpdateArgs u{x_dev, x_stride, nullptr, 0, rows, static_cast<int32_t>(cols), 1.0f, 0.0f, 0, w.squares, w.amax};
+    const PrepArgs u{x_dev, x_stride, nullptr, 0, rows, static_cast<int32_t>(cols), 1.0f, 0.0f, 0};
     const Result r{out_type == NE_F32 ? kFloat : kBfloat, out_dev, out_stride, nullptr, 0, nullptr, 0, 0.0f, 0.0f};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const hipError_t e = x_type == NE_F32 ? run_update<float, false>(u, w, steps, r, st) : run_update<bf16_t, false>(u, w, steps, r, st);
@@ -678,7 +745,7 @@ ne_status ne_muon_step(float* param_dev, int64_t param_stride, const void* grad_
     const MuonWs w = muon_layout(rows, cols, static_cast<char*>(workspace_dev));
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < w.total)
         return fail(NE_ERR_ARG, who + "workspace_dev is NULL, not 256-byte aligned, or smaller than ne_orthogonalize_workspace_bytes()");
-    const UpdateArgs u{grad_dev, grad_stride, momentum_dev, momentum_stride, rows, static_cast<int32_t>(cols), grad_scale, momentum, nesterov != 0, w.squares, w.amax};
+    const PrepArgs u{grad_dev, grad_stride, momentum_dev, momentum_stride, rows, static_cast<int32_t>(cols), grad_scale, momentum, nesterov != 0};
     const Result r{kParam, nullptr, 0, param_dev, param_stride, param_bf16_dev, param_bf16_stride, 1.0f - lr * weight_decay, lr * scale};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const hipError_t e = grad_type == NE_F32 ? run_update<float, true>(u, w, steps, r, st) : run_update<bf16_t, true>(u, w, steps, r, st);
