@@ -11,8 +11,8 @@
 // Products with X are of fp16 halves at a power of two (x 2^k = hi + lo, 22 bits), three matrix instructions each, with fp32 sums: about the error
 // of an fp32 product.  The first X's powers follow from its rows' largest magnitudes, those of later ones and of P from what they are: singular values of X stay
 // below 1.3, of P of three steps below 41.  G is the sum of a long contraction: sums of 256 rows are added to a second set of registers, and the
-// workgroups' shares in 64 bits.  Matrices of the small side are fp32, each taken apart into three bf16 parts (24 bits) for its products, of
-// which the six largest are taken.
+// workgroups' shares in 64 bits.  Matrices of the small side are fp32, taken apart into three bf16 parts (24 bits) for their products, of which
+// the six largest are taken.
 #include "ne_tiles.h"
 
 namespace {
@@ -323,16 +323,6 @@ __global__ void __launch_bounds__(256, 2) gram_kernel(GramArgs a)
                 out[(first_row<4>() + 32 * im + sum_row(i) + lane_row()) * kSide + first_col<4>() + 32 * in + (lane & 31)] = all[im][in][i] + acc[im][in][i];
 }
 
-// The splits' sums, joined in 64 bits and scaled; both triangles.
-struct GramJoinArgs {
-    const float* part;
-    uint32_t tiles, splits;
-    int32_t padded_small;
-    const int32_t* split_shift;     // NULL: X's halves are of X 2^kHalfShift
-    const double* inverse;
-    float* g;               // [padded_small][padded_small]
-};
-
 __device__ __forceinline__ void put(const Halves& to, int64_t row, int64_t col, float x, int shift)
 {
     short hi, lo;
@@ -341,46 +331,196 @@ __device__ __forceinline__ void put(const Halves& to, int64_t row, int64_t col, 
     to.part[1][row * to.stride + col] = static_cast<uint16_t>(lo);
 }
 
-__global__ void __launch_bounds__(kThreads) gram_join_kernel(GramJoinArgs a)
+// The splits' sums, joined in 64 bits and scaled; both triangles.
+struct GramJoinArgs {
+    const float* part;
+    uint32_t tiles, splits;
+    int32_t side;
+    const int32_t* split_shift;     // NULL: X's halves are of X 2^kHalfShift
+    const double* inverse;
+    float* g;               // [side][side]
+};
+
+// 64 elements of a row of a tile pair, whose splits sixteen wavefronts share.
+__global__ void __launch_bounds__(1024) gram_join_kernel(GramJoinArgs a)
 {
-    // 64 elements of a row of a tile pair, whose splits four wavefronts share
-    __shared__ double lds[kThreads];
+    __shared__ double lds[1024];
     const uint32_t pairs = a.tiles * (a.tiles + 1) / 2, per = kSide * kSide / 64, pair = blockIdx.x / per, at = (blockIdx.x % per) * 64 + (threadIdx.x & 63);
     uint32_t ti, tj;
     pair_at(pair, a.tiles, ti, tj);
     const int64_t row = ti * kSide + at / kSide, col = tj * kSide + at % kSide;
-    if (row >= a.padded_small) return;      // (the same for all of the workgroup)
+    if (row >= a.side) return;      // (the same for all of the workgroup)
     double sum = 0.0;
     const float* from = a.part + static_cast<int64_t>(pair) * (kSide * kSide) + at;
-#pragma unroll 8
-    for (uint32_t s = threadIdx.x >> 6; s < a.splits; s += 4) {
-        const double x = static_cast<double>(from[static_cast<int64_t>(s) * pairs * (kSide * kSide)]);
-        sum += a.split_shift ? ldexp(x, -2 * a.split_shift[s]) : x;
+    constexpr int FLIGHT = 8;
+    for (uint32_t s0 = threadIdx.x >> 6; s0 < a.splits; s0 += 16 * FLIGHT) {
+        float x[FLIGHT];
+        int shift[FLIGHT];
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) {
+            const uint32_t s = s0 + 16 * f;
+            x[f] = 0.0f;
+            shift[f] = kHalfShift;
+            if (s >= a.splits) continue;
+            x[f] = from[static_cast<int64_t>(s) * pairs * (kSide * kSide)];
+            if (a.split_shift) shift[f] = a.split_shift[s];
+        }
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) sum += ldexp(static_cast<double>(x[f]), -2 * shift[f]);
     }
     lds[threadIdx.x] = sum;
     __syncthreads();
-    if (threadIdx.x >= 64 || col >= a.padded_small || row > col) return;
-    sum = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
+    if (threadIdx.x >= 64 || col >= a.side || row > col) return;
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += lds[w * 64 + threadIdx.x];
     if (a.split_shift) sum = sum * *a.inverse * *a.inverse;
-    else sum = ldexp(sum, -2 * kHalfShift);
-    a.g[row * a.padded_small + col] = a.g[col * a.padded_small + row] = static_cast<float>(sum);
+    a.g[row * a.side + col] = a.g[col * a.side + row] = static_cast<float>(sum);
 }
 
 // ---------------------------------------------------------------------------------------------
 // products of the small side
 // ---------------------------------------------------------------------------------------------
-// All of them are polynomials of one symmetric matrix, so they are symmetric, commute, and rows serve as columns.  A workgroup has a tile of
-// 32 x 32 on or above the diagonal, its four wavefronts a quarter of the contraction each, straight from L2 into the matrix cores' operands.
+// All of them are polynomials of one symmetric matrix, so they are symmetric (but for roundings) and commute.  They are fp32 [side][side], side a
+// multiple of 32.
+//
+// Up to kRowsSide a step is one launch: row by row, v Q(G) = kA v + kB v G + kC (v G) G, so a workgroup takes 16 rows of G and of P through
+// all products of the step, and nothing waits for another workgroup.  A wavefront has 16 columns, whose share of G stays in its registers; rows go
+// from product to product through LDS.  (Side 128, three steps and two: 5 launches in the place of 13, which took 71 us.)
+constexpr int kRowsSide = 256;
+
+struct RowsArgs {
+    const float* g;
+    const float* p;         // NULL: the first step, P = 1
+    float* next;            // NULL, or G Q(G)^2
+    float* out;             // P Q(G), or NULL: as halves
+    Halves halves;
+    int32_t side;
+};
+
+template <int WAVES>
+struct Rows {               // 16 rows as three bf16 parts
+    static constexpr int STRIDE = WAVES * 16 + 8;
+    bf16_t part[3][16][STRIDE];
+};
+
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs a)
+{
+    constexpr int STEPS = WAVES / 2;
+    __shared__ __align__(16) Rows<WAVES> v_rows[2], p_rows[2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * 16;
+    const int c = wave * 16 + col;
+    const bool works = wave * 16 < a.side;
+    const int steps = a.side / 32;
+    // (columns, not rows in their place: what roundings leave of G - G^T would grow 24 times a step, G times G^T no longer being a power of one matrix)
+    bf16x8 held[STEPS][3];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        float x[8] = {};
+        if (works && s < steps)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = a.g[static_cast<int64_t>(s * 32 + quarter * 8 + q) * a.side + c];
+        split_bf16<3>(x, held[s]);
+    }
+    // a lane's four results: rows 4 quarter .. + 3, its column
+    auto load = [&](const float* from, float (&x)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = works ? from[(row0 + quarter * 4 + i) * a.side + c] : 0.0f;
+    };
+    auto keep = [&](Rows<WAVES>& rows, const float (&x)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float rest = x[i];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const bf16_t y = static_cast<bf16_t>(rest);
+                rows.part[p][quarter * 4 + i][c] = y;
+                rest -= static_cast<float>(y);
+            }
+        }
+    };
+    auto times_g = [&](const Rows<WAVES>& rows, float (&x)[4]) {
+        // (the largest products in sums of every fourth step: an instruction's sum is cut off where the larger of what it adds ends)
+        f32x4 sum[4], small = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) sum[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (s >= steps) break;
+            bf16x8 y[3];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) y[p] = *reinterpret_cast<const bf16x8*>(&rows.part[p][col][s * 32 + quarter * 8]);
+            // (the smallest products first, apart from the largest)
+#pragma unroll
+            for (int of_parts = 2; of_parts >= 0; --of_parts) {
+                f32x4& to = of_parts > 0 ? small : sum[s % 4];
+#pragma unroll
+                for (int q = 0; q <= of_parts; ++q) to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[q], held[s][of_parts - q], to, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = ((sum[0][i] + sum[1][i]) + (sum[2][i] + sum[3][i])) + small[i];
+    };
+    float v[4], v1[4], v2[4], p[4], p1[4], p2[4];
+    load(a.g, v);
+    keep(v_rows[0], v);
+    if (a.p) {
+        load(a.p, p);
+        keep(p_rows[0], p);
+    }
+    __syncthreads();
+    const bool first = !a.p, moves = a.next != nullptr;
+    if (first || moves) times_g(v_rows[0], v1);
+    if (!first) times_g(p_rows[0], p1);
+    if (first) {            // P = 1: P G and P G G are G's rows and v G
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = row0 + quarter * 4 + i == c ? 1.0f : 0.0f;
+            p1[i] = v[i];
+            p2[i] = v1[i];
+        }
+    }
+    if (moves) keep(v_rows[1], v1);
+    if (!first) keep(p_rows[1], p1);
+    __syncthreads();
+    if (moves) times_g(v_rows[1], v2);
+    if (!first) times_g(p_rows[1], p2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + quarter * 4 + i;
+        const float x = fmaf(kC, p2[i], fmaf(kB, p1[i], kA * p[i]));
+        if (!works) continue;
+        if (a.out) a.out[row * a.side + c] = x;
+        else put(a.halves, row, c, x, kPShift);
+    }
+    if (!moves) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = fmaf(kC, v2[i], fmaf(kB, v1[i], kA * v[i]));
+    keep(v_rows[0], v);
+    __syncthreads();
+    times_g(v_rows[0], v1);
+    keep(v_rows[1], v1);
+    __syncthreads();
+    times_g(v_rows[1], v2);
+    if (works)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.next[(row0 + quarter * 4 + i) * a.side + c] = fmaf(kC, v2[i], fmaf(kB, v1[i], kA * v[i]));
+}
+
+// Larger sides: a product is a launch, or two that do not wait for one another.  A workgroup has a tile of 32 x 32 on or above the diagonal, its four
+// wavefronts a quarter of the contraction each, straight from L2 into the matrix cores' operands.
 struct SmallJob {
     const float *a, *b;
     float* out;             // NULL: the halves of P, for the product with X
-    int32_t polynomial;     // out = kA + kB a + kC (a b), for a = b = G
+    int32_t polynomial;     // kA + kB a + kC (a b), for a = b = G, in the place of a b
 };
 
 struct SmallArgs {
     SmallJob job[2];
     Halves p;
-    int32_t side;           // multiple of 32
+    int32_t side;
 };
 
 __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
@@ -393,6 +533,11 @@ __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, steps = args.side / 16;
     const float* a = job.a + static_cast<int64_t>(ti * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
     const float* b = job.b + static_cast<int64_t>(tj * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
+    // (the polynomial's other term is fetched ahead of the sums)
+    float g[4] = {};
+    if (job.polynomial)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) g[q] = job.a[static_cast<int64_t>(ti * 32 + (threadIdx.x >> 5) + 8 * q) * args.side + tj * 32 + (threadIdx.x & 31)];
     f32x16 sum, small;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i] = small[i] = 0.0f;
@@ -421,17 +566,28 @@ __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
 #pragma unroll
     for (int i = 0; i < 16; ++i) lds[wave][(sum_row(i) + lane_row()) * 33 + (lane & 31)] = sum[i] + small[i];
     __syncthreads();
-    for (int i = threadIdx.x; i < 32 * 32; i += 256) {
-        const int r = i >> 5, c = i & 31, at = r * 33 + c;
-        const int64_t row = ti * 32 + r, col = tj * 32 + c;
-        if (row > col) continue;
+    float* all = lds[0];            // the results; on the diagonal those above it are both
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = (threadIdx.x >> 5) + 8 * q, c = threadIdx.x & 31, at = r * 33 + c;
         float x = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
-        if (job.polynomial) x = fmaf(kC, x, kB * job.a[row * args.side + col]) + (row == col ? kA : 0.0f);
-        if (job.out) {
-            job.out[row * args.side + col] = job.out[col * args.side + row] = x;
+        if (job.polynomial) x = fmaf(kC, x, kB * g[q]) + (ti == tj && r == c ? kA : 0.0f);
+        all[at] = x;                // (read by this thread alone so far)
+    }
+    __syncthreads();
+    auto write = [&](uint32_t i, uint32_t j, int r, int c, float x) {
+        const int64_t row = i * 32 + r, col = j * 32 + c;
+        if (job.out) job.out[row * args.side + col] = x;
+        else put(args.p, row, col, x, kPShift);
+    };
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = (threadIdx.x >> 5) + 8 * q, c = threadIdx.x & 31;
+        if (ti == tj) {
+            write(ti, tj, r, c, all[min(r, c) * 33 + max(r, c)]);
         } else {
-            put(args.p, row, col, x, kPShift);
-            if (row != col) put(args.p, col, row, x, kPShift);
+            write(ti, tj, r, c, all[r * 33 + c]);
+            write(tj, ti, r, c, all[c * 33 + r]);
         }
     }
 }
@@ -574,9 +730,27 @@ MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
     return w;
 }
 
-// The polynomial P of `steps` steps from G (w.small[0]) on, as halves in w.p.
+// The polynomial P of `steps` steps (three at most) from G (w.small[0]) on, as halves in w.p.
 hipError_t polynomial(const MuonWs& w, int steps, hipStream_t st)
 {
+    hipError_t e = hipSuccess;
+    if (w.padded_side <= kRowsSide) {
+        RowsArgs a{};
+        a.side = w.padded_side;
+        a.halves = w.p;
+        float *g = w.small[0], *next = w.small[1], *p = nullptr, *out = w.small[2], *other = w.small[3];
+        for (int s = 1; s <= steps && e == hipSuccess; ++s) {
+            a.g = g; a.p = p; a.next = s < steps ? next : nullptr; a.out = s < steps ? out : nullptr;
+            const dim3 grid(static_cast<unsigned>(w.padded_side / 16));
+            if (w.padded_side <= 128) hipLaunchKernelGGL(rows_kernel<8>, grid, dim3(512), 0, st, a);
+            else hipLaunchKernelGGL(rows_kernel<16>, grid, dim3(1024), 0, st, a);
+            e = hipGetLastError();
+            std::swap(g, next);
+            p = out;
+            std::swap(out, other);
+        }
+        return e;
+    }
     float *g = w.small[0], *q = w.small[1], *t = w.small[2], *next = w.small[3], *p = q, *q2 = w.small[4], *p2 = w.small[5];
     const uint32_t tiles = static_cast<uint32_t>(w.padded_side / 32);
     SmallArgs args{};
@@ -589,7 +763,6 @@ hipError_t polynomial(const MuonWs& w, int steps, hipStream_t st)
         jobs = 0;
         return hipGetLastError();
     };
-    hipError_t e;
     add(g, g, steps == 1 ? nullptr : q, true);
     if ((e = run()) != hipSuccess || steps == 1) return e;
     add(g, q, t, false);                            // G Q
@@ -677,7 +850,7 @@ hipError_t run_update(PrepArgs u, const MuonWs& w, int steps, const Result& r, h
         else hipLaunchKernelGGL(gram_kernel<false>, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_side, first ? w.split_shift : nullptr, w.inverse, w.small[0]};
-        hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(kThreads), 0, st, j);
+        hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(1024), 0, st, j);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if ((e = polynomial(w, now, st)) != hipSuccess) return e;
         left -= now;
