@@ -3,9 +3,13 @@
 A pair (src, ctx) is scored against every row of the context table instead of a few sampled ones:
 loss = -log softmax(context . vertex[src])[ctx].  A step looks up the batch's vertex rows, takes the softmax cross
 entropy against the whole context table without keeping the scores, brings the gradients back to both tables (the
-vertex table's by sorted ids) and moves both with AdamW.  Every part is a call of the library; torch allocates and marks the pairs that are left out.
+vertex table's by sorted ids) and moves both with AdamW, or with Muon, whose updates have singular values near 1.  With an entropy weight the
+objective also holds up the entropy of what the model answers.  predict() answers with it: the most probable contexts of given nodes.  Every part is a call
+of the library; torch allocates and marks the pairs that are left out.
 """
 from __future__ import annotations
+
+import math
 
 import torch
 
@@ -16,16 +20,25 @@ class SoftmaxTrainer:
     """Trains vertex and context (float32 [num_nodes][dim], CUDA, updated in place) on batches of at most `batch` pairs.
 
     compute: torch.float32, or torch.bfloat16 for products and gradients in bf16 on rounded copies of the tables that
-    every step of AdamW writes.  state_bits: 32, or 8 for AdamW states of a byte each."""
+    every step of the optimizer writes.  state_bits: 32, or 8 for AdamW states of a byte each.
+
+    optimizer: "adamw", or "muon" (momentum with Nesterov's look ahead, Newton-Schulz updates of each table as one matrix, scaled to elements as
+    large as AdamW's: learning rates are comparable).  entropy_weight: what is minimised is loss - entropy_weight * entropy."""
 
     def __init__(self, vertex: torch.Tensor, context: torch.Tensor, batch: int, state_bits: int = 32, weight_decay: float = 0.0,
-                 compute: torch.dtype = torch.float32, seed: int = 0):
+                 compute: torch.dtype = torch.float32, seed: int = 0, optimizer: str = "adamw", momentum: float = 0.95,
+                 entropy_weight: float = 0.0):
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
         if vertex.shape != context.shape or vertex.dim() != 2:
             raise ValueError("vertex and context must both be [num_nodes][dim]")
+        if optimizer not in ("adamw", "muon") or (optimizer == "muon" and state_bits != 32):
+            raise ValueError("optimizer must be 'adamw', or 'muon' with state_bits 32")
+        if not math.isfinite(entropy_weight):
+            raise ValueError("entropy_weight must be finite")
         V, d = vertex.shape
         dev = vertex.device
+        self.entropy_weight, self.momentum, self.weight_decay = entropy_weight, momentum, weight_decay
         self.batch, self.steps = batch, 0
         self.tables = [vertex, context]
         copies = None
@@ -37,7 +50,16 @@ class SoftmaxTrainer:
         self.loss, self.lse = (torch.empty(batch, dtype=torch.float32, device=dev) for _ in range(2))
         size = max(ne.ne_embed_workspace_bytes(V, d, batch), ne.ne_xent_workspace_bytes(batch, V, d, compute, False),
                    ne.ne_xent_workspace_bytes(batch, V, d, compute, True))
+        if entropy_weight:
+            self.entropy = torch.empty(batch, dtype=torch.float32, device=dev)
+            size = max(size, ne.ne_logprob_workspace_bytes(batch, V, d, compute), ne.ne_logprob_workspace_bytes(batch, V, d, compute, grad=True))
+        if optimizer == "muon":
+            size = max(size, ne.ne_orthogonalize_workspace_bytes(V, d))
         self.work = torch.empty(size, dtype=torch.uint8, device=dev)     # one after the other on one stream: shared by the calls
+        self.opt, self.copies, self.answers_work = None, copies, None
+        if optimizer == "muon":
+            self.momenta = [torch.zeros((V, d), device=dev) for _ in range(2)]
+            return
         kw = {}
         if state_bits == 8:
             states = [[torch.zeros((V, d), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) for _ in range(2)] for _ in range(2)]
@@ -62,9 +84,41 @@ class SoftmaxTrainer:
         ctx = torch.where(src.clamp(0, self.tables[0].shape[0] - 1) == src, pairs[:, 1], -1)
         h, dh, loss, lse = self.h[:n], self.dh[:n], self.loss[:n], self.lse[:n]
         ne.ne_embed_lookup(self.rows[0], src, h)
-        ne.ne_xent_loss(h, self.rows[1], ctx, loss, lse, self.work)
-        ne.ne_xent_grad(h, self.rows[1], ctx, lse, dh, self.grads[1], self.work, scale=1.0 / n)
+        if self.entropy_weight:
+            entropy = self.entropy[:n]
+            ne.ne_logprob(h, self.rows[1], ctx, lse, self.work, logp=loss, entropy=entropy)
+            ne.ne_logprob_grad(h, self.rows[1], ctx, lse, entropy, dh, self.grads[1], self.work, logp_scale=-1.0 / n, entropy_scale=-self.entropy_weight / n)
+            loss.neg_()
+        else:
+            ne.ne_xent_loss(h, self.rows[1], ctx, loss, lse, self.work)
+            ne.ne_xent_grad(h, self.rows[1], ctx, lse, dh, self.grads[1], self.work, scale=1.0 / n)
         ne.ne_embed_grad(src, dh, self.grads[0], self.work)
         self.steps += 1
-        ne.ne_adamw_step(self.opt, self.steps, lr)
+        if self.opt is not None:
+            ne.ne_adamw_step(self.opt, self.steps, lr)
+            return loss
+        for i, table in enumerate(self.tables):
+            ne.ne_muon_step(table, self.grads[i], self.momenta[i], self.work, lr, momentum=self.momentum, weight_decay=self.weight_decay,
+                            scale=0.2 * math.sqrt(max(table.shape)), param_bf16=self.copies[i] if self.copies is not None else None)
         return loss
+
+    def predict(self, nodes: torch.Tensor, k: int = 10):
+        """The k most probable contexts of nodes int32 [n] (CUDA, n <= batch) at the current tables: (ids int32 [n][k], their log probabilities
+        float32 [n][k], the entropies float32 [n]).  A node outside the tables has no answers: -1, minus infinity, 0."""
+        n = int(nodes.numel())
+        if n < 1 or n > self.batch:
+            raise ValueError(f"answers are given for 1 to {self.batch} nodes at a time")
+        if not 1 <= k <= ne.NE_TOP_MAX:
+            raise ValueError(f"k must be 1 to {ne.NE_TOP_MAX}")
+        V, d = self.tables[0].shape
+        dev = self.tables[0].device
+        size = ne.ne_logprob_workspace_bytes(self.batch, V, d, self.h.dtype, k=k)
+        if self.answers_work is None or self.answers_work.numel() < size:
+            self.answers_work = torch.empty(size, dtype=torch.uint8, device=dev)
+        h = self.h[:n]
+        ne.ne_embed_lookup(self.rows[0], nodes, h)
+        ids = torch.empty((n, k), dtype=torch.int32, device=dev)
+        logp, lse, entropy = torch.empty((n, k), device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev)
+        # (the nodes themselves mark the rows that count)
+        ne.ne_logprob(h, self.rows[1], nodes, lse, self.answers_work, entropy=entropy, top_ids=ids, top_logp=logp)
+        return ids, logp, entropy

@@ -96,14 +96,34 @@ def evaluate(tables: ne.Tables, num_nodes: int, all_edges: np.ndarray, test_edge
     return auc(score(tables, test_edges, second_from_context), score(tables, negatives, second_from_context))
 
 
+def hits(tables: ne.Tables, edges: np.ndarray, k: int = 10, batch: int = 8192) -> float:
+    """Share of the edges' ends whose other end is among the k nodes that the full softmax over the context table makes most probable for them
+    (both directions of every edge; nothing is left out of the k, neither the node itself nor neighbours that training has seen)."""
+    dev, V, d = tables.vertex.device, tables.num_nodes, tables.dim
+    e = np.asarray(edges, dtype=np.int64)
+    pairs = torch.from_numpy(np.concatenate([e, e[:, ::-1]]).astype(np.int32)).to(dev)
+    batch = min(batch, int(pairs.shape[0]))
+    work = torch.empty(ne.ne_logprob_workspace_bytes(batch, V, d, torch.float32, k=k), dtype=torch.uint8, device=dev)
+    h, lse = torch.empty((batch, d), device=dev), torch.empty(batch, device=dev)
+    ids, logp = torch.empty((batch, k), dtype=torch.int32, device=dev), torch.empty((batch, k), device=dev)
+    found = torch.zeros((), dtype=torch.int64, device=dev)
+    for s in range(0, int(pairs.shape[0]), batch):
+        src, dst = pairs[s:s + batch, 0].contiguous(), pairs[s:s + batch, 1]
+        n = int(src.numel())
+        ne.ne_embed_lookup(tables.vertex, src, h[:n])
+        ne.ne_logprob(h[:n], tables.context, None, lse[:n], work, top_ids=ids[:n], top_logp=logp[:n])
+        found += (ids[:n] == dst[:, None]).any(dim=1).sum()
+    return float(found) / int(pairs.shape[0])
+
+
 def train(train_edges: np.ndarray, num_nodes: int, dim: int = 64, epochs: int = 3, negatives: int = 5,
           batch: int = 4096, lr0: float = 0.025, walk_length: int = 40, window: int = 5, seed: int = 0,
-          mode: str = "sync", device: str = "cuda:0"):
+          mode: str = "sync", device: str = "cuda:0", optimizer: str = "adamw", entropy_weight: float = 0.0):
     """Embeddings from walks over the training edges: per epoch one walk per node, window pairs shuffled,
     batches of `batch` pairs through ne_train_block (mode "sync", the exact step) or ne_train_block_async
     (mode "async", the per-sample mode), or the walks themselves through ne_train_walks (mode "walks": the exact step on batches of
     whole walks, unshuffled), or SoftmaxTrainer (mode "softmax": the full softmax over all nodes in the place of sampled
-    negatives, AdamW with 32-bit states; lr0 is Adam's), learning rate decaying linearly over the run.  Returns (Tables, Alias); the handles keep
+    negatives, AdamW with 32-bit states, or Muon, as `optimizer` says, and its `entropy_weight`; lr0 is Adam's), learning rate decaying linearly over the run.  Returns (Tables, Alias); the handles keep
     their device tensors alive (tables.vertex, tables.context)."""
     dev = torch.device(device)
     graph = wl.build_graph(num_nodes, torch.from_numpy(np.asarray(train_edges, dtype=np.int64)))
@@ -122,7 +142,7 @@ def train(train_edges: np.ndarray, num_nodes: int, dim: int = 64, epochs: int = 
     if mode == "softmax":
         # as the sampled objective starts, but with context rows that differ: a table of zeros has no gradient towards vertex rows
         context.copy_(vertex[torch.randperm(num_nodes, generator=torch.Generator().manual_seed(seed)).to(dev)])
-        trainer = SoftmaxTrainer(vertex, context, batch, seed=seed)
+        trainer = SoftmaxTrainer(vertex, context, batch, seed=seed, optimizer=optimizer, entropy_weight=entropy_weight)
     if mode == "walks":
         # on-device augmentation: the walks themselves are the input; a batch is as many whole walks as hold
         # about `batch` samples
@@ -177,16 +197,23 @@ def main(argv=None) -> int:
     ap.add_argument("--walk-length", type=int, default=40)
     ap.add_argument("--window", type=int, default=5)
     ap.add_argument("--mode", default="sync", choices=["sync", "walks", "async", "softmax"])
+    ap.add_argument("--optimizer", default="adamw", choices=["adamw", "muon"], help="of mode softmax")
+    ap.add_argument("--entropy-weight", type=float, default=0.0, help="of mode softmax: what is minimised is loss - weight * entropy of the answers")
+    ap.add_argument("--hits", type=int, default=0, metavar="K", help="also report the share of held-out ends among the K most probable nodes (1 to 64)")
     ap.add_argument("--seed", type=int, default=0)
     args = ap.parse_args(argv)
+    if not 0 <= args.hits <= ne.NE_TOP_MAX:
+        ap.error(f"--hits takes 0 to {ne.NE_TOP_MAX}")
     edges, n = read_edge_list(args.edges)
     train_edges, test_edges = split_edges(edges, args.test_fraction, args.seed)
     tables, _alias = train(train_edges, n, dim=args.dim, epochs=args.epochs, negatives=args.negatives, batch=args.batch,
-                           lr0=args.lr, walk_length=args.walk_length, window=args.window, seed=args.seed, mode=args.mode)
+                           lr0=args.lr, walk_length=args.walk_length, window=args.window, seed=args.seed, mode=args.mode,
+                           optimizer=args.optimizer, entropy_weight=args.entropy_weight)
     all_edges = np.concatenate([train_edges, test_edges])
+    more = {f"hits_at_{args.hits}": hits(tables, test_edges, args.hits)} if args.hits else {}
     print(json.dumps({"nodes": n, "train_edges": int(train_edges.shape[0]), "test_edges": int(test_edges.shape[0]),
                       "auc_vertex_context": evaluate(tables, n, all_edges, test_edges, args.seed + 1, True),
-                      "auc_vertex_vertex": evaluate(tables, n, all_edges, test_edges, args.seed + 1, False)}))
+                      "auc_vertex_vertex": evaluate(tables, n, all_edges, test_edges, args.seed + 1, False), **more}))
     return 0
 
 
