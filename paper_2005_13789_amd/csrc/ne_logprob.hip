@@ -17,6 +17,8 @@ namespace {
 // Chunks of table rows.  kWide: 64.  kNarrow: 16, what a lane has of 32 rows of a tile.  kStreamed: 16, a tile of few rows' kernel.
 enum Chunks { kNone, kWide, kNarrow, kStreamed };
 constexpr int chunk_log2(int chunks) { return chunks == kWide ? 6 : 4; }
+constexpr int64_t kLateGroups = 512;
+constexpr int64_t kUngrouped = 1024;                   // chunks that a wavefront looks through
 constexpr int64_t kTeamsOfMany = 512;                  // rows of H up to which sixteen wavefronts look for the answers of each
 constexpr float kNoScore = -1e30f;                     // below all scores: they are bounded by kMostScore
 constexpr float kMostScore = 1e29f;
@@ -93,13 +95,14 @@ __device__ __forceinline__ uint32_t magnitude_bits(const T (&x)[8])
     return bits & (sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu);
 }
 
-template <class T>
-__device__ __forceinline__ void norms_of(const NormArgs& a, uint32_t block, uint32_t blocks, uint32_t* lds)
-{
-    float total = 0.0f, largest = 0.0f;
+// A lane's share of the norms: pieces of a row from column e on, all rows' pieces of one column after the other.
+struct NormShare {
+    float total = 0.0f;
     uint32_t most = 0;
     int at = 0;
-    for_eights(static_cast<const T*>(a.w), a.w_stride, a.num_rows, a.dim, a.dim, block, blocks, [&](int64_t, int e, const T (&x)[8]) {
+    template <class T>
+    __device__ __forceinline__ void see(int e, const T (&x)[8])
+    {
         if (e != at) {
             total += __uint_as_float(most);
             most = 0;
@@ -107,20 +110,34 @@ __device__ __forceinline__ void norms_of(const NormArgs& a, uint32_t block, uint
         }
         float squares = 0.0f;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float y = static_cast<float>(x[q]);
-            squares = fmaf(y, y, squares);
-            if (sizeof(T) == 4) largest = fmaxf(largest, finite_abs(y));
-        }
+        for (int q = 0; q < 8; ++q) squares = fmaf(static_cast<float>(x[q]), static_cast<float>(x[q]), squares);
         if (magnitude_bits(x) && squares < 0x1p-126f) squares = 0x1p-126f;      // (squares of small values may be 0)
         most = max(most, __float_as_uint(squares) & 0x7FFFFFFFu);
+    }
+    // of `width` columns, by all of a workgroup
+    __device__ __forceinline__ void leave(int width, uint32_t* norm, uint32_t* lds)
+    {
+        total += __uint_as_float(most);
+        int lanes = 1;
+        while (lanes < 64 && 8 * lanes < width) lanes *= 2;
+        for (int o = 1; o < lanes; o <<= 1) total += __shfl_xor(total, o, 64);
+        const uint32_t all = block_max_bits(__float_as_uint(total) & 0x7FFFFFFFu, lds);
+        if (threadIdx.x == 0) *norm = all;
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void norms_of(const NormArgs& a, uint32_t block, uint32_t blocks, uint32_t* lds)
+{
+    NormShare share;
+    float largest = 0.0f;
+    for_eights(static_cast<const T*>(a.w), a.w_stride, a.num_rows, a.dim, a.dim, block, blocks, [&](int64_t, int e, const T (&x)[8]) {
+        share.see(e, x);
+        if (sizeof(T) == 4)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) largest = fmaxf(largest, finite_abs(static_cast<float>(x[q])));
     });
-    total += __uint_as_float(most);
-    int lanes = 1;
-    while (lanes < 64 && 8 * lanes < a.dim) lanes *= 2;
-    for (int o = 1; o < lanes; o <<= 1) total += __shfl_xor(total, o, 64);
-    const uint32_t all = block_max_bits(__float_as_uint(total) & 0x7FFFFFFFu, lds);
-    if (threadIdx.x == 0) a.norms[block] = all;
+    share.leave(a.dim, a.norms + block, lds);
     if (sizeof(T) == 2 || !a.amax) return;
     float h = 0.0f;
     for_eights(static_cast<const T*>(a.h), a.h_stride, a.n, a.dim, a.dim, block, blocks, [&](int64_t i, int, const T (&x)[8]) {
@@ -142,11 +159,19 @@ __global__ void __launch_bounds__(kThreads) norms_kernel(NormArgs a)
 }
 
 // bf16: rows of H into stages and the table's norms in one launch, and the table's rows where they cannot be used as they lie.
+template <bool DIRECT>
 __global__ void __launch_bounds__(kThreads) prepare_kernel(PackJobs jobs, NormArgs a)
 {
     __shared__ uint32_t lds[kThreads / 64];
-    if (blockIdx.y == 0) norms_of<bf16_t>(a, blockIdx.x, gridDim.x, lds);
-    else pack_rows<1, kThreads>(jobs.job[blockIdx.y - 1], blockIdx.x, gridDim.x, reinterpret_cast<float*>(lds));
+    if (blockIdx.y == 1) {
+        pack_rows<1, kThreads>(jobs.job[0], blockIdx.x, gridDim.x, reinterpret_cast<float*>(lds));
+    } else if constexpr (DIRECT) {
+        norms_of<bf16_t>(a, blockIdx.x, gridDim.x, lds);
+    } else {
+        NormShare share;
+        pack_rows<1, kThreads>(jobs.job[1], blockIdx.x, gridDim.x, reinterpret_cast<float*>(lds), [&](int e, const auto& x) { share.see(e, x); });
+        share.leave(jobs.job[1].padded, a.norms + blockIdx.x, lds);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -161,9 +186,13 @@ struct TileArgs {
     Softmax* stat;                 // [n][splits]
     float2* best;                  // [n][chunks]
     int64_t chunks;
+    float* group;                  // NULL, or [n][groups]: the best of group_tiles tiles' halves one after the other
+    int64_t groups;
+    uint32_t group_tiles;          // a power of two
     const uint32_t* norms;         // [norm_count]
     uint32_t norm_count;
     uint32_t* norm;
+    uint32_t* late;                // NULL, or a number that becomes 0
 };
 
 template <int P, int W, int KS, int CHUNKS>
@@ -179,14 +208,22 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
         uint32_t all = 0;
         for (uint32_t i = threadIdx.x; i < a.norm_count; i += 64 * W) all = max(all, a.norms[i]);
         all = block_max_bits(all, reinterpret_cast<uint32_t*>(lds));
-        if (threadIdx.x == 0) *a.norm = all;
+        if (threadIdx.x == 0) {
+            *a.norm = all;
+            if (a.late) *a.late = 0;
+        }
         __syncthreads();
     }
     const float factor = score_factor<P>(a.shift), to_log2 = kLog2e * factor;
     Softmax s[2] = {{kNoScore, 0.0f, 0.0f, 0.0f}, {kNoScore, 0.0f, 0.0f, 0.0f}};
+    uint32_t seen = 0;
+    float of_group[2] = {-INFINITY, -INFINITY};
+    const uint32_t tile1 = min(tile0 + per, a.row_tiles);
     const float low = fmaxf(-3e38f, kNoScore / factor);          // (in units of the sums; below all of them)
-    all_scores<P, W, KS>(a.w, a.h, token_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
+    all_scores<P, W, KS>(a.w, a.h, token_tile, 0, tile0, tile1, a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
         const uint32_t row0 = tile_row0 + m0;
+        ++seen;
+        const bool group_ends = CHUNKS != kNone && a.group && ((seen & (a.group_tiles - 1)) == 0 || tile0 + seen == tile1);
         if (row0 + 32 * MT > a.num_rows) {
             const int left = static_cast<int>(a.num_rows - (row0 + lane_row()));     // (the difference is small where both are not)
 #pragma unroll
@@ -230,6 +267,15 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) t = fmaxf(t, acc[im][j][i]);
             }
+            if constexpr (CHUNKS != kNone) {
+                of_group[j] = fmaxf(of_group[j], t);
+                if (group_ends) {
+                    const float both = fmaxf(of_group[j], __shfl_xor(of_group[j], 32, 64));
+                    const uint32_t group = 2 * (split * ((per + a.group_tiles - 1) / a.group_tiles) + (seen - 1) / a.group_tiles) + (m0 ? 1 : 0);
+                    if (lane < 32 && token < a.n) a.group[token * a.groups + group] = both * factor;
+                    of_group[j] = -INFINITY;
+                }
+            }
             const float now = fmaxf(s[j].top, t * to_log2), d = s[j].top - now, e = __builtin_amdgcn_exp2f(d);
             float sum = 0.0f, moment = 0.0f;
 #pragma unroll
@@ -245,6 +291,15 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
             s[j].top = now;
         }
     });
+    if (CHUNKS != kNone && a.group) {      // a split that ends early has no more groups
+        const uint32_t of_split = (per + a.group_tiles - 1) / a.group_tiles;
+        for (uint32_t g = (seen + a.group_tiles - 1) / a.group_tiles; g < of_split; ++g)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t token = static_cast<int64_t>(token_tile) * R + n0 + 32 * j + (lane & 31);
+                if (lane < 32 && token < a.n) a.group[token * a.groups + 2 * (split * of_split + g) + (m0 ? 1 : 0)] = -INFINITY;
+            }
+    }
     // lanes l and l + 32 and the two wavefronts of a column have the same rows of H
     Softmax* shared = reinterpret_cast<Softmax*>(lds);
 #pragma unroll
@@ -424,14 +479,20 @@ struct FinishArgs {
     const int32_t* shift;          // NULL, or powers of two of W and H
     const float2* best;            // [n][chunks]
     int64_t chunks;
+    const float* group;            // NULL, or [n][groups]
+    uint32_t groups, group_tiles, per_split, row_tiles, tile_rows;
+    uint32_t* late;                // NULL, or number of rows that sixteen wavefronts take over, and the rows
     float *logp, *lse, *entropy;   // logp, entropy: NULL where not wanted
     int32_t* top_ids;
     float* top_logp;
 };
 
-// A row of H is a team's: a wavefront where there are many rows (four teams a workgroup, which never wait for one another), or sixteen.
+// A row of H is a team's: a wavefront where there are many rows (four teams a workgroup, which never wait for one another), or sixteen.  Where there are
+// many rows and many chunks, the wavefront does not look through all records: tiles also leave the best of every group of them behind, the threshold
+// follows from these, and only the records of groups that reach it are read (8192 rows of 200 003 x 512: 170 us without groups).
 template <int WAVES> constexpr int threads_of() { return WAVES == 1 ? kThreads : 64 * WAVES; }
-template <int WAVES> constexpr int most_found() { return WAVES == 1 ? 128 : WAVES == 4 ? 512 : 2048; }       // candidates that a team looks at together
+template <int WAVES> constexpr int most_found() { return WAVES == 1 ? 192 : 2048; }       // candidates that a team looks at together
+constexpr uint32_t kMostGroups = 2048, kMostHits = 256;         // groups of a row; those that a wavefront notes
 
 template <int WAVES>
 __device__ __forceinline__ void team_sync()
@@ -449,48 +510,70 @@ struct Team {
     Softmax stats[WAVES];
     float norms[WAVES];
     float maxima[WAVES == 1 ? 1 : 64 * WAVES];
+    uint16_t hits[WAVES == 1 ? kMostHits : 1];         // groups that reach the threshold
     uint32_t count, bits[WAVES];
     float threshold;
 };
 
-// Eight elements of a row, from `at` on; of fewer than eight columns elements one by one, zeros behind them.
-template <class T>
-__device__ __forceinline__ void load_piece(const T* row, int at, int dim, T (&x)[8])
+// Scores of table rows, LANES lanes each, with products and sums in 64 bits, in an order that depends on dim alone.  A row's last piece ends with the row:
+// what it has in common with the piece before it is multiplied with zeros.  FLIGHT rows of a group of lanes are in flight; of their sums a lane passes
+// on half in each exchange, until it has the row that its last bits name.
+template <class T, int FLIGHT, int LANES>
+__device__ __forceinline__ void exact_scores_by(const FinishArgs& a, const T* h, const uint32_t* ids, double* scores, uint32_t count, uint32_t thread, uint32_t threads)
 {
-    if (dim >= 8) __builtin_memcpy(x, row + at, 8 * sizeof(T));
-    else load_eight(row, 0, dim, x);
-}
-
-// Scores of table rows, 16 lanes each, with products and sums in 64 bits, in an order that depends on dim alone.  A row's last piece ends with the row:
-// what it has in common with the piece before it is multiplied with zeros.
-template <class T, int WAVES>
-__device__ __forceinline__ void exact_scores(const FinishArgs& a, const T* h, const uint32_t* ids, double* scores, uint32_t count, uint32_t thread)
-{
-    constexpr uint32_t FLIGHT = WAVES == 1 ? 4 : 2, GROUPS = WAVES * 4;
-    const int lane = thread & 15;
-    for (uint32_t c = (thread >> 4) * FLIGHT; c < count; c += GROUPS * FLIGHT) {
-        double sum[FLIGHT] = {};
+    constexpr int BITS = FLIGHT == 8 ? 3 : FLIGHT == 4 ? 2 : 1;
+    static_assert(1 << BITS == FLIGHT);
+    const int lane = thread % LANES;
+    for (uint32_t c = thread / LANES * FLIGHT; c < count; c += threads / LANES * FLIGHT) {
         const T* row[FLIGHT];
 #pragma unroll
-        for (uint32_t f = 0; f < FLIGHT; ++f) row[f] = static_cast<const T*>(a.w) + static_cast<int64_t>(ids[min(c + f, count - 1)]) * a.w_stride;
-        for (int e = lane * 8; e < a.dim; e += 128) {
-            const int at = max(min(e, a.dim - 8), 0);
+        for (int f = 0; f < FLIGHT; ++f) row[f] = static_cast<const T*>(a.w) + static_cast<int64_t>(ids[min(c + f, count - 1)]) * a.w_stride;
+        double sum[FLIGHT] = {};
+        for (int e = lane * 8; e < a.dim; e += 8 * LANES) {
+            const int at = min(e, a.dim - 8);
             T x[FLIGHT][8], y[8];
-            load_piece(h, at, a.dim, y);
+            __builtin_memcpy(y, h + at, 8 * sizeof(T));
 #pragma unroll
-            for (uint32_t f = 0; f < FLIGHT; ++f) load_piece(row[f], at, a.dim, x[f]);
+            for (int f = 0; f < FLIGHT; ++f) __builtin_memcpy(x[f], row[f] + at, 8 * sizeof(T));
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const double z = at + q >= e ? static_cast<double>(static_cast<float>(y[q])) : 0.0;
 #pragma unroll
-                for (uint32_t f = 0; f < FLIGHT; ++f) sum[f] = fma(static_cast<double>(static_cast<float>(x[f][q])), z, sum[f]);
+                for (int f = 0; f < FLIGHT; ++f) sum[f] = fma(static_cast<double>(static_cast<float>(x[f][q])), z, sum[f]);
+            }
+        }
+        uint32_t which = 0;
+#pragma unroll
+        for (int bit = 0; bit < BITS; ++bit) {
+            const bool upper = lane >> bit & 1;
+            const int half = FLIGHT >> (bit + 1);
+            if (upper) which += half;
+#pragma unroll
+            for (int f = 0; f < half; ++f) {
+                const double mine = upper ? sum[f + half] : sum[f], theirs = upper ? sum[f] : sum[f + half];
+                sum[f] = mine + __shfl_xor(theirs, 1 << bit, 64);
             }
         }
 #pragma unroll
-        for (uint32_t f = 0; f < FLIGHT; ++f) {
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) sum[f] += __shfl_xor(sum[f], o, 16);
-            if (lane == 0 && c + f < count) scores[c + f] = sum[f];
+        for (int o = FLIGHT; o < LANES; o <<= 1) sum[0] += __shfl_xor(sum[0], o, 64);
+        if (lane < FLIGHT && c + which < count) scores[c + which] = sum[0];
+    }
+}
+
+template <class T, int WAVES>
+__device__ __forceinline__ void exact_scores(const FinishArgs& a, const T* h, const uint32_t* ids, double* scores, uint32_t count, uint32_t thread)
+{
+    constexpr int FLIGHT = WAVES == 1 ? 4 : 2;
+    if (a.dim > 256) {
+        exact_scores_by<T, FLIGHT, 64>(a, h, ids, scores, count, thread, 64 * WAVES);
+    } else if (a.dim >= 8) {
+        exact_scores_by<T, FLIGHT, 16>(a, h, ids, scores, count, thread, 64 * WAVES);
+    } else {
+        for (uint32_t c = thread; c < count; c += 64 * WAVES) {
+            const T* row = static_cast<const T*>(a.w) + static_cast<int64_t>(ids[c]) * a.w_stride;
+            double sum = 0.0;
+            for (int e = 0; e < a.dim; ++e) sum = fma(static_cast<double>(static_cast<float>(row[e])), static_cast<double>(static_cast<float>(h[e])), sum);
+            scores[c] = sum;
         }
     }
 }
@@ -542,15 +625,12 @@ __device__ __forceinline__ double log2_of(float top, float sum)
     return static_cast<double>(top) + e + static_cast<double>(log2f(m));
 }
 
+// The answers of row i, by a team.
 template <class T, int WAVES>
-__global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs a)
+__device__ __forceinline__ void answer_row(const FinishArgs& a, Team<WAVES>& team, int64_t i)
 {
-    __shared__ Team<WAVES> teams[threads_of<WAVES>() / 64 / WAVES];
     constexpr uint32_t MOST = most_found<WAVES>(), THREADS = 64 * WAVES;
     const uint32_t thread = threadIdx.x % THREADS, lane = thread & 63, wave = thread >> 6;
-    Team<WAVES>& team = teams[threadIdx.x / THREADS];
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * (threads_of<WAVES>() / THREADS) + threadIdx.x / THREADS;
-    if (i >= a.n) return;
     // (what is loaded first does not wait for the id)
     const T* h = static_cast<const T*>(a.h) + i * a.h_stride;
     const uint32_t id = a.ids ? static_cast<uint32_t>(a.ids[i]) : 0xFFFFFFFFu, k = a.k;
@@ -580,14 +660,10 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
     // the row's norm and softmax, and the table's largest norm
     float squares = 0.0f;
     for (int e = thread * 8; e < a.dim; e += 8 * THREADS) {
-        const int at = max(min(e, a.dim - 8), 0);
         T x[8];
-        load_piece(h, at, a.dim, x);
+        load_eight(h, e, a.dim, x);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float y = at + q >= e ? static_cast<float>(x[q]) : 0.0f;
-            squares = fmaf(y, y, squares);
-        }
+        for (int q = 0; q < 8; ++q) squares = fmaf(static_cast<float>(x[q]), static_cast<float>(x[q]), squares);
         if (magnitude_bits(x) && squares < 0x1p-126f) squares = 0x1p-126f;      // (squares of small values may be 0)
     }
     for (uint32_t p = thread + THREADS; p < a.splits; p += THREADS) {
@@ -658,7 +734,18 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
             mine[0] = fmaxf(mine[0], b[f].x);
         }
     };
-    if (held) {
+    bool grouped = WAVES == 1 && a.group;
+    const float* group = a.group + i * a.groups;
+    if (grouped) {
+        for (uint32_t g0 = 0; g0 < a.groups; g0 += HELD * THREADS) {
+#pragma unroll
+            for (int f = 0; f < HELD; ++f) {
+                const uint32_t g = g0 + thread + f * THREADS;
+                record[f] = make_float2(g < a.groups ? group[g] : -INFINITY, 0.0f);
+            }
+            see(record);
+        }
+    } else if (held) {
         see(record);
     } else {
         for (int64_t c = 0; c < a.chunks; c += HELD * THREADS) {
@@ -667,7 +754,7 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
         }
     }
     float t = -INFINITY;
-    if (a.chunks >= k) {
+    if ((grouped ? a.groups : a.chunks) >= k) {
         if constexpr (WAVES == 1) {
             t = reached_by(mine, k);
         } else {
@@ -685,10 +772,39 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
         }
         t -= 2.0f * off_by + fabsf(t) * 0x1p-15f;
     }
-    // Candidates of chunks c0 .. c1 - 1 go to team.ids[64 ..]: a chunk's best, or all of its rows.  Returns their number, of which those beyond MOST
-    // are not written.
+    // The records to look at: of all chunks, or of the chunks of groups that reach t, one group after the other.
     const int log2_rows = chunk_log2(a.kind);
-    auto collect = [&](int64_t c0, int64_t c1) {
+    const uint32_t per_tile = a.tile_rows >> (log2_rows + 1), per_group = per_tile * a.group_tiles;
+    int64_t records = a.chunks;
+    if constexpr (WAVES == 1) {
+        if (grouped) {
+            uint32_t hits = 0;
+            for (uint32_t g0 = 0; g0 < a.groups; g0 += 64) {
+                const uint32_t g = g0 + lane;
+                const bool hit = g < a.groups && group[g] >= t;
+                const uint64_t mask = __ballot(hit);
+                const uint32_t to = hits + __popcll(mask & ((1ull << lane) - 1));
+                if (hit && to < kMostHits) team.hits[to] = static_cast<uint16_t>(g);
+                hits += __popcll(mask);
+            }
+            if (hits <= kMostHits) records = static_cast<int64_t>(hits) * per_group;
+            else grouped = false;
+            team_sync<WAVES>();
+        }
+    }
+    // (of a group: 2 (its split, its place there) + its half of the tiles)
+    const uint32_t groups_of_split = grouped ? (a.per_split + a.group_tiles - 1) / a.group_tiles : 1;
+    auto chunk_of = [&](int64_t r) -> int64_t {
+        if (!grouped) return r;
+        const uint32_t at = static_cast<uint32_t>(r), group_id = team.hits[at / per_group], in = at % per_group;
+        const uint32_t split = (group_id >> 1) / groups_of_split, tile = split * a.per_split + (group_id >> 1) % groups_of_split * a.group_tiles + in / per_tile;
+        const bool there = tile < min((split + 1) * a.per_split, a.row_tiles);
+        const int64_t first = (static_cast<int64_t>(tile) * a.tile_rows + (group_id & 1) * (a.tile_rows / 2)) >> log2_rows;
+        return there ? first + in % per_tile : a.chunks;
+    };
+    // Candidates of records r0 .. r1 - 1 go to team.ids[64 ..]: a chunk's best, or all of its rows.  Returns their number, of which those beyond MOST
+    // are not written.
+    auto collect = [&](int64_t r0, int64_t r1) {
         uint32_t count = 0;
         if (WAVES > 1) {
             if (thread == 0) team.count = 0;
@@ -713,18 +829,29 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
         auto row_of = [&](uint32_t chunk, uint32_t place) {
             return a.kind == kNarrow ? (chunk >> 1) * 32 + 8 * (place >> 2) + 4 * (chunk & 1) + (place & 3) : (chunk << log2_rows) + place;
         };
-        for (int64_t c = held ? 0 : c0; c < c1; c += HELD * THREADS) {
-            if (!held) load_records<THREADS>(best, c, c1, thread, record);
+        for (int64_t r = held ? 0 : r0; r < r1; r += HELD * THREADS) {
+            uint32_t chunk[HELD];
 #pragma unroll
             for (int f = 0; f < HELD; ++f) {
-                const int64_t mine = c + thread + f * THREADS;
-                const bool reaches = record[f].x >= t && mine >= c0 && mine < c1;
+                const int64_t mine = r + thread + f * THREADS, c = mine >= r0 && mine < r1 ? chunk_of(mine) : a.chunks;
+                chunk[f] = static_cast<uint32_t>(c);
+                if (held) {
+                    if (c >= a.chunks) chunk[f] = 0xFFFFFFFFu;
+                } else {
+                    record[f] = make_float2(-INFINITY, -INFINITY);
+                    if (c < a.chunks) record[f] = best[c];
+                    else chunk[f] = 0xFFFFFFFFu;
+                }
+            }
+#pragma unroll
+            for (int f = 0; f < HELD; ++f) {
+                const bool reaches = chunk[f] != 0xFFFFFFFFu && record[f].x >= t;
                 if (!__any(reaches)) continue;
                 const bool whole = reaches && record[f].y >= t;
-                const uint32_t one = row_of(static_cast<uint32_t>(mine), __float_as_uint(record[f].x) & ((1u << log2_rows) - 1));
+                const uint32_t one = row_of(chunk[f], __float_as_uint(record[f].x) & ((1u << log2_rows) - 1));
                 write(reaches && !whole && one < a.num_rows, one);       // (narrow chunks behind the last row hold nothing)
                 for (uint64_t wholes = __ballot(whole); wholes; wholes &= wholes - 1) {
-                    const uint32_t chunk = __builtin_amdgcn_readlane(static_cast<uint32_t>(mine), __builtin_ctzll(wholes)), row = row_of(chunk, lane);
+                    const uint32_t all = __builtin_amdgcn_readlane(chunk[f], __builtin_ctzll(wholes)), row = row_of(all, lane);
                     write(lane < 1u << log2_rows && row < a.num_rows, row);
                 }
             }
@@ -736,17 +863,22 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
         return count;
     };
     const int64_t part = MOST >> log2_rows;         // chunks whose rows all fit
-    int64_t at = 0, to = 0, span = a.chunks;        // so many chunks at a time that there is room for their candidates
+    int64_t at = 0, to = 0, span = records;         // so many records at a time that there is room for their candidates
     auto next_candidates = [&]() {
         at = to;
         while (true) {
-            to = min(at + span, a.chunks);
+            to = min(at + span, records);
             const uint32_t count = collect(at, to);
             if (count <= MOST) return count;
             span = max(span / 2, part);
         }
     };
     uint32_t count = next_candidates(), have = 0;
+    // A row of many candidates would take one wavefront several times as long as the others: sixteen take it over.
+    if (WAVES == 1 && a.late && count + (records - to) > a.k + (a.kind == kWide ? 40u : 112u)) {
+        if (lane == 0) a.late[1 + atomicAdd(a.late, 1u)] = static_cast<uint32_t>(i);
+        return;
+    }
     bool given = a.logp != nullptr;
     while (true) {
         if (given && thread == 0) team.ids[64 + count] = id;
@@ -757,7 +889,7 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
         given = false;
         // the best so far lie in front of the candidates
         const uint32_t all = have + count, base = 64 - have;
-        const bool last = to >= a.chunks;
+        const bool last = to >= records;
         for (uint32_t c = thread; c < all; c += THREADS) {
             const uint32_t my_id = team.ids[base + c];
             const double my_score = team.scores[base + c];
@@ -804,6 +936,28 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
     }
 }
 
+template <class T, int WAVES>
+__global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs a)
+{
+    constexpr int TEAMS = threads_of<WAVES>() / 64 / WAVES;
+    __shared__ Team<WAVES> teams[TEAMS];
+    const uint32_t which = threadIdx.x / (64 * WAVES);
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * TEAMS + which;
+    if (i < a.n) answer_row<T, WAVES>(a, teams[which], i);
+}
+
+// Rows that wavefronts left, sixteen for each.
+template <class T>
+__global__ void __launch_bounds__(1024) late_answers_kernel(FinishArgs a)
+{
+    __shared__ Team<16> team;
+    const uint32_t count = a.late[0];
+    for (uint32_t r = blockIdx.x; r < count; r += gridDim.x) {
+        answer_row<T, 16>(a, team, a.late[1 + r]);
+        __syncthreads();
+    }
+}
+
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
@@ -811,7 +965,9 @@ struct AnswerWs : Packs {
     uint32_t row_tiles, splits;
     int32_t few_blocks, kind;
     int64_t chunks;
-    uint32_t *norms, *norm;
+    uint32_t groups, group_tiles, per_split;
+    float* group;
+    uint32_t *norms, *norm, *late;
     Softmax* stat;
     float2* best;
     size_t total;
@@ -852,6 +1008,16 @@ AnswerWs answer_layout(int64_t n, int64_t num_rows, int32_t dim, int32_t type, i
     }
     w.stat = take.get<Softmax>(static_cast<size_t>(w.splits) * n);
     w.best = k ? take.get<float2>(static_cast<size_t>(w.chunks) * n) : nullptr;
+    w.late = k && !w.few_blocks && n > kTeamsOfMany ? take.get<uint32_t>(static_cast<size_t>(n) + 1) : nullptr;
+    w.per_split = static_cast<uint32_t>(ceil_div(w.row_tiles, w.splits));
+    if (!w.few_blocks && n > kTeamsOfMany && w.chunks > kUngrouped) {
+        // as large as leaves several times k of them, and at most kMostGroups
+        auto groups = [&](uint32_t tiles) { return static_cast<uint32_t>(2 * w.splits * ceil_div(w.per_split, tiles)); };
+        w.group_tiles = 1;
+        while (w.group_tiles < w.per_split && (groups(w.group_tiles) > kMostGroups || groups(2 * w.group_tiles) >= std::max<uint32_t>(256, 6 * k))) w.group_tiles *= 2;
+        w.groups = groups(w.group_tiles);
+        w.group = take.get<float>(static_cast<size_t>(w.groups) * n);
+    }
     w.total = take.total();
     return w;
 }
@@ -865,6 +1031,7 @@ size_t answer_bytes(int64_t n, int64_t num_rows, int32_t dim, int32_t type, int3
     // shares of few rows; of tiles: as many workgroups as run in four rounds, or one for every tile
     bytes += (std::min<int64_t>(ceil_div(num_rows, 64), kFewGroups) * few + tokens + std::min<int64_t>(ceil_div(num_rows, 128) * tokens, 4 * 512 * 128)) * 16;
     bytes += std::max(chunk_count(num_rows, k ? kStreamed : kNone) * few, chunk_count(num_rows, chunks_of(num_rows, k)) * n) * 8;
+    if (k && n > kTeamsOfMany) bytes += (kMostGroups + 1) * 4 * n;
     if (!few_blocks_of(n, num_rows, dim, parts)) bytes += parts * 2 * padded * (tokens + num_rows);
     return static_cast<size_t>(bytes);
 }
@@ -923,7 +1090,8 @@ hipError_t tile_answers(const SoftmaxCall& x, const AnswerWs& w, hipStream_t st)
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(pack_kernel<2>, dim3(blocks, 2), dim3(kThreads), 0, st, jobs);
     } else {
-        hipLaunchKernelGGL(prepare_kernel, dim3(blocks, direct ? 2 : 3), dim3(kThreads), 0, st, jobs, norms);
+        if (direct) hipLaunchKernelGGL(prepare_kernel<true>, dim3(blocks, 2), dim3(kThreads), 0, st, jobs, norms);
+        else hipLaunchKernelGGL(prepare_kernel<false>, dim3(blocks, 2), dim3(kThreads), 0, st, jobs, norms);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -933,7 +1101,7 @@ hipError_t tile_answers(const SoftmaxCall& x, const AnswerWs& w, hipStream_t st)
     a.h = packed_operand(w.h, w.tokens, w.padded);
     a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles; a.splits = w.splits;
     a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.best = w.best; a.chunks = w.chunks;
-    a.norms = w.norms; a.norm_count = P == 2 ? kAmaxBlocks : blocks; a.norm = w.norm;
+    a.group = w.group; a.groups = w.groups; a.group_tiles = w.group_tiles; a.late = w.late; a.norms = w.norms; a.norm_count = P == 2 ? kAmaxBlocks : blocks; a.norm = w.norm;
     const dim3 grid(static_cast<unsigned>(ceil_div(w.tokens, w.large_scores ? 256 : 128) * w.splits));
     const int held = held_stages(w, w.row_tiles, w.splits, a.steps);
     if (P == 1 && w.large_scores) hipLaunchKernelGGL((answer_tiles_kernel<1, 8, 0, CHUNKS>), grid, dim3(512), 0, st, a);
@@ -987,12 +1155,16 @@ ne_status ne_logprob(const void* h_dev, int64_t h_stride, const void* w_dev, int
     if (e == hipSuccess) {
         const FinishArgs f{h_dev, w_dev, h_stride, w_stride, ids_dev, n, static_cast<uint32_t>(num_rows), w.splits, w.few_blocks ? w.splits : 1,
                            static_cast<uint32_t>(k), dim, w.kind, w.stat, w.few_blocks ? w.norms : w.norm, f32 && !w.few_blocks ? w.shift : nullptr, w.best,
-                           w.chunks, logp_dev, lse_dev, entropy_dev, top_ids_dev, top_logp_dev};
+                           w.chunks, w.group, w.groups, w.group_tiles, w.per_split, w.row_tiles, w.large_scores ? 256u : 128u, w.late, logp_dev, lse_dev, entropy_dev,
+                           top_ids_dev, top_logp_dev};
         auto launch = [&](auto kernel, int64_t groups, int threads) { hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(threads), 0, st, f); };
         if (n <= kTeamsOfMany) f32 ? launch(answers_kernel<float, 16>, n, 1024) : launch(answers_kernel<bf16_t, 16>, n, 1024);
-        else if (w.chunks > 1024) f32 ? launch(answers_kernel<float, 4>, n, kThreads) : launch(answers_kernel<bf16_t, 4>, n, kThreads);
         else f32 ? launch(answers_kernel<float, 1>, ceil_div(n, 4), kThreads) : launch(answers_kernel<bf16_t, 1>, ceil_div(n, 4), kThreads);
         e = hipGetLastError();
+        if (e == hipSuccess && w.late) {
+            f32 ? launch(late_answers_kernel<float>, std::min<int64_t>(n, kLateGroups), 1024) : launch(late_answers_kernel<bf16_t>, std::min<int64_t>(n, kLateGroups), 1024);
+            e = hipGetLastError();
+        }
     }
     if (e != hipSuccess) return fail(NE_ERR_HIP, std::string("log probability launch: ") + hipGetErrorString(e));
     return NE_OK;

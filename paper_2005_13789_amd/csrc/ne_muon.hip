@@ -509,8 +509,10 @@ __global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs a)
         for (int i = 0; i < 4; ++i) a.next[(row0 + quarter * 4 + i) * a.side + c] = fmaf(kC, v2[i], fmaf(kB, v1[i], kA * v[i]));
 }
 
-// Larger sides: a product is a launch, or two that do not wait for one another.  A workgroup has a tile of 32 x 32 on or above the diagonal, its four
-// wavefronts a quarter of the contraction each, straight from L2 into the matrix cores' operands.
+// Larger sides: a product is a launch, or two that do not wait for one another.  A workgroup has a tile of 32 x 32 on or above the diagonal, its eight
+// wavefronts a share of the contraction each, straight from L2 into the matrix cores' operands.
+constexpr int kSmallWaves = 8;
+
 struct SmallJob {
     const float *a, *b;
     float* out;             // NULL: the halves of P, for the product with X
@@ -523,9 +525,10 @@ struct SmallArgs {
     int32_t side;
 };
 
-__global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
+__global__ void __launch_bounds__(64 * kSmallWaves) small_kernel(SmallArgs args)
 {
-    __shared__ __align__(16) float lds[4][32 * 33];
+    constexpr int WAVES = kSmallWaves, EACH = 1024 / (64 * WAVES), ROWS = 2 * WAVES;       // elements of a thread, rows of a turn
+    __shared__ __align__(16) float lds[WAVES][32 * 33];
     const SmallJob& job = args.job[blockIdx.y];
     const uint32_t tiles = args.side / 32;
     uint32_t ti, tj;
@@ -534,21 +537,21 @@ __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
     const float* a = job.a + static_cast<int64_t>(ti * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
     const float* b = job.b + static_cast<int64_t>(tj * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
     // (the polynomial's other term is fetched ahead of the sums)
-    float g[4] = {};
+    float g[EACH] = {};
     if (job.polynomial)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) g[q] = job.a[static_cast<int64_t>(ti * 32 + (threadIdx.x >> 5) + 8 * q) * args.side + tj * 32 + (threadIdx.x & 31)];
+        for (int q = 0; q < EACH; ++q) g[q] = job.a[static_cast<int64_t>(ti * 32 + (threadIdx.x >> 5) + ROWS * q) * args.side + tj * 32 + (threadIdx.x & 31)];
     f32x16 sum, small;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i] = small[i] = 0.0f;
     constexpr int FLIGHT = 4;
-    for (int s0 = wave; s0 < steps; s0 += 4 * FLIGHT) {
+    for (int s0 = wave; s0 < steps; s0 += WAVES * FLIGHT) {
         float x[FLIGHT][8] = {}, y[FLIGHT][8] = {};
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
-            if (s0 + 4 * f >= steps) break;
-            __builtin_memcpy(x[f], a + (s0 + 4 * f) * 16, 32);
-            __builtin_memcpy(y[f], b + (s0 + 4 * f) * 16, 32);
+            if (s0 + WAVES * f >= steps) break;
+            __builtin_memcpy(x[f], a + (s0 + WAVES * f) * 16, 32);
+            __builtin_memcpy(y[f], b + (s0 + WAVES * f) * 16, 32);
         }
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
@@ -568,9 +571,10 @@ __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
     __syncthreads();
     float* all = lds[0];            // the results; on the diagonal those above it are both
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int r = (threadIdx.x >> 5) + 8 * q, c = threadIdx.x & 31, at = r * 33 + c;
+    for (int q = 0; q < EACH; ++q) {
+        const int r = (threadIdx.x >> 5) + ROWS * q, c = threadIdx.x & 31, at = r * 33 + c;
         float x = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
+        x += (lds[4][at] + lds[5][at]) + (lds[6][at] + lds[7][at]);
         if (job.polynomial) x = fmaf(kC, x, kB * g[q]) + (ti == tj && r == c ? kA : 0.0f);
         all[at] = x;                // (read by this thread alone so far)
     }
@@ -581,8 +585,8 @@ __global__ void __launch_bounds__(256) small_kernel(SmallArgs args)
         else put(args.p, row, col, x, kPShift);
     };
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int r = (threadIdx.x >> 5) + 8 * q, c = threadIdx.x & 31;
+    for (int q = 0; q < EACH; ++q) {
+        const int r = (threadIdx.x >> 5) + ROWS * q, c = threadIdx.x & 31;
         if (ti == tj) {
             write(ti, tj, r, c, all[min(r, c) * 33 + max(r, c)]);
         } else {
@@ -759,7 +763,7 @@ hipError_t polynomial(const MuonWs& w, int steps, hipStream_t st)
     int jobs = 0;
     auto add = [&](const float* a, const float* b, float* out, bool poly) { args.job[jobs++] = SmallJob{a, b, out, poly ? 1 : 0}; };
     auto run = [&]() {
-        hipLaunchKernelGGL(small_kernel, dim3(tiles * (tiles + 1) / 2, jobs), dim3(256), 0, st, args);
+        hipLaunchKernelGGL(small_kernel, dim3(tiles * (tiles + 1) / 2, jobs), dim3(64 * kSmallWaves), 0, st, args);
         jobs = 0;
         return hipGetLastError();
     };

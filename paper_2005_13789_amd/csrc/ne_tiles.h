@@ -398,8 +398,9 @@ struct PackJobs {
     PackArgs job[3];
 };
 
-template <int P, int THREADS>
-__device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uint32_t blocks, float* lds)
+// look(e, x): sees every eight elements that are packed, from column e on.
+template <int P, int THREADS, class Look>
+__device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uint32_t blocks, float* lds, Look look)
 {
     typedef typename std::conditional<P == 2, float, bf16_t>::type T;
     int k = 0;
@@ -413,6 +414,7 @@ __device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uin
     float largest = 0.0f;
     auto write = [&](int64_t r, int e0, const T (&x)[8]) {
         s16x8 out[P] = {};
+        look(e0, x);
         const bool counts = !a.targets || static_cast<uint32_t>(a.targets[r]) < a.num_targets;
         const float c = a.c ? a.c[r] : 1.0f;
         if (P == 2 || a.amax) {
@@ -442,6 +444,12 @@ __device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uin
         largest = block_max<THREADS>(largest, lds);
         if (threadIdx.x == 0) a.amax_out[block] = largest;
     }
+}
+
+template <int P, int THREADS>
+__device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uint32_t blocks, float* lds)
+{
+    pack_rows<P, THREADS>(a, block, blocks, lds, [](int, const auto&) {});
 }
 
 template <int P>

@@ -134,6 +134,17 @@ def test_large_tiles(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,d,k", [(513, 40_000, 24, 64), (1500, 70_001, 20, 5), (700, 66_000, 33, 1), (5000, 17_000, 16, 30), (600, 131_073, 8, 12)])
+def test_many_rows_of_large_tables(n, V, d, k, dtype):
+    """Groups of tiles, whose best decide which records are read; splits of the table that end early."""
+    say("groups", n, V, d, k, dtype)
+    h, w, ids = make(n, V, d, dtype, n + k)
+    check(h, w, ids, answers(h, w, ids, k, fill=255), k)
+    w[:] = w[torch.arange(V, device=DEV) % 1000]       # equal rows in many groups
+    check(h[:520], w, ids[:520], answers(h[:520], w, ids[:520], k, fill=127), k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [5, 300])
 def test_equal_scores(n, dtype):
     """Equal rows tie exactly: the lowest ids first, whichever tiles they are in; a table of zeros, and rows of zeros."""
