@@ -685,6 +685,85 @@ __global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
     });
 }
 
+// X P and its G in one pass: up to 128 columns a workgroup has whole rows of X P, turns them into halves in LDS, multiplies them there and writes them
+// from there.  P's rows stay in registers, X travels in a ring of four stages.  (1 M x 128: 345 us, both apart 383.  P of all steps at once, so that X P need not be written, would have
+// values up to 485 where X has no direction, whose roundings would be 485 / 41 times as large in all others.)
+struct NextGramArgs {
+    Operand x, p;           // both by rows (P is symmetric)
+    uint32_t row_tiles, splits;
+    int32_t steps;
+    int64_t padded_tall;
+    const int32_t* shifts;
+    const double* inverse;
+    Halves next;
+    float* part;            // [splits][kSide][kSide]
+};
+
+template <int KS>
+__global__ void __launch_bounds__(256, 1) next_gram_kernel(NextGramArgs a)
+{
+    constexpr int STAGE = operand_bytes<4>();       // 32 rows of X P, both halves
+    __shared__ __align__(16) unsigned char lds[4 * STAGE + 4 * STAGE];
+    unsigned char* rows = lds + 4 * STAGE;
+    const int lane = threadIdx.x & 63, m0 = first_row<4>(), n0 = first_col<4>();
+    const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = blockIdx.x * per;
+    const double inverse = a.shifts ? *a.inverse : 1.0;
+    f32x16 all[2][2];
+    clear(all);
+    all_scores<2, 4, KS>(a.x, a.p, 0, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+#pragma unroll
+        for (int im = 0; im < 2; ++im) {
+            const int64_t row0 = static_cast<int64_t>(tile_row0) + m0 + 32 * im;
+            // (rows behind the last are the last again)
+            const int shift = !a.shifts ? kHalfShift : row0 < a.padded_tall ? a.shifts[row0 / kBlock] : 0;
+            const float factor = static_cast<float>(ldexp(inverse, kHalfShift - (shift + kPShift)));
+            // (column after column, a row of X P along the contraction: four of a lane's values are side by side)
+            unsigned char* stage = rows + ((m0 >> 5) + im) * STAGE;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int col = n0 + 32 * j + (lane & 31);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f16x4 hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = row0 < a.padded_tall ? acc[im][j][4 * q + e] * factor : 0.0f;
+                        hi[e] = static_cast<f16_t>(x);
+                        lo[e] = static_cast<f16_t>(x - static_cast<float>(hi[e]));
+                    }
+                    unsigned char* at = stage + col * 64 + ((q ^ ((col >> 2) & 3)) << 4) + (lane >> 5) * 8;
+                    *reinterpret_cast<f16x4*>(at) = hi;
+                    *reinterpret_cast<f16x4*>(at + STAGE / 2) = lo;
+                    if (row0 >= a.padded_tall || col >= a.next.stride) continue;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t to = (row0 + 8 * q + lane_row() + e) * a.next.stride + col;
+                        const f16_t h = hi[e], l = lo[e];       // (a cast of a vector's element would take the vector's first)
+                        a.next.part[0][to] = __builtin_bit_cast(uint16_t, h);
+                        a.next.part[1][to] = __builtin_bit_cast(uint16_t, l);
+                    }
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (X's next stages travel on)
+        f32x16 g[2][2];
+        clear(g);
+#pragma unroll
+        for (int stage = 0; stage < 4; ++stage) multiply<2, 4, true, true>(rows + stage * STAGE, g, 0);
+#pragma unroll
+        for (int im = 0; im < 2; ++im)
+#pragma unroll
+            for (int in = 0; in < 2; ++in) all[im][in] += g[im][in];
+    });
+    float* out = a.part + static_cast<int64_t>(blockIdx.x) * (kSide * kSide);
+#pragma unroll
+    for (int im = 0; im < 2; ++im)
+#pragma unroll
+        for (int in = 0; in < 2; ++in)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[(m0 + 32 * im + sum_row(i) + lane_row()) * kSide + n0 + 32 * in + (lane & 31)] = all[im][in][i];
+}
+
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
@@ -701,6 +780,13 @@ struct MuonWs {
     Halves p;
     size_t total;
 };
+
+// Workgroups of next_gram_kernel: one a CU.
+uint32_t next_gram_splits(int64_t padded_tall)
+{
+    const int64_t tiles = ceil_div(padded_tall, kSide), per = ceil_div(tiles, 256);
+    return static_cast<uint32_t>(ceil_div(tiles, per));
+}
 
 MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
 {
@@ -726,7 +812,8 @@ MuonWs muon_layout(int64_t rows, int64_t cols, char* base)
         for (auto& p : x.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_tall) * w.padded_side);
         x.stride = w.padded_side;
     }
-    w.part = take.get<float>(static_cast<size_t>(w.splits) * w.pairs * kSide * kSide);
+    const uint32_t most_splits = w.padded_side <= kSide ? std::max(w.splits, next_gram_splits(w.padded_tall)) : w.splits;
+    w.part = take.get<float>(static_cast<size_t>(most_splits) * w.pairs * kSide * kSide);
     for (auto*& m : w.small) m = take.get<float>(static_cast<size_t>(w.padded_side) * w.padded_side);
     for (auto& p : w.p.part) p = take.get<uint16_t>(static_cast<size_t>(w.padded_side) * w.padded_side);
     w.p.stride = w.padded_side;
@@ -842,23 +929,44 @@ hipError_t run_update(PrepArgs u, const MuonWs& w, int steps, const Result& r, h
     else if (kBlock * w.padded_side / 8 <= kPieces * kThreads) hipLaunchKernelGGL((prep_kernel<T, MOMENTUM, true>), grid, dim3(kThreads), 0, st, u);
     else hipLaunchKernelGGL((prep_kernel<T, MOMENTUM, false>), grid, dim3(kThreads), 0, st, u);
     hipError_t e = hipGetLastError();
-    int which = 0, take = 3;            // the first G serves three steps, later ones two
-    for (int left = steps; left > 0 && e == hipSuccess; which ^= 1, take = 2) {
-        const int now = std::min(left, take);
-        const bool first = left == steps;
+    auto join = [&](uint32_t splits, bool first) {
+        const GramJoinArgs j{w.part, w.tiles, splits, w.padded_side, first ? w.split_shift : nullptr, w.inverse, w.small[0]};
+        hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(1024), 0, st, j);
+        return hipGetLastError();
+    };
+    auto gram = [&](const Halves& x, bool first) {
         GramArgs g{};
-        g.x = Operand{{w.x[which].part[0], w.x[which].part[1]}, w.padded_side, static_cast<uint32_t>(w.padded_tall - 1), static_cast<uint32_t>(w.padded_side)};
+        g.x = Operand{{x.part[0], x.part[1]}, w.padded_side, static_cast<uint32_t>(w.padded_tall - 1), static_cast<uint32_t>(w.padded_side)};
         g.tiles = w.tiles; g.splits = w.splits; g.share = w.share; g.stages = w.stages; g.part = w.part;
         g.shifts = w.shifts; g.split_shift = w.split_shift; g.squares = w.squares; g.square_count = grid.x; g.inverse = w.inverse;
         if (first) hipLaunchKernelGGL(gram_kernel<true>, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
         else hipLaunchKernelGGL(gram_kernel<false>, dim3(w.pairs * w.splits), dim3(256), 0, st, g);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        const GramJoinArgs j{w.part, w.tiles, w.splits, w.padded_side, first ? w.split_shift : nullptr, w.inverse, w.small[0]};
-        hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(1024), 0, st, j);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        const hipError_t failed = hipGetLastError();
+        return failed != hipSuccess ? failed : join(w.splits, first);
+    };
+    auto next_gram = [&](const Halves& x, const Halves& next, bool first) {
+        NextGramArgs a{};
+        a.x = packed_operand(x.part, w.padded_tall, w.padded_side);
+        a.p = packed_operand(w.p.part, w.padded_side, w.padded_side);
+        a.row_tiles = static_cast<uint32_t>(ceil_div(w.padded_tall, kSide));
+        a.splits = next_gram_splits(w.padded_tall);
+        a.steps = w.padded_side / step_of<2>();
+        a.padded_tall = w.padded_tall; a.shifts = first ? w.shifts : nullptr; a.inverse = w.inverse; a.next = next; a.part = w.part;
+        if (a.steps > 2) hipLaunchKernelGGL(next_gram_kernel<4>, dim3(a.splits), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(next_gram_kernel<2>, dim3(a.splits), dim3(256), 0, st, a);
+        const hipError_t failed = hipGetLastError();
+        return failed != hipSuccess ? failed : join(a.splits, false);
+    };
+    if (e == hipSuccess) e = gram(w.x[0], true);
+    int which = 0, take = 3;            // the first G serves three steps, later ones two
+    for (int left = steps; left > 0 && e == hipSuccess; which ^= 1, take = 2) {
+        const int now = std::min(left, take);
+        const bool first = left == steps;
         if ((e = polynomial(w, now, st)) != hipSuccess) return e;
         left -= now;
-        e = apply(w, w.x[which], first, left > 0 ? &w.x[which ^ 1] : nullptr, r, st);
+        if (left == 0) e = apply(w, w.x[which], first, nullptr, r, st);
+        else if (w.padded_side <= kSide) e = next_gram(w.x[which], w.x[which ^ 1], first);
+        else if ((e = apply(w, w.x[which], first, &w.x[which ^ 1], r, st)) == hipSuccess) e = gram(w.x[which ^ 1], false);
     }
     return e;
 }
