@@ -19,7 +19,8 @@ enum Chunks { kNone, kWide, kNarrow, kStreamed };
 constexpr int chunk_log2(int chunks) { return chunks == kWide ? 6 : 4; }
 constexpr int64_t kLateGroups = 512;
 constexpr int64_t kUngrouped = 1024;                   // chunks that a wavefront looks through
-constexpr int64_t kTeamsOfMany = 512;                  // rows of H up to which sixteen wavefronts look for the answers of each
+constexpr int64_t kChunksOfFour = 4096;                 // chunks that four wavefronts look through
+constexpr int64_t kTeamsOfMany = 512;                  // rows of H up to which several wavefronts look for the answers of each
 constexpr float kNoScore = -1e30f;                     // below all scores: they are bounded by kMostScore
 constexpr float kMostScore = 1e29f;
 
@@ -487,11 +488,14 @@ struct FinishArgs {
     float* top_logp;
 };
 
-// A row of H is a team's: a wavefront where there are many rows (four teams a workgroup, which never wait for one another), or sixteen.  Where there are
+// A row of H is a team's: a wavefront where there are many rows (four teams a workgroup, which never wait for one another); otherwise four, or sixteen
+// where there are many chunks (one row, 12 501 chunks: 15 us with sixteen; 48 rows, 625 chunks: 10.5 with four, 14.5 with sixteen).  Where there are
 // many rows and many chunks, the wavefront does not look through all records: tiles also leave the best of every group of them behind, the threshold
-// follows from these, and only the records of groups that reach it are read (8192 rows of 200 003 x 512: 170 us without groups).
+// follows from these, and only the records of groups that reach it are read.  Rows of many candidates are left to sixteen wavefronts, as the launch would
+// wait for them (8192 rows of 200 003 x 512, k = 16: 170 us with neither, 52 and 58 with both).
+// Bound by chains of dependent loads (records, rows of the table) and by instructions, not by memory.
 template <int WAVES> constexpr int threads_of() { return WAVES == 1 ? kThreads : 64 * WAVES; }
-template <int WAVES> constexpr int most_found() { return WAVES == 1 ? 192 : 2048; }       // candidates that a team looks at together
+template <int WAVES> constexpr int most_found() { return WAVES == 1 ? 192 : WAVES == 4 ? 1024 : 2048; }       // candidates that a team looks at together
 constexpr uint32_t kMostGroups = 2048, kMostHits = 256;         // groups of a row; those that a wavefront notes
 
 template <int WAVES>
@@ -1158,7 +1162,8 @@ ne_status ne_logprob(const void* h_dev, int64_t h_stride, const void* w_dev, int
                            w.chunks, w.group, w.groups, w.group_tiles, w.per_split, w.row_tiles, w.large_scores ? 256u : 128u, w.late, logp_dev, lse_dev, entropy_dev,
                            top_ids_dev, top_logp_dev};
         auto launch = [&](auto kernel, int64_t groups, int threads) { hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(threads), 0, st, f); };
-        if (n <= kTeamsOfMany) f32 ? launch(answers_kernel<float, 16>, n, 1024) : launch(answers_kernel<bf16_t, 16>, n, 1024);
+        if (n <= kTeamsOfMany && w.chunks <= kChunksOfFour) f32 ? launch(answers_kernel<float, 4>, n, 256) : launch(answers_kernel<bf16_t, 4>, n, 256);
+        else if (n <= kTeamsOfMany) f32 ? launch(answers_kernel<float, 16>, n, 1024) : launch(answers_kernel<bf16_t, 16>, n, 1024);
         else f32 ? launch(answers_kernel<float, 1>, ceil_div(n, 4), kThreads) : launch(answers_kernel<bf16_t, 1>, ceil_div(n, 4), kThreads);
         e = hipGetLastError();
         if (e == hipSuccess && w.late) {

@@ -341,10 +341,11 @@ struct GramJoinArgs {
     float* g;               // [side][side]
 };
 
-// 64 elements of a row of a tile pair, whose splits sixteen wavefronts share.
-__global__ void __launch_bounds__(1024) gram_join_kernel(GramJoinArgs a)
+// 64 elements of a row of a tile pair, whose splits the wavefronts share: sixteen of them, or four where there are few.
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) gram_join_kernel(GramJoinArgs a)
 {
-    __shared__ double lds[1024];
+    __shared__ double lds[64 * WAVES];
     const uint32_t pairs = a.tiles * (a.tiles + 1) / 2, per = kSide * kSide / 64, pair = blockIdx.x / per, at = (blockIdx.x % per) * 64 + (threadIdx.x & 63);
     uint32_t ti, tj;
     pair_at(pair, a.tiles, ti, tj);
@@ -353,12 +354,12 @@ __global__ void __launch_bounds__(1024) gram_join_kernel(GramJoinArgs a)
     double sum = 0.0;
     const float* from = a.part + static_cast<int64_t>(pair) * (kSide * kSide) + at;
     constexpr int FLIGHT = 8;
-    for (uint32_t s0 = threadIdx.x >> 6; s0 < a.splits; s0 += 16 * FLIGHT) {
+    for (uint32_t s0 = threadIdx.x >> 6; s0 < a.splits; s0 += WAVES * FLIGHT) {
         float x[FLIGHT];
         int shift[FLIGHT];
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
-            const uint32_t s = s0 + 16 * f;
+            const uint32_t s = s0 + WAVES * f;
             x[f] = 0.0f;
             shift[f] = kHalfShift;
             if (s >= a.splits) continue;
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(1024) gram_join_kernel(GramJoinArgs a)
     if (threadIdx.x >= 64 || col >= a.side || row > col) return;
     sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) sum += lds[w * 64 + threadIdx.x];
+    for (int w = 0; w < WAVES; ++w) sum += lds[w * 64 + threadIdx.x];
     if (a.split_shift) sum = sum * *a.inverse * *a.inverse;
     a.g[row * a.side + col] = a.g[col * a.side + row] = static_cast<float>(sum);
 }
@@ -931,7 +932,9 @@ hipError_t run_update(PrepArgs u, const MuonWs& w, int steps, const Result& r, h
     hipError_t e = hipGetLastError();
     auto join = [&](uint32_t splits, bool first) {
         const GramJoinArgs j{w.part, w.tiles, splits, w.padded_side, first ? w.split_shift : nullptr, w.inverse, w.small[0]};
-        hipLaunchKernelGGL(gram_join_kernel, dim3(w.pairs * (kSide * kSide / 64)), dim3(1024), 0, st, j);
+        const dim3 blocks(w.pairs * (kSide * kSide / 64));
+        if (splits <= 64) hipLaunchKernelGGL(gram_join_kernel<4>, blocks, dim3(256), 0, st, j);
+        else hipLaunchKernelGGL(gram_join_kernel<16>, blocks, dim3(1024), 0, st, j);
         return hipGetLastError();
     };
     auto gram = [&](const Halves& x, bool first) {
