@@ -1,0 +1,166 @@
+"""Answers, their gradients and Newton-Schulz updates where offsets pass 32 bits, and updates of the largest sides, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2005_13789_amd as ne
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+A, B, C = 3.4445, -4.7750, 2.0315
+LONG = {torch.bfloat16: (17_000_003, 136), torch.float32: (9_000_001, 256)}        # more than 2^31 elements, 2^32 bytes
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+@pytest.mark.parametrize("n,dtype", [(3, torch.bfloat16), (3, torch.float32), (600, torch.bfloat16), (600, torch.float32), (2100, torch.bfloat16)])
+def test_long_tables(n, dtype):
+    say("long table", n, dtype)
+    V, d = LONG[dtype]
+    k, piece, u = 5, 250_000, 2.0 ** -24
+    torch.manual_seed(n)
+    w = torch.empty(V, d, dtype=dtype, device=DEV).normal_(std=d ** -0.25)
+    h = torch.empty(n, d, dtype=dtype, device=DEV).normal_(std=d ** -0.25)
+    w[-2:] *= 3                                         # the last rows are among the answers, or far below them
+    ids = torch.randint(0, V, (n,), device=DEV, dtype=torch.int32)
+    ids[0], ids[-1] = V - 1, V
+    ok = ids < V
+    lse, logp, entropy, top_logp = (torch.full(s, float("nan"), device=DEV) for s in ((n,), (n,), (n,), (n, k)))
+    top = torch.full((n, k), -7, dtype=torch.int32, device=DEV)
+    work = torch.empty(ne.ne_logprob_workspace_bytes(n, V, d, dtype, k=k), dtype=torch.uint8, device=DEV)
+    ne.ne_logprob(h, w, ids, lse, work, logp=logp, entropy=entropy, top_ids=top, top_logp=top_logp)
+    del work
+    say("answered")
+    H = h.double() * ok[:, None]
+    z = torch.full((n,), -math.inf, dtype=torch.float64, device=DEV)
+    most, terms = torch.zeros_like(z), torch.zeros_like(z)
+    best, best_ids = torch.empty(n, 0, dtype=torch.float64, device=DEV), torch.empty(n, 0, dtype=torch.int64, device=DEV)
+    for v in range(0, V, piece):
+        W = w[v:v + piece].double()
+        S = H @ W.t()
+        z = torch.logaddexp(z, torch.logsumexp(S, 1))
+        most, terms = torch.maximum(most, S.abs().amax(1)), torch.maximum(terms, (H.abs() @ W.abs().t()).amax(1))
+        x, i = S.topk(min(k, S.shape[1]), dim=1)
+        x, i = torch.cat([best, x], 1), torch.cat([best_ids, i + v], 1)
+        best, order = x.topk(k, dim=1)
+        best_ids = i.gather(1, order)
+    # a score's error and that of a sum of V terms in pieces, as a sum of d products in fp32 has them
+    tol = 2 * u * ((2 * d + 32) * terms + 4 * (most + z.abs() + 1)) + u * (V / 64 + 64)
+    given = (H * w[ids.clamp(0, V - 1).long()].double()).sum(1) - z
+    assert bool(((lse.double() - z).abs() <= tol)[ok].all()) and bool(((logp.double() - given).abs() <= tol + u * given.abs())[ok].all())
+    assert torch.equal(top[ok].long(), best_ids[ok])
+    assert bool(((top_logp.double() - (best - z[:, None])).abs() <= tol[:, None] + u * (best - z[:, None]).abs())[ok].all())
+    assert bool((top[~ok] == -1).all()) and bool((lse[~ok] == 0).all()) and bool((entropy[~ok] == 0).all())
+    E, mean = torch.zeros_like(z), torch.zeros_like(z)
+    for v in range(0, V, piece):
+        L = H @ w[v:v + piece].double().t() - z[:, None]
+        p = torch.exp(L)
+        E -= (p * L).sum(1)
+        mean += (p * L.abs()).sum(1)
+    tol_e = 2 * tol * (2 + mean) + u * (V / 64 + 64) * (1 + E)
+    assert bool(((entropy.double() - E).abs() <= tol_e)[ok].all())
+    if n > 600:
+        return
+    say("gradients")
+    dw = torch.full((V, d), float("nan"), dtype=dtype, device=DEV)
+    work = torch.empty(ne.ne_logprob_workspace_bytes(n, V, d, dtype, grad=True), dtype=torch.uint8, device=DEV)
+    l, e = 1.0, -0.25
+    ne.ne_logprob_grad(h, w, ids, lse, entropy, None, dw, work, logp_scale=l, entropy_scale=e)
+    op = U[dtype] if dtype == torch.bfloat16 else 2.0 ** -22
+    for v in sorted({0, 2 ** 31 // d - 500, 2 ** 32 // (d * dtype.itemsize) - 500, V - 1000}):
+        L = H @ w[v:v + 1000].double().t() - z[:, None]
+        p = torch.exp(L)
+        hot = (ids[:, None] == torch.arange(v, v + 1000, device=DEV)[None, :]).double()
+        G = (l * (hot - p) - e * p * (L + E[:, None])) * ok[:, None]
+        parts = abs(l) + abs(e) * (L.abs() + E[:, None] + 10)
+        err = (p * ((2 * tol + 8 * u)[:, None] * parts + abs(e) * (2 * tol + tol_e)[:, None]) + op * G.abs() + 2.0 ** -38 * (abs(l) + 8 * abs(e))) * ok[:, None]
+        want = G.t() @ H
+        t = 1.01 * (err.t() @ H.abs() + ((2 * n + 64) * u + 2.0 ** -22) * (G.abs().t() @ H.abs()))
+        t = t + U[dtype] * (want.abs() + t) + 1e-30
+        assert bool(((dw[v:v + 1000].double() - want).abs() <= t).all()), v
+
+
+def settled(s, steps):
+    for _ in range(steps):
+        s = (A * s + B * s ** 3 + C * s ** 5).abs()
+    return s
+
+
+def tolerance(g, steps=5):
+    """From x^T x in 64 bits: a product is off by eta = 4 2^-22 of the norms of its operands, four of them a step; G's error changes a direction of singular value
+    s by eta (1 + s_max^2 / s^2) of itself as long as a G serves (three steps, then two), and a step after that multiplies what there is by 3 at most."""
+    s = torch.linalg.eigvalsh(g.cpu()).clamp(min=0).sqrt()
+    s = s / torch.linalg.vector_norm(s)
+    eta, at = 4 * 2.0 ** -22, s.clone()
+    total = 12 * eta * (1 + at.max() ** 2 / at.clamp(min=1e-12) ** 2)
+    at = settled(at, 3)
+    total = 9 * total + 8 * eta * (1 + at.max() ** 2 / at.clamp(min=1e-12) ** 2)
+    at = settled(at, 2)
+    return float(torch.linalg.vector_norm(total.clamp(max=2.0) * at) / torch.linalg.vector_norm(at))
+
+
+def polynomial(g, steps=5):
+    """P with orthogonalized x = x P, from x^T x in 64 bits."""
+    one = torch.eye(g.shape[0], dtype=torch.float64, device=g.device)
+    norm = g.diagonal().sum().sqrt()
+    g, p = g / norm ** 2, one / norm
+    for _ in range(steps):
+        q = A * one + B * g + C * (g @ g)
+        p, g = p @ q, q @ g @ q
+    return p
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_long_updates(wide):
+    """More than 2^32 elements, in place."""
+    say("long update", wide)
+    tall, side, piece = 70_000_001, 63, 1_000_000
+    torch.manual_seed(5)
+    x = torch.empty((side, tall) if wide else (tall, side), dtype=torch.bfloat16, device=DEV).normal_()
+    by_rows = x.t() if wide else x
+    g = torch.zeros(side, side, dtype=torch.float64, device=DEV)
+    for r in range(0, tall, piece):
+        y = by_rows[r:r + piece].double().contiguous()
+        g += y.t() @ y
+    p = polynomial(g)
+    places = [0, 2 ** 31 // side - 500, 2 ** 32 // side - 500, tall - 1000]
+    want = [by_rows[r:r + 1000].double() @ p for r in places]
+    work = torch.empty(ne.ne_orthogonalize_workspace_bytes(*x.shape), dtype=torch.uint8, device=DEV)
+    ne.ne_orthogonalize(x, x, work)
+    # (a direction's error is its share of all rows': of a thousand of them, twice that)
+    tol = 2 * tolerance(g) + U[torch.bfloat16]
+    for r, y in zip(places, want):
+        assert float((by_rows[r:r + 1000].double() - y).norm() / y.norm()) <= tol, r
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(1500, 2048), (4500, 4096), (4096, 4096)])
+def test_largest_sides(rows, cols, dtype):
+    say("largest sides", rows, cols, dtype)
+    torch.manual_seed(rows)
+    x = torch.empty(rows, cols, device=DEV).normal_().to(dtype)
+    y = x.double() if rows >= cols else x.double().t().contiguous()
+    g = y.t() @ y
+    tol = tolerance(g) + 2.0 ** -24
+    say("tolerance", tol)
+    y = y / y.norm()
+    for _ in range(5):
+        g = y.t() @ y
+        y = A * y + y @ (B * g + C * (g @ g))
+    out = torch.full((rows, cols), float("nan"), device=DEV)
+    work = torch.empty(ne.ne_orthogonalize_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV).fill_(255)
+    ne.ne_orthogonalize(x, out, work)
+    err = float(((out if rows >= cols else out.t()).double() - y).norm() / y.norm())
+    say("error", err)
+    assert err <= tol
+
+
+def test_sides_beyond_the_largest_are_refused():
+    assert ne.ne_orthogonalize_workspace_bytes(4097, 4097) == 0 and ne.ne_orthogonalize_workspace_bytes(4096, 5000) > 0
+    x = torch.zeros(4097, 4097, device=DEV)
+    with pytest.raises(ne.NeError):
+        ne.ne_orthogonalize(x, x, torch.empty(1 << 20, dtype=torch.uint8, device=DEV))
