@@ -414,12 +414,13 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
  *   logp_dev     : NULL, or device, float[n] (needs ids).       entropy_dev : NULL, or device, float[n].
  *   lse_dev      : device, float[n].
  *   k            : 0 <= k <= NE_TOP_MAX; k > 0: top_ids_dev int32[n][k] and top_logp_dev float[n][k].
- *   workspace_dev : at least ne_logprob_workspace_bytes(n, num_rows, dim, type, k, 0) bytes, which grow with n and with k from 0 to 1: 8 bytes for
- *                   every 64 rows of w and row of h (for every 16 where n is small) with k > 0, and as for ne_xent_loss.
+ *   workspace_dev : at least ne_logprob_workspace_bytes(n, num_rows, dim, type, k, 0) bytes, which do not shrink as n grows, but may as k
+ *                   does: with k > 0 8 bytes for every 64 rows of w and row of h (for every 16 where n is small, or 320 k^2 more than num_rows), up to
+ *                   8 KB for a row of h, and as for ne_xent_loss.
  * Precision.  lse and entropy as ne_xent_loss has its lse.  Log probabilities are a score with products and sums in 64 bits less lse, and ids
  * are ordered by such scores: which ids are answered, and in which order, depends on the values of h and w alone.
- * A value in a row of h that is not finite makes that row's lse, logp, entropy and top_logp NaN and its top_ids -1; one in w all rows', as do norms of rows
- * (a bound of them) whose product is 1e29 or more.
+ * A value in a row of h that is not finite, or a norm of 2^63 or more, makes that row's lse, logp, entropy and top_logp NaN and its top_ids -1; one in
+ * w all rows', as do norms of rows (a bound of them) whose product is 1e29 or more.
  * ne_logprob_grad gives the gradients of  sum_i logp_scale * logp_grad[i] * logp[i] + entropy_scale * entropy_grad[i] * entropy[i],
  *   dh = G . W and dw = G^T . H,  G_iv = l_i ([v == id[i]] - p_iv) - e_i p_iv (s_iv - lse[i] + entropy[i]),
  * written whole (rows that have no answers: dh 0).  Both have the type of h and w; one of them may be NULL.
@@ -494,7 +495,7 @@ void ne_destroy_adamw(ne_adamw* opt);
  *                    type and stride), and must not overlap it otherwise.
  *   steps          : 1 .. NE_ORTHOGONAL_MAX_STEPS.
  *   workspace_dev  : at least ne_orthogonalize_workspace_bytes(rows, cols) bytes (0 there = invalid arguments or an empty matrix): 8 bytes an element
- *                    and up to 33 MB for sums.
+ *                    (sides up to multiples of 32), 28 for each of the smaller side's square, and up to 65 MB for sums.
  * Precision: products of operands with 22 bits, fp32 sums, the norm and the sums of G's parts in 64 bits: as far from the values in 64 bits as the same
  * products one after the other in fp32.  Elements below 2^-16 of the largest keep 2^-38 of it.  A value that is not finite makes the result NaN.
  *   0 <= rows, cols; max(rows, cols) < 2^31 - 128, min(rows, cols) <= NE_ORTHOGONAL_MAX_SIDE.  An empty matrix is a no-op.

@@ -30,7 +30,7 @@ struct Halves {
     int64_t stride;
 };
 
-
+// ---------------------------------------------------------------------------------------------
 // momentum, norm, X's first halves
 // ---------------------------------------------------------------------------------------------
 // Every 32 rows of X (a stage of G's contraction) have a power of two of their own, which their largest magnitude sets, so that one pass is enough: the
