@@ -659,18 +659,19 @@ __device__ __forceinline__ void finish(const ApplyArgs& a, int64_t row, int col,
         if (row + sum_row(i) < a.tall) a.copy[copy_first + sum_row(i) * copy_step] = static_cast<bf16_t>(p[i]);
 }
 
-template <int KS, Last L, bool WIDE>
-__global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
+template <int W, int KS, Last L, bool WIDE>
+__global__ void __launch_bounds__(64 * W, 2) apply_kernel(ApplyArgs a)
 {
-    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<4>()];
-    const int lane = threadIdx.x & 63, m0 = first_row<4>(), n0 = first_col<4>();
+    __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
+    constexpr int MT = W / 2;
+    const int lane = threadIdx.x & 63, m0 = first_row<W>(), n0 = first_col<W>();
     uint32_t col_tile, split;
     pair_of(by_xcd(blockIdx.x, gridDim.x), a.col_tiles, a.splits, col_tile, split);
     const uint32_t per = (a.row_tiles + a.splits - 1) / a.splits, tile0 = split * per;
     const double inverse = a.shifts ? *a.inverse : 1.0;
-    all_scores<2, 4, KS>(a.x, a.p, col_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[2][2]) {
+    all_scores<2, W, KS>(a.x, a.p, col_tile, 0, tile0, min(tile0 + per, a.row_tiles), a.steps, lds, [&](uint32_t tile_row0, f32x16 (&acc)[MT][2]) {
 #pragma unroll
-        for (int im = 0; im < 2; ++im) {
+        for (int im = 0; im < MT; ++im) {
             const int64_t row0 = static_cast<int64_t>(tile_row0) + m0 + 32 * im;
             if (row0 >= a.padded_tall) continue;
             const int shift = a.shifts ? a.shifts[row0 / kBlock] : kHalfShift;
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(256, 2) apply_kernel(ApplyArgs a)
                 float x[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = acc[im][j][i] * factor;
-                finish<L, WIDE>(a, row0 + lane_row(), col_tile * kSide + n0 + 32 * j + (lane & 31), x);
+                finish<L, WIDE>(a, row0 + lane_row(), col_tile * rows_of<W>() + n0 + 32 * j + (lane & 31), x);
             }
         }
     });
@@ -887,16 +888,16 @@ struct Result {
     float keep, step;
 };
 
-template <int KS>
+template <int W, int KS>
 void launch_apply(const ApplyArgs& a, Last kind, bool wide, dim3 grid, hipStream_t st)
 {
-    if (kind == kNext) hipLaunchKernelGGL((apply_kernel<KS, kNext, false>), grid, dim3(256), 0, st, a);
-    else if (kind == kFloat && !wide) hipLaunchKernelGGL((apply_kernel<KS, kFloat, false>), grid, dim3(256), 0, st, a);
-    else if (kind == kFloat) hipLaunchKernelGGL((apply_kernel<KS, kFloat, true>), grid, dim3(256), 0, st, a);
-    else if (kind == kBfloat && !wide) hipLaunchKernelGGL((apply_kernel<KS, kBfloat, false>), grid, dim3(256), 0, st, a);
-    else if (kind == kBfloat) hipLaunchKernelGGL((apply_kernel<KS, kBfloat, true>), grid, dim3(256), 0, st, a);
-    else if (!wide) hipLaunchKernelGGL((apply_kernel<KS, kParam, false>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((apply_kernel<KS, kParam, true>), grid, dim3(256), 0, st, a);
+    if (kind == kNext) hipLaunchKernelGGL((apply_kernel<W, KS, kNext, false>), grid, dim3(64 * W), 0, st, a);
+    else if (kind == kFloat && !wide) hipLaunchKernelGGL((apply_kernel<W, KS, kFloat, false>), grid, dim3(64 * W), 0, st, a);
+    else if (kind == kFloat) hipLaunchKernelGGL((apply_kernel<W, KS, kFloat, true>), grid, dim3(64 * W), 0, st, a);
+    else if (kind == kBfloat && !wide) hipLaunchKernelGGL((apply_kernel<W, KS, kBfloat, false>), grid, dim3(64 * W), 0, st, a);
+    else if (kind == kBfloat) hipLaunchKernelGGL((apply_kernel<W, KS, kBfloat, true>), grid, dim3(64 * W), 0, st, a);
+    else if (!wide) hipLaunchKernelGGL((apply_kernel<W, KS, kParam, false>), grid, dim3(64 * W), 0, st, a);
+    else hipLaunchKernelGGL((apply_kernel<W, KS, kParam, true>), grid, dim3(64 * W), 0, st, a);
 }
 
 hipError_t apply(const MuonWs& w, const Halves& x, bool first, const Halves* next, const Result& r, hipStream_t st)
@@ -904,9 +905,11 @@ hipError_t apply(const MuonWs& w, const Halves& x, bool first, const Halves* nex
     ApplyArgs a{};
     a.x = packed_operand(x.part, w.padded_tall, w.padded_side);     // (X's rows of zeros stay such)
     a.p = packed_operand(w.p.part, w.padded_side, w.padded_side);
-    a.row_tiles = static_cast<uint32_t>(ceil_div(w.tall, kSide));
-    a.col_tiles = w.tiles;
-    a.splits = splits_of(a.row_tiles, a.col_tiles, false);
+    const bool large = w.padded_side > 256 && round_up(w.padded_side, 256) * 8 <= w.padded_side * 9 && ceil_div(w.tall, 256) * ceil_div(w.padded_side, 256) >= 256;
+    const int64_t tile = large ? 256 : kSide;
+    a.row_tiles = static_cast<uint32_t>(ceil_div(w.tall, tile));
+    a.col_tiles = static_cast<uint32_t>(ceil_div(w.padded_side, tile));
+    a.splits = splits_of(a.row_tiles, a.col_tiles, large);
     a.steps = w.padded_side / step_of<2>();
     a.tall = w.tall; a.padded_tall = w.padded_tall; a.small = w.side; a.padded_small = w.padded_side; a.shifts = first ? w.shifts : nullptr; a.inverse = w.inverse;
     if (next) a.next = *next;
@@ -915,9 +918,10 @@ hipError_t apply(const MuonWs& w, const Halves& x, bool first, const Halves* nex
     const Last kind = next ? kNext : r.kind;
     const dim3 grid(a.col_tiles * a.splits);
     const int held = a.steps > 4 || ceil_div(a.row_tiles, a.splits) < 3 ? 0 : a.steps > 2 ? 4 : 2;
-    if (held == 0) launch_apply<0>(a, kind, w.wide, grid, st);
-    else if (held == 2) launch_apply<2>(a, kind, w.wide, grid, st);
-    else launch_apply<4>(a, kind, w.wide, grid, st);
+    if (large) launch_apply<8, 0>(a, kind, w.wide, grid, st);
+    else if (held == 0) launch_apply<4, 0>(a, kind, w.wide, grid, st);
+    else if (held == 2) launch_apply<4, 2>(a, kind, w.wide, grid, st);
+    else launch_apply<4, 4>(a, kind, w.wide, grid, st);
     return hipGetLastError();
 }
 
