@@ -153,6 +153,7 @@ __device__ __forceinline__ void norms_of(const NormArgs& a, uint32_t block, uint
     }
 }
 
+// (10 007 rows against 10 000, 100 columns fp32, 8 MB: 7 us, mostly a launch's.)
 __global__ void __launch_bounds__(kThreads) norms_kernel(NormArgs a)
 {
     __shared__ uint32_t lds[kThreads / 64];
@@ -160,6 +161,7 @@ __global__ void __launch_bounds__(kThreads) norms_kernel(NormArgs a)
 }
 
 // bf16: rows of H into stages and the table's norms in one launch, and the table's rows where they cannot be used as they lie.
+// (Bound by memory: 200 003 x 512 as it lies, 205 MB: 60 us with 8192 rows of H; 199 879 x 438 packed with its norms: 96, 172 as two passes.)
 template <bool DIRECT>
 __global__ void __launch_bounds__(kThreads) prepare_kernel(PackJobs jobs, NormArgs a)
 {
@@ -196,6 +198,10 @@ struct TileArgs {
     uint32_t* late;                // NULL, or a number that becomes 0
 };
 
+// Tiles, stages and operands are the cross entropy's; a workgroup keeps a tile of H's rows and goes through its split of the table.  What is added to
+// a score there, for the moment one multiply-add, for records two instructions, runs on the vector units beside the matrix cores, and is why these wait:
+// 8192 rows against 200 003 x 512 bf16, k = 16: 1840 to 2010 us, 0.83 to 0.91 PFLOP/s (k = 0: 1690); 10 007 against 10 000 x 100 fp32: 112 (the loss 100).
+// Chunks of 64 rows take an exchange between lanes a chunk; those of 16 are a lane's own, four times as many records (80 MB of 8 bytes there).
 template <int P, int W, int KS, int CHUNKS>
 __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
 {
@@ -322,7 +328,8 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
 // few rows of H: the table streams through registers once, straight from memory
 // ---------------------------------------------------------------------------------------------
 // As for the cross entropy's loss: a wavefront has 16 table rows at a time, as the matrix cores' first operand; H lies in LDS as second operands, in
-// blocks of 16 rows; fp32 operands are split into three bf16 parts.
+// blocks of 16 rows; fp32 operands are split into three bf16 parts.  Bound by reading the table: 200 003 x 256 bf16 for one row 21 us, 4.9 TB/s; fp32 for 16 rows
+// 40 to 52 us, 3.9 to 5.1 TB/s.
 struct FewAnswerArgs {
     const void *h, *w;
     int64_t h_stride, w_stride;
@@ -950,7 +957,8 @@ __global__ void __launch_bounds__(threads_of<WAVES>()) answers_kernel(FinishArgs
     if (i < a.n) answer_row<T, WAVES>(a, teams[which], i);
 }
 
-// Rows that wavefronts left, sixteen for each.
+// Rows that wavefronts left, sixteen for each: a workgroup's LDS leaves room for one on a CU, and 512 workgroups share all rows.  (8192 rows of 200 003 x 512: 58 us;
+// with no row left, 4.)
 template <class T>
 __global__ void __launch_bounds__(1024) late_answers_kernel(FinishArgs a)
 {

@@ -93,7 +93,9 @@ __device__ __forceinline__ int block_shift(float top, int32_t* shifts, int64_t b
     return shift;
 }
 
-// (HELD: a thread's pieces stay in registers; otherwise they are read again.)
+// Bound by memory: with momentum every element is 4 bytes of momentum read and 4 written, 4 of X's halves written, and the gradient's (1 M x 128 fp32: 372 us,
+// 5.5 TB/s; 200 003 x 512 bf16: 300).  HELD: a thread's pieces stay in registers from the first look to the halves; otherwise, beyond 512 columns, they are
+// read again, from L2.
 template <class T, bool MOMENTUM, bool HELD>
 __global__ void __launch_bounds__(kThreads) prep_kernel(PrepArgs a)
 {
@@ -247,6 +249,9 @@ __device__ __forceinline__ void pair_at(uint32_t p, uint32_t tiles, uint32_t& i,
     j = i + p;
 }
 
+// G is symmetric: tiles of 128 x 128 on and above the diagonal, X's rows shared out among enough workgroups to fill the CUs; a diagonal tile has one
+// operand in LDS.  Bound by what the matrix cores' operands take out of LDS (200 003 x 512, ten tiles: 255 us, 0.63 PFLOP/s of halves; adding up every
+// stage, FIRST, 300), at one tile by memory (1 M x 128: 143 us, 3.6 TB/s).
 // FIRST: of X as it came, whose blocks of rows have powers of two of their own: a stage's sums are added by themselves.
 template <bool FIRST>
 __global__ void __launch_bounds__(256, 2) gram_kernel(GramArgs a)
@@ -331,7 +336,7 @@ __device__ __forceinline__ void put(const Halves& to, int64_t row, int64_t col, 
     to.part[1][row * to.stride + col] = static_cast<uint16_t>(lo);
 }
 
-// The splits' sums, joined in 64 bits and scaled; both triangles.
+// The splits' sums, joined in 64 bits and scaled; both triangles.  Bound by the launch and one chain of reads (1 M x 128, 512 splits, 34 MB: 7.5 us).
 struct GramJoinArgs {
     const float* part;
     uint32_t tiles, splits;
@@ -510,9 +515,11 @@ __global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs a)
         for (int i = 0; i < 4; ++i) a.next[(row0 + quarter * 4 + i) * a.side + c] = fmaf(kC, v2[i], fmaf(kB, v1[i], kA * v[i]));
 }
 
-// Larger sides: a product is a launch, or two that do not wait for one another.  A workgroup has a tile of 32 x 32 on or above the diagonal, its eight
-// wavefronts a share of the contraction each, straight from L2 into the matrix cores' operands.
-constexpr int kSmallWaves = 8;
+// Larger sides: a product is a launch, or two that do not wait for one another.  A workgroup has a tile of 32 x 32, or of 64 x 64 where there are
+// enough of them, on or above the diagonal, its eight wavefronts a share of the contraction each, straight from L2 into the matrix cores' operands.
+// (Larger tiles from 1024 on: whole updates of 1000 x 1000 506 and 463 us, 4096 x 4096 15.3 and 10.0 ms; half as many reads and conversions to parts, which
+// bound it, but a quarter of the workgroups.  Side 320: 6.4 us a launch, thirteen of them; 512: 8.)
+constexpr int kSmallWaves = 8, kSmallLarge = 1024;
 
 struct SmallJob {
     const float *a, *b;
@@ -526,73 +533,102 @@ struct SmallArgs {
     int32_t side;
 };
 
+template <int T>
 __global__ void __launch_bounds__(64 * kSmallWaves) small_kernel(SmallArgs args)
 {
-    constexpr int WAVES = kSmallWaves, EACH = 1024 / (64 * WAVES), ROWS = 2 * WAVES;       // elements of a thread, rows of a turn
-    __shared__ __align__(16) float lds[WAVES][32 * 33];
+    constexpr int WAVES = kSmallWaves, SIDE = 32 * T, EACH = SIDE * SIDE / (64 * WAVES), ROWS = 64 * WAVES / SIDE;      // elements of a thread, rows of a turn
+    __shared__ __align__(16) float lds[WAVES][SIDE * (SIDE + 1)];
     const SmallJob& job = args.job[blockIdx.y];
-    const uint32_t tiles = args.side / 32;
+    const int side = args.side;
+    const uint32_t tiles = (side + SIDE - 1) / SIDE;
     uint32_t ti, tj;
     pair_at(blockIdx.x, tiles, ti, tj);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, steps = args.side / 16;
-    const float* a = job.a + static_cast<int64_t>(ti * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
-    const float* b = job.b + static_cast<int64_t>(tj * 32 + (lane & 31)) * args.side + (lane >> 5) * 8;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, steps = side / 16, r0 = threadIdx.x / SIDE, c = threadIdx.x % SIDE;
+    // (rows behind the last are the last again, and not written)
+    const float *a[T], *b[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        a[t] = job.a + static_cast<int64_t>(min(static_cast<int>(ti) * SIDE + 32 * t + (lane & 31), side - 1)) * side + (lane >> 5) * 8;
+        b[t] = job.b + static_cast<int64_t>(min(static_cast<int>(tj) * SIDE + 32 * t + (lane & 31), side - 1)) * side + (lane >> 5) * 8;
+    }
+    auto inside = [&](uint32_t i, uint32_t j, int r, int col) { return T == 1 || (static_cast<int>(i) * SIDE + r < side && static_cast<int>(j) * SIDE + col < side); };
     // (the polynomial's other term is fetched ahead of the sums)
     float g[EACH] = {};
     if (job.polynomial)
 #pragma unroll
-        for (int q = 0; q < EACH; ++q) g[q] = job.a[static_cast<int64_t>(ti * 32 + (threadIdx.x >> 5) + ROWS * q) * args.side + tj * 32 + (threadIdx.x & 31)];
-    f32x16 sum, small;
+        for (int q = 0; q < EACH; ++q)
+            if (inside(ti, tj, r0 + ROWS * q, c)) g[q] = job.a[static_cast<int64_t>(ti * SIDE + r0 + ROWS * q) * side + tj * SIDE + c];
+    f32x16 sum[T][T], small[T][T];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum[i] = small[i] = 0.0f;
-    constexpr int FLIGHT = 4;
+    for (int m = 0; m < T; ++m)
+#pragma unroll
+        for (int n = 0; n < T; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[m][n][i] = small[m][n][i] = 0.0f;
+    constexpr int FLIGHT = 4 / T;
     for (int s0 = wave; s0 < steps; s0 += WAVES * FLIGHT) {
-        float x[FLIGHT][8] = {}, y[FLIGHT][8] = {};
+        float x[FLIGHT][T][8] = {}, y[FLIGHT][T][8] = {};
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
             if (s0 + WAVES * f >= steps) break;
-            __builtin_memcpy(x[f], a + (s0 + WAVES * f) * 16, 32);
-            __builtin_memcpy(y[f], b + (s0 + WAVES * f) * 16, 32);
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                __builtin_memcpy(x[f][t], a[t] + (s0 + WAVES * f) * 16, 32);
+                __builtin_memcpy(y[f][t], b[t] + (s0 + WAVES * f) * 16, 32);
+            }
         }
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f) {
-            bf16x8 u[3], v[3];
-            split_bf16<3>(x[f], u);
-            split_bf16<3>(y[f], v);
+            bf16x8 u[T][3], v[T][3];
 #pragma unroll
-            for (int of_parts = 2; of_parts >= 0; --of_parts) {
-                f32x16& to = of_parts > 0 ? small : sum;
-#pragma unroll
-                for (int q = 0; q <= of_parts; ++q) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[q], v[of_parts - q], to, 0, 0, 0);
+            for (int t = 0; t < T; ++t) {
+                split_bf16<3>(x[f][t], u[t]);
+                split_bf16<3>(y[f][t], v[t]);
             }
+#pragma unroll
+            for (int of_parts = 2; of_parts >= 0; --of_parts)
+#pragma unroll
+                for (int q = 0; q <= of_parts; ++q)
+#pragma unroll
+                    for (int m = 0; m < T; ++m)
+#pragma unroll
+                        for (int n = 0; n < T; ++n) {
+                            f32x16& to = of_parts > 0 ? small[m][n] : sum[m][n];
+                            to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[m][q], v[n][of_parts - q], to, 0, 0, 0);
+                        }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) lds[wave][(sum_row(i) + lane_row()) * 33 + (lane & 31)] = sum[i] + small[i];
+    for (int m = 0; m < T; ++m)
+#pragma unroll
+        for (int n = 0; n < T; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) lds[wave][(32 * m + sum_row(i) + lane_row()) * (SIDE + 1) + 32 * n + (lane & 31)] = sum[m][n][i] + small[m][n][i];
     __syncthreads();
     float* all = lds[0];            // the results; on the diagonal those above it are both
 #pragma unroll
     for (int q = 0; q < EACH; ++q) {
-        const int r = (threadIdx.x >> 5) + ROWS * q, c = threadIdx.x & 31, at = r * 33 + c;
+        const int r = r0 + ROWS * q, at = r * (SIDE + 1) + c;
         float x = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
         x += (lds[4][at] + lds[5][at]) + (lds[6][at] + lds[7][at]);
         if (job.polynomial) x = fmaf(kC, x, kB * g[q]) + (ti == tj && r == c ? kA : 0.0f);
         all[at] = x;                // (read by this thread alone so far)
     }
     __syncthreads();
-    auto write = [&](uint32_t i, uint32_t j, int r, int c, float x) {
-        const int64_t row = i * 32 + r, col = j * 32 + c;
-        if (job.out) job.out[row * args.side + col] = x;
-        else put(args.p, row, col, x, kPShift);
+    auto write = [&](uint32_t i, uint32_t j, int r, int col, float x) {
+        if (!inside(i, j, r, col)) return;
+        const int64_t to_row = i * SIDE + r, to_col = j * SIDE + col;
+        if (job.out) job.out[to_row * side + to_col] = x;
+        else put(args.p, to_row, to_col, x, kPShift);
     };
 #pragma unroll
     for (int q = 0; q < EACH; ++q) {
-        const int r = (threadIdx.x >> 5) + ROWS * q, c = threadIdx.x & 31;
+        const int r = r0 + ROWS * q;
         if (ti == tj) {
-            write(ti, tj, r, c, all[min(r, c) * 33 + max(r, c)]);
+            write(ti, tj, r, c, all[min(r, c) * (SIDE + 1) + max(r, c)]);
         } else {
-            write(ti, tj, r, c, all[r * 33 + c]);
-            write(tj, ti, r, c, all[c * 33 + r]);
+            write(ti, tj, r, c, all[r * (SIDE + 1) + c]);
+            write(tj, ti, r, c, all[c * (SIDE + 1) + r]);
         }
     }
 }
@@ -659,6 +695,10 @@ __device__ __forceinline__ void finish(const ApplyArgs& a, int64_t row, int col,
         if (row + sum_row(i) < a.tall) a.copy[copy_first + sum_row(i) * copy_step] = static_cast<bf16_t>(p[i]);
 }
 
+// A workgroup has a tile of P's columns and rows of X one after the other; up to 128 columns P stays in registers.  A tile's results go out as they
+// lie, 32 columns of a row side by side.  Narrow X is bound by memory (1 M x 128 with parameters: 350 us, 4.4 TB/s), 512 columns by operands out of LDS and
+// by results, which nothing else runs beside (200 003 x 512: 397 us, with parameters and their bf16 copy 475; 0.8 PFLOP/s of halves).  Turned, so that a lane has
+// four and four columns of one row, wider stores were slower: 422 and 605 us, lines being written in quarters.
 template <int W, int KS, Last L, bool WIDE>
 __global__ void __launch_bounds__(64 * W, 2) apply_kernel(ApplyArgs a)
 {
@@ -845,14 +885,17 @@ hipError_t polynomial(const MuonWs& w, int steps, hipStream_t st)
         return e;
     }
     float *g = w.small[0], *q = w.small[1], *t = w.small[2], *next = w.small[3], *p = q, *q2 = w.small[4], *p2 = w.small[5];
-    const uint32_t tiles = static_cast<uint32_t>(w.padded_side / 32);
+    const bool large = w.padded_side >= kSmallLarge;
+    const uint32_t tiles = static_cast<uint32_t>(ceil_div(w.padded_side, large ? 64 : 32));
     SmallArgs args{};
     args.side = w.padded_side;
     args.p = w.p;
     int jobs = 0;
     auto add = [&](const float* a, const float* b, float* out, bool poly) { args.job[jobs++] = SmallJob{a, b, out, poly ? 1 : 0}; };
     auto run = [&]() {
-        hipLaunchKernelGGL(small_kernel, dim3(tiles * (tiles + 1) / 2, jobs), dim3(64 * kSmallWaves), 0, st, args);
+        const dim3 grid(tiles * (tiles + 1) / 2, jobs);
+        if (large) hipLaunchKernelGGL(small_kernel<2>, grid, dim3(64 * kSmallWaves), 0, st, args);
+        else hipLaunchKernelGGL(small_kernel<1>, grid, dim3(64 * kSmallWaves), 0, st, args);
         jobs = 0;
         return hipGetLastError();
     };
@@ -905,7 +948,10 @@ hipError_t apply(const MuonWs& w, const Halves& x, bool first, const Halves* nex
     ApplyArgs a{};
     a.x = packed_operand(x.part, w.padded_tall, w.padded_side);     // (X's rows of zeros stay such)
     a.p = packed_operand(w.p.part, w.padded_side, w.padded_side);
-    const bool large = w.padded_side > 256 && round_up(w.padded_side, 256) * 8 <= w.padded_side * 9 && ceil_div(w.tall, 256) * ceil_div(w.padded_side, 256) >= 256;
+    // Tiles of 256 x 256, one a CU, read half as much LDS for a product: where columns fill them to 8 / 9 and the last of their rounds is not mostly empty
+    // (whole update, small tiles and large: 50 000 x 512, 392 tiles: 496 and 471 us; 20 000 x 1000, 316: 913 and 901; 33 000 x 512, 258: 402 and 412).
+    const int64_t large_tiles = ceil_div(w.tall, 256) * ceil_div(w.padded_side, 256);
+    const bool large = w.padded_side > 256 && round_up(w.padded_side, 256) * 8 <= w.padded_side * 9 && large_tiles * 10 >= round_up(large_tiles, 256) * 6;
     const int64_t tile = large ? 256 : kSide;
     a.row_tiles = static_cast<uint32_t>(ceil_div(w.tall, tile));
     a.col_tiles = static_cast<uint32_t>(ceil_div(w.padded_side, tile));

@@ -302,6 +302,8 @@ struct CoefArgs {
     const Mix* mix;                // with entropies only: [n]
 };
 
+// ENTROPY: one multiply-add and one product more a score, beside the exponential (4096 rows against 10 000 x 128 fp32: 61 us, 8192 against 200 003 x 512 bf16:
+// 13 pieces of 178).
 template <int P, int W, int KS, bool ENTROPY>
 __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 {
@@ -767,7 +769,7 @@ __global__ void __launch_bounds__(1024) few_join_kernel(FewJoinArgs a)
 
 // Gradients of sum_i l_i logp_i + e_i entropy_i: with f = |l| + 8 |e|, a = l / f and b = e / f the coefficient of table row v is
 //     - f [ p (a + b (s - lse + entropy)) - a [v = id] ],
-// the bracket at most 1 in magnitude (p |log p| < 0.37, p entropy < 6 for tables of less than 2^31 rows), as that of the loss alone is.
+// the bracket at most 1 in magnitude (p |log p| < 0.37, p entropy < 6 for tables of less than 2^31 rows), as that of the loss alone is.  (A launch: 3 to 5 us.)
 struct MixArgs {
     const int32_t* ids;            // NULL: no log probabilities, and all rows count
     const float *logp_grad, *entropy_grad, *entropy;      // the gradients: NULL for 1
