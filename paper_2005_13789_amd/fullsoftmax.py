@@ -34,6 +34,8 @@ class SoftmaxTrainer:
             raise ValueError("vertex and context must both be [num_nodes][dim]")
         if optimizer not in ("adamw", "muon") or (optimizer == "muon" and state_bits != 32):
             raise ValueError("optimizer must be 'adamw', or 'muon' with state_bits 32")
+        if optimizer == "muon" and min(vertex.shape) > ne.NE_ORTHOGONAL_MAX_SIDE:
+            raise ValueError(f"Muon takes tables whose smaller side is at most {ne.NE_ORTHOGONAL_MAX_SIDE}")
         if not math.isfinite(entropy_weight):
             raise ValueError("entropy_weight must be finite")
         V, d = vertex.shape

@@ -164,3 +164,31 @@ def test_sides_beyond_the_largest_are_refused():
     x = torch.zeros(4097, 4097, device=DEV)
     with pytest.raises(ne.NeError):
         ne.ne_orthogonalize(x, x, torch.empty(1 << 20, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("copy", [False, True])
+@pytest.mark.parametrize("rows,cols", [(30_011, 500), (500, 30_011), (16_400, 1024)])
+def test_steps_of_long_matrices(rows, cols, copy):
+    """Large tiles, with parameters as results; rows and columns that end inside them."""
+    say("step", rows, cols, copy)
+    torch.manual_seed(cols)
+    p, m, g = (torch.empty(rows, cols, device=DEV).normal_(std=s) for s in (0.1, 1e-3, 1e-3))
+    pad = torch.full((rows, cols + 5), 7.0, device=DEV)
+    view = pad[:, 2:2 + cols]
+    view.copy_(p)
+    c = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV) if copy else None
+    lr, beta, decay, scale = 0.02, 0.95, 0.1, 0.2 * math.sqrt(max(rows, cols))
+    want_m = beta * m.double() + g.double()
+    u = g.double() + beta * want_m
+    y = u if rows >= cols else u.t().contiguous()
+    gram = y.t() @ y
+    o = y @ polynomial(gram)
+    o = o if rows >= cols else o.t()
+    work = torch.empty(ne.ne_orthogonalize_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV).fill_(255)
+    ne.ne_muon_step(view, g, m, work, lr, momentum=beta, weight_decay=decay, scale=scale, param_bf16=c)
+    want = p.double() * (1 - lr * decay) - lr * scale * o
+    # an update's error (its operands are momentum in fp32, three roundings of 2^-24), and three roundings of the parameter
+    tol = (tolerance(gram) + 3 * 2.0 ** -24) * lr * scale * float(o.norm()) + 3 * 2.0 ** -24 * float(p.double().norm())
+    assert float((view.double() - want).norm()) <= tol
+    assert bool((pad[:, :2] == 7).all()) and bool((pad[:, 2 + cols:] == 7).all())
+    assert c is None or torch.equal(c, view.to(torch.bfloat16))

@@ -119,3 +119,9 @@ def test_trainer_and_command_line_refusals():
     for args in (["--hits", "65"], ["--hits", "-1"], ["--optimizer", "sgd"]):
         with pytest.raises(SystemExit):
             linkpred.main(["nowhere.txt", *args])
+
+
+def test_tables_of_too_long_sides_for_muon_are_refused():
+    t = torch.empty(5000, ne.NE_ORTHOGONAL_MAX_SIDE + 1, device="meta")
+    with pytest.raises(ValueError, match="smaller side"):
+        SoftmaxTrainer(t, t, 4, optimizer="muon")
