@@ -772,7 +772,7 @@ __global__ void __launch_bounds__(1024) few_join_kernel(FewJoinArgs a)
 // the bracket at most 1 in magnitude (p |log p| < 0.37, p entropy < 6 for tables of less than 2^31 rows), as that of the loss alone is.  (A launch: 3 to 5 us.)
 struct MixArgs {
     const int32_t* ids;            // NULL: no log probabilities, and all rows count
-    const float *logp_grad, *entropy_grad, *entropy;      // the gradients: NULL for 1
+    const float *logp_grad, *entropy_grad, *entropy;      // the gradients: NULL for 1; the entropies are there
     float logp_scale, entropy_scale;
     int64_t n;
     uint32_t num_rows;
@@ -1269,10 +1269,15 @@ ne_status ne_logprob_grad(const void* h_dev, int64_t h_stride, const void* w_dev
     if (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < logprob_grad_bytes(n, num_rows, dim, type))
         return fail(NE_ERR_ARG, who + "workspace_dev is NULL, not 256-byte aligned, or smaller than ne_logprob_workspace_bytes()");
     if (!dh_dev && !dw_dev) return NE_OK;
+    if (!ids_dev && entropy_scale == 0.0f) {        // (of nothing; entropy_dev may be NULL)
+        if (dh_dev) NE_HIP_CHECK(clear_gradient(dh_dev, dh_stride, n, dim, type, st));
+        if (dw_dev) NE_HIP_CHECK(clear_gradient(dw_dev, dw_stride, num_rows, dim, type, st));
+        return NE_OK;
+    }
     const XentWs w = xent_layout(n, num_rows, dim, type, true, static_cast<char*>(workspace_dev) + mix_bytes(n));
     SoftmaxCall x{h_dev, w_dev, h_stride, w_stride, n, num_rows, dim, type, ids_dev, logp_grad_dev};
     hipError_t e;
-    if (entropy_scale == 0.0f && ids_dev) {         // the loss's gradient with its sign turned
+    if (entropy_scale == 0.0f) {                    // the loss's gradient with its sign turned
         e = gradients(x, w, nullptr, lse_dev, -logp_scale, dh_dev, dh_stride, dw_dev, dw_stride, st);
     } else {
         Carver take{static_cast<char*>(workspace_dev)};

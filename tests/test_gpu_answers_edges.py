@@ -1,0 +1,43 @@
+"""Calls of the answers and of their gradients at the edges of what the header allows: nothing asked for, scores of exactly 0, very large and very
+small ones, more candidates than a workgroup looks at together, coefficients that add up to nothing."""
+import math
+
+import pytest
+import torch
+
+import paper_2005_13789_amd as ne
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def normal(n, d, dtype, seed, sd):
+    return (torch.randn(n, d, generator=torch.Generator().manual_seed(seed)) * sd).to(dtype).to(DEV)
+
+
+def work(n, V, d, dtype, k=0, grad=False):
+    return torch.empty(ne.ne_logprob_workspace_bytes(n, V, d, dtype, k=k, grad=grad), dtype=torch.uint8, device=DEV)
+
+
+# ---------------------------------------------------------------------------------------------
+# gradients of nothing
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,d,pad", [(1, 8, 0), (20, 40, 3), (300, 64, 0)])
+def test_gradients_of_nothing(n, d, pad, dtype):
+    """Without ids and with both scales 0 entropies may be left out, and the gradients are zeros, also behind rows that are longer than dim."""
+    V = 70
+    say("nothing", n, d, pad, dtype)
+    h, w = normal(n, d, dtype, 1, 1.0), normal(V, d, dtype, 2, 1.0)
+    lse = torch.zeros(n, device=DEV)
+    for dh_too, dw_too in ((True, True), (True, False), (False, True)):
+        big_h, big_w = (torch.full((r, d + pad), 3.0, dtype=dtype, device=DEV) for r in (n, V))
+        dh, dw = big_h[:, :d] if dh_too else None, big_w[:, :d] if dw_too else None
+        ne.ne_logprob_grad(h, w, None, lse, None, dh, dw, work(n, V, d, dtype, grad=True), logp_scale=0.0)
+        for g, big in ((dh, big_h), (dw, big_w)):
+            assert bool((big[:, :d] == (3.0 if g is None else 0.0)).all()) and bool((big[:, d:] == 3.0).all())
