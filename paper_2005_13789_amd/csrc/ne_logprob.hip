@@ -870,6 +870,7 @@ __device__ __forceinline__ void answer_row(const FinishArgs& a, Team<WAVES>& tea
         if (WAVES > 1) {
             __syncthreads();
             count = team.count;
+            __syncthreads();        // (the next call begins by clearing it, at once where there was no room: all have read it by then)
         }
         return count;
     };

@@ -41,3 +41,32 @@ def test_gradients_of_nothing(n, d, pad, dtype):
         ne.ne_logprob_grad(h, w, None, lse, None, dh, dw, work(n, V, d, dtype, grad=True), logp_scale=0.0)
         for g, big in ((dh, big_h), (dw, big_w)):
             assert bool((big[:, :d] == (3.0 if g is None else 0.0)).all()) and bool((big[:, d:] == 3.0).all())
+
+
+# ---------------------------------------------------------------------------------------------
+# more candidates than are looked at together
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,d", [(1, 5000, 16), (40, 70_003, 8), (300, 9000, 24), (600, 20_001, 16)])
+def test_many_equal_rows(n, V, d, dtype):
+    """Thousands of rows tie, so candidates come in several turns, each of which may be cut in halves over and over: teams of four wavefronts, of
+    sixteen, and those that rows are left to.  The answers are the lowest ids, every time."""
+    k = 64
+    say("many equal", n, V, d, dtype)
+    h, w = normal(n, d, dtype, 3, 1.0), normal(1, d, dtype, 4, 1.0).expand(V, d).contiguous()
+    other = torch.arange(V, device=DEV) % 1000 == 7         # some rows differ, and are behind the others whatever h is
+    w[other] = 0
+    s = (h.double() @ w[:1].double().t())[:, 0]
+    rows = torch.arange(V, device=DEV)
+    first, zeros = rows[~other][:k], rows[other]
+    lse, entropy = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    space = work(n, V, d, dtype, k)
+    # positive scores: the equal rows; negative ones: the rows of zeros, then the equal rows
+    want = torch.where((s > 0)[:, None], first[None], torch.cat([zeros, first])[:k][None]).to(torch.int32)
+    for turn in range(8):
+        ids, logp = torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)
+        ne.ne_logprob(h, w, None, lse, space, entropy=entropy, top_ids=ids, top_logp=logp)
+        assert torch.equal(ids, want), turn
+        if turn == 0:
+            kept = logp
+        assert torch.equal(logp, kept), turn
