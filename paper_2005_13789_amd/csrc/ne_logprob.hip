@@ -58,6 +58,11 @@ struct Best {
         second = fmaxf(fminf(first, f), fmaxf(second, s));
         first = fmaxf(first, f);
     }
+    // As it is left behind: both scores times a power of two, which must not touch the place (of a score of 0 it is all there is).
+    __device__ __forceinline__ float2 record(float factor, uint32_t mask) const
+    {
+        return make_float2(__uint_as_float((__float_as_uint(first * factor) & mask) | (__float_as_uint(first) & ~mask)), second * factor);
+    }
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -256,7 +261,7 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
                     b.first = __uint_as_float(__float_as_uint(b.first) | lane_row());
                     b.join_lanes(32);
                     const uint32_t chunk = (row0 >> 6) + c;
-                    if (lane < 32 && token < a.n && chunk < a.chunks) best[chunk] = make_float2(b.first * factor, b.second * factor);
+                    if (lane < 32 && token < a.n && chunk < a.chunks) best[chunk] = b.record(factor, ~63u);
                 }
             } else if constexpr (CHUNKS == kNarrow) {
 #pragma unroll
@@ -266,7 +271,7 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
                     for (int i = 0; i < 16; ++i) b.see(acc[im][j][i], i, ~15u);
                     t = fmaxf(t, b.first);
                     const uint32_t chunk = 2 * ((row0 >> 5) + im) + (lane >> 5);
-                    if (token < a.n && chunk < a.chunks) best[chunk] = make_float2(b.first * factor, b.second * factor);
+                    if (token < a.n && chunk < a.chunks) best[chunk] = b.record(factor, ~15u);
                 }
             } else {
 #pragma unroll

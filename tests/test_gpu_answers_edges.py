@@ -70,3 +70,37 @@ def test_many_equal_rows(n, V, d, dtype):
         if turn == 0:
             kept = logp
         assert torch.equal(logp, kept), turn
+
+
+# ---------------------------------------------------------------------------------------------
+# scores of exactly 0, and products below fp32's normal numbers
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,k", [(40, 3000, 1), (300, 3000, 1), (300, 3000, 12), (300, 100_003, 3), (700, 70_003, 2)])
+def test_rows_of_zeros_are_best(n, V, k, dtype):
+    """All scores are negative but for those of single rows of zeros, wherever in a chunk of table rows these lie."""
+    d = 64
+    say("zeros are best", n, V, k, dtype)
+    h, w = normal(n, d, dtype, 5, 1.0).abs(), -normal(V, d, dtype, 6, 1.0).abs()
+    for places in ([5], [17, 1000 + 46], [63, 129, 1000 + 31], [V - 1]):
+        some = w.clone()
+        some[places] = 0
+        lse, ids, logp = torch.empty(n, device=DEV), torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)
+        ne.ne_logprob(h, some, None, lse, work(n, V, d, dtype, k), top_ids=ids, top_logp=logp)
+        S = h.double() @ some.double().t()
+        S[:, places] = 0
+        want = torch.sort(S, dim=1, descending=True, stable=True)[1][:, :k]
+        assert torch.equal(ids.long(), want), places
+
+
+@pytest.mark.parametrize("n", [40, 300])
+def test_best_of_very_small_products(n):
+    """Products around the smallest numbers of fp32: places in the records survive the scaling, and scores in 64 bits decide."""
+    V, d, k = 1500, 64, 5
+    for size in (1e-17, 1e-20, 1e-23):
+        say("small products", n, size)
+        h, w = normal(n, d, torch.float32, 7, size), normal(V, d, torch.float32, 8, size)
+        lse, ids, logp = torch.empty(n, device=DEV), torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)
+        ne.ne_logprob(h, w, None, lse, work(n, V, d, torch.float32, k), top_ids=ids, top_logp=logp)
+        want = torch.sort(h.double().cpu() @ w.double().cpu().t(), dim=1, descending=True, stable=True)[1][:, :k]
+        assert torch.equal(ids.cpu().long(), want)
