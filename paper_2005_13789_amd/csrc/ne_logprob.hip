@@ -23,15 +23,21 @@ constexpr int64_t kChunksOfFour = 4096;                 // chunks that four wave
 constexpr int64_t kTeamsOfMany = 512;                  // rows of H up to which several wavefronts look for the answers of each
 constexpr float kNoScore = -1e30f;                     // below all scores: they are bounded by kMostScore
 constexpr float kMostScore = 1e29f;
+// Scores, in powers of two, from which on a softmax's maximum is taken from the sums as they are and subtracted before anything is multiplied: a
+// maximum with a place in its low bits is 2^-17 of itself too small or too large, up to 1 here, and a product's rounding is no exponent's any more.
+constexpr float kLargeScore = 0x1p17f;
 
 // A row's softmax so far: maximum and, relative to it, the sums of e^x and x e^x (all in powers of two).
 struct Softmax {
     float top, sum, moment, unused;
 };
 
+// How far a maximum is below a new one, as far as that counts: 2^-1000 is 0, and a sum times more would be infinite where scores are very large.
+__device__ __forceinline__ float below(float top, float now) { return fmaxf(top - now, -1000.0f); }
+
 __device__ __forceinline__ void join(Softmax& a, float top, float sum, float moment)
 {
-    const float now = fmaxf(a.top, top), da = a.top - now, db = top - now, ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    const float now = fmaxf(a.top, top), da = below(a.top, now), db = below(top, now), ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
     a.moment = fmaf(a.sum, da, a.moment) * ea + fmaf(sum, db, moment) * eb;
     a.sum = a.sum * ea + sum * eb;
     a.top = now;
@@ -288,16 +294,31 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
                     of_group[j] = -INFINITY;
                 }
             }
-            const float now = fmaxf(s[j].top, t * to_log2), d = s[j].top - now, e = __builtin_amdgcn_exp2f(d);
+            const bool large = fabsf(t) * to_log2 > kLargeScore, some_large = __any(large);
+            if (some_large) {
+                float top = low;
+#pragma unroll
+                for (int im = 0; im < MT; ++im)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[im][j][i]);
+                t = large ? top : t;        // (every row by its own scores, whichever are beside it)
+            }
+            const float here = t * to_log2, now = fmaxf(s[j].top, here), d = below(s[j].top, now), e = __builtin_amdgcn_exp2f(d);
+            const float rest = here < now ? here - now : 0.0f;      // (here - now alone would become one multiply-add, without here's rounding)
             float sum = 0.0f, moment = 0.0f;
+            auto add = [&](float x) {
+                const float p = __builtin_amdgcn_exp2f(x);
+                sum += p;
+                moment = fmaf(p, x, moment);
+            };
 #pragma unroll
-            for (int im = 0; im < MT; ++im)
+            for (int im = 0; im < MT && !some_large; ++im)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = fmaf(acc[im][j][i], to_log2, -now), p = __builtin_amdgcn_exp2f(x);
-                    sum += p;
-                    moment = fmaf(p, x, moment);
-                }
+                for (int i = 0; i < 16; ++i) add(fmaf(acc[im][j][i], to_log2, -now));
+#pragma unroll
+            for (int im = 0; im < MT && some_large; ++im)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) add(large ? fmaf(acc[im][j][i] - t, to_log2, rest) : fmaf(acc[im][j][i], to_log2, -now));
             s[j].moment = fmaf(fmaf(s[j].sum, d, s[j].moment), e, moment);
             s[j].sum = fmaf(s[j].sum, e, sum);
             s[j].top = now;
@@ -434,11 +455,15 @@ __global__ void __launch_bounds__(THREADS) answer_few_kernel(FewAnswerArgs a)
                 if (tile * 16 + quarter * 4 + i >= a.num_rows) acc[i] = kNoScore;
                 best.see(acc[i], i, ~15u);
             }
-            const float now = fmaxf(s[b].top, best.first * kLog2e), d = s[b].top - now, e = __builtin_amdgcn_exp2f(d);
+            float t = best.first;
+            const bool large = fabsf(t) * kLog2e > kLargeScore;
+            if (large) t = fmaxf(fmaxf(acc[0], acc[1]), fmaxf(acc[2], acc[3]));
+            const float here = t * kLog2e, now = fmaxf(s[b].top, here), d = below(s[b].top, now), e = __builtin_amdgcn_exp2f(d);
+            const float rest = here < now ? here - now : 0.0f;      // (here - now alone would become one multiply-add, without here's rounding)
             float sum = 0.0f, moment = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = fmaf(acc[i], kLog2e, -now), p = __builtin_amdgcn_exp2f(x);
+                const float x = large ? fmaf(acc[i] - t, kLog2e, rest) : fmaf(acc[i], kLog2e, -now), p = __builtin_amdgcn_exp2f(x);
                 sum += p;
                 moment = fmaf(p, x, moment);
             }

@@ -104,3 +104,52 @@ def test_best_of_very_small_products(n):
         ne.ne_logprob(h, w, None, lse, work(n, V, d, torch.float32, k), top_ids=ids, top_logp=logp)
         want = torch.sort(h.double().cpu() @ w.double().cpu().t(), dim=1, descending=True, stable=True)[1][:, :k]
         assert torch.equal(ids.cpu().long(), want)
+
+
+# ---------------------------------------------------------------------------------------------
+# very large scores
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,k", [(3, 700, 5), (60, 1000, 40), (300, 900, 3), (300, 5000, 2), (600, 2000, 20)])
+def test_large_scores(n, V, k, dtype):
+    """Scores of 2^20 to 1e28: probabilities are 0 and 1 (or shares of a few rows that fp32 cannot tell apart), everything stays finite, and what the best ids are
+    asked for besides changes lse by no more than its own error."""
+    d, u = 40, 2.0 ** -24
+    for size in (2.0 ** 20, 2.0 ** 24, 2.0 ** 25, 2.0 ** 27, 2.0 ** 30, 1e12, 1e20, 1e27):
+        say("large", n, V, k, dtype, size)
+        h, w = normal(n, d, dtype, 9, (size / d) ** 0.5), normal(V, d, dtype, 10, (size / d) ** 0.5 / 4)
+        S, A = h.double().cpu() @ w.double().cpu().t(), h.double().cpu().abs() @ w.double().cpu().abs().t()
+        z = torch.logsumexp(S, 1)
+        # a score: d products and sums, of 22-bit operands; its exponent: four roundings of numbers as large as the largest scores; a sum of V terms
+        tol = 2 * u * ((2 * d + 32) * A.max(1).values + 4 * (S.abs().max(1).values + z.abs() + 1)) + u * (V / 64 + 64)
+        for want_k in (0, k):
+            lse, entropy = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+            ids, logp = (torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)) if want_k else (None, None)
+            ne.ne_logprob(h, w, None, lse, work(n, V, d, dtype, want_k), entropy=entropy, top_ids=ids, top_logp=logp)
+            err = (lse.double().cpu() - z).abs()
+            assert bool((err <= tol).all()), (want_k, float((err / tol).max()))
+            assert bool((entropy >= -1e-5).all()) and bool((entropy <= math.log(V) + 1e-5).all()), want_k
+        values, order = torch.sort(S, dim=1, descending=True, stable=True)
+        assert torch.equal(ids.cpu().long(), order[:, :k])
+        lp = values[:, :k] - z[:, None]
+        assert bool(((logp.double().cpu() - lp).abs() <= tol[:, None] + u * lp.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [2, 300])
+def test_many_equal_large_scores_of_both_signs(n, dtype):
+    """Thousands of rows far below the best ones, in whichever order they come: their shares of the entropy are 0, not infinity times 0."""
+    V, d, k = 40_000, 8, 3
+    h = torch.full((n, d), 3e13, dtype=dtype, device=DEV)
+    sign = torch.where(torch.arange(V, device=DEV) < V // 2, -1.0, 1.0)
+    for flip in (1, -1):
+        say("both signs", n, dtype, flip)
+        w = (sign[:, None] * flip * torch.full((V, d), 3e13, device=DEV)).to(dtype)
+        for want_k in (0, k):
+            lse, entropy = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+            ids, logp = (torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)) if want_k else (None, None)
+            ne.ne_logprob(h, w, None, lse, work(n, V, d, dtype, want_k), entropy=entropy, top_ids=ids, top_logp=logp)
+            # log of V / 2 equal terms: sums of ones are exact, a logarithm and a product are off by 2^-23 of it each
+            assert bool(((entropy - math.log(V // 2)).abs() <= 2.0 ** -22 * 10).all()) and bool(torch.isfinite(lse).all())
+        first = 0 if flip < 0 else V // 2
+        assert bool((ids == first + torch.arange(k, device=DEV, dtype=torch.int32)).all())
