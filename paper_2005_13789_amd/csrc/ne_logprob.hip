@@ -242,8 +242,9 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
         const uint32_t row0 = tile_row0 + m0;
         ++seen;
         const bool group_ends = CHUNKS != kNone && a.group && ((seen & (a.group_tiles - 1)) == 0 || tile0 + seen == tile1);
-        if (row0 + 32 * MT > a.num_rows) {
-            const int left = static_cast<int>(a.num_rows - (row0 + lane_row()));     // (the difference is small where both are not)
+        const bool ends = row0 + 32 * MT > a.num_rows;
+        const int left = static_cast<int>(a.num_rows - (row0 + lane_row()));     // (the difference is small where both are not)
+        if (ends) {
 #pragma unroll
             for (int im = 0; im < MT; ++im)
 #pragma unroll
@@ -294,14 +295,15 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
                     of_group[j] = -INFINITY;
                 }
             }
-            const bool large = fabsf(t) * to_log2 > kLargeScore, some_large = __any(large);
-            if (some_large) {
+            // (rows behind the last count for nothing, however little `low` is once it is scaled; every row of H goes by its own scores, whichever are beside it)
+            const bool large = fabsf(t) * to_log2 > kLargeScore, apart = ends || __any(large);
+            if (apart) {
                 float top = low;
 #pragma unroll
                 for (int im = 0; im < MT; ++im)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[im][j][i]);
-                t = large ? top : t;        // (every row by its own scores, whichever are beside it)
+                t = large ? top : t;
             }
             const float here = t * to_log2, now = fmaxf(s[j].top, here), d = below(s[j].top, now), e = __builtin_amdgcn_exp2f(d);
             const float rest = here < now ? here - now : 0.0f;      // (here - now alone would become one multiply-add, without here's rounding)
@@ -312,13 +314,13 @@ __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)
                 moment = fmaf(p, x, moment);
             };
 #pragma unroll
-            for (int im = 0; im < MT && !some_large; ++im)
+            for (int im = 0; im < MT && !apart; ++im)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) add(fmaf(acc[im][j][i], to_log2, -now));
 #pragma unroll
-            for (int im = 0; im < MT && some_large; ++im)
+            for (int im = 0; im < MT && apart; ++im)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) add(large ? fmaf(acc[im][j][i] - t, to_log2, rest) : fmaf(acc[im][j][i], to_log2, -now));
+                for (int i = 0; i < 16; ++i) add(ends && 32 * im + sum_row(i) >= left ? -1000.0f : large ? fmaf(acc[im][j][i] - t, to_log2, rest) : fmaf(acc[im][j][i], to_log2, -now));
             s[j].moment = fmaf(fmaf(s[j].sum, d, s[j].moment), e, moment);
             s[j].sum = fmaf(s[j].sum, e, sum);
             s[j].top = now;

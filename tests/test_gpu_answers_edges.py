@@ -153,3 +153,27 @@ def test_many_equal_large_scores_of_both_signs(n, dtype):
             assert bool(((entropy - math.log(V // 2)).abs() <= 2.0 ** -22 * 10).all()) and bool(torch.isfinite(lse).all())
         first = 0 if flip < 0 else V // 2
         assert bool((ids == first + torch.arange(k, device=DEV, dtype=torch.int32)).all())
+
+
+# ---------------------------------------------------------------------------------------------
+# very small products
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n,V,d", [(40, 900, 64), (150, 900, 64), (300, 65, 40), (300, 1, 33), (600, 2049, 100)])
+@pytest.mark.parametrize("sizes", [(1.0, 1e-30), (1e-30, 1.0), (1e-16, 1e-16), (1e-19, 1e-20), (1e-25, 1e-10)])
+def test_small_products(n, V, d, sizes):
+    """Scores next to nothing: every row of the table has the same probability, and what lies behind the table's last row has none."""
+    k = 4
+    say("small products", n, V, d, sizes)
+    h, w = normal(n, d, torch.float32, 11, sizes[0]), normal(V, d, torch.float32, 12, sizes[1])
+    z = math.log(V)             # scores are below 1e-20
+    for want_k in (0, k):
+        lse, entropy, given = (torch.empty(n, device=DEV) for _ in range(3))
+        ids, logp = (torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)) if want_k else (None, None)
+        which = torch.arange(n, device=DEV, dtype=torch.int32) % V
+        ne.ne_logprob(h, w, which, lse, work(n, V, d, torch.float32, want_k), logp=given, entropy=entropy, top_ids=ids, top_logp=logp)
+        # a sum of ones is exact; its logarithm, a product and a rounding: 2^-24 of at most 8 each, and of what they are joined from
+        tol = 2.0 ** -24 * (8 + 8 * z)
+        assert float((lse.double() - z).abs().max()) <= tol and float((entropy.double() - z).abs().max()) <= tol and float((given.double() + z).abs().max()) <= tol
+    have = min(k, V)
+    want = torch.sort(h.double().cpu() @ w.double().cpu().t(), dim=1, descending=True, stable=True)[1][:, :have]
+    assert torch.equal(ids.cpu().long()[:, :have], want) and float((logp[:, :have].double() + z).abs().max()) <= tol
