@@ -387,7 +387,7 @@ struct PackArgs {
     uint32_t num_targets;
     const float* c;                // NULL, or factors of the rows
     int32_t dim, padded;
-    uint16_t* out[2];
+    uint16_t* out[2];              // P == 1: NULL where only the largest magnitude is wanted
     const float* amax;             // NULL: bf16 as it is (factors aside); otherwise `maxima` largest magnitudes, for fp16 parts
     int32_t* shift;                // receives their power of two
     int32_t maxima;
@@ -432,7 +432,8 @@ __device__ __forceinline__ void pack_rows(const PackArgs& a, uint32_t block, uin
                 for (int e = 0; e < 8; ++e) largest = fmaxf(largest, finite_abs(c * static_cast<float>(x[e])));
         }
 #pragma unroll
-        for (int p = 0; p < P; ++p) *reinterpret_cast<s16x8*>(a.out[p] + r * a.padded + e0) = out[p];
+        for (int p = 0; p < P; ++p)
+            if (P == 2 || a.out[p]) *reinterpret_cast<s16x8*>(a.out[p] + r * a.padded + e0) = out[p];
     };
     for_eights<THREADS>(static_cast<const T*>(a.in), a.in_stride, a.rows, a.dim, a.padded, block, blocks, write);
     // rows beyond the last one: zeros
@@ -765,8 +766,8 @@ uint32_t pack_blocks(const Packs& w, int64_t rows, int threads, int64_t most)
 }
 
 // Packs H and, where it cannot be used as it is, W.  With dw, c H for its product, too: in fp32 its halves, if there are factors; in bf16 it is to be
-// fp16, which `later` says how, as its largest magnitude is found here.
-hipError_t pack(const SoftmaxCall& x, const Packs& w, bool dw, Operand* h, Operand* hc, Operand* wo, PackArgs* later, hipStream_t st)
+// fp16, which `later` says how, as its largest magnitude is found here.  table_max (bf16; NULL, or kMostPack numbers) receives `maxima` largest magnitudes of W.
+hipError_t pack(const SoftmaxCall& x, const Packs& w, bool dw, Operand* h, Operand* hc, Operand* wo, PackArgs* later, float* table_max, int32_t* maxima, hipStream_t st)
 {
     const bool direct = usable_as_it_lies(x);
     const bool f32 = x.type == NE_F32;
@@ -801,7 +802,13 @@ hipError_t pack(const SoftmaxCall& x, const Packs& w, bool dw, Operand* h, Opera
     } else {
         add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, w.w, 0);
     }
+    if (table_max) {
+        uint16_t* const none[2] = {};
+        if (direct) add(x.w, x.w_stride, x.num_rows, x.num_rows, nullptr, nullptr, none, 0);
+        jobs.job[count - 1].amax_out = table_max;
+    }
     const dim3 grid(pack_blocks(w, most, kThreads, kMostPack), static_cast<unsigned>(count));
+    if (table_max) *maxima = static_cast<int32_t>(grid.x);
     if (dw && !f32) {
         *later = jobs.job[0];
         later->c = jobs.job[0].c = x.c;

@@ -18,7 +18,8 @@
 // Types: bf16 operands go to the matrix cores as they are.  G of bf16 tables is held in fp16, which keeps 11 bits where bf16 keeps 8.  dW
 // multiplies it with H in fp16.  dH, for which the table would have to be turned into fp16, rounds it to bf16 in registers, but takes the
 // target's coefficient whole.  So both gradients' errors are those of their own rounding: 0.0017.  (With G in bf16 0.0021, and dH 0.013 where the
-// table's rows share a part ten times as large as what tells them apart: a row's coefficients add up to nothing, their roundings do not.)
+// table's rows share a part ten times as large as what tells them apart: a row's coefficients add up to nothing, their roundings do not.)  Where entropies count the
+// target's coefficient is not the only large one, and dH takes the table in fp16 (table_kernel): its error is 0.0017 to 0.0021 there.
 // fp32 operands are split into two fp16 halves at a common power of two, x 2^k = hi + lo with 22 bits (of elements down to 2^-16 of the
 // largest; smaller ones are off by up to 2^-38 of it, fp16 ending there), and a product is hi hi + hi lo + lo hi: about the error of an fp32
 // product at three matrix instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
@@ -274,6 +275,45 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------
+// a bf16 table as fp16
+// ---------------------------------------------------------------------------------------------
+// Where entropies count, several of a row's coefficients are large and they add up to nothing, so where the table's rows share a part it is the roundings of
+// all of them that is left of it in dH: with G in bf16 dH is off by 0.011 where that part is ten times what tells rows apart, with G's 11 bits by 0.002 (its own rounding
+// 0.0017).  So a bf16 table goes into fp16, too, piece by piece, where it was packed or would have been.
+// bf16 to fp16, times a power of two: exponents less `bias` (how much smaller fp16's are, for the largest to have fp16's largest), which lies in the places
+// of both formats' exponents.  Elements keep all of their 8 bits from 2^-29 of the largest on; smaller ones are off by less than 2^-30 of it.
+__device__ __forceinline__ s16x8 to_half(s16x8 x, uint16_t bias)
+{
+    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+    const u16x8 u = __builtin_bit_cast(u16x8, x), sign = u & static_cast<uint16_t>(0x8000);
+    return __builtin_bit_cast(s16x8, (__builtin_elementwise_sub_sat(u ^ sign, u16x8(bias)) << static_cast<uint16_t>(3)) | sign);
+}
+
+// That bias for a largest magnitude, and the power of two that it makes.
+__device__ __forceinline__ int half_bias(float largest) { return max(static_cast<int>(__float_as_uint(largest) >> 23) - 30, 0); }
+__device__ __forceinline__ int half_shift(int bias) { return 112 - bias; }
+
+struct TableArgs {
+    const void* in;
+    uint16_t* out;                 // (may be in)
+    int64_t in_stride, out_stride, rows;
+    int32_t width;                 // a multiple of 8
+    const int32_t* shift;
+};
+
+// Bound by memory (8192 rows of H against 200 003 x 512: 13 launches of 7.2 us, and 42 us for the table's largest magnitude, which packing finds; as G need not be turned in
+// registers the gradients take 80 us more in all, of 7430. Turning the table there, in the place of G, took 2200: a large tile has twice as many operands of it.)
+__global__ void __launch_bounds__(kThreads) table_kernel(TableArgs a)
+{
+    const uint16_t bias = static_cast<uint16_t>((half_shift(0) - *a.shift) << 7);
+    for_eights(static_cast<const bf16_t*>(a.in), a.in_stride, a.rows, a.width, a.width, blockIdx.x, gridDim.x, [&](int64_t r, int e, const bf16_t (&x)[8]) {
+        s16x8 y;
+        __builtin_memcpy(&y, x, 16);
+        *reinterpret_cast<s16x8*>(a.out + r * a.out_stride + e) = to_half(y, bias);
+    });
+}
+
+// ---------------------------------------------------------------------------------------------
 // G of a piece of the table
 // ---------------------------------------------------------------------------------------------
 // The scores again, with the exponentials written as operands of the next products instead of added up: of bf16 tables G 2^14 in fp16, off by 2^-12 of
@@ -298,8 +338,11 @@ struct CoefArgs {
     uint32_t blocks;               // workgroups that make G; bf16: further ones of the first piece bring c H into fp16 (1000 x 3000 x 64: 37 us with a
                                    // launch of its own, 32 so)
     PackArgs hc;
-    float* rest;                   // bf16 only: [tokens]  what rounding to bf16 takes from the target's coefficient
+    float* rest;                   // bf16 only: [tokens]  what rounding takes from the target's coefficient: to bf16, or where entropies count to fp16
     const Mix* mix;                // with entropies only: [n]
+    const float* table_max;        // NULL, or `maxima` largest magnitudes of the table, ...
+    int32_t maxima;
+    int32_t* table_shift;          // ... which leave the power of two behind that it takes as fp16
 };
 
 // ENTROPY: one multiply-add and one product more a score, beside the exponential (4096 rows against 10 000 x 128 fp32: 61 us, 8192 against 200 003 x 512 bf16:
@@ -312,6 +355,13 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
     if (P == 1 && blockIdx.x >= a.blocks) {
         pack_rows<1, 64 * W>(a.hc, blockIdx.x - a.blocks, gridDim.x - a.blocks, reinterpret_cast<float*>(lds));
         return;
+    }
+    if (ENTROPY && P == 1 && a.table_max && blockIdx.x == 0) {
+        float top = 0.0f;
+        for (int i = threadIdx.x; i < a.maxima; i += 64 * W) top = fmaxf(top, a.table_max[i]);
+        top = block_max<64 * W>(top, reinterpret_cast<float*>(lds));
+        if (threadIdx.x == 0) *a.table_shift = half_shift(half_bias(top));
+        __syncthreads();
     }
     const int lane = threadIdx.x & 63, m0 = first_row<W>(), n0 = first_col<W>();
     uint32_t token_tile, split;
@@ -356,7 +406,7 @@ __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
                             if (P == 1) {
                                 const float g = acc[im][j][i];
                                 const float stored = static_cast<float>(static_cast<f16_t>(g));
-                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - static_cast<float>(static_cast<bf16_t>(stored));
+                                a.rest[token_tile * R + n0 + 32 * j + (lane & 31)] = g - (ENTROPY ? stored : static_cast<float>(static_cast<bf16_t>(stored)));
                             }
                         }
             }
@@ -414,7 +464,8 @@ struct ProductArgs {
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
 // (bf16: turning G from fp16 to bf16 in registers takes up to 4 % of the gradients' time, 8192 x 200 003 x 512 5180 -> 5370 us; W in fp16 would
 // take a pass over the table.)
-template <int P, int W>
+// ENTROPY, bf16: the table is there as fp16, so that dH, too, sees G's 11 bits.
+template <int P, int W, bool ENTROPY>
 __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
@@ -429,7 +480,7 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
     constexpr int R = rows_of<W>(), MT = W / 2;
     f32x16 acc[MT][2];
-    if (dh) product_tile<P, W, true, P == 1 ? kToBf16 : kPlain>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
+    if (dh) product_tile<P, W, true, P == 2 ? kPlain : ENTROPY ? kHalf : kToBf16>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
     else product_tile<P, W, false, P == 1 ? kHalf : kPlain>(a.h, a.g_cols, col * R, tile * R, s0, s1, lds, acc);
     const uint32_t row0 = tile * R + first_col<W>() + (lane & 31), col0 = col * R + first_row<W>() + 4 * (lane >> 5);
     if (!dh && !a.dw) {
@@ -549,8 +600,12 @@ __global__ void __launch_bounds__(kThreads) reduce_kernel(ReduceArgs a)
     if (!in) return;
     const int k = -((a.shift ? *a.shift : 0) + kGShift);
     const float all[4] = {sum.x, sum.y, sum.z, sum.w};
+    auto whole = [&](float sum, float w) {
+        if (a.rest && a.shift) return fmaf(ldexpf(rest, -kGShift), w, ldexpf(sum, k));      // (the table's power of two is not the coefficient's)
+        return ldexpf(a.rest ? fmaf(rest, w, sum) : sum, k);
+    };
 #pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = counts ? ldexpf(a.rest ? fmaf(rest, x[q], all[q]) : all[q], k) * a.scale * c : 0.0f;
+    for (int q = 0; q < 4; ++q) x[q] = counts ? whole(all[q], x[q]) * a.scale * c : 0.0f;
     store_some<T, 4>(static_cast<T*>(a.out) + r * a.out_stride + e, a.dim - e, x);
 }
 
@@ -814,6 +869,7 @@ struct XentWs : Packs {
     float* target_score;
     uint16_t* g[2];
     float *dh, *dw, *rest;
+    float* table_max;                  // with entropies: largest magnitudes of a bf16 table
     size_t total;
 };
 
@@ -1028,7 +1084,7 @@ hipError_t run_loss(const SoftmaxCall& x, const XentWs& w, float* loss, float* l
 {
     ScoreArgs a{};
     Operand unused;
-    hipError_t e = pack(x, w, false, &a.h, &unused, &a.w, nullptr, st);
+    hipError_t e = pack(x, w, false, &a.h, &unused, &a.w, nullptr, nullptr, nullptr, st);
     if (e != hipSuccess) return e;
     a.targets = x.targets; a.shift = w.shift; a.n = x.n; a.num_rows = static_cast<uint32_t>(x.num_rows); a.row_tiles = w.row_tiles;
     a.splits = w.splits; a.tokens = static_cast<uint32_t>(w.tokens); a.steps = w.padded / step_of<P>(); a.stat = w.stat; a.target_score = w.target_score;
@@ -1070,7 +1126,8 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
 {
     CoefArgs ca{};
     ProductArgs pa{};
-    hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, &ca.hc, st);
+    const bool halves = P == 1 && ENTROPY && dh;       // dH's product takes the table as fp16
+    hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, &ca.hc, halves ? w.table_max : nullptr, &ca.maxima, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
     ca.targets = x.targets; ca.shift = w.shift; ca.lse = lse; ca.n = x.n; ca.g_stride = w.piece; ca.rest = w.rest; ca.mix = mix;
@@ -1082,6 +1139,8 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
     pa.h_splits = w.h_splits; pa.w_splits = w.w_splits; pa.w_share = w.w_share;
     pa.w_stages = w.w_stages;
     pa.out_stride = dw_stride; pa.dim = x.dim; pa.scale = scale; pa.shift = w.shift + (x.c ? 2 : 1);
+    ca.table_max = halves ? w.table_max : nullptr;
+    ca.table_shift = w.shift;
     auto reduce = [&](ReduceArgs r) {
         r.cols = pa.cols; r.dim = x.dim; r.scale = scale;
         const dim3 grid(static_cast<unsigned>(ceil_div(r.rows, r.splits >= 16 ? 1 : 4)), static_cast<unsigned>(ceil_div(x.dim, 256)));
@@ -1107,7 +1166,14 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
         pa.g_rows = Operand{{w.g[0], w.g[1]}, w.piece, static_cast<uint32_t>(w.tokens - 1), static_cast<uint32_t>(w.piece)};
         pa.g_cols = pa.g_rows;
         pa.w = all;
-        for (int p = 0; p < P; ++p) pa.w.part[p] = all.part[p] + base * all.stride;
+        if (halves) {
+            const TableArgs t{all.part[0] + base * all.stride, w.w[0] + base * w.padded, all.stride, w.padded, rows, static_cast<int32_t>(all.width), w.shift};
+            hipLaunchKernelGGL(table_kernel, dim3(pack_blocks(w, rows, kThreads, kMostPack)), dim3(kThreads), 0, st, t);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+            pa.w.part[0] = w.w[0];
+            pa.w.stride = w.padded;
+        }
+        for (int p = 0; p < P; ++p) pa.w.part[p] += base * pa.w.stride;
         pa.w.last = static_cast<uint32_t>(rows - 1);
         pa.h_tiles = dh ? static_cast<uint32_t>(ceil_div(w.tokens, edge)) : 0;
         pa.w_tiles = dw ? static_cast<uint32_t>(ceil_div(rows, edge)) : 0;
@@ -1118,8 +1184,8 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
         pa.out = dw ? static_cast<T*>(dw) + base * dw_stride : nullptr;
         const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
         if (!blocks) continue;
-        if (P == 1 && w.large_products) hipLaunchKernelGGL((products_kernel<1, 8>), dim3(blocks), dim3(512), 0, st, pa);
-        else hipLaunchKernelGGL((products_kernel<P, 4>), dim3(blocks), dim3(256), 0, st, pa);
+        if (P == 1 && w.large_products) hipLaunchKernelGGL((products_kernel<1, 8, ENTROPY>), dim3(blocks), dim3(512), 0, st, pa);
+        else hipLaunchKernelGGL((products_kernel<P, 4, P == 1 && ENTROPY>), dim3(blocks), dim3(256), 0, st, pa);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (dw && w.dw) {
@@ -1134,7 +1200,7 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
     if (dh) {
         ReduceArgs r{};
         r.in = w.dh; r.split_stride = w.tokens * pa.cols; r.splits = w.h_splits; r.rows = x.n; r.out = dh; r.out_stride = dh_stride;
-        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = x.c; r.shift = P == 2 ? w.shift : nullptr;
+        r.targets = x.targets; r.num_targets = ca.num_rows; r.c = x.c; r.shift = P == 2 || halves ? w.shift : nullptr;
         r.rest = x.targets ? w.rest : nullptr; r.w = static_cast<const bf16_t*>(x.w); r.w_stride = x.w_stride;
         return reduce(r);
     }
@@ -1182,8 +1248,8 @@ size_t xent_need(int64_t n, int64_t num_rows, int32_t dim, int32_t type, bool gr
     return std::max(xent_bytes(n, num_rows, dim, type, grad), xent_layout(n, num_rows, dim, type, grad, nullptr).total);
 }
 
-// A row's factors lie in front of the gradients' workspace.
-size_t mix_bytes(int64_t n) { return static_cast<size_t>(round_up(n * static_cast<int64_t>(sizeof(Mix)), 256) + round_up(n * 4, 256)); }
+// Rows' factors and the table's largest magnitudes lie in front of the gradients' workspace.
+size_t mix_bytes(int64_t n) { return static_cast<size_t>(round_up(n * static_cast<int64_t>(sizeof(Mix)), 256) + round_up(n * 4, 256) + kMostPack * 4); }
 
 }  // namespace
 
@@ -1274,7 +1340,7 @@ ne_status ne_logprob_grad(const void* h_dev, int64_t h_stride, const void* w_dev
         if (dw_dev) NE_HIP_CHECK(clear_gradient(dw_dev, dw_stride, num_rows, dim, type, st));
         return NE_OK;
     }
-    const XentWs w = xent_layout(n, num_rows, dim, type, true, static_cast<char*>(workspace_dev) + mix_bytes(n));
+    XentWs w = xent_layout(n, num_rows, dim, type, true, static_cast<char*>(workspace_dev) + mix_bytes(n));
     SoftmaxCall x{h_dev, w_dev, h_stride, w_stride, n, num_rows, dim, type, ids_dev, logp_grad_dev};
     hipError_t e;
     if (entropy_scale == 0.0f) {                    // the loss's gradient with its sign turned
@@ -1283,6 +1349,7 @@ ne_status ne_logprob_grad(const void* h_dev, int64_t h_stride, const void* w_dev
         Carver take{static_cast<char*>(workspace_dev)};
         Mix* mix = take.get<Mix>(static_cast<size_t>(n));
         float* c = take.get<float>(static_cast<size_t>(n));
+        w.table_max = take.get<float>(kMostPack);
         const MixArgs a{ids_dev, logp_grad_dev, entropy_grad_dev, entropy_dev, logp_scale, entropy_scale, n, static_cast<uint32_t>(num_rows), mix, c};
         hipLaunchKernelGGL(mix_kernel, dim3(static_cast<unsigned>(ceil_div(n, kThreads))), dim3(kThreads), 0, st, a);
         e = hipGetLastError();

@@ -177,3 +177,49 @@ def test_small_products(n, V, d, sizes):
     have = min(k, V)
     want = torch.sort(h.double().cpu() @ w.double().cpu().t(), dim=1, descending=True, stable=True)[1][:, :have]
     assert torch.equal(ids.cpu().long()[:, :have], want) and float((logp[:, :have].double() + z).abs().max()) <= tol
+
+
+# ---------------------------------------------------------------------------------------------
+# coefficients that add up to nothing
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("shared,scale", [(0.0, 0), (10.0, 0), (30.0, 0), (10.0, 50), (10.0, -50)])
+@pytest.mark.parametrize("n,V,d", [(64, 4000, 300), (40, 3001, 296), (700, 2000, 64), (600, 90_000, 512)])
+def test_gradients_of_tables_with_a_shared_part(n, V, d, shared, scale):
+    """bf16: rows of w share a part that is larger than what tells them apart, so that a row's coefficients of the entropy, several of them large,
+    cancel in dh.  Coefficients keep 11 bits (2^-11 of themselves), a score d roundings of fp32 sums, outputs 2^-8; roundings are independent, so their sums'
+    squares add up: a uniform one is 3^-1/2 of its largest on average, and what many of them make is held to 1.2 (all outputs) and 2 (a row's few large
+    coefficients) of what is expected.  h and w take powers of two that cancel in the
+    scores (norms stay below the 2^63 from which answers are NaN: rows have about 2^6)."""
+    if V > 10_000 and (shared, scale) not in ((10.0, 0), (10.0, -50)):
+        return
+    say("shared part", n, V, d, shared, scale)
+    gen = torch.Generator().manual_seed(13)
+    sd = d ** -0.25
+    h = (torch.randn(n, d, generator=gen) * sd).bfloat16().to(DEV)
+    w = (torch.randn(V, d, generator=gen) * sd + shared * sd * torch.randn(1, d, generator=gen)).bfloat16().to(DEV)
+    ids = torch.randint(0, V, (n,), generator=gen).to(torch.int32).to(DEV)
+    H, W = h.double(), w.double()
+    S = H @ W.t()
+    z = torch.logsumexp(S, 1)
+    L = S - z[:, None]
+    p = L.exp()
+    E = -(p * L).sum(1)
+    h, w = h * 2.0 ** -scale, w * 2.0 ** scale
+    lse, entropy = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    ne.ne_logprob(h, w, ids, lse, work(n, V, d, torch.bfloat16), entropy=entropy)
+    size = lambda x: float(torch.linalg.vector_norm(x))  # noqa: E731
+    for l, e, given in ((0.0, 1.0, True), (0.0, 1.0, False), (1.0, 1.0, True), (1.0, 0.05, True)):
+        dh, dw = torch.full_like(h, float("nan")), torch.full_like(w, float("nan"))
+        ne.ne_logprob_grad(h, w, ids if given else None, lse, entropy, dh, dw, work(n, V, d, torch.bfloat16, grad=True), logp_scale=l, entropy_scale=e)
+        G = -l * p - e * p * (L + E[:, None])
+        G[torch.arange(n, device=DEV), ids.long()] += l
+        score = 2 * d ** 0.5 * 2.0 ** -24 * float(S.abs().max() + z.abs().max())
+        each = 2.0 ** -11 / 3 ** 0.5 * G.abs() + score * (G.abs() + (l + e) * p)
+        for got, want, err in ((dh.double() * 2.0 ** -scale, G @ W, (each ** 2 @ (W ** 2).sum(1)).sum() ** 0.5),
+                               (dw.double() * 2.0 ** scale, G.t() @ H, ((each ** 2).sum(1) @ (H ** 2).sum(1)) ** 0.5)):
+            floor = 2.0 ** -38 * (l + 8 * e) * (n * V) ** 0.5 * float((W if got.shape[0] == n else H).abs().max()) * d ** 0.5
+            tol = 1.2 * 2.0 ** -8 / 3 ** 0.5 * size(want) + 2 * float(err) + floor
+            # (dw: c h in fp16, too)
+            tol = tol if got.shape[0] == n else tol + 2 * 2.0 ** -11 / 3 ** 0.5 * size(G.abs().t() @ H.abs())
+            assert size(got - want) <= tol, (l, e, given, got.shape, size(got - want) / size(want), tol / size(want))
+            say("  ", l, e, given, tuple(got.shape), size(got - want) / size(want), tol / size(want))
