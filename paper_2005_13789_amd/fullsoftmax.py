@@ -58,7 +58,7 @@ class SoftmaxTrainer:
         if optimizer == "muon":
             size = max(size, ne.ne_orthogonalize_workspace_bytes(V, d))
         self.work = torch.empty(size, dtype=torch.uint8, device=dev)     # one after the other on one stream: shared by the calls
-        self.opt, self.copies, self.answers_work = None, copies, None
+        self.opt, self.copies = None, copies
         if optimizer == "muon":
             self.momenta = [torch.zeros((V, d), device=dev) for _ in range(2)]
             return
@@ -106,7 +106,8 @@ class SoftmaxTrainer:
 
     def predict(self, nodes: torch.Tensor, k: int = 10):
         """The k most probable contexts of nodes int32 [n] (CUDA, n <= batch) at the current tables: (ids int32 [n][k], their log probabilities
-        float32 [n][k], the entropies float32 [n]).  A node outside the tables has no answers: -1, minus infinity, 0."""
+        float32 [n][k], the entropies float32 [n]).  A node outside the tables has no answers: -1, minus infinity, 0.
+        The workspace is the call's own, of n nodes (ne_logprob_workspace_bytes)."""
         n = int(nodes.numel())
         if n < 1 or n > self.batch:
             raise ValueError(f"answers are given for 1 to {self.batch} nodes at a time")
@@ -114,13 +115,11 @@ class SoftmaxTrainer:
             raise ValueError(f"k must be 1 to {ne.NE_TOP_MAX}")
         V, d = self.tables[0].shape
         dev = self.tables[0].device
-        size = ne.ne_logprob_workspace_bytes(self.batch, V, d, self.h.dtype, k=k)
-        if self.answers_work is None or self.answers_work.numel() < size:
-            self.answers_work = torch.empty(size, dtype=torch.uint8, device=dev)
+        work = torch.empty(ne.ne_logprob_workspace_bytes(n, V, d, self.h.dtype, k=k), dtype=torch.uint8, device=dev)
         h = self.h[:n]
         ne.ne_embed_lookup(self.rows[0], nodes, h)
         ids = torch.empty((n, k), dtype=torch.int32, device=dev)
         logp, lse, entropy = torch.empty((n, k), device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev)
         # (the nodes themselves mark the rows that count)
-        ne.ne_logprob(h, self.rows[1], nodes, lse, self.answers_work, entropy=entropy, top_ids=ids, top_logp=logp)
+        ne.ne_logprob(h, self.rows[1], nodes, lse, work, entropy=entropy, top_ids=ids, top_logp=logp)
         return ids, logp, entropy
