@@ -96,13 +96,25 @@ def evaluate(tables: ne.Tables, num_nodes: int, all_edges: np.ndarray, test_edge
     return auc(score(tables, test_edges, second_from_context), score(tables, negatives, second_from_context))
 
 
+def answers_batch(num_nodes: int, dim: int, k: int, most: int, room: int) -> int:
+    """Rows, at most `most`, whose answers from a float32 table take a workspace of no more than `room` bytes (one row, whatever it takes).  Large batches
+    pack a copy of the table and leave records of every part of it behind for every row; up to 192 rows stream through it and leave only the records, at up
+    to three times the time a row (3 M nodes of 128, k = 10: 3.0 us a row at 8192 rows, 3.4 at 2048, 4.8 at 512, 8.6 at 192)."""
+    while most > 1 and ne.ne_logprob_workspace_bytes(most, num_nodes, dim, torch.float32, k=k) > room:
+        most = most // 2 if most > 2 * 192 else max(most - 64, most // 2)
+    return most
+
+
 def hits(tables: ne.Tables, edges: np.ndarray, k: int = 10, batch: int = 8192) -> float:
     """Share of the edges' ends whose other end is among the k nodes that the full softmax over the context table makes most probable for them
-    (both directions of every edge; nothing is left out of the k, neither the node itself nor neighbours that training has seen)."""
+    (both directions of every edge; nothing is left out of the k, neither the node itself nor neighbours that training has seen).
+    batch: rows that are answered at a time; fewer where their workspace would take more than both tables (4 GiB where these are small), or than half of
+    the memory that is free."""
     dev, V, d = tables.vertex.device, tables.num_nodes, tables.dim
     e = np.asarray(edges, dtype=np.int64)
     pairs = torch.from_numpy(np.concatenate([e, e[:, ::-1]]).astype(np.int32)).to(dev)
-    batch = min(batch, int(pairs.shape[0]))
+    free = torch.cuda.mem_get_info(dev)[0] + torch.cuda.memory_reserved(dev) - torch.cuda.memory_allocated(dev)
+    batch = answers_batch(V, d, k, min(batch, int(pairs.shape[0])), min(max(4 << 30, 8 * V * d), free // 2))
     work = torch.empty(ne.ne_logprob_workspace_bytes(batch, V, d, torch.float32, k=k), dtype=torch.uint8, device=dev)
     h, lse = torch.empty((batch, d), device=dev), torch.empty(batch, device=dev)
     ids, logp = torch.empty((batch, k), dtype=torch.int32, device=dev), torch.empty((batch, k), device=dev)
