@@ -38,6 +38,9 @@ class SoftmaxTrainer:
             raise ValueError(f"Muon takes tables whose smaller side is at most {ne.NE_ORTHOGONAL_MAX_SIDE}")
         if not math.isfinite(entropy_weight):
             raise ValueError("entropy_weight must be finite")
+        mu, decay = torch.tensor([momentum, weight_decay], dtype=torch.float32).tolist()       # as the step takes them
+        if optimizer == "muon" and not (0.0 <= mu < 1.0 and 0.0 <= decay < math.inf):
+            raise ValueError("Muon takes a momentum of 0 to 1, 1 excluded, and a finite weight_decay >= 0")
         V, d = vertex.shape
         dev = vertex.device
         self.entropy_weight, self.momentum, self.weight_decay = entropy_weight, momentum, weight_decay
