@@ -137,6 +137,8 @@ def train(train_edges: np.ndarray, num_nodes: int, dim: int = 64, epochs: int = 
     whole walks, unshuffled), or SoftmaxTrainer (mode "softmax": the full softmax over all nodes in the place of sampled
     negatives, AdamW with 32-bit states, or Muon, as `optimizer` says, and its `entropy_weight`; lr0 is Adam's), learning rate decaying linearly over the run.  Returns (Tables, Alias); the handles keep
     their device tensors alive (tables.vertex, tables.context)."""
+    if mode != "softmax" and (optimizer != "adamw" or entropy_weight != 0.0):
+        raise ValueError("optimizer and entropy_weight are of mode softmax")
     dev = torch.device(device)
     graph = wl.build_graph(num_nodes, torch.from_numpy(np.asarray(train_edges, dtype=np.int64)))
     vertex = torch.empty((num_nodes, dim), dtype=torch.float32, device=dev)
@@ -216,6 +218,8 @@ def main(argv=None) -> int:
     args = ap.parse_args(argv)
     if not 0 <= args.hits <= ne.NE_TOP_MAX:
         ap.error(f"--hits takes 0 to {ne.NE_TOP_MAX}")
+    if args.mode != "softmax" and (args.optimizer != "adamw" or args.entropy_weight != 0.0):
+        ap.error("--optimizer and --entropy-weight are of --mode softmax")
     edges, n = read_edge_list(args.edges)
     train_edges, test_edges = split_edges(edges, args.test_fraction, args.seed)
     tables, _alias = train(train_edges, n, dim=args.dim, epochs=args.epochs, negatives=args.negatives, batch=args.batch,
