@@ -112,6 +112,8 @@ def hits(tables: ne.Tables, edges: np.ndarray, k: int = 10, batch: int = 8192) -
     the memory that is free."""
     dev, V, d = tables.vertex.device, tables.num_nodes, tables.dim
     e = np.asarray(edges, dtype=np.int64)
+    if e.size == 0:
+        raise ValueError("hits are of one edge at least")
     pairs = torch.from_numpy(np.concatenate([e, e[:, ::-1]]).astype(np.int32)).to(dev)
     free = torch.cuda.mem_get_info(dev)[0] + torch.cuda.memory_reserved(dev) - torch.cuda.memory_allocated(dev)
     batch = answers_batch(V, d, k, min(batch, int(pairs.shape[0])), min(max(4 << 30, 8 * V * d), free // 2))
