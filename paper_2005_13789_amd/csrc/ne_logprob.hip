@@ -737,6 +737,9 @@ __device__ __forceinline__ void answer_row(const FinishArgs& a, Team<WAVES>& tea
             largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), o, 64)));
         }
     }
+    // (joined in another order a sum is rounded otherwise: what every thread goes on with is the first lane's, the same in all wavefronts)
+    auto first_lane = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+    s = Softmax{first_lane(s.top), first_lane(s.sum), first_lane(s.moment), 0.0f};
     // Bounds of both norms: squares and roots are rounded, and those of small values left something out.
     const float left_out = 0x1p-62f * sqrtf(static_cast<float>(a.dim));
     const float h_norm = squares == 0.0f ? 0.0f : 1.001f * sqrtf(squares) + left_out;

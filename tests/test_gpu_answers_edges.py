@@ -223,3 +223,27 @@ def test_gradients_of_tables_with_a_shared_part(n, V, d, shared, scale):
             tol = tol if got.shape[0] == n else tol + 2 * 2.0 ** -11 / 3 ** 0.5 * size(G.abs().t() @ H.abs())
             assert size(got - want) <= tol, (l, e, given, got.shape, size(got - want) / size(want), tol / size(want))
             say("  ", l, e, given, tuple(got.shape), size(got - want) / size(want), tol / size(want))
+
+
+# ---------------------------------------------------------------------------------------------
+# the same bits every time
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,d,k", [(1, 200_003, 64, 10), (48, 10_000, 128, 20), (300, 70_003, 24, 33), (600, 3000, 64, 16), (700, 40_001, 16, 64)])
+def test_answers_are_the_same_every_time(n, V, d, k, dtype):
+    """Whichever thread comes upon a row first; and an id has the same log probability as a given one and as one of the best."""
+    say("same", n, V, d, k, dtype)
+    h, w = normal(n, d, dtype, 14, d ** -0.25), normal(V, d, dtype, 15, d ** -0.25)
+    w[V // 2:V // 2 + 300] = w[:300]                # some tie, so rows have many candidates
+    given, first = torch.zeros(n, dtype=torch.int32, device=DEV), None
+    for turn in range(12):
+        lse, entropy, logp = (torch.empty(n, device=DEV) for _ in range(3))
+        ids, best = torch.full((n, k), -7, dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)
+        space = work(n, V, d, dtype, k).fill_(17 * turn)
+        ne.ne_logprob(h, w, given, lse, space, logp=logp, entropy=entropy, top_ids=ids, top_logp=best)
+        if turn:                                    # the given ids were some of the best of the turn before
+            assert torch.equal(logp, best[:, turn % k])
+        got = [lse, entropy, ids, best]
+        first = first or [x.clone() for x in got]
+        assert all(torch.equal(a, b) for a, b in zip(got, first)), turn
+        given = ids[:, (turn + 1) % k].contiguous()
