@@ -430,7 +430,7 @@ ne_status ne_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, i
  *   dh_dev, dw_dev : device, row strides >= dim; must not overlap the inputs or each other.
  *   workspace_dev : at least ne_logprob_workspace_bytes(n, num_rows, dim, type, 0, 1) bytes.
  * Its precision is that of ne_xent_grad, coefficients being those of G over |l_i| + 8 |e_i|; but with NE_BF16 and entropies dh has the coefficients with 11 bits, too,
- * and elements of w that are below 2^-29 of the largest are off by up to 2^-30 of it there.  Values that are not finite: the gradients are not specified.
+ * and, of 512 rows and more, elements of w that are below 2^-29 of the largest are off by up to 2^-30 of it there.  Values that are not finite: the gradients are not specified.
  *   0 <= n <= 2^24, 0 < num_rows < 2^31, 1 <= dim <= NE_OP_MAX_DIM; n == 0 is a no-op for ne_logprob and writes zeros to dw.
  * Errors: NE_ERR_ARG, NE_ERR_HIP.
  */

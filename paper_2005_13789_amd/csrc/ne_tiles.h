@@ -162,13 +162,23 @@ __device__ __forceinline__ s16x8 fragment(const unsigned char* lds, int part, in
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// What operands hold: as their parts say (one: bf16, two: fp16 halves), fp16, or the second one fp16 that becomes bf16 for its products.
-enum Kind { kPlain, kHalf, kToBf16 };
+// What operands hold: as their parts say (one: bf16, two: fp16 halves), fp16, or the second one fp16 that becomes bf16 for its products, rounded or as the sum of two.
+enum Kind { kPlain, kHalf, kToBf16, kToTwoBf16 };
 
 __device__ __forceinline__ s16x8 to_bf16(s16x8 x)
 {
     typedef float f32x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(s16x8, __builtin_convertvector(__builtin_convertvector(__builtin_bit_cast(f16x8, x), f32x8), bf16x8));
+}
+
+// Returns what rounding leaves out, which bf16 holds exactly.
+__device__ __forceinline__ s16x8 to_two_bf16(s16x8& x)
+{
+    typedef float f32x8 __attribute__((ext_vector_type(8)));
+    const f32x8 whole = __builtin_convertvector(__builtin_bit_cast(f16x8, x), f32x8);
+    const bf16x8 most = __builtin_convertvector(whole, bf16x8);
+    x = __builtin_bit_cast(s16x8, most);
+    return __builtin_bit_cast(s16x8, __builtin_convertvector(whole - __builtin_convertvector(most, f32x8), bf16x8));
 }
 
 template <int P, Kind K = kPlain>
@@ -192,7 +202,7 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
     const unsigned char* B = stage + b_at;
     // Operands of the next 16 indices are read while these are multiplied: a read takes as long as four products.  (The compiler would
     // reuse the registers at once and wait for every read.)
-    s16x8 a[2][P][MT], b[2][P][2];
+    s16x8 a[2][P][MT], b[2][P][2], more[2][2];
     auto read = [&](int kk) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -207,6 +217,9 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
         if (K == kToBf16)
 #pragma unroll
             for (int in = 0; in < 2; ++in) b[kk & 1][0][in] = to_bf16(b[kk & 1][0][in]);
+        if (K == kToTwoBf16)
+#pragma unroll
+            for (int in = 0; in < 2; ++in) more[kk & 1][in] = to_two_bf16(b[kk & 1][0][in]);
     };
     read(0);
     convert(0);
@@ -221,6 +234,7 @@ __device__ __forceinline__ void multiply(const unsigned char* stage, f32x16 (&ac
 #pragma unroll
             for (int in = 0; in < 2; ++in) {
                 acc[im][in] = mfma<P, K>(a[at][0][im], b[at][0][in], acc[im][in]);
+                if (K == kToTwoBf16) acc[im][in] = mfma<P>(a[at][0][im], more[at][in], acc[im][in]);
                 if (P == 2) {
                     acc[im][in] = mfma<P>(a[at][0][im], b[at][P - 1][in], acc[im][in]);
                     acc[im][in] = mfma<P>(a[at][P - 1][im], b[at][0][in], acc[im][in]);

@@ -19,7 +19,7 @@
 // multiplies it with H in fp16.  dH, for which the table would have to be turned into fp16, rounds it to bf16 in registers, but takes the
 // target's coefficient whole.  So both gradients' errors are those of their own rounding: 0.0017.  (With G in bf16 0.0021, and dH 0.013 where the
 // table's rows share a part ten times as large as what tells them apart: a row's coefficients add up to nothing, their roundings do not.)  Where entropies count the
-// target's coefficient is not the only large one, and dH takes the table in fp16 (table_kernel): its error is 0.0017 to 0.0021 there.
+// target's coefficient is not the only large one, and dH takes all of them with 11 bits (its error is 0.0017 to 0.0021 there).
 // fp32 operands are split into two fp16 halves at a common power of two, x 2^k = hi + lo with 22 bits (of elements down to 2^-16 of the
 // largest; smaller ones are off by up to 2^-38 of it, fp16 ending there), and a product is hi hi + hi lo + lo hi: about the error of an fp32
 // product at three matrix instructions, 408 TF as a large library product runs (1225 TF in bf16), where one in fp32 makes 154.
@@ -40,6 +40,7 @@ constexpr int64_t kGBytes = 512 << 20, kGLeast = 64 << 20, kGCached = 256 << 20,
 // In stages: the fewest of a product's workgroup; what a tile takes besides (1, 4 and 8 choose alike); what a launch takes.
 constexpr int kLeastShare = 8, kTileCost = 1, kLaunchCost = 10;
 constexpr int kGShift = 14;            // fp16 halves of G are those of G 2^14
+constexpr int64_t kHalfTable = 512;    // rows of H from which on a bf16 table becomes fp16 for dH where entropies count
 
 // ---------------------------------------------------------------------------------------------
 // scores: the softmax's maximum and sum of every row of H, and its target's score
@@ -279,7 +280,10 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(FewArgs a)
 // ---------------------------------------------------------------------------------------------
 // Where entropies count, several of a row's coefficients are large and they add up to nothing, so where the table's rows share a part it is the roundings of
 // all of them that is left of it in dH: with G in bf16 dH is off by 0.011 where that part is ten times what tells rows apart, with G's 11 bits by 0.002 (its own rounding
-// 0.0017).  So a bf16 table goes into fp16, too, piece by piece, where it was packed or would have been.
+// 0.0017).  So dH's product takes G, in fp16, as the sum of two bf16 numbers; or, of kHalfTable rows of H and more, a bf16 table becomes fp16, too, piece by piece, where
+// it was packed or would have been.  That costs passes over the table, which many rows share, instead of a fourth more matrix instructions (us of the
+// gradients, G rounded to bf16, as two, table in fp16: 64 rows of 200 003 x 512 180, 191, 306; 300 rows 365, 429, 493; 600 rows 558, 661, 666; 1500 rows 1171, 1464,
+// 1278; 400 of 199 999 x 300 447, 513, 494; 800 of 100 000 x 128 131, 141, 148).
 // bf16 to fp16, times a power of two: exponents less `bias` (how much smaller fp16's are, for the largest to have fp16's largest), which lies in the places
 // of both formats' exponents.  Elements keep all of their 8 bits from 2^-29 of the largest on; smaller ones are off by less than 2^-30 of it.
 __device__ __forceinline__ s16x8 to_half(s16x8 x, uint16_t bias)
@@ -464,8 +468,8 @@ struct ProductArgs {
 // (The gradients' columns are the first operand, so that they run along a lane's registers and are written side by side.)
 // (bf16: turning G from fp16 to bf16 in registers takes up to 4 % of the gradients' time, 8192 x 200 003 x 512 5180 -> 5370 us; W in fp16 would
 // take a pass over the table.)
-// ENTROPY, bf16: the table is there as fp16, so that dH, too, sees G's 11 bits.
-template <int P, int W, bool ENTROPY>
+// DH: how dH's product takes G and the table.
+template <int P, int W, Kind DH>
 __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
 {
     __shared__ __align__(16) unsigned char lds[2 * stage_bytes<W>()];
@@ -480,7 +484,7 @@ __global__ void __launch_bounds__(64 * W, 2) products_kernel(ProductArgs a)
     const uint32_t s0 = min(split * share, stages), s1 = min(s0 + share, stages);
     constexpr int R = rows_of<W>(), MT = W / 2;
     f32x16 acc[MT][2];
-    if (dh) product_tile<P, W, true, P == 2 ? kPlain : ENTROPY ? kHalf : kToBf16>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
+    if (dh) product_tile<P, W, true, DH>(a.w, a.g_rows, col * R, tile * R, s0, s1, lds, acc);
     else product_tile<P, W, false, P == 1 ? kHalf : kPlain>(a.h, a.g_cols, col * R, tile * R, s0, s1, lds, acc);
     const uint32_t row0 = tile * R + first_col<W>() + (lane & 31), col0 = col * R + first_row<W>() + 4 * (lane >> 5);
     if (!dh && !a.dw) {
@@ -1126,7 +1130,7 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
 {
     CoefArgs ca{};
     ProductArgs pa{};
-    const bool halves = P == 1 && ENTROPY && dh;       // dH's product takes the table as fp16
+    const bool halves = P == 1 && ENTROPY && dh && x.n >= kHalfTable;      // dH's product takes the table as fp16
     hipError_t e = pack(x, w, dw != nullptr, &ca.h, &pa.h, &ca.w, &ca.hc, halves ? w.table_max : nullptr, &ca.maxima, st);
     if (e != hipSuccess) return e;
     const Operand all = ca.w;
@@ -1184,8 +1188,11 @@ hipError_t run_grad(const SoftmaxCall& x, const XentWs& w, const Mix* mix, const
         pa.out = dw ? static_cast<T*>(dw) + base * dw_stride : nullptr;
         const uint32_t blocks = (pa.h_tiles * pa.h_splits + pa.w_tiles * pa.w_splits) * pa.col_tiles;
         if (!blocks) continue;
-        if (P == 1 && w.large_products) hipLaunchKernelGGL((products_kernel<1, 8, ENTROPY>), dim3(blocks), dim3(512), 0, st, pa);
-        else hipLaunchKernelGGL((products_kernel<P, 4, P == 1 && ENTROPY>), dim3(blocks), dim3(256), 0, st, pa);
+        constexpr Kind DH = P == 2 ? kPlain : ENTROPY ? kToTwoBf16 : kToBf16, DH_HALVES = P == 1 && ENTROPY ? kHalf : DH;
+        if (P == 1 && w.large_products && halves) hipLaunchKernelGGL((products_kernel<1, 8, ENTROPY ? kHalf : kToBf16>), dim3(blocks), dim3(512), 0, st, pa);
+        else if (P == 1 && w.large_products) hipLaunchKernelGGL((products_kernel<1, 8, ENTROPY ? kToTwoBf16 : kToBf16>), dim3(blocks), dim3(512), 0, st, pa);
+        else if (halves) hipLaunchKernelGGL((products_kernel<P, 4, DH_HALVES>), dim3(blocks), dim3(256), 0, st, pa);
+        else hipLaunchKernelGGL((products_kernel<P, 4, DH>), dim3(blocks), dim3(256), 0, st, pa);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (dw && w.dw) {
