@@ -211,7 +211,7 @@ struct TileArgs {
 
 // Tiles, stages and operands are the cross entropy's; a workgroup keeps a tile of H's rows and goes through its split of the table.  What is added to
 // a score there, for the moment one multiply-add, for records two instructions, runs on the vector units beside the matrix cores, and is why these wait:
-// 8192 rows against 200 003 x 512 bf16, k = 16: 1840 to 2010 us, 0.83 to 0.91 PFLOP/s (k = 0: 1690); 10 007 against 10 000 x 100 fp32: 112 (the loss 100).
+// 8192 rows against 200 003 x 512 bf16, k = 16: 1890 to 2070 us, 0.81 to 0.89 PFLOP/s (k = 0: 1690 to 1790); 10 007 against 10 000 x 100 fp32: 121 (the loss 100).
 // Chunks of 64 rows take an exchange between lanes a chunk; those of 16 are a lane's own, four times as many records (80 MB of 8 bytes there).
 template <int P, int W, int KS, int CHUNKS>
 __global__ void __launch_bounds__(64 * W, 2) answer_tiles_kernel(TileArgs a)

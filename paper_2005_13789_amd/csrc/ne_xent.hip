@@ -350,7 +350,7 @@ struct CoefArgs {
 };
 
 // ENTROPY: one multiply-add and one product more a score, beside the exponential (4096 rows against 10 000 x 128 fp32: 61 us, 8192 against 200 003 x 512 bf16:
-// 13 pieces of 178).
+// 13 pieces of 181).
 template <int P, int W, int KS, bool ENTROPY>
 __global__ void __launch_bounds__(64 * W, 2) coef_kernel(CoefArgs a)
 {
